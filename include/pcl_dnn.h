@@ -6,8 +6,8 @@
  *
  * Conventions that hold for every entry point
  * -------------------------------------------
- *  - All tensor pointers are DEVICE pointers to fp32 data, contiguous, and at
- *    least 16-byte aligned.  The caller owns every buffer, including the
+ *  - All tensor pointers are DEVICE pointers to fp32 data (void*: of the call's
+ *    dtype), contiguous, and at least 16-byte aligned.  The caller owns every buffer, including the
  *    workspace; the library allocates no device memory.
  *  - Layouts: activations and their gradients are NHWC (N minibatch, H x W
  *    feature map, C feature maps innermost); convolution weights and their
@@ -55,8 +55,15 @@ enum {
     PCL_ERR_CUDA = 5,              /* a CUDA runtime/driver call failed               */
     PCL_ERR_DEVICE_TIMEOUT = 6,    /* a bounded device-side wait ran out              */
     PCL_ERR_SCRATCH_LIMIT = 7,     /* problem larger than the built-in scratch array  */
-    PCL_ERR_BAD_LABEL = 8          /* pcl_softmax_xent met a label outside [0, K)     */
+    PCL_ERR_BAD_LABEL = 8          /* a call met a class label or token id outside its range */
 };
+
+/* Element types of the calls that take more than fp32 (the void* tensors of the vocabulary calls and of the
+ * orthogonalised update below). */
+enum { PCL_F32 = 0, PCL_BF16 = 1, PCL_F16 = 2 };
+
+/* ignore_label / pad_id: no label or id is special */
+#define PCL_NO_ID (-2147483647 - 1)
 
 enum { PCL_PASS_FWD = 0, PCL_PASS_BWD_DATA = 1, PCL_PASS_BWD_WEIGHTS = 2 };
 
@@ -303,6 +310,74 @@ int pcl_maxpool2x2_bwd_codes(int N, int H, int W, int C, const unsigned char* co
  * its last bits may differ from run to run. */
 int pcl_softmax_xent(int N, int K, const float* logits, const int* labels,
                      float* loss, float* dlogits, void* cuda_stream);
+
+/* Embedding lookup: the first layer of a network whose input is a token, i.e. an FC layer on one-hot rows.
+ *   out[n,:] = scale * table[ids[n],:]          (computed in fp32, rounded once)
+ * Rows of the padding id `pad_id` (PCL_NO_ID: none; it need not lie in [0, V)) are zero.  So are rows of other ids outside
+ * [0, V): those are never used as an index, and the next pcl_last_device_status() returns PCL_ERR_BAD_LABEL.
+ * ids: device int32 [N]; table: [V][C] in; out: [N][C] out; dtype: type of table and out. */
+int pcl_embedding_fwd(int N, int V, int C, int dtype, const int* ids, const void* table, float scale, int pad_id,
+                      void* out, void* cuda_stream);
+
+/* Gradient of the table, by sorted tokens:
+ *   dtable[v,:] = scale * sum_{n: ids[n] = v} dy[n,:]      (fp32 sums, every row written, 0 where v does not occur)
+ * The rows of a token are added in a fixed order: bitwise reproducible.  Tokens of the padding id and ids outside [0, V)
+ * (PCL_ERR_BAD_LABEL, as above) add nothing.  dy: [N][C] in, dtable: [V][C] out, both of type dtype.
+ * Workspace: pcl_embedding_workspace_bytes(N, V, C), 256-byte aligned. */
+size_t pcl_embedding_workspace_bytes(int N, int V, int C);
+int pcl_embedding_bwd(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id,
+                      void* dtable, void* ws, size_t ws_bytes, void* cuda_stream);
+/* The same with the SGD step applied in place, table[v,:] <- table[v,:] - lr * dtable[v,:], to the rows that occur; dtable
+ * is not stored and the other rows are not touched.  table: [V][C] in/out of type dtype (the update is computed in fp32 and
+ * rounded once). */
+int pcl_embedding_bwd_sgd(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id,
+                          void* table, float lr, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Softmax cross-entropy of a fully-connected layer without its logits: pcl_fc_fwd() (act NONE) and pcl_softmax_xent() for
+ * class counts whose logits are too large to keep.  With z[n,k] = bias[k] + sum_c x[n,c] * w[k,c]:
+ *   lse[n]      = log sum_k exp z[n,k]
+ *   row_loss[n] = lse[n] - z[n, labels[n]]      0 for rows whose label is ignore_label (PCL_NO_ID: none) or out of range
+ *   loss        = mean of row_loss over the rows whose label is not ignore_label (0 if there is none)
+ * A label outside [0, K) that is not ignore_label is treated as in pcl_softmax_xent(): never used as an index, no target,
+ * and the next pcl_last_device_status() returns PCL_ERR_BAD_LABEL.  Logits of -inf (a bias that masks classes) have
+ * probability 0; a row whose logits all are -inf has lse -inf, loss inf and gradient 0; a NaN or +inf logit makes its
+ * row's results NaN.  All sums are in a fixed order.
+ * dtype PCL_BF16 / PCL_F16: products on the 16-bit tensor cores, exact products and fp32 sums.  PCL_F32: TF32 products, as
+ * everywhere in this library.
+ * x: [N][C], w: [K][C], bias: [K] or NULL, all in, of type dtype; labels: int32 [N]; loss: [1], row_loss: [N], lse: [N]
+ * out, fp32.  Workspace: pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, PCL_PASS_FWD), 256-byte aligned. */
+size_t pcl_fc_softmax_xent_workspace_bytes(int N, int C, int K, int dtype, int pass);
+int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias,
+                            const int* labels, int ignore_label, float* loss, float* row_loss, float* lse,
+                            void* ws, size_t ws_bytes, void* cuda_stream);
+/* Its gradient, from the forward call's lse.  The logits are computed again, piece by piece of the classes:
+ *   dz[n,k] = g[n] * (exp(z[n,k] - lse[n]) - [k == labels[n]]),   exactly 0 for rows whose label is ignore_label
+ *   dx = dz w,   dw = dz^T x,   dbias[k] = sum_n dz[n,k]
+ * g = row_grad (the gradient of each row's loss, fp32 [N]), or, for row_grad == NULL, 1 / (number of rows whose label is not
+ * ignore_label), the gradient of `loss`.  With 16-bit types dz is rounded to that type between the products (fp16: after
+ * scaling by a power of two that keeps it in range); the results are rounded once.
+ * dx: [N][C] out or NULL; dw: [K][C] out; dbias: [K] out or NULL; all of type dtype.  Deterministic.
+ * Workspace: pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, PCL_PASS_BWD_DATA). */
+int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias,
+                            const int* labels, int ignore_label, const float* lse, const float* row_grad,
+                            void* dx, void* dw, void* dbias, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Orthogonalisation of `count` matrices by Newton-Schulz steps (the direction of the Muon update):
+ *   X = g / (|g|_F + 1e-7);   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X     (a, b, c = 3.4445, -4.7750, 2.0315;
+ *   for a matrix with more rows than columns the same on its transpose);   out = X
+ * g, out: [count][M][N] of type dtype (out may be g).  steps >= 1 (5 is usual).  The products take fp16 operands with fp32
+ * sums; relative error (2-norm) of the result 1e-3 .. 2e-3 besides the rounding to dtype.  A zero matrix gives zero.
+ * Workspace: pcl_orthogonalize_workspace_bytes(count, M, N), 256-byte aligned. */
+size_t pcl_orthogonalize_workspace_bytes(int count, int M, int N);
+int pcl_orthogonalize(int count, int M, int N, int dtype, const void* g, void* out, int steps,
+                      void* ws, size_t ws_bytes, void* cuda_stream);
+/* The update built on it, for weights that pcl_sgd_update() would step along dw:
+ *   momentum <- mu * momentum + dw;   u = nesterov ? dw + mu * momentum : momentum
+ *   w <- (1 - lr * weight_decay) * w - lr * sqrt(max(1, M / N)) * orthogonalize(u)
+ * w: [count][M][N] in/out, dw: [count][M][N] in, of type dtype; momentum: [count][M][N] fp32 in/out. */
+int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const void* dw, float* momentum, float mu,
+                          int nesterov, float lr, float weight_decay, int steps, void* ws, size_t ws_bytes,
+                          void* cuda_stream);
 
 /* Synchronises the stream, then reads and clears the device status word of the
  * current device.  PCL_OK, PCL_ERR_DEVICE_TIMEOUT, PCL_ERR_BAD_LABEL or PCL_ERR_CUDA. */

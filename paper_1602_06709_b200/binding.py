@@ -21,6 +21,8 @@ OK = 0
 ERR_BAD_ARG, ERR_UNSUPPORTED_SHAPE, ERR_MISALIGNED, ERR_WORKSPACE, ERR_CUDA, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6
 ERR_SCRATCH_LIMIT = 7
 ERR_BAD_LABEL = 8
+F32, BF16, F16 = 0, 1, 2
+NO_ID = -2 ** 31
 
 EXPORTS = [
     "pcl_set_path", "pcl_conv_out_dims", "pcl_conv_workspace_bytes", "pcl_fc_workspace_bytes",
@@ -31,6 +33,9 @@ EXPORTS = [
     "pcl_maxpool2x2_bwd_colsum_workspace_bytes", "pcl_maxpool2x2_bwd_colsum", "pcl_conv_fwd_pool", "pcl_conv_fwd_pool_is_fused",
     "pcl_conv_bwd_weights_pooled", "pcl_conv_bwd_weights_pooled_is_fused", "pcl_conv_bwd_weights_pooled_workspace_bytes",
     "pcl_maxpool2x2_fwd_codes", "pcl_maxpool2x2_bwd_codes", "pcl_last_wait_code", "pcl_set_tuning", "pcl_reset_tuning", "pcl_fc_bwd_fused", "pcl_conv_plan_describe", "pcl_conv_staged_input_bytes",
+    "pcl_embedding_fwd", "pcl_embedding_workspace_bytes", "pcl_embedding_bwd", "pcl_embedding_bwd_sgd",
+    "pcl_fc_softmax_xent_workspace_bytes", "pcl_fc_softmax_xent_fwd", "pcl_fc_softmax_xent_bwd",
+    "pcl_orthogonalize_workspace_bytes", "pcl_orthogonalize", "pcl_orthogonal_update",
     "pcl_conv_bwd_weights_pooled_staged", "pcl_conv_bwd_weights_sgd", "pcl_conv_bwd_weights_sgd_workspace_bytes",
     "pcl_fc_bwd_fused_sgd", "pcl_fc_bwd_fused_sgd_workspace_bytes", "pcl_plan_cache_stats",
 ]
@@ -100,6 +105,19 @@ def lib() -> ctypes.CDLL:
         L.pcl_maxpool2x2_fwd.argtypes = [ci, ci, ci, ci, vp, vp, vp]
         L.pcl_maxpool2x2_bwd.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp, vp]
         L.pcl_softmax_xent.argtypes = [ci, ci, vp, vp, vp, vp, vp]
+        L.pcl_embedding_fwd.argtypes = [ci, ci, ci, ci, vp, vp, cf, ci, vp, vp]
+        L.pcl_embedding_workspace_bytes.argtypes = [ci, ci, ci]
+        L.pcl_embedding_workspace_bytes.restype = sz
+        L.pcl_embedding_bwd.argtypes = [ci, ci, ci, ci, vp, vp, cf, ci, vp, vp, sz, vp]
+        L.pcl_embedding_bwd_sgd.argtypes = [ci, ci, ci, ci, vp, vp, cf, ci, vp, cf, vp, sz, vp]
+        L.pcl_fc_softmax_xent_workspace_bytes.argtypes = [ci, ci, ci, ci, ci]
+        L.pcl_fc_softmax_xent_workspace_bytes.restype = sz
+        L.pcl_fc_softmax_xent_fwd.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp, ci, vp, vp, vp, vp, sz, vp]
+        L.pcl_fc_softmax_xent_bwd.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.pcl_orthogonalize_workspace_bytes.argtypes = [ci, ci, ci]
+        L.pcl_orthogonalize_workspace_bytes.restype = sz
+        L.pcl_orthogonalize.argtypes = [ci, ci, ci, ci, vp, vp, ci, vp, sz, vp]
+        L.pcl_orthogonal_update.argtypes = [ci, ci, ci, ci, vp, vp, vp, cf, ci, cf, cf, ci, vp, sz, vp]
         L.pcl_last_device_status.argtypes = [vp]
         L.pcl_launch_count.restype = ctypes.c_ulonglong
         L.pcl_last_wait_code.restype = ctypes.c_uint
@@ -362,6 +380,114 @@ def softmax_xent(N, K, logits, labels, loss, dlogits, stream=None):
     assert labels.dtype == torch.int32
     _check(lib().pcl_softmax_xent(N, K, _ptr(logits), _ptr(labels), _ptr(loss), _ptr(dlogits), _stream(stream)),
            "pcl_softmax_xent")
+
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
+
+def dtype_code(t) -> int:
+    """The library's type code of a tensor (PCL_F32 / PCL_BF16 / PCL_F16)."""
+    if t.dtype not in _DTYPES:
+        raise TypeError(f"fp32, bf16 or fp16 tensors are wanted, not {t.dtype}")
+    return _DTYPES[t.dtype]
+
+
+def _typed(where, sizes, typed=(), fp32=(), int32=()):
+    """Checks the tensors of a call: (tensor, element count) pairs, None allowed; all on one device, the current one.
+    Returns the type code of the first of `typed`, which all share it."""
+    if any(not isinstance(n, int) or n <= 0 for n in sizes):
+        raise PclError(ERR_BAD_ARG, where)
+    code = dtype_code(typed[0][0])
+    dev = typed[0][0].device
+    for group, want in ((typed, typed[0][0].dtype), (fp32, torch.float32), (int32, torch.int32)):
+        for t, n in group:
+            if t is None:
+                continue
+            if t.dtype != want:
+                raise TypeError(f"{where}: a {want} tensor is wanted, not {t.dtype}")
+            if t.numel() != n:
+                raise ValueError(f"{where}: a tensor of {n} elements is wanted, not {t.numel()}")
+    for t, _ in (*typed, *fp32, *int32):
+        if t is not None and (not t.is_cuda or t.device != dev or dev.index != torch.cuda.current_device()):
+            raise ValueError(f"{where}: all tensors must be on the current device")
+    return code
+
+
+def _id(v):
+    return NO_ID if v is None else int(v)
+
+
+def embedding_workspace_bytes(N, V, C) -> int:
+    return int(lib().pcl_embedding_workspace_bytes(N, V, C))
+
+
+def embedding_fwd(N, V, C, ids, table, scale, out, pad_id=None, stream=None):
+    """out[n] = scale * table[ids[n]]; rows of pad_id are zero."""
+    d = _typed("pcl_embedding_fwd", (N, V, C), [(table, V * C), (out, N * C)], int32=[(ids, N)])
+    _check(lib().pcl_embedding_fwd(N, V, C, d, _ptr(ids), _ptr(table), ctypes.c_float(scale), _id(pad_id), _ptr(out),
+                                   _stream(stream)), "pcl_embedding_fwd")
+
+
+def embedding_bwd(N, V, C, ids, dy, scale, dtable, pad_id=None, ws=None, stream=None):
+    """dtable[v] = scale * sum of dy[n] over the tokens n with ids[n] == v; every row is written."""
+    d = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_embedding_bwd(N, V, C, d, _ptr(ids), _ptr(dy), ctypes.c_float(scale), _id(pad_id), _ptr(dtable), wp, wb,
+                                   _stream(stream)), "pcl_embedding_bwd")
+
+
+def embedding_bwd_sgd(N, V, C, ids, dy, scale, table, lr, pad_id=None, ws=None, stream=None):
+    """table[v] -= lr * dtable[v] in place for the rows that occur; dtable is not stored."""
+    d = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_embedding_bwd_sgd(N, V, C, d, _ptr(ids), _ptr(dy), ctypes.c_float(scale), _id(pad_id), _ptr(table),
+                                       ctypes.c_float(lr), wp, wb, _stream(stream)), "pcl_embedding_bwd_sgd")
+
+
+def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
+    """dtype: dtype_code() of the operands; which: PASS_FWD or PASS_BWD_DATA."""
+    return int(lib().pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, which))
+
+
+def fc_softmax_xent_fwd(N, C, K, x, w, bias, labels, loss, row_loss, lse, ignore_label=None, ws=None, stream=None):
+    """Mean loss, loss and log-sum-exp of each row of softmax(x w^T + bias), without storing the logits."""
+    d = _typed("pcl_fc_softmax_xent_fwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K)],
+               [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_fc_softmax_xent_fwd(N, C, K, d, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _id(ignore_label),
+                                         _ptr(loss), _ptr(row_loss), _ptr(lse), wp, wb, _stream(stream)),
+           "pcl_fc_softmax_xent_fwd")
+
+
+def fc_softmax_xent_bwd(N, C, K, x, w, bias, labels, lse, row_grad, dx, dw, dbias, ignore_label=None, ws=None, stream=None):
+    """dx (or None), dw and dbias (or None) from the forward call's lse; row_grad: gradient of each row's loss, or None for
+    the gradient of the mean."""
+    d = _typed("pcl_fc_softmax_xent_bwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K), (dx, N * C), (dw, K * C), (dbias, K)],
+               [(lse, N), (row_grad, N)], [(labels, N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_fc_softmax_xent_bwd(N, C, K, d, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _id(ignore_label), _ptr(lse),
+                                         _ptr(row_grad), _ptr(dx), _ptr(dw), _ptr(dbias), wp, wb, _stream(stream)),
+           "pcl_fc_softmax_xent_bwd")
+
+
+def orthogonalize_workspace_bytes(count, M, N) -> int:
+    return int(lib().pcl_orthogonalize_workspace_bytes(count, M, N))
+
+
+def orthogonalize(count, M, N, g, out, steps=5, ws=None, stream=None):
+    """out = g / |g| after `steps` Newton-Schulz steps, for each of `count` M x N matrices."""
+    d = _typed("pcl_orthogonalize", (count, M, N), [(g, count * M * N), (out, count * M * N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_orthogonalize(count, M, N, d, _ptr(g), _ptr(out), steps, wp, wb, _stream(stream)), "pcl_orthogonalize")
+
+
+def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_decay=0.0, steps=5, ws=None, stream=None):
+    """momentum <- mu momentum + dw, then w <- (1 - lr weight_decay) w - lr sqrt(max(1, M/N)) * orthogonalize(direction)."""
+    d = _typed("pcl_orthogonal_update", (count, M, N), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_orthogonal_update(count, M, N, d, _ptr(w), _ptr(dw), _ptr(momentum), ctypes.c_float(mu),
+                                       1 if nesterov else 0, ctypes.c_float(lr), ctypes.c_float(weight_decay), steps, wp, wb,
+                                       _stream(stream)), "pcl_orthogonal_update")
 
 
 def last_device_status(stream=None) -> int:

@@ -82,7 +82,7 @@ const char* const kKernelNames[KID_COUNT] = {
     "tc_fprop_kernel", "tc_wgrad_kernel", "generic_fwd", "generic_bwd_data", "generic_bwd_weights", "sgd_kernel",
     "reduce_splits_kernel", "zero_kernel", "transpose_flip_kernel", "act_grad_kernel", "colsum_kernel",
     "maxpool_fwd_kernel", "maxpool_bwd_kernel", "softmax_xent_kernel", "stage_pad_c4_kernel", "stage_w4_kernel",
-    "unpad_reduce_kernel"};
+    "unpad_reduce_kernel", "tc_gemm16_kernel", "embedding_kernel", "vocab_loss_kernel", "orthogonalize_kernel"};
 
 cudaEvent_t prof_event() {
     if (g_prof_pool_used == g_prof_pool.size()) {
@@ -1130,6 +1130,116 @@ int pcl_softmax_xent(int N, int K, const float* logits, const int* labels, float
     return launch_softmax_xent(N, K, logits, labels, loss, dlogits, static_cast<cudaStream_t>(cuda_stream));
 }
 
+namespace {
+bool known_dtype(int t) { return t == PCL_F32 || t == PCL_BF16 || t == PCL_F16; }
+// The workspace checks every call with a mandatory workspace makes.
+int check_ws(const void* ws, size_t ws_bytes, size_t need) {
+    if (!ws || ws_bytes < need) return PCL_ERR_WORKSPACE;
+    return (reinterpret_cast<uintptr_t>(ws) & 255) ? PCL_ERR_MISALIGNED : PCL_OK;
+}
+int check_embedding(int N, int V, int C, int dtype, const int* ids, const void* a, const void* b) {
+    if (N <= 0 || V <= 0 || C <= 0 || !known_dtype(dtype) || !ids || !a || !b) return PCL_ERR_BAD_ARG;
+    if (V == INT_MAX) return PCL_ERR_UNSUPPORTED_SHAPE;      // (the key of tokens without a row is V)
+    return aligned16(ids) && aligned16(a) && aligned16(b) ? PCL_OK : PCL_ERR_MISALIGNED;
+}
+int embedding_bwd_impl(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id, void* out,
+                       bool sgd, float lr, void* ws, size_t ws_bytes, void* cuda_stream) {
+    int rc = check_embedding(N, V, C, dtype, ids, dy, out);
+    if (rc == PCL_OK) rc = check_ws(ws, ws_bytes, embedding_workspace_bytes(N, V, C));
+    if (rc != PCL_OK) return rc;
+    return launch_embedding_bwd(N, V, C, dtype, ids, dy, scale, pad_id, out, sgd, lr, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+int check_vocab_loss(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels) {
+    if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || !x || !w || !labels) return PCL_ERR_BAD_ARG;
+    return aligned16(x) && aligned16(w) && aligned16(bias) && aligned16(labels) ? PCL_OK : PCL_ERR_MISALIGNED;
+}
+}  // namespace
+
+int pcl_embedding_fwd(int N, int V, int C, int dtype, const int* ids, const void* table, float scale, int pad_id, void* out,
+                      void* cuda_stream) {
+    const int rc = check_embedding(N, V, C, dtype, ids, table, out);
+    if (rc != PCL_OK) return rc;
+    return launch_embedding_fwd(N, V, C, dtype, ids, table, scale, pad_id, out, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t pcl_embedding_workspace_bytes(int N, int V, int C) {
+    return N <= 0 || V <= 0 || C <= 0 ? 0 : embedding_workspace_bytes(N, V, C);
+}
+
+int pcl_embedding_bwd(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id, void* dtable,
+                      void* ws, size_t ws_bytes, void* cuda_stream) {
+    return embedding_bwd_impl(N, V, C, dtype, ids, dy, scale, pad_id, dtable, false, 0.f, ws, ws_bytes, cuda_stream);
+}
+
+int pcl_embedding_bwd_sgd(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id, void* table,
+                          float lr, void* ws, size_t ws_bytes, void* cuda_stream) {
+    return embedding_bwd_impl(N, V, C, dtype, ids, dy, scale, pad_id, table, true, lr, ws, ws_bytes, cuda_stream);
+}
+
+size_t pcl_fc_softmax_xent_workspace_bytes(int N, int C, int K, int dtype, int pass) {
+    if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || (pass != PCL_PASS_FWD && pass != PCL_PASS_BWD_DATA)) return 0;
+    return vocab_loss_workspace_bytes(N, C, K, dtype, pass == PCL_PASS_BWD_DATA);
+}
+
+int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels,
+                            int ignore_label, float* loss, float* row_loss, float* lse, void* ws, size_t ws_bytes,
+                            void* cuda_stream) {
+    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels);
+    if (rc != PCL_OK) return rc;
+    if (!loss || !row_loss || !lse) return PCL_ERR_BAD_ARG;
+    if (!aligned16(loss) || !aligned16(row_loss) || !aligned16(lse)) return PCL_ERR_MISALIGNED;
+    rc = check_ws(ws, ws_bytes, vocab_loss_workspace_bytes(N, C, K, dtype, false));
+    if (rc != PCL_OK) return rc;
+    return launch_vocab_loss_fwd(N, C, K, dtype, x, w, bias, labels, ignore_label, loss, row_loss, lse, ws,
+                                 static_cast<cudaStream_t>(cuda_stream));
+}
+
+int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels,
+                            int ignore_label, const float* lse, const float* row_grad, void* dx, void* dw, void* dbias,
+                            void* ws, size_t ws_bytes, void* cuda_stream) {
+    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels);
+    if (rc != PCL_OK) return rc;
+    if (!lse || !dw) return PCL_ERR_BAD_ARG;
+    if (!aligned16(lse) || !aligned16(row_grad) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias)) return PCL_ERR_MISALIGNED;
+    rc = check_ws(ws, ws_bytes, vocab_loss_workspace_bytes(N, C, K, dtype, true));
+    if (rc != PCL_OK) return rc;
+    return launch_vocab_loss_bwd(N, C, K, dtype, x, w, bias, labels, ignore_label, lse, row_grad, dx, dw, dbias, ws,
+                                 static_cast<cudaStream_t>(cuda_stream));
+}
+
+namespace {
+int check_ortho(int count, int M, int N, int dtype, int steps, const void* a, const void* b) {
+    if (count <= 0 || M <= 0 || N <= 0 || steps <= 0 || !known_dtype(dtype) || !a || !b) return PCL_ERR_BAD_ARG;
+    if (count > 65535) return PCL_ERR_UNSUPPORTED_SHAPE;     // (a grid dimension)
+    return aligned16(a) && aligned16(b) ? PCL_OK : PCL_ERR_MISALIGNED;
+}
+}  // namespace
+
+size_t pcl_orthogonalize_workspace_bytes(int count, int M, int N) {
+    return count <= 0 || M <= 0 || N <= 0 ? 0 : orthogonalize_workspace_bytes(count, M, N);
+}
+
+int pcl_orthogonalize(int count, int M, int N, int dtype, const void* g, void* out, int steps, void* ws, size_t ws_bytes,
+                      void* cuda_stream) {
+    int rc = check_ortho(count, M, N, dtype, steps, g, out);
+    if (rc == PCL_OK) rc = check_ws(ws, ws_bytes, orthogonalize_workspace_bytes(count, M, N));
+    if (rc != PCL_OK) return rc;
+    const OrthoArgs o{count, M, N, dtype, steps, g, out};
+    return launch_orthogonalize(o, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const void* dw, float* momentum, float mu, int nesterov,
+                          float lr, float weight_decay, int steps, void* ws, size_t ws_bytes, void* cuda_stream) {
+    int rc = check_ortho(count, M, N, dtype, steps, w, dw);
+    if (rc == PCL_OK && !momentum) rc = PCL_ERR_BAD_ARG;
+    if (rc == PCL_OK && !aligned16(momentum)) rc = PCL_ERR_MISALIGNED;
+    if (rc == PCL_OK) rc = check_ws(ws, ws_bytes, orthogonalize_workspace_bytes(count, M, N));
+    if (rc != PCL_OK) return rc;
+    OrthoArgs o{count, M, N, dtype, steps, dw, w};
+    o.momentum = momentum; o.mu = mu; o.nesterov = nesterov; o.lr = lr; o.weight_decay = weight_decay;
+    return launch_orthogonalize(o, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
 static std::atomic<unsigned int> g_last_wait_code{0};
 
 int pcl_last_device_status(void* cuda_stream) {
@@ -1197,7 +1307,7 @@ const char* pcl_status_string(int status) {
         case PCL_ERR_CUDA: return "CUDA call failed";
         case PCL_ERR_DEVICE_TIMEOUT: return "device-side wait timed out";
         case PCL_ERR_SCRATCH_LIMIT: return "problem exceeds the capacity of the built-in scratch array";
-        case PCL_ERR_BAD_LABEL: return "a class label lies outside [0, K)";
+        case PCL_ERR_BAD_LABEL: return "a class label or token id lies outside its range";
     }
     return "unknown status";
 }

@@ -22,7 +22,7 @@ __device__ __forceinline__ float sigmoid_fast(float x) { return __fdividef(1.f, 
 enum KernelId {
     KID_TC_FPROP = 0, KID_TC_WGRAD, KID_GENERIC_FWD, KID_GENERIC_DGRAD, KID_GENERIC_WGRAD, KID_SGD, KID_REDUCE_SPLITS,
     KID_ZERO, KID_TRANSPOSE_FLIP, KID_ACT_GRAD, KID_COLSUM, KID_MAXPOOL_FWD, KID_MAXPOOL_BWD, KID_SOFTMAX_XENT,
-    KID_STAGE_PAD_C4, KID_STAGE_W4, KID_UNPAD_REDUCE, KID_COUNT
+    KID_STAGE_PAD_C4, KID_STAGE_W4, KID_UNPAD_REDUCE, KID_TC_GEMM16, KID_EMBEDDING, KID_VOCAB_LOSS, KID_ORTHO, KID_COUNT
 };
 
 // Brackets one kernel launch: counts it and, while profiling is switched on
@@ -278,6 +278,75 @@ int launch_maxpool_bwd_colsum(int N, int H, int W, int C, const float* x, const 
                               float* dx, float* colsum_rows, cudaStream_t st);
 int launch_softmax_xent(int N, int K, const float* logits, const int* labels, float* loss, float* dlogits,
                         cudaStream_t st);
+
+// ---- 16-bit GEMM on tcgen05 (kind::f16) ---------------------------------------
+// acc[b][r][c] = sum_k A[b](r, k) * B[b](c, k), fp32 accumulators; what happens to acc is the epilogue's kind.
+enum DType { DT_F32 = PCL_F32, DT_BF16 = PCL_BF16, DT_F16 = PCL_F16 };
+inline size_t dtype_bytes(int t) { return t == DT_F32 ? 4 : 2; }
+struct Gemm16Operand {
+    const void* ptr;        // 16-bit elements, 16-byte aligned
+    long ld;                // elements between rows (K-major: rows of the operand; MN-major: reduction indices), % 8 == 0
+    long batch_stride;      // elements between the matrices of a batch, % 8 == 0
+    bool mn_major;          // element (r, k) at ptr[k * ld + r] instead of ptr[r * ld + k]
+};
+enum Gemm16Epi { GEMM16_LINEAR = 0, GEMM16_STATS, GEMM16_DZ };
+struct Gemm16Args {
+    int M, N, K, batch;     // rows of A, rows of B (columns of the result), reduction length, matrices
+    bool bf16;              // element type of both operands (else fp16)
+    Gemm16Operand a, b;
+    int epi;
+    // Only the tiles on and above the diagonal are computed and the others written as their mirror image (M == N, A = B or
+    // a product that is symmetric; GEMM16_LINEAR with a 16-bit `out` and no `out2`).
+    bool symmetric = false;
+    // GEMM16_LINEAR: v = alpha * (alpha_dev ? *alpha_dev : 1) * acc + beta * src;  out = v, or, with `update`,
+    // out = keep * out - step * v in place.  out2 (fp16) = scale2 * v.
+    float alpha = 1.f;
+    const float* alpha_dev = nullptr;
+    float beta = 0.f;
+    const void* src = nullptr; int src_type = DT_F32; long src_ld = 0, src_batch = 0;
+    void* out = nullptr; int out_type = DT_F32; long out_ld = 0, out_batch = 0;
+    void* out2 = nullptr; long out2_ld = 0, out2_batch = 0; float scale2 = 1.f;
+    bool update = false; float keep = 1.f, step = 0.f;
+    // GEMM16_STATS / GEMM16_DZ: z[r][c] = acc + bias[c]; the columns are classes col0 .. col0 + N - 1.
+    const void* bias = nullptr;         // [N], type of the operands
+    const int* labels = nullptr;        // [M]
+    int col0 = 0;
+    // STATS: part[r][2 * tile + half] = (max, sum of exp(z - max)) of half a tile's columns; label_z[r] = z[r][label]
+    float2* part = nullptr; int part_ld = 0;
+    float* label_z = nullptr;
+    // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0
+    const float* lse = nullptr;
+    const float* row_scale = nullptr;
+};
+int gemm16_stats_parts(int M, int N);   // float2 entries per row that STATS writes
+int launch_gemm16(const Gemm16Args& a, cudaStream_t st);
+
+// ---- embedding (embedding.cu) -------------------------------------------------
+size_t embedding_workspace_bytes(int N, int V, int C);
+int launch_embedding_fwd(int N, int V, int C, int type, const int* ids, const void* table, float scale, int pad_id, void* out,
+                         cudaStream_t st);
+// sgd: `out` is the table, row <- row - lr * gradient for the rows that occur; else `out` is the gradient, every row written
+int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const void* dy, float scale, int pad_id, void* out,
+                         bool sgd, float lr, void* ws, cudaStream_t st);
+
+// ---- FC softmax cross-entropy in pieces of the classes (vocab_loss.cu) ---------
+size_t vocab_loss_workspace_bytes(int N, int C, int K, int type, bool backward);
+int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const void* w, const void* bias, const int* labels,
+                          int ignore_label, float* loss, float* row_loss, float* lse, void* ws, cudaStream_t st);
+int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const void* w, const void* bias, const int* labels,
+                          int ignore_label, const float* lse, const float* row_grad, void* dx, void* dw, void* dbias, void* ws,
+                          cudaStream_t st);
+
+// ---- orthogonalised update (orthogonalize.cu) ---------------------------------
+struct OrthoArgs {
+    int count, M, N, type, steps;
+    const void* g;                      // [count][M][N]: the gradient
+    void* out;                          // [count][M][N]: the direction, or the weights with `momentum`
+    float* momentum = nullptr;          // [count][M][N] fp32 in/out; null: out = the direction of g
+    float mu = 0.f; int nesterov = 0; float lr = 0.f, weight_decay = 0.f;
+};
+size_t orthogonalize_workspace_bytes(int count, int M, int N);
+int launch_orthogonalize(const OrthoArgs& a, void* ws, cudaStream_t st);
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

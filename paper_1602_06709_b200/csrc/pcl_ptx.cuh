@@ -164,6 +164,11 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap* m, uint32_t src,
                  ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
                  : "memory");
 }
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* m, uint32_t src, int c0, int c1, int c2) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 ::"l"(reinterpret_cast<uint64_t>(m)), "r"(src), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // all earlier groups of this thread have finished READING their shared-memory source
 __device__ __forceinline__ void bulk_wait_group_read0() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
@@ -472,6 +477,33 @@ __device__ __forceinline__ void umma_kstep_tf32(uint32_t d_tmem, uint32_t a_lo, 
     else PCL_UMMA_KSTEP_BODY("1");
 }
 #undef PCL_UMMA_KSTEP_BODY
+// 16-bit operands (kind::f16, both bf16 or both fp16): the four K = 16 MMAs of a 64-element reduction block.  kAStep /
+// kBStep: sixteen-byte units between the K = 16 slices (2 for a K-major 128-byte row, 128 for an MN-major tile whose
+// 8-deep reduction groups are 1 KB apart).
+#define PCL_UMMA_KSTEP16_BODY(CG)                                                                                 \
+    asm volatile(                                                                                                 \
+        "{\n\t.reg .pred p, pe;\n\t.reg .b64 da, db;\n\t.reg .b32 al, bl;\n\t"                                    \
+        "setp.ne.b32 p, %6, 0;\n\t"                                                                               \
+        "elect.sync _|pe, 0xffffffff;\n\t"                                                                        \
+        "mov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %4};\n\t"                                                      \
+        "@pe tcgen05.mma.cta_group::" CG ".kind::f16 [%0], da, db, %5, p;\n\t"                                     \
+        "setp.ne.b32 p, 1, 0;\n\t"                                                                                \
+        "add.u32 al, %1, %7;\n\tadd.u32 bl, %2, %8;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %4};\n\t"          \
+        "@pe tcgen05.mma.cta_group::" CG ".kind::f16 [%0], da, db, %5, p;\n\t"                                     \
+        "add.u32 al, al, %7;\n\tadd.u32 bl, bl, %8;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %4};\n\t"          \
+        "@pe tcgen05.mma.cta_group::" CG ".kind::f16 [%0], da, db, %5, p;\n\t"                                     \
+        "add.u32 al, al, %7;\n\tadd.u32 bl, bl, %8;\n\tmov.b64 da, {al, %3};\n\tmov.b64 db, {bl, %4};\n\t"          \
+        "@pe tcgen05.mma.cta_group::" CG ".kind::f16 [%0], da, db, %5, p;\n\t}"                                    \
+        ::"r"(d_tmem), "r"(a_lo), "r"(b_lo), "r"(a_hi), "r"(b_hi), "r"(idesc), "r"(acc_first), "n"(kAStep),       \
+        "n"(kBStep)                                                                                               \
+        : "memory")
+template <bool kPair, int kAStep, int kBStep>
+__device__ __forceinline__ void umma_kstep_f16(uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t a_hi,
+                                               uint32_t b_hi, uint32_t idesc, uint32_t acc_first) {
+    if constexpr (kPair) PCL_UMMA_KSTEP16_BODY("2");
+    else PCL_UMMA_KSTEP16_BODY("1");
+}
+#undef PCL_UMMA_KSTEP16_BODY
 // The same with a K-major A (k-block = 2 units) and the k-block stride of B in a register (2: K-major, 64: MN-major).
 // `nsl` (1..4): how many of the four K = 8 slices are issued; the rest are known to multiply zeros only (few-channel
 // layers pack fewer than 32 live reduction elements into a block) and are skipped by a guard predicate.
@@ -534,6 +566,13 @@ __host__ __device__ constexpr uint32_t make_idesc_tf32(uint32_t n, bool a_mn_maj
                                                        uint32_t m = 128u) {
     return (1u << 4) | (2u << 7) | (2u << 10) | (static_cast<uint32_t>(a_mn_major) << 15) |
            (static_cast<uint32_t>(b_mn_major) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+
+// The same for kind::f16: A / B format 0 = fp16, 1 = bf16 (both operands alike).
+__host__ __device__ constexpr uint32_t make_idesc_f16(uint32_t n, bool bf16, bool a_mn_major, bool b_mn_major, uint32_t m) {
+    return (1u << 4) | (static_cast<uint32_t>(bf16) << 7) | (static_cast<uint32_t>(bf16) << 10) |
+           (static_cast<uint32_t>(a_mn_major) << 15) | (static_cast<uint32_t>(b_mn_major) << 16) | ((n >> 3) << 17) |
+           ((m >> 4) << 24);
 }
 
 // Wait codes recorded in the device status word (which role gave up).

@@ -1,0 +1,177 @@
+"""Newton-Schulz orthogonalisation and the update built on it against float64."""
+import math
+
+import pytest
+import torch
+
+from gpu_helpers import check_guards, guarded, workspace
+from paper_1602_06709_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+A_, B_, C_, EPS = 3.4445, -4.7750, 2.0315, 1e-7
+# 2-norm of the error over the 2-norm of the result.  Roundings to fp16 are off by 2^-11 at most and 2^-11 / sqrt(3) in the
+# mean, 2e-4 of a value of average mantissa.  One step holds X in B X, A = X X^T and B; with |X| ~ 1 the errors of X, A and B
+# enter the result with weights of about 2 |b + 2c|, |b| + 2 |c| and |b + c| (5, 9 and 3), independently: 2e-4 * 11 = 2.2e-3 a
+# step.  Three steps have |X| of that size (the ones before raise the small singular values from below 0.1, where A and B are
+# small against a): 2.2e-3 * sqrt(3) = 3.8e-3, to which the rounding of the result adds half a step of its type.
+NS_TOL = 5e-3
+
+
+def half_step(t):
+    return torch.finfo(t).eps / 2
+
+
+def reference(u, steps=5):
+    out = []
+    for m in u.double():
+        m = m / (m.norm() + EPS)
+        flip = m.shape[0] > m.shape[1]
+        m = m.t() if flip else m
+        for _ in range(steps):
+            g = m @ m.t()
+            m = A_ * m + (B_ * g + C_ * (g @ g)) @ m
+        out.append(m.t() if flip else m)
+    return torch.stack(out)
+
+
+def spectrum(count, M, N, kind, seed):
+    g = torch.Generator().manual_seed(seed)
+    d = min(M, N)
+    if kind == "gauss":
+        return torch.randn(count, M, N, generator=g)
+    if kind == "lowrank":
+        r = min(8, d)
+        return torch.randn(count, M, r, generator=g) @ torch.randn(count, r, N, generator=g) + 0.05 * torch.randn(count, M, N, generator=g)
+    u = torch.linalg.qr(torch.randn(count, M, d, generator=g, dtype=torch.float64))[0]
+    v = torch.linalg.qr(torch.randn(count, N, d, generator=g, dtype=torch.float64))[0]
+    s = torch.arange(1, d + 1, dtype=torch.float64) ** (-1.0 if kind == "decay" else 0.0)
+    return ((u * s) @ v.transpose(1, 2)).float()
+
+
+def run(g, steps=5):
+    count, M, N = g.shape
+    out = guarded((count, M, N), g.dtype)
+    B.orthogonalize(count, M, N, g, out, steps=steps, ws=workspace(B.orthogonalize_workspace_bytes(count, M, N)))
+    B.check_device_status()
+    check_guards()
+    return out
+
+
+def assert_close(got, ref, t):
+    for a, b in zip(got.double().cpu(), ref.cpu()):
+        err, norm = float((a - b).norm()), float(b.norm())
+        assert err <= (NS_TOL + half_step(t)) * norm, f"{err / norm:.3e}"
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("count,M,N", [(1, 1, 1), (1, 1, 50), (2, 50, 1), (1, 7, 5), (3, 16, 33), (1, 33, 100), (1, 100, 33),
+                                       (2, 128, 128), (1, 129, 257), (1, 300, 1000), (1, 1000, 300), (1, 640, 640)])
+def test_direction(t, count, M, N):
+    g = guarded((count, M, N), t, fill=0)
+    g.copy_(spectrum(count, M, N, "gauss", M + N))
+    assert_close(run(g), reference(g), t)
+
+
+@pytest.mark.parametrize("kind", ["gauss", "lowrank", "decay", "flat"])
+@pytest.mark.parametrize("M,N", [(256, 256), (200, 520), (520, 200)])
+def test_spectra(kind, M, N):
+    g = guarded((2, M, N), torch.float32, fill=0)
+    g.copy_(spectrum(2, M, N, kind, 3))
+    assert_close(run(g), reference(g), torch.float32)
+
+
+def test_pairs_of_ctas_and_symmetric_tiles():
+    """Enough tiles for the CTA-pair form, ragged in both directions."""
+    g = guarded((2, 2100, 2310), torch.bfloat16, fill=0)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    g.copy_(torch.randn(2, 2100, 2310, device="cuda", generator=gen))
+    assert_close(run(g), reference(g), torch.bfloat16)
+    tall = guarded((2, 2310, 2100), torch.bfloat16, fill=0)
+    tall.copy_(g.transpose(1, 2))
+    assert_close(run(tall), reference(tall), torch.bfloat16)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 7])
+def test_steps(steps):
+    g = guarded((1, 96, 160), torch.float32, fill=0)
+    g.copy_(spectrum(1, 96, 160, "gauss", 9))
+    assert_close(run(g, steps), reference(g, steps), torch.float32)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e-7, 1.0, 1e15, 1e25])
+def test_norms_out_of_the_range_of_fp32_squares(scale):
+    g = guarded((1, 64, 80), torch.float32, fill=0)
+    g.copy_(spectrum(1, 64, 80, "gauss", 4) * scale)
+    got, ref = run(g), reference(g)
+    # (below |g| ~ 1e-7 the eps of the definition makes X small: fp16 has no numbers below 2^-24 of the scaled unit)
+    if scale >= 1e-7:
+        assert_close(got, ref, torch.float32)
+    else:
+        assert float((got.double() - ref).abs().max()) <= 485 * 2.0 ** -37 + NS_TOL * float(ref.abs().max())
+
+
+def test_zero_and_nan_matrices_of_a_batch():
+    g = guarded((3, 40, 24), torch.float32, fill=0)
+    g.copy_(spectrum(3, 40, 24, "gauss", 5))
+    g[0] = 0
+    g[2, 3, 4] = float("nan")
+    got = run(g)
+    assert not bool(got[0].any()) and bool(got[2].isnan().all())
+    assert_close(got[1:2], reference(g[1:2]), torch.float32)
+
+
+def test_in_place_and_repeatable():
+    g = guarded((2, 130, 260), torch.bfloat16, fill=0)
+    g.copy_(spectrum(2, 130, 260, "gauss", 6))
+    first = run(g)
+    assert torch.equal(first, run(g))
+    B.orthogonalize(2, 130, 260, g, g, ws=workspace(B.orthogonalize_workspace_bytes(2, 130, 260)))
+    assert torch.equal(first, g)
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("count,M,N", [(1, 5, 3), (2, 64, 96), (1, 257, 70), (1, 300, 300)])
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_update(t, count, M, N, nesterov):
+    mu, lr, wd = 0.9, 0.05, 0.1
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    mk = lambda dt, std: guarded((count, M, N), dt, fill=0).copy_(torch.randn(count, M, N, device="cuda", generator=gen) * std)
+    w, dw, m = mk(t, 0.1), mk(t, 1e-2), mk(torch.float32, 1e-2)
+    w0, m0 = w.double(), m.double()
+    B.orthogonal_update(count, M, N, w, dw, m, mu, nesterov, lr, wd, ws=workspace(B.orthogonalize_workspace_bytes(count, M, N)))
+    B.check_device_status()
+    check_guards()
+    mu64 = float(torch.tensor(mu, dtype=torch.float32))
+    m1 = mu64 * m0 + dw.double()
+    assert bool(((m.double() - m1).abs() <= 2.0 ** -23 * (m0.abs() + dw.double().abs())).all())
+    o = reference(dw.double() + mu64 * m1 if nesterov else m1)
+    step = lr * math.sqrt(max(1.0, M / N))
+    want = (1 - lr * wd) * w0 - step * o
+    for a, b, d in zip(w.double(), want, o):
+        # the direction's error, fp32 arithmetic of the update, one rounding (fp16: subnormals are absolute)
+        bound = step * NS_TOL * float(d.norm()) + (half_step(t) + 2.0 ** -21) * float(b.norm()) + math.sqrt(M * N) * 2.0 ** -25
+        assert float((a - b).norm()) <= bound
+
+
+def test_update_graph_replay():
+    M, N = 192, 320
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.randn(1, M, N, device="cuda", generator=gen).bfloat16()
+    dw = torch.randn(1, M, N, device="cuda", generator=gen).bfloat16()
+    m = torch.zeros(1, M, N, device="cuda")
+    ws = workspace(B.orthogonalize_workspace_bytes(1, M, N))
+    we, me = w.clone(), m.clone()
+    call = lambda w, m: B.orthogonal_update(1, M, N, w, dw, m, 0.9, True, 0.02, ws=ws)
+    call(we, me)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(w, m)
+    for k in range(3):
+        if k:
+            dw.normal_()
+            call(we, me)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w, we) and torch.equal(m, me)
