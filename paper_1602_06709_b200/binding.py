@@ -392,25 +392,32 @@ def dtype_code(t) -> int:
     return _DTYPES[t.dtype]
 
 
-def _typed(where, sizes, typed=(), fp32=(), int32=()):
-    """Checks the tensors of a call: (tensor, element count) pairs, None allowed; all on one device, the current one.
-    Returns the type code of the first of `typed`, which all share it."""
-    if any(not isinstance(n, int) or n <= 0 for n in sizes):
-        raise PclError(ERR_BAD_ARG, where)
-    code = dtype_code(typed[0][0])
-    dev = typed[0][0].device
-    for group, want in ((typed, typed[0][0].dtype), (fp32, torch.float32), (int32, torch.int32)):
+def _typed(where, sizes, typed, fp32=(), int32=()):
+    """Checks the tensors of a call -- (tensor, element count) pairs, None allowed -- and returns the type code that those of
+    `typed` share; all must be on one device, the current one."""
+    for n in sizes:
+        if type(n) is not int or n <= 0:
+            raise PclError(ERR_BAD_ARG, where)
+    first = typed[0][0]
+    code, dev = dtype_code(first), first.device
+    for group, want in ((typed, first.dtype), (fp32, torch.float32), (int32, torch.int32)):
         for t, n in group:
             if t is None:
                 continue
             if t.dtype != want:
                 raise TypeError(f"{where}: a {want} tensor is wanted, not {t.dtype}")
-            if t.numel() != n:
-                raise ValueError(f"{where}: a tensor of {n} elements is wanted, not {t.numel()}")
-    for t, _ in (*typed, *fp32, *int32):
-        if t is not None and (not t.is_cuda or t.device != dev or dev.index != torch.cuda.current_device()):
-            raise ValueError(f"{where}: all tensors must be on the current device")
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{where}: a contiguous tensor of {n} elements is wanted")
+            if t.device != dev:
+                raise ValueError(f"{where}: all tensors must be on one device")
+    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
+        raise ValueError(f"{where}: all tensors must be on the current CUDA device")
     return code
+
+
+def _addr(t):
+    """Address of a tensor that _typed() has checked (0 for None)."""
+    return 0 if t is None else t.data_ptr()
 
 
 def _id(v):
@@ -424,7 +431,7 @@ def embedding_workspace_bytes(N, V, C) -> int:
 def embedding_fwd(N, V, C, ids, table, scale, out, pad_id=None, stream=None):
     """out[n] = scale * table[ids[n]]; rows of pad_id are zero."""
     d = _typed("pcl_embedding_fwd", (N, V, C), [(table, V * C), (out, N * C)], int32=[(ids, N)])
-    _check(lib().pcl_embedding_fwd(N, V, C, d, _ptr(ids), _ptr(table), ctypes.c_float(scale), _id(pad_id), _ptr(out),
+    _check(lib().pcl_embedding_fwd(N, V, C, d, _addr(ids), _addr(table), scale, _id(pad_id), _addr(out),
                                    _stream(stream)), "pcl_embedding_fwd")
 
 
@@ -432,7 +439,7 @@ def embedding_bwd(N, V, C, ids, dy, scale, dtable, pad_id=None, ws=None, stream=
     """dtable[v] = scale * sum of dy[n] over the tokens n with ids[n] == v; every row is written."""
     d = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_embedding_bwd(N, V, C, d, _ptr(ids), _ptr(dy), ctypes.c_float(scale), _id(pad_id), _ptr(dtable), wp, wb,
+    _check(lib().pcl_embedding_bwd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(dtable), wp, wb,
                                    _stream(stream)), "pcl_embedding_bwd")
 
 
@@ -440,8 +447,8 @@ def embedding_bwd_sgd(N, V, C, ids, dy, scale, table, lr, pad_id=None, ws=None, 
     """table[v] -= lr * dtable[v] in place for the rows that occur; dtable is not stored."""
     d = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_embedding_bwd_sgd(N, V, C, d, _ptr(ids), _ptr(dy), ctypes.c_float(scale), _id(pad_id), _ptr(table),
-                                       ctypes.c_float(lr), wp, wb, _stream(stream)), "pcl_embedding_bwd_sgd")
+    _check(lib().pcl_embedding_bwd_sgd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(table),
+                                       lr, wp, wb, _stream(stream)), "pcl_embedding_bwd_sgd")
 
 
 def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
@@ -454,8 +461,8 @@ def fc_softmax_xent_fwd(N, C, K, x, w, bias, labels, loss, row_loss, lse, ignore
     d = _typed("pcl_fc_softmax_xent_fwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K)],
                [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_fc_softmax_xent_fwd(N, C, K, d, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _id(ignore_label),
-                                         _ptr(loss), _ptr(row_loss), _ptr(lse), wp, wb, _stream(stream)),
+    _check(lib().pcl_fc_softmax_xent_fwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label),
+                                         _addr(loss), _addr(row_loss), _addr(lse), wp, wb, _stream(stream)),
            "pcl_fc_softmax_xent_fwd")
 
 
@@ -465,8 +472,8 @@ def fc_softmax_xent_bwd(N, C, K, x, w, bias, labels, lse, row_grad, dx, dw, dbia
     d = _typed("pcl_fc_softmax_xent_bwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K), (dx, N * C), (dw, K * C), (dbias, K)],
                [(lse, N), (row_grad, N)], [(labels, N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_fc_softmax_xent_bwd(N, C, K, d, _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _id(ignore_label), _ptr(lse),
-                                         _ptr(row_grad), _ptr(dx), _ptr(dw), _ptr(dbias), wp, wb, _stream(stream)),
+    _check(lib().pcl_fc_softmax_xent_bwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label), _addr(lse),
+                                         _addr(row_grad), _addr(dx), _addr(dw), _addr(dbias), wp, wb, _stream(stream)),
            "pcl_fc_softmax_xent_bwd")
 
 
@@ -478,15 +485,15 @@ def orthogonalize(count, M, N, g, out, steps=5, ws=None, stream=None):
     """out = g / |g| after `steps` Newton-Schulz steps, for each of `count` M x N matrices."""
     d = _typed("pcl_orthogonalize", (count, M, N), [(g, count * M * N), (out, count * M * N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_orthogonalize(count, M, N, d, _ptr(g), _ptr(out), steps, wp, wb, _stream(stream)), "pcl_orthogonalize")
+    _check(lib().pcl_orthogonalize(count, M, N, d, _addr(g), _addr(out), steps, wp, wb, _stream(stream)), "pcl_orthogonalize")
 
 
 def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_decay=0.0, steps=5, ws=None, stream=None):
     """momentum <- mu momentum + dw, then w <- (1 - lr weight_decay) w - lr sqrt(max(1, M/N)) * orthogonalize(direction)."""
     d = _typed("pcl_orthogonal_update", (count, M, N), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)])
     wp, wb = _ws(ws)
-    _check(lib().pcl_orthogonal_update(count, M, N, d, _ptr(w), _ptr(dw), _ptr(momentum), ctypes.c_float(mu),
-                                       1 if nesterov else 0, ctypes.c_float(lr), ctypes.c_float(weight_decay), steps, wp, wb,
+    _check(lib().pcl_orthogonal_update(count, M, N, d, _addr(w), _addr(dw), _addr(momentum), mu,
+                                       1 if nesterov else 0, lr, weight_decay, steps, wp, wb,
                                        _stream(stream)), "pcl_orthogonal_update")
 
 

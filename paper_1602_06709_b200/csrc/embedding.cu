@@ -2,9 +2,11 @@
 // or of dy is read once, a row of the output written once.
 //
 // Gradient: dtable[v] = scale * sum over tokens n with ids[n] = v of dy[n].  The tokens are sorted by id (stable, so equal
-// ids stay in index order), then every 32 consecutive sorted tokens are one work item: segments that lie inside an item
-// are summed and written directly, the two that may cross its borders leave partial sums that a second pass adds in
-// order.  The work is even whatever the ids' frequencies are, and the additions have a fixed order (no atomics).
+// ids stay in index order) by one cluster of CTAs, while the other CTAs of that launch zero the gradient's last rows, as many
+// as fit the sort's time (the sort is latency, the zeroing bandwidth).  Then every kItemTokens consecutive sorted tokens are one work item.  An item sums the
+// segments (runs of equal ids) that begin in it; only segments of more than kLongSegment tokens are cut at the items' borders
+// into partial sums that a last pass adds in order.  The work is even whatever the ids' frequencies are, and the
+// additions have a fixed order (no atomics).  Blocks that zero the remaining rows that do not occur run between the items' blocks.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <limits.h>
@@ -16,11 +18,15 @@ namespace pcl {
 
 namespace {
 
-constexpr int kItemTokens = 32;
+constexpr int kItemTokens = 16;
+constexpr int kLongSegment = 32;
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = 32;
 constexpr int kMaxSortCtas = 8;          // portable cluster size
-constexpr int kMaxBins = 256;
+constexpr int kMaxBits = 9;              // bits of a digit
+constexpr int kHistLd = (1 << kMaxBits) + 1;                  // (odd: a column over the warps meets every bank once)
+constexpr size_t kZeroInSort = size_t(100) << 20;             // bytes zeroed beside the sort (about its 20 us)
+constexpr int kMaxRun = 8192;            // tokens per CTA that the shared-memory sort takes
 
 template <class T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
@@ -33,6 +39,13 @@ template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return
 
 template <class T, int kVec> struct alignas(sizeof(T) * kVec) Pack { T e[kVec]; };
 
+// Output rows are not read again by these kernels: they should not push the table's rows out of L2.
+template <class T, int kVec>
+__device__ __forceinline__ void store_streaming(Pack<T, kVec>* p, const Pack<T, kVec>& v) {
+    if constexpr (sizeof(T) * kVec == 16) __stcs(reinterpret_cast<uint4*>(p), *reinterpret_cast<const uint4*>(&v));
+    else *p = v;
+}
+
 // ids that name no row (outside [0, V)) and the padding id
 __device__ __forceinline__ bool row_exists(int id, int V, int pad_id, unsigned int* status) {
     if (id == pad_id) return false;
@@ -43,6 +56,7 @@ __device__ __forceinline__ bool row_exists(int id, int V, int pad_id, unsigned i
     return true;
 }
 
+// Two rows per pass of a thread group, and two vectors of each: four independent loads per thread in flight.
 template <class T, int kVec>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ table,
                                                             float scale, int pad_id, T* __restrict__ out, int N, int V, int C,
@@ -50,259 +64,391 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restric
     const int tpr = 1 << tpr_log2;                   // threads per row
     const int vecs = C / kVec;
     const int lane = threadIdx.x & (tpr - 1);
-    const long rows_per_pass = long(gridDim.x) * (256 >> tpr_log2);
-    for (long n = long(blockIdx.x) * (256 >> tpr_log2) + (threadIdx.x >> tpr_log2); n < N; n += rows_per_pass) {
-        const int id = ids[n];
-        const bool there = row_exists(id, V, pad_id, status);
-        const Pack<T, kVec>* src = reinterpret_cast<const Pack<T, kVec>*>(table + size_t(there ? id : 0) * C);
-        Pack<T, kVec>* dst = reinterpret_cast<Pack<T, kVec>*>(out + size_t(n) * C);
-        for (int i = lane; i < vecs; i += tpr) {
-            Pack<T, kVec> v;
-            if (there) {
-                v = src[i];
+    const long groups = long(gridDim.x) * (256 >> tpr_log2);
+    for (long n = long(blockIdx.x) * (256 >> tpr_log2) + (threadIdx.x >> tpr_log2); n < N; n += 2 * groups) {
+        bool there[2];
+        const Pack<T, kVec>* src[2];
+        Pack<T, kVec>* dst[2];
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) v.e[j] = from_f32<T>(scale * to_f32<T>(v.e[j]));
-            } else {
+        for (int r = 0; r < 2; ++r) {
+            const long row = n + r * groups;
+            const int id = row < N ? ids[row] : pad_id;
+            there[r] = row < N && row_exists(id, V, pad_id, status);
+            src[r] = reinterpret_cast<const Pack<T, kVec>*>(table + size_t(there[r] ? id : 0) * C);
+            dst[r] = row < N ? reinterpret_cast<Pack<T, kVec>*>(out + size_t(row) * C) : nullptr;
+        }
+        for (int i = lane; i < vecs; i += 2 * tpr) {
+            Pack<T, kVec> v[2][2];
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) v.e[j] = from_f32<T>(0.f);
-            }
-            dst[i] = v;
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (there[r] && i + h * tpr < vecs) v[r][h] = src[r][i + h * tpr];
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!dst[r] || i + h * tpr >= vecs) continue;
+                    Pack<T, kVec> o;
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) o.e[j] = from_f32<T>(there[r] ? scale * to_f32<T>(v[r][h].e[j]) : 0.f);
+                    store_streaming(&dst[r][i + h * tpr], o);
+                }
         }
     }
 }
 
 // Stable radix sort of (id, token) by one cluster of CTAs.  Every warp owns a run of consecutive tokens; per pass it counts
 // its digits, the counts are turned into positions (over digits, then CTAs, then warps, which keeps equal digits in
-// token order), and the warp scatters its run in order.  Tokens without a row get the key V and end up last.
-// Also leaves, per table row, the first sorted position of its tokens (-1: none).
+// token order), and the warp scatters its run in order.  Tokens without a row get the key V and end up last.  Each CTA
+// owns a run of 2^run_log2 positions in its shared memory, and scattering writes the owner's (distributed shared memory);
+// more tokens than that are kept in global memory instead (kShared = false).
+// Leaves the sorted keys and tokens and, for each id that occurs, the bounds of its segment.
 struct SortArgs {
     const int* ids;
     int N, V, pad_id;
     int passes, bits;             // digits of `bits` bits, least significant first
+    int ctas;                     // of the sorting cluster (cluster 0)
+    int run_log2;                 // positions per CTA (kShared)
     int per_warp;                 // tokens per warp, a multiple of 32
-    int* keys[2];
-    int* idx[2];
-    int* totals;                  // [kMaxSortCtas][kMaxBins]
-    int* head;                    // [V]
+    int *keys0, *keys1;           // written by the even and the odd passes (kShared: the last pass's, once)
+    int *idx0, *idx1;
+    int2* bounds;                 // [V]: first position and end of the segment of an id, (-1, -1) if it does not occur
+    int* long_count;              // set to 0 here
+    uint4* zero; size_t zero16;   // what the other CTAs clear: 16-byte units, and the bytes behind them
+    unsigned char* zero_tail; int zero_tail_bytes;
     unsigned int* status;
 };
+template <bool kShared>
 __device__ __forceinline__ void sort_barrier(bool cluster) {
-    if (cluster) { __threadfence(); cluster_sync_all(); __threadfence(); }     // (also drops stale L1 lines)
-    else __syncthreads();
+    if (!cluster) { __syncthreads(); return; }
+    if (!kShared) __threadfence();
+    cluster_sync_all();
+    if (!kShared) __threadfence();                            // (drops stale L1 lines)
 }
-__global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a, int ctas) {
-    __shared__ int hist[kSortWarps][kMaxBins];
-    __shared__ int base[kMaxBins];
-    __shared__ int warp_sum[8];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cta = blockIdx.x;
+// The lanes of `act` (to which the calling lane belongs) that hold the same digit of `bits` bits.
+__device__ __forceinline__ unsigned same_digit(unsigned act, int d, int bits) {
+    unsigned same = act;
+    for (int b = 0; b < bits; ++b) {
+        const unsigned m = __ballot_sync(act, (d >> b) & 1);
+        same &= (d >> b) & 1 ? m : ~m;
+    }
+    return same;
+}
+__device__ __forceinline__ int ld_cluster(uint32_t addr) {
+    int v;
+    asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, int x, int y) {
+    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ uint32_t map_addr(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+template <bool kShared>
+__global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a) {
+    extern __shared__ int sort_smem[];       // hist [32][kHistLd], totals [512], (kShared) [2] runs of (key, token)
+    __shared__ int warp_sum[16];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (int(blockIdx.x) >= a.ctas) {         // the other clusters: zeros
+        const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+        const size_t stride = size_t(gridDim.x - a.ctas) * kSortThreads;
+        const size_t i0 = size_t(blockIdx.x - a.ctas) * kSortThreads + threadIdx.x;
+#pragma unroll 4
+        for (size_t i = i0; i < a.zero16; i += stride) a.zero[i] = z;
+        if (i0 < size_t(a.zero_tail_bytes)) a.zero_tail[i0] = 0;
+        return;
+    }
+    int(*hist)[kHistLd] = reinterpret_cast<int(*)[kHistLd]>(sort_smem);
+    int* totals = sort_smem + kSortWarps * kHistLd;
+    int2* runs = reinterpret_cast<int2*>(totals + (1 << kMaxBits));           // [2][1 << run_log2]
+    const int cta = blockIdx.x, ctas = a.ctas;
     const bool cluster = ctas > 1;
-    const long run0 = (long(cta) * kSortWarps + warp) * a.per_warp;
-    const long run1 = run0 + a.per_warp < a.N ? run0 + a.per_warp : a.N;
-    const int bins = 1 << a.bits;
-    for (int v = cta * kSortThreads + threadIdx.x; v < a.V; v += ctas * kSortThreads) a.head[v] = -1;
+    if (cta == 0 && threadIdx.x == 0) *a.long_count = 0;
+    for (int v = cta * kSortThreads + threadIdx.x; v < a.V; v += ctas * kSortThreads) a.bounds[v] = make_int2(-1, -1);
+    const int bins = 1 << a.bits, run_size = 1 << a.run_log2;
+    // this warp's tokens, as positions of the sequence; kShared: offsets in this CTA's run
+    const long cta0 = kShared ? long(cta) << a.run_log2 : 0;
+    const long r0 = (kShared ? cta0 : long(cta) * kSortWarps * a.per_warp) + long(warp) * a.per_warp;
+    long r1 = r0 + a.per_warp;
+    if (kShared && r1 > cta0 + run_size) r1 = cta0 + run_size;
+    if (r1 > a.N) r1 = a.N;
+    auto id_key = [&](long i) {
+        const int id = a.ids[i];
+        return row_exists(id, a.V, a.pad_id, a.status) ? id : a.V;
+    };
+    if (kShared) {
+#pragma unroll 2
+        for (long i = r0 + lane; i < r1; i += 32) runs[i - cta0] = make_int2(id_key(i), int(i));
+        __syncwarp();
+    }
     for (int pass = 0; pass < a.passes; ++pass) {
-        const int shift = pass * a.bits;
-        const int* src_key = a.keys[(pass & 1) ^ 1];
-        const int* src_idx = a.idx[(pass & 1) ^ 1];
-        int* dst_key = a.keys[pass & 1];
-        int* dst_idx = a.idx[pass & 1];
-        auto key_of = [&](long i) {
-            if (pass > 0) return src_key[i];
-            const int id = a.ids[i];
-            return row_exists(id, a.V, a.pad_id, a.status) ? id : a.V;
+        const int shift = pass * a.bits, from = pass & 1;     // kShared: buffer read in this pass
+        const int2* run = runs + (size_t(from) << a.run_log2) - cta0;
+        auto pair_of = [&](long i) {
+            if (kShared) return run[i];
+            return pass > 0 ? make_int2((from ? a.keys0 : a.keys1)[i], (from ? a.idx0 : a.idx1)[i]) : make_int2(id_key(i), int(i));
         };
         for (int d = lane; d < bins; d += 32) hist[warp][d] = 0;
         __syncwarp();
-        for (long i0 = run0; i0 < run1; i0 += 32) {
+        for (long i0 = r0; i0 < r1; i0 += 32) {
             const long i = i0 + lane;
-            const bool in = i < run1;
+            const bool in = i < r1;
             const unsigned act = __ballot_sync(0xffffffffu, in);
             if (in) {
-                const int d = (key_of(i) >> shift) & (bins - 1);
-                const unsigned same = __match_any_sync(act, d);
+                const int d = (pair_of(i).x >> shift) & (bins - 1);
+                const unsigned same = same_digit(act, d, a.bits);
                 if (lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
             }
             __syncwarp();
         }
         __syncthreads();
-        if (threadIdx.x < bins) {
-            int run = 0;
-            for (int w = 0; w < kSortWarps; ++w) { const int c = hist[w][threadIdx.x]; hist[w][threadIdx.x] = run; run += c; }
-            a.totals[cta * kMaxBins + threadIdx.x] = run;
+        const int d0 = threadIdx.x;                           // thread d: digit d's counts of the warps become offsets
+        int total = 0;
+        if (d0 < bins) {
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; ++w) { const int c = hist[w][d0]; hist[w][d0] = total; total += c; }
+            totals[d0] = total;
         }
-        sort_barrier(cluster);
-        if (threadIdx.x < kMaxBins) {
-            const int d = threadIdx.x;
-            int all = 0, before = 0;
-            if (d < bins)
-                for (int c = 0; c < ctas; ++c) {
-                    const int v = *static_cast<volatile int*>(a.totals + c * kMaxBins + d);
-                    if (c < cta) before += v;
-                    all += v;
-                }
-            int inc = all;                               // inclusive scan over the digits
+        sort_barrier<kShared>(cluster);
+        int all = total, before = 0;                          // over the CTAs, and those before this one
+        if (cluster && d0 < bins) {
+            const uint32_t mine = smem_u32(totals + d0);
+            all = 0;
+#pragma unroll 4
+            for (int c = 0; c < ctas; ++c) {
+                const int v = ld_cluster(map_addr(mine, c));
+                if (c < cta) before += v;
+                all += v;
+            }
+        }
+        if (d0 < (1 << kMaxBits)) {                           // exclusive scan over the digits
+            if (d0 >= bins) all = 0;
+            int inc = all;
             for (int o = 1; o < 32; o <<= 1) { const int u = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += u; }
             if (lane == 31) warp_sum[warp] = inc;
-            base[d] = inc - all + before;
+            before += inc - all;
         }
         __syncthreads();
-        if (threadIdx.x < kMaxBins) {
-            int off = 0;
-            for (int w = 0; w < warp; ++w) off += warp_sum[w];
-            base[threadIdx.x] += off;
+        if (d0 < bins) {
+            for (int w = 0; w < warp; ++w) before += warp_sum[w];
+#pragma unroll 8
+            for (int w = 0; w < kSortWarps; ++w) hist[w][d0] += before;
         }
         __syncthreads();
-        for (int d = lane; d < bins; d += 32) hist[warp][d] += base[d];
-        __syncwarp();
-        for (long i0 = run0; i0 < run1; i0 += 32) {
+        const uint32_t dst_run = smem_u32(runs + ((from ^ 1) << a.run_log2));
+        for (long i0 = r0; i0 < r1; i0 += 32) {
             const long i = i0 + lane;
-            const bool in = i < run1;
+            const bool in = i < r1;
             const unsigned act = __ballot_sync(0xffffffffu, in);
             if (in) {
-                const int k = key_of(i), t = pass > 0 ? src_idx[i] : int(i);
-                const int d = (k >> shift) & (bins - 1);
-                const unsigned same = __match_any_sync(act, d);
+                const int2 kt = pair_of(i);
+                const int d = (kt.x >> shift) & (bins - 1);
+                const unsigned same = same_digit(act, d, a.bits);
                 const int pos = hist[warp][d] + __popc(same & ((1u << lane) - 1u));
                 __syncwarp(act);
                 if (lane == __ffs(same) - 1) hist[warp][d] += __popc(same);
-                dst_key[pos] = k;
-                dst_idx[pos] = t;
+                if (kShared) {
+                    const uint32_t off = (uint32_t(pos) & uint32_t(run_size - 1)) * 8u;
+                    if (cluster) st_cluster(map_addr(dst_run + off, uint32_t(pos) >> a.run_log2), kt.x, kt.y);
+                    else runs[((from ^ 1) << a.run_log2) + pos] = kt;
+                } else {
+                    (from ? a.keys1 : a.keys0)[pos] = kt.x;
+                    (from ? a.idx1 : a.idx0)[pos] = kt.y;
+                }
             }
             __syncwarp();
         }
-        sort_barrier(cluster);
+        sort_barrier<kShared>(cluster);
     }
-    const int* keys = a.keys[(a.passes - 1) & 1];
-    for (long i = long(cta) * kSortThreads + threadIdx.x; i < a.N; i += long(ctas) * kSortThreads) {
-        const int k = keys[i];
-        if (k < a.V && (i == 0 || keys[i - 1] != k)) a.head[k] = int(i);
+    const int last = a.passes & 1;                            // kShared: the buffer of the last pass
+    int* sorted = (a.passes & 1) ? a.keys0 : a.keys1;
+    int* sorted_idx = (a.passes & 1) ? a.idx0 : a.idx1;
+    const long e0 = kShared ? cta0 : 0;
+    const long e1 = kShared ? (cta0 + run_size < a.N ? cta0 + run_size : a.N) : a.N;
+    const long step = kShared ? kSortThreads : long(ctas) * kSortThreads;
+    for (long i = e0 + (kShared ? 0 : long(cta) * kSortThreads) + threadIdx.x; i < e1; i += step) {
+        int k, before = -1, after = -1;
+        if (kShared) {
+            const int o = int(i - cta0);
+            const int2* mine = runs + (last << a.run_log2);
+            k = mine[o].x;
+            if (i > 0) before = o > 0 ? mine[o - 1].x : ld_cluster(map_addr(smem_u32(mine + run_size - 1), cta - 1));
+            if (i + 1 < a.N) after = o + 1 < run_size ? mine[o + 1].x : ld_cluster(map_addr(smem_u32(mine), cta + 1));
+            sorted[i] = k;
+            sorted_idx[i] = mine[o].y;
+        } else {
+            k = sorted[i];
+            if (i > 0) before = sorted[i - 1];
+            if (i + 1 < a.N) after = sorted[i + 1];
+        }
+        if (k < a.V) {
+            if (before != k) a.bounds[k].x = int(i);
+            if (after != k) a.bounds[k].y = int(i) + 1;
+        }
     }
+    if (kShared && cluster) cluster_sync_all();               // (the neighbours may still read this CTA's run)
 }
 
 struct GradArgs {
     const int* keys;              // sorted ids (V: no row)
     const int* idx;               // their tokens
-    const int* head;              // [V]
-    float* part;                  // [items][2][C]: sums of an item's first segment (begun before it) and of its last (goes on)
+    const int2* bounds;           // [V] segment of an id, (-1, -1) if it does not occur
+    int zero_rows;                // rows [0, zero_rows) that do not occur are zeroed here
+    int item_blocks, zero_blocks;
+    float* part;                  // [items][2][C]: sums of an item's share of a long segment begun before it, and begun in it
     float scale, lr;
     int N, V, C, items;
-    int tpi_log2;                 // threads per item
-    int item_blocks;              // blocks that take items; the others write the rows that do not occur
+    int* long_count;              // long segments and the items they begin in
+    int* long_items;
+    int wpi_log2;                 // warps per item
     int sgd;
 };
 
 template <class T, int kVec>
-__device__ __forceinline__ void write_row(const GradArgs& a, T* out, int key, int i, const float (&sum)[kVec]) {
-    Pack<T, kVec>* dst = reinterpret_cast<Pack<T, kVec>*>(out + size_t(key) * a.C) + i;
+__device__ __forceinline__ void write_row(const GradArgs& a, T* out, int key, int i, const float (&sum)[kVec], const Pack<T, kVec>& old) {
     Pack<T, kVec> o;
     if (a.sgd) {
-        o = *dst;
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) o.e[j] = from_f32<T>(fmaf(-a.lr, a.scale * sum[j], to_f32<T>(o.e[j])));
+        for (int j = 0; j < kVec; ++j) o.e[j] = from_f32<T>(fmaf(-a.lr, a.scale * sum[j], to_f32<T>(old.e[j])));
     } else {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) o.e[j] = from_f32<T>(a.scale * sum[j]);
     }
-    *dst = o;
+    reinterpret_cast<Pack<T, kVec>*>(out + size_t(key) * a.C)[i] = o;
 }
 
-template <class T, int kVec>
-__global__ void __launch_bounds__(256) embedding_grad_kernel(GradArgs a, const T* __restrict__ dy, T* __restrict__ out) {
-    const int vecs = a.C / kVec;
-    if (int(blockIdx.x) >= a.item_blocks) {          // rows that do not occur are zero: one warp per row
-        const int warps = (gridDim.x - a.item_blocks) * 8, lane = threadIdx.x & 31;
-        for (int v = (blockIdx.x - a.item_blocks) * 8 + (threadIdx.x >> 5); v < a.V; v += warps) {
-            if (a.head[v] >= 0) continue;
-            Pack<T, kVec> z;
+// One warp per item and 32 vectors of a row.  The item's keys and tokens are held by the lanes (a window of 32 sorted
+// positions), so that per batch of tokens only their rows are waited for; with kSgd the table's old rows come with them.
+template <class T, int kVec, bool kSgd>
+__global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradArgs a, const T* __restrict__ dy, T* __restrict__ out) {
+    constexpr int kBatch = 4;
+    using P = Pack<T, kVec>;
+    const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    // the zeroing blocks are spread evenly among the others
+    const long all = long(a.item_blocks) + a.zero_blocks, b = blockIdx.x;
+    const int zeros_before = int(b * a.zero_blocks / all);
+    if (!kSgd && int((b + 1) * a.zero_blocks / all) != zeros_before) {
+        P z;
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) z.e[j] = from_f32<T>(0.f);
-            Pack<T, kVec>* dst = reinterpret_cast<Pack<T, kVec>*>(out + size_t(v) * a.C);
+        for (int j = 0; j < kVec; ++j) z.e[j] = from_f32<T>(0.f);
+        for (int v = zeros_before * 8 + w; v < a.zero_rows; v += a.zero_blocks * 8) {
+            if (a.bounds[v].x >= 0) continue;
+            P* dst = reinterpret_cast<P*>(out + size_t(v) * a.C);
+#pragma unroll 4
             for (int i = lane; i < vecs; i += 32) dst[i] = z;
         }
         return;
     }
-    const int tpi = 1 << a.tpi_log2, per_block = 256 >> a.tpi_log2;
-    const int strips = (vecs + tpi - 1) >> a.tpi_log2;
-    const long works = long(a.items) * strips;
-    for (long wk = long(blockIdx.x) * per_block + (threadIdx.x >> a.tpi_log2); wk < works; wk += long(a.item_blocks) * per_block) {
-        const int item = int(wk / strips);
-        const int i = int(wk - long(item) * strips) * tpi + (threadIdx.x & (tpi - 1));
-        if (i >= vecs) continue;
-        const int p0 = item * kItemTokens;
-        const int p1 = p0 + kItemTokens < a.N ? p0 + kItemTokens : a.N;
-        int key = a.keys[p0];
-        if (key >= a.V) continue;
-        bool begun_before = p0 > 0 && a.keys[p0 - 1] == key;
+    const int wpi = 1 << a.wpi_log2;                          // warps per item
+    const int item = int(b - zeros_before) * (8 >> a.wpi_log2) + (w >> a.wpi_log2);
+    if (item >= a.items) return;
+    const int p0 = item * kItemTokens;
+    const int p1 = p0 + kItemTokens < a.N ? p0 + kItemTokens : a.N;
+    int wb = p0, key, tok;
+    unsigned ends;
+    auto load_window = [&]() {                                // (whether lane 31 ends a segment is not known in it)
+        key = wb + lane < a.N ? a.keys[wb + lane] : -1;
+        tok = wb + lane < a.N ? a.idx[wb + lane] : 0;
+        const int next = __shfl_down_sync(0xffffffffu, key, 1);
+        ends = __ballot_sync(0xffffffffu, lane < 31 && key != next);
+    };
+    load_window();
+    const int k0 = __shfl_sync(0xffffffffu, key, 0);
+    if (k0 >= a.V) return;
+    // [.., rows_end): the item's tokens that have a row
+    const int rows_end = p0 + __popc(__ballot_sync(0xffffffffu, p0 + lane < p1 && key < a.V));
+    const int k1 = __shfl_sync(0xffffffffu, key, rows_end - 1 - p0);
+    const int2 s0 = a.bounds[k0], s1 = a.bounds[k1];
+    const int done = s0.x < p0 ? (s0.y < rows_end ? s0.y : rows_end) : p0;      // [p0, done): of a segment begun before
+    const bool front = done > p0 && s0.y - s0.x > kLongSegment;                 // ... whose share is summed here
+    const bool goes_on = s1.x >= p0 && s1.y > p1;                               // the last segment begins here
+    const bool back = goes_on && s1.y - s1.x > kLongSegment;
+    const int begin = front ? p0 : done, stop = back || !goes_on ? rows_end : s1.y;
+    if (back && (w & (wpi - 1)) == 0 && lane == 0) a.long_items[atomicAdd(a.long_count, 1)] = item;
+    for (int strip = w & (wpi - 1); strip < strips; strip += wpi) {
+        const int i = strip * 32 + lane;
+        const bool col = i < vecs;
         float sum[kVec];
 #pragma unroll
         for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
-        for (int p = p0; p < p1; p += 4) {
-            int k4[4];
-            Pack<T, kVec> v4[4];
+        for (int p = begin; p < stop; p += kBatch) {
+            if (p < wb || p + kBatch > wb + 31) { wb = p; load_window(); }
+            P v[kBatch], old[kSgd ? kBatch : 1];
+            bool row_ends[kBatch];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                k4[q] = p + q < p1 ? a.keys[p + q] : a.V;
-                if (k4[q] < a.V) v4[q] = reinterpret_cast<const Pack<T, kVec>*>(dy + size_t(a.idx[p + q]) * a.C)[i];
-            }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (k4[q] != key && key < a.V && p + q < p1) {          // the segment ends here
-                    if (begun_before) {
-#pragma unroll
-                        for (int j = 0; j < kVec; ++j) a.part[(size_t(item) * 2) * a.C + size_t(i) * kVec + j] = sum[j];
-                    } else {
-                        write_row<T, kVec>(a, out, key, i, sum);
-                    }
-                    begun_before = false;
-#pragma unroll
-                    for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
-                    key = k4[q];
+            for (int q = 0; q < kBatch; ++q) {
+                const int o = p - wb + q;
+                const size_t t = size_t(__shfl_sync(0xffffffffu, tok, o));
+                const int k = kSgd ? __shfl_sync(0xffffffffu, key, o) : 0;
+                row_ends[q] = (ends >> o) & 1u;
+                if (p + q < stop && col) {
+                    v[q] = reinterpret_cast<const P*>(dy + t * a.C)[i];
+                    if (kSgd && row_ends[q]) old[q] = reinterpret_cast<const P*>(out + size_t(k) * a.C)[i];
                 }
-                if (k4[q] < a.V)
-#pragma unroll
-                    for (int j = 0; j < kVec; ++j) sum[j] += to_f32<T>(v4[q].e[j]);
             }
-        }
-        if (key < a.V) {
-            const bool goes_on = p1 < a.N && a.keys[p1] == key;
-            if (begun_before || goes_on) {
-                float* dst = a.part + (size_t(item) * 2 + (begun_before ? 0 : 1)) * a.C + size_t(i) * kVec;
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) dst[j] = sum[j];
-            } else {
-                write_row<T, kVec>(a, out, key, i, sum);
+            for (int q = 0; q < kBatch; ++q) {
+                if (p + q >= stop) break;
+                const int k = __shfl_sync(0xffffffffu, key, p - wb + q);
+                if (!col) continue;
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) sum[j] += to_f32<T>(v[q].e[j]);
+                if (!row_ends[q] && p + q + 1 != stop) continue;
+                const bool share0 = front && p + q < done, share1 = back && p + q >= s1.x;
+                if (share0 || share1) {
+                    float* dst = a.part + (size_t(item) * 2 + (share0 ? 0 : 1)) * a.C + size_t(i) * kVec;
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) dst[j] = sum[j];
+                } else {
+                    write_row<T, kVec>(a, out, k, i, sum, old[kSgd ? q : 0]);
+                }
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
             }
         }
     }
 }
 
-// Segments that cross items: the item in which one begins adds up the partial sums in order.
+// Long segments: the shares of a segment are added up in a fixed order, every eighth by one warp, then the warps' sums.
 template <class T, int kVec>
 __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradArgs a, T* __restrict__ out) {
-    const int vecs = a.C / kVec;
-    const int tpi = 1 << a.tpi_log2, per_block = 256 >> a.tpi_log2;
-    const int strips = (vecs + tpi - 1) >> a.tpi_log2;
-    const long works = long(a.items) * strips;
-    for (long wk = long(blockIdx.x) * per_block + (threadIdx.x >> a.tpi_log2); wk < works; wk += long(gridDim.x) * per_block) {
-        const int item = int(wk / strips);
-        const int i = int(wk - long(item) * strips) * tpi + (threadIdx.x & (tpi - 1));
-        const int p0 = item * kItemTokens, p1 = p0 + kItemTokens;
-        if (i >= vecs || p1 >= a.N) continue;
-        const int key = a.keys[p1 - 1];
-        if (key >= a.V || a.keys[p1] != key) continue;                                   // does not go on
-        if (a.keys[p0] == key && p0 > 0 && a.keys[p0 - 1] == key) continue;              // did not begin here
+    __shared__ float sums[8][32][kVec + 1];
+    const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const long works = long(*a.long_count) * strips;
+    for (long wk = blockIdx.x; wk < works; wk += gridDim.x) {
+        const int item = a.long_items[wk / strips], i = int(wk % strips) * 32 + lane;
+        const int key = a.keys[item * kItemTokens + kItemTokens - 1];
+        const int last = (a.bounds[key].y - 1) / kItemTokens;
         float sum[kVec];
-        const float* src = a.part + (size_t(item) * 2 + 1) * a.C + size_t(i) * kVec;
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum[j] = src[j];
-        for (int it = item + 1; it < a.items; ++it) {
-            const float* f = a.part + size_t(it) * 2 * a.C + size_t(i) * kVec;
+        for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
+        if (i < vecs) {
+#pragma unroll 8
+            for (int it = item + w; it <= last; it += 8) {
+                const float* src = a.part + (size_t(it) * 2 + (it == item ? 1 : 0)) * a.C + size_t(i) * kVec;
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) sum[j] += f[j];
-            const int e = (it + 1) * kItemTokens;
-            if (e >= a.N || a.keys[e] != key) break;
+                for (int j = 0; j < kVec; ++j) sum[j] += src[j];
+            }
         }
-        write_row<T, kVec>(a, out, key, i, sum);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) sums[w][lane][j] = sum[j];
+        __syncthreads();
+        if (w == 0 && i < vecs) {
+            for (int o = 1; o < 8; ++o)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) sum[j] += sums[o][lane][j];
+            Pack<T, kVec> old;
+            if (a.sgd) old = reinterpret_cast<const Pack<T, kVec>*>(out + size_t(key) * a.C)[i];
+            write_row<T, kVec>(a, out, key, i, sum, old);
+        }
+        __syncthreads();
     }
 }
 
@@ -312,15 +458,17 @@ int log2_threads(int vecs) {
     return l;
 }
 
-struct BwdLayout { size_t keys[2], idx[2], totals, head, part, total; };
+struct BwdLayout { size_t keys[2], idx[2], bounds, long_count, long_items, part, total; };
 BwdLayout bwd_layout(int N, int V, int C) {
     BwdLayout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
+    const size_t items = (size_t(N) + kItemTokens - 1) / kItemTokens;
     for (int i = 0; i < 2; ++i) { l.keys[i] = take(size_t(N) * 4); l.idx[i] = take(size_t(N) * 4); }
-    l.totals = take(size_t(kMaxSortCtas) * kMaxBins * 4);
-    l.head = take(size_t(V) * 4);
-    l.part = take(size_t((N + kItemTokens - 1) / kItemTokens) * 2 * C * 4);
+    l.bounds = take(size_t(V) * 8);
+    l.long_count = take(4);
+    l.long_items = take((size_t(N) / kLongSegment + 1) * 4);
+    l.part = take(N > kLongSegment ? items * 2 * C * 4 : 0);
     l.total = at;
     return l;
 }
@@ -330,7 +478,7 @@ int run_fwd(int N, int V, int C, const int* ids, const void* table, float scale,
             cudaStream_t st) {
     const int tl = log2_threads(C / kVec);
     const long rows_per_block = 256 >> tl;
-    const long blocks = (N + rows_per_block - 1) / rows_per_block, cap = long(device_sm_count()) * 8;
+    const long blocks = (N + 2 * rows_per_block - 1) / (2 * rows_per_block), cap = long(device_sm_count()) * 8;
     LaunchScope scope(KID_EMBEDDING, 2.0 * sizeof(T) * double(N) * C, st);
     embedding_fwd_kernel<T, kVec><<<int(blocks < cap ? blocks : cap), 256, 0, st>>>(
         ids, static_cast<const T*>(table), scale, pad_id, static_cast<T*>(out), N, V, C, tl, status);
@@ -339,23 +487,50 @@ int run_fwd(int N, int V, int C, const int* ids, const void* table, float scale,
 
 template <class T, int kVec>
 int run_grad(GradArgs a, const void* dy, void* out, cudaStream_t st) {
-    a.tpi_log2 = log2_threads(a.C / kVec);
-    const int tpi = 1 << a.tpi_log2;
-    const long strips = (a.C / kVec + tpi - 1) / tpi, works = long(a.items) * strips, per_block = 256 / tpi;
-    const long cap = long(device_sm_count()) * 16;
-    const long want = (works + per_block - 1) / per_block;
-    a.item_blocks = int(want < cap ? want : cap);
-    const int zero_blocks = a.sgd ? 0 : int((a.V + 7) / 8 < device_sm_count() * 8 ? (a.V + 7) / 8 : device_sm_count() * 8);
+    const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
+    while (a.wpi_log2 < 3 && (1 << a.wpi_log2) < strips) ++a.wpi_log2;
+    const int per_block = 8 >> a.wpi_log2, blocks = (a.items + per_block - 1) / per_block;
     {
-        LaunchScope scope(KID_EMBEDDING, double(sizeof(T)) * a.C * (double(a.N) + a.V), st);
-        embedding_grad_kernel<T, kVec><<<a.item_blocks + zero_blocks, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<T*>(out));
+        LaunchScope scope(KID_EMBEDDING, double(sizeof(T)) * a.C * double(a.N), st);
+        a.item_blocks = blocks;
+        const int zero_cap = device_sm_count() * 8;
+        a.zero_blocks = (a.zero_rows + 7) / 8 < zero_cap ? (a.zero_rows + 7) / 8 : zero_cap;
+        if (a.sgd) embedding_grad_kernel<T, kVec, true><<<blocks, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<T*>(out));
+        else embedding_grad_kernel<T, kVec, false><<<blocks + a.zero_blocks, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<T*>(out));
     }
     if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
-    if (a.items > 1) {
-        LaunchScope scope(KID_EMBEDDING, 0.0, st);
-        embedding_grad_join_kernel<T, kVec><<<a.item_blocks, 256, 0, st>>>(a, static_cast<T*>(out));
-    }
+    if (a.N <= kLongSegment) return PCL_OK;
+    LaunchScope scope(KID_EMBEDDING, 0.0, st);
+    const long most = (long(a.N) / kLongSegment) * ((vecs + 31) / 32), cap = long(device_sm_count()) * 8;
+    embedding_grad_join_kernel<T, kVec><<<int(most < cap ? most : cap), 256, 0, st>>>(a, static_cast<T*>(out));
     return cudaGetLastError() == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+}
+
+int log2_up(long v) {
+    int l = 0;
+    while ((1L << l) < v) ++l;
+    return l;
+}
+
+template <bool kShared>
+int run_sort(const SortArgs& s, size_t smem, int blocks, cudaStream_t st) {
+    static PerDeviceOnce once;
+    const int rc = once.run([&] {
+        return cudaFuncSetAttribute(embedding_sort_kernel<kShared>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - 1024) ==
+                       cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    });
+    if (rc != PCL_OK) return rc;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3(blocks);
+    lc.blockDim = dim3(kSortThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {unsigned(s.ctas), 1u, 1u};
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    return cudaLaunchKernelEx(&lc, embedding_sort_kernel<kShared>, s) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
 }
 
 }  // namespace
@@ -384,37 +559,51 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     char* base = static_cast<char*>(ws);
     SortArgs s{};
     s.ids = ids; s.N = N; s.V = V; s.pad_id = pad_id; s.status = status;
-    int key_bits = 1;
-    while (key_bits < 31 && (long(V) >> key_bits) != 0) ++key_bits;          // keys 0 .. V
-    s.passes = (key_bits + 7) / 8;
+    const int key_bits = log2_up(long(V) + 1);                               // keys 0 .. V
+    s.passes = (key_bits + kMaxBits - 1) / kMaxBits;
     s.bits = (key_bits + s.passes - 1) / s.passes;
-    int ctas = 1;
-    while (ctas < kMaxSortCtas && long(ctas) * kSortThreads * 4 < N) ctas *= 2;
-    const long per_warp = (N + long(ctas) * kSortWarps - 1) / (long(ctas) * kSortWarps);
-    s.per_warp = int((per_warp + 31) / 32 * 32);
-    for (int i = 0; i < 2; ++i) {
-        s.keys[i] = reinterpret_cast<int*>(base + l.keys[i]);
-        s.idx[i] = reinterpret_cast<int*>(base + l.idx[i]);
+    // Tokens per CTA: 1024 where one CTA takes them all, up to kMaxRun with eight; beyond, the sequence stays in global memory.
+    const bool shared = N <= kMaxSortCtas * kMaxRun;
+    size_t smem = size_t(kSortWarps * kHistLd + (1 << kMaxBits)) * 4;
+    if (shared) {
+        s.run_log2 = log2_up((N + kMaxSortCtas - 1) / kMaxSortCtas);
+        if (s.run_log2 < 10) s.run_log2 = 10;
+        s.ctas = 1 << log2_up((long(N) + (1 << s.run_log2) - 1) >> s.run_log2);
+        s.per_warp = (1 << s.run_log2) / kSortWarps;
+        smem += size_t(16) << s.run_log2;
+    } else {
+        s.ctas = kMaxSortCtas;
+        const long per_warp = (N + long(s.ctas) * kSortWarps - 1) / (long(s.ctas) * kSortWarps);
+        s.per_warp = int((per_warp + 31) / 32 * 32);
     }
-    s.totals = reinterpret_cast<int*>(base + l.totals);
-    s.head = reinterpret_cast<int*>(base + l.head);
+    s.keys0 = reinterpret_cast<int*>(base + l.keys[0]); s.keys1 = reinterpret_cast<int*>(base + l.keys[1]);
+    s.idx0 = reinterpret_cast<int*>(base + l.idx[0]); s.idx1 = reinterpret_cast<int*>(base + l.idx[1]);
+    s.bounds = reinterpret_cast<int2*>(base + l.bounds);
+    s.long_count = reinterpret_cast<int*>(base + l.long_count);
+    int zero_blocks = 0, zero_row0 = 0;
+    if (!sgd) {
+        // whole rows from the end, of which the first starts on a 16-byte boundary (every eighth row does)
+        const size_t row = size_t(C) * dtype_bytes(type), rows = kZeroInSort / row;
+        if (rows < size_t(V)) zero_row0 = (V - int(rows)) / 8 * 8;
+        const size_t bytes = size_t(V - zero_row0) * row;
+        s.zero = reinterpret_cast<uint4*>(static_cast<char*>(out) + zero_row0 * row);
+        s.zero16 = bytes / 16;
+        s.zero_tail = reinterpret_cast<unsigned char*>(s.zero + s.zero16);
+        s.zero_tail_bytes = int(bytes % 16);
+        const size_t want = (s.zero16 + 4 * kSortThreads - 1) / (4 * kSortThreads) + 1, cap = size_t(device_sm_count()) * 2;
+        zero_blocks = int((want < cap ? want : cap) + s.ctas - 1) / s.ctas * s.ctas;
+    }
     {
-        LaunchScope scope(KID_EMBEDDING, 16.0 * double(N) * s.passes, st);
-        cudaLaunchConfig_t lc = {};
-        lc.gridDim = dim3(ctas);
-        lc.blockDim = dim3(kSortThreads);
-        lc.stream = st;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim = {unsigned(ctas), 1u, 1u};
-        lc.attrs = attr;
-        lc.numAttrs = 1;
-        if (cudaLaunchKernelEx(&lc, embedding_sort_kernel, s, ctas) != cudaSuccess) return PCL_ERR_CUDA;
+        LaunchScope scope(KID_EMBEDDING, 16.0 * double(N) * s.passes + (sgd ? 0.0 : double(V) * C * dtype_bytes(type)), st);
+        const int rc = shared ? run_sort<true>(s, smem, s.ctas + zero_blocks, st) : run_sort<false>(s, smem, s.ctas + zero_blocks, st);
+        if (rc != PCL_OK) return rc;
     }
     GradArgs g{};
-    g.keys = s.keys[(s.passes - 1) & 1]; g.idx = s.idx[(s.passes - 1) & 1]; g.head = s.head;
+    g.keys = (s.passes & 1) ? s.keys0 : s.keys1; g.idx = (s.passes & 1) ? s.idx0 : s.idx1; g.bounds = s.bounds;
     g.part = reinterpret_cast<float*>(base + l.part);
-    g.scale = scale; g.lr = lr; g.N = N; g.V = V; g.C = C; g.items = (N + kItemTokens - 1) / kItemTokens; g.sgd = sgd;
+    g.long_count = s.long_count; g.long_items = reinterpret_cast<int*>(base + l.long_items);
+    g.scale = scale; g.lr = lr; g.N = N; g.V = V; g.C = C; g.items = (N - 1) / kItemTokens + 1; g.sgd = sgd;
+    g.zero_rows = zero_row0;
     if (type == DT_F32)
         return C % 4 == 0 ? run_grad<float, 4>(g, dy, out, st) : run_grad<float, 1>(g, dy, out, st);
     if (type == DT_BF16)

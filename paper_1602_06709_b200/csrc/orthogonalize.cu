@@ -21,69 +21,120 @@ namespace {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr double kNsEps = 1e-7;
 constexpr float kScaleX = 16384.f, kScaleB = 8192.f;        // of X and A, and of B
-constexpr int kNormBlocks = 64;                             // partial sums per matrix
+constexpr int kMaxNormBlocks = 1024;                        // partial sums per matrix
 
-__device__ __forceinline__ float elem(const void* p, int type, size_t i) {
-    if (type == DT_F32) return static_cast<const float*>(p)[i];
-    if (type == DT_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
-    return __half2float(static_cast<const __half*>(p)[i]);
+// kVec consecutive elements as fp32
+template <int kVec>
+__device__ __forceinline__ void load_vec(const void* p, int type, size_t i, float (&o)[kVec]) {
+    if constexpr (kVec == 1) {
+        o[0] = type == DT_F32 ? static_cast<const float*>(p)[i]
+             : type == DT_BF16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
+    } else {
+        static_assert(kVec == 4, "");
+        if (type == DT_F32) {
+            const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + i);
+            o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p) + i);
+            if (type == DT_BF16) {
+                o[0] = __uint_as_float(v.x << 16); o[1] = __uint_as_float(v.x & 0xffff0000u);
+                o[2] = __uint_as_float(v.y << 16); o[3] = __uint_as_float(v.y & 0xffff0000u);
+            } else {
+                const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), b = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
+                o[0] = a.x; o[1] = a.y; o[2] = b.x; o[3] = b.y;
+            }
+        }
+    }
+}
+template <int kVec>
+__device__ __forceinline__ void store_vec(float* p, size_t i, const float (&v)[kVec]) {
+    if constexpr (kVec == 1) p[i] = v[0];
+    else *reinterpret_cast<float4*>(p + i) = make_float4(v[0], v[1], v[2], v[3]);
 }
 
 struct StageArgs {
     const void* g; int type;
     float* momentum; float mu; int nesterov;
-    double* part;               // [count][kNormBlocks]
+    double* part;               // [count][kMaxNormBlocks]
+    int parts;
     float* x;                   // [count][M][ld] fp32 (null: not needed)
     __half* xh;                 // [count][M][ld]
     int M, N, ld;
 };
 
 // Sum of squares of U (64-bit: the squares of a gradient leave the range of fp32), and the momentum update.
+template <int kVec>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(StageArgs a) {
     __shared__ double red[8];
     const size_t n = size_t(a.M) * a.N, off = n * blockIdx.y;
     double sum = 0.0;
-    for (size_t i = size_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += size_t(gridDim.x) * 256) {
-        float u = elem(a.g, a.type, off + i);
+#pragma unroll 2
+    for (size_t i = (size_t(blockIdx.x) * 256 + threadIdx.x) * kVec; i < n; i += size_t(gridDim.x) * 256 * kVec) {
+        float u[kVec];
+        load_vec<kVec>(a.g, a.type, off + i, u);
         if (a.momentum) {
-            const float m = fmaf(a.mu, a.momentum[off + i], u);
-            a.momentum[off + i] = m;
-            u = a.nesterov ? fmaf(a.mu, m, u) : m;
+            float m[kVec];
+            load_vec<kVec>(a.momentum, DT_F32, off + i, m);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                m[j] = fmaf(a.mu, m[j], u[j]);
+                u[j] = a.nesterov ? fmaf(a.mu, m[j], u[j]) : m[j];
+            }
+            store_vec<kVec>(a.momentum, off + i, m);
         }
-        sum += double(u) * double(u);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) sum += double(u[j]) * double(u[j]);
     }
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; ++i) sum += red[i];
-        a.part[size_t(blockIdx.y) * kNormBlocks + blockIdx.x] = sum;
+        a.part[size_t(blockIdx.y) * kMaxNormBlocks + blockIdx.x] = sum;
     }
 }
 
 // X0 in fp32 and as the first product's fp16 operand.
+template <int kVec>
 __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
-    __shared__ float inv_s;
-    if (threadIdx.x == 0) {
-        double sum = 0.0;
-        for (int i = 0; i < kNormBlocks; ++i) sum += a.part[size_t(blockIdx.y) * kNormBlocks + i];
-        inv_s = float(1.0 / (sqrt(sum) + kNsEps));
-    }
+    __shared__ double red[8];
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.parts; i += 256) sum += a.part[size_t(blockIdx.y) * kMaxNormBlocks + i];
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
     __syncthreads();
-    const float inv = inv_s;
+    sum = 0.0;
+    for (int i = 0; i < 8; ++i) sum += red[i];
+    const float inv = float(1.0 / (sqrt(sum) + kNsEps));
     const size_t off = size_t(a.M) * a.N * blockIdx.y, off_x = size_t(a.M) * a.ld * blockIdx.y;
     for (int r = blockIdx.x; r < a.M; r += gridDim.x)
-        for (int c = threadIdx.x; c < a.N; c += 256) {
-            const size_t i = off + size_t(r) * a.N + c;
-            float u = elem(a.g, a.type, i);
+#pragma unroll 2
+        for (int c = threadIdx.x * kVec; c < a.N; c += 256 * kVec) {
+            const size_t i = off + size_t(r) * a.N + c, o = off_x + size_t(r) * a.ld + c;
+            float u[kVec];
             if (a.momentum) {
-                const float m = a.momentum[i];
-                u = a.nesterov ? fmaf(a.mu, m, u) : m;
+                float m[kVec];
+                load_vec<kVec>(a.momentum, DT_F32, i, m);
+                if (a.nesterov) {
+                    load_vec<kVec>(a.g, a.type, i, u);
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) u[j] = fmaf(a.mu, m[j], u[j]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) u[j] = m[j];
+                }
+            } else {
+                load_vec<kVec>(a.g, a.type, i, u);
             }
-            const float v = u * inv;
-            const size_t o = off_x + size_t(r) * a.ld + c;
-            if (a.x) a.x[o] = v;
-            a.xh[o] = __float2half_rn(v * kScaleX);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) u[j] *= inv;
+            if (a.x) store_vec<kVec>(a.x, o, u);
+            if constexpr (kVec == 1) {
+                a.xh[o] = __float2half_rn(u[0] * kScaleX);
+            } else {
+                const __half2 lo = __floats2half2_rn(u[0] * kScaleX, u[1] * kScaleX), hi = __floats2half2_rn(u[2] * kScaleX, u[3] * kScaleX);
+                *reinterpret_cast<uint2*>(a.xh + o) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+            }
         }
 }
 
@@ -95,7 +146,7 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     l.ld = int(align_up(N, 8));
     l.d = M < N ? M : N;
     l.ldd = int(align_up(l.d, 8));
-    l.part = take(size_t(count) * kNormBlocks * 8);
+    l.part = take(size_t(count) * kMaxNormBlocks * 8);
     l.x = take(size_t(count) * M * l.ld * 4);
     for (size_t& o : l.xh) o = take(size_t(count) * M * l.ld * 2);
     l.a = take(size_t(count) * l.d * l.ldd * 2);
@@ -116,17 +167,26 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     void *A = base + l.a, *B = base + l.b;
     const bool wide = o.M <= o.N;
     const long xb = long(o.M) * l.ld, db = long(l.d) * l.ldd;
-    StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), o.steps > 1 ? x : nullptr,
+    StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), 0, o.steps > 1 ? x : nullptr,
                 xh[0], o.M, o.N, l.ld};
+    // four elements at a time where every row starts on a multiple of four (16 bytes of fp32, 8 bytes of the 16-bit types)
+    const bool vec = o.N % 4 == 0;
     const double elems = double(o.count) * o.M * o.N;
+    const size_t per_block = 256 * 4 * 4, want = (size_t(o.M) * o.N + per_block - 1) / per_block;
+    const size_t cap = size_t(device_sm_count()) * 8 / o.count + 1;
+    s.parts = int(want < cap ? want : cap);
+    if (s.parts > kMaxNormBlocks) s.parts = kMaxNormBlocks;
     {
         LaunchScope scope(KID_ORTHO, elems * (o.momentum ? 8.0 + dtype_bytes(o.type) : double(dtype_bytes(o.type))), st);
-        ortho_norm_kernel<<<dim3(kNormBlocks, o.count), 256, 0, st>>>(s);
+        if (vec) ortho_norm_kernel<4><<<dim3(s.parts, o.count), 256, 0, st>>>(s);
+        else ortho_norm_kernel<1><<<dim3(s.parts, o.count), 256, 0, st>>>(s);
     }
     if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
     {
         LaunchScope scope(KID_ORTHO, elems * (6.0 + dtype_bytes(o.type) + (o.momentum ? 4.0 : 0.0)), st);
-        ortho_stage_kernel<<<dim3(o.M < 2048 ? o.M : 2048, o.count), 256, 0, st>>>(s);
+        const dim3 grid(o.M < 2048 ? o.M : 2048, o.count);
+        if (vec) ortho_stage_kernel<4><<<grid, 256, 0, st>>>(s);
+        else ortho_stage_kernel<1><<<grid, 256, 0, st>>>(s);
     }
     if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
     int cur = 0;
