@@ -4,7 +4,7 @@
 //
 // Every product runs on the 16-bit tensor cores with fp16 operands scaled by powers of two: all values are bounded (|X|, |A|
 // <= 1.5, |B| <= 2.9 by the polynomial), so fp16 has the three mantissa bits that bf16 lacks at no loss of range.  X
-// itself stays in fp32 until the last step; the last step takes the rounded X in its linear term too, so that the
+// itself keeps 22 bits until the last step, in two fp16 planes of which the products see the first; the last step takes the rounded X in its linear term too, so that the
 // rounding is passed on by the polynomial's derivative (which is small at 1) instead of by B alone.  Relative error of the
 // result (2-norm) 3e-4 .. 1.6e-3 on random, decaying and nearly low-rank spectra, where bf16 iterates give 1e-2 .. 2e-1.
 // A and A A are symmetric: the tiles below the diagonal are copies of those above it.
@@ -13,6 +13,7 @@
 #include <math.h>
 
 #include "pcl_internal.h"
+#include "pcl_ptx.cuh"
 
 namespace pcl {
 
@@ -57,15 +58,18 @@ struct StageArgs {
     float* momentum; float mu; int nesterov;
     double* part;               // [count][kMaxNormBlocks]
     int parts;
-    float* x;                   // [count][M][ld] fp32 (null: not needed)
-    __half* xh;                 // [count][M][ld]
+    __half* xh;                 // [count][M][ld] X0 * kScaleX
+    __half* xl;                 // what rounding left, times 2^11 (null: not needed)
     int M, N, ld;
+    int* counters;              // of the products' split workspace, to be zeroed (null: none)
 };
 
 // Sum of squares of U (64-bit: the squares of a gradient leave the range of fp32), and the momentum update.
 template <int kVec>
 __global__ void __launch_bounds__(256) ortho_norm_kernel(StageArgs a) {
     __shared__ double red[8];
+    grid_dependency_wait();
+    grid_dependents_launch();
     const size_t n = size_t(a.M) * a.N, off = n * blockIdx.y;
     double sum = 0.0;
 #pragma unroll 2
@@ -94,13 +98,17 @@ __global__ void __launch_bounds__(256) ortho_norm_kernel(StageArgs a) {
     }
 }
 
-// X0 in fp32 and as the first product's fp16 operand.
+// X0 in two fp16 planes.
 template <int kVec>
 __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
     __shared__ double red[8];
     double sum = 0.0;
+    grid_dependency_wait();
+    grid_dependents_launch();
     for (int i = threadIdx.x; i < a.parts; i += 256) sum += a.part[size_t(blockIdx.y) * kMaxNormBlocks + i];
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (a.counters && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int i = threadIdx.x; i < int(kGemm16CounterBytes / 4); i += 256) a.counters[i] = 0;
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
     __syncthreads();
     sum = 0.0;
@@ -127,18 +135,41 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
                 load_vec<kVec>(a.g, a.type, i, u);
             }
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) u[j] *= inv;
-            if (a.x) store_vec<kVec>(a.x, o, u);
+            for (int j = 0; j < kVec; ++j) u[j] *= inv * kScaleX;
+            alignas(8) __half h[kVec], l[kVec];
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) {
+                h[j] = __float2half_rn(u[j]);
+                l[j] = __float2half_rn((u[j] - __half2float(h[j])) * 2048.f);
+            }
             if constexpr (kVec == 1) {
-                a.xh[o] = __float2half_rn(u[0] * kScaleX);
+                a.xh[o] = h[0];
+                if (a.xl) a.xl[o] = l[0];
             } else {
-                const __half2 lo = __floats2half2_rn(u[0] * kScaleX, u[1] * kScaleX), hi = __floats2half2_rn(u[2] * kScaleX, u[3] * kScaleX);
-                *reinterpret_cast<uint2*>(a.xh + o) = make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+                *reinterpret_cast<uint2*>(a.xh + o) = *reinterpret_cast<const uint2*>(h);
+                if (a.xl) *reinterpret_cast<uint2*>(a.xl + o) = *reinterpret_cast<const uint2*>(l);
             }
         }
 }
 
-struct OrthoLayout { size_t part, x, xh[2], a, b, total; int ld, d, ldd; };
+// The three products of a step, with everything their tiling depends on.
+Gemm16Args gram_args(int count, int M, int N) {
+    const int d = M < N ? M : N;
+    Gemm16Args a{d, d, M < N ? N : M, count, false, {}, {}, GEMM16_SYM};
+    a.split_ws = reinterpret_cast<void*>(256);               // (until the workspace is known)
+    return a;
+}
+Gemm16Args square_args(int count, int M, int N) {
+    const int d = M < N ? M : N;
+    return gram_args(count, d, d);
+}
+Gemm16Args apply_args(int count, int M, int N) {
+    Gemm16Args a{M, N, M < N ? M : N, count, false, {}, {}, GEMM16_STEP};
+    a.split_ws = reinterpret_cast<void*>(256);
+    return a;
+}
+
+struct OrthoLayout { size_t part, xl, xh[2], a, b, split, split_bytes, total; int ld, d, ldd; };
 OrthoLayout ortho_layout(int count, int M, int N) {
     OrthoLayout l{};
     size_t at = 0;
@@ -147,10 +178,15 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     l.d = M < N ? M : N;
     l.ldd = int(align_up(l.d, 8));
     l.part = take(size_t(count) * kMaxNormBlocks * 8);
-    l.x = take(size_t(count) * M * l.ld * 4);
+    l.xl = take(size_t(count) * M * l.ld * 2);
     for (size_t& o : l.xh) o = take(size_t(count) * M * l.ld * 2);
     l.a = take(size_t(count) * l.d * l.ldd * 2);
     l.b = take(size_t(count) * l.d * l.ldd * 2);
+    for (const Gemm16Args& a : {gram_args(count, M, N), square_args(count, M, N), apply_args(count, M, N)}) {
+        const size_t b = gemm16_split_ws_bytes(a);
+        if (b > l.split_bytes) l.split_bytes = b;
+    }
+    l.split = take(l.split_bytes);
     l.total = at;
     return l;
 }
@@ -162,13 +198,13 @@ size_t orthogonalize_workspace_bytes(int count, int M, int N) { return ortho_lay
 int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     const OrthoLayout l = ortho_layout(o.count, o.M, o.N);
     char* base = static_cast<char*>(ws);
-    float* x = reinterpret_cast<float*>(base + l.x);
+    __half* xl = reinterpret_cast<__half*>(base + l.xl);
     __half* xh[2] = {reinterpret_cast<__half*>(base + l.xh[0]), reinterpret_cast<__half*>(base + l.xh[1])};
     void *A = base + l.a, *B = base + l.b;
     const bool wide = o.M <= o.N;
     const long xb = long(o.M) * l.ld, db = long(l.d) * l.ldd;
-    StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), 0, o.steps > 1 ? x : nullptr,
-                xh[0], o.M, o.N, l.ld};
+    StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), 0, xh[0],
+                o.steps > 1 ? xl : nullptr, o.M, o.N, l.ld, l.split_bytes ? reinterpret_cast<int*>(base + l.split) : nullptr};
     // four elements at a time where every row starts on a multiple of four (16 bytes of fp32, 8 bytes of the 16-bit types)
     const bool vec = o.N % 4 == 0;
     const double elems = double(o.count) * o.M * o.N;
@@ -178,52 +214,55 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     if (s.parts > kMaxNormBlocks) s.parts = kMaxNormBlocks;
     {
         LaunchScope scope(KID_ORTHO, elems * (o.momentum ? 8.0 + dtype_bytes(o.type) : double(dtype_bytes(o.type))), st);
-        if (vec) ortho_norm_kernel<4><<<dim3(s.parts, o.count), 256, 0, st>>>(s);
-        else ortho_norm_kernel<1><<<dim3(s.parts, o.count), 256, 0, st>>>(s);
+        const int rc = launch_chained(vec ? ortho_norm_kernel<4> : ortho_norm_kernel<1>, dim3(s.parts, o.count), dim3(256), 0, st, 1, s);
+        if (rc != PCL_OK) return rc;
     }
-    if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
     {
-        LaunchScope scope(KID_ORTHO, elems * (6.0 + dtype_bytes(o.type) + (o.momentum ? 4.0 : 0.0)), st);
-        const dim3 grid(o.M < 2048 ? o.M : 2048, o.count);
-        if (vec) ortho_stage_kernel<4><<<grid, 256, 0, st>>>(s);
-        else ortho_stage_kernel<1><<<grid, 256, 0, st>>>(s);
+        LaunchScope scope(KID_ORTHO, elems * (4.0 + dtype_bytes(o.type) + (o.momentum ? 4.0 : 0.0)), st);
+        const int rc = launch_chained(vec ? ortho_stage_kernel<4> : ortho_stage_kernel<1>, dim3(o.M < 2048 ? o.M : 2048, o.count),
+                                      dim3(256), 0, st, 1, s);
+        if (rc != PCL_OK) return rc;
     }
-    if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
     int cur = 0;
     for (int it = 0; it < o.steps; ++it) {
         const bool last = it + 1 == o.steps;
         const Gemm16Operand gram{xh[cur], l.ld, xb, !wide};
-        Gemm16Args g1{l.d, l.d, wide ? o.N : o.M, o.count, false, gram, gram, GEMM16_LINEAR};
-        g1.symmetric = true;
+        Gemm16Args g1 = gram_args(o.count, o.M, o.N);
+        g1.a = g1.b = gram;
+        g1.split_ws = base + l.split;
         g1.alpha = 1.f / kScaleX;                             // kScaleX^2 A -> kScaleX A
         g1.out = A; g1.out_type = DT_F16; g1.out_ld = l.ldd; g1.out_batch = db;
         int rc = launch_gemm16(g1, st);
         if (rc != PCL_OK) return rc;
         const Gemm16Operand am{A, l.ldd, db, false}, bm{B, l.ldd, db, false};
-        Gemm16Args g2{l.d, l.d, l.d, o.count, false, am, am, GEMM16_LINEAR};
-        g2.symmetric = true;
+        Gemm16Args g2 = square_args(o.count, o.M, o.N);
+        g2.a = g2.b = am;
+        g2.split_ws = base + l.split;
         g2.alpha = kNsC * kScaleB / (kScaleX * kScaleX);
         g2.src = A; g2.src_type = DT_F16; g2.src_ld = l.ldd; g2.src_batch = db; g2.beta = kNsB * kScaleB / kScaleX;
         g2.out = B; g2.out_type = DT_F16; g2.out_ld = l.ldd; g2.out_batch = db;
         rc = launch_gemm16(g2, st);
         if (rc != PCL_OK) return rc;
-        Gemm16Args g3{o.M, o.N, l.d, o.count, false, wide ? bm : Gemm16Operand{xh[cur], l.ld, xb, false},
-                      wide ? Gemm16Operand{xh[cur], l.ld, xb, true} : bm, GEMM16_LINEAR};
-        g3.alpha = 1.f / (kScaleX * kScaleB);
-        if (last) {
-            g3.src = xh[cur]; g3.src_type = DT_F16; g3.beta = kNsA / kScaleX;
+        Gemm16Args g3 = apply_args(o.count, o.M, o.N);
+        g3.a = wide ? bm : Gemm16Operand{xh[cur], l.ld, xb, false};
+        g3.b = wide ? Gemm16Operand{xh[cur], l.ld, xb, true} : bm;
+        g3.split_ws = base + l.split;
+        g3.src = xh[cur]; g3.src_type = DT_F16; g3.src_ld = l.ld; g3.src_batch = xb;
+        if (last) {                                           // to the caller's matrix
+            g3.epi = GEMM16_GENERAL;
+            g3.alpha = 1.f / (kScaleX * kScaleB); g3.beta = kNsA / kScaleX;
             g3.out = o.out; g3.out_type = o.type; g3.out_ld = o.N; g3.out_batch = long(o.M) * o.N;
             if (o.momentum) {
                 g3.update = true;
                 g3.keep = 1.f - o.lr * o.weight_decay;
                 g3.step = o.lr * sqrtf(o.M > o.N ? float(o.M) / float(o.N) : 1.f);
             }
-        } else {
-            g3.src = x; g3.src_type = DT_F32; g3.beta = kNsA;
-            if (it + 2 < o.steps) { g3.out = x; g3.out_type = DT_F32; g3.out_ld = l.ld; g3.out_batch = xb; }
-            g3.out2 = xh[cur ^ 1]; g3.out2_ld = l.ld; g3.out2_batch = xb; g3.scale2 = kScaleX;
+        } else {                                              // kScaleX X, in two planes (the second in place)
+            g3.alpha = 1.f / kScaleB; g3.beta = kNsA;
+            g3.src_lo = xl;
+            g3.out = xh[cur ^ 1]; g3.out_ld = l.ld; g3.out_batch = xb;
+            if (it + 2 < o.steps) g3.out_lo = xl;
         }
-        g3.src_ld = l.ld; g3.src_batch = xb;
         rc = launch_gemm16(g3, st);
         if (rc != PCL_OK) return rc;
         cur ^= 1;

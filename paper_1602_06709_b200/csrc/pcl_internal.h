@@ -18,6 +18,27 @@ namespace pcl {
 __device__ __forceinline__ float sigmoid_fast(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 #endif
 
+#ifdef __CUDACC__
+// Launch of a kernel that may start before the one in front of it has ended (see grid_dependency_wait() in pcl_ptx.cuh);
+// cluster > 1: in clusters of that many CTAs.
+template <class... P, class... A>
+int launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, unsigned cluster, const A&... args) {
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = grid;
+    lc.blockDim = block;
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&lc, kernel, P(args)...) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+}
+#endif
+
 // Kernel families, for launch counting and the optional per-kernel timing.
 enum KernelId {
     KID_TC_FPROP = 0, KID_TC_WGRAD, KID_GENERIC_FWD, KID_GENERIC_DGRAD, KID_GENERIC_WGRAD, KID_SGD, KID_REDUCE_SPLITS,
@@ -289,24 +310,30 @@ struct Gemm16Operand {
     long batch_stride;      // elements between the matrices of a batch, % 8 == 0
     bool mn_major;          // element (r, k) at ptr[k * ld + r] instead of ptr[r * ld + k]
 };
-enum Gemm16Epi { GEMM16_LINEAR = 0, GEMM16_STATS, GEMM16_DZ };
+enum Gemm16Epi {
+    GEMM16_GENERAL = 0,     // v = alpha * (alpha_dev ? *alpha_dev : 1) * acc + beta * src;  out = v, or, with `update`,
+                            // out = keep * out - step * v in place; any types, any alignment
+    GEMM16_STORE,           // (what GENERAL becomes where out can be stored through TMA as it is)
+    GEMM16_SYM,             // out = alpha * acc + beta * src in fp16, where the result is symmetric: only the tiles on and above
+                            // the diagonal are computed, the others are their mirror images
+    GEMM16_STEP,            // v = alpha * acc + beta * (src + src_lo / 2^11), out = fp16(v), out_lo = fp16((v - out) * 2^11)
+    GEMM16_PARTS,           // the reduction in k_parts parts, each part's fp32 sums to out + part * out_batch (batch = 1)
+    GEMM16_STATS, GEMM16_DZ // softmax over classes, see below
+};
 struct Gemm16Args {
     int M, N, K, batch;     // rows of A, rows of B (columns of the result), reduction length, matrices
     bool bf16;              // element type of both operands (else fp16)
     Gemm16Operand a, b;
     int epi;
-    // Only the tiles on and above the diagonal are computed and the others written as their mirror image (M == N, A = B or
-    // a product that is symmetric; GEMM16_LINEAR with a 16-bit `out` and no `out2`).
-    bool symmetric = false;
-    // GEMM16_LINEAR: v = alpha * (alpha_dev ? *alpha_dev : 1) * acc + beta * src;  out = v, or, with `update`,
-    // out = keep * out - step * v in place.  out2 (fp16) = scale2 * v.
     float alpha = 1.f;
     const float* alpha_dev = nullptr;
     float beta = 0.f;
     const void* src = nullptr; int src_type = DT_F32; long src_ld = 0, src_batch = 0;
+    const void* src_lo = nullptr;            // laid out like src
     void* out = nullptr; int out_type = DT_F32; long out_ld = 0, out_batch = 0;
-    void* out2 = nullptr; long out2_ld = 0, out2_batch = 0; float scale2 = 1.f;
+    void* out_lo = nullptr;                  // laid out like out; may be null (then it is not written) or src_lo
     bool update = false; float keep = 1.f, step = 0.f;
+    int k_parts = 0;
     // GEMM16_STATS / GEMM16_DZ: z[r][c] = acc + bias[c]; the columns are classes col0 .. col0 + N - 1.
     const void* bias = nullptr;         // [N], type of the operands
     const int* labels = nullptr;        // [M]
@@ -317,8 +344,15 @@ struct Gemm16Args {
     // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0
     const float* lse = nullptr;
     const float* row_scale = nullptr;
+    // Scratch of gemm16_split_ws_bytes(), 256-byte aligned, or null (then nothing is split).
+    void* split_ws = nullptr;
 };
-int gemm16_stats_parts(int M, int N);   // float2 entries per row that STATS writes
+int gemm16_stats_parts(const Gemm16Args& a);      // float2 entries per row that STATS writes
+// Bytes of split_ws with which launch_gemm16(a) would split reductions (0: it would not).  Its first kGemm16CounterBytes have
+// to be zero before the first launch that is given it (each launch leaves them zero).
+constexpr size_t kGemm16CounterBytes = 8192;
+size_t gemm16_split_ws_bytes(const Gemm16Args& a);
+int gemm16_parts(const Gemm16Args& a);            // parts in which PARTS should cut the reduction to fill the GPU (1: none)
 int launch_gemm16(const Gemm16Args& a, cudaStream_t st);
 
 // ---- embedding (embedding.cu) -------------------------------------------------

@@ -12,6 +12,12 @@ __device__ __forceinline__ uint32_t smem_u32(const void* p) {
     return static_cast<uint32_t>(__cvta_generic_to_shared(p));
 }
 
+// Programmatic dependent launch: a kernel launched through launch_chained() may start before the kernel in front of it in the
+// stream has ended.  Every one of its threads passes grid_dependency_wait() before it touches global memory: from there on the
+// previous kernel has ended and its writes are visible.
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependents_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // ----------------------------------------------------------------- mbarrier
 __device__ __forceinline__ void mbar_init(uint64_t* bar, uint32_t count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count) : "memory");
@@ -504,6 +510,18 @@ __device__ __forceinline__ void umma_kstep_f16(uint32_t d_tmem, uint32_t a_lo, u
     else PCL_UMMA_KSTEP16_BODY("1");
 }
 #undef PCL_UMMA_KSTEP16_BODY
+// One K = 16 MMA of 16-bit operands.
+template <bool kPair>
+__device__ __forceinline__ void umma_f16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (kPair)
+        asm volatile("{\n\t.reg .pred p, pe;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|pe, 0xffffffff;\n\t"
+                     "@pe tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, pe;\n\tsetp.ne.b32 p, %4, 0;\n\telect.sync _|pe, 0xffffffff;\n\t"
+                     "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
 // The same with a K-major A (k-block = 2 units) and the k-block stride of B in a register (2: K-major, 64: MN-major).
 // `nsl` (1..4): how many of the four K = 8 slices are issued; the rest are known to multiply zeros only (few-channel
 // layers pack fewer than 32 live reduction elements into a block) and are skipped by a guard predicate.

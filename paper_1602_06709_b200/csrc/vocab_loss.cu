@@ -9,6 +9,7 @@
 #include <math.h>
 
 #include "pcl_internal.h"
+#include "pcl_ptx.cuh"
 
 namespace pcl {
 
@@ -17,9 +18,11 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A piece of dz (or, with fp32 operands, of the logits) takes at most this much workspace.
 constexpr size_t kPieceBytes = size_t(256) << 20;
+// Nor has a piece of dz more classes than this: dx sums over them in one accumulator, and the tensor core's additions
+// truncate (the pieces are added in fp32, rounded).
+constexpr int kMostClasses = 16384;
 
-__device__ __forceinline__ float elem(const void* p, int type, size_t i) {
-    if (type == DT_F32) return static_cast<const float*>(p)[i];
+__device__ __forceinline__ float elem16(const void* p, int type, size_t i) {
     if (type == DT_BF16) return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
     return __half2float(static_cast<const __half*>(p)[i]);
 }
@@ -27,15 +30,16 @@ __device__ __forceinline__ float elem(const void* p, int type, size_t i) {
 // Rows whose length is no multiple of 8 elements cannot be read by TMA (16-byte strides): they are copied to padded rows.
 __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restrict__ src, uint16_t* __restrict__ dst, long rows,
                                                        int C, int ldc) {
+    grid_dependency_wait();
+    grid_dependents_launch();
     for (long r = blockIdx.x; r < rows; r += gridDim.x)
         for (int c = threadIdx.x; c < ldc; c += blockDim.x) dst[r * ldc + c] = c < C ? src[r * C + c] : uint16_t(0);
 }
 int launch_pad_rows(const void* src, void* dst, long rows, int C, int ldc, cudaStream_t st) {
     LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(rows) * C, st);
     const long cap = long(device_sm_count()) * 16;
-    pad_rows_kernel<<<int(rows < cap ? rows : cap), 256, 0, st>>>(static_cast<const uint16_t*>(src), static_cast<uint16_t*>(dst),
-                                                                  rows, C, ldc);
-    return cudaGetLastError() == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    return launch_chained(pad_rows_kernel, dim3(unsigned(rows < cap ? rows : cap)), dim3(256), 0, st, 1, static_cast<const uint16_t*>(src),
+                          static_cast<uint16_t*>(dst), rows, C, ldc);
 }
 
 // (max, sum of exp(z - max)) pairs of disjoint sets of classes, joined.  A set without a finite logit is (-inf, 0).
@@ -70,6 +74,8 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const float2* __restrict
                                                         const float* __restrict__ label_z, const int* __restrict__ labels,
                                                         int ignore_label, int N, int K, float* __restrict__ row_loss,
                                                         float* __restrict__ lse, unsigned int* status) {
+    grid_dependency_wait();
+    grid_dependents_launch();
     const int lane = threadIdx.x & 31;
     for (int n = blockIdx.x * 8 + (threadIdx.x >> 5); n < N; n += gridDim.x * 8) {
         float m = -INFINITY, s = 0.f;
@@ -82,11 +88,48 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const float2* __restrict
     }
 }
 
+// The same from the parts of the products themselves (reductions that are cut to fill the GPU): one block per row adds them up,
+// with the bias, to the logits.
+__device__ __forceinline__ float2 block_join(float m, float s) {
+    __shared__ float ms[8], ss[8];
+    join_warp(m, s);
+    if ((threadIdx.x & 31) == 0) { ms[threadIdx.x >> 5] = m; ss[threadIdx.x >> 5] = s; }
+    __syncthreads();
+    m = ms[0]; s = ss[0];
+    for (int i = 1; i < 8; ++i) join(m, s, ms[i], ss[i]);
+    __syncthreads();
+    return make_float2(m, s);
+}
+__global__ void __launch_bounds__(256) loss_parts_kernel(const float* __restrict__ z, int parts, size_t part_step, int ld,
+                                                         const void* __restrict__ bias, int type, const int* __restrict__ labels,
+                                                         int ignore_label, int N, int K, float* __restrict__ label_z,
+                                                         float* __restrict__ row_loss, float* __restrict__ lse, unsigned int* status) {
+    grid_dependency_wait();
+    grid_dependents_launch();
+    for (int n = blockIdx.x; n < N; n += gridDim.x) {
+        const int label = labels[n];
+        float m = -INFINITY, s = 0.f;
+        for (int k = threadIdx.x; k < K; k += 256) {
+            const float* src = z + size_t(n) * ld + k;
+            float v = 0.f;
+#pragma unroll 4
+            for (int p = 0; p < parts; ++p) v += src[p * part_step];
+            if (bias) v += elem16(bias, type, k);
+            if (k == label) label_z[n] = v;
+            join(m, s, v, v == -INFINITY ? 0.f : 1.f);
+        }
+        const float2 r = block_join(m, s);
+        if (threadIdx.x == 0) finish_row(n, r.x, r.y, labels, ignore_label, K, label_z, row_loss, lse, status);
+    }
+}
+
 // Mean over the rows that count (fixed order; 0 if none does).
 __global__ void __launch_bounds__(1024) loss_mean_kernel(const float* __restrict__ row_loss, const int* __restrict__ labels,
                                                          int ignore_label, int N, float* __restrict__ loss) {
     __shared__ double sums[32];
     __shared__ int counts[32];
+    grid_dependency_wait();
+    grid_dependents_launch();
     double sum = 0.0;
     int count = 0;
     for (int n = threadIdx.x; n < N; n += 1024) {
@@ -108,9 +151,13 @@ __global__ void __launch_bounds__(1024) loss_mean_kernel(const float* __restrict
 // of rows lies far below; bf16 has the exponents of fp32.
 __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__ labels, int ignore_label,
                                                          const float* __restrict__ row_grad, int N, int f16,
-                                                         float* __restrict__ row_scale, float* __restrict__ alpha) {
+                                                         float* __restrict__ row_scale, float* __restrict__ alpha, int* counters) {
     __shared__ int counts[32];
     __shared__ float tops[32];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    if (counters)                                         // of the products' split workspace
+        for (int i = threadIdx.x; i < int(kGemm16CounterBytes / 4); i += 1024) counters[i] = 0;
     int count = 0;
     float top = 0.f;
     for (int n = threadIdx.x; n < N; n += 1024)
@@ -139,36 +186,41 @@ __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__
     if (threadIdx.x == 0) alpha[0] = row_grad ? 1.f / up : 1.f / (up * float(count > 0 ? count : 1));
 }
 
-// db[k] = alpha * sum_n dz[n][k].  32 columns x 8 row lanes per block, rows in a fixed order.
-template <class T>
-__global__ void __launch_bounds__(256) dz_colsum_kernel(const T* __restrict__ dz, int N, int P, int ld, const float* alpha,
-                                                        T* __restrict__ db) {
-    __shared__ float sums[8][33];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const int k = blockIdx.x * 32 + lane;
-    float s = 0.f;
-    if (k < P)
-        for (int n = w; n < N; n += 8) s += float(dz[size_t(n) * ld + k]);
-    sums[w][lane] = s;
+// db[k] = alpha * sum_n dz[n][k].  A block takes 64 columns, eight at a time per thread (rows of dz are padded to 64), and 32 rows
+// at once; the 32 sums of a column are added in order.
+__global__ void __launch_bounds__(256) dz_colsum_kernel(const uint16_t* __restrict__ dz, int N, int P, int ld, int type, const float* alpha,
+                                                        void* __restrict__ db) {
+    __shared__ float sums[32][65];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const int c8 = (threadIdx.x & 7) * 8, r0 = threadIdx.x >> 3;
+    const uint16_t* src = dz + blockIdx.x * 64 + c8;
+    float s[8] = {};
+#pragma unroll 4
+    for (int n = r0; n < N; n += 32) {
+        const uint4 v = *reinterpret_cast<const uint4*>(src + size_t(n) * ld);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+            s[2 * i] += type == DT_BF16 ? __uint_as_float(w[i] << 16) : f.x;
+            s[2 * i + 1] += type == DT_BF16 ? __uint_as_float(w[i] & 0xffff0000u) : f.y;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[r0][c8 + i] = s[i];
     __syncthreads();
-    if (w == 0 && k < P) {
-        s = 0.f;
-        for (int i = 0; i < 8; ++i) s += sums[i][lane];
-        db[k] = T(s * alpha[0]);
+    const int k = blockIdx.x * 64 + threadIdx.x;
+    if (threadIdx.x < 64 && k < P) {
+        float total = 0.f;
+        for (int i = 0; i < 32; ++i) total += sums[i][threadIdx.x];
+        total *= alpha[0];
+        if (type == DT_BF16) static_cast<__nv_bfloat16*>(db)[k] = __float2bfloat16_rn(total);
+        else static_cast<__half*>(db)[k] = __float2half_rn(total);
     }
 }
 
 // ---- fp32 operands: a piece of the logits is in the workspace
-__device__ __forceinline__ float2 block_join(float m, float s) {
-    __shared__ float ms[8], ss[8];
-    join_warp(m, s);
-    if ((threadIdx.x & 31) == 0) { ms[threadIdx.x >> 5] = m; ss[threadIdx.x >> 5] = s; }
-    __syncthreads();
-    m = ms[0]; s = ss[0];
-    for (int i = 1; i < 8; ++i) join(m, s, ms[i], ss[i]);
-    __syncthreads();
-    return make_float2(m, s);
-}
 // one block per row; state[n] = (max, sum) over the pieces so far
 __global__ void __launch_bounds__(256) piece_stats_kernel(const float* __restrict__ z, int N, int P, int col0,
                                                           const int* __restrict__ labels, float2* __restrict__ state,
@@ -222,14 +274,40 @@ int stage_classes(int C, int K) {
     return p < size_t(K) ? int(p) : K;
 }
 
-struct Layout { size_t part, label_z, row_scale, alpha, xs, wst, dz, dx, fc, total; int piece, parts, ldc, ldp; };
+// The products, with everything their tiling depends on; P classes of a piece.
+Gemm16Args stats_args(int N, int C, int P, bool bf16) {
+    Gemm16Args a{N, P, C, 1, bf16, {}, {}, GEMM16_STATS};
+    a.split_ws = reinterpret_cast<void*>(256);               // (until the workspace is known)
+    return a;
+}
+Gemm16Args dz_args(int N, int C, int P, bool bf16) {
+    Gemm16Args a = stats_args(N, C, P, bf16);
+    a.epi = GEMM16_DZ;
+    return a;
+}
+Gemm16Args dx_args(int N, int C, int P, bool bf16) {
+    Gemm16Args a{N, C, P, 1, bf16, {}, {}, GEMM16_GENERAL};
+    a.split_ws = reinterpret_cast<void*>(256);
+    return a;
+}
+Gemm16Args dw_args(int N, int C, int P, bool bf16) {
+    Gemm16Args a{P, C, N, 1, bf16, {}, {}, GEMM16_GENERAL};
+    a.split_ws = reinterpret_cast<void*>(256);
+    return a;
+}
+
+struct Layout { size_t part, label_z, row_scale, alpha, xs, wst, dz, dx, fc, split, split_bytes, total; int piece, parts, k_parts, ldc, ldp; };
 Layout layout(int N, int C, int K, int type, bool backward) {
     Layout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
     l.ldc = int(align_up(C, 8));
-    const bool stage = type != DT_F32 && C % 8 != 0;
+    const bool stage = type != DT_F32 && C % 8 != 0, bf16 = type == DT_BF16;
     l.alpha = take(4);
+    auto split = [&](const Gemm16Args& a) {
+        const size_t b = gemm16_split_ws_bytes(a);
+        if (b > l.split_bytes) l.split_bytes = b;
+    };
     if (type == DT_F32) {
         l.piece = piece_classes(N, K, 4);
         if (backward) l.row_scale = take(size_t(N) * 4);
@@ -247,19 +325,28 @@ Layout layout(int N, int C, int K, int type, bool backward) {
     } else if (!backward) {
         l.piece = stage ? stage_classes(C, K) : K;
         l.label_z = take(size_t(N) * 4);
+        if (l.piece == K) l.k_parts = gemm16_parts(stats_args(N, C, K, bf16));
+        if (l.k_parts > 1) {
+            l.ldp = int(align_up(K, 32));
+            l.dz = take(size_t(l.k_parts) * N * l.ldp * 4);
+        }
         const int last = K - (K - 1) / l.piece * l.piece;
-        l.parts = (K - 1) / l.piece * gemm16_stats_parts(N, l.piece) + gemm16_stats_parts(N, last);
+        l.parts = (K - 1) / l.piece * gemm16_stats_parts(stats_args(N, C, l.piece, bf16)) + gemm16_stats_parts(stats_args(N, C, last, bf16));
         l.part = take(size_t(N) * l.parts * 8);
         if (stage) { l.xs = take(size_t(N) * l.ldc * 2); l.wst = take(size_t(l.piece) * l.ldc * 2); }
     } else {
         l.piece = piece_classes(N, K, 2);
+        if (l.piece > kMostClasses) l.piece = kMostClasses;
         if (stage && l.piece > stage_classes(C, K)) l.piece = stage_classes(C, K);
         l.ldp = int(align_up(l.piece, 64));
         l.row_scale = take(size_t(N) * 4);
         l.dz = take(size_t(N) * l.ldp * 2);
         if (l.piece < K) l.dx = take(size_t(N) * C * 4);
         if (stage) { l.xs = take(size_t(N) * l.ldc * 2); l.wst = take(size_t(l.piece) * l.ldc * 2); }
+        const int last = K - (K - 1) / l.piece * l.piece;
+        for (int p : {l.piece, last}) { split(dz_args(N, C, p, bf16)); split(dx_args(N, C, p, bf16)); split(dw_args(N, C, p, bf16)); }
     }
+    l.split = take(l.split_bytes);
     l.total = at;
     return l;
 }
@@ -277,9 +364,10 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
     unsigned int* status = device_status_ptr();
     if (!status) return PCL_ERR_CUDA;
     int rc = PCL_OK, parts = 0, part_ld = l.parts;
+    bool joined = false;                                      // lse and row_loss are written
     if (type == DT_F32) {
         float* z = reinterpret_cast<float*>(base + l.dz);
-        const size_t fc_bytes = l.total - l.fc;
+        const size_t fc_bytes = l.split - l.fc;
         for (int p0 = 0; p0 < K; p0 += l.piece) {
             const int P = K - p0 < l.piece ? K - p0 : l.piece;
             rc = pcl_fc_fwd(N, C, P, static_cast<const float*>(x), static_cast<const float*>(w) + size_t(p0) * C,
@@ -306,26 +394,38 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
                 if (rc != PCL_OK) return rc;
                 wp = base + l.wst;
             }
-            Gemm16Args a{N, P, C, 1, type == DT_BF16, {xs, l.ldc, 0, false}, {wp, l.ldc, 0, false}, GEMM16_STATS};
+            Gemm16Args a = stats_args(N, C, P, type == DT_BF16);
+            a.a = {xs, l.ldc, 0, false}; a.b = {wp, l.ldc, 0, false};
+            a.split_ws = nullptr;
+            if (l.k_parts > 1) {
+                a.epi = GEMM16_PARTS; a.k_parts = l.k_parts;
+                a.out = base + l.dz; a.out_ld = l.ldp; a.out_batch = long(N) * l.ldp;
+                rc = launch_gemm16(a, st);
+                if (rc != PCL_OK) return rc;
+                LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(N) * K * l.k_parts, st);
+                rc = launch_chained(loss_parts_kernel, dim3(row_blocks(N)), dim3(256), 0, st, 1, reinterpret_cast<const float*>(base + l.dz),
+                                    l.k_parts, size_t(N) * l.ldp, l.ldp, bias, type, labels, ignore_label, N, K, label_z, row_loss, lse,
+                                    status);
+                if (rc != PCL_OK) return rc;
+                joined = true;
+                break;
+            }
             a.bias = bias ? static_cast<const uint16_t*>(bias) + p0 : nullptr;
             a.labels = labels; a.col0 = p0; a.part = part + parts; a.part_ld = part_ld; a.label_z = label_z;
             rc = launch_gemm16(a, st);
             if (rc != PCL_OK) return rc;
-            parts += gemm16_stats_parts(N, P);
+            parts += gemm16_stats_parts(a);
         }
     }
-    {
+    if (!joined) {
         LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N) * parts, st);
         const int blocks = (N + 7) / 8, cap = device_sm_count() * 8;
-        loss_rows_kernel<<<blocks < cap ? blocks : cap, 256, 0, st>>>(part, part_ld, parts, label_z, labels, ignore_label, N, K,
-                                                                      row_loss, lse, status);
+        rc = launch_chained(loss_rows_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, 1, part, part_ld, parts, label_z, labels,
+                            ignore_label, N, K, row_loss, lse, status);
+        if (rc != PCL_OK) return rc;
     }
-    if ((rc = launched()) != PCL_OK) return rc;
-    {
-        LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N), st);
-        loss_mean_kernel<<<1, 1024, 0, st>>>(row_loss, labels, ignore_label, N, loss);
-    }
-    return launched();
+    LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N), st);
+    return launch_chained(loss_mean_kernel, dim3(1), dim3(1024), 0, st, 1, row_loss, labels, ignore_label, N, loss);
 }
 
 int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const void* w, const void* bias, const int* labels,
@@ -338,12 +438,13 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
     int rc = PCL_OK;
     {
         LaunchScope scope(KID_VOCAB_LOSS, 12.0 * double(N), st);
-        grad_rows_kernel<<<1, 1024, 0, st>>>(labels, ignore_label, row_grad, N, type == DT_F16, row_scale, alpha);
+        rc = launch_chained(grad_rows_kernel, dim3(1), dim3(1024), 0, st, 1, labels, ignore_label, row_grad, N, int(type == DT_F16), row_scale,
+                            alpha, l.split_bytes ? reinterpret_cast<int*>(base + l.split) : nullptr);
     }
-    if ((rc = launched()) != PCL_OK) return rc;
+    if (rc != PCL_OK) return rc;
     if (type == DT_F32) {
         float* z = reinterpret_cast<float*>(base + l.dz);
-        const size_t fc_bytes = (l.piece < K ? l.dx : l.total) - l.fc;
+        const size_t fc_bytes = (l.piece < K ? l.dx : l.split) - l.fc;
         for (int p0 = 0; p0 < K; p0 += l.piece) {
             const int P = K - p0 < l.piece ? K - p0 : l.piece;
             const float* wp = static_cast<const float*>(w) + size_t(p0) * C;
@@ -385,7 +486,9 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
             if (rc != PCL_OK) return rc;
             wp = base + l.wst;
         }
-        Gemm16Args z{N, P, C, 1, bf16, {xs, l.ldc, 0, false}, {wp, l.ldc, 0, false}, GEMM16_DZ};
+        Gemm16Args z = dz_args(N, C, P, bf16);
+        z.a = {xs, l.ldc, 0, false}; z.b = {wp, l.ldc, 0, false};
+        z.split_ws = base + l.split;
         z.bias = bias ? static_cast<const uint16_t*>(bias) + p0 : nullptr;
         z.labels = labels; z.col0 = p0; z.lse = lse; z.row_scale = row_scale;
         z.out = dz; z.out_type = type; z.out_ld = l.ldp;
@@ -393,16 +496,14 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
         if (rc != PCL_OK) return rc;
         if (dbias) {
             LaunchScope scope(KID_VOCAB_LOSS, 2.0 * double(N) * P, st);
-            if (bf16)
-                dz_colsum_kernel<__nv_bfloat16><<<(P + 31) / 32, 256, 0, st>>>(reinterpret_cast<const __nv_bfloat16*>(dz), N, P, l.ldp, alpha,
-                                                                               static_cast<__nv_bfloat16*>(dbias) + p0);
-            else
-                dz_colsum_kernel<__half><<<(P + 31) / 32, 256, 0, st>>>(reinterpret_cast<const __half*>(dz), N, P, l.ldp, alpha,
-                                                                        static_cast<__half*>(dbias) + p0);
-            if ((rc = launched()) != PCL_OK) return rc;
+            rc = launch_chained(dz_colsum_kernel, dim3((P + 63) / 64), dim3(256), 0, st, 1, dz, N, P, l.ldp, type, alpha,
+                                static_cast<uint16_t*>(dbias) + p0);
+            if (rc != PCL_OK) return rc;
         }
         if (dx) {
-            Gemm16Args g{N, C, P, 1, bf16, {dz, l.ldp, 0, false}, {wp, l.ldc, 0, true}, GEMM16_LINEAR};
+            Gemm16Args g = dx_args(N, C, P, bf16);
+            g.a = {dz, l.ldp, 0, false}; g.b = {wp, l.ldc, 0, true};
+            g.split_ws = base + l.split;
             const bool last = p0 + l.piece >= K;
             g.alpha_dev = alpha;
             if (p0 > 0) { g.src = dx_acc; g.src_type = DT_F32; g.src_ld = C; g.beta = 1.f; }
@@ -410,7 +511,9 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
             rc = launch_gemm16(g, st);
             if (rc != PCL_OK) return rc;
         }
-        Gemm16Args g{P, C, N, 1, bf16, {dz, l.ldp, 0, true}, {xs, l.ldc, 0, true}, GEMM16_LINEAR};
+        Gemm16Args g = dw_args(N, C, P, bf16);
+        g.a = {dz, l.ldp, 0, true}; g.b = {xs, l.ldc, 0, true};
+        g.split_ws = base + l.split;
         g.alpha_dev = alpha;
         g.out = static_cast<uint16_t*>(dw) + size_t(p0) * C; g.out_type = type; g.out_ld = C;
         rc = launch_gemm16(g, st);

@@ -66,7 +66,7 @@ def assert_close(got, ref, t):
 
 @pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("count,M,N", [(1, 1, 1), (1, 1, 50), (2, 50, 1), (1, 7, 5), (3, 16, 33), (1, 33, 100), (1, 100, 33),
-                                       (2, 128, 128), (1, 129, 257), (1, 300, 1000), (1, 1000, 300), (1, 640, 640)])
+                                       (2, 128, 128), (1, 129, 257), (1, 300, 1000), (1, 1000, 300), (1, 640, 640), (4, 260, 520), (1, 1500, 1412)])
 def test_direction(t, count, M, N):
     g = guarded((count, M, N), t, fill=0)
     g.copy_(spectrum(count, M, N, "gauss", M + N))

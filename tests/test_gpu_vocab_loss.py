@@ -107,7 +107,8 @@ class Case:
 
 
 SIZES = [(1, 8, 1), (1, 64, 2), (2, 72, 257), (7, 33, 100), (128, 64, 128), (129, 65, 129), (130, 136, 300), (256, 256, 1000),
-         (300, 520, 2049), (1, 1024, 9000), (64, 24, 20000), (513, 7, 511)]
+         (300, 520, 2049), (1, 1024, 9000), (64, 24, 20000), (513, 7, 511),
+         (256, 4096, 1000), (40, 2010, 300), (3, 1100, 17), (1000, 1032, 4000)]
 
 
 @pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
@@ -134,8 +135,9 @@ def test_given_row_gradients(t, scale):
 
 
 @pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
-def test_many_row_tiles_run_as_pairs(t):
-    c = Case(2500, 200, 3100, t, True, 0.1, seed=8)
+@pytest.mark.parametrize("N,C,K", [(2500, 200, 3100), (2500, 520, 4900), (1024, 2048, 8192)])
+def test_many_row_tiles_run_as_pairs(t, N, C, K):
+    c = Case(N, C, K, t, True, 0.1, seed=8)
     c.forward()
     c.backward()
     c.check()
