@@ -384,7 +384,8 @@ int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const voi
 int pcl_last_device_status(void* cuda_stream);
 /* Which wait gave up when pcl_last_device_status() last returned PCL_ERR_DEVICE_TIMEOUT (0 if it never did):
  * 0x101 producer waiting for a free slot, 0x102 MMA issuer waiting for operands, 0x103 MMA issuer waiting for a
- * free accumulator, 0x104 epilogue waiting for an accumulator, 0x106 MMA issuer waiting for its turn.  Diagnostic. */
+ * free accumulator, 0x104 epilogue waiting for an accumulator, 0x106 MMA issuer waiting for its turn, 0x107 a kernel of
+ * several products waiting for all of its CTAs.  Diagnostic. */
 unsigned int pcl_last_wait_code(void);
 
 /* Number of kernels this library has launched since it was loaded. */

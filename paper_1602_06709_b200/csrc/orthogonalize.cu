@@ -8,12 +8,15 @@
 // rounding is passed on by the polynomial's derivative (which is small at 1) instead of by B alone.  Relative error of the
 // result (2-norm) 3e-4 .. 1.6e-3 on random, decaying and nearly low-rank spectra, where bf16 iterates give 1e-2 .. 2e-1.
 // A and A A are symmetric: the tiles below the diagonal are copies of those above it.
+//
+// All 3 * steps products run in ONE cooperative launch (the roles of the 16-bit GEMM, see tc_gemm16.cu, one product after
+// another) with a barrier of all CTAs between them: a launch of its own costs every product its set-up and the fetching
+// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 118 -> 75 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
 
-#include "pcl_internal.h"
-#include "pcl_ptx.cuh"
+#include "gemm16_device.cuh"
 
 namespace pcl {
 
@@ -61,7 +64,7 @@ struct StageArgs {
     __half* xh;                 // [count][M][ld] X0 * kScaleX
     __half* xl;                 // what rounding left, times 2^11 (null: not needed)
     int M, N, ld;
-    int* counters;              // of the products' split workspace, to be zeroed (null: none)
+    int* counters;              // of the products, to be zeroed
 };
 
 // Sum of squares of U (64-bit: the squares of a gradient leave the range of fp32), and the momentum update.
@@ -107,7 +110,7 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
     grid_dependents_launch();
     for (int i = threadIdx.x; i < a.parts; i += 256) sum += a.part[size_t(blockIdx.y) * kMaxNormBlocks + i];
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if (a.counters && blockIdx.x == 0 && blockIdx.y == 0)
+    if (blockIdx.x == 0 && blockIdx.y == 0)
         for (int i = threadIdx.x; i < int(kGemm16CounterBytes / 4); i += 256) a.counters[i] = 0;
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
     __syncthreads();
@@ -153,23 +156,34 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
 }
 
 // The three products of a step, with everything their tiling depends on.
-Gemm16Args gram_args(int count, int M, int N) {
+Gemm16Args gram_args(int count, int M, int N, int form) {
     const int d = M < N ? M : N;
     Gemm16Args a{d, d, M < N ? N : M, count, false, {}, {}, GEMM16_SYM};
+    a.form = form;
     a.split_ws = reinterpret_cast<void*>(256);               // (until the workspace is known)
     return a;
 }
-Gemm16Args square_args(int count, int M, int N) {
+Gemm16Args square_args(int count, int M, int N, int form) {
     const int d = M < N ? M : N;
-    return gram_args(count, d, d);
+    return gram_args(count, d, d, form);
 }
-Gemm16Args apply_args(int count, int M, int N) {
+Gemm16Args apply_args(int count, int M, int N, int form) {
     Gemm16Args a{M, N, M < N ? M : N, count, false, {}, {}, GEMM16_STEP};
+    a.form = form;
     a.split_ws = reinterpret_cast<void*>(256);
     return a;
 }
+// CTA pairs or single CTAs for all three.
+int ortho_form(int count, int M, int N) {
+    double time[2];
+    for (int f = 0; f < 2; ++f) {
+        const int form = f == 0 ? GEMM16_FORM_PAIR : GEMM16_FORM_SINGLE;
+        time[f] = plan16(gram_args(count, M, N, form)).time + plan16(square_args(count, M, N, form)).time + plan16(apply_args(count, M, N, form)).time;
+    }
+    return time[0] <= time[1] ? GEMM16_FORM_PAIR : GEMM16_FORM_SINGLE;
+}
 
-struct OrthoLayout { size_t part, xl, xh[2], a, b, split, split_bytes, total; int ld, d, ldd; };
+struct OrthoLayout { size_t part, xl, xh[2], a, b, counters, total; int ld, d, ldd, form; };
 OrthoLayout ortho_layout(int count, int M, int N) {
     OrthoLayout l{};
     size_t at = 0;
@@ -177,18 +191,157 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     l.ld = int(align_up(N, 8));
     l.d = M < N ? M : N;
     l.ldd = int(align_up(l.d, 8));
+    l.form = ortho_form(count, M, N);
     l.part = take(size_t(count) * kMaxNormBlocks * 8);
     l.xl = take(size_t(count) * M * l.ld * 2);
     for (size_t& o : l.xh) o = take(size_t(count) * M * l.ld * 2);
     l.a = take(size_t(count) * l.d * l.ldd * 2);
     l.b = take(size_t(count) * l.d * l.ldd * 2);
-    for (const Gemm16Args& a : {gram_args(count, M, N), square_args(count, M, N), apply_args(count, M, N)}) {
+    size_t split = kGemm16CounterBytes;
+    for (const Gemm16Args& a : {gram_args(count, M, N, l.form), square_args(count, M, N, l.form), apply_args(count, M, N, l.form)}) {
         const size_t b = gemm16_split_ws_bytes(a);
-        if (b > l.split_bytes) l.split_bytes = b;
+        if (b > split) split = b;
     }
-    l.split = take(l.split_bytes);
+    l.counters = take(split);
     l.total = at;
     return l;
+}
+
+struct OrthoParams {
+    CUtensorMap xk[2], xmn[2], a, b;             // operands: X K-major and MN-major, A, B
+    CUtensorMap x_out[2], a_out, b_out, lo_out;  // results, and what is added to them
+    Gemm16Params gram, square, step, final;
+    const void* x[2];
+    void* out;
+    int steps, wide;
+    unsigned* barrier;                           // CTAs that have ended a product, summed over the products
+};
+
+// All CTAs have ended product `done` (0-based): called by the producing warp of each when it has issued its own copies.  Its
+// epilogue warps have completed their stores (phase_end_bar); the counter is waited for no longer than the library's wait
+// limit.  Then this CTA's epilogue warps may go on (phase_go_bar).
+__device__ __forceinline__ bool ortho_barrier(Gemm16Ctx& c, const OrthoParams& o, int done) {
+    if (!bounded_wait_addr_warp(smem_u32(&c.sh->phase_end_bar), done & 1, &c.sh->abort_flag, c.status, WAIT_GRID)) return false;
+    int ok = 1;
+    if (c.lane == 0) {
+        __threadfence();
+        atomicAdd(o.barrier, 1u);
+        const unsigned want = gridDim.x * unsigned(done + 1);
+        unsigned long long t0 = 0, limit = 0;
+        for (unsigned spin = 0;; ++spin) {
+            unsigned v;
+            asm volatile("ld.acquire.gpu.u32 %0, [%1];" : "=r"(v) : "l"(o.barrier) : "memory");
+            if (int(v - want) >= 0) break;
+            if ((spin & 63u) == 63u) {
+                const unsigned long long now = global_nanos();
+                if (t0 == 0) { t0 = now; limit = wait_limit_nanos(c.status); }
+                else if (now - t0 > limit) {
+                    ok = 0;
+                    *static_cast<volatile uint32_t*>(&c.sh->abort_flag) = 1u;
+                    atomicCAS(c.status, 0u, unsigned(WAIT_GRID));
+                    break;
+                }
+            }
+        }
+        if (ok) mbar_arrive(&c.sh->phase_go_bar);
+    }
+    ok = __shfl_sync(0xffffffffu, ok, 0);
+    asm volatile("fence.proxy.async;" ::: "memory");          // (the products' results are read through TMA)
+    return ok != 0;
+}
+
+template <bool kPair>
+__global__ void __launch_bounds__(kThreads16, 1) orthogonalize_kernel(const __grid_constant__ OrthoParams o) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ Gemm16Shared sh;
+    Gemm16Ctx c = gemm16_begin<kPair>(&sh, smem_raw, o.gram.status, kStages16 - 1);
+    const int products = 3 * o.steps;
+    if (c.warp == 0) {
+        bool ok = true;
+        for (int i = 0; i < products && ok; ++i) {
+            const int step = i / 3, kind = i - 3 * step, cur = step & 1;
+            const Gemm16Params& p = kind == 0 ? o.gram : kind == 1 ? o.square : o.step;
+            const Item16 tile = decode_item(p, c.first < p.items ? c.first : 0);
+            if (i > 0) ok = ortho_barrier(c, o, i - 1);
+            if (!ok) break;
+            if (kind == 2 && o.wide) ok = produce_items<kPair, false, true>(c, p, tile, &o.b, &o.xmn[cur]);
+            else if (kind == 0 && !o.wide) ok = produce_items<kPair, true, true>(c, p, tile, &o.xmn[cur], &o.xmn[cur]);
+            else
+                ok = produce_items<kPair, false, false>(c, p, tile, kind == 1 ? &o.a : &o.xk[cur],
+                                                        kind == 1 ? &o.a : kind == 0 ? &o.xk[cur] : &o.b);
+        }
+        if (!ok) drain_producer(c);
+    } else if (c.warp == 1) {
+        if (c.pair_rank == 0) {
+            bool ok = true;
+            for (int i = 0; i < products && ok; ++i) {
+                const int kind = i % 3;
+                if (kind == 2 && o.wide) ok = issue_items<kPair, false, true, false>(c, o.step);
+                else if (kind == 0 && !o.wide) ok = issue_items<kPair, true, true, false>(c, o.gram);
+                else ok = issue_items<kPair, false, false, false>(c, kind == 0 ? o.gram : kind == 1 ? o.square : o.step);
+            }
+        }
+        __syncwarp();
+    } else {
+        bool ok = true;
+        for (int i = 0; i < products && ok; ++i) {
+            const int step = i / 3, kind = i - 3 * step, cur = step & 1;
+            if (i > 0)      // (what is added to the product comes from the products before)
+                ok = bounded_wait_warp(&sh.phase_go_bar, (i - 1) & 1, &sh.abort_flag, c.status, WAIT_GRID);
+            if (!ok) break;
+            if (kind < 2)
+                ok = finish_items<kPair, GEMM16_SYM, false>(c, kind == 0 ? o.gram : o.square, kind == 0 ? &o.a_out : &o.b_out, nullptr,
+                                                            nullptr, nullptr, kind == 0 ? nullptr : &o.a_out);
+            else if (step + 1 < o.steps)
+                ok = finish_items<kPair, GEMM16_STEP, false>(c, o.step, &o.x_out[cur ^ 1], step + 2 < o.steps ? &o.lo_out : nullptr, nullptr, nullptr,
+                                                             &o.x_out[cur], &o.lo_out);
+            else
+                ok = finish_items<kPair, GEMM16_FINAL, false>(c, o.final, nullptr, nullptr, o.x[cur], o.out);
+            __syncwarp();
+            if (c.lane == 0) {
+                bulk_wait_group0();
+                asm volatile("fence.proxy.async;" ::: "memory");
+                mbar_arrive(&sh.phase_end_bar);
+            }
+        }
+        if (!ok) drain_fetch(c);
+        __syncwarp();
+    }
+    gemm16_end<kPair>(c);
+}
+
+template <bool kPair>
+int launch_ortho_kernel(const OrthoParams& o, cudaStream_t st) {
+    static PerDeviceOnce once;
+    static std::atomic<int> resident[64];        // CTAs (pairs) that run at the same time, per device
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return PCL_ERR_CUDA;
+    cudaLaunchConfig_t lc = {};
+    lc.blockDim = dim3(kThreads16);
+    lc.dynamicSmemBytes = kSmem16Fetch;
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kPair ? 2 : 1; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeCooperative;
+    attr[1].val.cooperative = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+    const int rc = once.run([&] {
+        if (cudaFuncSetAttribute(orthogonalize_kernel<kPair>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem16Fetch) != cudaSuccess) return int(PCL_ERR_CUDA);
+        int n = 0;
+        lc.gridDim = dim3(kPair ? 2 : 1);
+        if (cudaOccupancyMaxActiveClusters(&n, orthogonalize_kernel<kPair>, &lc) != cudaSuccess || n < 1) return int(PCL_ERR_CUDA);
+        resident[dev].store(n);
+        return int(PCL_OK);
+    });
+    if (rc != PCL_OK) return rc;
+    int most = o.gram.items > o.square.items ? o.gram.items : o.square.items;
+    if (o.step.items > most) most = o.step.items;
+    const int n = resident[dev].load();
+    lc.gridDim = dim3(unsigned(most < n ? most : n) * (kPair ? 2 : 1));
+    lc.numAttrs = 2;
+    return cudaLaunchKernelEx(&lc, orthogonalize_kernel<kPair>, o) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
 }
 
 }  // namespace
@@ -204,7 +357,7 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     const bool wide = o.M <= o.N;
     const long xb = long(o.M) * l.ld, db = long(l.d) * l.ldd;
     StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), 0, xh[0],
-                o.steps > 1 ? xl : nullptr, o.M, o.N, l.ld, l.split_bytes ? reinterpret_cast<int*>(base + l.split) : nullptr};
+                o.steps > 1 ? xl : nullptr, o.M, o.N, l.ld, reinterpret_cast<int*>(base + l.counters)};
     // four elements at a time where every row starts on a multiple of four (16 bytes of fp32, 8 bytes of the 16-bit types)
     const bool vec = o.N % 4 == 0;
     const double elems = double(o.count) * o.M * o.N;
@@ -223,51 +376,50 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
                                       dim3(256), 0, st, 1, s);
         if (rc != PCL_OK) return rc;
     }
-    int cur = 0;
-    for (int it = 0; it < o.steps; ++it) {
-        const bool last = it + 1 == o.steps;
-        const Gemm16Operand gram{xh[cur], l.ld, xb, !wide};
-        Gemm16Args g1 = gram_args(o.count, o.M, o.N);
-        g1.a = g1.b = gram;
-        g1.split_ws = base + l.split;
-        g1.alpha = 1.f / kScaleX;                             // kScaleX^2 A -> kScaleX A
-        g1.out = A; g1.out_type = DT_F16; g1.out_ld = l.ldd; g1.out_batch = db;
-        int rc = launch_gemm16(g1, st);
-        if (rc != PCL_OK) return rc;
-        const Gemm16Operand am{A, l.ldd, db, false}, bm{B, l.ldd, db, false};
-        Gemm16Args g2 = square_args(o.count, o.M, o.N);
-        g2.a = g2.b = am;
-        g2.split_ws = base + l.split;
-        g2.alpha = kNsC * kScaleB / (kScaleX * kScaleX);
-        g2.src = A; g2.src_type = DT_F16; g2.src_ld = l.ldd; g2.src_batch = db; g2.beta = kNsB * kScaleB / kScaleX;
-        g2.out = B; g2.out_type = DT_F16; g2.out_ld = l.ldd; g2.out_batch = db;
-        rc = launch_gemm16(g2, st);
-        if (rc != PCL_OK) return rc;
-        Gemm16Args g3 = apply_args(o.count, o.M, o.N);
-        g3.a = wide ? bm : Gemm16Operand{xh[cur], l.ld, xb, false};
-        g3.b = wide ? Gemm16Operand{xh[cur], l.ld, xb, true} : bm;
-        g3.split_ws = base + l.split;
-        g3.src = xh[cur]; g3.src_type = DT_F16; g3.src_ld = l.ld; g3.src_batch = xb;
-        if (last) {                                           // to the caller's matrix
-            g3.epi = GEMM16_GENERAL;
-            g3.alpha = 1.f / (kScaleX * kScaleB); g3.beta = kNsA / kScaleX;
-            g3.out = o.out; g3.out_type = o.type; g3.out_ld = o.N; g3.out_batch = long(o.M) * o.N;
-            if (o.momentum) {
-                g3.update = true;
-                g3.keep = 1.f - o.lr * o.weight_decay;
-                g3.step = o.lr * sqrtf(o.M > o.N ? float(o.M) / float(o.N) : 1.f);
-            }
-        } else {                                              // kScaleX X, in two planes (the second in place)
-            g3.alpha = 1.f / kScaleB; g3.beta = kNsA;
-            g3.src_lo = xl;
-            g3.out = xh[cur ^ 1]; g3.out_ld = l.ld; g3.out_batch = xb;
-            if (it + 2 < o.steps) g3.out_lo = xl;
-        }
-        rc = launch_gemm16(g3, st);
-        if (rc != PCL_OK) return rc;
-        cur ^= 1;
+    // the products
+    OrthoParams op;
+    const Gemm16Operand xk[2] = {{xh[0], l.ld, xb, false}, {xh[1], l.ld, xb, false}}, xmn[2] = {{xh[0], l.ld, xb, true}, {xh[1], l.ld, xb, true}};
+    const Gemm16Operand am{A, l.ldd, db, false}, bm{B, l.ldd, db, false};
+    Gemm16Args g1 = gram_args(o.count, o.M, o.N, l.form), g2 = square_args(o.count, o.M, o.N, l.form), g3 = apply_args(o.count, o.M, o.N, l.form);
+    g1.alpha = 1.f / kScaleX;                                 // kScaleX^2 A -> kScaleX A
+    g2.alpha = kNsC * kScaleB / (kScaleX * kScaleX);
+    g2.beta = kNsB * kScaleB / kScaleX;
+    g3.alpha = 1.f / kScaleB; g3.beta = kNsA;                 // kScaleX X, in two planes (the second in place)
+    Gemm16Args g4 = g3;                                       // the last step's: to the caller's matrix
+    g4.epi = GEMM16_FINAL;
+    g4.src = xh[0]; g4.src_type = DT_F16; g4.src_ld = l.ld; g4.src_batch = xb;
+    g4.alpha = 1.f / (kScaleX * kScaleB); g4.beta = kNsA / kScaleX;
+    g4.out = o.out; g4.out_type = o.type; g4.out_ld = o.N; g4.out_batch = long(o.M) * o.N;
+    if (o.momentum) {
+        g4.update = true;
+        g4.keep = 1.f - o.lr * o.weight_decay;
+        g4.step = o.lr * sqrtf(o.M > o.N ? float(o.M) / float(o.N) : 1.f);
     }
-    return PCL_OK;
+    int rc = PCL_OK;
+    auto fill = [&](Gemm16Params& p, Gemm16Args& a, const Plan16& pl) {
+        a.split_ws = base + l.counters;
+        if (rc == PCL_OK) rc = fill_params16(p, a, pl);
+    };
+    const Plan16 pl1 = plan16(g1), pl2 = plan16(g2), pl3 = plan16(g3);
+    fill(op.gram, g1, pl1); fill(op.square, g2, pl2); fill(op.step, g3, pl3); fill(op.final, g4, pl3);
+    auto operand = [&](CUtensorMap* m, const Gemm16Operand& a, int rows, int K) { if (rc == PCL_OK) rc = operand_tmap(m, a, rows, K, o.count, false); };
+    for (int i = 0; i < 2; ++i) {
+        operand(&op.xk[i], xk[i], o.M, o.N);
+        operand(&op.xmn[i], xmn[i], o.N, o.M);
+        if (rc == PCL_OK) rc = make_tmap16(&op.x_out[i], xh[i], DT_F16, o.N, o.M, o.count, l.ld, xb, 32, 32);
+        op.x[i] = xh[i];
+    }
+    operand(&op.a, am, l.d, l.d);
+    operand(&op.b, bm, l.d, l.d);
+    if (rc == PCL_OK) rc = make_tmap16(&op.lo_out, xl, DT_F16, o.N, o.M, o.count, l.ld, xb, 32, 32);
+    if (rc == PCL_OK) rc = make_tmap16(&op.a_out, A, DT_F16, l.d, l.d, o.count, l.ldd, db, 32, 32);
+    if (rc == PCL_OK) rc = make_tmap16(&op.b_out, B, DT_F16, l.d, l.d, o.count, l.ldd, db, 32, 32);
+    if (rc != PCL_OK) return rc;
+    op.out = o.out; op.steps = o.steps; op.wide = wide;
+    op.barrier = reinterpret_cast<unsigned*>(base + l.counters) + kGemm16CounterBytes / 4 - 1;      // (the tiles' counters end before)
+    const double m = l.d, k = o.M < o.N ? o.N : o.M;
+    LaunchScope scope(KID_ORTHO, o.steps * o.count * (3.0 * m * m * k + m * m * m), st);
+    return l.form == GEMM16_FORM_PAIR ? launch_ortho_kernel<true>(op, st) : launch_ortho_kernel<false>(op, st);
 }
 
 }  // namespace pcl

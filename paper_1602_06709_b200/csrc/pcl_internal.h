@@ -311,15 +311,17 @@ struct Gemm16Operand {
     bool mn_major;          // element (r, k) at ptr[k * ld + r] instead of ptr[r * ld + k]
 };
 enum Gemm16Epi {
-    GEMM16_GENERAL = 0,     // v = alpha * (alpha_dev ? *alpha_dev : 1) * acc + beta * src;  out = v, or, with `update`,
-                            // out = keep * out - step * v in place; any types, any alignment
+    GEMM16_GENERAL = 0,     // out = alpha * (alpha_dev ? *alpha_dev : 1) * acc + beta * src (src fp32 or null); any type, any alignment
     GEMM16_STORE,           // (what GENERAL becomes where out can be stored through TMA as it is)
-    GEMM16_SYM,             // out = alpha * acc + beta * src in fp16, where the result is symmetric: only the tiles on and above
-                            // the diagonal are computed, the others are their mirror images
-    GEMM16_STEP,            // v = alpha * acc + beta * (src + src_lo / 2^11), out = fp16(v), out_lo = fp16((v - out) * 2^11)
     GEMM16_PARTS,           // the reduction in k_parts parts, each part's fp32 sums to out + part * out_batch (batch = 1)
-    GEMM16_STATS, GEMM16_DZ // softmax over classes, see below
+    GEMM16_STATS, GEMM16_DZ,// softmax over classes, see below
+    // the orthogonalised update's, in its own kernel:
+    GEMM16_SYM,             // out = alpha * acc + beta * src in fp16, where the result is symmetric: the tiles below the diagonal
+                            // may be stored as mirror images instead of being computed
+    GEMM16_STEP,            // v = alpha * acc + beta * (src + src_lo / 2^11), out = fp16(v), out_lo = fp16((v - out) * 2^11)
+    GEMM16_FINAL            // v = alpha * acc + beta * src (fp16);  out = v, or, with `update`, out = keep * out - step * v in place
 };
+enum Gemm16Form { GEMM16_FORM_AUTO = 0, GEMM16_FORM_PAIR, GEMM16_FORM_SINGLE };
 struct Gemm16Args {
     int M, N, K, batch;     // rows of A, rows of B (columns of the result), reduction length, matrices
     bool bf16;              // element type of both operands (else fp16)
@@ -329,11 +331,10 @@ struct Gemm16Args {
     const float* alpha_dev = nullptr;
     float beta = 0.f;
     const void* src = nullptr; int src_type = DT_F32; long src_ld = 0, src_batch = 0;
-    const void* src_lo = nullptr;            // laid out like src
     void* out = nullptr; int out_type = DT_F32; long out_ld = 0, out_batch = 0;
-    void* out_lo = nullptr;                  // laid out like out; may be null (then it is not written) or src_lo
     bool update = false; float keep = 1.f, step = 0.f;
     int k_parts = 0;
+    int form = GEMM16_FORM_AUTO;             // CTA pairs, single CTAs, or whichever takes less time
     // GEMM16_STATS / GEMM16_DZ: z[r][c] = acc + bias[c]; the columns are classes col0 .. col0 + N - 1.
     const void* bias = nullptr;         // [N], type of the operands
     const int* labels = nullptr;        // [M]

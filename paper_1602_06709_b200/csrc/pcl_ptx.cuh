@@ -601,6 +601,7 @@ enum : uint32_t {
     WAIT_EPI_TMEM_FULL = 0x104,
     WAIT_DRAIN = 0x105,
     WAIT_ISSUE_TURN = 0x106,
+    WAIT_GRID = 0x107,
 };
 
 }  // namespace pcl
