@@ -392,14 +392,37 @@ def dtype_code(t) -> int:
     return _DTYPES[t.dtype]
 
 
-def _typed(where, sizes, typed, fp32=(), int32=()):
-    """Checks the tensors of a call -- (tensor, element count) pairs, None allowed -- and returns the type code that those of
-    `typed` share; all must be on one device, the current one."""
+def _typed(where, sizes, typed, fp32=(), int32=(), stream=None):
+    """Checks the tensors of a call -- (tensor, element count) pairs, None allowed; all contiguous, on the current device --
+    and returns the type code that those of `typed` share, and the stream handle.  (Written for few interpreter steps: the
+    smallest of these calls launch a kernel of two microseconds.)"""
     for n in sizes:
         if type(n) is not int or n <= 0:
             raise PclError(ERR_BAD_ARG, where)
     first = typed[0][0]
-    code, dev = dtype_code(first), first.device
+    want, dev = first.dtype, first.get_device()
+    code = _DTYPES.get(want, -1)
+    ok = code >= 0 and dev >= 0
+    for t, n in typed:
+        if t is not None and not (t.dtype is want and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
+            ok = False
+    for t, n in fp32:
+        if t is not None and not (t.dtype is torch.float32 and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
+            ok = False
+    for t, n in int32:
+        if not (t.dtype is torch.int32 and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
+            ok = False
+    if not ok:
+        _explain(where, typed, fp32, int32)
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+    return code, (stream.cuda_stream if stream is not None else _raw_stream(dev))
+
+
+def _explain(where, typed, fp32, int32):
+    """Raises what is wrong with the tensors of a call."""
+    first = typed[0][0]
+    dtype_code(first)
     for group, want in ((typed, first.dtype), (fp32, torch.float32), (int32, torch.int32)):
         for t, n in group:
             if t is None:
@@ -408,11 +431,15 @@ def _typed(where, sizes, typed, fp32=(), int32=()):
                 raise TypeError(f"{where}: a {want} tensor is wanted, not {t.dtype}")
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"{where}: a contiguous tensor of {n} elements is wanted")
-            if t.device != dev:
-                raise ValueError(f"{where}: all tensors must be on one device")
-    if dev.type != "cuda" or dev.index != torch.cuda.current_device():
-        raise ValueError(f"{where}: all tensors must be on the current CUDA device")
-    return code
+    raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+
+
+def _raw_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):          # (the handle without a Stream object around it)
+    _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _addr(t):
@@ -430,25 +457,25 @@ def embedding_workspace_bytes(N, V, C) -> int:
 
 def embedding_fwd(N, V, C, ids, table, scale, out, pad_id=None, stream=None):
     """out[n] = scale * table[ids[n]]; rows of pad_id are zero."""
-    d = _typed("pcl_embedding_fwd", (N, V, C), [(table, V * C), (out, N * C)], int32=[(ids, N)])
+    d, s = _typed("pcl_embedding_fwd", (N, V, C), [(table, V * C), (out, N * C)], int32=[(ids, N)], stream=stream)
     _check(lib().pcl_embedding_fwd(N, V, C, d, _addr(ids), _addr(table), scale, _id(pad_id), _addr(out),
-                                   _stream(stream)), "pcl_embedding_fwd")
+                                   s), "pcl_embedding_fwd")
 
 
 def embedding_bwd(N, V, C, ids, dy, scale, dtable, pad_id=None, ws=None, stream=None):
     """dtable[v] = scale * sum of dy[n] over the tokens n with ids[n] == v; every row is written."""
-    d = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)])
+    d, s = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_embedding_bwd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(dtable), wp, wb,
-                                   _stream(stream)), "pcl_embedding_bwd")
+                                   s), "pcl_embedding_bwd")
 
 
 def embedding_bwd_sgd(N, V, C, ids, dy, scale, table, lr, pad_id=None, ws=None, stream=None):
     """table[v] -= lr * dtable[v] in place for the rows that occur; dtable is not stored."""
-    d = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)])
+    d, s = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_embedding_bwd_sgd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(table),
-                                       lr, wp, wb, _stream(stream)), "pcl_embedding_bwd_sgd")
+                                       lr, wp, wb, s), "pcl_embedding_bwd_sgd")
 
 
 def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
@@ -458,22 +485,22 @@ def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
 
 def fc_softmax_xent_fwd(N, C, K, x, w, bias, labels, loss, row_loss, lse, ignore_label=None, ws=None, stream=None):
     """Mean loss, loss and log-sum-exp of each row of softmax(x w^T + bias), without storing the logits."""
-    d = _typed("pcl_fc_softmax_xent_fwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K)],
-               [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)])
+    d, s = _typed("pcl_fc_softmax_xent_fwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K)],
+               [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_fc_softmax_xent_fwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label),
-                                         _addr(loss), _addr(row_loss), _addr(lse), wp, wb, _stream(stream)),
+                                         _addr(loss), _addr(row_loss), _addr(lse), wp, wb, s),
            "pcl_fc_softmax_xent_fwd")
 
 
 def fc_softmax_xent_bwd(N, C, K, x, w, bias, labels, lse, row_grad, dx, dw, dbias, ignore_label=None, ws=None, stream=None):
     """dx (or None), dw and dbias (or None) from the forward call's lse; row_grad: gradient of each row's loss, or None for
     the gradient of the mean."""
-    d = _typed("pcl_fc_softmax_xent_bwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K), (dx, N * C), (dw, K * C), (dbias, K)],
-               [(lse, N), (row_grad, N)], [(labels, N)])
+    d, s = _typed("pcl_fc_softmax_xent_bwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K), (dx, N * C), (dw, K * C), (dbias, K)],
+               [(lse, N), (row_grad, N)], [(labels, N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_fc_softmax_xent_bwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label), _addr(lse),
-                                         _addr(row_grad), _addr(dx), _addr(dw), _addr(dbias), wp, wb, _stream(stream)),
+                                         _addr(row_grad), _addr(dx), _addr(dw), _addr(dbias), wp, wb, s),
            "pcl_fc_softmax_xent_bwd")
 
 
@@ -483,18 +510,18 @@ def orthogonalize_workspace_bytes(count, M, N) -> int:
 
 def orthogonalize(count, M, N, g, out, steps=5, ws=None, stream=None):
     """out = g / |g| after `steps` Newton-Schulz steps, for each of `count` M x N matrices."""
-    d = _typed("pcl_orthogonalize", (count, M, N), [(g, count * M * N), (out, count * M * N)])
+    d, s = _typed("pcl_orthogonalize", (count, M, N), [(g, count * M * N), (out, count * M * N)], stream=stream)
     wp, wb = _ws(ws)
-    _check(lib().pcl_orthogonalize(count, M, N, d, _addr(g), _addr(out), steps, wp, wb, _stream(stream)), "pcl_orthogonalize")
+    _check(lib().pcl_orthogonalize(count, M, N, d, _addr(g), _addr(out), steps, wp, wb, s), "pcl_orthogonalize")
 
 
 def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_decay=0.0, steps=5, ws=None, stream=None):
     """momentum <- mu momentum + dw, then w <- (1 - lr weight_decay) w - lr sqrt(max(1, M/N)) * orthogonalize(direction)."""
-    d = _typed("pcl_orthogonal_update", (count, M, N), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)])
+    d, s = _typed("pcl_orthogonal_update", (count, M, N), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_orthogonal_update(count, M, N, d, _addr(w), _addr(dw), _addr(momentum), mu,
                                        1 if nesterov else 0, lr, weight_decay, steps, wp, wb,
-                                       _stream(stream)), "pcl_orthogonal_update")
+                                       s), "pcl_orthogonal_update")
 
 
 def last_device_status(stream=None) -> int:

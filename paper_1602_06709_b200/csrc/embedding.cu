@@ -2,9 +2,9 @@
 // or of dy is read once, a row of the output written once.
 //
 // Gradient: dtable[v] = scale * sum over tokens n with ids[n] = v of dy[n].  The tokens are sorted by id (stable, so equal
-// ids stay in index order) by one cluster of CTAs, while the other CTAs of that launch zero the gradient's last rows, as many
-// as fit the sort's time (the sort is latency, the zeroing bandwidth).  Then every kItemTokens consecutive sorted tokens are one work item.  An item sums the
-// segments (runs of equal ids) that begin in it; only segments of more than kLongSegment tokens are cut at the items' borders
+// ids stay in index order) by one cluster of CTAs, while the other CTAs of that launch fetch dy into L2 where it fits and
+// zero the gradient's last rows, as much as the sort's time allows (the sort is latency, the rest bandwidth).  Then every 8 or 16 consecutive sorted tokens are one work item.  An item sums the
+// segments (runs of equal ids) that begin in it; only segments of more than twice that are cut at the items' borders
 // into partial sums that a last pass adds in order.  The work is even whatever the ids' frequencies are, and the
 // additions have a fixed order (no atomics).  Blocks that zero the remaining rows that do not occur run between the items' blocks.
 #include <cuda_bf16.h>
@@ -18,14 +18,16 @@ namespace pcl {
 
 namespace {
 
-constexpr int kItemTokens = 16;
-constexpr int kLongSegment = 32;
+// Sorted tokens per work item, and the segment length from which a segment is cut at the items' borders: few tokens are spread
+// over more warps (5000 tokens: 18.5 -> 13 us with items of 8), many leave fewer partial sums.
+inline int item_tokens(int N) { return N <= 8192 ? 8 : 16; }
+inline int long_segment(int N) { return 2 * item_tokens(N); }
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = 32;
 constexpr int kMaxSortCtas = 8;          // portable cluster size
 constexpr int kMaxBits = 9;              // bits of a digit
 constexpr int kHistLd = (1 << kMaxBits) + 1;                  // (odd: a column over the warps meets every bank once)
-constexpr size_t kZeroInSort = size_t(100) << 20;             // bytes zeroed beside the sort (about its 20 us)
+constexpr size_t kBesideSort = size_t(100) << 20;             // bytes fetched and zeroed beside the sort (in about its 20 us)
 constexpr int kMaxRun = 8192;            // tokens per CTA that the shared-memory sort takes
 
 template <class T> __device__ __forceinline__ float to_f32(T v);
@@ -62,6 +64,8 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restric
                                                             float scale, int pad_id, T* __restrict__ out, int N, int V, int C,
                                                             int tpr_log2, unsigned int* status) {
     const int tpr = 1 << tpr_log2;                   // threads per row
+    grid_dependency_wait();
+    grid_dependents_launch();
     const int vecs = C / kVec;
     const int lane = threadIdx.x & (tpr - 1);
     const long groups = long(gridDim.x) * (256 >> tpr_log2);
@@ -117,6 +121,8 @@ struct SortArgs {
     int* long_count;              // set to 0 here
     uint4* zero; size_t zero16;   // what the other CTAs clear: 16-byte units, and the bytes behind them
     unsigned char* zero_tail; int zero_tail_bytes;
+    const char* dy; size_t dy_lines;                          // ... and fetch into L2: 128-byte lines of dy, and (sgd) the rows of
+    const char* table; size_t row_bytes;                      // the table that the ids name
     unsigned int* status;
 };
 template <bool kShared>
@@ -126,6 +132,7 @@ __device__ __forceinline__ void sort_barrier(bool cluster) {
     cluster_sync_all();
     if (!kShared) __threadfence();                            // (drops stale L1 lines)
 }
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 // The lanes of `act` (to which the calling lane belongs) that hold the same digit of `bits` bits.
 __device__ __forceinline__ unsigned same_digit(unsigned act, int d, int bits) {
     unsigned same = act;
@@ -153,11 +160,20 @@ template <bool kShared>
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a) {
     extern __shared__ int sort_smem[];       // hist [32][kHistLd], totals [512], (kShared) [2] runs of (key, token)
     __shared__ int warp_sum[16];
+    grid_dependency_wait();
+    grid_dependents_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (int(blockIdx.x) >= a.ctas) {         // the other clusters: zeros
         const uint4 z = make_uint4(0u, 0u, 0u, 0u);
         const size_t stride = size_t(gridDim.x - a.ctas) * kSortThreads;
         const size_t i0 = size_t(blockIdx.x - a.ctas) * kSortThreads + threadIdx.x;
+        for (size_t i = i0; i < a.dy_lines; i += stride) prefetch_l2(a.dy + i * 128);
+        if (a.table)
+            for (size_t n = i0 >> 5; n < size_t(a.N); n += stride >> 5) {
+                const int id = a.ids[n];
+                if (id == a.pad_id || id < 0 || id >= a.V) continue;
+                for (size_t o = size_t(lane) * 128; o < a.row_bytes; o += 32 * 128) prefetch_l2(a.table + size_t(id) * a.row_bytes + o);
+            }
 #pragma unroll 4
         for (size_t i = i0; i < a.zero16; i += stride) a.zero[i] = z;
         if (i0 < size_t(a.zero_tail_bytes)) a.zero_tail[i0] = 0;
@@ -302,7 +318,7 @@ struct GradArgs {
     int item_blocks, zero_blocks;
     float* part;                  // [items][2][C]: sums of an item's share of a long segment begun before it, and begun in it
     float scale, lr;
-    int N, V, C, items;
+    int N, V, C, items, item_tokens;
     int* long_count;              // long segments and the items they begin in
     int* long_items;
     int wpi_log2;                 // warps per item
@@ -322,14 +338,17 @@ __device__ __forceinline__ void write_row(const GradArgs& a, T* out, int key, in
     reinterpret_cast<Pack<T, kVec>*>(out + size_t(key) * a.C)[i] = o;
 }
 
-// One warp per item and 32 vectors of a row.  The item's keys and tokens are held by the lanes (a window of 32 sorted
-// positions), so that per batch of tokens only their rows are waited for; with kSgd the table's old rows come with them.
+// One warp per item and 32 vectors of a row (single elements, where rows are not aligned for vectors: 64).  The item's keys
+// and tokens are held by the lanes (a window of 32 sorted positions), so that per batch of tokens only their rows are waited
+// for; with kSgd the table's old rows come with them.
 template <class T, int kVec, bool kSgd>
 __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradArgs a, const T* __restrict__ dy, T* __restrict__ out) {
-    constexpr int kBatch = 4;
+    constexpr int kBatch = kVec == 1 && !kSgd ? 8 : 4, kRep = kVec == 1 ? 2 : 1;        // tokens at a time; vectors per lane, 32 apart
     using P = Pack<T, kVec>;
-    const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
+    const int vecs = a.C / kVec, strips = (vecs + 32 * kRep - 1) / (32 * kRep);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    grid_dependency_wait();
+    grid_dependents_launch();
     // the zeroing blocks are spread evenly among the others
     const long all = long(a.item_blocks) + a.zero_blocks, b = blockIdx.x;
     const int zeros_before = int(b * a.zero_blocks / all);
@@ -348,8 +367,8 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
     const int wpi = 1 << a.wpi_log2;                          // warps per item
     const int item = int(b - zeros_before) * (8 >> a.wpi_log2) + (w >> a.wpi_log2);
     if (item >= a.items) return;
-    const int p0 = item * kItemTokens;
-    const int p1 = p0 + kItemTokens < a.N ? p0 + kItemTokens : a.N;
+    const int p0 = item * a.item_tokens;
+    const int p1 = p0 + a.item_tokens < a.N ? p0 + a.item_tokens : a.N;
     int wb = p0, key, tok;
     unsigned ends;
     auto load_window = [&]() {                                // (whether lane 31 ends a segment is not known in it)
@@ -366,20 +385,21 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
     const int k1 = __shfl_sync(0xffffffffu, key, rows_end - 1 - p0);
     const int2 s0 = a.bounds[k0], s1 = a.bounds[k1];
     const int done = s0.x < p0 ? (s0.y < rows_end ? s0.y : rows_end) : p0;      // [p0, done): of a segment begun before
-    const bool front = done > p0 && s0.y - s0.x > kLongSegment;                 // ... whose share is summed here
+    const bool front = done > p0 && s0.y - s0.x > 2 * a.item_tokens;                 // ... whose share is summed here
     const bool goes_on = s1.x >= p0 && s1.y > p1;                               // the last segment begins here
-    const bool back = goes_on && s1.y - s1.x > kLongSegment;
+    const bool back = goes_on && s1.y - s1.x > 2 * a.item_tokens;
     const int begin = front ? p0 : done, stop = back || !goes_on ? rows_end : s1.y;
     if (back && (w & (wpi - 1)) == 0 && lane == 0) a.long_items[atomicAdd(a.long_count, 1)] = item;
     for (int strip = w & (wpi - 1); strip < strips; strip += wpi) {
-        const int i = strip * 32 + lane;
-        const bool col = i < vecs;
-        float sum[kVec];
+        const int i0 = strip * 32 * kRep + lane;
+        float sum[kRep][kVec];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
+        for (int h = 0; h < kRep; ++h)
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) sum[h][j] = 0.f;
         for (int p = begin; p < stop; p += kBatch) {
             if (p < wb || p + kBatch > wb + 31) { wb = p; load_window(); }
-            P v[kBatch], old[kSgd ? kBatch : 1];
+            P v[kBatch][kRep], old[kSgd ? kBatch : 1][kRep];
             bool row_ends[kBatch];
 #pragma unroll
             for (int q = 0; q < kBatch; ++q) {
@@ -387,29 +407,36 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
                 const size_t t = size_t(__shfl_sync(0xffffffffu, tok, o));
                 const int k = kSgd ? __shfl_sync(0xffffffffu, key, o) : 0;
                 row_ends[q] = (ends >> o) & 1u;
-                if (p + q < stop && col) {
-                    v[q] = reinterpret_cast<const P*>(dy + t * a.C)[i];
-                    if (kSgd && row_ends[q]) old[q] = reinterpret_cast<const P*>(out + size_t(k) * a.C)[i];
-                }
+#pragma unroll
+                for (int h = 0; h < kRep; ++h)
+                    if (p + q < stop && i0 + 32 * h < vecs) {
+                        v[q][h] = reinterpret_cast<const P*>(dy + t * a.C)[i0 + 32 * h];
+                        if (kSgd && row_ends[q]) old[q][h] = reinterpret_cast<const P*>(out + size_t(k) * a.C)[i0 + 32 * h];
+                    }
             }
 #pragma unroll
             for (int q = 0; q < kBatch; ++q) {
                 if (p + q >= stop) break;
                 const int k = __shfl_sync(0xffffffffu, key, p - wb + q);
-                if (!col) continue;
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) sum[j] += to_f32<T>(v[q].e[j]);
-                if (!row_ends[q] && p + q + 1 != stop) continue;
+                const bool flush = row_ends[q] || p + q + 1 == stop;
                 const bool share0 = front && p + q < done, share1 = back && p + q >= s1.x;
-                if (share0 || share1) {
-                    float* dst = a.part + (size_t(item) * 2 + (share0 ? 0 : 1)) * a.C + size_t(i) * kVec;
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) dst[j] = sum[j];
-                } else {
-                    write_row<T, kVec>(a, out, k, i, sum, old[kSgd ? q : 0]);
+                for (int h = 0; h < kRep; ++h) {
+                    const int i = i0 + 32 * h;
+                    if (i >= vecs) continue;
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) sum[h][j] += to_f32<T>(v[q][h].e[j]);
+                    if (!flush) continue;
+                    if (share0 || share1) {
+                        float* dst = a.part + (size_t(item) * 2 + (share0 ? 0 : 1)) * a.C + size_t(i) * kVec;
+#pragma unroll
+                        for (int j = 0; j < kVec; ++j) dst[j] = sum[h][j];
+                    } else {
+                        write_row<T, kVec>(a, out, k, i, sum[h], old[kSgd ? q : 0][h]);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) sum[h][j] = 0.f;
                 }
-#pragma unroll
-                for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
             }
         }
     }
@@ -419,13 +446,15 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
 template <class T, int kVec>
 __global__ void __launch_bounds__(256) embedding_grad_join_kernel(GradArgs a, T* __restrict__ out) {
     __shared__ float sums[8][32][kVec + 1];
+    grid_dependency_wait();
+    grid_dependents_launch();
     const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
     const long works = long(*a.long_count) * strips;
     for (long wk = blockIdx.x; wk < works; wk += gridDim.x) {
         const int item = a.long_items[wk / strips], i = int(wk % strips) * 32 + lane;
-        const int key = a.keys[item * kItemTokens + kItemTokens - 1];
-        const int last = (a.bounds[key].y - 1) / kItemTokens;
+        const int key = a.keys[(item + 1) * a.item_tokens - 1];
+        const int last = (a.bounds[key].y - 1) / a.item_tokens;
         float sum[kVec];
 #pragma unroll
         for (int j = 0; j < kVec; ++j) sum[j] = 0.f;
@@ -463,12 +492,12 @@ BwdLayout bwd_layout(int N, int V, int C) {
     BwdLayout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
-    const size_t items = (size_t(N) + kItemTokens - 1) / kItemTokens;
+    const size_t items = (size_t(N) + item_tokens(N) - 1) / item_tokens(N);
     for (int i = 0; i < 2; ++i) { l.keys[i] = take(size_t(N) * 4); l.idx[i] = take(size_t(N) * 4); }
     l.bounds = take(size_t(V) * 8);
     l.long_count = take(4);
-    l.long_items = take((size_t(N) / kLongSegment + 1) * 4);
-    l.part = take(N > kLongSegment ? items * 2 * C * 4 : 0);
+    l.long_items = take((size_t(N) / long_segment(N) + 1) * 4);
+    l.part = take(N > long_segment(N) ? items * 2 * C * 4 : 0);
     l.total = at;
     return l;
 }
@@ -480,14 +509,13 @@ int run_fwd(int N, int V, int C, const int* ids, const void* table, float scale,
     const long rows_per_block = 256 >> tl;
     const long blocks = (N + 2 * rows_per_block - 1) / (2 * rows_per_block), cap = long(device_sm_count()) * 8;
     LaunchScope scope(KID_EMBEDDING, 2.0 * sizeof(T) * double(N) * C, st);
-    embedding_fwd_kernel<T, kVec><<<int(blocks < cap ? blocks : cap), 256, 0, st>>>(
-        ids, static_cast<const T*>(table), scale, pad_id, static_cast<T*>(out), N, V, C, tl, status);
-    return cudaGetLastError() == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    return launch_chained(embedding_fwd_kernel<T, kVec>, dim3(unsigned(blocks < cap ? blocks : cap)), dim3(256), 0, st, 1, ids,
+                          static_cast<const T*>(table), scale, pad_id, static_cast<T*>(out), N, V, C, tl, status);
 }
 
 template <class T, int kVec>
 int run_grad(GradArgs a, const void* dy, void* out, cudaStream_t st) {
-    const int vecs = a.C / kVec, strips = (vecs + 31) / 32;
+    const int vecs = a.C / kVec, per_strip = kVec == 1 ? 64 : 32, strips = (vecs + per_strip - 1) / per_strip;
     while (a.wpi_log2 < 3 && (1 << a.wpi_log2) < strips) ++a.wpi_log2;
     const int per_block = 8 >> a.wpi_log2, blocks = (a.items + per_block - 1) / per_block;
     {
@@ -495,15 +523,15 @@ int run_grad(GradArgs a, const void* dy, void* out, cudaStream_t st) {
         a.item_blocks = blocks;
         const int zero_cap = device_sm_count() * 8;
         a.zero_blocks = (a.zero_rows + 7) / 8 < zero_cap ? (a.zero_rows + 7) / 8 : zero_cap;
-        if (a.sgd) embedding_grad_kernel<T, kVec, true><<<blocks, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<T*>(out));
-        else embedding_grad_kernel<T, kVec, false><<<blocks + a.zero_blocks, 256, 0, st>>>(a, static_cast<const T*>(dy), static_cast<T*>(out));
+        const int rc = launch_chained(a.sgd ? embedding_grad_kernel<T, kVec, true> : embedding_grad_kernel<T, kVec, false>,
+                                      dim3(blocks + (a.sgd ? 0 : a.zero_blocks)), dim3(256), 0, st, 1, a, static_cast<const T*>(dy),
+                                      static_cast<T*>(out));
+        if (rc != PCL_OK) return rc;
     }
-    if (cudaGetLastError() != cudaSuccess) return PCL_ERR_CUDA;
-    if (a.N <= kLongSegment) return PCL_OK;
+    if (a.N <= long_segment(a.N)) return PCL_OK;
     LaunchScope scope(KID_EMBEDDING, 0.0, st);
-    const long most = (long(a.N) / kLongSegment) * ((vecs + 31) / 32), cap = long(device_sm_count()) * 8;
-    embedding_grad_join_kernel<T, kVec><<<int(most < cap ? most : cap), 256, 0, st>>>(a, static_cast<T*>(out));
-    return cudaGetLastError() == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    const long most = (long(a.N) / long_segment(a.N)) * ((vecs + 31) / 32), cap = long(device_sm_count()) * 8;
+    return launch_chained(embedding_grad_join_kernel<T, kVec>, dim3(unsigned(most < cap ? most : cap)), dim3(256), 0, st, 1, a, static_cast<T*>(out));
 }
 
 int log2_up(long v) {
@@ -520,17 +548,7 @@ int run_sort(const SortArgs& s, size_t smem, int blocks, cudaStream_t st) {
                        cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
     });
     if (rc != PCL_OK) return rc;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(blocks);
-    lc.blockDim = dim3(kSortThreads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim = {unsigned(s.ctas), 1u, 1u};
-    lc.attrs = attr;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, embedding_sort_kernel<kShared>, s) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    return launch_chained(embedding_sort_kernel<kShared>, dim3(blocks), dim3(kSortThreads), smem, st, unsigned(s.ctas), s);
 }
 
 }  // namespace
@@ -580,29 +598,41 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     s.idx0 = reinterpret_cast<int*>(base + l.idx[0]); s.idx1 = reinterpret_cast<int*>(base + l.idx[1]);
     s.bounds = reinterpret_cast<int2*>(base + l.bounds);
     s.long_count = reinterpret_cast<int*>(base + l.long_count);
-    int zero_blocks = 0, zero_row0 = 0;
+    // What the other SMs do meanwhile: fetch dy (and the table's rows) into L2 if they fit, then zeros.
+    const size_t row = size_t(C) * dtype_bytes(type);
+    size_t fetched = size_t(N) * row * (sgd ? 2 : 1);
+    if (fetched > kBesideSort) fetched = size_t(N) * row <= kBesideSort ? size_t(N) * row : 0;
+    if (fetched) {
+        s.dy = static_cast<const char*>(dy);
+        s.dy_lines = (size_t(N) * row + 127) / 128;
+        if (sgd && fetched > size_t(N) * row) { s.table = static_cast<const char*>(out); s.row_bytes = row; }
+    }
+    int other_blocks = int((fetched + 127) / 128 / kSortThreads) + 1, zero_row0 = 0;
+    const int most_blocks = device_sm_count() * 2;
     if (!sgd) {
         // whole rows from the end, of which the first starts on a 16-byte boundary (every eighth row does)
-        const size_t row = size_t(C) * dtype_bytes(type), rows = kZeroInSort / row;
+        const size_t rows = (kBesideSort - fetched) / row;
         if (rows < size_t(V)) zero_row0 = (V - int(rows)) / 8 * 8;
         const size_t bytes = size_t(V - zero_row0) * row;
         s.zero = reinterpret_cast<uint4*>(static_cast<char*>(out) + zero_row0 * row);
         s.zero16 = bytes / 16;
         s.zero_tail = reinterpret_cast<unsigned char*>(s.zero + s.zero16);
         s.zero_tail_bytes = int(bytes % 16);
-        const size_t want = (s.zero16 + 4 * kSortThreads - 1) / (4 * kSortThreads) + 1, cap = size_t(device_sm_count()) * 2;
-        zero_blocks = int((want < cap ? want : cap) + s.ctas - 1) / s.ctas * s.ctas;
+        const size_t want = (s.zero16 + 4 * kSortThreads - 1) / (4 * kSortThreads) + 1;
+        if (want > size_t(other_blocks)) other_blocks = int(want < size_t(most_blocks) ? want : size_t(most_blocks));
     }
+    if (other_blocks > most_blocks) other_blocks = most_blocks;
+    other_blocks = (other_blocks + s.ctas - 1) / s.ctas * s.ctas;                // (whole clusters)
     {
         LaunchScope scope(KID_EMBEDDING, 16.0 * double(N) * s.passes + (sgd ? 0.0 : double(V) * C * dtype_bytes(type)), st);
-        const int rc = shared ? run_sort<true>(s, smem, s.ctas + zero_blocks, st) : run_sort<false>(s, smem, s.ctas + zero_blocks, st);
+        const int rc = shared ? run_sort<true>(s, smem, s.ctas + other_blocks, st) : run_sort<false>(s, smem, s.ctas + other_blocks, st);
         if (rc != PCL_OK) return rc;
     }
     GradArgs g{};
     g.keys = (s.passes & 1) ? s.keys0 : s.keys1; g.idx = (s.passes & 1) ? s.idx0 : s.idx1; g.bounds = s.bounds;
     g.part = reinterpret_cast<float*>(base + l.part);
     g.long_count = s.long_count; g.long_items = reinterpret_cast<int*>(base + l.long_items);
-    g.scale = scale; g.lr = lr; g.N = N; g.V = V; g.C = C; g.items = (N - 1) / kItemTokens + 1; g.sgd = sgd;
+    g.scale = scale; g.lr = lr; g.N = N; g.V = V; g.C = C; g.item_tokens = item_tokens(N); g.items = (N - 1) / g.item_tokens + 1; g.sgd = sgd;
     g.zero_rows = zero_row0;
     if (type == DT_F32)
         return C % 4 == 0 ? run_grad<float, 4>(g, dy, out, st) : run_grad<float, 1>(g, dy, out, st);
