@@ -58,6 +58,7 @@ struct Gemm16Params {
     int col0;
     float2* part; int part_ld;
     float* label_z;
+    unsigned* clear;
     const float* lse;
     const float* row_scale;
     unsigned int* status;
@@ -821,7 +822,7 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
         return !ptr || ((reinterpret_cast<uintptr_t>(ptr) & (4 * dtype_bytes(type) - 1)) == 0 && ld % 4 == 0 && (a.batch == 1 || bs % 4 == 0));
     };
     p.quads = a.N % 4 == 0 && four(a.src, a.src_type, a.src_ld, a.src_batch) && four(a.out, a.out_type, a.out_ld, a.out_batch);
-    p.bias = a.bias; p.labels = a.labels; p.col0 = a.col0; p.part = a.part; p.part_ld = a.part_ld; p.label_z = a.label_z;
+    p.bias = a.bias; p.labels = a.labels; p.col0 = a.col0; p.part = a.part; p.part_ld = a.part_ld; p.label_z = a.label_z; p.clear = a.clear;
     p.lse = a.lse; p.row_scale = a.row_scale;
     p.status = device_status_ptr();
     if (!p.status) return PCL_ERR_CUDA;

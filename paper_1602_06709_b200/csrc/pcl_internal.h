@@ -342,6 +342,7 @@ struct Gemm16Args {
     // STATS: part[r][2 * tile + half] = (max, sum of exp(z - max)) of half a tile's columns; label_z[r] = z[r][label]
     float2* part = nullptr; int part_ld = 0;
     float* label_z = nullptr;
+    unsigned* clear = nullptr;               // a word that the launch sets to 0 (null: none)
     // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0
     const float* lse = nullptr;
     const float* row_scale = nullptr;

@@ -37,6 +37,8 @@ tc_gemm16_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     const Item16 tile = decode_item(p, c.first);         // (the grid has at most p.items CTAs or pairs)
     grid_dependency_wait();
     grid_dependents_launch();
+    if (kEpi == GEMM16_STATS || kEpi == GEMM16_PARTS)
+        if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) *p.clear = 0u;
     if (c.warp == 0) {
         if (!produce_items<kPair, kAMn, kBMn>(c, p, tile, &tm_a, &tm_b)) drain_producer(c);
     } else if (c.warp == 1) {

@@ -69,11 +69,42 @@ __device__ __forceinline__ void finish_row(int n, float m, float s, const int* l
     row_loss[n] = loss;
 }
 
+// Mean over the rows that count, by the last block of the grid to end (`ended` counts them; the launch in front of it set it to
+// 0): fixed order, 0 if no row counts.
+__device__ __forceinline__ void mean_by_last_block(unsigned* ended, const float* row_loss, const int* labels, int ignore_label, int N,
+                                                   float* loss) {
+    __shared__ double sums[8];
+    __shared__ int counts[8];
+    __shared__ bool last;
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last = atomicAdd(ended, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __threadfence();
+    double sum = 0.0;
+    int count = 0;
+#pragma unroll 4
+    for (int n = threadIdx.x; n < N; n += 256) {
+        sum += __ldcg(row_loss + n);
+        count += labels[n] != ignore_label;
+    }
+    for (int o = 16; o > 0; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); count += __shfl_xor_sync(0xffffffffu, count, o); }
+    if ((threadIdx.x & 31) == 0) { sums[threadIdx.x >> 5] = sum; counts[threadIdx.x >> 5] = count; }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0; count = 0;
+        for (int i = 0; i < 8; ++i) { sum += sums[i]; count += counts[i]; }
+        loss[0] = count ? float(sum / count) : 0.f;
+    }
+}
+
 // One warp per row: joins the parts that the product's epilogue left.
 __global__ void __launch_bounds__(256) loss_rows_kernel(const float2* __restrict__ part, int part_ld, int parts,
                                                         const float* __restrict__ label_z, const int* __restrict__ labels,
                                                         int ignore_label, int N, int K, float* __restrict__ row_loss,
-                                                        float* __restrict__ lse, unsigned int* status) {
+                                                        float* __restrict__ lse, float* __restrict__ loss, unsigned* ended,
+                                                        unsigned int* status) {
     grid_dependency_wait();
     grid_dependents_launch();
     const int lane = threadIdx.x & 31;
@@ -86,6 +117,7 @@ __global__ void __launch_bounds__(256) loss_rows_kernel(const float2* __restrict
         join_warp(m, s);
         if (lane == 0) finish_row(n, m, s, labels, ignore_label, K, label_z, row_loss, lse, status);
     }
+    mean_by_last_block(ended, row_loss, labels, ignore_label, N, loss);
 }
 
 // The same from the parts of the products themselves (reductions that are cut to fill the GPU): one block per row adds them up,
@@ -103,7 +135,8 @@ __device__ __forceinline__ float2 block_join(float m, float s) {
 __global__ void __launch_bounds__(256) loss_parts_kernel(const float* __restrict__ z, int parts, size_t part_step, int ld,
                                                          const void* __restrict__ bias, int type, const int* __restrict__ labels,
                                                          int ignore_label, int N, int K, float* __restrict__ label_z,
-                                                         float* __restrict__ row_loss, float* __restrict__ lse, unsigned int* status) {
+                                                         float* __restrict__ row_loss, float* __restrict__ lse, float* __restrict__ loss,
+                                                         unsigned* ended, unsigned int* status) {
     grid_dependency_wait();
     grid_dependents_launch();
     for (int n = blockIdx.x; n < N; n += gridDim.x) {
@@ -121,29 +154,7 @@ __global__ void __launch_bounds__(256) loss_parts_kernel(const float* __restrict
         const float2 r = block_join(m, s);
         if (threadIdx.x == 0) finish_row(n, r.x, r.y, labels, ignore_label, K, label_z, row_loss, lse, status);
     }
-}
-
-// Mean over the rows that count (fixed order; 0 if none does).
-__global__ void __launch_bounds__(1024) loss_mean_kernel(const float* __restrict__ row_loss, const int* __restrict__ labels,
-                                                         int ignore_label, int N, float* __restrict__ loss) {
-    __shared__ double sums[32];
-    __shared__ int counts[32];
-    grid_dependency_wait();
-    grid_dependents_launch();
-    double sum = 0.0;
-    int count = 0;
-    for (int n = threadIdx.x; n < N; n += 1024) {
-        sum += row_loss[n];
-        count += labels[n] != ignore_label;
-    }
-    for (int o = 16; o > 0; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); count += __shfl_xor_sync(0xffffffffu, count, o); }
-    if ((threadIdx.x & 31) == 0) { sums[threadIdx.x >> 5] = sum; counts[threadIdx.x >> 5] = count; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0; count = 0;
-        for (int i = 0; i < 32; ++i) { sum += sums[i]; count += counts[i]; }
-        loss[0] = count ? float(sum / count) : 0.f;
-    }
+    mean_by_last_block(ended, row_loss, labels, ignore_label, N, loss);
 }
 
 // What a row's dz is multiplied with, and what the products are multiplied with afterwards.  16-bit dz is kept in range by a
@@ -224,7 +235,8 @@ __global__ void __launch_bounds__(256) dz_colsum_kernel(const uint16_t* __restri
 // one block per row; state[n] = (max, sum) over the pieces so far
 __global__ void __launch_bounds__(256) piece_stats_kernel(const float* __restrict__ z, int N, int P, int col0,
                                                           const int* __restrict__ labels, float2* __restrict__ state,
-                                                          float* __restrict__ label_z) {
+                                                          float* __restrict__ label_z, unsigned* ended) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *ended = 0u;
     for (int n = blockIdx.x; n < N; n += gridDim.x) {
         const float* row = z + size_t(n) * P;
         float m = -INFINITY, s = 0.f;
@@ -364,7 +376,7 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
     unsigned int* status = device_status_ptr();
     if (!status) return PCL_ERR_CUDA;
     int rc = PCL_OK, parts = 0, part_ld = l.parts;
-    bool joined = false;                                      // lse and row_loss are written
+    unsigned* ended = reinterpret_cast<unsigned*>(base + l.alpha);
     if (type == DT_F32) {
         float* z = reinterpret_cast<float*>(base + l.dz);
         const size_t fc_bytes = l.split - l.fc;
@@ -374,7 +386,7 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
                             bias ? static_cast<const float*>(bias) + p0 : nullptr, z, PCL_ACT_NONE, base + l.fc, fc_bytes, st);
             if (rc != PCL_OK) return rc;
             LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(N) * P, st);
-            piece_stats_kernel<<<row_blocks(N), 256, 0, st>>>(z, N, P, p0, labels, part, label_z);
+            piece_stats_kernel<<<row_blocks(N), 256, 0, st>>>(z, N, P, p0, labels, part, label_z, ended);
             if ((rc = launched()) != PCL_OK) return rc;
         }
         parts = part_ld = 1;
@@ -397,18 +409,16 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
             Gemm16Args a = stats_args(N, C, P, type == DT_BF16);
             a.a = {xs, l.ldc, 0, false}; a.b = {wp, l.ldc, 0, false};
             a.split_ws = nullptr;
+            a.clear = ended;
             if (l.k_parts > 1) {
                 a.epi = GEMM16_PARTS; a.k_parts = l.k_parts;
                 a.out = base + l.dz; a.out_ld = l.ldp; a.out_batch = long(N) * l.ldp;
                 rc = launch_gemm16(a, st);
                 if (rc != PCL_OK) return rc;
                 LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(N) * K * l.k_parts, st);
-                rc = launch_chained(loss_parts_kernel, dim3(row_blocks(N)), dim3(256), 0, st, 1, reinterpret_cast<const float*>(base + l.dz),
+                return launch_chained(loss_parts_kernel, dim3(row_blocks(N)), dim3(256), 0, st, 1, reinterpret_cast<const float*>(base + l.dz),
                                     l.k_parts, size_t(N) * l.ldp, l.ldp, bias, type, labels, ignore_label, N, K, label_z, row_loss, lse,
-                                    status);
-                if (rc != PCL_OK) return rc;
-                joined = true;
-                break;
+                                    loss, ended, status);
             }
             a.bias = bias ? static_cast<const uint16_t*>(bias) + p0 : nullptr;
             a.labels = labels; a.col0 = p0; a.part = part + parts; a.part_ld = part_ld; a.label_z = label_z;
@@ -417,15 +427,10 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
             parts += gemm16_stats_parts(a);
         }
     }
-    if (!joined) {
-        LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N) * parts, st);
-        const int blocks = (N + 7) / 8, cap = device_sm_count() * 8;
-        rc = launch_chained(loss_rows_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, 1, part, part_ld, parts, label_z, labels,
-                            ignore_label, N, K, row_loss, lse, status);
-        if (rc != PCL_OK) return rc;
-    }
-    LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N), st);
-    return launch_chained(loss_mean_kernel, dim3(1), dim3(1024), 0, st, 1, row_loss, labels, ignore_label, N, loss);
+    LaunchScope scope(KID_VOCAB_LOSS, 8.0 * double(N) * parts, st);
+    const int blocks = (N + 7) / 8, cap = device_sm_count() * 8;
+    return launch_chained(loss_rows_kernel, dim3(blocks < cap ? blocks : cap), dim3(256), 0, st, 1, part, part_ld, parts, label_z, labels,
+                          ignore_label, N, K, row_loss, lse, loss, ended, status);
 }
 
 int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const void* w, const void* bias, const int* labels,
