@@ -89,11 +89,12 @@ class _GraphStep:
     def capture_step(self):
         """Call once, after construction (or after any eager steps).  The library's one-time setup (function
         attributes, its device status word) must not fall into the capture, so one eager step runs first, with the
-        parameters put back afterwards."""
-        saved = self.store.params.clone()
+        parameters (and moments) put back afterwards."""
+        saved = [(t, t.clone()) for t in self._step_state()]
         self.step()
         torch.cuda.synchronize()
-        self.store.params.copy_(saved)
+        for t, old in saved:
+            t.copy_(old)
         del saved
         self._graphs = {}
         for _ in range(2):
@@ -105,6 +106,10 @@ class _GraphStep:
             self._graphs[self.x.data_ptr()] = g
             self.x, self._alt_x = self._alt_x, self.x
             self.labels, self._alt_labels = self._alt_labels, self.labels
+
+    def _step_state(self):
+        """The tensors that a step updates."""
+        return [self.store.params]
 
     def run_step(self):
         """step(), through the captured graph when there is one for the current input buffer."""
@@ -353,12 +358,24 @@ class VggA(_HostFeed):
 
 class Dnn(_HostFeed):
     """Fully-connected DNN: dims[0] inputs, sigmoid hidden layers, linear output
-    layer with softmax cross-entropy (the 7-layer ASR network shape of Sec. 5.4)."""
+    layer with softmax cross-entropy (the 7-layer ASR network shape of Sec. 5.4).
 
-    def __init__(self, N: int, dims=None, lr: float = 0.01, cfg: str = "cfg4", fused_update: bool = False):
+    stored_logits = False: the output layer and the loss run as one call that never stores the N x dims[-1] logits and their
+    gradient (pcl_fc_softmax_xent_fwd / _bwd), for output layers over very many classes.
+    hidden_update = "orthogonal": the weight matrices between the first and the output layer are stepped along the
+    orthogonalised momentum of their gradient (pcl_orthogonal_update, rate hidden_lr); everything else by plain SGD."""
+
+    def __init__(self, N: int, dims=None, lr: float = 0.01, cfg: str = "cfg4", fused_update: bool = False,
+                 stored_logits: bool = True, hidden_update: str = "sgd", hidden_lr: float = 0.02, momentum: float = 0.95):
         dims = dims if dims is not None else inputs.CFG4_DIMS
+        if hidden_update not in ("sgd", "orthogonal"):
+            raise ValueError(f"unknown hidden_update {hidden_update!r}")
+        if hidden_update == "orthogonal" and fused_update:
+            raise ValueError("the orthogonalised update needs stored gradients: fused_update must be off")
         self.N, self.dims, self.lr = N, dims, lr
         self.fused_update = fused_update      # (as in VggA: weights updated by their own weight-gradient call)
+        self.stored_logits, self.hidden_update = stored_logits, hidden_update
+        self.hidden_lr, self.momentum = hidden_lr, momentum
         self.layers = list(zip(dims[:-1], dims[1:]))
         shapes = []
         for C, K in self.layers:
@@ -369,8 +386,9 @@ class Dnn(_HostFeed):
             self.store.p(2 * j).copy_(torch.from_numpy(w))
         dev = "cuda"
         self.x = torch.empty(N, dims[0], device=dev)
-        self.out = [torch.empty(N, K, device=dev) for _, K in self.layers]
-        self.dout = [torch.empty(N, K, device=dev) for _, K in self.layers]
+        stored = len(self.layers) if stored_logits else len(self.layers) - 1
+        self.out = [torch.empty(N, K, device=dev) if j < stored else None for j, (_, K) in enumerate(self.layers)]
+        self.dout = [torch.empty(N, K, device=dev) if j < stored else None for j, (_, K) in enumerate(self.layers)]
         self.labels = torch.zeros(N, dtype=torch.int32, device=dev)
         self._feed_init()
         self.loss = torch.zeros(1, device=dev)
@@ -378,6 +396,16 @@ class Dnn(_HostFeed):
                  for C, K in self.layers)
         if fused_update:
             ws = max([ws] + [B.fc_bwd_fused_sgd_workspace_bytes(N, C, K) for C, K in self.layers])
+        if not stored_logits:
+            C, K = self.layers[-1]
+            self.row_loss, self.lse = torch.empty(N, device=dev), torch.empty(N, device=dev)
+            ws = max([ws] + [B.fc_softmax_xent_workspace_bytes(N, C, K, B.F32, p) for p in (B.PASS_FWD, B.PASS_BWD_DATA)])
+        self.moments = {}
+        if hidden_update == "orthogonal":
+            for j in range(1, len(self.layers) - 1):
+                C, K = self.layers[j]
+                self.moments[j] = torch.zeros(K, C, device=dev)
+                ws = max(ws, B.orthogonalize_workspace_bytes(1, K, C))
         self.ws = torch.empty(max(ws, 256), dtype=torch.uint8, device=dev)
         self.fc_flops_fwd = [2 * N * C * K for C, K in self.layers]
 
@@ -386,7 +414,12 @@ class Dnn(_HostFeed):
     def dw(self, j): return self.store.g(2 * j)
     def db(self, j): return self.store.g(2 * j + 1)
 
+    def _step_state(self):
+        return [self.store.params, *self.moments.values()]
+
     def param_buckets(self):
+        if self.hidden_update != "sgd":
+            raise ValueError("the gradient exchange updates strips of the parameters: plain SGD only")
         return self.store.layer_buckets()
 
     def forward(self, before_layer=None):
@@ -395,6 +428,10 @@ class Dnn(_HostFeed):
         for j, (C, K) in enumerate(self.layers):
             if before_layer:
                 before_layer(j)
+            if j + 1 == n and not self.stored_logits:
+                B.fc_softmax_xent_fwd(self.N, C, K, a, self.w(j), self.b(j), self.labels, self.loss, self.row_loss, self.lse,
+                                      ws=self.ws)
+                return
             act = B.ACT_SIGMOID if j + 1 < n else B.ACT_NONE
             B.fc_fwd(self.N, C, K, a, self.w(j), self.b(j), self.out[j], act, self.ws)
             a = self.out[j]
@@ -406,21 +443,38 @@ class Dnn(_HostFeed):
             C, K = self.layers[j]
             a = self.out[j - 1] if j > 0 else self.x
             dx = self.dout[j - 1] if j > 0 else None          # first layer: no backpropagation
-            # dout[j] already is dz_j (the softmax gradient, or formed by the layer above together with db_j)
-            if self.fused_update:
-                B.fc_bwd_fused_sgd(self.N, C, K, a, self.w(j), None, B.ACT_NONE, self.dout[j], dx,
-                                   B.ACT_SIGMOID if j > 0 else B.ACT_NONE, self.db(j - 1) if j > 0 else None, self.lr,
-                                   self.db(j) if j + 1 == n else None, self.ws)
+            if j + 1 == n and not self.stored_logits:
+                B.fc_softmax_xent_bwd(self.N, C, K, a, self.w(j), self.b(j), self.labels, self.lse, None, dx, self.dw(j),
+                                      self.db(j), ws=self.ws)
+                if self.fused_update:
+                    B.sgd_update(self.w(j), self.dw(j), self.lr)
             else:
-                B.fc_bwd_fused(self.N, C, K, a, self.w(j), None, B.ACT_NONE, self.dout[j], dx,
-                               B.ACT_SIGMOID if j > 0 else B.ACT_NONE, self.db(j - 1) if j > 0 else None, self.dw(j),
-                               self.db(j) if j + 1 == n else None, self.ws)
+                # dout[j] already is dz_j (the softmax gradient, or formed by the layer above together with db_j), except
+                # below a loss without stored logits, which leaves the gradient of this layer's output
+                top = j + 1 == n
+                below_loss = j + 2 == n and not self.stored_logits
+                y, act = (self.out[j], B.ACT_SIGMOID) if below_loss else (None, B.ACT_NONE)
+                db = self.db(j) if top or below_loss else None
+                x_act, dx_db = (B.ACT_SIGMOID, self.db(j - 1)) if j > 0 else (B.ACT_NONE, None)
+                if self.fused_update:
+                    B.fc_bwd_fused_sgd(self.N, C, K, a, self.w(j), y, act, self.dout[j], dx, x_act, dx_db, self.lr, db, self.ws)
+                else:
+                    B.fc_bwd_fused(self.N, C, K, a, self.w(j), y, act, self.dout[j], dx, x_act, dx_db, self.dw(j), db, self.ws)
             if after_layer:
                 after_layer(j)
             if after_backprop:
                 after_backprop(j)
 
     def update(self):
+        if self.hidden_update == "orthogonal":
+            for j, (C, K) in enumerate(self.layers):
+                if j in self.moments:
+                    B.orthogonal_update(1, K, C, self.w(j), self.dw(j), self.moments[j], self.momentum, True, self.hidden_lr,
+                                        ws=self.ws)
+                else:
+                    B.sgd_update(self.w(j), self.dw(j), self.lr)
+                B.sgd_update(self.b(j), self.db(j), self.lr)
+            return
         t = self.store.tail_offset if self.fused_update else 0
         B.sgd_update(self.store.params[t:], self.store.grads[t:], self.lr)
 
