@@ -227,12 +227,19 @@ __device__ __forceinline__ void general_chunk(const Gemm16Params& p, const void*
 }
 // 32 rows of 64 bytes (32 fp16 values), swizzled over 64 bytes: sixteen-byte unit u of row r.
 __device__ __forceinline__ uint32_t half_tile_addr(uint32_t tile, uint32_t r, uint32_t u) { return tile + r * 64 + ((u ^ ((r >> 1) & 3)) << 4); }
-__device__ __forceinline__ void stage_half_row(uint32_t tile, int lane, const float (&v)[32]) {
+__device__ __forceinline__ void stage_half_row(uint32_t tile, int lane, const uint32_t (&h)[16]) {
 #pragma unroll
-    for (uint32_t u = 0; u < 4; ++u)
-        st_shared_u4(half_tile_addr(tile, lane, u), pack16(v[8 * u], v[8 * u + 1], false), pack16(v[8 * u + 2], v[8 * u + 3], false),
-                     pack16(v[8 * u + 4], v[8 * u + 5], false), pack16(v[8 * u + 6], v[8 * u + 7], false));
+    for (uint32_t u = 0; u < 4; ++u) st_shared_u4(half_tile_addr(tile, lane, u), h[4 * u], h[4 * u + 1], h[4 * u + 2], h[4 * u + 3]);
 }
+// Two fp32 multiply-adds in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 o;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(o.x), "=f"(o.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return o;
+}
+__device__ __forceinline__ float2 half2_value(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 // What the warps of a CTA share.
 struct Gemm16Shared {
@@ -466,16 +473,6 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             tma_load_3d_addr<false>(src_stg, tm_src, smem_u32(src_bar), col, row0, tile.b);
             if (kEpi == GEMM16_STEP) tma_load_3d_addr<false>(src_stg + 2048, tm_src_lo, smem_u32(src_bar), col, row0, tile.b);
         };
-        auto add_half8 = [&](uint32_t plane, int u, float scale, float* v) {
-            const float4 q = ld_shared_v4(half_tile_addr(plane, lane, u));
-            const uint32_t w[4] = {__float_as_uint(q.x), __float_as_uint(q.y), __float_as_uint(q.z), __float_as_uint(q.w)};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                v[2 * i] = fmaf(scale, f.x, v[2 * i]);
-                v[2 * i + 1] = fmaf(scale, f.y, v[2 * i + 1]);
-            }
-        };
 
         // ---- 32 columns of the finished accumulator (the code is kept short: a launch of a few microseconds fetches
         // every instruction from L2 once)
@@ -508,9 +505,15 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                 const float ref = nm == -INFINITY ? 0.f : nm;                 // (an empty chunk adds exp(-inf) = 0)
                 float add = 0.f;
                 if (fabsf(ref) < kScaledLimit) {
-                    const float ref2 = ref * kLog2e;
+                    const float2 l2 = make_float2(kLog2e, kLog2e), ref2 = make_float2(-ref * kLog2e, -ref * kLog2e);
+                    float2 two = make_float2(0.f, 0.f);
+                    const float2 one = make_float2(1.f, 1.f);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) add += ex2(fmaf(v[j], kLog2e, -ref2));
+                    for (int j = 0; j < 16; ++j) {
+                        const float2 e = fma2(make_float2(v[2 * j], v[2 * j + 1]), l2, ref2);
+                        two = fma2(make_float2(ex2(e.x), ex2(e.y)), one, two);
+                    }
+                    add = two.x + two.y;
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) add += ex2((v[j] - ref) * kLog2e);
@@ -518,33 +521,59 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                 sum = sum * ex2((mx - ref) * kLog2e) + add;
                 mx = nm;
             } else if constexpr (kEpi == GEMM16_SYM || kEpi == GEMM16_STEP) {
-                // fp16 tiles of 32 x 32
+                // fp16 tiles of 32 x 32, two elements at a time
+                float2 w[16];
+                const float2 al = make_float2(alpha, alpha), zero = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] *= alpha;
+                for (int j = 0; j < 16; ++j) w[j] = make_float2(v[2 * j], v[2 * j + 1]);
                 if (fetches) {                                                    // STEP: src + src_lo / 2^11, X to 22 bits
                     if (!bounded_wait_warp(src_bar, c.src_phase, &c.sh->abort_flag, c.status, WAIT_EPI_TMEM_FULL)) { ok = false; return; }
                     c.src_pending = false;
                     c.src_phase ^= 1u;
+                    const float2 be = make_float2(p.beta, p.beta), bl = make_float2(p.beta / kLoScale, p.beta / kLoScale);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if constexpr (kEpi == GEMM16_STEP) add_half8(src_stg + 2048, j, p.beta / kLoScale, &v[8 * j]);
-                        add_half8(src_stg, j, p.beta, &v[8 * j]);
+                    for (int u = 0; u < 4; ++u) {
+                        const float4 hi = ld_shared_v4(half_tile_addr(src_stg, lane, u));
+                        float4 lo;
+                        if constexpr (kEpi == GEMM16_STEP) lo = ld_shared_v4(half_tile_addr(src_stg + 2048, lane, u));
+                        const float h4[4] = {hi.x, hi.y, hi.z, hi.w};
+                        const float l4[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            float2& x = w[4 * u + i];
+                            float2 s = zero;
+                            if constexpr (kEpi == GEMM16_STEP) s = fma2(half2_value(__float_as_uint(l4[i])), bl, zero);
+                            x = fma2(x, al, fma2(half2_value(__float_as_uint(h4[i])), be, s));
+                        }
                     }
                     if (cc + 32 < kHalf && col + 32 < p.N) fetch(col + 32);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) w[j] = fma2(w[j], al, zero);
                 }
+                uint32_t h[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) h[j] = pack16(w[j].x, w[j].y, false);
                 staging_wait(lane);
-                stage_half_row(stg, lane, v);
+                stage_half_row(stg, lane, h);
                 const bool mirror = kEpi == GEMM16_SYM && p.symmetric && tile.n > tile.m;
                 if (mirror) {                                                 // transposed: this lane's row is column `lane`
 #pragma unroll
                     for (uint32_t j = 0; j < 32; ++j)
                         asm volatile("st.shared.b16 [%0], %1;" ::"r"(half_tile_addr(stg + 2048, j, lane >> 3) + (lane & 7) * 2),
-                                     "h"(__half_as_ushort(__float2half_rn(v[j]))) : "memory");
+                                     "h"(static_cast<unsigned short>(j & 1 ? h[j >> 1] >> 16 : h[j >> 1])) : "memory");
                 }
-                if (kEpi == GEMM16_STEP && tm_lo) {                        // what the rounding to fp16 left
+                if (kEpi == GEMM16_STEP && tm_lo) {                           // what the rounding to fp16 left (exact in fp32)
+                    const float2 minus = make_float2(-1.f, -1.f);
+                    const __half2 up = __float2half2_rn(kLoScale);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = (v[j] - __half2float(__float2half_rn(v[j]))) * kLoScale;
-                    stage_half_row(stg + 2048, lane, v);
+                    for (int j = 0; j < 16; ++j) {
+                        const float2 r = fma2(half2_value(h[j]), minus, w[j]);
+                        const uint32_t q = pack16(r.x, r.y, false);
+                        const __half2 s = __hmul2(*reinterpret_cast<const __half2*>(&q), up);
+                        h[j] = *reinterpret_cast<const uint32_t*>(&s);
+                    }
+                    stage_half_row(stg + 2048, lane, h);
                 }
                 if (row0 < p.M) {
                     fence_proxy_async_shared();
@@ -606,7 +635,10 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] -= j == rel ? 1.f : 0.f;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = g == 0.f ? 0.f : g * v[j];      // (rows left out: exactly 0, whatever z is)
+                    for (int j = 0; j < 32; ++j) v[j] *= g;
+                    if (g == 0.f)                                                 // rows left out: exactly 0, whatever z is
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = 0.f;
                 } else {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] *= alpha;
@@ -761,7 +793,7 @@ inline int operand_tmap(CUtensorMap* tm, const Gemm16Operand& o, int rows, int K
 
 // Pairs or single CTAs, and in how many parts the last wave's reductions are cut.  Times in microseconds, from launches of the
 // four forms on a B200: a 64-deep block takes its MMAs' time (0.27 pair, 0.135 single) or that of its copies, 32 KB per CTA at
-// the 9.5 TB/s or more that L2 delivers to all SMs together (0.40 when the GPU is full); start and a tile's epilogue that nothing
+// the 11.8 TB/s that L2 delivers to all SMs together (0.41 when the GPU is full); start and a tile's epilogue that nothing
 // overlaps 6 (pair) or 5, and 1.5 more where it writes a mirror image (so the whole of a small symmetric result is computed
 // where there are SMs to spare); a part costs its trip through L2, 1.2 (128 KB per CTA) or 0.6, plus 4 for the count.
 struct Plan16 { bool pair, mirrored; int splits, part_blocks; long tiles, full_tiles; double time; };
@@ -782,7 +814,7 @@ inline Plan16 plan16(const Gemm16Args& a) {
         const long tile = pair ? 256 : 128, slots = pair ? sms / 2 : sms;
         const long mt = (a.M + tile - 1) / tile, nt = (a.N + tile - 1) / tile;
         const long tiles = (mirrored ? mt * (mt + 1) / 2 : mt * nt) * a.batch;
-        const double mma = pair ? 0.27 : 0.135, copy = (pair ? 2.0 : 1.0) * 32768.0 / 9.5e6, epi = (pair ? 6.0 : 5.0) + (mirrored ? 1.5 : 0.0);
+        const double mma = pair ? 0.27 : 0.135, copy = (pair ? 2.0 : 1.0) * 32768.0 / 11.8e6, epi = (pair ? 6.0 : 5.0) + (mirrored ? 1.5 : 0.0);
         auto block = [&](long active) { return mma > copy * active ? mma : copy * active; };
         const long whole = tiles / slots, rest = tiles - whole * slots;
         for (long s = 1; s <= 16 && (s == 1 || (joins && rest > 0 && s * rest <= kMostParts)); ++s) {
