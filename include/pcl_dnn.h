@@ -8,7 +8,8 @@
  * -------------------------------------------
  *  - All tensor pointers are DEVICE pointers to fp32 data (void*: of the call's
  *    dtype), contiguous, and at least 16-byte aligned.  The caller owns every buffer, including the
- *    workspace; the library allocates no device memory.
+ *    workspace; the library allocates no device memory.  Calls that may overlap
+ *    on the GPU (other streams, other captured graphs) need workspaces of their own.
  *  - Layouts: activations and their gradients are NHWC (N minibatch, H x W
  *    feature map, C feature maps innermost); convolution weights and their
  *    gradients are KRSC (K output maps, R x S kernel, C input maps innermost);
@@ -70,7 +71,9 @@ enum { PCL_PASS_FWD = 0, PCL_PASS_BWD_DATA = 1, PCL_PASS_BWD_WEIGHTS = 2 };
 /* Which kernel family the conv / fc calls use.  PCL_PATH_AUTO picks the tensor
  * core (tcgen05 TF32) kernels whenever the shape is eligible and the generic
  * CUDA-core kernels otherwise; the other two values force one family (a forced
- * tensor-core path returns PCL_ERR_UNSUPPORTED_SHAPE on ineligible shapes).
+ * tensor-core path returns PCL_ERR_UNSUPPORTED_SHAPE on ineligible shapes; so does
+ * the forced generic path in the calls that have tensor-core kernels only: 16-bit
+ * pcl_fc_softmax_xent_* and the orthogonalised update).
  * Process-wide setting, intended for tests. */
 enum { PCL_PATH_AUTO = 0, PCL_PATH_TENSOR = 1, PCL_PATH_GENERIC = 2 };
 int pcl_set_path(int path);

@@ -1149,8 +1149,12 @@ int embedding_bwd_impl(int N, int V, int C, int dtype, const int* ids, const voi
     if (rc != PCL_OK) return rc;
     return launch_embedding_bwd(N, V, C, dtype, ids, dy, scale, pad_id, out, sgd, lr, ws, static_cast<cudaStream_t>(cuda_stream));
 }
-int check_vocab_loss(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels) {
+int check_vocab_loss(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels, bool backward) {
     if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || !x || !w || !labels) return PCL_ERR_BAD_ARG;
+    // fp32 runs on the FC kernels: a forced tensor-core path takes what they take (checked here, before anything is launched),
+    // and the 16-bit products have tensor-core kernels only
+    if (dtype == PCL_F32 && g_path.load() == PCL_PATH_TENSOR && (C % 4 != 0 || (backward && K % 4 != 0))) return PCL_ERR_UNSUPPORTED_SHAPE;
+    if (dtype != PCL_F32 && g_path.load() == PCL_PATH_GENERIC) return PCL_ERR_UNSUPPORTED_SHAPE;
     return aligned16(x) && aligned16(w) && aligned16(bias) && aligned16(labels) ? PCL_OK : PCL_ERR_MISALIGNED;
 }
 }  // namespace
@@ -1184,7 +1188,7 @@ size_t pcl_fc_softmax_xent_workspace_bytes(int N, int C, int K, int dtype, int p
 int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels,
                             int ignore_label, float* loss, float* row_loss, float* lse, void* ws, size_t ws_bytes,
                             void* cuda_stream) {
-    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels);
+    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels, false);
     if (rc != PCL_OK) return rc;
     if (!loss || !row_loss || !lse) return PCL_ERR_BAD_ARG;
     if (!aligned16(loss) || !aligned16(row_loss) || !aligned16(lse)) return PCL_ERR_MISALIGNED;
@@ -1197,7 +1201,7 @@ int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const
 int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels,
                             int ignore_label, const float* lse, const float* row_grad, void* dx, void* dw, void* dbias,
                             void* ws, size_t ws_bytes, void* cuda_stream) {
-    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels);
+    int rc = check_vocab_loss(N, C, K, dtype, x, w, bias, labels, true);
     if (rc != PCL_OK) return rc;
     if (!lse || !dw) return PCL_ERR_BAD_ARG;
     if (!aligned16(lse) || !aligned16(row_grad) || !aligned16(dx) || !aligned16(dw) || !aligned16(dbias)) return PCL_ERR_MISALIGNED;
@@ -1211,6 +1215,7 @@ namespace {
 int check_ortho(int count, int M, int N, int dtype, int steps, const void* a, const void* b) {
     if (count <= 0 || M <= 0 || N <= 0 || steps <= 0 || !known_dtype(dtype) || !a || !b) return PCL_ERR_BAD_ARG;
     if (count > 65535) return PCL_ERR_UNSUPPORTED_SHAPE;     // (a grid dimension)
+    if (g_path.load() == PCL_PATH_GENERIC) return PCL_ERR_UNSUPPORTED_SHAPE;      // (tensor-core kernels only)
     return aligned16(a) && aligned16(b) ? PCL_OK : PCL_ERR_MISALIGNED;
 }
 }  // namespace

@@ -314,3 +314,34 @@ def test_short_workspace_is_refused():
         B.fc_softmax_xent_fwd(40, 64, 100, c.x, c.w, None, c.labels, torch.empty(1, device="cuda"), torch.empty(40, device="cuda"),
                               torch.empty(40, device="cuda"), ws=short)
     assert e.value.code == B.ERR_WORKSPACE
+
+
+def test_offsets_beyond_32_bits():
+    """Weights and their gradient of more than 2^31 elements: the classes at the end are read and written in place."""
+    N, C, K = 24, 4096, 530000
+    w = torch.zeros(K, C, dtype=torch.bfloat16, device="cuda")
+    dw = torch.empty_like(w)
+    g = torch.Generator(device="cuda").manual_seed(18)
+    x = torch.randn(N, C, device="cuda", generator=g).bfloat16()
+    w[K - 40:] = (torch.randn(40, C, device="cuda", generator=g) / 8).bfloat16()
+    labels = torch.randint(K - 40, K, (N,), device="cuda", generator=g).int()
+    loss, row, lse, dx = torch.empty(1, device="cuda"), torch.empty(N, device="cuda"), torch.empty(N, device="cuda"), torch.empty_like(x)
+    ws = workspace(max(B.fc_softmax_xent_workspace_bytes(N, C, K, B.BF16, p) for p in (B.PASS_FWD, B.PASS_BWD_DATA)))
+    B.fc_softmax_xent_fwd(N, C, K, x, w, None, labels, loss, row, lse, ws=ws)
+    B.fc_softmax_xent_bwd(N, C, K, x, w, None, labels, lse, None, dx, dw, None, ws=ws)
+    B.check_device_status()
+    check_guards()
+    z = x.double() @ w[K - 40:].double().t()
+    ref = torch.logsumexp(torch.cat([z, torch.full((N, 1), math.log(K - 40), device="cuda", dtype=torch.float64)], 1), 1)
+    # z off by 4098 * 2^-23 of the sum of its terms' sizes at most, and the sums of K terms
+    ez = 4098 * 2.0 ** -23 * float((x.double().abs() @ w[K - 40:].double().abs().t()).max())
+    assert bool(((lse.double() - ref).abs() <= ez + 2.0 ** -10).all())
+    p = torch.exp(z - ref[:, None])
+    p.scatter_add_(1, (labels.long() - (K - 40))[:, None], torch.full((N, 1), -1.0, device="cuda", dtype=torch.float64))
+    want = (p / N).t() @ x.double()
+    # dz and the result are rounded to bf16 (2^-8 each of their terms' sizes), p is off by the error of z and lse
+    bound = (p.abs() / N * (2.0 ** -8 + 2 * ez + 2.0 ** -9) + 2.0 ** -9 * (p.abs() + 1) / N * 2 * ez).t() @ x.double().abs() + 2.0 ** -8 * want.abs() + 1e-9
+    assert bool(((dw[K - 40:].double() - want).abs() <= bound).all())
+    # everywhere else p is the same tiny number
+    tiny = float(torch.exp(-ref).max()) / N * float(x.double().abs().sum(0).max()) * 1.1
+    assert float(dw[: K - 40 : 997].abs().max()) <= tiny

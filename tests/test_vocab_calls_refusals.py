@@ -100,3 +100,20 @@ def test_binding_checks_types_and_sizes(B):
         B.embedding_fwd(4, 4, 8, ids.int(), a, 1.0, a.clone())
     with pytest.raises(B.PclError):
         B.orthogonalize(0, 4, 8, a, a)
+
+
+def test_forced_kernel_families(B):
+    """A forced family that a call cannot run on is refused before anything is launched."""
+    L = B.lib()
+    big = 1 << 40
+    loss = lambda C, K, d: L.pcl_fc_softmax_xent_bwd(4, C, K, d, OK16, OK16, NULL, OK16, -1, OK16, NULL, NULL, OK16, NULL, OK16, big, NULL)
+    fwd = lambda C, K, d: L.pcl_fc_softmax_xent_fwd(4, C, K, d, OK16, OK16, NULL, OK16, -1, OK16, OK16, OK16, OK16, big, NULL)
+    try:
+        B.set_path(B.PATH_TENSOR)
+        assert loss(6, 8, B.F32) == B.ERR_UNSUPPORTED_SHAPE and loss(8, 7, B.F32) == B.ERR_UNSUPPORTED_SHAPE
+        assert fwd(6, 8, B.F32) == B.ERR_UNSUPPORTED_SHAPE
+        B.set_path(B.PATH_GENERIC)
+        assert fwd(8, 8, B.BF16) == B.ERR_UNSUPPORTED_SHAPE and loss(8, 8, B.F16) == B.ERR_UNSUPPORTED_SHAPE
+        assert L.pcl_orthogonalize(1, 8, 8, B.F32, OK16, OK16, 5, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+    finally:
+        B.set_path(B.PATH_AUTO)
