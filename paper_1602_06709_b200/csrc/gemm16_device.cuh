@@ -44,7 +44,11 @@ __device__ __forceinline__ int divide(int n, const FastDiv& f) {
 struct Gemm16Params {
     int M, N, k_blocks, last_slices, batch;
     int m_tiles, n_tiles;
-    FastDiv per_matrix, per_group, by_splits;        // tiles of a matrix; of kGroupM rows of tiles; parts of a tile
+    // The order of the tiles: the whole ones of all matrices, then those of the ragged last row, then those of the ragged last
+    // column (so the cheap ones come last).
+    int m_whole, n_whole, core_tiles, bottom_tiles;  // whole rows and columns of tiles; tiles of the first two kinds
+    FastDiv by_core, by_group, by_bottom, by_right;  // tiles of one matrix of each kind; of kGroupM rows of whole tiles
+    FastDiv by_splits;                               // parts of a tile
     int full_tiles, splits, part_blocks, items;      // tiles [0, full_tiles) are one item each, the others `splits`
     int* counters; float4* parts;                    // of the split tiles
     int symmetric, bf16;
@@ -108,6 +112,9 @@ __device__ __forceinline__ void st_shared_u4(uint32_t addr, uint32_t x, uint32_t
 
 // Work item: a tile of one matrix and the reduction blocks [k0, k1) of it; part < 0: all of them.
 struct Item16 { int b, m, n, k0, k1, part, split_tile; };
+// A CTA's (pair's) items: one of each wave, in turn from the wave's front and from its back, so that with items in the order of
+// falling cost all CTAs get about the same (8200 x 4100 update, 4100 being 16 tiles and 4 columns: its square product 88 -> 75 us,
+// the whole 2.49 -> 2.44 ms).  hop in the roles' loops: the steps to the next item, in turn.
 // Columns the MMAs of a tile compute: the last tile's are rounded up to 32.
 __device__ __forceinline__ int tile_width(const Gemm16Params& p, int n, int bn) {
     const int left = p.N - n * bn;
@@ -125,19 +132,33 @@ __device__ __forceinline__ Item16 decode_item(const Gemm16Params& p, int i) {
         o.k0 = o.part * p.part_blocks;
         o.k1 = o.k0 + p.part_blocks < p.k_blocks ? o.k0 + p.part_blocks : p.k_blocks;
     }
-    o.b = divide(t, p.per_matrix);
-    int r = t - o.b * int(p.per_matrix.d);
-    if (p.symmetric) {                       // tiles (m, n >= m), row by row
-        int m = 0;
-        while (r >= p.n_tiles - m) { r -= p.n_tiles - m; ++m; }
-        o.m = m; o.n = m + r;
+    if (t < p.core_tiles) {
+        o.b = divide(t, p.by_core);
+        int r = t - o.b * int(p.by_core.d);
+        if (p.symmetric) {                       // tiles (m, n >= m), row by row
+            int m = 0;
+            while (r >= p.n_whole - m) { r -= p.n_whole - m; ++m; }
+            o.m = m; o.n = m + r;
+            return o;
+        }
+        const int g = divide(r, p.by_group);
+        r -= g * int(p.by_group.d);
+        const int left = p.m_whole - g * kGroupM;
+        if (left >= kGroupM) { o.n = r / kGroupM; o.m = g * kGroupM + (r - o.n * kGroupM); }
+        else { o.n = r / left; o.m = g * kGroupM + (r - o.n * left); }
         return o;
     }
-    const int g = divide(r, p.per_group);
-    r -= g * int(p.per_group.d);
-    const int left = p.m_tiles - g * kGroupM;
-    if (left >= kGroupM) { o.n = r / kGroupM; o.m = g * kGroupM + (r - o.n * kGroupM); }
-    else { o.n = r / left; o.m = g * kGroupM + (r - o.n * left); }
+    t -= p.core_tiles;
+    if (t < p.bottom_tiles) {
+        o.b = divide(t, p.by_bottom);
+        o.n = t - o.b * int(p.by_bottom.d);
+        o.m = p.m_whole;
+    } else {
+        t -= p.bottom_tiles;
+        o.b = divide(t, p.by_right);
+        o.m = t - o.b * int(p.by_right.d);
+        o.n = p.n_whole;
+    }
     return o;
 }
 
@@ -314,7 +335,7 @@ __device__ __forceinline__ bool produce_items(Gemm16Ctx& c, const Gemm16Params& 
     constexpr int kTileM = kPair ? 256 : 128, kBN = kTileM;
     const uint32_t full0 = smem_u32(&c.sh->full_bar[0]), empty0 = smem_u32(&c.sh->empty_bar[0]);
     const uint32_t full_dst0 = kPair ? map_to_cta(&c.sh->full_bar[0], 0) : full0;
-    for (int t = c.first; t < p.items;) {
+    for (int t = c.first, hop = 2 * (c.stride - c.first) - 1; t < p.items;) {
         const int ra = tile.m * kTileM + int(c.pair_rank) * 128;
         const int rb = tile.n * kBN + (kPair ? int(c.pair_rank) * (tile_width(p, tile.n, kBN) / 2) : 0);
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
@@ -336,7 +357,8 @@ __device__ __forceinline__ bool produce_items(Gemm16Ctx& c, const Gemm16Params& 
             ++c.issued;
             if (++c.stage == c.stages) { c.stage = 0; c.phase ^= 1u; }
         }
-        t += c.stride;
+        t += hop;
+        hop = 2 * c.stride - hop;
         if (t < p.items) tile = decode_item(p, t);
     }
     return true;
@@ -369,7 +391,7 @@ __device__ __forceinline__ bool issue_items(Gemm16Ctx& c, const Gemm16Params& p)
     const uint32_t a_hi = uint32_t(da >> 32), b_hi = uint32_t(db >> 32), a_lo0 = uint32_t(da), b_lo0 = uint32_t(db);
     const uint32_t full0 = smem_u32(&c.sh->full_bar[0]), empty0 = smem_u32(&c.sh->empty_bar[0]);
     const uint32_t af0 = smem_u32(&c.sh->acc_full_bar[0]), ae0 = smem_u32(&c.sh->acc_empty_bar[0]);
-    for (int t = c.first; t < p.items; t += c.stride) {
+    for (int t = c.first, hop = 2 * (c.stride - c.first) - 1; t < p.items; t += hop, hop = 2 * c.stride - hop) {
         const Item16 tile = decode_item(p, t);
         const uint32_t idesc = idesc0 | (uint32_t(tile_width(p, tile.n, kBN)) >> 3 << 17);
         for (int kb = tile.k0; kb < tile.k1; ++c.it) {
@@ -431,7 +453,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             else mbar_arrive(&c.sh->acc_empty_bar[buf]);
         }
     };
-    for (int t = c.first; t < p.items && ok; t += c.stride) {
+    for (int t = c.first, hop = 2 * (c.stride - c.first) - 1; t < p.items && ok; t += hop, hop = 2 * c.stride - hop) {
         const Item16 tile = decode_item(p, t);
         const int row0 = tile.m * kTileM + int(c.pair_rank) * 128 + quarter * 32, row = row0 + lane;
         const int cbase = tile.n * kBN + half * kHalf;
@@ -814,14 +836,33 @@ inline Plan16 plan16(const Gemm16Args& a) {
         const long tile = pair ? 256 : 128, slots = pair ? sms / 2 : sms;
         const long mt = (a.M + tile - 1) / tile, nt = (a.N + tile - 1) / tile;
         const long tiles = (mirrored ? mt * (mt + 1) / 2 : mt * nt) * a.batch;
+        // whole tiles, and those of the ragged last row and column: the first copies less, the second also has narrower MMAs
+        const long mw = a.M / tile, nw = a.N / tile;
+        const long core = (mirrored ? nw * (nw + 1) / 2 : mw * nw) * a.batch, bottom = mirrored || mt == mw ? 0 : nw * a.batch;
+        const long right = nt == nw ? 0 : mt * a.batch;
+        const double fm = double(a.M - mw * tile) / tile, fn = double(a.N - nw * tile) / tile;
         const double mma = pair ? 0.27 : 0.135, copy = (pair ? 2.0 : 1.0) * 32768.0 / 11.8e6, epi = (pair ? 6.0 : 5.0) + (mirrored ? 1.5 : 0.0);
-        auto block = [&](long active) { return mma > copy * active ? mma : copy * active; };
-        const long whole = tiles / slots, rest = tiles - whole * slots;
-        for (long s = 1; s <= 16 && (s == 1 || (joins && rest > 0 && s * rest <= kMostParts)); ++s) {
+        struct Costs { double core, bottom, right; };
+        auto block = [&](long active) {
+            auto most = [](double x, double y) { return x > y ? x : y; };
+            return Costs{most(mma, copy * active), most(mma, copy * active * (1.0 + fm) / 2), most(mma * most(fn, 0.5), copy * active * (1.0 + fn) / 2)};
+        };
+        const Costs full = block(slots);
+        const long whole = core / slots;
+        for (long s = 1; s <= 16 && (s == 1 || (joins && s * (tiles - whole * slots) <= kMostParts)); ++s) {
             const long part = (kb + s - 1) / s, splits = (kb + part - 1) / part;
-            if (splits != s) continue;
-            const long waves = (rest * s + slots - 1) / slots;
-            const double t = whole * kb * block(slots) + waves * part * block(waves > 1 ? slots : rest * s) + epi + (s > 1 ? 4.0 + s * (pair ? 1.2 : 0.6) : 0.0);
+            if (splits != s || (s > 1 && tiles == whole * slots)) continue;
+            const long c1 = (core - whole * slots) * s, items = c1 + (bottom + right) * s;
+            double last = 0.0;                               // of the items behind the whole waves
+            if (items <= slots) {
+                const Costs one = block(whole ? slots : items);
+                last = c1 ? one.core : bottom ? one.bottom : right ? one.right : 0.0;
+            } else {
+                const double waves = double((c1 + slots - 1) / slots) * full.core, end = right ? full.right : bottom ? full.bottom : 0.0;
+                const double even = (c1 * full.core + s * (bottom * full.bottom + right * full.right)) / slots + end / 2;
+                last = waves > even ? waves : even;
+            }
+            const double t = whole * kb * full.core + part * last + epi + (s > 1 ? 4.0 + s * (pair ? 1.2 : 0.6) : 0.0);
             if (t < best.time) best = Plan16{pair, mirrored, int(s), int(part), tiles, s > 1 ? whole * slots : tiles, t};
         }
     }
@@ -838,8 +879,17 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
     p.m_tiles = (a.M + tile - 1) / tile;
     p.n_tiles = (a.N + tile - 1) / tile;
     if (pl.tiles > 2000000000L) return PCL_ERR_UNSUPPORTED_SHAPE;
-    p.per_matrix = fast_div(unsigned(pl.tiles / a.batch));
-    p.per_group = fast_div(unsigned(kGroupM * p.n_tiles));
+    p.m_whole = a.M / tile;
+    p.n_whole = a.N / tile;
+    const long core = pl.mirrored ? long(p.n_whole) * (p.n_whole + 1) / 2 : long(p.m_whole) * p.n_whole;
+    const int bottom = pl.mirrored || p.m_tiles == p.m_whole ? 0 : p.n_whole;
+    p.core_tiles = int(core * a.batch);
+    p.bottom_tiles = bottom * a.batch;
+    auto divisor = [](long d) { return fast_div(unsigned(d > 0 ? d : 1)); };       // (0: no tile of the kind)
+    p.by_core = divisor(core);
+    p.by_group = divisor(long(kGroupM) * p.n_whole);
+    p.by_bottom = divisor(bottom);
+    p.by_right = divisor(p.m_tiles);
     p.by_splits = fast_div(unsigned(pl.splits));
     p.full_tiles = int(pl.full_tiles); p.splits = pl.splits; p.part_blocks = pl.part_blocks;
     p.items = int(pl.full_tiles + (pl.tiles - pl.full_tiles) * pl.splits);

@@ -188,9 +188,10 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     OrthoLayout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
-    l.ld = int(align_up(N, 8));
+    // rows of whole 128-byte lines: TMA writes a row of a tile into other rows' sectors otherwise (8200 x 4100: 2.44 -> 2.03 ms)
+    l.ld = int(align_up(N, 64));
     l.d = M < N ? M : N;
-    l.ldd = int(align_up(l.d, 8));
+    l.ldd = int(align_up(l.d, 64));
     l.form = ortho_form(count, M, N);
     l.part = take(size_t(count) * kMaxNormBlocks * 8);
     l.xl = take(size_t(count) * M * l.ld * 2);

@@ -27,19 +27,30 @@ __device__ __forceinline__ float elem16(const void* p, int type, size_t i) {
     return __half2float(static_cast<const __half*>(p)[i]);
 }
 
-// Rows whose length is no multiple of 8 elements cannot be read by TMA (16-byte strides): they are copied to padded rows.
+// Where C is no multiple of 8, x and w are copied to padded rows (TMA needs strides of 16 bytes): a warp per row, 16 bytes per
+// store, at the rate of memory (1024 rows, 1001 -> 50021: 33 us of 132).  Rows of whole 128-byte lines, where TMA reads a row
+// of a tile from one line instead of two, are not worth a copy by themselves (3001 rows, 1032 -> 50021: forward 275 -> 266 us,
+// backward 914 -> 876, but 1024 rows 97 -> 116 and 377 -> 394).
 __global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restrict__ src, uint16_t* __restrict__ dst, long rows,
                                                        int C, int ldc) {
     grid_dependency_wait();
     grid_dependents_launch();
-    for (long r = blockIdx.x; r < rows; r += gridDim.x)
-        for (int c = threadIdx.x; c < ldc; c += blockDim.x) dst[r * ldc + c] = c < C ? src[r * C + c] : uint16_t(0);
+    for (long r = blockIdx.x * 8l + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8l) {
+        const uint16_t* row = src + r * C;
+#pragma unroll 2
+        for (int c = (threadIdx.x & 31) * 8; c < ldc; c += 256) {
+            uint32_t e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = c + i < C ? __ldg(row + c + i) : 0u;
+            *reinterpret_cast<uint4*>(dst + r * ldc + c) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+        }
+    }
 }
 int launch_pad_rows(const void* src, void* dst, long rows, int C, int ldc, cudaStream_t st) {
     LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(rows) * C, st);
-    const long cap = long(device_sm_count()) * 16;
-    return launch_chained(pad_rows_kernel, dim3(unsigned(rows < cap ? rows : cap)), dim3(256), 0, st, 1, static_cast<const uint16_t*>(src),
-                          static_cast<uint16_t*>(dst), rows, C, ldc);
+    const long cap = long(device_sm_count()) * 8, blocks = (rows + 7) / 8;
+    return launch_chained(pad_rows_kernel, dim3(unsigned(blocks < cap ? blocks : cap)), dim3(256), 0, st, 1,
+                          static_cast<const uint16_t*>(src), static_cast<uint16_t*>(dst), rows, C, ldc);
 }
 
 // (max, sum of exp(z - max)) pairs of disjoint sets of classes, joined.  A set without a finite logit is (-inf, 0).
@@ -279,9 +290,11 @@ int piece_classes(int N, int K, size_t elem_bytes) {
     if (p < 256) p = 256;
     return p < size_t(K) ? int(p) : K;
 }
+// Row length of the padded copies: whole 128-byte lines, unless that more than doubles a row.
+int staged_ld(int C) { return int(align_up(C, C >= 64 ? 64 : 8)); }
 // Rows of w that are staged at a time where C is no multiple of 8.
 int stage_classes(int C, int K) {
-    size_t p = kPieceBytes / (align_up(C, 8) * 2) / 256 * 256;
+    size_t p = kPieceBytes / (size_t(staged_ld(C)) * 2) / 256 * 256;
     if (p < 256) p = 256;
     return p < size_t(K) ? int(p) : K;
 }
@@ -308,13 +321,14 @@ Gemm16Args dw_args(int N, int C, int P, bool bf16) {
     return a;
 }
 
-struct Layout { size_t part, label_z, row_scale, alpha, xs, wst, dz, dx, fc, split, split_bytes, total; int piece, parts, k_parts, ldc, ldp; };
+struct Layout { size_t part, label_z, row_scale, alpha, xs, wst, dz, dx, fc, split, split_bytes, total; int piece, parts, k_parts, ldc, ldp; bool stage; };
 Layout layout(int N, int C, int K, int type, bool backward) {
     Layout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
-    l.ldc = int(align_up(C, 8));
-    const bool stage = type != DT_F32 && C % 8 != 0, bf16 = type == DT_BF16;
+    const bool stage = l.stage = type != DT_F32 && C % 8 != 0;
+    const bool bf16 = type == DT_BF16;
+    l.ldc = stage ? staged_ld(C) : C;
     l.alpha = take(4);
     auto split = [&](const Gemm16Args& a) {
         const size_t b = gemm16_split_ws_bytes(a);
@@ -391,7 +405,7 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
         }
         parts = part_ld = 1;
     } else {
-        const bool stage = C % 8 != 0;
+        const bool stage = l.stage;
         const void* xs = x;
         if (stage) {
             rc = launch_pad_rows(x, base + l.xs, N, C, l.ldc, st);
@@ -474,7 +488,7 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
         }
         return PCL_OK;
     }
-    const bool stage = C % 8 != 0, bf16 = type == DT_BF16;
+    const bool stage = l.stage, bf16 = type == DT_BF16;
     uint16_t* dz = reinterpret_cast<uint16_t*>(base + l.dz);
     float* dx_acc = reinterpret_cast<float*>(base + l.dx);
     const void* xs = x;
