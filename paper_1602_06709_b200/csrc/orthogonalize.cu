@@ -4,14 +4,15 @@
 //
 // Every product runs on the 16-bit tensor cores with fp16 operands scaled by powers of two: all values are bounded (|X|, |A|
 // <= 1.5, |B| <= 2.9 by the polynomial), so fp16 has the three mantissa bits that bf16 lacks at no loss of range.  X
-// itself keeps 22 bits until the last step, in two fp16 planes of which the products see the first; the last step takes the rounded X in its linear term too, so that the
-// rounding is passed on by the polynomial's derivative (which is small at 1) instead of by B alone.  Relative error of the
-// result (2-norm) 3e-4 .. 1.6e-3 on random, decaying and nearly low-rank spectra, where bf16 iterates give 1e-2 .. 2e-1.
+// itself keeps 22 bits until the last step, in two fp16 planes of which the products see the first; the last step takes the
+// rounded X in its linear term too, so that the rounding is passed on by the polynomial's derivative (which is small at 1)
+// instead of by B alone.  Relative error of the result (2-norm) 3e-4 .. 1.6e-3 on random, decaying and nearly low-rank
+// spectra, where bf16 iterates give 1e-2 .. 2e-1.  (Narrow matrices: orthogonalize_narrow.cu.)
 // A and A A are symmetric: the tiles below the diagonal are copies of those above it.
 //
 // All 3 * steps products run in ONE cooperative launch (the roles of the 16-bit GEMM, see tc_gemm16.cu, one product after
 // another) with a barrier of all CTAs between them: a launch of its own costs every product its set-up and the fetching
-// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 118 -> 75 us).
+// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 122 -> 102 us).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -347,9 +348,12 @@ int launch_ortho_kernel(const OrthoParams& o, cudaStream_t st) {
 
 }  // namespace
 
-size_t orthogonalize_workspace_bytes(int count, int M, int N) { return ortho_layout(count, M, N).total; }
+size_t orthogonalize_workspace_bytes(int count, int M, int N) {
+    return orthogonalize_is_narrow(count, M, N) ? orthogonalize_narrow_workspace_bytes(count, M, N) : ortho_layout(count, M, N).total;
+}
 
 int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
+    if (orthogonalize_is_narrow(o.count, o.M, o.N)) return launch_orthogonalize_narrow(o, ws, st);
     const OrthoLayout l = ortho_layout(o.count, o.M, o.N);
     char* base = static_cast<char*>(ws);
     __half* xl = reinterpret_cast<__half*>(base + l.xl);

@@ -383,6 +383,10 @@ struct OrthoArgs {
 };
 size_t orthogonalize_workspace_bytes(int count, int M, int N);
 int launch_orthogonalize(const OrthoArgs& a, void* ws, cudaStream_t st);
+// of matrices with a short side (orthogonalize_narrow.cu); the two above go there where that is so
+bool orthogonalize_is_narrow(int count, int M, int N);
+size_t orthogonalize_narrow_workspace_bytes(int count, int M, int N);
+int launch_orthogonalize_narrow(const OrthoArgs& a, void* ws, cudaStream_t st);
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 

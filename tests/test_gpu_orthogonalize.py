@@ -175,3 +175,95 @@ def test_update_graph_replay():
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(w, we) and torch.equal(m, me)
+
+
+# ---- narrow matrices: the steps run on d x d matrices in 64 bits, the result is one product in fp32
+def narrow_reference(u, steps=5):
+    """X and |P| |X0| in float64, with X = P X0 (the transpose of tall matrices)."""
+    outs, sizes = [], []
+    for m in u.double():
+        flip = m.shape[0] > m.shape[1]
+        m = m.t() if flip else m
+        x0 = m / (m.norm() + EPS)
+        p, a = torch.eye(m.shape[0], dtype=torch.float64, device=m.device), x0 @ x0.t()
+        for _ in range(steps):
+            q = A_ * torch.eye(m.shape[0], dtype=torch.float64, device=m.device) + B_ * a + C_ * (a @ a)
+            p, a = q @ p, q @ a @ q
+        out, size = p @ x0, p.abs() @ x0.abs()
+        outs.append(out.t() if flip else out)
+        sizes.append(size.t() if flip else size)
+    return torch.stack(outs), torch.stack(sizes)
+
+
+def narrow_bound(ref, size, d, t):
+    # X0 and P rounded to fp32, d multiply-adds and 1 / |U| rounded (half a step, 2^-24 of the terms' sizes, each), the 64-bit
+    # steps' 1e-11, and the result's rounding (fp16: its subnormals are absolute)
+    return (d + 4) * 2.0 ** -24 * size + half_step(t) * ref.abs() * (1 + 2.0 ** -10) + 2.0 ** -25
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("count,d,k", [(1, 1, 1), (2, 1, 70), (1, 7, 7), (3, 16, 64), (1, 17, 63), (1, 23, 1367), (2, 32, 65), (1, 33, 200),
+                                       (1, 50, 50), (5, 64, 129), (1, 64, 4096), (1, 31, 20000), (40, 9, 100), (33, 32, 130)])
+@pytest.mark.parametrize("tall", [False, True])
+def test_narrow(t, count, d, k, tall):
+    M, N = (k, d) if tall else (d, k)
+    g = guarded((count, M, N), t, fill=0)
+    g.copy_(spectrum(count, M, N, "gauss", d + k))
+    got = run(g)
+    ref, size = narrow_reference(g)
+    assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, d, t)).all())
+    assert torch.equal(got, run(g))
+
+
+@pytest.mark.parametrize("kind", ["lowrank", "decay", "flat", "steep"])
+@pytest.mark.parametrize("count,M,N", [(2, 64, 500), (40, 300, 24)])
+def test_narrow_spectra(kind, count, M, N):
+    g = guarded((count, M, N), torch.float32, fill=0)
+    g.copy_(spectrum(count, M, N, "decay" if kind == "steep" else kind, 3))
+    if kind == "steep":                          # singular values down to 1e-5 of the largest
+        g.mul_(torch.logspace(0, -5, M if M < N else N, device="cuda").view(*((-1, 1) if M < N else (1, -1))))
+    got = run(g)
+    ref, size = narrow_reference(g)
+    assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, min(M, N), torch.float32)).all())
+
+
+@pytest.mark.parametrize("steps", [1, 2, 7])
+def test_narrow_steps(steps):
+    g = guarded((1, 30, 90), torch.float32, fill=0)
+    g.copy_(spectrum(1, 30, 90, "gauss", 9))
+    got = run(g, steps)
+    ref, size = narrow_reference(g, steps)
+    # (seven steps let roundings of small singular values grow to 12^2 times the 1e-11 of five)
+    assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, 30, torch.float32) + 1e-9).all())
+
+
+def test_narrow_matrices_in_tensor_core_form():
+    """Many matrices of 33 to 64 rows run on the tensor cores."""
+    g = guarded((36, 50, 140), torch.bfloat16, fill=0)
+    g.copy_(spectrum(36, 50, 140, "gauss", 2))
+    assert_close(run(g), reference(g), torch.bfloat16)
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("count,M,N", [(1, 40, 20000), (1, 1000, 21), (40, 12, 77)])
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_narrow_update(t, count, M, N, nesterov):
+    mu, lr, wd = 0.9, 0.05, 0.1
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    mk = lambda dt, std: guarded((count, M, N), dt, fill=0).copy_(torch.randn(count, M, N, device="cuda", generator=gen) * std)
+    w, dw, m = mk(t, 0.1), mk(t, 1e-2), mk(torch.float32, 1e-2)
+    w0, m0 = w.double(), m.double()
+    B.orthogonal_update(count, M, N, w, dw, m, mu, nesterov, lr, wd, ws=workspace(B.orthogonalize_workspace_bytes(count, M, N)))
+    B.check_device_status()
+    check_guards()
+    mu64 = float(torch.tensor(mu, dtype=torch.float32))
+    assert bool(((m.double() - (mu64 * m0 + dw.double())).abs() <= 2.0 ** -23 * (m0.abs() + dw.double().abs())).all())
+    # U from the momentum as it was stored; its rounding, where one follows, is 2^-24 of its terms
+    u = dw.double() + mu64 * m.double() if nesterov else m.double()
+    o, size = narrow_reference(u)
+    step = lr * math.sqrt(max(1.0, M / N))
+    want = (1 - lr * wd) * w0 - step * o
+    # the rounding of U moves |U| and every X0 by 2^-24 of its terms' sizes at most, X by |P| (and P's change) times that: the
+    # sizes of the terms of U are below |dw| + |m|, whose part of `size` is bounded by the largest row sum of |P| times the largest of them
+    bound = step * (narrow_bound(o, size, min(M, N), torch.float32) + (2.0 ** -20 * size.max() if nesterov else 0)) + (half_step(t) + 2.0 ** -22) * (want.abs() + w0.abs() + step * o.abs())
+    assert bool(((w.double() - want).abs() <= bound).all())
