@@ -170,9 +170,10 @@ __global__ void __launch_bounds__(256) loss_parts_kernel(const float* __restrict
 
 // What a row's dz is multiplied with, and what the products are multiplied with afterwards.  16-bit dz is kept in range by a
 // power of two: fp16 has no normal numbers below 2^-14, and a probability over 100 000 classes divided by the number
-// of rows lies far below; bf16 has the exponents of fp32.
+// of rows lies far below; bf16 has the exponents of fp32.  The largest row gradient goes into the products' factor whole: where all
+// are the same, as in a mean, its rounding would otherwise be in every element of dz in the same direction.
 __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__ labels, int ignore_label,
-                                                         const float* __restrict__ row_grad, int N, int f16,
+                                                         const float* __restrict__ row_grad, int N, int type,
                                                          float* __restrict__ row_scale, float* __restrict__ alpha, int* counters) {
     __shared__ int counts[32];
     __shared__ float tops[32];
@@ -196,16 +197,14 @@ __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__
     count = 0; top = 0.f;
     for (int i = 0; i < 32; ++i) { count += counts[i]; top = fmaxf(top, tops[i]); }
     if (!row_grad) top = 1.f;
-    float up = 1.f;
-    if (f16 && top > 0.f && top < 1e30f) {
-        int e;
-        frexpf(top, &e);                                  // top = f * 2^e, f in [0.5, 1)
-        const int shift = 14 - e < 100 ? 14 - e : 100;    // |dz| <= 2 * 2^14
-        up = ldexpf(1.f, shift);
+    const float up = type == DT_F16 ? 16384.f : 1.f;      // |dz| <= 2^14
+    const bool whole = !row_grad || (type != DT_F32 && top > 1e-30f && top < 1e30f);
+    for (int n = threadIdx.x; n < N; n += 1024) {
+        float g = labels[n] == ignore_label ? 0.f : row_grad ? row_grad[n] : 1.f;
+        if (whole) g = g / top * up;
+        row_scale[n] = g;
     }
-    for (int n = threadIdx.x; n < N; n += 1024)
-        row_scale[n] = labels[n] == ignore_label ? 0.f : (row_grad ? row_grad[n] * up : up);
-    if (threadIdx.x == 0) alpha[0] = row_grad ? 1.f / up : 1.f / (up * float(count > 0 ? count : 1));
+    if (threadIdx.x == 0) alpha[0] = !whole ? 1.f : row_grad ? top / up : 1.f / (up * float(count > 0 ? count : 1));
 }
 
 // db[k] = alpha * sum_n dz[n][k].  A block takes 64 columns, eight at a time per thread (rows of dz are padded to 64), and 32 rows
@@ -457,7 +456,7 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
     int rc = PCL_OK;
     {
         LaunchScope scope(KID_VOCAB_LOSS, 12.0 * double(N), st);
-        rc = launch_chained(grad_rows_kernel, dim3(1), dim3(1024), 0, st, 1, labels, ignore_label, row_grad, N, int(type == DT_F16), row_scale,
+        rc = launch_chained(grad_rows_kernel, dim3(1), dim3(1024), 0, st, 1, labels, ignore_label, row_grad, N, type, row_scale,
                             alpha, l.split_bytes ? reinterpret_cast<int*>(base + l.split) : nullptr);
     }
     if (rc != PCL_OK) return rc;

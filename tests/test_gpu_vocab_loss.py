@@ -345,3 +345,22 @@ def test_offsets_beyond_32_bits():
     # everywhere else p is the same tiny number
     tiny = float(torch.exp(-ref).max()) / N * float(x.double().abs().sum(0).max()) * 1.1
     assert float(dw[: K - 40 : 997].abs().max()) <= tiny
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("C", [128, 131])
+def test_equal_row_gradients_are_a_factor(t, C):
+    """The same gradient c for every row: its own rounding to 16 bits must not be in every element of the result."""
+    c = 1 + 2.0 ** -12 + 2.0 ** -9 + 2.0 ** -8 if t == torch.float16 else 1 + 2.0 ** -9 + 2.0 ** -5
+    results = []
+    for grad in (1.0, c):
+        case = Case(300, C, 500, t, False, 0.0)
+        case.row_grad = guarded((300,))
+        case.row_grad.fill_(grad)
+        case.forward()
+        case.backward()
+        check_guards()
+        results.append([v.double() for v in (case.dx, case.dw)])
+    for one, both in zip(*results):
+        # the same sums, of dz of the same roundings: two roundings of the results remain (fp16: subnormals are absolute)
+        assert bool(((both - c * one).abs() <= 2 * half_step(t) * (c * one).abs() * (1 + 2.0 ** -7) + 2.0 ** -24).all())
