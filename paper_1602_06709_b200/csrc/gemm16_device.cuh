@@ -100,6 +100,15 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ void pack16(const float (&v)[32], bool bf16, uint32_t (&h)[16]) {
+    if (bf16) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) h[j] = pack16(v[2 * j], v[2 * j + 1], true);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) h[j] = pack16(v[2 * j], v[2 * j + 1], false);
+    }
+}
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -449,7 +458,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-            if constexpr (kPair) mbar_arrive_cluster(ae_dst0 + 8 * buf);
+            if constexpr (kPair) mbar_arrive_cluster_read(ae_dst0 + 8 * buf);
             else mbar_arrive(&c.sh->acc_empty_bar[buf]);
         }
     };
@@ -665,13 +674,13 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] *= alpha;
                 }
+                uint32_t h[16];
+                pack16(v, p.bf16 != 0, h);
                 const bool odd = (cc & 32) != 0;                               // 16-bit: two chunks fill the staging tile's rows
                 if (!odd) staging_wait(lane);
 #pragma unroll
                 for (uint32_t j = 0; j < 4; ++j)
-                    st_shared_u4(stg_row + (((j + (odd ? 4u : 0u)) ^ sw) << 4), pack16(v[8 * j], v[8 * j + 1], p.bf16 != 0),
-                                 pack16(v[8 * j + 2], v[8 * j + 3], p.bf16 != 0), pack16(v[8 * j + 4], v[8 * j + 5], p.bf16 != 0),
-                                 pack16(v[8 * j + 6], v[8 * j + 7], p.bf16 != 0));
+                    st_shared_u4(stg_row + (((j + (odd ? 4u : 0u)) ^ sw) << 4), h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
                 if ((odd || col + 32 >= p.N) && row0 < p.M)
                     staging_store(tm_out, stg, lane, odd ? col - 32 : col, row0, tile.b);
             }
@@ -763,6 +772,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             }
             if (finish) {
                 if (fetches && joined && cbase < p.N) fetch(cbase);
+                bool held = !joined;
                 for (int cc = 0; cc < kHalf && cbase + cc < p.N && ok; cc += 32) {
                     float v[32];
                     if (joined) {
@@ -773,11 +783,12 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                         tmem_ld_wait();
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(u[j]);
+                        if (cc + 32 >= kHalf || cbase + cc + 32 >= p.N) { release(buf); held = false; }
                     }
                     process(cc, v);
                 }
+                if (held) release(buf);                        // (a tile without columns for this warp)
             }
-            if (!joined) release(buf);
             ++c.it;
         }
         if constexpr (kEpi == GEMM16_STATS) {
@@ -829,6 +840,7 @@ inline Plan16 plan16(const Gemm16Args& a) {
         return Plan16{false, false, a.k_parts, int(part), tiles, 0, 0.0};
     }
     const bool joins = a.split_ws && a.epi != GEMM16_STATS;
+    const long least = a.most_blocks > 0 ? (kb + a.most_blocks - 1) / a.most_blocks : 1;          // parts of every tile
     for (int form = 0; form < 4; ++form) {
         const bool pair = form % 2 == 0, mirrored = form >= 2;
         if (a.form == GEMM16_FORM_PAIR ? !pair : a.form == GEMM16_FORM_SINGLE ? pair : false) continue;
@@ -848,8 +860,8 @@ inline Plan16 plan16(const Gemm16Args& a) {
             return Costs{most(mma, copy * active), most(mma, copy * active * (1.0 + fm) / 2), most(mma * most(fn, 0.5), copy * active * (1.0 + fn) / 2)};
         };
         const Costs full = block(slots);
-        const long whole = core / slots;
-        for (long s = 1; s <= 16 && (s == 1 || (joins && s * (tiles - whole * slots) <= kMostParts)); ++s) {
+        const long whole = least > 1 ? 0 : core / slots;
+        for (long s = least; (s <= 16 || s == least) && (s == 1 || (joins && s * (tiles - whole * slots) <= kMostParts)); ++s) {
             const long part = (kb + s - 1) / s, splits = (kb + part - 1) / part;
             if (splits != s || (s > 1 && tiles == whole * slots)) continue;
             const long c1 = (core - whole * slots) * s, items = c1 + (bottom + right) * s;

@@ -296,6 +296,11 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar_cluster_addr) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
 }
+// The same without release at cluster scope, which waits for all of the thread's stores to be visible (1 us): for an arrival that
+// says no more than that tensor memory has been read (tcgen05.wait::ld and tcgen05.fence::before_thread_sync stand before it).
+__device__ __forceinline__ void mbar_arrive_cluster_read(uint32_t bar_cluster_addr) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar_cluster_addr) : "memory");
+}
 __device__ __forceinline__ void tma_load_3d_pair(void* dst, const CUtensorMap* m, uint32_t bar_cluster_addr, int c0,
                                                  int c1, int c2) {
     asm volatile(
