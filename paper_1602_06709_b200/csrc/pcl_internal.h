@@ -348,7 +348,9 @@ struct Gemm16Args {
     const float* row_scale = nullptr;
     // Scratch of gemm16_split_ws_bytes(), 256-byte aligned, or null (then nothing is split).
     void* split_ws = nullptr;
+    int most_blocks = 0;                     // 64-element blocks that one accumulator may sum (0: any number); the parts of longer reductions are split
 };
+bool gemm16_possible(const Gemm16Args& a);        // with that limit and kMostParts parts
 int gemm16_stats_parts(const Gemm16Args& a);      // float2 entries per row that STATS writes
 // Bytes of split_ws with which launch_gemm16(a) would split reductions (0: it would not).  Its first kGemm16CounterBytes have
 // to be zero before the first launch that is given it (each launch leaves them zero).

@@ -102,6 +102,8 @@ size_t gemm16_split_ws_bytes(const Gemm16Args& args) {
     return kGemm16CounterBytes + size_t(pl.tiles - pl.full_tiles) * pl.splits * (pl.pair ? 256 * 256 : 128 * 128) * 4;
 }
 
+bool gemm16_possible(const Gemm16Args& a) { return plan16(a).time < 1e299; }
+
 int gemm16_parts(const Gemm16Args& a) {
     const long sms = device_sm_count(), kb = (a.K + 63) / 64, tiles = long((a.M + 127) / 128) * ((a.N + 127) / 128);
     long s = sms / tiles;
@@ -138,6 +140,7 @@ int launch_gemm16(const Gemm16Args& a, cudaStream_t st) {
         default: return PCL_ERR_BAD_ARG;
     }
     const Plan16 pl = plan16(a);
+    if (pl.time >= 1e299) return PCL_ERR_UNSUPPORTED_SHAPE;
     Gemm16Params p;
     int rc = fill_params16(p, a, pl);
     if (rc != PCL_OK) return rc;

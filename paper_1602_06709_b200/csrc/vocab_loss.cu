@@ -18,8 +18,9 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // A piece of dz (or, with fp32 operands, of the logits) takes at most this much workspace.
 constexpr size_t kPieceBytes = size_t(256) << 20;
-// Nor has a piece of dz more classes than this: dx sums over them in one accumulator, and the tensor core's additions
-// truncate (the pieces are added in fp32, rounded).
+// dx sums over no more classes than this in one accumulator: the tensor core's additions truncate.  What goes beyond is added in
+// fp32, rounded: the parts of a split product where there are few enough tiles (39 rows, 304 -> 123078: 107 us, 255 in
+// pieces), else pieces of so many classes.
 constexpr int kMostClasses = 16384;
 
 __device__ __forceinline__ float elem16(const void* p, int type, size_t i) {
@@ -311,6 +312,7 @@ Gemm16Args dz_args(int N, int C, int P, bool bf16) {
 }
 Gemm16Args dx_args(int N, int C, int P, bool bf16) {
     Gemm16Args a{N, C, P, 1, bf16, {}, {}, GEMM16_GENERAL};
+    a.most_blocks = kMostClasses / 64;
     a.split_ws = reinterpret_cast<void*>(256);
     return a;
 }
@@ -361,8 +363,8 @@ Layout layout(int N, int C, int K, int type, bool backward) {
         if (stage) { l.xs = take(size_t(N) * l.ldc * 2); l.wst = take(size_t(l.piece) * l.ldc * 2); }
     } else {
         l.piece = piece_classes(N, K, 2);
-        if (l.piece > kMostClasses) l.piece = kMostClasses;
         if (stage && l.piece > stage_classes(C, K)) l.piece = stage_classes(C, K);
+        if (l.piece > kMostClasses && !gemm16_possible(dx_args(N, C, l.piece, bf16))) l.piece = kMostClasses;
         l.ldp = int(align_up(l.piece, 64));
         l.row_scale = take(size_t(N) * 4);
         l.dz = take(size_t(N) * l.ldp * 2);
