@@ -2,11 +2,12 @@
 // or of dy is read once, a row of the output written once.
 //
 // Gradient: dtable[v] = scale * sum over tokens n with ids[n] = v of dy[n].  The tokens are sorted by id (stable, so equal
-// ids stay in index order) by one cluster of CTAs, while the other CTAs of that launch fetch dy into L2 where it fits and
-// zero the gradient's last rows, as much as the sort's time allows (the sort is latency, the rest bandwidth).  Then every 8 or 16 consecutive sorted tokens are one work item.  An item sums the
-// segments (runs of equal ids) that begin in it; only segments of more than twice that are cut at the items' borders
-// into partial sums that a last pass adds in order.  The work is even whatever the ids' frequencies are, and the
-// additions have a fixed order (no atomics).  Blocks that zero the remaining rows that do not occur run between the items' blocks.
+// ids stay in index order): few of them by counting, more by one cluster of CTAs.  The other CTAs of that launch fetch dy into L2 where it
+// fits and zero the gradient's last rows, as much as the sort's time allows (the sort is latency, the rest bandwidth).  Then
+// every 8 or 16 consecutive sorted tokens are one work item.  An item sums the segments (runs of equal ids) that begin in it; only
+// segments of more than twice that are cut at the items' borders into partial sums that a last pass adds in order.  The work is
+// even whatever the ids' frequencies are, and the additions have a fixed order (no atomics).  Blocks that zero the remaining
+// rows that do not occur run between the items' blocks.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <limits.h>
@@ -29,6 +30,11 @@ constexpr int kMaxBits = 9;              // bits of a digit
 constexpr int kHistLd = (1 << kMaxBits) + 1;                  // (odd: a column over the warps meets every bank once)
 constexpr size_t kBesideSort = size_t(100) << 20;             // bytes fetched and zeroed beside the sort (in about its 20 us)
 constexpr int kMaxRun = 8192;            // tokens per CTA that the shared-memory sort takes
+constexpr int kRankThreads = 512;
+// Tokens that are sorted by counting: 1 token 7.1 -> 4.3 us, 100 10.1 -> 7.0, 2000 17.0 -> 12.3, 4096 19.7 -> 18.8 (whole gradient calls),
+// but 6000 21.8 -> 27.0, because the work is quadratic.
+constexpr int kMostRanked = 4096;
+constexpr size_t kBesideRank = size_t(32) << 20;              // in its 5 us
 
 template <class T> __device__ __forceinline__ float to_f32(T v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
@@ -117,7 +123,7 @@ struct SortArgs {
     int per_warp;                 // tokens per warp, a multiple of 32
     int *keys0, *keys1;           // written by the even and the odd passes (kShared: the last pass's, once)
     int *idx0, *idx1;
-    int2* bounds;                 // [V]: first position and end of the segment of an id, (-1, -1) if it does not occur
+    int2* bounds;                 // [V]: first position and end of the segment of an id; anything where it does not occur
     int* long_count;              // set to 0 here
     uint4* zero; size_t zero16;   // what the other CTAs clear: 16-byte units, and the bytes behind them
     unsigned char* zero_tail; int zero_tail_bytes;
@@ -156,6 +162,88 @@ __device__ __forceinline__ uint32_t map_addr(uint32_t addr, uint32_t rank) {
     return r;
 }
 
+// What the blocks from `first` on do beside the sorting ones: fetch dy and the rows of the table that the ids name into L2, zeros.
+__device__ __forceinline__ void beside_sort(const SortArgs& a, int first) {
+    const int lane = threadIdx.x & 31;
+    const uint4 z = make_uint4(0u, 0u, 0u, 0u);
+    const size_t stride = size_t(gridDim.x - first) * blockDim.x;
+    const size_t i0 = size_t(blockIdx.x - first) * blockDim.x + threadIdx.x;
+    for (size_t i = i0; i < a.dy_lines; i += stride) prefetch_l2(a.dy + i * 128);
+    if (a.table)
+        for (size_t n = i0 >> 5; n < size_t(a.N); n += stride >> 5) {
+            const int id = a.ids[n];
+            if (id == a.pad_id || id < 0 || id >= a.V) continue;
+            for (size_t o = size_t(lane) * 128; o < a.row_bytes; o += 32 * 128) prefetch_l2(a.table + size_t(id) * a.row_bytes + o);
+        }
+#pragma unroll 4
+    for (size_t i = i0; i < a.zero16; i += stride) a.zero[i] = z;
+    if (i0 < size_t(a.zero_tail_bytes)) a.zero_tail[i0] = 0;
+}
+
+// The same for few tokens, without passes: a token's position is the number of tokens with a smaller id, or the same id and a smaller
+// index.  A block takes 32 tokens, one per lane, and its warps compare them with all tokens, 32 at a time (four integer instructions a
+// comparison of 32 lanes, at half rate: N^2 / 2000 cycles with all SMs).  No block needs another's result.
+__global__ void __launch_bounds__(kRankThreads) embedding_rank_kernel(SortArgs a) {
+    constexpr int kWarps = kRankThreads / 32, kChunks = 4;
+    __shared__ __align__(16) int others[kWarps][kChunks * 32];
+    __shared__ int counts[kWarps][3][32];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    if (int(blockIdx.x) >= a.ctas) { beside_sort(a, a.ctas); return; }
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, own = blockIdx.x;
+    if (own == 0 && threadIdx.x == 0) *a.long_count = 0;
+    const int chunks = (a.N + 31) / 32, n = own * 32 + lane;
+    auto key_of = [&](int i) {               // (behind the last token: larger than all keys)
+        const int id = i < a.N ? a.ids[i] : INT_MAX;
+        return i >= a.N ? INT_MAX : id == a.pad_id || id < 0 || id >= a.V ? a.V : id;
+    };
+    const int key = key_of(n);
+    int pos = 0, less = 0, upto = 0;         // tokens before this one; of smaller ids; of ids up to this one's
+    for (int c0 = warp; c0 < chunks; c0 += kWarps * kChunks) {
+        int k[kChunks];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) k[i] = key_of((c0 + i * kWarps) * 32 + lane);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) others[warp][i * 32 + lane] = k[i];
+        __syncwarp();
+#pragma unroll 1
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = c0 + i * kWarps;
+            if (c >= chunks) break;
+            int l = 0, u = 32, first = 0;     // first: of the ids up to this one's those of smaller indices (own chunk)
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const int4 o = *reinterpret_cast<const int4*>(&others[warp][i * 32 + j]);
+                const int q[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    l += int(unsigned(q[e] - key) >> 31);        // (keys are not negative: the sign is the comparison)
+                    u -= int(unsigned(key - q[e]) >> 31);
+                }
+            }
+            if (c == own)
+                for (int j = 0; j < 32; ++j) {
+                    const int q = others[warp][i * 32 + j];
+                    first += q < key || (q == key && j < lane);
+                }
+            less += l;
+            upto += u;
+            pos += c < own ? u : c > own ? l : first;
+        }
+    }
+    counts[warp][0][lane] = pos; counts[warp][1][lane] = less; counts[warp][2][lane] = upto;
+    __syncthreads();
+    if (warp > 0 || n >= a.N) return;
+    pos = less = upto = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) { pos += counts[w][0][lane]; less += counts[w][1][lane]; upto += counts[w][2][lane]; }
+    if (key == a.V) row_exists(a.ids[n], a.V, a.pad_id, a.status);
+    a.keys1[pos] = key;
+    a.idx1[pos] = n;
+    if (key < a.V && pos == less) a.bounds[key] = make_int2(less, upto);
+}
+
 template <bool kShared>
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a) {
     extern __shared__ int sort_smem[];       // hist [32][kHistLd], totals [512], (kShared) [2] runs of (key, token)
@@ -163,29 +251,13 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
     grid_dependency_wait();
     grid_dependents_launch();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (int(blockIdx.x) >= a.ctas) {         // the other clusters: zeros
-        const uint4 z = make_uint4(0u, 0u, 0u, 0u);
-        const size_t stride = size_t(gridDim.x - a.ctas) * kSortThreads;
-        const size_t i0 = size_t(blockIdx.x - a.ctas) * kSortThreads + threadIdx.x;
-        for (size_t i = i0; i < a.dy_lines; i += stride) prefetch_l2(a.dy + i * 128);
-        if (a.table)
-            for (size_t n = i0 >> 5; n < size_t(a.N); n += stride >> 5) {
-                const int id = a.ids[n];
-                if (id == a.pad_id || id < 0 || id >= a.V) continue;
-                for (size_t o = size_t(lane) * 128; o < a.row_bytes; o += 32 * 128) prefetch_l2(a.table + size_t(id) * a.row_bytes + o);
-            }
-#pragma unroll 4
-        for (size_t i = i0; i < a.zero16; i += stride) a.zero[i] = z;
-        if (i0 < size_t(a.zero_tail_bytes)) a.zero_tail[i0] = 0;
-        return;
-    }
+    if (int(blockIdx.x) >= a.ctas) { beside_sort(a, a.ctas); return; }
     int(*hist)[kHistLd] = reinterpret_cast<int(*)[kHistLd]>(sort_smem);
     int* totals = sort_smem + kSortWarps * kHistLd;
     int2* runs = reinterpret_cast<int2*>(totals + (1 << kMaxBits));           // [2][1 << run_log2]
     const int cta = blockIdx.x, ctas = a.ctas;
     const bool cluster = ctas > 1;
     if (cta == 0 && threadIdx.x == 0) *a.long_count = 0;
-    for (int v = cta * kSortThreads + threadIdx.x; v < a.V; v += ctas * kSortThreads) a.bounds[v] = make_int2(-1, -1);
     const int bins = 1 << a.bits, run_size = 1 << a.run_log2;
     // this warp's tokens, as positions of the sequence; kShared: offsets in this CTA's run
     const long cta0 = kShared ? long(cta) << a.run_log2 : 0;
@@ -313,7 +385,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(SortArgs a
 struct GradArgs {
     const int* keys;              // sorted ids (V: no row)
     const int* idx;               // their tokens
-    const int2* bounds;           // [V] segment of an id, (-1, -1) if it does not occur
+    const int2* bounds;           // [V] segment of an id that occurs
     int zero_rows;                // rows [0, zero_rows) that do not occur are zeroed here
     int item_blocks, zero_blocks;
     float* part;                  // [items][2][C]: sums of an item's share of a long segment begun before it, and begun in it
@@ -357,7 +429,8 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
 #pragma unroll
         for (int j = 0; j < kVec; ++j) z.e[j] = from_f32<T>(0.f);
         for (int v = zeros_before * 8 + w; v < a.zero_rows; v += a.zero_blocks * 8) {
-            if (a.bounds[v].x >= 0) continue;
+            const int at = a.bounds[v].x;                     // (of an id that does not occur: anything)
+            if (unsigned(at) < unsigned(a.N) && a.keys[at] == v) continue;
             P* dst = reinterpret_cast<P*>(out + size_t(v) * a.C);
 #pragma unroll 4
             for (int i = lane; i < vecs; i += 32) dst[i] = z;
@@ -581,9 +654,12 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     s.passes = (key_bits + kMaxBits - 1) / kMaxBits;
     s.bits = (key_bits + s.passes - 1) / s.passes;
     // Tokens per CTA: 1024 where one CTA takes them all, up to kMaxRun with eight; beyond, the sequence stays in global memory.
-    const bool shared = N <= kMaxSortCtas * kMaxRun;
+    const bool rank = N <= kMostRanked, shared = N <= kMaxSortCtas * kMaxRun;
     size_t smem = size_t(kSortWarps * kHistLd + (1 << kMaxBits)) * 4;
-    if (shared) {
+    if (rank) {
+        s.ctas = (N + 31) / 32;
+        s.passes = 0;
+    } else if (shared) {
         s.run_log2 = log2_up((N + kMaxSortCtas - 1) / kMaxSortCtas);
         if (s.run_log2 < 10) s.run_log2 = 10;
         s.ctas = 1 << log2_up((long(N) + (1 << s.run_log2) - 1) >> s.run_log2);
@@ -601,7 +677,8 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     // What the other SMs do meanwhile: fetch dy (and the table's rows) into L2 if they fit, then zeros.
     const size_t row = size_t(C) * dtype_bytes(type);
     size_t fetched = size_t(N) * row * (sgd ? 2 : 1);
-    if (fetched > kBesideSort) fetched = size_t(N) * row <= kBesideSort ? size_t(N) * row : 0;
+    const size_t beside = rank ? kBesideRank : kBesideSort;
+    if (fetched > beside) fetched = size_t(N) * row <= beside ? size_t(N) * row : 0;
     if (fetched) {
         s.dy = static_cast<const char*>(dy);
         s.dy_lines = (size_t(N) * row + 127) / 128;
@@ -611,7 +688,7 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     const int most_blocks = device_sm_count() * 2;
     if (!sgd) {
         // whole rows from the end, of which the first starts on a 16-byte boundary (every eighth row does)
-        const size_t rows = (kBesideSort - fetched) / row;
+        const size_t rows = (beside - fetched) / row;
         if (rows < size_t(V)) zero_row0 = (V - int(rows)) / 8 * 8;
         const size_t bytes = size_t(V - zero_row0) * row;
         s.zero = reinterpret_cast<uint4*>(static_cast<char*>(out) + zero_row0 * row);
@@ -622,10 +699,11 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
         if (want > size_t(other_blocks)) other_blocks = int(want < size_t(most_blocks) ? want : size_t(most_blocks));
     }
     if (other_blocks > most_blocks) other_blocks = most_blocks;
-    other_blocks = (other_blocks + s.ctas - 1) / s.ctas * s.ctas;                // (whole clusters)
+    if (!rank) other_blocks = (other_blocks + s.ctas - 1) / s.ctas * s.ctas;     // (whole clusters)
     {
         LaunchScope scope(KID_EMBEDDING, 16.0 * double(N) * s.passes + (sgd ? 0.0 : double(V) * C * dtype_bytes(type)), st);
-        const int rc = shared ? run_sort<true>(s, smem, s.ctas + other_blocks, st) : run_sort<false>(s, smem, s.ctas + other_blocks, st);
+        const int rc = rank ? launch_chained(embedding_rank_kernel, dim3(s.ctas + other_blocks), dim3(kRankThreads), 0, st, 1, s)
+                     : shared ? run_sort<true>(s, smem, s.ctas + other_blocks, st) : run_sort<false>(s, smem, s.ctas + other_blocks, st);
         if (rc != PCL_OK) return rc;
     }
     GradArgs g{};

@@ -218,3 +218,27 @@ def test_graph_replay_and_second_stream():
         torch.cuda.current_stream().wait_stream(side)
         torch.cuda.synchronize()
         assert torch.equal(grad, eager)
+
+
+@pytest.mark.parametrize("N", [1, 31, 32, 33, 2047, 4095, 4096, 4097])
+def test_workspace_that_held_anything(N):
+    """What the workspace held before the call (the segments of an earlier one, or all ones) does not matter."""
+    V, C = 700, 40
+    g = torch.Generator(device="cuda").manual_seed(N)
+    ws = workspace(B.embedding_workspace_bytes(N, V, C))
+    for fill in (0, 255, None):
+        if fill is not None:
+            ws.fill_(fill)
+        ids = torch.randint(-1 if fill else 0, V if fill else V // 2, (N,), device="cuda", generator=g).int()
+        dy = torch.randn(N, C, device="cuda", generator=g)
+        dt = guarded((V, C))
+        B.embedding_bwd(N, V, C, ids, dy, 0.5, dt, pad_id=-1, ws=ws)
+        B.check_device_status()
+        check_guards()
+        want = torch.zeros(V, C, dtype=torch.float64, device="cuda")
+        size = torch.zeros(V, C, dtype=torch.float64, device="cuda")
+        rows, there = ids.long().clamp(min=0), (ids >= 0)[:, None]
+        want.index_add_(0, rows, 0.5 * dy.double() * there)
+        size.index_add_(0, rows, 0.5 * dy.double().abs() * there)
+        # at most N additions and the scale, 2^-24 of the terms' sizes each
+        assert bool(((dt.double() - want).abs() <= (int(there.sum()) + 1) * 2.0 ** -24 * size).all())
