@@ -48,7 +48,7 @@ struct Gemm16Params {
     // column (so the cheap ones come last).
     int m_whole, n_whole, core_tiles, bottom_tiles;  // whole rows and columns of tiles; tiles of the first two kinds
     FastDiv by_core, by_group, by_bottom, by_right;  // tiles of one matrix of each kind; of kGroupM rows of whole tiles
-    FastDiv by_splits;                               // parts of a tile
+    FastDiv by_rest;                                 // split tiles
     int full_tiles, splits, part_blocks, items;      // tiles [0, full_tiles) are one item each, the others `splits`
     int* counters; float4* parts;                    // of the split tiles
     int symmetric, bf16;
@@ -135,9 +135,9 @@ __device__ __forceinline__ Item16 decode_item(const Gemm16Params& p, int i) {
     o.k0 = 0; o.k1 = p.k_blocks; o.part = -1; o.split_tile = 0;
     if (i >= p.full_tiles) {
         const int j = i - p.full_tiles;
-        o.split_tile = divide(j, p.by_splits);
+        o.part = divide(j, p.by_rest);                       // (part by part: the same reduction blocks at the same time)
+        o.split_tile = j - o.part * int(p.by_rest.d);
         t = p.full_tiles + o.split_tile;
-        o.part = j - o.split_tile * p.splits;
         o.k0 = o.part * p.part_blocks;
         o.k1 = o.k0 + p.part_blocks < p.k_blocks ? o.k0 + p.part_blocks : p.k_blocks;
     }
@@ -902,7 +902,7 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
     p.by_group = divisor(long(kGroupM) * p.n_whole);
     p.by_bottom = divisor(bottom);
     p.by_right = divisor(p.m_tiles);
-    p.by_splits = fast_div(unsigned(pl.splits));
+    p.by_rest = fast_div(unsigned(pl.tiles > pl.full_tiles ? pl.tiles - pl.full_tiles : 1));
     p.full_tiles = int(pl.full_tiles); p.splits = pl.splits; p.part_blocks = pl.part_blocks;
     p.items = int(pl.full_tiles + (pl.tiles - pl.full_tiles) * pl.splits);
     p.counters = static_cast<int*>(a.split_ws);
