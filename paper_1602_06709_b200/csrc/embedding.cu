@@ -54,6 +54,12 @@ __device__ __forceinline__ void store_streaming(Pack<T, kVec>* p, const Pack<T, 
     else *p = v;
 }
 
+// Vectors per thread and row in the lookup; per lane and token in the gradient.  Rows are taken in the longest vectors that all of them
+// start on a multiple of (32768 tokens, bf16 rows of 2048 / 2044 / 2046 / 2047: lookup 48 / 53 / 62 / 66 us, gradient
+// 154 / 170 / 206 / 262 us; with single elements for the last three 75 and 420): short ones are bound by the number of instructions.
+template <int kVec> constexpr int kLoads = kVec == 1 ? 8 : kVec == 2 ? 4 : 2;
+template <int kVec, bool kSgd> constexpr int kReps = kVec == 1 && kSgd ? 2 : 1;
+
 // ids that name no row (outside [0, V)) and the padding id
 __device__ __forceinline__ bool row_exists(int id, int V, int pad_id, unsigned int* status) {
     if (id == pad_id) return false;
@@ -64,11 +70,13 @@ __device__ __forceinline__ bool row_exists(int id, int V, int pad_id, unsigned i
     return true;
 }
 
-// Two rows per pass of a thread group, and two vectors of each: four independent loads per thread in flight.
+// Two rows per pass of a thread group, and two vectors of each (more of shorter ones, where rows are not aligned for 16 bytes): that many
+// independent loads per thread in flight.
 template <class T, int kVec>
 __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restrict__ ids, const T* __restrict__ table,
                                                             float scale, int pad_id, T* __restrict__ out, int N, int V, int C,
                                                             int tpr_log2, unsigned int* status) {
+    constexpr int kHalves = kLoads<kVec>;
     const int tpr = 1 << tpr_log2;                   // threads per row
     grid_dependency_wait();
     grid_dependents_launch();
@@ -87,17 +95,17 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restric
             src[r] = reinterpret_cast<const Pack<T, kVec>*>(table + size_t(there[r] ? id : 0) * C);
             dst[r] = row < N ? reinterpret_cast<Pack<T, kVec>*>(out + size_t(row) * C) : nullptr;
         }
-        for (int i = lane; i < vecs; i += 2 * tpr) {
-            Pack<T, kVec> v[2][2];
+        for (int i = lane; i < vecs; i += kHalves * tpr) {
+            Pack<T, kVec> v[2][kHalves];
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < kHalves; ++h)
                     if (there[r] && i + h * tpr < vecs) v[r][h] = src[r][i + h * tpr];
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int h = 0; h < kHalves; ++h) {
                     if (!dst[r] || i + h * tpr >= vecs) continue;
                     Pack<T, kVec> o;
 #pragma unroll
@@ -106,6 +114,21 @@ __global__ void __launch_bounds__(256) embedding_fwd_kernel(const int* __restric
                 }
         }
     }
+}
+
+// A row of zeros by a warp, in 16-byte stores whatever its alignment (the bf16 gradient of 32768 tokens, 131072 x 2047:
+// 420 -> 390 us).
+template <class T>
+__device__ __forceinline__ void zero_row(T* row, int C, int lane) {
+    constexpr int kUnit = 16 / int(sizeof(T));
+    int head = int((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / int(sizeof(T));
+    if (head > C) head = C;
+    const int units = (C - head) / kUnit, tail = C - head - units * kUnit;
+    uint4* body = reinterpret_cast<uint4*>(row + head);
+#pragma unroll 4
+    for (int i = lane; i < units; i += 32) body[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (lane < head) row[lane] = from_f32<T>(0.f);
+    if (lane < tail) row[head + units * kUnit + lane] = from_f32<T>(0.f);
 }
 
 // Stable radix sort of (id, token) by one cluster of CTAs.  Every warp owns a run of consecutive tokens; per pass it counts
@@ -410,12 +433,12 @@ __device__ __forceinline__ void write_row(const GradArgs& a, T* out, int key, in
     reinterpret_cast<Pack<T, kVec>*>(out + size_t(key) * a.C)[i] = o;
 }
 
-// One warp per item and 32 vectors of a row (single elements, where rows are not aligned for vectors: 64).  The item's keys
+// One warp per item and 32 vectors of a row (kSgd, single elements: 64).  The item's keys
 // and tokens are held by the lanes (a window of 32 sorted positions), so that per batch of tokens only their rows are waited
 // for; with kSgd the table's old rows come with them.
 template <class T, int kVec, bool kSgd>
-__global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradArgs a, const T* __restrict__ dy, T* __restrict__ out) {
-    constexpr int kBatch = kVec == 1 && !kSgd ? 8 : 4, kRep = kVec == 1 ? 2 : 1;        // tokens at a time; vectors per lane, 32 apart
+__global__ void __launch_bounds__(256, kSgd || kVec < 8 ? 4 : 3) embedding_grad_kernel(GradArgs a, const T* __restrict__ dy, T* __restrict__ out) {
+    constexpr int kBatch = 4, kRep = kReps<kVec, kSgd>;             // tokens at a time; vectors per lane, 32 apart
     using P = Pack<T, kVec>;
     const int vecs = a.C / kVec, strips = (vecs + 32 * kRep - 1) / (32 * kRep);
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
@@ -425,15 +448,10 @@ __global__ void __launch_bounds__(256, kSgd ? 4 : 3) embedding_grad_kernel(GradA
     const long all = long(a.item_blocks) + a.zero_blocks, b = blockIdx.x;
     const int zeros_before = int(b * a.zero_blocks / all);
     if (!kSgd && int((b + 1) * a.zero_blocks / all) != zeros_before) {
-        P z;
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) z.e[j] = from_f32<T>(0.f);
         for (int v = zeros_before * 8 + w; v < a.zero_rows; v += a.zero_blocks * 8) {
             const int at = a.bounds[v].x;                     // (of an id that does not occur: anything)
             if (unsigned(at) < unsigned(a.N) && a.keys[at] == v) continue;
-            P* dst = reinterpret_cast<P*>(out + size_t(v) * a.C);
-#pragma unroll 4
-            for (int i = lane; i < vecs; i += 32) dst[i] = z;
+            zero_row(out + size_t(v) * a.C, a.C, lane);
         }
         return;
     }
@@ -578,7 +596,7 @@ BwdLayout bwd_layout(int N, int V, int C) {
 template <class T, int kVec>
 int run_fwd(int N, int V, int C, const int* ids, const void* table, float scale, int pad_id, void* out, unsigned int* status,
             cudaStream_t st) {
-    const int tl = log2_threads(C / kVec);
+    const int tl = log2_threads((C / kVec + kLoads<kVec> / 2 - 1) / (kLoads<kVec> / 2));
     const long rows_per_block = 256 >> tl;
     const long blocks = (N + 2 * rows_per_block - 1) / (2 * rows_per_block), cap = long(device_sm_count()) * 8;
     LaunchScope scope(KID_EMBEDDING, 2.0 * sizeof(T) * double(N) * C, st);
@@ -588,7 +606,7 @@ int run_fwd(int N, int V, int C, const int* ids, const void* table, float scale,
 
 template <class T, int kVec>
 int run_grad(GradArgs a, const void* dy, void* out, cudaStream_t st) {
-    const int vecs = a.C / kVec, per_strip = kVec == 1 ? 64 : 32, strips = (vecs + per_strip - 1) / per_strip;
+    const int vecs = a.C / kVec, per_strip = 32 * (a.sgd ? kReps<kVec, true> : kReps<kVec, false>), strips = (vecs + per_strip - 1) / per_strip;
     while (a.wpi_log2 < 3 && (1 << a.wpi_log2) < strips) ++a.wpi_log2;
     const int per_block = 8 >> a.wpi_log2, blocks = (a.items + per_block - 1) / per_block;
     {
@@ -632,14 +650,15 @@ int launch_embedding_fwd(int N, int V, int C, int type, const int* ids, const vo
                          cudaStream_t st) {
     unsigned int* status = device_status_ptr();
     if (!status) return PCL_ERR_CUDA;
-    if (type == DT_F32)
-        return C % 4 == 0 ? run_fwd<float, 4>(N, V, C, ids, table, scale, pad_id, out, status, st)
-                          : run_fwd<float, 1>(N, V, C, ids, table, scale, pad_id, out, status, st);
-    if (type == DT_BF16)
-        return C % 8 == 0 ? run_fwd<__nv_bfloat16, 8>(N, V, C, ids, table, scale, pad_id, out, status, st)
-                          : run_fwd<__nv_bfloat16, 1>(N, V, C, ids, table, scale, pad_id, out, status, st);
-    return C % 8 == 0 ? run_fwd<__half, 8>(N, V, C, ids, table, scale, pad_id, out, status, st)
-                      : run_fwd<__half, 1>(N, V, C, ids, table, scale, pad_id, out, status, st);
+    auto run = [&](auto zero) {              // with the longest vectors that every row starts on a multiple of
+        using T = decltype(zero);
+        if constexpr (sizeof(T) == 2)
+            if (C % 8 == 0) return run_fwd<T, 8>(N, V, C, ids, table, scale, pad_id, out, status, st);
+        return C % 4 == 0 ? run_fwd<T, 4>(N, V, C, ids, table, scale, pad_id, out, status, st)
+             : C % 2 == 0 ? run_fwd<T, 2>(N, V, C, ids, table, scale, pad_id, out, status, st)
+                          : run_fwd<T, 1>(N, V, C, ids, table, scale, pad_id, out, status, st);
+    };
+    return type == DT_F32 ? run(float{}) : type == DT_BF16 ? run(__nv_bfloat16{}) : run(__half{});
 }
 
 int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const void* dy, float scale, int pad_id, void* out,
@@ -712,11 +731,13 @@ int launch_embedding_bwd(int N, int V, int C, int type, const int* ids, const vo
     g.long_count = s.long_count; g.long_items = reinterpret_cast<int*>(base + l.long_items);
     g.scale = scale; g.lr = lr; g.N = N; g.V = V; g.C = C; g.item_tokens = item_tokens(N); g.items = (N - 1) / g.item_tokens + 1; g.sgd = sgd;
     g.zero_rows = zero_row0;
-    if (type == DT_F32)
-        return C % 4 == 0 ? run_grad<float, 4>(g, dy, out, st) : run_grad<float, 1>(g, dy, out, st);
-    if (type == DT_BF16)
-        return C % 8 == 0 ? run_grad<__nv_bfloat16, 8>(g, dy, out, st) : run_grad<__nv_bfloat16, 1>(g, dy, out, st);
-    return C % 8 == 0 ? run_grad<__half, 8>(g, dy, out, st) : run_grad<__half, 1>(g, dy, out, st);
+    auto run = [&](auto zero) {
+        using T = decltype(zero);
+        if constexpr (sizeof(T) == 2)
+            if (C % 8 == 0) return run_grad<T, 8>(g, dy, out, st);
+        return C % 4 == 0 ? run_grad<T, 4>(g, dy, out, st) : C % 2 == 0 ? run_grad<T, 2>(g, dy, out, st) : run_grad<T, 1>(g, dy, out, st);
+    };
+    return type == DT_F32 ? run(float{}) : type == DT_BF16 ? run(__nv_bfloat16{}) : run(__half{});
 }
 
 }  // namespace pcl

@@ -242,3 +242,29 @@ def test_workspace_that_held_anything(N):
         size.index_add_(0, rows, 0.5 * dy.double().abs() * there)
         # at most N additions and the scale, 2^-24 of the terms' sizes each
         assert bool(((dt.double() - want).abs() <= (int(there.sum()) + 1) * 2.0 ** -24 * size).all())
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("C", [1, 2, 3, 4, 6, 12, 130, 132, 515, 1022])
+def test_row_lengths(t, C):
+    """Rows that start on multiples of one, two, four and eight elements."""
+    N, V = 700, 90
+    g = torch.Generator(device="cuda").manual_seed(C)
+    ids = torch.randint(0, V // 2, (N,), device="cuda", generator=g).int()
+    mk = lambda shape: guarded(shape, t, fill=0).copy_(torch.randn(shape, device="cuda", generator=g))
+    table, dy, out, dt = mk((V, C)), mk((N, C)), guarded((N, C), t), guarded((V, C), t)
+    old = table.double()
+    ws = workspace(B.embedding_workspace_bytes(N, V, C))
+    B.embedding_fwd(N, V, C, ids, table, 0.5, out)
+    B.embedding_bwd(N, V, C, ids, dy, 0.5, dt, ws=ws)
+    assert torch.equal(out, (0.5 * table.float()[ids.long()]).to(t))
+    B.embedding_bwd_sgd(N, V, C, ids, dy, 0.5, table, 0.25, ws=ws)
+    B.check_device_status()
+    check_guards()
+    want = torch.zeros(V, C, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), 0.5 * dy.double())
+    size = torch.zeros(V, C, dtype=torch.float64, device="cuda").index_add_(0, ids.long(), 0.5 * dy.double().abs())
+    h, n = torch.finfo(t).eps / 2, int(torch.bincount(ids.long()).max())
+    # n additions, the scale and the step in fp32 (2^-24 of the terms' sizes each), one rounding (fp16: subnormals are absolute)
+    assert bool(((dt.double() - want).abs() <= (n + 2) * 2.0 ** -24 * size + h * want.abs() * 1.001 + 2.0 ** -25).all())
+    new = old - 0.25 * want
+    assert bool(((table.double() - new).abs() <= (n + 4) * 2.0 ** -24 * (size + old.abs()) + h * new.abs() * 1.001 + 2.0 ** -25).all())
