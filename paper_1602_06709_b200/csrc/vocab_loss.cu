@@ -29,29 +29,40 @@ __device__ __forceinline__ float elem16(const void* p, int type, size_t i) {
 }
 
 // Where C is no multiple of 8, x and w are copied to padded rows (TMA needs strides of 16 bytes): a warp per row, 16 bytes per
-// store, at the rate of memory (1024 rows, 1001 -> 50021: 33 us of 132).  Rows of whole 128-byte lines, where TMA reads a row
+// store, in the longest loads that every row starts on a multiple of (950 rows, 3358 -> 77338, forward: 740 us with single
+// elements, 553 with two; 3357: 672).  Rows of whole 128-byte lines, where TMA reads a row
 // of a tile from one line instead of two, are not worth a copy by themselves (3001 rows, 1032 -> 50021: forward 275 -> 266 us,
 // backward 914 -> 876, but 1024 rows 97 -> 116 and 377 -> 394).
-__global__ void __launch_bounds__(256) pad_rows_kernel(const uint16_t* __restrict__ src, uint16_t* __restrict__ dst, long rows,
-                                                       int C, int ldc) {
+struct PadSource { const uint16_t* src; uint16_t* dst; long rows; };
+template <int kVec>      // elements per load: every row starts on a multiple of so many
+__global__ void __launch_bounds__(256) pad_rows_kernel(PadSource first, PadSource second, int C, int ldc) {
     grid_dependency_wait();
     grid_dependents_launch();
-    for (long r = blockIdx.x * 8l + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8l) {
-        const uint16_t* row = src + r * C;
+    for (long n = blockIdx.x * 8l + (threadIdx.x >> 5); n < first.rows + second.rows; n += gridDim.x * 8l) {
+        const bool one = n < first.rows;
+        const long r = one ? n : n - first.rows;
+        const uint16_t* row = (one ? first.src : second.src) + r * C;
+        uint16_t* dst = (one ? first.dst : second.dst) + r * ldc;
 #pragma unroll 2
         for (int c = (threadIdx.x & 31) * 8; c < ldc; c += 256) {
-            uint32_t e[8];
+            alignas(16) uint16_t e[8] = {};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = c + i < C ? __ldg(row + c + i) : 0u;
-            *reinterpret_cast<uint4*>(dst + r * ldc + c) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            for (int i = 0; i < 8; i += kVec)
+                if (c + i < C) {
+                    if constexpr (kVec == 4) *reinterpret_cast<uint2*>(e + i) = __ldg(reinterpret_cast<const uint2*>(row + c + i));
+                    else if constexpr (kVec == 2) *reinterpret_cast<uint32_t*>(e + i) = __ldg(reinterpret_cast<const uint32_t*>(row + c + i));
+                    else e[i] = __ldg(row + c + i);
+                }
+            *reinterpret_cast<uint4*>(dst + c) = *reinterpret_cast<const uint4*>(e);
         }
     }
 }
-int launch_pad_rows(const void* src, void* dst, long rows, int C, int ldc, cudaStream_t st) {
+PadSource pad_source(const void* src, void* dst, long rows) { return {static_cast<const uint16_t*>(src), static_cast<uint16_t*>(dst), rows}; }
+int launch_pad_rows(const PadSource& first, const PadSource& second, int C, int ldc, cudaStream_t st) {
+    const long rows = first.rows + second.rows;
     LaunchScope scope(KID_VOCAB_LOSS, 4.0 * double(rows) * C, st);
     const long cap = long(device_sm_count()) * 8, blocks = (rows + 7) / 8;
-    return launch_chained(pad_rows_kernel, dim3(unsigned(blocks < cap ? blocks : cap)), dim3(256), 0, st, 1,
-                          static_cast<const uint16_t*>(src), static_cast<uint16_t*>(dst), rows, C, ldc);
+    return launch_chained(C % 4 == 0 ? pad_rows_kernel<4> : C % 2 == 0 ? pad_rows_kernel<2> : pad_rows_kernel<1>, dim3(unsigned(blocks < cap ? blocks : cap)), dim3(256), 0, st, 1, first, second, C, ldc);
 }
 
 // (max, sum of exp(z - max)) pairs of disjoint sets of classes, joined.  A set without a finite logit is (-inf, 0).
@@ -408,16 +419,12 @@ int launch_vocab_loss_fwd(int N, int C, int K, int type, const void* x, const vo
     } else {
         const bool stage = l.stage;
         const void* xs = x;
-        if (stage) {
-            rc = launch_pad_rows(x, base + l.xs, N, C, l.ldc, st);
-            if (rc != PCL_OK) return rc;
-            xs = base + l.xs;
-        }
+        if (stage) xs = base + l.xs;
         for (int p0 = 0; p0 < K; p0 += l.piece) {
             const int P = K - p0 < l.piece ? K - p0 : l.piece;
             const void* wp = static_cast<const uint16_t*>(w) + size_t(p0) * C;
-            if (stage) {
-                rc = launch_pad_rows(wp, base + l.wst, P, C, l.ldc, st);
+            if (stage) {                     // (x with the first piece of w)
+                rc = launch_pad_rows(pad_source(x, base + l.xs, p0 == 0 ? N : 0), pad_source(wp, base + l.wst, P), C, l.ldc, st);
                 if (rc != PCL_OK) return rc;
                 wp = base + l.wst;
             }
@@ -493,16 +500,12 @@ int launch_vocab_loss_bwd(int N, int C, int K, int type, const void* x, const vo
     uint16_t* dz = reinterpret_cast<uint16_t*>(base + l.dz);
     float* dx_acc = reinterpret_cast<float*>(base + l.dx);
     const void* xs = x;
-    if (stage) {
-        rc = launch_pad_rows(x, base + l.xs, N, C, l.ldc, st);
-        if (rc != PCL_OK) return rc;
-        xs = base + l.xs;
-    }
+    if (stage) xs = base + l.xs;
     for (int p0 = 0; p0 < K; p0 += l.piece) {
         const int P = K - p0 < l.piece ? K - p0 : l.piece;
         const void* wp = static_cast<const uint16_t*>(w) + size_t(p0) * C;
-        if (stage) {
-            rc = launch_pad_rows(wp, base + l.wst, P, C, l.ldc, st);
+        if (stage) {                     // (x with the first piece of w)
+            rc = launch_pad_rows(pad_source(x, base + l.xs, p0 == 0 ? N : 0), pad_source(wp, base + l.wst, P), C, l.ldc, st);
             if (rc != PCL_OK) return rc;
             wp = base + l.wst;
         }
