@@ -68,29 +68,15 @@ struct Gemm16Params {
     unsigned int* status;
 };
 
-// 32 consecutive elements of a 16-bit vector as fp32; `valid` of them exist.  16-byte aligned.  (Read from L2: in a kernel of
-// several products an L1 line may be older than the product before.)
-__device__ __forceinline__ void load_chunk16(const void* base, bool bf16, size_t off, int valid, float (&o)[32]) {
-    const uint16_t* s = static_cast<const uint16_t*>(base) + off;
-    if (valid >= 32) {
+__device__ __forceinline__ float2 half2_value(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+// Elements i .. i + 3 of a 16-bit vector of n (0 behind its end); i is a multiple of four, the vector 8-byte aligned.
+__device__ __forceinline__ uint2 load_four16(const void* base, int i, int n) {
+    const uint16_t* s = static_cast<const uint16_t*>(base) + i;
+    if (i + 4 <= n) return __ldg(reinterpret_cast<const uint2*>(s));
+    uint32_t e[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint4 v = __ldcg(reinterpret_cast<const uint4*>(s) + j);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-                o[8 * j + 2 * i] = bf16 ? __uint_as_float(w[i] << 16) : f.x;
-                o[8 * j + 2 * i + 1] = bf16 ? __uint_as_float(w[i] & 0xffff0000u) : f.y;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const uint16_t u = j < valid ? __ldcg(s + j) : uint16_t(0);
-            o[j] = bf16 ? __uint_as_float(uint32_t(u) << 16) : __half2float(__ushort_as_half(u));
-        }
-    }
+    for (int j = 0; j < 4; ++j) e[j] = i + j < n ? __ldg(s + j) : 0u;
+    return make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
 }
 __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
     if (bf16) {
@@ -269,7 +255,6 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
         : "=f"(o.x), "=f"(o.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return o;
 }
-__device__ __forceinline__ float2 half2_value(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
 
 // What the warps of a CTA share.
 struct Gemm16Shared {
@@ -469,7 +454,11 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
         const bool row_ok = row < p.M;
         int label = -1;
         float lse = 0.f, g = 0.f;
+        uint2 bias = make_uint2(0u, 0u);
         if constexpr (kClasses) {
+            // the bias of the warp's columns, four per lane: it arrives while the warp waits for the product (a chunk's 64 bytes loaded where
+            // they are added took 500 cycles a chunk)
+            if (p.bias) bias = load_four16(p.bias, cbase + 4 * (lane & (kHalf / 4 - 1)), p.N);
             if (row_ok) label = p.labels[row] - p.col0;
             if constexpr (kEpi == GEMM16_DZ) {
                 if (row_ok) { lse = p.lse[row]; g = p.row_scale[row]; }
@@ -512,10 +501,13 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             const int valid = p.N - col < 32 ? p.N - col : 32;
             if constexpr (kClasses) {
                 if (p.bias) {
-                    float s[32];
-                    load_chunk16(p.bias, p.bf16 != 0, col, valid, s);
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] += s[j];
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t two = __shfl_sync(0xffffffffu, j & 1 ? bias.y : bias.x, cc / 4 + j / 2);
+                        const float2 h = half2_value(two);
+                        v[2 * j] += p.bf16 ? __uint_as_float(two << 16) : h.x;
+                        v[2 * j + 1] += p.bf16 ? __uint_as_float(two & 0xffff0000u) : h.y;
+                    }
                 }
             }
             if constexpr (kEpi == GEMM16_STATS) {
@@ -657,7 +649,10 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                     const float ref2 = ref * kLog2e;
                     if (fabsf(ref) < kScaledLimit) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(v[j], kLog2e, -ref2));
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 e = fma2(make_float2(v[j], v[j + 1]), make_float2(kLog2e, kLog2e), make_float2(-ref2, -ref2));
+                            v[j] = ex2(e.x); v[j + 1] = ex2(e.y);
+                        }
                     } else {
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = ex2((v[j] - ref) * kLog2e);
