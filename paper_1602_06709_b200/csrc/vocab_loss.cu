@@ -16,7 +16,8 @@ namespace pcl {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-// A piece of dz (or, with fp32 operands, of the logits) takes at most this much workspace.
+// A piece of dz (or, with fp32 operands, of the logits) takes at most this much workspace.  (Smaller pieces, which would stay in L2,
+// cost more launches and waves than they save: 1024 rows, 1024 -> 100000 backward 571 us with 64 MB, 486 with 256.)
 constexpr size_t kPieceBytes = size_t(256) << 20;
 // dx sums over no more classes than this in one accumulator: the tensor core's additions truncate.  What goes beyond is added in
 // fp32, rounded: the parts of a split product where there are few enough tiles (39 rows, 304 -> 123078: 107 us, 255 in

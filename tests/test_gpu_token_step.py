@@ -188,7 +188,8 @@ def test_dnn_options_captured():
         assert torch.equal(a.w(j), b.w(j)) and torch.equal(a.b(j), b.b(j))
 
 
-def test_first_calls_of_a_process_may_be_captured():
+@pytest.mark.parametrize("C", [64, 96])      # (the update's two forms)
+def test_first_calls_of_a_process_may_be_captured(C):
     """A process whose very first calls are captured into a graph (the library's one-time set-up falls into the capture)."""
     code = """
 import sys
@@ -196,7 +197,7 @@ sys.path[:0] = [%r, %r]
 import torch
 from test_gpu_token_step import TokenStep
 from paper_1602_06709_b200 import binding as B
-s = TokenStep(256, 300, 64, 520, torch.bfloat16)
+s = TokenStep(256, 300, %d, 520, torch.bfloat16)
 torch.cuda.synchronize()
 g = torch.cuda.CUDAGraph()
 with torch.cuda.graph(g):
@@ -204,12 +205,12 @@ with torch.cuda.graph(g):
 g.replay()
 torch.cuda.synchronize()
 B.check_device_status()
-e = TokenStep(256, 300, 64, 520, torch.bfloat16)
+e = TokenStep(256, 300, %d, 520, torch.bfloat16)
 e.step()
 torch.cuda.synchronize()
 assert all(torch.equal(getattr(s, n), getattr(e, n)) for n in ("table", "w", "moment", "loss", "dx"))
 print("equal")
 """
     here = os.path.dirname(os.path.abspath(__file__))
-    r = subprocess.run([sys.executable, "-c", code % (here, os.path.dirname(here))], capture_output=True, text=True, timeout=120)
+    r = subprocess.run([sys.executable, "-c", code % (here, os.path.dirname(here), C, C)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "equal" in r.stdout, r.stderr[-2000:]
