@@ -852,7 +852,11 @@ inline Plan16 plan16(const Gemm16Args& a) {
         struct Costs { double core, bottom, right; };
         auto block = [&](long active) {
             auto most = [](double x, double y) { return x > y ? x : y; };
-            return Costs{most(mma, copy * active), most(mma, copy * active * (1.0 + fm) / 2), most(mma * most(fn, 0.5), copy * active * (1.0 + fn) / 2)};
+            Costs c{most(mma, copy * active), most(mma, copy * active * (1.0 + fm) / 2), most(mma * most(fn, 0.5), copy * active * (1.0 + fn) / 2)};
+            // STATS (without the spilling sums of kLong) of one row of tiles: B comes from memory, once, to pairs at 4.8 TB/s and to
+            // single CTAs at 4.0 (2 rows, 2816 -> 105536: 125 and 147 us)
+            if (mt == 1 && a.epi == GEMM16_STATS && (a.bf16 || kb <= 2 * kRunBlocks)) { const double feed = active * (pair ? 32768.0 / 4.8e6 : 16384.0 / 4.0e6); c.core = most(c.core, feed); c.bottom = most(c.bottom, feed); }
+            return c;
         };
         const Costs full = block(slots);
         const long whole = least > 1 ? 0 : core / slots;

@@ -17,7 +17,7 @@
 // The tensor core truncates when it adds to the accumulator, which biases a sum a little with every addition, more so with
 // fp16 operands, whose products have 22 significant bits (bf16: 16).  The STATS epilogue, whose results are fp32, therefore takes
 // long fp16 reductions in runs of kRunBlocks blocks and adds the runs in registers (kLong: 128 sums a thread, some of which the
-// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us, 1.6 times its reads).
+// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us).
 //
 // Every kernel starts before the one in front of it has ended (programmatic dependent launch): barriers, TMEM and tensor maps
 // are set up meanwhile, and griddepcontrol.wait stands before the first access to global memory.
