@@ -12,7 +12,7 @@
 //
 // All 3 * steps products run in ONE cooperative launch (the roles of the 16-bit GEMM, see tc_gemm16.cu, one product after
 // another) with a barrier of all CTAs between them: a launch of its own costs every product its set-up and the fetching
-// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 122 -> 102 us).
+// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 122 -> 102 us; now 88).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -248,7 +248,7 @@ __device__ __forceinline__ bool ortho_barrier(Gemm16Ctx& c, const OrthoParams& o
         if (ok) mbar_arrive(&c.sh->phase_go_bar);
     }
     ok = __shfl_sync(0xffffffffu, ok, 0);
-    asm volatile("fence.proxy.async;" ::: "memory");          // (the products' results are read through TMA)
+    asm volatile("fence.proxy.async.global;" ::: "memory");   // (the products' results are read through TMA)
     return ok != 0;
 }
 
@@ -301,8 +301,7 @@ __global__ void __launch_bounds__(kThreads16, 1) orthogonalize_kernel(const __gr
                 ok = finish_items<kPair, GEMM16_FINAL, false>(c, o.final, nullptr, nullptr, o.x[cur], o.out);
             __syncwarp();
             if (c.lane == 0) {
-                bulk_wait_group0();
-                asm volatile("fence.proxy.async;" ::: "memory");
+                bulk_wait_group0();      // (their completion includes the proxy fence on this side; a full one took 0.6 us a product)
                 mbar_arrive(&sh.phase_end_bar);
             }
         }
