@@ -826,6 +826,9 @@ inline int operand_tmap(CUtensorMap* tm, const Gemm16Operand& o, int rows, int K
 // where there are SMs to spare); a part costs its trip through L2, 1.2 (128 KB per CTA) or 0.6, plus 4 for the count.
 struct Plan16 { bool pair, mirrored; int splits, part_blocks; long tiles, full_tiles; double time; };
 constexpr long kMostParts = 256;                              // 64 MB of workspace
+// Counters of a launch: one per split tile and epilogue warp of it.
+inline long counter_words(const Plan16& pl) { return (pl.tiles - pl.full_tiles) * (pl.pair ? 16 : 8); }
+static_assert(kMostParts / 2 * 16 * 4 <= long(kGemm16CounterBytes), "a tile in two parts has 16 counters");
 inline Plan16 plan16(const Gemm16Args& a) {
     const long sms = device_sm_count(), kb = (a.K + 63) / 64;
     Plan16 best{};
@@ -889,7 +892,7 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
     p.last_slices = (a.K - (p.k_blocks - 1) * 64 + 15) / 16;
     p.m_tiles = (a.M + tile - 1) / tile;
     p.n_tiles = (a.N + tile - 1) / tile;
-    if (pl.tiles > 2000000000L) return PCL_ERR_UNSUPPORTED_SHAPE;
+    if (pl.tiles > 2000000000L || (pl.splits > 1 && a.epi != GEMM16_PARTS && counter_words(pl) * 4 > long(kGemm16CounterBytes))) return PCL_ERR_UNSUPPORTED_SHAPE;
     p.m_whole = a.M / tile;
     p.n_whole = a.N / tile;
     const long core = pl.mirrored ? long(p.n_whole) * (p.n_whole + 1) / 2 : long(p.m_whole) * p.n_whole;

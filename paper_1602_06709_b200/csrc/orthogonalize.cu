@@ -66,6 +66,7 @@ struct StageArgs {
     __half* xl;                 // what rounding left, times 2^11 (null: not needed)
     int M, N, ld;
     int* counters;              // of the products, to be zeroed
+    unsigned* barrier;          // of all CTAs, to be zeroed
 };
 
 // Sum of squares of U (64-bit: the squares of a gradient leave the range of fp32), and the momentum update.
@@ -112,7 +113,10 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
     for (int i = threadIdx.x; i < a.parts; i += 256) sum += a.part[size_t(blockIdx.y) * kMaxNormBlocks + i];
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (blockIdx.x == 0 && blockIdx.y == 0)
+    {
         for (int i = threadIdx.x; i < int(kGemm16CounterBytes / 4); i += 256) a.counters[i] = 0;
+        if (threadIdx.x == 0) *a.barrier = 0u;
+    }
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = sum;
     __syncthreads();
     sum = 0.0;
@@ -184,7 +188,7 @@ int ortho_form(int count, int M, int N) {
     return time[0] <= time[1] ? GEMM16_FORM_PAIR : GEMM16_FORM_SINGLE;
 }
 
-struct OrthoLayout { size_t part, xl, xh[2], a, b, counters, total; int ld, d, ldd, form; };
+struct OrthoLayout { size_t part, xl, xh[2], a, b, barrier, counters, total; int ld, d, ldd, form; };
 OrthoLayout ortho_layout(int count, int M, int N) {
     OrthoLayout l{};
     size_t at = 0;
@@ -199,6 +203,7 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     for (size_t& o : l.xh) o = take(size_t(count) * M * l.ld * 2);
     l.a = take(size_t(count) * l.d * l.ldd * 2);
     l.b = take(size_t(count) * l.d * l.ldd * 2);
+    l.barrier = take(4);                                     // (all words of the counters may be in use: 128 tiles of pairs in two parts)
     size_t split = kGemm16CounterBytes;
     for (const Gemm16Args& a : {gram_args(count, M, N, l.form), square_args(count, M, N, l.form), apply_args(count, M, N, l.form)}) {
         const size_t b = gemm16_split_ws_bytes(a);
@@ -361,7 +366,8 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     const bool wide = o.M <= o.N;
     const long xb = long(o.M) * l.ld, db = long(l.d) * l.ldd;
     StageArgs s{o.g, o.type, o.momentum, o.mu, o.nesterov, reinterpret_cast<double*>(base + l.part), 0, xh[0],
-                o.steps > 1 ? xl : nullptr, o.M, o.N, l.ld, reinterpret_cast<int*>(base + l.counters)};
+                o.steps > 1 ? xl : nullptr, o.M, o.N, l.ld, reinterpret_cast<int*>(base + l.counters),
+                reinterpret_cast<unsigned*>(base + l.barrier)};
     // four elements at a time where every row starts on a multiple of four (16 bytes of fp32, 8 bytes of the 16-bit types)
     const bool vec = o.N % 4 == 0;
     const double elems = double(o.count) * o.M * o.N;
@@ -420,7 +426,7 @@ int launch_orthogonalize(const OrthoArgs& o, void* ws, cudaStream_t st) {
     if (rc == PCL_OK) rc = make_tmap16(&op.b_out, B, DT_F16, l.d, l.d, o.count, l.ldd, db, 32, 32);
     if (rc != PCL_OK) return rc;
     op.out = o.out; op.steps = o.steps; op.wide = wide;
-    op.barrier = reinterpret_cast<unsigned*>(base + l.counters) + kGemm16CounterBytes / 4 - 1;      // (the tiles' counters end before)
+    op.barrier = reinterpret_cast<unsigned*>(base + l.barrier);
     const double m = l.d, k = o.M < o.N ? o.N : o.M;
     LaunchScope scope(KID_ORTHO, o.steps * o.count * (3.0 * m * m * k + m * m * m), st);
     return l.form == GEMM16_FORM_PAIR ? launch_ortho_kernel<true>(op, st) : launch_ortho_kernel<false>(op, st);

@@ -267,3 +267,24 @@ def test_narrow_update(t, count, M, N, nesterov):
     # sizes of the terms of U are below |dw| + |m|, whose part of `size` is bounded by the largest row sum of |P| times the largest of them
     bound = step * (narrow_bound(o, size, min(M, N), torch.float32) + (2.0 ** -20 * size.max() if nesterov else 0)) + (half_step(t) + 2.0 ** -22) * (want.abs() + w0.abs() + step * o.abs())
     assert bool(((w.double() - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("count,M,N", [(1, 5824, 22016), (1, 4592, 10172), (2, 4183, 4850)])
+def test_products_that_use_every_counter_of_the_split_tiles(count, M, N):
+    """128 tiles of CTA pairs in two parts each: the barrier between the products is no counter of theirs."""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    g = guarded((count, M, N), torch.bfloat16, fill=0)
+    for m in g:
+        m.copy_(torch.randn(M, N, device="cuda", generator=gen))
+    got = run(g)                                  # (into NaN: a block that is left out shows)
+    assert bool(got.isfinite().all())
+    for b in range(count):                        # (one matrix at a time in float64)
+        ref = reference(g[b:b + 1])[0]
+        err, norm = float((got[b].double() - ref).norm()), float(ref.norm())
+        assert err <= (NS_TOL + half_step(torch.bfloat16)) * norm
+        # 32 x 128 blocks, the parts of a warp: none is off by more than its own share of rounding explains.  The direction's elements
+        # are alike in size, so a block's error is its share of the whole's, within the spread of 4096 elements' squares
+        e = (got[b].double() - ref)[:M // 32 * 32, :N // 128 * 128].reshape(M // 32, 32, N // 128, 128)
+        share = e.square().sum((1, 3)).sqrt()
+        assert float(share.max()) <= 4 * (NS_TOL + half_step(torch.bfloat16)) * norm * math.sqrt(4096 / (M * N))
+        del ref, e, share
