@@ -354,7 +354,7 @@ int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const
                             const int* labels, int ignore_label, float* loss, float* row_loss, float* lse,
                             void* ws, size_t ws_bytes, void* cuda_stream);
 /* Its gradient, from the forward call's lse.  The logits are computed again, piece by piece of the classes:
- *   dz[n,k] = g[n] * (exp(z[n,k] - lse[n]) - [k == labels[n]]),   exactly 0 for rows whose label is ignore_label
+ *   dz[n,k] = g[n] * (exp(z[n,k] - lse[n]) - [k == labels[n]]),   exactly 0 for rows whose label is ignore_label or whose lse is -inf
  *   dx = dz w,   dw = dz^T x,   dbias[k] = sum_n dz[n,k]
  * g = row_grad (the gradient of each row's loss, fp32 [N]), or, for row_grad == NULL, 1 / (number of rows whose label is not
  * ignore_label), the gradient of `loss`.  With 16-bit types dz is rounded to that type between the products (fp16: after

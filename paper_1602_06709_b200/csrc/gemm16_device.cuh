@@ -461,7 +461,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             if (p.bias) bias = load_four16(p.bias, cbase + 4 * (lane & (kHalf / 4 - 1)), p.N);
             if (row_ok) label = p.labels[row] - p.col0;
             if constexpr (kEpi == GEMM16_DZ) {
-                if (row_ok) { lse = p.lse[row]; g = p.row_scale[row]; }
+                if (row_ok) { lse = p.lse[row]; g = lse == -INFINITY ? 0.f : p.row_scale[row]; }     // (no finite logit: no gradient)
             }
         }
         if constexpr (kEpi == GEMM16_GENERAL || kEpi == GEMM16_FINAL) {
@@ -645,9 +645,8 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             } else {
                 if constexpr (kEpi == GEMM16_DZ) {
                     const int rel = label - col;
-                    const float ref = lse == -INFINITY ? 0.f : lse;           // a row without any finite logit has p = 0
-                    const float ref2 = ref * kLog2e;
-                    if (fabsf(ref) < kScaledLimit) {
+                    const float ref2 = lse * kLog2e;
+                    if (fabsf(lse) < kScaledLimit) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             const float2 e = fma2(make_float2(v[j], v[j + 1]), make_float2(kLog2e, kLog2e), make_float2(-ref2, -ref2));
@@ -655,14 +654,14 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                         }
                     } else {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) v[j] = ex2((v[j] - ref) * kLog2e);
+                        for (int j = 0; j < 32; ++j) v[j] = ex2((v[j] - lse) * kLog2e);
                     }
                     if (rel >= 0 && rel < 32)
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] -= j == rel ? 1.f : 0.f;
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] *= g;
-                    if (g == 0.f)                                                 // rows left out: exactly 0, whatever z is
+                    if (g == 0.f)                                                 // rows left out or without a finite logit: exactly 0, whatever z is
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0.f;
                 } else {

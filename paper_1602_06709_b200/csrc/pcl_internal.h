@@ -343,7 +343,7 @@ struct Gemm16Args {
     float2* part = nullptr; int part_ld = 0;
     float* label_z = nullptr;
     unsigned* clear = nullptr;               // a word that the launch sets to 0 (null: none)
-    // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0
+    // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0 or lse[r] == -inf
     const float* lse = nullptr;
     const float* row_scale = nullptr;
     // Scratch of gemm16_split_ws_bytes(), 256-byte aligned, or null (then nothing is split).

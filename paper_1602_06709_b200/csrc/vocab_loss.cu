@@ -281,10 +281,10 @@ __global__ void __launch_bounds__(256) piece_dz_kernel(float* __restrict__ z, in
                                                        const float* __restrict__ alpha) {
     for (int n = blockIdx.x; n < N; n += gridDim.x) {
         float* row = z + size_t(n) * P;
-        const float g = row_scale[n] * alpha[0], l = lse[n], ref = l == -INFINITY ? 0.f : l;
+        const float l = lse[n], g = l == -INFINITY ? 0.f : row_scale[n] * alpha[0];     // (no finite logit: no gradient)
         const int rel = labels[n] - col0;
         for (int k = threadIdx.x; k < P; k += 256) {
-            const float q = exp2f((row[k] - ref) * kLog2e) - (k == rel ? 1.f : 0.f);
+            const float q = exp2f((row[k] - l) * kLog2e) - (k == rel ? 1.f : 0.f);
             row[k] = g == 0.f ? 0.f : g * q;
         }
     }

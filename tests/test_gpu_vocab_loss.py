@@ -364,3 +364,35 @@ def test_equal_row_gradients_are_a_factor(t, C):
     for one, both in zip(*results):
         # the same sums, of dz of the same roundings: two roundings of the results remain (fp16: subnormals are absolute)
         assert bool(((both - c * one).abs() <= 2 * half_step(t) * (c * one).abs() * (1 + 2.0 ** -7) + 2.0 ** -24).all())
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("N,C,K", [(130, 64, 400), (40, 72, 9001)])
+def test_rows_without_a_class_have_no_gradient(t, N, C, K):
+    """Logits that all are -inf: lse -inf, loss inf, and dz exactly 0 for the row, as if it were left out with the same row gradients."""
+    c = Case(N, C, K, t, True, 0.0, seed=19)
+    c.w[:, 0] = 0.5                              # (so that a row of x that begins with -inf has no finite logit)
+    lost = [0, 17, N - 1]
+    c.x[lost, 0] = float("-inf")
+    c.forward()
+    c.backward()
+    B.check_device_status()
+    check_guards()
+    assert bool((c.lse[lost] == float("-inf")).all()) and bool((c.row_loss[lost] == float("inf")).all())
+    assert not bool(c.dx[lost].any())
+    assert bool(c.dx.isfinite().all()) and bool(c.dw[:, 1:].isfinite().all()) and bool(c.db.isfinite().all())
+    # (column 0 of dw is a product with -inf)
+    dx, dw, db = c.dx, c.dw, c.db
+    c.labels[lost] = IGNORE
+    c.row_grad = guarded((N,))
+    c.row_grad.fill_(1.0 / N)
+    c.backward()
+    B.check_device_status()
+    assert torch.equal(c.dx, dx) and torch.equal(c.dw[:, 1:], dw[:, 1:]) and torch.equal(c.db, db)
+    # every class of every row
+    c = Case(N, C, K, t, True, 0.0, seed=20)
+    c.bias.fill_(float("-inf"))
+    c.forward()
+    c.backward()
+    B.check_device_status()
+    assert not bool(c.dx.any()) and not bool(c.dw.any()) and not bool(c.db.any())
