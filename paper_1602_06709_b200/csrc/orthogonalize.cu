@@ -250,10 +250,13 @@ __device__ __forceinline__ bool ortho_barrier(Gemm16Ctx& c, const OrthoParams& o
                 }
             }
         }
+        // (the products' results are read through TMA: by this warp, whose lanes have a fence below, and by the epilogue warps, which
+        // the arrival lets go, so that one has to stand before it)
+        asm volatile("fence.proxy.async.global;" ::: "memory");
         if (ok) mbar_arrive(&c.sh->phase_go_bar);
     }
     ok = __shfl_sync(0xffffffffu, ok, 0);
-    asm volatile("fence.proxy.async.global;" ::: "memory");   // (the products' results are read through TMA)
+    asm volatile("fence.proxy.async.global;" ::: "memory");
     return ok != 0;
 }
 

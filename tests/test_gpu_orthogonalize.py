@@ -288,3 +288,26 @@ def test_products_that_use_every_counter_of_the_split_tiles(count, M, N):
         share = e.square().sum((1, 3)).sqrt()
         assert float(share.max()) <= 4 * (NS_TOL + half_step(torch.bfloat16)) * norm * math.sqrt(4096 / (M * N))
         del ref, e, share
+
+
+@pytest.mark.parametrize("t,count,M,N", [(torch.bfloat16, 8, 256, 512), (torch.bfloat16, 1, 1030, 1100), (torch.float32, 2, 130, 260),
+                                         (torch.float16, 1, 700, 2000)])
+def test_repeated_calls_give_the_same_bits(t, count, M, N):
+    """Every product reads, through the asynchronous proxy, what the CTAs have stored before the barrier in front of it: a product that
+    met older tiles would differ from call to call."""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    g = guarded((count, M, N), t, fill=0)
+    g.copy_(torch.randn(count, M, N, device="cuda", generator=gen))
+    ws = workspace(B.orthogonalize_workspace_bytes(count, M, N))
+    first, out = guarded((count, M, N), t), guarded((count, M, N), t)
+    B.orthogonalize(count, M, N, g, first, ws=ws)
+    assert_close(first, reference(g), t)
+    differ = torch.zeros((), dtype=torch.int64, device="cuda")
+    for k in range(200):
+        if k % 2:
+            ws.fill_(k)                           # (and what the workspace held does not matter)
+        B.orthogonalize(count, M, N, g, out, ws=ws)
+        differ += (out != first).sum()
+    B.check_device_status()
+    check_guards()
+    assert int(differ) == 0
