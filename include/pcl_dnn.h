@@ -63,7 +63,7 @@ enum {
  * orthogonalised update below). */
 enum { PCL_F32 = 0, PCL_BF16 = 1, PCL_F16 = 2 };
 
-/* ignore_label / pad_id: no label or id is special */
+/* ignore_label / pad_id: no label or id is special (as a label or id it is itself out of range) */
 #define PCL_NO_ID (-2147483647 - 1)
 
 enum { PCL_PASS_FWD = 0, PCL_PASS_BWD_DATA = 1, PCL_PASS_BWD_WEIGHTS = 2 };

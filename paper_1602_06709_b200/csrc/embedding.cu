@@ -62,7 +62,7 @@ template <int kVec, bool kSgd> constexpr int kReps = kVec == 1 && kSgd ? 2 : 1;
 
 // ids that name no row (outside [0, V)) and the padding id
 __device__ __forceinline__ bool row_exists(int id, int V, int pad_id, unsigned int* status) {
-    if (id == pad_id) return false;
+    if (is_special(id, pad_id)) return false;
     if (id < 0 || id >= V) {
         atomicCAS(status, 0u, static_cast<unsigned int>(kStatusBadLabel));
         return false;

@@ -459,7 +459,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             // the bias of the warp's columns, four per lane: it arrives while the warp waits for the product (a chunk's 64 bytes loaded where
             // they are added took 500 cycles a chunk)
             if (p.bias) bias = load_four16(p.bias, cbase + 4 * (lane & (kHalf / 4 - 1)), p.N);
-            if (row_ok) label = p.labels[row] - p.col0;
+            if (row_ok) label = max(p.labels[row], -1) - p.col0;
             if constexpr (kEpi == GEMM16_DZ) {
                 if (row_ok) { lse = p.lse[row]; g = lse == -INFINITY ? 0.f : p.row_scale[row]; }     // (no finite logit: no gradient)
             }

@@ -16,6 +16,8 @@ namespace pcl {
 // Logistic function from the two approximate special-function instructions (ex2 and rcp, each within 2 ulp): an
 // IEEE division per element costs a one-tile GEMM's epilogue several microseconds.
 __device__ __forceinline__ float sigmoid_fast(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+// Whether a label or id is the call's special one (ignored, padding); PCL_NO_ID says that there is none, and is itself out of range.
+__device__ __forceinline__ bool is_special(int v, int special) { return v == special && v != PCL_NO_ID; }
 #endif
 
 #ifdef __CUDACC__

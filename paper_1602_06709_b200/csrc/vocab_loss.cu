@@ -86,7 +86,7 @@ __device__ __forceinline__ void finish_row(int n, float m, float s, const int* l
     lse[n] = l;
     const int label = labels[n];
     float loss = 0.f;
-    if (label != ignore_label) {
+    if (!is_special(label, ignore_label)) {
         if (label < 0 || label >= K) atomicCAS(status, 0u, static_cast<unsigned int>(kStatusBadLabel));
         else loss = label_z[n] == -INFINITY ? INFINITY : l - label_z[n];
     }
@@ -111,7 +111,7 @@ __device__ __forceinline__ void mean_by_last_block(unsigned* ended, const float*
 #pragma unroll 4
     for (int n = threadIdx.x; n < N; n += 256) {
         sum += __ldcg(row_loss + n);
-        count += labels[n] != ignore_label;
+        count += !is_special(labels[n], ignore_label);
     }
     for (int o = 16; o > 0; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); count += __shfl_xor_sync(0xffffffffu, count, o); }
     if ((threadIdx.x & 31) == 0) { sums[threadIdx.x >> 5] = sum; counts[threadIdx.x >> 5] = count; }
@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__
     int count = 0;
     float top = 0.f;
     for (int n = threadIdx.x; n < N; n += 1024)
-        if (labels[n] != ignore_label) {
+        if (!is_special(labels[n], ignore_label)) {
             ++count;
             if (row_grad) top = fmaxf(top, fabsf(row_grad[n]));
         }
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(1024) grad_rows_kernel(const int* __restrict__
     const float up = type == DT_F16 ? 16384.f : 1.f;      // |dz| <= 2^14
     const bool whole = !row_grad || (type != DT_F32 && top > 1e-30f && top < 1e30f);
     for (int n = threadIdx.x; n < N; n += 1024) {
-        float g = labels[n] == ignore_label ? 0.f : row_grad ? row_grad[n] : 1.f;
+        float g = is_special(labels[n], ignore_label) ? 0.f : row_grad ? row_grad[n] : 1.f;
         if (whole) g = g / top * up;
         row_scale[n] = g;
     }
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(256) piece_stats_kernel(const float* __restric
             float m0 = v.x, s0 = v.y;
             if (col0 > 0) { const float2 o = state[n]; m0 = o.x; s0 = o.y; join(m0, s0, v.x, v.y); }
             state[n] = make_float2(m0, s0);
-            const int rel = labels[n] - col0;
+            const int rel = max(labels[n], -1) - col0;
             if (rel >= 0 && rel < P) label_z[n] = row[rel];
         }
     }
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(256) piece_dz_kernel(float* __restrict__ z, in
     for (int n = blockIdx.x; n < N; n += gridDim.x) {
         float* row = z + size_t(n) * P;
         const float l = lse[n], g = l == -INFINITY ? 0.f : row_scale[n] * alpha[0];     // (no finite logit: no gradient)
-        const int rel = labels[n] - col0;
+        const int rel = max(labels[n], -1) - col0;
         for (int k = threadIdx.x; k < P; k += 256) {
             const float q = exp2f((row[k] - l) * kLog2e) - (k == rel ? 1.f : 0.f);
             row[k] = g == 0.f ? 0.f : g * q;

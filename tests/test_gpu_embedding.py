@@ -268,3 +268,22 @@ def test_row_lengths(t, C):
     assert bool(((dt.double() - want).abs() <= (n + 2) * 2.0 ** -24 * size + h * want.abs() * 1.001 + 2.0 ** -25).all())
     new = old - 0.25 * want
     assert bool(((table.double() - new).abs() <= (n + 4) * 2.0 ** -24 * (size + old.abs()) + h * new.abs() * 1.001 + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("N", [70, 5000])
+def test_the_lowest_id_is_out_of_range(N):
+    """-2^31 stands for "no id is special" as the padding id, so that as an id it is one out of range like -1."""
+    V, C = 100, 40
+    ids = make_ids(N, V, "uniform", 7)
+    ids[5] = -2 ** 31
+    table, dy = put((V, C), torch.float32, 1.0, 8), put((N, C), torch.float32, 1.0, 9)
+    out, grad = guarded((N, C)), guarded((V, C))
+    ws = workspace(B.embedding_workspace_bytes(N, V, C))
+    B.embedding_fwd(N, V, C, ids, table, 1.0, out)
+    assert B.last_device_status() == B.ERR_BAD_LABEL and bool((out[5] == 0).all())
+    B.embedding_bwd(N, V, C, ids, dy, 1.0, grad, ws=ws)
+    assert B.last_device_status() == B.ERR_BAD_LABEL
+    ref, mag = reference_grad(ids, dy, V, 1.0, None)
+    assert bool(((grad.cpu().double() - ref).abs() <= N * 2.0 ** -23 * mag).all())
+    B.embedding_bwd_sgd(N, V, C, ids, dy, 1.0, table, 0.5, ws=ws)
+    assert B.last_device_status() == B.ERR_BAD_LABEL

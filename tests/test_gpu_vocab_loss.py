@@ -396,3 +396,22 @@ def test_rows_without_a_class_have_no_gradient(t, N, C, K):
     c.backward()
     B.check_device_status()
     assert not bool(c.dx.any()) and not bool(c.dw.any()) and not bool(c.db.any())
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32])
+def test_the_lowest_label_is_ignored_only_if_asked_for(t):
+    """-2^31 stands for "no label is special" as the ignored label, so that as a label it is one out of range like -1."""
+    c = Case(60, 64, 200, t, True, 0.0, seed=21)
+    c.ignore = None
+    c.labels[7] = -1
+    c.forward()
+    assert B.last_device_status() == B.ERR_BAD_LABEL
+    c.backward()
+    want = [v.clone() for v in (c.loss, c.row_loss, c.dx, c.dw, c.db)]
+    c.labels[7] = -2 ** 31
+    c.forward()
+    assert B.last_device_status() == B.ERR_BAD_LABEL
+    c.backward()
+    assert B.last_device_status() == B.OK
+    for got, ref in zip((c.loss, c.row_loss, c.dx, c.dw, c.db), want):
+        assert torch.equal(got, ref)
