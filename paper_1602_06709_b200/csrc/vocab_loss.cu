@@ -88,7 +88,7 @@ __device__ __forceinline__ void finish_row(int n, float m, float s, const int* l
     float loss = 0.f;
     if (!is_special(label, ignore_label)) {
         if (label < 0 || label >= K) atomicCAS(status, 0u, static_cast<unsigned int>(kStatusBadLabel));
-        else loss = label_z[n] == -INFINITY ? INFINITY : l - label_z[n];
+        else loss = label_z[n] == -INFINITY && l == -INFINITY ? INFINITY : l - label_z[n];      // (NaN where l is)
     }
     row_loss[n] = loss;
 }

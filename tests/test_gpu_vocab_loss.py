@@ -415,3 +415,20 @@ def test_the_lowest_label_is_ignored_only_if_asked_for(t):
     assert B.last_device_status() == B.OK
     for got, ref in zip((c.loss, c.row_loss, c.dx, c.dw, c.db), want):
         assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("N,C,K", [(130, 64, 400), (8, 2048, 300), (40, 72, 9001)])
+def test_nan_and_infinite_logits_at_a_masked_label(t, N, C, K):
+    """A row with a NaN or +inf logit has NaN results, also where the label's own class is masked with -inf."""
+    c = Case(N, C, K, t, True, 0.0, seed=22)
+    c.bias[:9] = float("-inf")
+    c.bias[40] = float("nan")
+    c.labels[: N // 2] = 3
+    c.forward()
+    B.check_device_status()
+    assert bool(c.lse.isnan().all()) and bool(c.row_loss.isnan().all()) and math.isnan(c.loss.item())
+    c.bias[40] = float("inf")
+    c.forward()
+    B.check_device_status()
+    assert bool(c.lse.isnan().all()) and bool(c.row_loss.isnan().all())
