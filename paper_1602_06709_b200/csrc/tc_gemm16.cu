@@ -17,7 +17,8 @@
 // The tensor core truncates when it adds to the accumulator, which biases a sum a little with every addition, more so with
 // fp16 operands, whose products have 22 significant bits (bf16: 16).  The STATS epilogue, whose results are fp32, therefore takes
 // long fp16 reductions in runs of kRunBlocks blocks and adds the runs in registers (kLong: 128 sums a thread, some of which the
-// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us).
+// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us).  bf16 reductions stay in one run: their
+// log-sum-exp is 2e-4 off at C = 4096 and 1.6e-3 at 16384 where all products have the same sign (z = 28; 1e-5 and 4e-5 where they do not).
 //
 // Every kernel starts before the one in front of it has ended (programmatic dependent launch): barriers, TMEM and tensor maps
 // are set up meanwhile, and griddepcontrol.wait stands before the first access to global memory.
@@ -111,6 +112,10 @@ int gemm16_parts(const Gemm16Args& a) {
     if (s > kb / 4) s = kb / 4;                               // at least four blocks each
     if (s > 8) s = 8;
     if (s < 2) return 1;
+    // ... and, of fp16, at most what the STATS epilogue takes in one run (256 x 16384 -> 3500, products of one sign: parts of 128 blocks
+    // put the log-sum-exp 1.1e-3 off, at 28, in 54 us; now 76)
+    const long least = a.bf16 ? 1 : (kb + 2 * kRunBlocks - 1) / (2 * kRunBlocks);
+    if (s < least) s = least;
     const long part = (kb + s - 1) / s;
     return int((kb + part - 1) / part);
 }

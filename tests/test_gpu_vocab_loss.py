@@ -432,3 +432,20 @@ def test_nan_and_infinite_logits_at_a_masked_label(t, N, C, K):
     c.forward()
     B.check_device_status()
     assert bool(c.lse.isnan().all()) and bool(c.row_loss.isnan().all())
+
+
+@pytest.mark.parametrize("N,C,K", [(256, 16384, 3500), (256, 4096, 1000), (128, 32768, 900)])
+def test_long_sums_of_one_sign_in_parts(N, C, K):
+    """Few rows, long fp16 reductions: no accumulator sums more than 2048 products.  The tensor core truncates at every addition of 16
+    products, by less than 2^-23 of the sum: 128 additions, and the parts are added in fp32."""
+    g = torch.Generator(device="cuda").manual_seed(23)
+    c = Case(N, C, K, torch.float16)
+    c.x.copy_(torch.rand(N, C, device="cuda", generator=g) + 0.5)
+    c.w.copy_((torch.rand(K, C, device="cuda", generator=g) + 0.5) * (20 / C))
+    c.forward()
+    B.check_device_status()
+    check_guards()
+    z = c.x.double() @ c.w.double().t()
+    lse = torch.logsumexp(z, 1)
+    # (ex2, the sums over the classes and the log: 2^-18)
+    assert float((c.lse.double() - lse).abs().max()) <= 128 * 2.0 ** -23 * float(z.max()) + (C / 2048 + 2) * 2.0 ** -24 * float(z.max()) + 2.0 ** -18
