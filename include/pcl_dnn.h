@@ -314,6 +314,9 @@ int pcl_maxpool2x2_bwd_codes(int N, int H, int W, int C, const unsigned char* co
 int pcl_softmax_xent(int N, int K, const float* logits, const int* labels,
                      float* loss, float* dlogits, void* cuda_stream);
 
+/* The embedding, pcl_fc_softmax_xent and orthogonalisation calls below take sizes up to 2^31 - 65537 in each dimension (and 65535
+ * matrices); larger ones return PCL_ERR_UNSUPPORTED_SHAPE, and their workspace query 0. */
+
 /* Embedding lookup: the first layer of a network whose input is a token, i.e. an FC layer on one-hot rows.
  *   out[n,:] = scale * table[ids[n],:]          (computed in fp32, rounded once)
  * Rows of the padding id `pad_id` (PCL_NO_ID: none; it need not lie in [0, V)) are zero.  So are rows of other ids outside

@@ -1132,6 +1132,11 @@ int pcl_softmax_xent(int N, int K, const float* logits, const int* labels, float
 
 namespace {
 bool known_dtype(int t) { return t == PCL_F32 || t == PCL_BF16 || t == PCL_F16; }
+// The kernels of these calls step through rows and columns with 32-bit indices, by at most a grid of blocks beyond the end.
+bool fits_index(int a, int b, int c = 0) {
+    constexpr int kMost = INT_MAX - 65536;
+    return a <= kMost && b <= kMost && c <= kMost;
+}
 // The workspace checks every call with a mandatory workspace makes.
 int check_ws(const void* ws, size_t ws_bytes, size_t need) {
     if (!ws || ws_bytes < need) return PCL_ERR_WORKSPACE;
@@ -1139,7 +1144,7 @@ int check_ws(const void* ws, size_t ws_bytes, size_t need) {
 }
 int check_embedding(int N, int V, int C, int dtype, const int* ids, const void* a, const void* b) {
     if (N <= 0 || V <= 0 || C <= 0 || !known_dtype(dtype) || !ids || !a || !b) return PCL_ERR_BAD_ARG;
-    if (V == INT_MAX) return PCL_ERR_UNSUPPORTED_SHAPE;      // (the key of tokens without a row is V)
+    if (!fits_index(N, V, C)) return PCL_ERR_UNSUPPORTED_SHAPE;
     return aligned16(ids) && aligned16(a) && aligned16(b) ? PCL_OK : PCL_ERR_MISALIGNED;
 }
 int embedding_bwd_impl(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id, void* out,
@@ -1151,6 +1156,7 @@ int embedding_bwd_impl(int N, int V, int C, int dtype, const int* ids, const voi
 }
 int check_vocab_loss(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias, const int* labels, bool backward) {
     if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || !x || !w || !labels) return PCL_ERR_BAD_ARG;
+    if (!fits_index(N, C, K)) return PCL_ERR_UNSUPPORTED_SHAPE;
     // fp32 runs on the FC kernels: a forced tensor-core path takes what they take (checked here, before anything is launched),
     // and the 16-bit products have tensor-core kernels only
     if (dtype == PCL_F32 && g_path.load() == PCL_PATH_TENSOR && (C % 4 != 0 || (backward && K % 4 != 0))) return PCL_ERR_UNSUPPORTED_SHAPE;
@@ -1167,7 +1173,7 @@ int pcl_embedding_fwd(int N, int V, int C, int dtype, const int* ids, const void
 }
 
 size_t pcl_embedding_workspace_bytes(int N, int V, int C) {
-    return N <= 0 || V <= 0 || C <= 0 ? 0 : embedding_workspace_bytes(N, V, C);
+    return N <= 0 || V <= 0 || C <= 0 || !fits_index(N, V, C) ? 0 : embedding_workspace_bytes(N, V, C);
 }
 
 int pcl_embedding_bwd(int N, int V, int C, int dtype, const int* ids, const void* dy, float scale, int pad_id, void* dtable,
@@ -1181,7 +1187,7 @@ int pcl_embedding_bwd_sgd(int N, int V, int C, int dtype, const int* ids, const 
 }
 
 size_t pcl_fc_softmax_xent_workspace_bytes(int N, int C, int K, int dtype, int pass) {
-    if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || (pass != PCL_PASS_FWD && pass != PCL_PASS_BWD_DATA)) return 0;
+    if (N <= 0 || C <= 0 || K <= 0 || !fits_index(N, C, K) || !known_dtype(dtype) || (pass != PCL_PASS_FWD && pass != PCL_PASS_BWD_DATA)) return 0;
     return vocab_loss_workspace_bytes(N, C, K, dtype, pass == PCL_PASS_BWD_DATA);
 }
 
@@ -1214,14 +1220,14 @@ int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const
 namespace {
 int check_ortho(int count, int M, int N, int dtype, int steps, const void* a, const void* b) {
     if (count <= 0 || M <= 0 || N <= 0 || steps <= 0 || !known_dtype(dtype) || !a || !b) return PCL_ERR_BAD_ARG;
-    if (count > 65535) return PCL_ERR_UNSUPPORTED_SHAPE;     // (a grid dimension)
+    if (count > 65535 || !fits_index(M, N)) return PCL_ERR_UNSUPPORTED_SHAPE;     // (count: a grid dimension)
     if (g_path.load() == PCL_PATH_GENERIC) return PCL_ERR_UNSUPPORTED_SHAPE;      // (tensor-core kernels only)
     return aligned16(a) && aligned16(b) ? PCL_OK : PCL_ERR_MISALIGNED;
 }
 }  // namespace
 
 size_t pcl_orthogonalize_workspace_bytes(int count, int M, int N) {
-    return count <= 0 || M <= 0 || N <= 0 ? 0 : orthogonalize_workspace_bytes(count, M, N);
+    return count <= 0 || count > 65535 || M <= 0 || N <= 0 || !fits_index(M, N) ? 0 : orthogonalize_workspace_bytes(count, M, N);
 }
 
 int pcl_orthogonalize(int count, int M, int N, int dtype, const void* g, void* out, int steps, void* ws, size_t ws_bytes,

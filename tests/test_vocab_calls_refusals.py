@@ -117,3 +117,23 @@ def test_forced_kernel_families(B):
         assert L.pcl_orthogonalize(1, 8, 8, B.F32, OK16, OK16, 5, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
     finally:
         B.set_path(B.PATH_AUTO)
+
+
+@pytest.mark.parametrize("size", [2 ** 31 - 1, 2 ** 31 - 16, 2 ** 31 - 9000, 2 ** 31 - 65536])
+def test_sizes_that_indices_would_pass_32_bits_for(B, size):
+    """Kernels step through a dimension by up to a grid of blocks: the last sizes of an int are refused before anything is launched."""
+    L, big = B.lib(), 1 << 60
+    for N, V, C in ((size, 4, 4), (4, size, 4), (4, 4, size)):
+        assert L.pcl_embedding_fwd(N, V, C, 1, OK16, OK16, f(1), 0, OK16, NULL) == B.ERR_UNSUPPORTED_SHAPE
+        assert L.pcl_embedding_bwd(N, V, C, 1, OK16, OK16, f(1), 0, OK16, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+        assert L.pcl_embedding_bwd_sgd(N, V, C, 1, OK16, OK16, f(1), 0, OK16, f(1), OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+        assert B.embedding_workspace_bytes(N, V, C) == 0
+        for d in (0, 1, 2):
+            assert L.pcl_fc_softmax_xent_fwd(N, V, C, d, OK16, OK16, NULL, OK16, -1, OK16, OK16, OK16, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+            assert L.pcl_fc_softmax_xent_bwd(N, V, C, d, OK16, OK16, NULL, OK16, -1, OK16, NULL, NULL, OK16, NULL, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+            assert B.fc_softmax_xent_workspace_bytes(N, V, C, d, B.PASS_FWD) == 0 and B.fc_softmax_xent_workspace_bytes(N, V, C, d, B.PASS_BWD_DATA) == 0
+    for M, N in ((size, 4), (4, size)):
+        assert L.pcl_orthogonalize(1, M, N, 1, OK16, OK16, 5, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+        assert L.pcl_orthogonal_update(1, M, N, 1, OK16, OK16, OK16, f(0.9), 1, f(0.1), f(0), 5, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
+        assert B.orthogonalize_workspace_bytes(1, M, N) == 0
+    assert B.orthogonalize_workspace_bytes(65536, 4, 4) == 0
