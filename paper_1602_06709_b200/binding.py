@@ -397,7 +397,7 @@ def _typed(where, sizes, typed, fp32=(), int32=(), stream=None):
     and returns the type code that those of `typed` share, and the stream handle.  (Written for few interpreter steps: the
     smallest of these calls launch a kernel of two microseconds.)"""
     for n in sizes:
-        if type(n) is not int or n <= 0:
+        if type(n) is not int or n <= 0 or n > 2147483647:          # (ctypes would cut larger ones to 32 bits)
             raise PclError(ERR_BAD_ARG, where)
     first = typed[0][0]
     want, dev = first.dtype, first.get_device()
@@ -448,11 +448,22 @@ def _addr(t):
 
 
 def _id(v):
-    return NO_ID if v is None else int(v)
+    """pad_id / ignore_label as the library takes it."""
+    if v is None:
+        return NO_ID
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:          # (ctypes would cut it to 32 bits, i.e. to another id)
+        raise ValueError(f"an id or label is a 32-bit integer, not {v}")
+    return v
+
+
+def _size(n):
+    """A size as the library takes it: what does not fit in 32 bits is refused there like the largest that does."""
+    return min(n, 2147483647)
 
 
 def embedding_workspace_bytes(N, V, C) -> int:
-    return int(lib().pcl_embedding_workspace_bytes(N, V, C))
+    return int(lib().pcl_embedding_workspace_bytes(*map(_size, (N, V, C))))
 
 
 def embedding_fwd(N, V, C, ids, table, scale, out, pad_id=None, stream=None):
@@ -480,7 +491,7 @@ def embedding_bwd_sgd(N, V, C, ids, dy, scale, table, lr, pad_id=None, ws=None, 
 
 def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
     """dtype: dtype_code() of the operands; which: PASS_FWD or PASS_BWD_DATA."""
-    return int(lib().pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, which))
+    return int(lib().pcl_fc_softmax_xent_workspace_bytes(*map(_size, (N, C, K)), dtype, which))
 
 
 def fc_softmax_xent_fwd(N, C, K, x, w, bias, labels, loss, row_loss, lse, ignore_label=None, ws=None, stream=None):
@@ -505,19 +516,19 @@ def fc_softmax_xent_bwd(N, C, K, x, w, bias, labels, lse, row_grad, dx, dw, dbia
 
 
 def orthogonalize_workspace_bytes(count, M, N) -> int:
-    return int(lib().pcl_orthogonalize_workspace_bytes(count, M, N))
+    return int(lib().pcl_orthogonalize_workspace_bytes(*map(_size, (count, M, N))))
 
 
 def orthogonalize(count, M, N, g, out, steps=5, ws=None, stream=None):
     """out = g / |g| after `steps` Newton-Schulz steps, for each of `count` M x N matrices."""
-    d, s = _typed("pcl_orthogonalize", (count, M, N), [(g, count * M * N), (out, count * M * N)], stream=stream)
+    d, s = _typed("pcl_orthogonalize", (count, M, N, steps), [(g, count * M * N), (out, count * M * N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_orthogonalize(count, M, N, d, _addr(g), _addr(out), steps, wp, wb, s), "pcl_orthogonalize")
 
 
 def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_decay=0.0, steps=5, ws=None, stream=None):
     """momentum <- mu momentum + dw, then w <- (1 - lr weight_decay) w - lr sqrt(max(1, M/N)) * orthogonalize(direction)."""
-    d, s = _typed("pcl_orthogonal_update", (count, M, N), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)], stream=stream)
+    d, s = _typed("pcl_orthogonal_update", (count, M, N, steps), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)], stream=stream)
     wp, wb = _ws(ws)
     _check(lib().pcl_orthogonal_update(count, M, N, d, _addr(w), _addr(dw), _addr(momentum), mu,
                                        1 if nesterov else 0, lr, weight_decay, steps, wp, wb,

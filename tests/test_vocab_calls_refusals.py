@@ -137,3 +137,23 @@ def test_sizes_that_indices_would_pass_32_bits_for(B, size):
         assert L.pcl_orthogonal_update(1, M, N, 1, OK16, OK16, OK16, f(0.9), 1, f(0.1), f(0), 5, OK16, big, NULL) == B.ERR_UNSUPPORTED_SHAPE
         assert B.orthogonalize_workspace_bytes(1, M, N) == 0
     assert B.orthogonalize_workspace_bytes(65536, 4, 4) == 0
+
+
+def test_integers_beyond_32_bits(B):
+    """ctypes cuts integers to 32 bits: 2^32 would be the id 0."""
+    import torch
+    a, ids = torch.zeros(4, 8), torch.zeros(4, dtype=torch.int32)
+    assert B._id(None) == B.NO_ID and B._id(-2 ** 31) == B.NO_ID and B._id(2 ** 31 - 1) == 2 ** 31 - 1 and B._id(-1) == -1
+    for v in (2 ** 31, 2 ** 32, -2 ** 31 - 1):
+        with pytest.raises(ValueError):
+            B._id(v)
+    for steps in (2 ** 32 + 5, 0, -1, 5.0):
+        with pytest.raises(B.PclError) as e:
+            B.orthogonalize(1, 4, 8, a, a, steps=steps)
+        assert e.value.code == B.ERR_BAD_ARG
+        with pytest.raises(B.PclError):
+            B.orthogonal_update(1, 4, 8, a, a, a, 0.9, True, 0.1, steps=steps)
+    with pytest.raises(B.PclError):
+        B.embedding_fwd(4, 2 ** 32 + 4, 8, ids, a, 1.0, a)
+    assert B.embedding_workspace_bytes(4, 2 ** 32 + 4, 8) == 0 and B.orthogonalize_workspace_bytes(1, 2 ** 32 + 4, 8) == 0
+    assert B.fc_softmax_xent_workspace_bytes(4, 8, 2 ** 32 + 4, B.BF16, B.PASS_FWD) == 0
