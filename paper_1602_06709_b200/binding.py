@@ -392,9 +392,9 @@ def dtype_code(t) -> int:
     return _DTYPES[t.dtype]
 
 
-def _typed(where, sizes, typed, fp32=(), int32=(), stream=None):
-    """Checks the tensors of a call -- (tensor, element count) pairs, None allowed; all contiguous, on the current device --
-    and returns the type code that those of `typed` share, and the stream handle.  (Written for few interpreter steps: the
+def _typed(where, sizes, typed, fp32=(), int32=(), stream=None, ws=None):
+    """Checks the tensors of a call -- (tensor, element count) pairs, None allowed; all contiguous, on the current device,
+    and so the workspace -- and returns the type code that those of `typed` share, and the stream handle.  (Written for few interpreter steps: the
     smallest of these calls launch a kernel of two microseconds.)"""
     for n in sizes:
         if type(n) is not int or n <= 0 or n > 2147483647:          # (ctypes would cut larger ones to 32 bits)
@@ -412,6 +412,8 @@ def _typed(where, sizes, typed, fp32=(), int32=(), stream=None):
     for t, n in int32:
         if not (t.dtype is torch.int32 and t.numel() == n and t.get_device() == dev and t.is_contiguous()):
             ok = False
+    if ws is not None and ws.get_device() != dev:
+        ok = False
     if not ok:
         _explain(where, typed, fp32, int32)
     if dev != torch.cuda.current_device():
@@ -475,7 +477,7 @@ def embedding_fwd(N, V, C, ids, table, scale, out, pad_id=None, stream=None):
 
 def embedding_bwd(N, V, C, ids, dy, scale, dtable, pad_id=None, ws=None, stream=None):
     """dtable[v] = scale * sum of dy[n] over the tokens n with ids[n] == v; every row is written."""
-    d, s = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)], stream=stream)
+    d, s = _typed("pcl_embedding_bwd", (N, V, C), [(dy, N * C), (dtable, V * C)], int32=[(ids, N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_embedding_bwd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(dtable), wp, wb,
                                    s), "pcl_embedding_bwd")
@@ -483,7 +485,7 @@ def embedding_bwd(N, V, C, ids, dy, scale, dtable, pad_id=None, ws=None, stream=
 
 def embedding_bwd_sgd(N, V, C, ids, dy, scale, table, lr, pad_id=None, ws=None, stream=None):
     """table[v] -= lr * dtable[v] in place for the rows that occur; dtable is not stored."""
-    d, s = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)], stream=stream)
+    d, s = _typed("pcl_embedding_bwd_sgd", (N, V, C), [(dy, N * C), (table, V * C)], int32=[(ids, N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_embedding_bwd_sgd(N, V, C, d, _addr(ids), _addr(dy), scale, _id(pad_id), _addr(table),
                                        lr, wp, wb, s), "pcl_embedding_bwd_sgd")
@@ -497,7 +499,7 @@ def fc_softmax_xent_workspace_bytes(N, C, K, dtype: int, which: int) -> int:
 def fc_softmax_xent_fwd(N, C, K, x, w, bias, labels, loss, row_loss, lse, ignore_label=None, ws=None, stream=None):
     """Mean loss, loss and log-sum-exp of each row of softmax(x w^T + bias), without storing the logits."""
     d, s = _typed("pcl_fc_softmax_xent_fwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K)],
-               [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)], stream=stream)
+               [(loss, 1), (row_loss, N), (lse, N)], [(labels, N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_fc_softmax_xent_fwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label),
                                          _addr(loss), _addr(row_loss), _addr(lse), wp, wb, s),
@@ -508,7 +510,7 @@ def fc_softmax_xent_bwd(N, C, K, x, w, bias, labels, lse, row_grad, dx, dw, dbia
     """dx (or None), dw and dbias (or None) from the forward call's lse; row_grad: gradient of each row's loss, or None for
     the gradient of the mean."""
     d, s = _typed("pcl_fc_softmax_xent_bwd", (N, C, K), [(x, N * C), (w, K * C), (bias, K), (dx, N * C), (dw, K * C), (dbias, K)],
-               [(lse, N), (row_grad, N)], [(labels, N)], stream=stream)
+               [(lse, N), (row_grad, N)], [(labels, N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_fc_softmax_xent_bwd(N, C, K, d, _addr(x), _addr(w), _addr(bias), _addr(labels), _id(ignore_label), _addr(lse),
                                          _addr(row_grad), _addr(dx), _addr(dw), _addr(dbias), wp, wb, s),
@@ -521,14 +523,14 @@ def orthogonalize_workspace_bytes(count, M, N) -> int:
 
 def orthogonalize(count, M, N, g, out, steps=5, ws=None, stream=None):
     """out = g / |g| after `steps` Newton-Schulz steps, for each of `count` M x N matrices."""
-    d, s = _typed("pcl_orthogonalize", (count, M, N, steps), [(g, count * M * N), (out, count * M * N)], stream=stream)
+    d, s = _typed("pcl_orthogonalize", (count, M, N, steps), [(g, count * M * N), (out, count * M * N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_orthogonalize(count, M, N, d, _addr(g), _addr(out), steps, wp, wb, s), "pcl_orthogonalize")
 
 
 def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_decay=0.0, steps=5, ws=None, stream=None):
     """momentum <- mu momentum + dw, then w <- (1 - lr weight_decay) w - lr sqrt(max(1, M/N)) * orthogonalize(direction)."""
-    d, s = _typed("pcl_orthogonal_update", (count, M, N, steps), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)], stream=stream)
+    d, s = _typed("pcl_orthogonal_update", (count, M, N, steps), [(w, count * M * N), (dw, count * M * N)], [(momentum, count * M * N)], stream=stream, ws=ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_orthogonal_update(count, M, N, d, _addr(w), _addr(dw), _addr(momentum), mu,
                                        1 if nesterov else 0, lr, weight_decay, steps, wp, wb,

@@ -157,3 +157,26 @@ def test_integers_beyond_32_bits(B):
         B.embedding_fwd(4, 2 ** 32 + 4, 8, ids, a, 1.0, a)
     assert B.embedding_workspace_bytes(4, 2 ** 32 + 4, 8) == 0 and B.orthogonalize_workspace_bytes(1, 2 ** 32 + 4, 8) == 0
     assert B.fc_softmax_xent_workspace_bytes(4, 8, 2 ** 32 + 4, B.BF16, B.PASS_FWD) == 0
+
+
+def test_a_workspace_of_another_device(B):
+    import torch
+
+    class OnDevice:
+        """What the checks ask a tensor."""
+        def __init__(self, n, dtype, device):
+            self.n, self.dtype, self.device = n, dtype, device
+        def numel(self): return self.n
+        def get_device(self): return self.device
+        def is_contiguous(self): return True
+
+    mk = lambda n, dt=torch.float32: OnDevice(n, dt, 0)
+    a, r, ids = mk(32), mk(4), mk(4, torch.int32)
+    for device in (1, -1):
+        ws = OnDevice(1 << 20, torch.uint8, device)
+        for call in (lambda: B.embedding_bwd(4, 4, 8, ids, a, 1.0, a, ws=ws), lambda: B.embedding_bwd_sgd(4, 4, 8, ids, a, 1.0, a, 0.1, ws=ws),
+                     lambda: B.fc_softmax_xent_fwd(4, 8, 4, a, a, None, ids, mk(1), r, r, ws=ws),
+                     lambda: B.fc_softmax_xent_bwd(4, 8, 4, a, a, None, ids, r, None, a, a, None, ws=ws),
+                     lambda: B.orthogonalize(1, 4, 8, a, a, ws=ws), lambda: B.orthogonal_update(1, 4, 8, a, a, a, 0.9, True, 0.1, ws=ws)):
+            with pytest.raises(ValueError, match="current CUDA device"):
+                call()
