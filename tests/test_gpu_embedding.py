@@ -287,3 +287,15 @@ def test_the_lowest_id_is_out_of_range(N):
     assert bool(((grad.cpu().double() - ref).abs() <= N * 2.0 ** -23 * mag).all())
     B.embedding_bwd_sgd(N, V, C, ids, dy, 1.0, table, 0.5, ws=ws)
     assert B.last_device_status() == B.ERR_BAD_LABEL
+
+
+@pytest.mark.parametrize("t,N,V,C,kind,pad", [
+    # more tokens than one cluster's shared memory takes: the sorted sequence stays in global memory
+    (torch.float32, 65537, 300, 8, "zipf", None), (torch.bfloat16, 70000, 1000, 24, "zipf", 0), (torch.float16, 70000, 90000, 33, "uniform", 5),
+    (torch.float32, 66000, 2, 4, "two", 1), (torch.bfloat16, 200001, 513, 8, "zipf", None), (torch.bfloat16, 70000, 131072, 8, "mod", None),
+    # the shared-memory sort's largest, and three digits of ids in either
+    (torch.float32, 65536, 1000, 8, "uniform", None), (torch.float32, 5000, 16777300, 4, "zipf", None),
+    (torch.bfloat16, 5000, 16777300, 4, "uniform", 3), (torch.bfloat16, 70000, 16777300, 4, "zipf", 0)])
+@pytest.mark.parametrize("sgd", [False, True])
+def test_gradient_of_many_tokens_and_many_rows(t, N, V, C, kind, pad, sgd):
+    test_gradient(t, N, V, C, kind, pad, sgd)
