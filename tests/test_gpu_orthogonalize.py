@@ -311,3 +311,50 @@ def test_repeated_calls_give_the_same_bits(t, count, M, N):
     B.check_device_status()
     check_guards()
     assert int(differ) == 0
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e-7, 1.0, 1e15, 1e25, 1e36])
+@pytest.mark.parametrize("M,N", [(96, 160), (300, 130)])
+def test_tensor_core_form_norms_out_of_the_range_of_fp32_squares(scale, M, N):
+    g = guarded((1, M, N), torch.float32, fill=0)
+    g.copy_(spectrum(1, M, N, "gauss", 4) * scale)
+    got, ref = run(g), reference(g)
+    # (below |g| ~ 1e-7 the eps of the definition makes X small: the planes and the last step's operands have steps of 2^-24 of
+    # the scaled unit 2^-14, i.e. errors of 2^-39, which 3.4445^5 = 485 bounds)
+    if scale >= 1e-7:
+        assert_close(got, ref, torch.float32)
+    else:
+        assert float((got.double() - ref).abs().max()) <= 485 * 2.0 ** -37 + NS_TOL * float(ref.abs().max())
+
+
+def test_tensor_core_form_zero_and_nan_matrices_of_a_batch():
+    g = guarded((4, 80, 140), torch.float32, fill=0)
+    g.copy_(spectrum(4, 80, 140, "gauss", 5))
+    g[0] = 0
+    g[2, 3, 4] = float("nan")
+    g[3, 79, 139] = float("inf")
+    got = run(g)
+    assert not bool(got[0].any()) and bool(got[2:].isnan().all())
+    assert_close(got[1:2], reference(g[1:2]), torch.float32)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e-7, 1.0, 1e15, 1e25, 1e36])
+@pytest.mark.parametrize("M,N", [(64, 80), (200, 31)])
+def test_narrow_norms_out_of_the_range_of_fp32_squares(scale, M, N):
+    g = guarded((1, M, N), torch.float32, fill=0)
+    g.copy_(spectrum(1, M, N, "gauss", 4) * scale)
+    got = run(g)
+    ref, size = narrow_reference(g)
+    assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, min(M, N), torch.float32)).all())
+
+
+def test_narrow_zero_and_nan_matrices_of_a_batch():
+    g = guarded((4, 40, 24), torch.float32, fill=0)
+    g.copy_(spectrum(4, 40, 24, "gauss", 5))
+    g[0] = 0
+    g[2, 3, 4] = float("nan")
+    g[3, 39, 23] = float("inf")
+    got = run(g)
+    assert not bool(got[0].any()) and bool(got[2:].isnan().all())
+    ref, size = narrow_reference(g[1:2])
+    assert bool(((got[1:2].double() - ref).abs() <= narrow_bound(ref, size, 24, torch.float32)).all())
