@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
     __syncthreads();
     sum = 0.0;
     for (int i = 0; i < 8; ++i) sum += red[i];
-    const float inv = float(1.0 / (sqrt(sum) + kNsEps));
+    const float inv = float(kScaleX / (sqrt(sum) + kNsEps));       // (1 / norm by itself may lie below the range of fp32)
     const size_t off = size_t(a.M) * a.N * blockIdx.y, off_x = size_t(a.M) * a.ld * blockIdx.y;
     for (int r = blockIdx.x; r < a.M; r += gridDim.x)
 #pragma unroll 2
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(256) ortho_stage_kernel(StageArgs a) {
                 load_vec<kVec>(a.g, a.type, i, u);
             }
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) u[j] *= inv * kScaleX;
+            for (int j = 0; j < kVec; ++j) u[j] *= inv;
             alignas(8) __half h[kVec], l[kVec];
 #pragma unroll
             for (int j = 0; j < kVec; ++j) {

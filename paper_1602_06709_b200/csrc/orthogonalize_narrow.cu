@@ -40,7 +40,7 @@ struct NarrowArgs {
     int d, k, wide, pieces, chunks, steps;       // wide: the matrix is d x k, else k x d
     unsigned by_d;                               // e / d = e * by_d >> 20 for e < 4096
     double* part;                                // [count][chunks][dim][dim], dim = d rounded up to 16, 32 or 64
-    float* p; float* inv;                        // [count][kDim][kDim], [count]
+    float* p; float2* inv;                       // [count][kDim][kDim]; [count]: X0 = (U * x) * y, x a power of two
     void* out; float keep, step;
 };
 
@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kStepThreads) narrow_steps_kernel(NarrowArgs a
     __syncthreads();
     for (int i = threadIdx.x; i < side * kLd; i += kStepThreads) A[i] *= inv * inv;
     __syncthreads();
-    if (rank == 0 && threadIdx.x == 0) a.inv[matrix] = float(inv);
+    // (norms from 2^100: their reciprocal times 2^64, because fp32 has fewer bits below 2^-126)
+    if (rank == 0 && threadIdx.x == 0) a.inv[matrix] = inv < 0x1p-100 ? make_float2(0x1p-64f, float(inv * 0x1p64)) : make_float2(1.f, float(inv));
     for (int s = 0; s < a.steps; ++s) {
         const bool last = s + 1 == a.steps;
         each([&](int own, int row, bool has) {
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(256, 2) narrow_apply_kernel(NarrowArgs a) {
     const size_t base = size_t(blockIdx.y) * a.d * a.k;
     const float4* src = reinterpret_cast<const float4*>(a.p + size_t(blockIdx.y) * kDim * kDim);
     for (int i = threadIdx.x; i < a.d * (kDim / 4); i += 256) reinterpret_cast<float4*>(p)[i] = __ldcg(src + i);
-    const float inv = __ldcg(a.inv + blockIdx.y);
+    const float2 inv = __ldcg(a.inv + blockIdx.y);
     for (int piece = blockIdx.x; piece < a.pieces; piece += gridDim.x) {
         const int l0 = piece * kPiece, length = a.k - l0 < kPiece ? a.k - l0 : kPiece;
         const T* g = static_cast<const T*>(a.g) + base;
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(256, 2) narrow_apply_kernel(NarrowArgs a) {
         for (int i = 0; i < 4 * kB; ++i)
             if (const Place p = at(i); p.ok) {
                 const float v = !a.momentum ? value(u[i]) : a.nesterov ? fmaf(a.mu, m[i], value(u[i])) : m[i];
-                x[p.j * (kPiece + 4) + p.l] = v * inv;
+                x[p.j * (kPiece + 4) + p.l] = v * inv.x * inv.y;
             }
         __syncthreads();
         float acc[kB][4] = {};
@@ -320,7 +321,7 @@ NarrowLayout narrow_layout(int count, int M, int N) {
     if (l.chunks > most) l.chunks = most;
     l.part = take(size_t(count) * l.chunks * l.side * l.side * 8);
     l.p = take(size_t(count) * kDim * kDim * 4);
-    l.inv = take(size_t(count) * 4);
+    l.inv = take(size_t(count) * 8);
     l.total = at;
     return l;
 }
@@ -347,7 +348,7 @@ int launch_orthogonalize_narrow(const OrthoArgs& o, void* ws, cudaStream_t st) {
     const bool wide = o.M <= o.N;
     const int d = wide ? o.M : o.N, k = wide ? o.N : o.M;
     NarrowArgs a{o.g, o.type, o.momentum, o.mu, o.nesterov, d, k, wide, l.pieces, l.chunks, o.steps, unsigned((1u << 20) / unsigned(d) + 1),
-                 reinterpret_cast<double*>(base + l.part), reinterpret_cast<float*>(base + l.p), reinterpret_cast<float*>(base + l.inv),
+                 reinterpret_cast<double*>(base + l.part), reinterpret_cast<float*>(base + l.p), reinterpret_cast<float2*>(base + l.inv),
                  o.out, 1.f - o.lr * o.weight_decay, o.lr * sqrtf(o.M > o.N ? float(o.M) / float(o.N) : 1.f)};
     const double elems = double(o.count) * o.M * o.N, eb = double(dtype_bytes(o.type));
     {

@@ -358,3 +358,18 @@ def test_narrow_zero_and_nan_matrices_of_a_batch():
     assert not bool(got[0].any()) and bool(got[2:].isnan().all())
     ref, size = narrow_reference(g[1:2])
     assert bool(((got[1:2].double() - ref).abs() <= narrow_bound(ref, size, 24, torch.float32)).all())
+
+
+@pytest.mark.parametrize("count,M,N", [(1, 64, 20000), (1, 30000, 16), (1, 700, 30000)])
+def test_norms_beyond_the_range_of_fp32(count, M, N):
+    """|g| above 2^128 / 2^2, whose reciprocal has fewer bits as an fp32 number."""
+    gen = torch.Generator(device="cuda").manual_seed(M)
+    g = guarded((count, M, N), torch.float32, fill=0)
+    g.copy_(torch.randn(count, M, N, device="cuda", generator=gen) * 4e37)
+    assert bool(g.isfinite().all()) and float(g.double().norm()) > 2.0 ** 131
+    got = run(g)
+    if min(M, N) <= 64:
+        ref, size = narrow_reference(g)
+        assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, min(M, N), torch.float32)).all())
+    else:
+        assert_close(got, reference(g), torch.float32)
