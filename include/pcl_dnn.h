@@ -348,8 +348,10 @@ int pcl_embedding_bwd_sgd(int N, int V, int C, int dtype, const int* ids, const 
  * and the next pcl_last_device_status() returns PCL_ERR_BAD_LABEL.  Logits of -inf (a bias that masks classes) have
  * probability 0; a row whose logits all are -inf has lse -inf, loss inf and gradient 0; a NaN or +inf logit makes its
  * row's results NaN.  All sums are in a fixed order.
- * dtype PCL_BF16 / PCL_F16: products on the 16-bit tensor cores, exact products and fp32 sums.  PCL_F32: TF32 products, as
- * everywhere in this library.
+ * dtype PCL_BF16 / PCL_F16: products on the 16-bit tensor cores, exact products and fp32 sums whose additions truncate (products
+ * of one sign, C = 4096, logits of 28: lse 2e-4 off in bf16, 1e-4 in fp16; of either sign 1e-5).  PCL_F32: TF32 products, as
+ * everywhere in this library, and the logits stored after all, up to 256 MB of them at a time in the workspace (C % 4 != 0, and
+ * K % 4 != 0 in the gradient, run on the CUDA cores).
  * x: [N][C], w: [K][C], bias: [K] or NULL, all in, of type dtype; labels: int32 [N]; loss: [1], row_loss: [N], lse: [N]
  * out, fp32.  Workspace: pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, PCL_PASS_FWD), 256-byte aligned. */
 size_t pcl_fc_softmax_xent_workspace_bytes(int N, int C, int K, int dtype, int pass);
@@ -361,7 +363,8 @@ int pcl_fc_softmax_xent_fwd(int N, int C, int K, int dtype, const void* x, const
  *   dx = dz w,   dw = dz^T x,   dbias[k] = sum_n dz[n,k]
  * g = row_grad (the gradient of each row's loss, fp32 [N]), or, for row_grad == NULL, 1 / (number of rows whose label is not
  * ignore_label), the gradient of `loss`.  With 16-bit types dz is rounded to that type between the products (fp16: after
- * scaling by a power of two that keeps it in range); the results are rounded once.
+ * scaling by a power of two that keeps it in range); the results are rounded once.  x of the rows whose dz is 0 is still a factor
+ * of dw and has to be finite.
  * dx: [N][C] out or NULL; dw: [K][C] out; dbias: [K] out or NULL; all of type dtype.  Deterministic.
  * Workspace: pcl_fc_softmax_xent_workspace_bytes(N, C, K, dtype, PCL_PASS_BWD_DATA). */
 int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const void* w, const void* bias,
@@ -371,8 +374,11 @@ int pcl_fc_softmax_xent_bwd(int N, int C, int K, int dtype, const void* x, const
 /* Orthogonalisation of `count` matrices by Newton-Schulz steps (the direction of the Muon update):
  *   X = g / (|g|_F + 1e-7);   `steps` times:  A = X X^T,  X <- a X + (b A + c A A) X     (a, b, c = 3.4445, -4.7750, 2.0315;
  *   for a matrix with more rows than columns the same on its transpose);   out = X
- * g, out: [count][M][N] of type dtype (out may be g).  steps >= 1 (5 is usual).  The products take fp16 operands with fp32
- * sums; relative error (2-norm) of the result 1e-3 .. 2e-3 besides the rounding to dtype.  A zero matrix gives zero.
+ * g, out: [count][M][N] of type dtype (out may be g).  steps >= 1 (5 is usual).  A zero matrix gives zero.  Relative error
+ * (2-norm) of the result after 5 steps, besides the rounding to dtype: below 5e-3, as a rule 3e-4 .. 2e-3, because the products take
+ * fp16 operands; 1e-6 for matrices with a side of at most 32, or of at most 64 in calls of up to 32 matrices, whose steps are
+ * taken in 64 bits.  A product that lasts longer than the limit of the device-side waits (2 s: sides of some 100 000) ends in
+ * PCL_ERR_DEVICE_TIMEOUT; knob WAIT_LIMIT_US.
  * Workspace: pcl_orthogonalize_workspace_bytes(count, M, N), 256-byte aligned. */
 size_t pcl_orthogonalize_workspace_bytes(int count, int M, int N);
 int pcl_orthogonalize(int count, int M, int N, int dtype, const void* g, void* out, int steps,

@@ -108,8 +108,7 @@ __device__ __forceinline__ void st_shared_u4(uint32_t addr, uint32_t x, uint32_t
 // Work item: a tile of one matrix and the reduction blocks [k0, k1) of it; part < 0: all of them.
 struct Item16 { int b, m, n, k0, k1, part, split_tile; };
 // A CTA's (pair's) items: one of each wave, in turn from the wave's front and from its back, so that with items in the order of
-// falling cost all CTAs get about the same (8200 x 4100 update, 4100 being 16 tiles and 4 columns: its square product 88 -> 75 us,
-// the whole 2.49 -> 2.44 ms).  hop in the roles' loops: the steps to the next item, in turn.
+// falling cost all CTAs get about the same (8200 x 4100 update, 4100 being 16 tiles and 4 columns: its square product 88 -> 75 us).  hop in the roles' loops: the steps to the next item, in turn.
 // Columns the MMAs of a tile compute: the last tile's are rounded up to 32.
 __device__ __forceinline__ int tile_width(const Gemm16Params& p, int n, int bn) {
     const int left = p.N - n * bn;

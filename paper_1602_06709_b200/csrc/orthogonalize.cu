@@ -6,13 +6,14 @@
 // <= 1.5, |B| <= 2.9 by the polynomial), so fp16 has the three mantissa bits that bf16 lacks at no loss of range.  X
 // itself keeps 22 bits until the last step, in two fp16 planes of which the products see the first; the last step takes the
 // rounded X in its linear term too, so that the rounding is passed on by the polynomial's derivative (which is small at 1)
-// instead of by B alone.  Relative error of the result (2-norm) 3e-4 .. 1.6e-3 on random, decaying and nearly low-rank
-// spectra, where bf16 iterates give 1e-2 .. 2e-1.  (Narrow matrices: orthogonalize_narrow.cu.)
+// instead of by B alone.  Relative error of the result (2-norm) 3e-4 .. 2e-3 on random, decaying and nearly low-rank
+// spectra (up to 2.8e-3 where all singular values are alike; batches of 33 .. 64 rows 2.5e-3 and 4.1e-3), where bf16 iterates
+// give 1e-2 .. 2e-1.  The Gram product's sums are not cut: 2.0e-3 with 2^20 columns too.  (Narrow matrices: orthogonalize_narrow.cu.)
 // A and A A are symmetric: the tiles below the diagonal are copies of those above it.
 //
 // All 3 * steps products run in ONE cooperative launch (the roles of the 16-bit GEMM, see tc_gemm16.cu, one product after
 // another) with a barrier of all CTAs between them: a launch of its own costs every product its set-up and the fetching
-// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 122 -> 102 us; now 88).
+// of its code, together as much as a product of 512 x 512 matrices takes (8 x 256 x 512: 122 -> 102 us; now 90).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -193,7 +194,7 @@ OrthoLayout ortho_layout(int count, int M, int N) {
     OrthoLayout l{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t o = at; at += align_up(bytes, 256); return o; };
-    // rows of whole 128-byte lines: TMA writes a row of a tile into other rows' sectors otherwise (8200 x 4100: 2.44 -> 2.03 ms)
+    // rows of whole 128-byte lines: TMA writes a row of a tile into other rows' sectors otherwise (8200 x 4100: a sixth of the time)
     l.ld = int(align_up(N, 64));
     l.d = M < N ? M : N;
     l.ldd = int(align_up(l.d, 64));

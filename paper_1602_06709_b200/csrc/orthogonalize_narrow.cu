@@ -12,7 +12,7 @@
 // of 32 x 256: 42 us; 64 rows: 98 instead of 108 us, 32 of them 93 instead of 75).
 // Against the tensor-core form, where a matrix of 16 rows fills 6 % of a tile and the 15 products' latencies are all of the time:
 // 16 x 172 57 -> 16 us, 64 x 4096 140 -> 48 us, 1000 of 32 x 64 220 -> 149 us; many matrices of 64 rows are its side's
-// (1000 of 64 x 64: 291 instead of 548 us).  Its error, 2.0e-3 with 16 .. 40 rows against 1.2e-3 with 256, is 1e-7 here.
+// (1000 of 64 x 64: 291 instead of 548 us).  Its error, 2.0e-3 with 16 .. 40 rows against 1.6e-3 with 256, is 1e-7 here.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

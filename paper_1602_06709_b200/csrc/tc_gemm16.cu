@@ -17,8 +17,10 @@
 // The tensor core truncates when it adds to the accumulator, which biases a sum a little with every addition, more so with
 // fp16 operands, whose products have 22 significant bits (bf16: 16).  The STATS epilogue, whose results are fp32, therefore takes
 // long fp16 reductions in runs of kRunBlocks blocks and adds the runs in registers (kLong: 128 sums a thread, some of which the
-// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us).  bf16 reductions stay in one run: their
-// log-sum-exp is 2e-4 off at C = 4096 and 1.6e-3 at 16384 where all products have the same sign (z = 28; 1e-5 and 4e-5 where they do not).
+// pair form spills; its main loops are long enough to hide that: 2 rows, 2856 -> 105536 forward 186 us).  bf16
+// reductions stay in one run: their log-sum-exp is 2e-4 off at C = 4096 and 1.6e-3 at 16384 where all products have the same sign
+// (z = 28), and 1e-5 and 4e-5 where they do not.  So do those of the DZ epilogue: fp16, C = 4096, dx is 1.7e-3 off where all
+// products have the same sign, 2.4e-4 (the roundings') where they do not.
 //
 // Every kernel starts before the one in front of it has ended (programmatic dependent launch): barriers, TMEM and tensor maps
 // are set up meanwhile, and griddepcontrol.wait stands before the first access to global memory.

@@ -21,7 +21,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr size_t kPieceBytes = size_t(256) << 20;
 // dx sums over no more classes than this in one accumulator: the tensor core's additions truncate.  What goes beyond is added in
 // fp32, rounded: the parts of a split product where there are few enough tiles (39 rows, 304 -> 123078: 107 us, 255 in
-// pieces), else pieces of so many classes.
+// pieces), else pieces of so many classes.  dw's sums over the rows are not cut: where all products have the same sign they are 3e-5 to
+// 2e-4 low with 65536 rows and 4e-4 with 10^6, less than half a step of fp16 (4.9e-4).
 constexpr int kMostClasses = 16384;
 
 __device__ __forceinline__ float elem16(const void* p, int type, size_t i) {
