@@ -373,3 +373,36 @@ def test_norms_beyond_the_range_of_fp32(count, M, N):
         assert bool(((got.double() - ref).abs() <= narrow_bound(ref, size, min(M, N), torch.float32)).all())
     else:
         assert_close(got, reference(g), torch.float32)
+
+
+@pytest.mark.parametrize("M,N", [(33000, 66000), (66100, 32900), (40, 55000000), (100000000, 24)])
+def test_offsets_beyond_32_bits(M, N):
+    """A matrix of more than 2^31 elements that is zero but for its last corner, which decides the result."""
+    m, n = min(M, 512), min(N, 700)
+    g = torch.zeros(1, M, N, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(M % 1000)
+    corner = torch.randn(1, m, n, device="cuda", generator=gen).bfloat16()
+    g[:, M - m:, N - n:] = corner
+    ws = workspace(B.orthogonalize_workspace_bytes(1, M, N))
+    B.orthogonalize(1, M, N, g, g, ws=ws)
+    B.check_device_status()
+    check_guards()
+    got = g[:, M - m:, N - n:].clone()
+    assert_close(got, reference(corner), torch.bfloat16)
+    g[:, M - m:, N - n:] = 0
+    assert not bool(g.any())                     # zero rows and columns of X stay zero
+
+
+def test_batch_offsets_beyond_32_bits():
+    count, M, N = 36, 7800, 7800                 # 2.2e9 elements
+    g = torch.empty(count, M, N, dtype=torch.bfloat16, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    for m in g:
+        m.copy_(torch.randn(M, N, device="cuda", generator=gen))
+    out = torch.full_like(g, float("nan"))
+    B.orthogonalize(count, M, N, g, out, ws=workspace(B.orthogonalize_workspace_bytes(count, M, N)))
+    B.check_device_status()
+    check_guards()
+    for b in (0, count - 1):
+        assert_close(out[b:b + 1], reference(g[b:b + 1]), torch.bfloat16)
+    assert bool(out.isfinite().all())
