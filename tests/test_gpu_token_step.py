@@ -214,3 +214,36 @@ print("equal")
     here = os.path.dirname(os.path.abspath(__file__))
     r = subprocess.run([sys.executable, "-c", code % (here, os.path.dirname(here), C, C)], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0 and "equal" in r.stdout, r.stderr[-2000:]
+
+
+def test_updates_on_two_streams_at_once():
+    """The update's products are one cooperative launch that takes the whole GPU: two of them, and another call's products beside
+    them, on streams and workspaces of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    M, N = 1100, 1500
+    dw = torch.randn(1, M, N, device="cuda", generator=gen).bfloat16()
+    w0 = torch.randn(1, M, N, device="cuda", generator=gen).bfloat16()
+    mk = lambda: (w0.clone(), torch.zeros(1, M, N, device="cuda"), workspace(B.orthogonalize_workspace_bytes(1, M, N)))
+    steps = 12
+    call = lambda s: B.orthogonal_update(1, M, N, s[0], dw, s[1], 0.9, True, 0.02, ws=s[2])
+    want = mk()
+    for _ in range(steps):
+        call(want)
+    loss = [TokenStep(200, 300, 96, 500, torch.bfloat16) for _ in range(2)]
+    for _ in range(steps):
+        loss[0].step()
+    states, streams = [mk(), mk()], [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(steps):
+        for s, st in zip(streams, states):
+            with torch.cuda.stream(s):
+                call(st)
+        with torch.cuda.stream(streams[2]):
+            loss[1].step()
+    torch.cuda.synchronize()
+    B.check_device_status()
+    check_guards()
+    for st in states:
+        assert torch.equal(st[0], want[0]) and torch.equal(st[1], want[1])
+    for name in ("table", "w", "moment", "loss"):
+        assert torch.equal(getattr(loss[0], name), getattr(loss[1], name)), name
