@@ -59,8 +59,8 @@ enum {
     PCL_ERR_BAD_LABEL = 8          /* a call met a class label or token id outside its range */
 };
 
-/* Element types of the calls that take more than fp32 (the void* tensors of the vocabulary calls and of the
- * orthogonalised update below). */
+/* Element types of the calls that take more than fp32 (the void* tensors of the vocabulary calls, of the
+ * orthogonalised update and of the calls behind it). */
 enum { PCL_F32 = 0, PCL_BF16 = 1, PCL_F16 = 2 };
 
 /* ignore_label / pad_id: no label or id is special (as a label or id it is itself out of range) */
@@ -390,6 +390,70 @@ int pcl_orthogonalize(int count, int M, int N, int dtype, const void* g, void* o
 int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const void* dw, float* momentum, float mu,
                           int nesterov, float lr, float weight_decay, int steps, void* ws, size_t ws_bytes,
                           void* cuda_stream);
+
+/* RMS norm of the N rows of a residual stream.
+ *   h = x + residual (h = x for residual == NULL),   rstd[n] = 1 / sqrt(mean_c h[n,c]^2 + eps),   y[n,c] = h[n,c] * rstd[n] * w[c]
+ * The norm is that of the sum before it is rounded to dtype; sums are fp32 in a fixed order.  Rows whose squares leave fp32's range are
+ * scaled by a power of two first, so any finite row has a finite rstd; an infinity or NaN makes its row's results NaN (finite
+ * elements beside an infinity: 0).  Results are defined by the formula at eps = 0 too (a row of zeros: NaN).
+ * x, residual: [N][C] in; w: [C] in; h: [N][C] out or NULL (NULL where residual is); y: [N][C] out; all of type dtype; rstd: fp32 [N] out
+ * or NULL.  h may be x or residual, y may be any input of its size.  Sizes up to 2^31 - 65537 each; eps finite and >= 0. */
+int pcl_rms_norm_fwd(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps,
+                     void* h, void* y, float* rstd, void* cuda_stream);
+/* The same with y in 8 bits, one scale for each row (the operand of a product on 8-bit tensor cores):
+ *   y_scale[n] = max(max_c |y[n,c]| / 448, 2^-126),   y8[n,c] = e4m3(y[n,c] / y_scale[n])      (rounded to nearest, from fp32)
+ * y8: [N][C] bytes out, y_scale: fp32 [N] out.  A row with an infinity or NaN has a scale that is not finite. */
+int pcl_rms_norm_fwd_q8(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps,
+                        void* h, void* y8, float* y_scale, float* rstd, void* cuda_stream);
+/* Its gradient, from h and rstd of the forward call (x, where it had no residual):
+ *   g = dy * w,  n = h * rstd;    dx = dh + rstd * (g - n * mean_c(g * n)),    dw[c] = sum_n dy[n,c] * n[n,c]
+ * dh: the gradient that reaches h past the norm, or NULL; dx is the gradient of x and of the residual alike.  dw: [C] out or NULL, summed in
+ * fp32 in a fixed order.  dx may be h, dy or dh.  rstd: fp32 [N] in, everything else of type dtype.
+ * Workspace (not needed for dw == NULL): pcl_rms_norm_workspace_bytes(N, C), 256-byte aligned. */
+size_t pcl_rms_norm_workspace_bytes(int N, int C);
+int pcl_rms_norm_bwd(int N, int C, int dtype, const void* h, const void* w, const float* rstd, const void* dy, const void* dh,
+                     void* dx, void* dw, void* ws, size_t ws_bytes, void* cuda_stream);
+/* The rows of a matrix in 8 bits as above, without a norm (weights of an 8-bit layer):
+ *   scale[n] = max(max_c |x[n,c]| / 448, 2^-126),   q[n,c] = e4m3(x[n,c] / scale[n])  */
+int pcl_quantize_rows(int N, int C, int dtype, const void* x, void* q, float* scale, void* cuda_stream);
+
+/* Norm of `count` tensors as one vector, e.g. of the gradients of all parameters, and clipping by it:
+ *   norm = sqrt(sum_i sum_j grads[i][j]^2),   f = min(1, max_norm / (norm + 1e-6))
+ *   pcl_grad_clip:           out[i] = f * grads[i]           (out[i] may be grads[i])
+ *   pcl_sgd_update_clipped:  w[i] <- w[i] - lr * f * grads[i]
+ * grads, out, w: HOST arrays of `count` device pointers (aligned to their elements; NULL where sizes[i] is 0), sizes: elements of each (up to
+ * 2^34), dtypes: PCL_F32, PCL_BF16 or PCL_F16 for each (of both its tensors); all four are read before the call returns.  Tensors
+ * may be views of one buffer, but none that is written may overlap another.  norm: fp32 device scalar out.  Squares are
+ * summed in fp32 and 64 bits in a fixed order, and any finite tensors have the norm that they have in 64 bits.  A norm that is not
+ * finite goes by the formula: f is 0 or NaN (infinite and NaN elements become, and make weights, NaN).
+ * max_norm >= 0.  Workspace: pcl_grad_norm_workspace_bytes(count), 256-byte aligned. */
+size_t pcl_grad_norm_workspace_bytes(int count);
+int pcl_grad_norm(int count, const void* const* grads, const size_t* sizes, const int* dtypes, float* norm,
+                  void* ws, size_t ws_bytes, void* cuda_stream);
+int pcl_grad_clip(int count, const void* const* grads, void* const* out, const size_t* sizes, const int* dtypes, float max_norm,
+                  float* norm, void* ws, size_t ws_bytes, void* cuda_stream);
+int pcl_sgd_update_clipped(int count, void* const* w, const void* const* grads, const size_t* sizes, const int* dtypes, float lr,
+                           float max_norm, float* norm, void* ws, size_t ws_bytes, void* cuda_stream);
+
+/* Chooses a token of each row of logits z (the answer of the output layer whose loss is pcl_fc_softmax_xent_fwd).
+ *   p[k] ~ exp(z[k] / temperature).  In the order of falling z (equal logits: rising k) a first part of the tokens is kept:
+ *     the first top_k of them;
+ *     of these, those in front of which less than top_p of their probability lies;
+ *     of these, those with p[k] >= min_p * the largest p.
+ *   token = the first k, in rising order, at which the cumulated probability of the kept tokens exceeds `uniform` times their total
+ *   logprob = log of the probability with which it was chosen (p of the kept tokens, renormalised)
+ * uniform: fp32 [N] in [0, 1) (values outside count as the nearest inside; NaN as 0).  temperature, top_k, top_p, min_p: [N] device arrays, or
+ * NULL for 1, none, none, none.  temperature <= 0: the largest logit, the lowest k of equal ones, logprob 0.  top_k <= 0 or > K,
+ * top_p >= 1 or NaN, min_p <= 0 or NaN: no filter; top_p <= 0: the largest; min_p > 1: 1.
+ * Logits of -inf are never chosen; +inf takes everything.  A row without any finite or infinite positive logit, with a NaN, or with
+ * a NaN temperature has token -1 and logprob NaN.
+ * Weights are held in 64 bits (whole multiples of 2^-44 of the largest; 2^-(62 - log2 K) for K > 2^18; smaller ones are 0) and summed
+ * exactly: the same choice for the same inputs, always.  logits: [N][K] of type dtype; token: int32 [N] out; logprob: fp32 [N] out or
+ * NULL.  Sizes up to 2^31 - 65537 each.  Workspace: pcl_sample_tokens_workspace_bytes(N, K) (0 is possible), 256-byte aligned. */
+size_t pcl_sample_tokens_workspace_bytes(int N, int K);
+int pcl_sample_tokens(int N, int K, int dtype, const void* logits, const float* uniform, const float* temperature,
+                      const int* top_k, const float* top_p, const float* min_p, int* token, float* logprob,
+                      void* ws, size_t ws_bytes, void* cuda_stream);
 
 /* Synchronises the stream, then reads and clears the device status word of the
  * current device.  PCL_OK, PCL_ERR_DEVICE_TIMEOUT, PCL_ERR_BAD_LABEL or PCL_ERR_CUDA. */

@@ -38,6 +38,9 @@ EXPORTS = [
     "pcl_orthogonalize_workspace_bytes", "pcl_orthogonalize", "pcl_orthogonal_update",
     "pcl_conv_bwd_weights_pooled_staged", "pcl_conv_bwd_weights_sgd", "pcl_conv_bwd_weights_sgd_workspace_bytes",
     "pcl_fc_bwd_fused_sgd", "pcl_fc_bwd_fused_sgd_workspace_bytes", "pcl_plan_cache_stats",
+    "pcl_rms_norm_fwd", "pcl_rms_norm_fwd_q8", "pcl_rms_norm_workspace_bytes", "pcl_rms_norm_bwd", "pcl_quantize_rows",
+    "pcl_grad_norm_workspace_bytes", "pcl_grad_norm", "pcl_grad_clip", "pcl_sgd_update_clipped",
+    "pcl_sample_tokens_workspace_bytes", "pcl_sample_tokens",
 ]
 
 
@@ -118,6 +121,20 @@ def lib() -> ctypes.CDLL:
         L.pcl_orthogonalize_workspace_bytes.restype = sz
         L.pcl_orthogonalize.argtypes = [ci, ci, ci, ci, vp, vp, ci, vp, sz, vp]
         L.pcl_orthogonal_update.argtypes = [ci, ci, ci, ci, vp, vp, vp, cf, ci, cf, cf, ci, vp, sz, vp]
+        L.pcl_rms_norm_fwd.argtypes = [ci, ci, ci, vp, vp, vp, cf, vp, vp, vp, vp]
+        L.pcl_rms_norm_fwd_q8.argtypes = [ci, ci, ci, vp, vp, vp, cf, vp, vp, vp, vp, vp]
+        L.pcl_rms_norm_workspace_bytes.argtypes = [ci, ci]
+        L.pcl_rms_norm_workspace_bytes.restype = sz
+        L.pcl_rms_norm_bwd.argtypes = [ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.pcl_quantize_rows.argtypes = [ci, ci, ci, vp, vp, vp, vp]
+        L.pcl_grad_norm_workspace_bytes.argtypes = [ci]
+        L.pcl_grad_norm_workspace_bytes.restype = sz
+        L.pcl_grad_norm.argtypes = [ci, vp, vp, vp, vp, vp, sz, vp]
+        L.pcl_grad_clip.argtypes = [ci, vp, vp, vp, vp, cf, vp, vp, sz, vp]
+        L.pcl_sgd_update_clipped.argtypes = [ci, vp, vp, vp, vp, cf, cf, vp, vp, sz, vp]
+        L.pcl_sample_tokens_workspace_bytes.argtypes = [ci, ci]
+        L.pcl_sample_tokens_workspace_bytes.restype = sz
+        L.pcl_sample_tokens.argtypes = [ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.pcl_last_device_status.argtypes = [vp]
         L.pcl_launch_count.restype = ctypes.c_ulonglong
         L.pcl_last_wait_code.restype = ctypes.c_uint
@@ -535,6 +552,140 @@ def orthogonal_update(count, M, N, w, dw, momentum, mu, nesterov, lr, weight_dec
     _check(lib().pcl_orthogonal_update(count, M, N, d, _addr(w), _addr(dw), _addr(momentum), mu,
                                        1 if nesterov else 0, lr, weight_decay, steps, wp, wb,
                                        s), "pcl_orthogonal_update")
+
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _bytes8(where, like, tensors, types=(E4M3, torch.uint8)):
+    """Checks the 8-bit tensors of a call: (tensor, element count) pairs, contiguous, on the device of `like`."""
+    dev = like.get_device()
+    for t, n in tensors:
+        if t.dtype not in types:
+            raise TypeError(f"{where}: an 8-bit tensor (float8_e4m3fn or uint8) is wanted, not {t.dtype}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{where}: a contiguous tensor of {n} elements is wanted")
+        if t.get_device() != dev:
+            raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+
+
+def rms_norm_fwd(N, C, x, residual, w, eps, h, y, rstd=None, stream=None):
+    """h = x + residual (residual and h may be None), y = h / sqrt(mean(h^2) + eps) * w, rstd = 1 / sqrt(mean(h^2) + eps)."""
+    d, s = _typed("pcl_rms_norm_fwd", (N, C), [(x, N * C), (residual, N * C), (w, C), (h, N * C), (y, N * C)], [(rstd, N)], stream=stream)
+    _check(lib().pcl_rms_norm_fwd(N, C, d, _addr(x), _addr(residual), _addr(w), eps, _addr(h), _addr(y), _addr(rstd), s),
+           "pcl_rms_norm_fwd")
+
+
+def rms_norm_fwd_q8(N, C, x, residual, w, eps, h, y8, y_scale, rstd=None, stream=None):
+    """rms_norm_fwd with y as e4m3 values (a float8_e4m3fn or uint8 tensor) and a scale for each row."""
+    d, s = _typed("pcl_rms_norm_fwd_q8", (N, C), [(x, N * C), (residual, N * C), (w, C), (h, N * C)], [(rstd, N), (y_scale, N)], stream=stream)
+    _bytes8("pcl_rms_norm_fwd_q8", x, [(y8, N * C)])
+    _check(lib().pcl_rms_norm_fwd_q8(N, C, d, _addr(x), _addr(residual), _addr(w), eps, _addr(h), _addr(y8), _addr(y_scale),
+                                     _addr(rstd), s), "pcl_rms_norm_fwd_q8")
+
+
+def rms_norm_workspace_bytes(N, C) -> int:
+    return int(lib().pcl_rms_norm_workspace_bytes(*map(_size, (N, C))))
+
+
+def rms_norm_bwd(N, C, h, w, rstd, dy, dh, dx, dw, ws=None, stream=None):
+    """dx = dh (or 0) + the gradient through the norm; dw (or None): the gradient of its weights."""
+    d, s = _typed("pcl_rms_norm_bwd", (N, C), [(h, N * C), (w, C), (dy, N * C), (dh, N * C), (dx, N * C), (dw, C)], [(rstd, N)],
+                  stream=stream, ws=ws)
+    wp, wb = _ws(ws)
+    _check(lib().pcl_rms_norm_bwd(N, C, d, _addr(h), _addr(w), _addr(rstd), _addr(dy), _addr(dh), _addr(dx), _addr(dw), wp, wb, s),
+           "pcl_rms_norm_bwd")
+
+
+def quantize_rows(N, C, x, q, scale, stream=None):
+    """q: the rows of x as e4m3 values, scale: max |row| / 448."""
+    d, s = _typed("pcl_quantize_rows", (N, C), [(x, N * C)], [(scale, N)], stream=stream)
+    _bytes8("pcl_quantize_rows", x, [(q, N * C)])
+    _check(lib().pcl_quantize_rows(N, C, d, _addr(x), _addr(q), _addr(scale), s), "pcl_quantize_rows")
+
+
+class TensorList:
+    """Several tensors (contiguous, of one device, each fp32, bf16 or fp16) as the calls over many tensors take them.  The list is of the
+    tensors' memory as it is when the list is made, and keeps that memory alive."""
+
+    def __init__(self, tensors):
+        self.tensors = [t.detach() for t in tensors]
+        n = len(self.tensors)
+        if n == 0:
+            raise ValueError("a list of one tensor or more is wanted")
+        self.device = self.tensors[0].get_device()
+        for t in self.tensors:
+            if t.get_device() != self.device or self.device < 0 or not t.is_contiguous():
+                raise ValueError("contiguous tensors on one CUDA device are wanted")
+        self.dtypes = tuple(dtype_code(t) for t in self.tensors)
+        self.sizes = tuple(t.numel() for t in self.tensors)
+        self._pointers = (ctypes.c_void_p * n)(*[t.data_ptr() if t.numel() else None for t in self.tensors])
+        self._sizes = (ctypes.c_size_t * n)(*self.sizes)
+        self._dtypes = (ctypes.c_int * n)(*self.dtypes)
+        self.pointers, self.counts, self.types = (ctypes.addressof(a) for a in (self._pointers, self._sizes, self._dtypes))
+
+    def __len__(self):
+        return len(self.tensors)
+
+
+def _lists(where, lists, norm, stream, ws):
+    """Checks tensor lists (alike in sizes and types), the norm and the workspace; returns the stream handle."""
+    first = lists[0]
+    dev = first.device
+    for other in lists[1:]:
+        if other.sizes != first.sizes or other.dtypes != first.dtypes:
+            raise ValueError(f"{where}: lists of the same sizes and types are wanted")
+        if other.device != dev:
+            raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+    if norm.dtype is not torch.float32:
+        raise TypeError(f"{where}: a torch.float32 tensor is wanted, not {norm.dtype}")
+    if norm.numel() != 1:
+        raise ValueError(f"{where}: a tensor of 1 element is wanted")
+    if norm.get_device() != dev or (ws is not None and ws.get_device() != dev) or dev != torch.cuda.current_device():
+        raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+    return stream.cuda_stream if stream is not None else _raw_stream(dev)
+
+
+def grad_norm_workspace_bytes(tensors) -> int:
+    """tensors: a TensorList, or how many tensors."""
+    return int(lib().pcl_grad_norm_workspace_bytes(_size(tensors if isinstance(tensors, int) else len(tensors))))
+
+
+def grad_norm(grads, norm, ws=None, stream=None):
+    """norm = the 2-norm of all tensors of the list `grads` together."""
+    s = _lists("pcl_grad_norm", (grads,), norm, stream, ws)
+    wp, wb = _ws(ws)
+    _check(lib().pcl_grad_norm(len(grads), grads.pointers, grads.counts, grads.types, _addr(norm), wp, wb, s), "pcl_grad_norm")
+
+
+def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
+    """out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)); out may be grads."""
+    s = _lists("pcl_grad_clip", (grads, out), norm, stream, ws)
+    wp, wb = _ws(ws)
+    _check(lib().pcl_grad_clip(len(grads), grads.pointers, out.pointers, grads.counts, grads.types, max_norm, _addr(norm), wp, wb, s),
+           "pcl_grad_clip")
+
+
+def sgd_update_clipped(params, grads, lr, max_norm, norm, ws=None, stream=None):
+    """params[i] -= lr * min(1, max_norm / (norm + 1e-6)) * grads[i], in place."""
+    s = _lists("pcl_sgd_update_clipped", (grads, params), norm, stream, ws)
+    wp, wb = _ws(ws)
+    _check(lib().pcl_sgd_update_clipped(len(grads), params.pointers, grads.pointers, grads.counts, grads.types, lr, max_norm,
+                                        _addr(norm), wp, wb, s), "pcl_sgd_update_clipped")
+
+
+def sample_tokens_workspace_bytes(N, K) -> int:
+    return int(lib().pcl_sample_tokens_workspace_bytes(*map(_size, (N, K))))
+
+
+def sample_tokens(N, K, logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, ws=None, stream=None):
+    """token[n] of each row of logits, chosen by uniform[n] after temperature, top-k, top-p and min-p ([N] tensors, top_k int32)."""
+    ints = [(token, N)] if top_k is None else [(token, N), (top_k, N)]
+    d, s = _typed("pcl_sample_tokens", (N, K), [(logits, N * K)], [(uniform, N), (temperature, N), (top_p, N), (min_p, N), (logprob, N)], ints,
+                  stream=stream, ws=ws)
+    wp, wb = _ws(ws)
+    _check(lib().pcl_sample_tokens(N, K, d, _addr(logits), _addr(uniform), _addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p),
+                                   _addr(token), _addr(logprob), wp, wb, s), "pcl_sample_tokens")
 
 
 def last_device_status(stream=None) -> int:

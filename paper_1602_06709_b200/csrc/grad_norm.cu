@@ -1,0 +1,297 @@
+// Norm of many tensors as one vector, and what training does with it: clipped copies of them, or the clipped SGD step.
+//
+//   norm = sqrt(sum g^2),  f = min(1, max_norm / (norm + 1e-6));   out = f g   or   w <- w - lr f g
+//
+// Bound by memory: one launch reads the tensors, a second one reads them again and writes.  The work is cut into items of 16 KB that do not
+// cross tensors; the blocks take them in turn, the second launch from the end, where the first one left the L2 full.  The tensors'
+// addresses and sizes are kernel parameters, so a call needs no copy and can be captured.
+//
+// Every 64 bytes or so are squared and summed in fp32 and added up in 64 bits, in a fixed order; where an fp32 sum leaves the range in which it
+// loses nothing, the same squares are taken in 64 bits.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include "pcl_internal.h"
+#include "pcl_ptx.cuh"
+
+namespace pcl {
+
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kVectors = 4;                                  // 16-byte vectors of an item per thread
+constexpr unsigned kItemBytes = kBlock * kVectors * 16;
+constexpr int kBlocksPerSm = 4;
+constexpr int kMostTensors = 640;                            // of a launch: its parameters are limited to 32 KB
+
+// Tensors of a launch.  lead: elements between the 16-byte boundary below a gradient and its start; first: its first item.
+template <int kMost> struct Tensors {
+    int count;
+    unsigned items;
+    const void* g[kMost];
+    void* out[kMost];
+    unsigned long long n[kMost];
+    unsigned first[kMost];
+    unsigned char type[kMost], lead[kMost];
+};
+
+struct ApplyParams {
+    const double* partial;
+    int partials;
+    float max_norm, lr;
+    float* norm;
+};
+
+__device__ __forceinline__ void unpack(const uint4& q, int type, float (&v)[8]) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (type == DT_F32) { v[i] = __uint_as_float(u[i]); v[4 + i] = 0.f; }
+        else if (type == DT_BF16) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+        else { const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u[i])); v[2 * i] = h.x; v[2 * i + 1] = h.y; }
+    }
+}
+__device__ __forceinline__ uint32_t narrow(float v, int type) {
+    if (type == DT_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    return __half_as_ushort(__float2half_rn(v));
+}
+__device__ __forceinline__ uint4 pack(const float (&v)[8], int type) {
+    if (type == DT_F32) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = narrow(v[2 * i], type) | narrow(v[2 * i + 1], type) << 16;
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+// Element i of a vector as bits, and a vector of which only the elements [lo, hi) exist.
+template <class P>
+__device__ __forceinline__ uint4 load_some(const P* base, int type, int lo, int hi) {
+    uint32_t u[4] = {0u, 0u, 0u, 0u};
+    if (type == DT_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i >= lo && i < hi) u[i] = reinterpret_cast<const uint32_t*>(base)[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i >= lo && i < hi) u[i / 2] |= uint32_t(reinterpret_cast<const uint16_t*>(base)[i]) << (16 * (i % 2));
+    }
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+__device__ __forceinline__ void store_some(void* base, int type, const uint4& q, int lo, int hi) {
+    const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+    if (type == DT_F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i >= lo && i < hi) static_cast<uint32_t*>(base)[i] = u[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i >= lo && i < hi) static_cast<uint16_t*>(base)[i] = uint16_t(u[i / 2] >> (16 * (i % 2)));
+    }
+}
+
+// Sum over the block, in a fixed order; every thread gets it.
+__device__ __forceinline__ double block_sum(double s, double* words) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) words[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+    for (int i = 0; i < kBlock / 32; ++i) s += words[i];
+    return s;
+}
+__device__ __forceinline__ double sum_partials(const double* partial, int n, double* words) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < n; i += kBlock) s += __ldcg(partial + i);
+    return block_sum(s, words);
+}
+
+
+
+template <int kMost>
+__device__ __forceinline__ void find_tensor(const Tensors<kMost>& p, unsigned item, int& t) {      // (empty tensors have no items)
+    while (t + 1 < p.count && item >= p.first[t + 1]) ++t;
+    while (item < p.first[t]) --t;
+}
+
+// The elements [lo, hi) of a vector that belong to the tensor, from the vector's index and the tensor's size; all of them as a rule.
+struct Part { int lo, hi; };
+__device__ __forceinline__ Part part_of(unsigned long long vec, int per, int lead, unsigned long long n) {
+    const unsigned long long e = vec * per, end = n + lead;
+    return {e < unsigned(lead) ? int(lead - e) : 0, e + per <= end ? per : e < end ? int(end - e) : 0};
+}
+
+template <int kMost>
+__global__ void __launch_bounds__(kBlock) sum_squares_kernel(const __grid_constant__ Tensors<kMost> p, double* partial) {
+    __shared__ double words[kBlock / 32];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    double total = 0.0;
+    int t = 0;
+    for (unsigned item = blockIdx.x; item < p.items; item += gridDim.x) {
+        find_tensor(p, item, t);
+        const int type = p.type[t], lead = p.lead[t], per = type == DT_F32 ? 4 : 8;
+        const char* base = static_cast<const char*>(p.g[t]) - lead * (16 / per);
+        const unsigned long long v0 = (unsigned long long)(item - p.first[t]) * (kBlock * kVectors) + threadIdx.x;
+        uint4 q[kVectors];
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const unsigned long long vec = v0 + i * kBlock;
+            const Part e = part_of(vec, per, lead, p.n[t]);
+            q[i] = e.lo == 0 && e.hi == per ? *reinterpret_cast<const uint4*>(base + vec * 16)
+                                            : load_some(base + vec * 16, type, e.lo, e.hi);
+        }
+        float s = 0.f;
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            float v[8];
+            unpack(q[i], type, v);
+            any |= q[i].x | q[i].y | q[i].z | q[i].w;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s = fmaf(v[j], v[j], s);
+        }
+        if ((s > 1e-28f && s < 1e36f) || any == 0) {
+            total += double(s);
+        } else {                                              // squares that fp32 does not hold (or an infinity, or NaN)
+#pragma unroll
+            for (int i = 0; i < kVectors; ++i) {
+                float v[8];
+                unpack(q[i], type, v);
+#pragma unroll 1
+                for (int j = 0; j < 8; ++j) total = fma(double(v[j]), double(v[j]), total);
+            }
+        }
+    }
+    total = block_sum(total, words);
+    if (threadIdx.x == 0) partial[blockIdx.x] = total;
+}
+
+__global__ void __launch_bounds__(kBlock) norm_kernel(const double* partial, int n, float* norm) {
+    __shared__ double words[kBlock / 32];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const double s = sum_partials(partial, n, words);
+    if (threadIdx.x == 0) *norm = float(sqrt(s));
+}
+
+// kSgd: out are the weights, stepped in place; else out = f g.
+template <int kMost, bool kSgd>
+__global__ void __launch_bounds__(kBlock) apply_kernel(const __grid_constant__ Tensors<kMost> p, const ApplyParams a) {
+    __shared__ double words[kBlock / 32];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const double norm = sqrt(sum_partials(a.partial, a.partials, words));
+    const double ratio = double(a.max_norm) / (norm + 1e-6);
+    const float f = ratio >= 1.0 ? 1.f : float(ratio);       // (a NaN stays one)
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = float(norm);
+    const float step = -a.lr * f;
+    int t = p.count - 1;
+    for (unsigned i0 = blockIdx.x; i0 < p.items; i0 += gridDim.x) {
+        const unsigned item = p.items - 1 - i0;
+        find_tensor(p, item, t);
+        const int type = p.type[t], lead = p.lead[t], per = type == DT_F32 ? 4 : 8;
+        const char* base = static_cast<const char*>(p.g[t]) - lead * (16 / per);
+        char* out = static_cast<char*>(p.out[t]) - lead * (16 / per);
+        const bool even = (reinterpret_cast<uintptr_t>(out) & 15) == 0;      // out lies like g: whole vectors there too
+        const unsigned long long v0 = (unsigned long long)(item - p.first[t]) * (kBlock * kVectors) + threadIdx.x;
+        uint4 q[kVectors], w[kVectors];
+        Part e[kVectors];
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const unsigned long long vec = v0 + i * kBlock;
+            e[i] = part_of(vec, per, lead, p.n[t]);
+            const bool whole = e[i].lo == 0 && e[i].hi == per;
+            q[i] = whole ? *reinterpret_cast<const uint4*>(base + vec * 16) : load_some(base + vec * 16, type, e[i].lo, e[i].hi);
+            if (kSgd) w[i] = whole && even ? *reinterpret_cast<const uint4*>(out + vec * 16) : load_some(out + vec * 16, type, e[i].lo, e[i].hi);
+        }
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            float g[8], x[8];
+            unpack(q[i], type, g);
+            if (kSgd) unpack(w[i], type, x);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = kSgd ? fmaf(step, g[j], x[j]) : f * g[j];
+            const uint4 r = pack(g, type);
+            char* to = out + (v0 + i * kBlock) * 16;
+            if (e[i].lo == 0 && e[i].hi == per && even) *reinterpret_cast<uint4*>(to) = r;
+            else store_some(to, type, r, e[i].lo, e[i].hi);
+        }
+    }
+}
+
+int most_blocks() { return device_sm_count() * kBlocksPerSm; }
+
+// Tensors [from, to) of the call.
+template <int kMost>
+void fill(Tensors<kMost>& p, const TensorListArgs& a, int from, int to) {
+    p.count = 0;
+    p.items = 0;
+    for (int i = from; i < to; ++i) {
+        if (a.sizes[i] == 0) continue;
+        const int k = p.count++;
+        const size_t es = dtype_bytes(a.types[i]);
+        p.g[k] = a.grads[i];
+        p.out[k] = a.out ? a.out[i] : nullptr;
+        p.n[k] = a.sizes[i];
+        p.type[k] = (unsigned char)a.types[i];
+        p.lead[k] = (unsigned char)((reinterpret_cast<uintptr_t>(a.grads[i]) & 15) / es);
+        p.first[k] = p.items;
+        p.items += unsigned(((p.n[k] + p.lead[k]) * es + kItemBytes - 1) / kItemBytes);
+    }
+}
+
+template <int kMost>
+int launch_one(const TensorListArgs& a, int from, int to, bool apply, double* partial, int partials, int& blocks, cudaStream_t st) {
+    Tensors<kMost> p;
+    fill(p, a, from, to);
+    blocks = p.items < unsigned(most_blocks()) ? int(p.items) : most_blocks();
+    if (blocks == 0) {
+        if (!apply || from > 0) return PCL_OK;
+        blocks = 1;                                           // (the norm is written all the same)
+    }
+    if (!apply) return launch_chained(sum_squares_kernel<kMost>, dim3(blocks), dim3(kBlock), 0, st, 1, p, partial);
+    const ApplyParams ap{partial, partials, a.max_norm, a.lr, a.norm};
+    return a.sgd ? launch_chained(apply_kernel<kMost, true>, dim3(blocks), dim3(kBlock), 0, st, 1, p, ap)
+                 : launch_chained(apply_kernel<kMost, false>, dim3(blocks), dim3(kBlock), 0, st, 1, p, ap);
+}
+// (a short list is a short parameter block: what a launch costs grows with it)
+int launch_some(const TensorListArgs& a, int from, int to, bool apply, double* partial, int partials, int& blocks, cudaStream_t st) {
+    if (to - from <= 32) return launch_one<32>(a, from, to, apply, partial, partials, blocks, st);
+    if (to - from <= 128) return launch_one<128>(a, from, to, apply, partial, partials, blocks, st);
+    return launch_one<kMostTensors>(a, from, to, apply, partial, partials, blocks, st);
+}
+
+}  // namespace
+
+size_t grad_norm_workspace_bytes(int count) {
+    return align_up(size_t((count + kMostTensors - 1) / kMostTensors) * most_blocks() * sizeof(double), 256);
+}
+
+int launch_grad_norm(const TensorListArgs& a, void* ws, cudaStream_t st) {
+    double* partial = static_cast<double*>(ws);
+    double bytes = 0.0;
+    for (int i = 0; i < a.count; ++i) bytes += double(a.sizes[i]) * dtype_bytes(a.types[i]);
+    int partials = 0, blocks = 0;
+    for (int from = 0; from < a.count; from += kMostTensors) {
+        const int to = a.count - from < kMostTensors ? a.count : from + kMostTensors;
+        LaunchScope scope(KID_GRAD_NORM, bytes, st);
+        const int rc = launch_some(a, from, to, false, partial + partials, 0, blocks, st);
+        if (rc != PCL_OK) return rc;
+        partials += blocks;
+    }
+    if (!a.out) {
+        LaunchScope scope(KID_GRAD_NORM, 0.0, st);
+        return launch_chained(norm_kernel, dim3(1), dim3(kBlock), 0, st, 1, static_cast<const double*>(partial), partials, a.norm);
+    }
+    for (int from = 0; from < a.count; from += kMostTensors) {
+        const int to = a.count - from < kMostTensors ? a.count : from + kMostTensors;
+        LaunchScope scope(KID_GRAD_NORM, bytes * (a.sgd ? 3 : 2), st);
+        const int rc = launch_some(a, from, to, true, partial, partials, blocks, st);
+        if (rc != PCL_OK) return rc;
+    }
+    return PCL_OK;
+}
+
+}  // namespace pcl

@@ -3,6 +3,7 @@
 // the caller's stream.
 #include <atomic>
 #include <mutex>
+#include <float.h>
 #include <limits.h>
 #include <stdio.h>
 #include <string.h>
@@ -82,7 +83,8 @@ const char* const kKernelNames[KID_COUNT] = {
     "tc_fprop_kernel", "tc_wgrad_kernel", "generic_fwd", "generic_bwd_data", "generic_bwd_weights", "sgd_kernel",
     "reduce_splits_kernel", "zero_kernel", "transpose_flip_kernel", "act_grad_kernel", "colsum_kernel",
     "maxpool_fwd_kernel", "maxpool_bwd_kernel", "softmax_xent_kernel", "stage_pad_c4_kernel", "stage_w4_kernel",
-    "unpad_reduce_kernel", "tc_gemm16_kernel", "embedding_kernel", "vocab_loss_kernel", "orthogonalize_kernel"};
+    "unpad_reduce_kernel", "tc_gemm16_kernel", "embedding_kernel", "vocab_loss_kernel", "orthogonalize_kernel",
+    "rms_norm_kernel", "grad_norm_kernel", "sample_kernel"};
 
 cudaEvent_t prof_event() {
     if (g_prof_pool_used == g_prof_pool.size()) {
@@ -1249,6 +1251,119 @@ int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const voi
     OrthoArgs o{count, M, N, dtype, steps, dw, w};
     o.momentum = momentum; o.mu = mu; o.nesterov = nesterov; o.lr = lr; o.weight_decay = weight_decay;
     return launch_orthogonalize(o, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+namespace {
+int check_rows(int N, int C, int dtype) {
+    if (N <= 0 || C <= 0 || !known_dtype(dtype)) return PCL_ERR_BAD_ARG;
+    return fits_index(N, C) ? PCL_OK : PCL_ERR_UNSUPPORTED_SHAPE;
+}
+int rms_norm_fwd_impl(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps, void* h, void* y,
+                      float* scale, float* rstd, void* cuda_stream) {
+    const int rc = check_rows(N, C, dtype);
+    if (rc != PCL_OK) return rc;
+    if (!x || !w || !y || (h && !residual) || !(eps >= 0.f) || eps > FLT_MAX) return PCL_ERR_BAD_ARG;
+    if (!aligned16(x) || !aligned16(residual) || !aligned16(w) || !aligned16(h) || !aligned16(y) || !aligned16(scale) || !aligned16(rstd))
+        return PCL_ERR_MISALIGNED;
+    return launch_rms_norm_fwd(N, C, dtype, x, residual, w, eps, h, y, scale, rstd, static_cast<cudaStream_t>(cuda_stream));
+}
+}  // namespace
+
+int pcl_rms_norm_fwd(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps, void* h, void* y,
+                     float* rstd, void* cuda_stream) {
+    return rms_norm_fwd_impl(N, C, dtype, x, residual, w, eps, h, y, nullptr, rstd, cuda_stream);
+}
+
+int pcl_rms_norm_fwd_q8(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps, void* h, void* y8,
+                        float* y_scale, float* rstd, void* cuda_stream) {
+    if (N > 0 && C > 0 && !y_scale) return PCL_ERR_BAD_ARG;
+    return rms_norm_fwd_impl(N, C, dtype, x, residual, w, eps, h, y8, y_scale, rstd, cuda_stream);
+}
+
+size_t pcl_rms_norm_workspace_bytes(int N, int C) { return N <= 0 || C <= 0 || !fits_index(N, C) ? 0 : rms_norm_workspace_bytes(N, C); }
+
+int pcl_rms_norm_bwd(int N, int C, int dtype, const void* h, const void* w, const float* rstd, const void* dy, const void* dh,
+                     void* dx, void* dw, void* ws, size_t ws_bytes, void* cuda_stream) {
+    int rc = check_rows(N, C, dtype);
+    if (rc != PCL_OK) return rc;
+    if (!h || !w || !rstd || !dy || !dx) return PCL_ERR_BAD_ARG;
+    if (!aligned16(h) || !aligned16(w) || !aligned16(rstd) || !aligned16(dy) || !aligned16(dh) || !aligned16(dx) || !aligned16(dw))
+        return PCL_ERR_MISALIGNED;
+    if (dw) rc = check_ws(ws, ws_bytes, rms_norm_workspace_bytes(N, C));
+    if (rc != PCL_OK) return rc;
+    return launch_rms_norm_bwd(N, C, dtype, h, w, rstd, dy, dh, dx, dw, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int pcl_quantize_rows(int N, int C, int dtype, const void* x, void* q, float* scale, void* cuda_stream) {
+    const int rc = check_rows(N, C, dtype);
+    if (rc != PCL_OK) return rc;
+    if (!x || !q || !scale) return PCL_ERR_BAD_ARG;
+    if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return PCL_ERR_MISALIGNED;
+    return launch_quantize_rows(N, C, dtype, x, q, scale, static_cast<cudaStream_t>(cuda_stream));
+}
+
+namespace {
+// (a tensor's size is limited so that the pieces of all tensors of a launch can be counted in 32 bits)
+constexpr size_t kMostElements = size_t(1) << 34;
+int check_tensors(int count, const void* const* a, const void* const* b, bool two, const size_t* sizes, const int* dtypes, const float* norm,
+                  const void* ws, size_t ws_bytes) {
+    if (count <= 0 || !a || (two && !b) || !sizes || !dtypes || !norm) return PCL_ERR_BAD_ARG;
+    for (int i = 0; i < count; ++i) {
+        if (!known_dtype(dtypes[i])) return PCL_ERR_BAD_ARG;
+        if (sizes[i] == 0) continue;
+        if (sizes[i] > kMostElements) return PCL_ERR_UNSUPPORTED_SHAPE;
+        if (!a[i] || (two && !b[i])) return PCL_ERR_BAD_ARG;
+        const uintptr_t mask = dtype_bytes(dtypes[i]) - 1;
+        if ((reinterpret_cast<uintptr_t>(a[i]) & mask) || (two && (reinterpret_cast<uintptr_t>(b[i]) & mask))) return PCL_ERR_MISALIGNED;
+    }
+    if (reinterpret_cast<uintptr_t>(norm) & 3) return PCL_ERR_MISALIGNED;
+    return check_ws(ws, ws_bytes, grad_norm_workspace_bytes(count));
+}
+}  // namespace
+
+size_t pcl_grad_norm_workspace_bytes(int count) { return count <= 0 ? 0 : grad_norm_workspace_bytes(count); }
+
+int pcl_grad_norm(int count, const void* const* grads, const size_t* sizes, const int* dtypes, float* norm, void* ws, size_t ws_bytes,
+                  void* cuda_stream) {
+    const int rc = check_tensors(count, grads, nullptr, false, sizes, dtypes, norm, ws, ws_bytes);
+    if (rc != PCL_OK) return rc;
+    const TensorListArgs a{count, grads, nullptr, sizes, dtypes, false, 0.f, 0.f, norm};
+    return launch_grad_norm(a, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int pcl_grad_clip(int count, const void* const* grads, void* const* out, const size_t* sizes, const int* dtypes, float max_norm,
+                  float* norm, void* ws, size_t ws_bytes, void* cuda_stream) {
+    const int rc = check_tensors(count, grads, out, true, sizes, dtypes, norm, ws, ws_bytes);
+    if (rc != PCL_OK) return rc;
+    if (!(max_norm >= 0.f)) return PCL_ERR_BAD_ARG;
+    const TensorListArgs a{count, grads, out, sizes, dtypes, false, max_norm, 0.f, norm};
+    return launch_grad_norm(a, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+int pcl_sgd_update_clipped(int count, void* const* w, const void* const* grads, const size_t* sizes, const int* dtypes, float lr,
+                           float max_norm, float* norm, void* ws, size_t ws_bytes, void* cuda_stream) {
+    const int rc = check_tensors(count, grads, w, true, sizes, dtypes, norm, ws, ws_bytes);
+    if (rc != PCL_OK) return rc;
+    if (!(max_norm >= 0.f)) return PCL_ERR_BAD_ARG;
+    const TensorListArgs a{count, grads, w, sizes, dtypes, true, max_norm, lr, norm};
+    return launch_grad_norm(a, ws, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t pcl_sample_tokens_workspace_bytes(int N, int K) { return N <= 0 || K <= 0 || !fits_index(N, K) ? 0 : sample_tokens_workspace_bytes(N, K); }
+
+int pcl_sample_tokens(int N, int K, int dtype, const void* logits, const float* uniform, const float* temperature, const int* top_k,
+                      const float* top_p, const float* min_p, int* token, float* logprob, void* ws, size_t ws_bytes, void* cuda_stream) {
+    int rc = check_rows(N, K, dtype);
+    if (rc != PCL_OK) return rc;
+    if (!logits || !uniform || !token) return PCL_ERR_BAD_ARG;
+    if (!aligned16(logits) || !aligned16(uniform) || !aligned16(temperature) || !aligned16(top_k) || !aligned16(top_p) || !aligned16(min_p) ||
+        !aligned16(token) || !aligned16(logprob))
+        return PCL_ERR_MISALIGNED;
+    const size_t need = sample_tokens_workspace_bytes(N, K);
+    if (need) rc = check_ws(ws, ws_bytes, need);
+    if (rc != PCL_OK) return rc;
+    const SampleArgs a{N, K, dtype, logits, uniform, temperature, top_k, top_p, min_p, token, logprob};
+    return launch_sample_tokens(a, ws, static_cast<cudaStream_t>(cuda_stream));
 }
 
 static std::atomic<unsigned int> g_last_wait_code{0};

@@ -45,7 +45,8 @@ int launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cud
 enum KernelId {
     KID_TC_FPROP = 0, KID_TC_WGRAD, KID_GENERIC_FWD, KID_GENERIC_DGRAD, KID_GENERIC_WGRAD, KID_SGD, KID_REDUCE_SPLITS,
     KID_ZERO, KID_TRANSPOSE_FLIP, KID_ACT_GRAD, KID_COLSUM, KID_MAXPOOL_FWD, KID_MAXPOOL_BWD, KID_SOFTMAX_XENT,
-    KID_STAGE_PAD_C4, KID_STAGE_W4, KID_UNPAD_REDUCE, KID_TC_GEMM16, KID_EMBEDDING, KID_VOCAB_LOSS, KID_ORTHO, KID_COUNT
+    KID_STAGE_PAD_C4, KID_STAGE_W4, KID_UNPAD_REDUCE, KID_TC_GEMM16, KID_EMBEDDING, KID_VOCAB_LOSS, KID_ORTHO, KID_RMS_NORM, KID_GRAD_NORM,
+    KID_SAMPLE, KID_COUNT
 };
 
 // Brackets one kernel launch: counts it and, while profiling is switched on
@@ -391,6 +392,42 @@ int launch_orthogonalize(const OrthoArgs& a, void* ws, cudaStream_t st);
 bool orthogonalize_is_narrow(int count, int M, int N);
 size_t orthogonalize_narrow_workspace_bytes(int count, int M, int N);
 int launch_orthogonalize_narrow(const OrthoArgs& a, void* ws, cudaStream_t st);
+
+// ---- RMS norm (rms_norm.cu) -----------------------------------------------------
+size_t rms_norm_workspace_bytes(int N, int C);
+// scale: null, or the scales of y's rows, which are then e4m3 bytes
+int launch_rms_norm_fwd(int N, int C, int type, const void* x, const void* residual, const void* w, float eps, void* h, void* y,
+                        float* scale, float* rstd, cudaStream_t st);
+int launch_rms_norm_bwd(int N, int C, int type, const void* h, const void* w, const float* rstd, const void* dy, const void* dh,
+                        void* dx, void* dw, void* ws, cudaStream_t st);
+int launch_quantize_rows(int N, int C, int type, const void* x, void* q, float* scale, cudaStream_t st);
+
+// ---- norm and clipping of many tensors (grad_norm.cu) ---------------------------
+struct TensorListArgs {
+    int count;
+    const void* const* grads;
+    void* const* out;                   // null: the norm alone
+    const size_t* sizes;
+    const int* types;
+    bool sgd;                           // out are weights, w <- w - lr f g; else out = f g
+    float max_norm, lr;
+    float* norm;
+};
+size_t grad_norm_workspace_bytes(int count);
+int launch_grad_norm(const TensorListArgs& a, void* ws, cudaStream_t st);
+
+// ---- choice of tokens (sample_tokens.cu) ----------------------------------------
+struct SampleArgs {
+    int N, K, type;
+    const void* logits;
+    const float *uniform, *temperature;
+    const int* top_k;
+    const float *top_p, *min_p;
+    int* token;
+    float* logprob;
+};
+size_t sample_tokens_workspace_bytes(int N, int K);
+int launch_sample_tokens(const SampleArgs& a, void* ws, cudaStream_t st);
 
 inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
