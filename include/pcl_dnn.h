@@ -417,6 +417,16 @@ int pcl_rms_norm_bwd(int N, int C, int dtype, const void* h, const void* w, cons
  *   scale[n] = max(max_c |x[n,c]| / 448, 2^-126),   q[n,c] = e4m3(x[n,c] / scale[n])  */
 int pcl_quantize_rows(int N, int C, int dtype, const void* x, void* q, float* scale, void* cuda_stream);
 
+/* FC layer of 8-bit operands as the two calls above write them (forward only):
+ *   y[n,k] = act(x_scale[n] * w_scale[k] * sum_c x[n,c] * w[k,c] + bias[k])
+ * x: [N][C], w: [K][C], e4m3 bytes; x_scale: fp32 [N], w_scale: fp32 [K]; bias: [K] or NULL and y: [N][K] of type dtype; act: NONE,
+ * RELU or SIGMOID.  Products are exact, sums fp32 on the 8-bit tensor cores (whose additions truncate), the rest is fp32,
+ * rounded once.  C % 16 != 0: both operands are copied to padded rows in the workspace first.
+ * Workspace: pcl_fc_q8_workspace_bytes(N, C, K) (0 is possible), 256-byte aligned. */
+size_t pcl_fc_q8_workspace_bytes(int N, int C, int K);
+int pcl_fc_q8_fwd(int N, int C, int K, int dtype, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                  const void* bias, void* y, int act, void* ws, size_t ws_bytes, void* cuda_stream);
+
 /* Norm of `count` tensors as one vector, e.g. of the gradients of all parameters, and clipping by it:
  *   norm = sqrt(sum_i sum_j grads[i][j]^2),   f = min(1, max_norm / (norm + 1e-6))
  *   pcl_grad_clip:           out[i] = f * grads[i]           (out[i] may be grads[i])

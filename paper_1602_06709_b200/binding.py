@@ -39,6 +39,7 @@ EXPORTS = [
     "pcl_conv_bwd_weights_pooled_staged", "pcl_conv_bwd_weights_sgd", "pcl_conv_bwd_weights_sgd_workspace_bytes",
     "pcl_fc_bwd_fused_sgd", "pcl_fc_bwd_fused_sgd_workspace_bytes", "pcl_plan_cache_stats",
     "pcl_rms_norm_fwd", "pcl_rms_norm_fwd_q8", "pcl_rms_norm_workspace_bytes", "pcl_rms_norm_bwd", "pcl_quantize_rows",
+    "pcl_fc_q8_workspace_bytes", "pcl_fc_q8_fwd",
     "pcl_grad_norm_workspace_bytes", "pcl_grad_norm", "pcl_grad_clip", "pcl_sgd_update_clipped",
     "pcl_sample_tokens_workspace_bytes", "pcl_sample_tokens",
 ]
@@ -127,6 +128,9 @@ def lib() -> ctypes.CDLL:
         L.pcl_rms_norm_workspace_bytes.restype = sz
         L.pcl_rms_norm_bwd.argtypes = [ci, ci, ci, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.pcl_quantize_rows.argtypes = [ci, ci, ci, vp, vp, vp, vp]
+        L.pcl_fc_q8_workspace_bytes.argtypes = [ci, ci, ci]
+        L.pcl_fc_q8_workspace_bytes.restype = sz
+        L.pcl_fc_q8_fwd.argtypes = [ci, ci, ci, ci, vp, vp, vp, vp, vp, vp, ci, vp, sz, vp]
         L.pcl_grad_norm_workspace_bytes.argtypes = [ci]
         L.pcl_grad_norm_workspace_bytes.restype = sz
         L.pcl_grad_norm.argtypes = [ci, vp, vp, vp, vp, vp, sz, vp]
@@ -602,6 +606,19 @@ def quantize_rows(N, C, x, q, scale, stream=None):
     d, s = _typed("pcl_quantize_rows", (N, C), [(x, N * C)], [(scale, N)], stream=stream)
     _bytes8("pcl_quantize_rows", x, [(q, N * C)])
     _check(lib().pcl_quantize_rows(N, C, d, _addr(x), _addr(q), _addr(scale), s), "pcl_quantize_rows")
+
+
+def fc_q8_workspace_bytes(N, C, K) -> int:
+    return int(lib().pcl_fc_q8_workspace_bytes(*map(_size, (N, C, K))))
+
+
+def fc_q8_fwd(N, C, K, x, x_scale, w, w_scale, bias, y, act=ACT_NONE, ws=None, stream=None):
+    """y = act(x_scale[n] * w_scale[k] * (x w^T) + bias) of e4m3 operands (float8_e4m3fn or uint8 tensors)."""
+    d, s = _typed("pcl_fc_q8_fwd", (N, C, K), [(y, N * K), (bias, K)], [(x_scale, N), (w_scale, K)], stream=stream, ws=ws)
+    _bytes8("pcl_fc_q8_fwd", y, [(x, N * C), (w, K * C)])
+    wp, wb = _ws(ws)
+    _check(lib().pcl_fc_q8_fwd(N, C, K, d, _addr(x), _addr(x_scale), _addr(w), _addr(w_scale), _addr(bias), _addr(y), act, wp, wb, s),
+           "pcl_fc_q8_fwd")
 
 
 class TensorList:

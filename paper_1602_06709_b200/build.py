@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpcl_dnn.so")
 SOURCES = ["pcl_api.cu", "tc_fprop.cu", "tc_wgrad.cu", "generic_conv.cu", "elementwise.cu", "noalloc.cu",
            "tc_gemm16.cu", "embedding.cu", "vocab_loss.cu", "orthogonalize.cu", "orthogonalize_narrow.cu",
-           "rms_norm.cu", "grad_norm.cu", "sample_tokens.cu"]
+           "rms_norm.cu", "fc_q8.cu", "grad_norm.cu", "sample_tokens.cu"]
 HEADERS = ["pcl_internal.h", "pcl_ptx.cuh", "gemm16_device.cuh", os.path.join("..", "..", "include", "pcl_dnn.h")]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -65,10 +65,19 @@ struct Gemm16Params {
     unsigned* clear;
     const float* lse;
     const float* row_scale;
+    const float* col_scale; int act;
     unsigned int* status;
 };
 
 __device__ __forceinline__ float2 half2_value(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+// Elements i .. i + 3 of an fp32 vector of n (0 behind its end); i is a multiple of four, the vector 16-byte aligned.
+__device__ __forceinline__ float4 load_four32(const float* s, int i, int n) {
+    if (i + 4 <= n) return __ldg(reinterpret_cast<const float4*>(s + i));
+    float e[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) e[j] = i + j < n ? __ldg(s + i + j) : 0.f;
+    return make_float4(e[0], e[1], e[2], e[3]);
+}
 // Elements i .. i + 3 of a 16-bit vector of n (0 behind its end); i is a multiple of four, the vector 8-byte aligned.
 __device__ __forceinline__ uint2 load_four16(const void* base, int i, int n) {
     const uint16_t* s = static_cast<const uint16_t*>(base) + i;
@@ -374,10 +383,10 @@ __device__ __forceinline__ void drain_fetch(Gemm16Ctx& c) {
 }
 
 // ---- MMA issuer (of the leading CTA).  false: a wait ran out.
-template <bool kPair, bool kAMn, bool kBMn, bool kLong>
+template <bool kPair, bool kAMn, bool kBMn, bool kLong, bool kE4m3 = false>
 __device__ __forceinline__ bool issue_items(Gemm16Ctx& c, const Gemm16Params& p) {
     constexpr int kTileM = kPair ? 256 : 128, kBN = kTileM;
-    const uint32_t idesc0 = make_idesc_f16(0, p.bf16 != 0, kAMn, kBMn, kTileM);
+    const uint32_t idesc0 = make_idesc_f16(0, !kE4m3 && p.bf16 != 0, kAMn, kBMn, kTileM);
     // K-major: 8-row groups 1 KB apart.  MN-major: 64-row groups 8 KB apart, 8-deep reduction groups 1 KB apart.
     const uint64_t da = make_smem_desc(c.ring, kAMn ? 8192 : 0, 1024, kSwizzle128B);
     const uint64_t db = make_smem_desc(c.ring + 16384, kBMn ? 8192 : 0, 1024, kSwizzle128B);
@@ -399,10 +408,10 @@ __device__ __forceinline__ bool issue_items(Gemm16Ctx& c, const Gemm16Params& p)
                 tc_fence_after();
                 const uint32_t off = uint32_t(c.stage) * (kSlotBytes / 16);
                 if (kb + 1 < p.k_blocks || p.last_slices == 4)
-                    umma_kstep_f16<kPair, kAMn ? 128 : 2, kBMn ? 128 : 2>(d, a_lo0 + off, b_lo0 + off, a_hi, b_hi, idesc, accum);
+                    umma_kstep_f16<kPair, kAMn ? 128 : 2, kBMn ? 128 : 2, kE4m3>(d, a_lo0 + off, b_lo0 + off, a_hi, b_hi, idesc, accum);
                 else                     // a short last block: only the K = 16 slices that hold anything
                     for (int s = 0; s < p.last_slices; ++s)
-                        umma_f16<kPair>(d, (uint64_t(a_hi) << 32) | (a_lo0 + off + s * (kAMn ? 128 : 2)),
+                        umma_f16<kPair, kE4m3>(d, (uint64_t(a_hi) << 32) | (a_lo0 + off + s * (kAMn ? 128 : 2)),
                                         (uint64_t(b_hi) << 32) | (b_lo0 + off + s * (kBMn ? 128 : 2)), idesc, accum | (s > 0));
                 accum = 1;
                 umma_commit_addr<kPair>(empty0 + 8 * c.stage);
@@ -431,8 +440,9 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
     const uint32_t ae0 = smem_u32(&c.sh->acc_empty_bar[0]);
     const uint32_t ae_dst0 = kPair ? map_to_cta(&c.sh->acc_empty_bar[0], 0) : ae0;
     constexpr bool kClasses = kEpi == GEMM16_STATS || kEpi == GEMM16_DZ;
+    constexpr bool kScaled = kEpi == GEMM16_Q8 || kEpi == GEMM16_Q8_STORE;
     constexpr bool kJoins = kEpi != GEMM16_STATS && kEpi != GEMM16_PARTS;           // parts are joined by whichever comes last
-    const float alpha = kClasses ? 1.f : p.alpha * (p.alpha_dev ? __ldg(p.alpha_dev) : 1.f);
+    const float alpha = kClasses || kScaled ? 1.f : p.alpha * (p.alpha_dev ? __ldg(p.alpha_dev) : 1.f);
     const uint32_t warp_slot = kPair ? c.pair_rank * 8 + (warp - 2) : warp - 2;      // of a tile's epilogue warps
     constexpr uint32_t kWarpSlots = kPair ? 16 : 8;
     constexpr int kChunks = kHalf / 32;
@@ -461,6 +471,23 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             if (row_ok) label = max(p.labels[row], -1) - p.col0;
             if constexpr (kEpi == GEMM16_DZ) {
                 if (row_ok) { lse = p.lse[row]; g = lse == -INFINITY ? 0.f : p.row_scale[row]; }     // (no finite logit: no gradient)
+            }
+        }
+        // Q8: the scales and the bias of the warp's columns, four per lane, and its row's scale
+        float4 col_scale = make_float4(0.f, 0.f, 0.f, 0.f), shift = col_scale;
+        if constexpr (kScaled) {
+            const int at = cbase + 4 * (lane & (kHalf / 4 - 1));
+            if (row_ok) g = __ldg(p.row_scale + row);
+            col_scale = load_four32(p.col_scale, at, p.N);
+            if (p.bias) {
+                if (p.out_type == DT_F32) {
+                    shift = load_four32(static_cast<const float*>(p.bias), at, p.N);
+                } else {
+                    const uint2 b = load_four16(p.bias, at, p.N);
+                    const float2 lo = half2_value(b.x), hi = half2_value(b.y);
+                    shift = p.bf16 ? make_float4(__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xffff0000u))
+                                   : make_float4(lo.x, lo.y, hi.x, hi.y);
+                }
             }
         }
         if constexpr (kEpi == GEMM16_GENERAL || kEpi == GEMM16_FINAL) {
@@ -507,6 +534,27 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                         v[2 * j] += p.bf16 ? __uint_as_float(two << 16) : h.x;
                         v[2 * j + 1] += p.bf16 ? __uint_as_float(two & 0xffff0000u) : h.y;
                     }
+                }
+            }
+            if constexpr (kScaled) {
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float cs = j % 4 == 0 ? col_scale.x : j % 4 == 1 ? col_scale.y : j % 4 == 2 ? col_scale.z : col_scale.w;
+                    v[j] = v[j] * g * __shfl_sync(0xffffffffu, cs, cc / 4 + j / 4);
+                }
+                if (p.bias) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) {
+                        const float b = j % 4 == 0 ? shift.x : j % 4 == 1 ? shift.y : j % 4 == 2 ? shift.z : shift.w;
+                        v[j] += __shfl_sync(0xffffffffu, b, cc / 4 + j / 4);
+                    }
+                }
+                if (p.act == PCL_ACT_RELU) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];        // (NaN stays)
+                } else if (p.act == PCL_ACT_SIGMOID) {
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) v[j] = sigmoid_fast(v[j]);
                 }
             }
             if constexpr (kEpi == GEMM16_STATS) {
@@ -607,7 +655,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                         bulk_commit_group();
                     }
                 }
-            } else if constexpr (kEpi == GEMM16_GENERAL || kEpi == GEMM16_FINAL) {
+            } else if constexpr (kEpi == GEMM16_GENERAL || kEpi == GEMM16_FINAL || kEpi == GEMM16_Q8) {
                 // any type and alignment: the chunk is transposed through the staging tile, then all lanes take one row
 #pragma unroll
                 for (uint32_t j = 0; j < 8; ++j)
@@ -663,7 +711,7 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                     if (g == 0.f)                                                 // rows left out or without a finite logit: exactly 0, whatever z is
 #pragma unroll
                         for (int j = 0; j < 32; ++j) v[j] = 0.f;
-                } else {
+                } else if constexpr (!kScaled) {
 #pragma unroll
                     for (int j = 0; j < 32; ++j) v[j] *= alpha;
                 }
@@ -856,7 +904,7 @@ inline Plan16 plan16(const Gemm16Args& a) {
             Costs c{most(mma, copy * active), most(mma, copy * active * (1.0 + fm) / 2), most(mma * most(fn, 0.5), copy * active * (1.0 + fn) / 2)};
             // STATS (without the spilling sums of kLong) of one row of tiles: B comes from memory, once, to pairs at 4.8 TB/s and to
             // single CTAs at 4.0 (2 rows, 2816 -> 105536: 125 and 147 us)
-            if (mt == 1 && a.epi == GEMM16_STATS && (a.bf16 || kb <= 2 * kRunBlocks)) { const double feed = active * (pair ? 32768.0 / 4.8e6 : 16384.0 / 4.0e6); c.core = most(c.core, feed); c.bottom = most(c.bottom, feed); }
+            if (mt == 1 && (a.epi == GEMM16_Q8 || (a.epi == GEMM16_STATS && (a.bf16 || kb <= 2 * kRunBlocks)))) { const double feed = active * (pair ? 32768.0 / 4.8e6 : 16384.0 / 4.0e6); c.core = most(c.core, feed); c.bottom = most(c.bottom, feed); }
             return c;
         };
         const Costs full = block(slots);
@@ -917,7 +965,7 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
     };
     p.quads = a.N % 4 == 0 && four(a.src, a.src_type, a.src_ld, a.src_batch) && four(a.out, a.out_type, a.out_ld, a.out_batch);
     p.bias = a.bias; p.labels = a.labels; p.col0 = a.col0; p.part = a.part; p.part_ld = a.part_ld; p.label_z = a.label_z; p.clear = a.clear;
-    p.lse = a.lse; p.row_scale = a.row_scale;
+    p.lse = a.lse; p.row_scale = a.row_scale; p.col_scale = a.col_scale; p.act = a.act;
     p.status = device_status_ptr();
     if (!p.status) return PCL_ERR_CUDA;
     return PCL_OK;

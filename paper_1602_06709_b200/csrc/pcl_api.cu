@@ -84,7 +84,7 @@ const char* const kKernelNames[KID_COUNT] = {
     "reduce_splits_kernel", "zero_kernel", "transpose_flip_kernel", "act_grad_kernel", "colsum_kernel",
     "maxpool_fwd_kernel", "maxpool_bwd_kernel", "softmax_xent_kernel", "stage_pad_c4_kernel", "stage_w4_kernel",
     "unpad_reduce_kernel", "tc_gemm16_kernel", "embedding_kernel", "vocab_loss_kernel", "orthogonalize_kernel",
-    "rms_norm_kernel", "grad_norm_kernel", "sample_kernel"};
+    "rms_norm_kernel", "grad_norm_kernel", "sample_kernel", "pad_rows8_kernel"};
 
 cudaEvent_t prof_event() {
     if (g_prof_pool_used == g_prof_pool.size()) {
@@ -1300,6 +1300,24 @@ int pcl_quantize_rows(int N, int C, int dtype, const void* x, void* q, float* sc
     if (!x || !q || !scale) return PCL_ERR_BAD_ARG;
     if (!aligned16(x) || !aligned16(q) || !aligned16(scale)) return PCL_ERR_MISALIGNED;
     return launch_quantize_rows(N, C, dtype, x, q, scale, static_cast<cudaStream_t>(cuda_stream));
+}
+
+size_t pcl_fc_q8_workspace_bytes(int N, int C, int K) {
+    return N <= 0 || C <= 0 || K <= 0 || !fits_index(N, C, K) ? 0 : fc_q8_workspace_bytes(N, C, K);
+}
+
+int pcl_fc_q8_fwd(int N, int C, int K, int dtype, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                  const void* bias, void* y, int act, void* ws, size_t ws_bytes, void* cuda_stream) {
+    if (N <= 0 || C <= 0 || K <= 0 || !known_dtype(dtype) || !known_act(act) || !x || !x_scale || !w || !w_scale || !y) return PCL_ERR_BAD_ARG;
+    if (!fits_index(N, C, K)) return PCL_ERR_UNSUPPORTED_SHAPE;
+    if (g_path.load() == PCL_PATH_GENERIC) return PCL_ERR_UNSUPPORTED_SHAPE;       // (tensor-core kernels only)
+    if (!aligned16(x) || !aligned16(x_scale) || !aligned16(w) || !aligned16(w_scale) || !aligned16(bias) || !aligned16(y)) return PCL_ERR_MISALIGNED;
+    const size_t need = fc_q8_workspace_bytes(N, C, K);
+    if (need) {
+        const int rc = check_ws(ws, ws_bytes, need);
+        if (rc != PCL_OK) return rc;
+    }
+    return launch_fc_q8(N, C, K, dtype, x, x_scale, w, w_scale, bias, y, act, ws, static_cast<cudaStream_t>(cuda_stream));
 }
 
 namespace {

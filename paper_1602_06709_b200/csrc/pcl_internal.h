@@ -46,7 +46,7 @@ enum KernelId {
     KID_TC_FPROP = 0, KID_TC_WGRAD, KID_GENERIC_FWD, KID_GENERIC_DGRAD, KID_GENERIC_WGRAD, KID_SGD, KID_REDUCE_SPLITS,
     KID_ZERO, KID_TRANSPOSE_FLIP, KID_ACT_GRAD, KID_COLSUM, KID_MAXPOOL_FWD, KID_MAXPOOL_BWD, KID_SOFTMAX_XENT,
     KID_STAGE_PAD_C4, KID_STAGE_W4, KID_UNPAD_REDUCE, KID_TC_GEMM16, KID_EMBEDDING, KID_VOCAB_LOSS, KID_ORTHO, KID_RMS_NORM, KID_GRAD_NORM,
-    KID_SAMPLE, KID_COUNT
+    KID_SAMPLE, KID_PAD_ROWS8, KID_COUNT
 };
 
 // Brackets one kernel launch: counts it and, while profiling is switched on
@@ -318,6 +318,9 @@ enum Gemm16Epi {
     GEMM16_STORE,           // (what GENERAL becomes where out can be stored through TMA as it is)
     GEMM16_PARTS,           // the reduction in k_parts parts, each part's fp32 sums to out + part * out_batch (batch = 1)
     GEMM16_STATS, GEMM16_DZ,// softmax over classes, see below
+    GEMM16_Q8,              // operands e4m3, two to an element (K, ld and strides in elements of 16 bits), K-major: out = act(row_scale[r] *
+                            // col_scale[c] * acc + bias[c]); bias and out of type out_type (bf16: whether that is bf16), any alignment
+    GEMM16_Q8_STORE,        // (what Q8 becomes where out can be stored through TMA)
     // the orthogonalised update's, in its own kernel:
     GEMM16_SYM,             // out = alpha * acc + beta * src in fp16, where the result is symmetric: the tiles below the diagonal
                             // may be stored as mirror images instead of being computed
@@ -349,6 +352,7 @@ struct Gemm16Args {
     // DZ: out[r][c] = row_scale[r] * (exp(z - lse[r]) - [col0 + c == label]), 0 where row_scale[r] == 0 or lse[r] == -inf
     const float* lse = nullptr;
     const float* row_scale = nullptr;
+    const float* col_scale = nullptr; int act = 0;       // Q8
     // Scratch of gemm16_split_ws_bytes(), 256-byte aligned, or null (then nothing is split).
     void* split_ws = nullptr;
     int most_blocks = 0;                     // 64-element blocks that one accumulator may sum (0: any number); the parts of longer reductions are split
@@ -415,6 +419,11 @@ struct TensorListArgs {
 };
 size_t grad_norm_workspace_bytes(int count);
 int launch_grad_norm(const TensorListArgs& a, void* ws, cudaStream_t st);
+
+// ---- FC layer with 8-bit operands (fc_q8.cu) -------------------------------------
+size_t fc_q8_workspace_bytes(int N, int C, int K);
+int launch_fc_q8(int N, int C, int K, int out_type, const void* x, const float* x_scale, const void* w, const float* w_scale,
+                 const void* bias, void* y, int act, void* ws, cudaStream_t st);
 
 // ---- choice of tokens (sample_tokens.cu) ----------------------------------------
 struct SampleArgs {

@@ -1,5 +1,5 @@
 // 16-bit GEMM on tcgen05 (kind::f16: bf16 or fp16 operands, fp32 accumulators in TMEM), the contraction behind the
-// vocabulary loss and the orthogonalised update:  acc[r][c] = sum_k A(r, k) * B(c, k), either operand K-major or MN-major.
+// vocabulary loss and the orthogonalised update, and, with e4m3 operands (kind::f8f6f4), behind the 8-bit FC layer:  acc[r][c] = sum_k A(r, k) * B(c, k), either operand K-major or MN-major.
 //
 // Persistent, warp-specialised: warp 0 TMA producer, warp 1 MMA issuer, warps 2-9 epilogue (two per TMEM lane quarter).
 // Two accumulator sets: the epilogue of a tile overlaps the main loop of the next one.  A slot of the ring is one
@@ -21,6 +21,9 @@
 // reductions stay in one run: their log-sum-exp is 2e-4 off at C = 4096 and 1.6e-3 at 16384 where all products have the same sign
 // (z = 28), and 1e-5 and 4e-5 where they do not.  So do those of the DZ epilogue: fp16, C = 4096, dx is 1.7e-3 off where all
 // products have the same sign, 2.4e-4 (the roundings') where they do not.
+//
+// e4m3 operands (Q8) go through the same ring two to a 16-bit element: a block is 128 of them, a slice of a block one K = 32 MMA of the same
+// 32 bytes, and an MMA takes as long as one of 16-bit operands for twice the products.
 //
 // Every kernel starts before the one in front of it has ended (programmatic dependent launch): barriers, TMEM and tensor maps
 // are set up meanwhile, and griddepcontrol.wait stands before the first access to global memory.
@@ -46,7 +49,7 @@ tc_gemm16_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     if (c.warp == 0) {
         if (!produce_items<kPair, kAMn, kBMn>(c, p, tile, &tm_a, &tm_b)) drain_producer(c);
     } else if (c.warp == 1) {
-        if (c.pair_rank == 0) issue_items<kPair, kAMn, kBMn, kLong>(c, p);
+        if (c.pair_rank == 0) issue_items<kPair, kAMn, kBMn, kLong, kEpi == GEMM16_Q8 || kEpi == GEMM16_Q8_STORE>(c, p);
         __syncwarp();
     } else {
         finish_items<kPair, kEpi, kLong>(c, p, &tm_out, nullptr, p.src, p.out);
@@ -83,6 +86,8 @@ int launch_form(const Gemm16Args& a, int epi, const Maps16& m, const Gemm16Param
             return p.k_blocks > 2 * kRunBlocks && !p.bf16 ? launch_variant<kPair, false, false, GEMM16_STATS, true>(m, p, st)
                                                           : launch_variant<kPair, false, false, GEMM16_STATS>(m, p, st);
         case GEMM16_DZ * 4: return launch_variant<kPair, false, false, GEMM16_DZ>(m, p, st);
+        case GEMM16_Q8 * 4: return launch_variant<kPair, false, false, GEMM16_Q8>(m, p, st);
+        case GEMM16_Q8_STORE * 4: return launch_variant<kPair, false, false, GEMM16_Q8_STORE>(m, p, st);
         case GEMM16_STORE * 4 + 1: return launch_variant<kPair, false, true, GEMM16_STORE>(m, p, st);
         case GEMM16_STORE * 4 + 3: return launch_variant<kPair, true, true, GEMM16_STORE>(m, p, st);
         case GEMM16_GENERAL * 4 + 1: return launch_variant<kPair, false, true, GEMM16_GENERAL>(m, p, st);
@@ -145,6 +150,10 @@ int launch_gemm16(const Gemm16Args& a, cudaStream_t st) {
             if (a.update || (a.src && a.src_type != DT_F32)) return PCL_ERR_BAD_ARG;
             if (!a.src && a.out_type == t16 && every(a.out, t16, a.out_ld, a.out_batch)) epi = GEMM16_STORE;
             break;
+        case GEMM16_Q8:
+            if (!a.out || !a.row_scale || !a.col_scale || a.a.mn_major || a.b.mn_major || a.src) return PCL_ERR_BAD_ARG;
+            if (a.out_type == t16 && every(a.out, t16, a.out_ld, a.out_batch)) epi = GEMM16_Q8_STORE;
+            break;
         default: return PCL_ERR_BAD_ARG;
     }
     const Plan16 pl = plan16(a);
@@ -157,10 +166,10 @@ int launch_gemm16(const Gemm16Args& a, cudaStream_t st) {
     if (rc == PCL_OK) rc = operand_tmap(&m.b, a.b, a.N, a.K, a.batch, a.bf16);
     if (rc != PCL_OK) return rc;
     m.out = m.a;
-    if (epi == GEMM16_STORE || epi == GEMM16_DZ) rc = make_tmap16(&m.out, a.out, t16, a.N, a.M, a.batch, a.out_ld, a.out_batch, 64, 32);
+    if (epi == GEMM16_STORE || epi == GEMM16_DZ || epi == GEMM16_Q8_STORE) rc = make_tmap16(&m.out, a.out, t16, a.N, a.M, a.batch, a.out_ld, a.out_batch, 64, 32);
     if (epi == GEMM16_PARTS) rc = make_tmap16(&m.out, a.out, DT_F32, a.N, a.M, pl.splits, a.out_ld, a.out_batch, 32, 32);
     if (rc != PCL_OK) return rc;
-    LaunchScope scope(KID_TC_GEMM16, 2.0 * a.M * double(a.N) * a.K * a.batch , st);
+    LaunchScope scope(KID_TC_GEMM16, (a.epi == GEMM16_Q8 ? 4.0 : 2.0) * a.M * double(a.N) * a.K * a.batch, st);
     return pl.pair ? launch_form<true>(a, epi, m, p, st) : launch_form<false>(a, epi, m, p, st);
 }
 

@@ -55,6 +55,27 @@ def test_rms_norm_refusals(B):
         assert q(**bad) == B.ERR_MISALIGNED, bad
 
 
+def test_fc_q8_refusals(B):
+    L = B.lib()
+    need = B.fc_q8_workspace_bytes(4, 17, 8)
+    assert need > 0 and B.fc_q8_workspace_bytes(4, 0, 8) == 0 and B.fc_q8_workspace_bytes(4, 16, 2 ** 31 - 1) == 0
+
+    def call(N=4, C=17, K=8, d=1, x=OK16, xs=OK16, w=OK16, s=OK16, b=NULL, y=OK16, act=0, ws=OK16, wb=need):
+        return L.pcl_fc_q8_fwd(N, C, K, d, x, xs, w, s, b, y, act, ws, wb, NULL)
+
+    for bad in (dict(N=0), dict(C=0), dict(K=-1), dict(d=3), dict(act=3), dict(act=-1), dict(x=NULL), dict(xs=NULL), dict(w=NULL), dict(s=NULL), dict(y=NULL)):
+        assert call(**bad) == B.ERR_BAD_ARG, bad
+    for bad in (dict(x=ODD), dict(xs=ODD), dict(w=ODD), dict(s=ODD), dict(b=ODD), dict(y=ODD), dict(ws=P(4096 + 16))):
+        assert call(**bad) == B.ERR_MISALIGNED, bad
+    assert call(ws=NULL) == B.ERR_WORKSPACE and call(wb=need - 1) == B.ERR_WORKSPACE
+    assert call(K=2 ** 31 - 1) == B.ERR_UNSUPPORTED_SHAPE
+    B.set_path(B.PATH_GENERIC)
+    try:
+        assert call() == B.ERR_UNSUPPORTED_SHAPE
+    finally:
+        B.set_path(B.PATH_AUTO)
+
+
 def test_grad_norm_refusals(B):
     L = B.lib()
     need = B.grad_norm_workspace_bytes(2)
