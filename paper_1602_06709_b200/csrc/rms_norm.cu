@@ -3,19 +3,22 @@
 //   h = x + residual,  y[c] = h[c] * r * w[c],  r = 1 / sqrt(mean(h^2) + eps)
 //   dx = dh + r * (g - n * mean(g n)),  dw[c] = sum over the rows of dy[c] n[c],      g = dy w,  n = h r
 //
-// All of it is bound by memory.  A row is read once and stays in the registers of a group of threads: a group of 32 to 1024
-// threads takes a row, in chunks of 16 bytes, up to kMaxChunks a thread; a block holds several groups, each group walks over rows, and
-// the weights of its chunks stay in registers.  Chunks are counted in the flat tensor, not in the row, so that they are
-// aligned whatever the row length: a row of odd length starts and ends inside a chunk, and those two are read and written
-// element by element.  The distance between a group's rows is a multiple of a chunk's elements, so all of its rows start
-// at the same place of a chunk and the weights (and the sums of dw) in its registers keep their columns.
-// Rows too long for that (more than 32768 16-bit or 16384 fp32 elements; gradient: half of it) are walked over twice.
+// All of it is bound by memory: a row is read once, its values stay in the registers of a group of 32 to 512 threads (up to 32 each) until
+// its sum is known, or, in the gradient, in shared memory.
+//   Many rows: persistent blocks of several groups.  One warp copies sets of consecutive rows into a ring in shared memory (cp.async.bulk), so
+//   that what is in flight does not depend on registers; weights, and the sums of dw, stay in registers.
+//   Few rows (at most kFewRows per SM): a block takes a row, straight to registers, in one step.
+//   Rows of more than 16384 elements are walked over twice.
+// Threads take chunks of 16 bytes that are counted in the flat tensor, not in the row, and so are aligned whatever the row length: a row
+// of odd length starts and ends inside a chunk, and those two are written element by element.  The distance between a group's rows is a
+// multiple of a chunk's elements, so that all of them start at the same place of a chunk and registers keep their columns.
 //
 // Sums over a row are fp32 in a fixed tree.  h is rounded when it is stored, but the norm is that of the sum before rounding.  A row whose
 // sum of squares leaves fp32's range is scaled by a power of two first.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
+#include <limits.h>
 #include <math.h>
 
 #include "pcl_internal.h"
@@ -57,34 +60,34 @@ __device__ __forceinline__ Chunk<T> load_chunk(const T* p) {
     *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(p);
     return c;
 }
-// Which elements of a chunk belong to the row: [lo, hi).
+// Which elements of a chunk belong to the row: [lo, hi).  kWhole: all of them or none (rows are multiples of chunks).
 struct Span { int lo, hi; };
-template <class T>
+template <class T, bool kWhole = false>
 __device__ __forceinline__ Chunk<T> load_span(const T* p, Span s) {
     constexpr int E = Chunk<T>::E;
-    if (s.lo == 0 && s.hi == E) return load_chunk(p);
+    if (kWhole || (s.lo == 0 && s.hi == E)) return load_chunk(p);
     Chunk<T> c;
 #pragma unroll
     for (int i = 0; i < E; ++i) c.e[i] = i >= s.lo && i < s.hi ? p[i] : Elem<T>::put(0.f);
     return c;
 }
 // The weights of a chunk that starts at column c (aligned only where rows start on chunks).
-template <class T>
+template <class T, bool kWhole>
 __device__ __forceinline__ Chunk<T> load_weights(const T* w, int c, Span s, int shift) {
     constexpr int E = Chunk<T>::E;
-    if (shift == 0) return load_span(w + c, s);
+    if (kWhole || shift == 0) return load_span<T, kWhole>(w + c, s);
     Chunk<T> v;
 #pragma unroll
     for (int i = 0; i < E; ++i) v.e[i] = i >= s.lo && i < s.hi ? w[c + i] : Elem<T>::put(0.f);
     return v;
 }
-template <class T>
+template <class T, bool kWhole = false>
 __device__ __forceinline__ void store_span(T* p, Span s, const float (&v)[Chunk<T>::E]) {
     constexpr int E = Chunk<T>::E;
     Chunk<T> c;
 #pragma unroll
     for (int i = 0; i < E; ++i) c.e[i] = Elem<T>::put(v[i]);
-    if (s.lo == 0 && s.hi == E) {
+    if (kWhole || (s.lo == 0 && s.hi == E)) {
         *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&c);
     } else {
 #pragma unroll
@@ -93,7 +96,7 @@ __device__ __forceinline__ void store_span(T* p, Span s, const float (&v)[Chunk<
     }
 }
 // E values as e4m3 bytes.
-template <int E>
+template <int E, bool kWhole = false>
 __device__ __forceinline__ void store_span_q8(uint8_t* p, Span s, const float (&v)[E]) {
     uint32_t q[E / 4];
 #pragma unroll
@@ -102,7 +105,7 @@ __device__ __forceinline__ void store_span_q8(uint8_t* p, Span s, const float (&
         const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
         q[i] = lo | hi << 16;
     }
-    if (s.lo == 0 && s.hi == E) {
+    if (kWhole || (s.lo == 0 && s.hi == E)) {
         if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
         else *reinterpret_cast<uint32_t*>(p) = q[0];
     } else {
@@ -145,10 +148,12 @@ struct Group {
     }
 };
 
+constexpr int kPipeMost = 512;               // threads of a group, at most
+
 enum RowMode { ROW_NORM = 0, ROW_NORM_Q8, ROW_QUANTIZE };
 
 struct RowParams {
-    int N, C, group;             // group: threads that share a row
+    int N, C;
     float eps;
     const void *x, *residual, *w;
     void *h, *y;
@@ -167,52 +172,17 @@ __device__ __forceinline__ float row_rescale(uint32_t top, float eps) {
 }
 __device__ __forceinline__ bool out_of_range(float ss, float eps) { return !(ss < 1e38f) || (ss < 1e-24f && eps < 1e-20f); }
 
-template <class T, int V, RowMode kMode>
-__global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
+// The norm of a row whose values are in v (h in fp32): its factor r, the scale of v where the row had to be scaled first, and, of the 8-bit
+// forms, the scale of y.
+template <class T, int V, RowMode kMode, class Live>
+__device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int row, bool store, float (&v)[V][Chunk<T>::E], const Chunk<T> (&weight)[V],
+                                            const Live& live, float& r, float& inv) {
     constexpr int E = Chunk<T>::E;
-    __shared__ float2 words[64];
-    Group g{p.group, int(threadIdx.x) % p.group, int(threadIdx.x) / p.group, words};
-    const int groups = blockDim.x / p.group, total = groups * gridDim.x;
-    int row = blockIdx.x * groups + g.index;
-    const T* x = static_cast<const T*>(p.x);
-    const T* res = static_cast<const T*>(p.residual);
-    const T* w = static_cast<const T*>(p.w);
-    const int shift = int((size_t(row) * p.C) % E);           // (of all of this group's rows)
-    Span span[V];
-    Chunk<T> weight[V];
-    grid_dependency_wait();
-    grid_dependents_launch();
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const int c = (g.rank + i * p.group) * E - shift;     // the chunk's first column
-        span[i] = {c < 0 ? -c : 0, p.C - c < E ? (p.C - c > 0 ? p.C - c : 0) : E};
-        if (kMode != ROW_QUANTIZE && row < p.N && span[i].hi > span[i].lo) weight[i] = load_weights(w, c, span[i], shift);
-    }
-    const float mean = 1.f / float(p.C);
-    for (; row < p.N; row += total) {
-        const size_t at = size_t(row) * p.C - shift;
-        float v[V][E];
-        float ss = 0.f;
-        uint32_t top = 0;
-        Chunk<T> a[V], b[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (span[i].hi > span[i].lo) {
-                const size_t o = at + size_t(g.rank + i * p.group) * E;
-                a[i] = load_span(x + o, span[i]);
-                if (kMode != ROW_QUANTIZE && res) b[i] = load_span(res + o, span[i]);
-            }
+    auto measure = [&](float& ss, uint32_t& top) {
+        ss = 0.f; top = 0;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (span[i].hi <= span[i].lo) continue;
-            a[i].values(v[i]);
-            if (kMode != ROW_QUANTIZE && res) {
-                float r[E];
-                b[i].values(r);
-#pragma unroll
-                for (int j = 0; j < E; ++j) v[i][j] += r[j];
-                if (p.h) store_span(static_cast<T*>(p.h) + at + size_t(g.rank + i * p.group) * E, span[i], v[i]);
-            }
+            if (!live(i)) continue;
             float wf[E];
             if (kMode == ROW_NORM_Q8) weight[i].values(wf);
 #pragma unroll
@@ -223,60 +193,250 @@ __global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
             }
         }
         g.sum_and_max(ss, top);
-        float r = 1.f;
-        if (kMode != ROW_QUANTIZE) {
-            if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && top >= 0x7f800000u)) {
-                // (rare; every thread of the group takes it)
-                uint32_t big = 0;
-                float none = 0.f;
+    };
+    const float mean = 1.f / float(p.C);
+    float ss;
+    uint32_t top;
+    measure(ss, top);
+    r = 1.f;
+    if (kMode != ROW_QUANTIZE) {
+        float s = 1.f;
+        if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && top >= 0x7f800000u)) {       // (rare; every thread of the group takes it)
+            uint32_t big = 0;
+            float none = 0.f;
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if (live(i))
+#pragma unroll
+                    for (int j = 0; j < E; ++j) big = max(big, magnitude(v[i][j]));
+            g.sum_and_max(none, big);
+            s = row_rescale(big, p.eps);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[i][j] *= s;
+            measure(ss, top);
+        }
+        r = __frsqrt_rn(fmaf(ss, mean, (p.eps * s) * s));
+        if (store && g.rank == 0 && p.rstd) p.rstd[row] = r * s;
+    }
+    inv = 1.f;
+    if (kMode != ROW_NORM) {
+        const float most = __uint_as_float(top) * r / kLargestE4m3;
+        const float scale = most < kLeastScale ? kLeastScale : most;
+        if (store && g.rank == 0) p.scale[row] = scale;
+        inv = 1.f / scale;
+    }
+}
+template <class T, RowMode kMode, bool kWhole>
+__device__ __forceinline__ void row_store(const RowParams& p, size_t o, Span s, float (&v)[Chunk<T>::E], const Chunk<T>& weight, float r, float inv) {
+    constexpr int E = Chunk<T>::E;
+    float wf[E];
+    if (kMode != ROW_QUANTIZE) weight.values(wf);
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        if (kMode != ROW_QUANTIZE) v[j] = v[j] * r * wf[j];
+        if (kMode != ROW_NORM) v[j] *= inv;
+    }
+    if (kMode == ROW_NORM) store_span<T, kWhole>(static_cast<T*>(p.y) + o, s, v);
+    else store_span_q8<E, kWhole>(static_cast<uint8_t*>(p.y) + o, s, v);
+}
+
+// The chunks of a thread: V of a row, `group` apart.
+template <class T>
+struct Chunks {
+    int C, group, rank, shift;               // shift: elements of the first chunk in front of the row
+    __device__ __forceinline__ int column(int i) const { return (rank + i * group) * Chunk<T>::E - shift; }
+    __device__ __forceinline__ bool live(int i) const { return column(i) < C; }
+    __device__ __forceinline__ Span span(int i) const {
+        const int c = column(i);
+        return {c < 0 ? -c : 0, C - c < Chunk<T>::E ? C - c : Chunk<T>::E};
+    }
+};
+
+// ---- few rows: one to a block
+template <class T, int V, RowMode kMode, bool kWhole>
+__global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
+    constexpr int E = Chunk<T>::E;
+    __shared__ float2 words[64];
+    Group g{int(blockDim.x), int(threadIdx.x), 0, words};
+    const int row = blockIdx.x;
+    const T* x = static_cast<const T*>(p.x);
+    const T* res = static_cast<const T*>(p.residual);
+    const Chunks<T> ch{p.C, int(blockDim.x), int(threadIdx.x), kWhole ? 0 : int((size_t(row) * p.C) % E)};
+    auto live = [&](int i) { return ch.live(i); };
+    Chunk<T> weight[V];
+    float v[V][E];
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const size_t at = size_t(row) * p.C;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (live(i)) {
+            const Chunk<T> a = load_span<T, kWhole>(x + (at + ch.column(i)), ch.span(i));
+            Chunk<T> b;
+            if (kMode != ROW_QUANTIZE && res) b = load_span<T, kWhole>(res + (at + ch.column(i)), ch.span(i));
+            if (kMode != ROW_QUANTIZE) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
+            a.values(v[i]);
+            if (kMode != ROW_QUANTIZE && res) {
+                float u[E];
+                b.values(u);
+#pragma unroll
+                for (int j = 0; j < E; ++j) v[i][j] += u[j];
+            }
+        }
+    if (kMode != ROW_QUANTIZE && p.h)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (live(i)) store_span<T, kWhole>(static_cast<T*>(p.h) + (at + ch.column(i)), ch.span(i), v[i]);
+    float r, inv;
+    row_factors<T, V, kMode>(g, p, row, true, v, weight, live, r, inv);
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (live(i)) row_store<T, kMode, kWhole>(p, at + ch.column(i), ch.span(i), v[i], weight[i], r, inv);
+}
+
+// ---- many rows
+// A ring of `stages` slots in shared memory; a slot holds a set of rows (`per_group` to a group, `groups` apart) of each tensor.
+struct Pipe {
+    int group, per_group, sets, stages, slot;      // threads that share a row; bytes of one tensor's rows in a slot
+    unsigned int* status;
+};
+constexpr int kMostStages = 8;
+struct PipeShared {
+    uint64_t full[kMostStages], empty[kMostStages];
+    float2 words[64];
+    uint32_t abort_flag;
+};
+// The rows of a set: the bytes that are copied start and end on multiples of 16, and end inside the tensor (where it ends inside a chunk, the
+// rest is read from memory).
+struct Set { int first, rows; size_t from; uint32_t bytes; };
+template <class T>
+__device__ __forceinline__ Set rows_of(int s, int rows_per_set, int N, int C) {
+    Set o;
+    o.first = s * rows_per_set;
+    o.rows = min(rows_per_set, N - o.first);
+    const size_t total = size_t(N) * C * sizeof(T), end = (size_t(o.first) + o.rows) * C * sizeof(T);
+    o.from = size_t(o.first) * C * sizeof(T) & ~size_t(15);
+    const size_t up = (end + 15) & ~size_t(15);
+    o.bytes = uint32_t((up < total ? up : total & ~size_t(15)) - o.from);
+    return o;
+}
+__device__ __forceinline__ void pipe_begin(PipeShared& sh, int stages, int consumer_warps) {
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < stages; ++i) { mbar_init(&sh.full[i], 1); mbar_init(&sh.empty[i], consumer_warps); }
+        sh.abort_flag = 0;
+        mbar_fence_init();
+    }
+    __syncthreads();
+}
+// The copying thread.
+template <class T, int kTensors>
+__device__ __forceinline__ void pipe_produce(PipeShared& sh, const Pipe& q, uint8_t* ring, int groups, int N, int C, const void* const (&src)[kTensors]) {
+    int n = 0;
+    uint32_t tensors = 0;
+#pragma unroll
+    for (int t = 0; t < kTensors; ++t) tensors += src[t] != nullptr;
+    const int slots = tensors * q.slot;
+    bool ok = true;
+    for (int s = blockIdx.x; s < q.sets; s += gridDim.x, ++n) {
+        const int stage = n % q.stages;
+        if (n >= q.stages && !bounded_wait(&sh.empty[stage], (n / q.stages - 1) & 1, &sh.abort_flag, q.status, WAIT_PRODUCER_EMPTY)) { ok = false; break; }
+        const Set o = rows_of<T>(s, q.per_group * groups, N, C);
+        mbar_expect_tx_one(&sh.full[stage], o.bytes * tensors);
+        uint8_t* dst = ring + size_t(stage) * slots;
+#pragma unroll
+        for (int t = 0; t < kTensors; ++t)
+            if (src[t]) {
+                if (o.bytes) bulk_load(dst, static_cast<const uint8_t*>(src[t]) + o.from, o.bytes, &sh.full[stage]);
+                dst += q.slot;
+            }
+    }
+    if (!ok)          // given up: copies already under way still land in this block's shared memory; wait (bounded) for them
+        for (int i = max(0, n - q.stages); i < n; ++i)
+            for (int spin = 0; spin < 1 << 20 && !mbar_try_wait(&sh.full[i % q.stages], (i / q.stages) & 1); ++spin) {}
+}
+// A chunk of a slot, or, behind the copied bytes, of the tensor.
+template <class T, bool kWhole>
+__device__ __forceinline__ Chunk<T> pipe_chunk(const uint8_t* slot, const Set& o, const T* tensor, size_t element, Span s) {
+    const size_t at = element * sizeof(T) - o.from;
+    if (!kWhole && at >= o.bytes) return load_span<T, false>(tensor + element, s);
+    Chunk<T> c;
+    *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(slot + at);
+    return c;
+}
+
+template <class T, int V, RowMode kMode, bool kWhole, int kConsumers>
+__global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kConsumers == 256 ? 3 : 2) row_pipe_kernel(const RowParams p, const Pipe q) {
+    constexpr int E = Chunk<T>::E;
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ PipeShared sh;
+    constexpr int consumers = kConsumers;
+    const int groups = consumers / q.group;
+    pipe_begin(sh, q.stages, consumers / 32);
+    grid_dependency_wait();
+    grid_dependents_launch();
+    const T* x = static_cast<const T*>(p.x);
+    const T* res = static_cast<const T*>(p.residual);
+    if (int(threadIdx.x) >= consumers) {
+        if (int(threadIdx.x) == consumers) {
+            const void* const src[2] = {x, kMode != ROW_QUANTIZE ? res : nullptr};
+            pipe_produce<T, 2>(sh, q, ring, groups, p.N, p.C, src);
+        }
+        return;
+    }
+    Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
+    const Chunks<T> ch{p.C, q.group, g.rank, kWhole ? 0 : int((size_t(blockIdx.x) * q.per_group * groups + g.index) * p.C % E)};
+    auto live = [&](int i) { return ch.live(i); };
+    Chunk<T> weight[V];
+    if (kMode != ROW_QUANTIZE)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (live(i)) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
+    const int slots = (kMode != ROW_QUANTIZE && res ? 2 : 1) * q.slot;
+    bool ok = true;                                            // (a wait ran out: the rest of the loop keeps its barriers, but stores nothing)
+    int n = 0;
+    for (int s = blockIdx.x; s < q.sets; s += gridDim.x, ++n) {
+        const int stage = n % q.stages;
+        const Set o = rows_of<T>(s, q.per_group * groups, p.N, p.C);
+        ok = ok && bounded_wait(&sh.full[stage], (n / q.stages) & 1, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
+        const uint8_t* slot = ring + size_t(stage) * slots;
+        for (int k = 0; k < q.per_group; ++k) {
+            const int row = o.first + k * groups + g.index;
+            const bool mine = row < o.first + o.rows;          // (of the whole group)
+            const size_t at = size_t(row) * p.C;
+            float v[V][E];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (!live(i) || !mine) continue;
+                pipe_chunk<T, kWhole>(slot, o, x, at + ch.column(i), ch.span(i)).values(v[i]);
+                if (kMode != ROW_QUANTIZE && res) {
+                    float u[E];
+                    pipe_chunk<T, kWhole>(slot + q.slot, o, res, at + ch.column(i), ch.span(i)).values(u);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[i][j] += u[j];
+                }
+                if (!kWhole) {
+                    const Span e = ch.span(i);
+#pragma unroll
+                    for (int j = 0; j < E; ++j) v[i][j] = j >= e.lo && j < e.hi ? v[i][j] : 0.f;
+                }
+            }
+            if (k + 1 == q.per_group) {                        // the slot is read
+                __syncwarp();
+                if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[stage]);
+            }
+            if (!mine) continue;
+            if (kMode != ROW_QUANTIZE && p.h && ok)
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    if (span[i].hi > span[i].lo)
+                    if (live(i)) store_span<T, kWhole>(static_cast<T*>(p.h) + (at + ch.column(i)), ch.span(i), v[i]);
+            float r, inv;
+            row_factors<T, V, kMode>(g, p, row, ok, v, weight, live, r, inv);
+            if (ok)
 #pragma unroll
-                        for (int j = 0; j < E; ++j) big = max(big, magnitude(v[i][j]));
-                g.sum_and_max(none, big);
-                const float s = row_rescale(big, p.eps);
-                ss = 0.f; top = 0;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    if (span[i].hi <= span[i].lo) continue;
-                    float wf[E];
-                    if (kMode == ROW_NORM_Q8) weight[i].values(wf);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) {
-                        v[i][j] *= s;
-                        ss = fmaf(v[i][j], v[i][j], ss);
-                        if (kMode == ROW_NORM_Q8) top = max(top, magnitude(v[i][j] * wf[j]));
-                    }
-                }
-                g.sum_and_max(ss, top);
-                r = __frsqrt_rn(fmaf(ss, mean, (p.eps * s) * s));
-                if (g.rank == 0 && p.rstd) p.rstd[row] = r * s;
-            } else {
-                r = __frsqrt_rn(fmaf(ss, mean, p.eps));
-                if (g.rank == 0 && p.rstd) p.rstd[row] = r;
-            }
-        }
-        float inv = 1.f;
-        if (kMode != ROW_NORM) {
-            const float most = __uint_as_float(top) * r / kLargestE4m3;
-            const float scale = most < kLeastScale ? kLeastScale : most;
-            if (g.rank == 0) p.scale[row] = scale;
-            inv = 1.f / scale;
-        }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (span[i].hi <= span[i].lo) continue;
-            const size_t o = at + size_t(g.rank + i * p.group) * E;
-            float wf[E];
-            if (kMode != ROW_QUANTIZE) weight[i].values(wf);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                if (kMode != ROW_QUANTIZE) v[i][j] = v[i][j] * r * wf[j];
-                if (kMode != ROW_NORM) v[i][j] *= inv;
-            }
-            if (kMode == ROW_NORM) store_span(static_cast<T*>(p.y) + o, span[i], v[i]);
-            else store_span_q8<E>(static_cast<uint8_t*>(p.y) + o, span[i], v[i]);
+                for (int i = 0; i < V; ++i)
+                    if (live(i)) row_store<T, kMode, kWhole>(p, at + ch.column(i), ch.span(i), v[i], weight[i], r, inv);
         }
     }
 }
@@ -342,7 +502,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
 
 // ---- gradient
 struct GradParams {
-    int N, C, group;
+    int N, C;
     const void *h, *w;
     const float* rstd;
     const void *dy, *dh;
@@ -350,90 +510,116 @@ struct GradParams {
     float* parts;                // [blocks][C]: sums of dw over each block's rows, or null
 };
 
-template <class T, int V>
-__global__ void __launch_bounds__(512) row_grad_kernel(const GradParams p) {
+template <class T, int V, bool kWhole, int kConsumers>
+__global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) row_grad_kernel(const GradParams p, const Pipe q) {
     constexpr int E = Chunk<T>::E;
-    extern __shared__ float merged[];                          // [C], where a block has several groups
-    __shared__ float2 words[64];
-    Group g{p.group, int(threadIdx.x) % p.group, int(threadIdx.x) / p.group, words};
-    const int groups = blockDim.x / p.group, total = groups * gridDim.x;
-    int row = blockIdx.x * groups + g.index;
-    const T* h = static_cast<const T*>(p.h);
-    const T* w = static_cast<const T*>(p.w);
-    const T* dy = static_cast<const T*>(p.dy);
-    const T* dh = static_cast<const T*>(p.dh);
-    const int shift = int((size_t(row) * p.C) % E);
-    Span span[V];
-    Chunk<T> weight[V];
-    float dw[V][E];
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ PipeShared sh;
+    constexpr int consumers = kConsumers;
+    const int groups = consumers / q.group;
+    pipe_begin(sh, q.stages, consumers / 32);
     grid_dependency_wait();
     grid_dependents_launch();
+    const T* h = static_cast<const T*>(p.h);
+    const T* dy = static_cast<const T*>(p.dy);
+    const T* dh = static_cast<const T*>(p.dh);
+    if (int(threadIdx.x) >= consumers) {
+        if (int(threadIdx.x) == consumers) {
+            const void* const src[3] = {h, dy, dh};
+            pipe_produce<T, 3>(sh, q, ring, groups, p.N, p.C, src);
+        }
+        return;
+    }
+    Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
+    const Chunks<T> ch{p.C, q.group, g.rank, kWhole ? 0 : int((size_t(blockIdx.x) * q.per_group * groups + g.index) * p.C % E)};
+    auto live = [&](int i) { return ch.live(i); };
+    Chunk<T> weight[V];
+    float dw[V][E];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        const int c = (g.rank + i * p.group) * E - shift;
-        span[i] = {c < 0 ? -c : 0, p.C - c < E ? (p.C - c > 0 ? p.C - c : 0) : E};
 #pragma unroll
         for (int j = 0; j < E; ++j) dw[i][j] = 0.f;
-        if (row < p.N && span[i].hi > span[i].lo) weight[i] = load_weights(w, c, span[i], shift);
+        if (live(i)) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
     }
     const float mean = 1.f / float(p.C);
-    for (; row < p.N; row += total) {
-        const size_t at = size_t(row) * p.C - shift;
-        const float r = p.rstd[row];
-        Chunk<T> a[V], b[V], d[V];
-        float dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (span[i].hi > span[i].lo) {
-                const size_t o = at + size_t(g.rank + i * p.group) * E;
-                a[i] = load_span(h + o, span[i]);
-                b[i] = load_span(dy + o, span[i]);
-                if (dh) d[i] = load_span(dh + o, span[i]);
-            }
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (span[i].hi <= span[i].lo) continue;
-            float n[E], y[E], wf[E];
-            a[i].values(n); b[i].values(y); weight[i].values(wf);
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float t = n[j] * r * y[j];               // dy n
-                dw[i][j] += t;
-                dot = fmaf(t, wf[j], dot);
-            }
-        }
-        dot = g.sum(dot) * mean;
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            if (span[i].hi <= span[i].lo) continue;
-            float n[E], y[E], wf[E], o[E];
-            a[i].values(n); b[i].values(y); weight[i].values(wf);
-            if (dh) d[i].values(o);
-#pragma unroll
-            for (int j = 0; j < E; ++j) o[j] = fmaf(r, fmaf(n[j] * r, -dot, y[j] * wf[j]), dh ? o[j] : 0.f);
-            store_span(static_cast<T*>(p.dx) + at + size_t(g.rank + i * p.group) * E, span[i], o);
-        }
-    }
-    if (!p.parts) return;
-    // the groups' sums in the groups' order, then the block's to its row of the parts
-    float* part = p.parts + size_t(blockIdx.x) * p.C;
-    for (int q = 0; q < groups; ++q) {
-        if (q == g.index) {
+    const int slots = (dh ? 3 : 2) * q.slot, rows_per_set = q.per_group * groups;
+    bool ok = true;
+    int n = 0;
+    auto factor = [&](int s) {                                 // rstd of the group's first row of set s
+        const int row = s * rows_per_set + g.index;
+        return s < q.sets && row < p.N ? p.rstd[row] : 0.f;
+    };
+    float next = factor(blockIdx.x);
+    for (int s = blockIdx.x; s < q.sets; s += gridDim.x, ++n) {
+        const int stage = n % q.stages;
+        const Set o = rows_of<T>(s, rows_per_set, p.N, p.C);
+        float r = next;
+        next = factor(s + gridDim.x);
+        ok = ok && bounded_wait(&sh.full[stage], (n / q.stages) & 1, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
+        const uint8_t* slot = ring + size_t(stage) * slots;
+        for (int k = 0; k < q.per_group; ++k) {
+            const int row = o.first + k * groups + g.index;
+            if (row >= o.first + o.rows) break;                // (of the whole group)
+            if (k > 0) r = p.rstd[row];
+            const size_t at = size_t(row) * p.C;
+            float dot = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const int c = (g.rank + i * p.group) * E - shift;
+                if (!live(i)) continue;
+                float x[E], y[E], wf[E];
+                pipe_chunk<T, kWhole>(slot, o, h, at + ch.column(i), ch.span(i)).values(x);
+                pipe_chunk<T, kWhole>(slot + q.slot, o, dy, at + ch.column(i), ch.span(i)).values(y);
+                weight[i].values(wf);
+                const Span e = ch.span(i);
 #pragma unroll
-                for (int j = 0; j < E; ++j)
-                    if (j >= span[i].lo && j < span[i].hi) {
-                        if (groups == 1) part[c + j] = dw[i][j];
-                        else merged[c + j] = q == 0 ? dw[i][j] : merged[c + j] + dw[i][j];
-                    }
+                for (int j = 0; j < E; ++j) {
+                    float t = x[j] * r * y[j];                 // dy n
+                    if (!kWhole) t = j >= e.lo && j < e.hi ? t : 0.f;
+                    dw[i][j] += t;
+                    dot = fmaf(t, wf[j], dot);
+                }
+            }
+            dot = g.sum(dot) * mean;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                if (!live(i)) continue;
+                float x[E], y[E], wf[E], d[E];
+                pipe_chunk<T, kWhole>(slot, o, h, at + ch.column(i), ch.span(i)).values(x);
+                pipe_chunk<T, kWhole>(slot + q.slot, o, dy, at + ch.column(i), ch.span(i)).values(y);
+                if (dh) pipe_chunk<T, kWhole>(slot + 2 * q.slot, o, dh, at + ch.column(i), ch.span(i)).values(d);
+                weight[i].values(wf);
+#pragma unroll
+                for (int j = 0; j < E; ++j) d[j] = fmaf(r, fmaf(x[j] * r, -dot, y[j] * wf[j]), dh ? d[j] : 0.f);
+                if (ok) store_span<T, kWhole>(static_cast<T*>(p.dx) + (at + ch.column(i)), ch.span(i), d);
             }
         }
-        if (groups > 1) __syncthreads();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[stage]);          // the slot is read
     }
-    if (groups > 1)
-        for (int c = threadIdx.x; c < p.C; c += blockDim.x) part[c] = merged[c];
+    if (!p.parts) return;
+    // the groups' sums in the groups' order (in the ring, which is free now), then the block's to its row of the parts
+    float* part = p.parts + size_t(blockIdx.x) * p.C;
+    float* merged = reinterpret_cast<float*>(ring);
+    for (int t = 0; t < groups; ++t) {
+        if (groups > 1) named_barrier_sync(15, consumers);
+        if (t != g.index) continue;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            if (!live(i)) continue;
+            const int c = ch.column(i);
+            const Span e = ch.span(i);
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (kWhole || (j >= e.lo && j < e.hi)) {
+                    if (groups == 1) part[c + j] = dw[i][j];
+                    else merged[c + j] = t == 0 ? dw[i][j] : merged[c + j] + dw[i][j];
+                }
+        }
+    }
+    if (groups > 1) {
+        named_barrier_sync(15, consumers);
+        for (int c = threadIdx.x; c < p.C; c += consumers) part[c] = merged[c];
+    }
 }
 
 template <class T>
@@ -486,38 +672,101 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_parts_kernel(const float* 
     }
 }
 
-constexpr int kMaxChunks = 4;
-constexpr int kBlock = 512;                  // threads of a block of small groups
 constexpr int kMostParts = 296;              // blocks of the gradient
+constexpr int kFewRows = 2;
+constexpr int kMostRing = 216 * 1024;        // of all blocks of an SM
 
-// Threads that share a row of `chunks` chunks (a row that starts inside a chunk may have one more): as many as keep `v` chunks each.
-int group_size(int chunks, int v) {
-    int g = 32;
-    while (g * v < chunks) g *= 2;
-    return g;
-}
+// (a row that starts inside a chunk may have one more)
 int row_chunks(int C, int E) { return (C + E - 1) / E + (C % E != 0); }
 
+// A thread takes 16 elements of a row, 32 in rows that 512 threads would not cover, fewer in rows that need no 32; groups of 32 to 512 threads
+// follow from that.
+template <class T> constexpr int kMostV = 32 / Chunk<T>::E;
+template <class T> bool too_long(int C) { return row_chunks(C, Chunk<T>::E) > kPipeMost * kMostV<T>; }
+template <class T>
+struct PipeShape { Pipe q; int v, groups, consumers, grid; size_t smem; };
+template <class T>
+int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int most_blocks, int blocks_per_sm) {
+    constexpr int E = Chunk<T>::E;
+    const int chunks = row_chunks(C, E), sms = device_sm_count();
+    o.v = chunks <= 32 ? 1 : chunks <= 64 ? 2 : chunks <= kPipeMost * kMostV<T> / 2 ? kMostV<T> / 2 : kMostV<T>;
+    o.q.group = 32;
+    while (o.q.group * o.v < chunks) o.q.group *= 2;
+    o.consumers = o.q.group > 256 ? o.q.group : 256;
+    o.groups = o.consumers / o.q.group;
+    const size_t row = size_t(C) * sizeof(T);
+    // several rows to a group where they are short (and where a group's rows still start alike)
+    int m = 1;
+    if (o.groups % E == 0 || C % E == 0)
+        while (m < 16 && m * o.groups * row < 4096 && long(N) / (2 * m * o.groups) >= 8L * sms) m *= 2;
+    o.q.per_group = m;
+    const int rows = m * o.groups;
+    o.q.sets = (N + rows - 1) / rows;
+    o.q.slot = int(align_up(rows * row + 32, 128));
+    const size_t stage = size_t(o.q.slot) * tensors;
+    const size_t ring = kMostRing / blocks_per_sm / 128 * 128;
+    const size_t room = 2 * stage > ring ? kMostRing : ring;
+    const size_t stages = room / stage;
+    if (stages < 1) return PCL_ERR_UNSUPPORTED_SHAPE;
+    o.q.stages = int(stages < size_t(kMostStages) ? stages : kMostStages);
+    o.smem = stage * o.q.stages;
+    o.grid = sms * (room == kMostRing ? 1 : blocks_per_sm);
+    if (o.grid > most_blocks) o.grid = most_blocks;
+    const int unit = C % E == 0 || rows >= E ? 1 : E / rows;    // (a group's rows are a multiple of E apart)
+    o.grid = o.grid / unit * unit;
+    if (o.grid > o.q.sets) o.grid = o.q.sets;
+    o.q.status = device_status_ptr();
+    return o.q.status ? PCL_OK : PCL_ERR_CUDA;
+}
+template <class K>
+int allow_smem(PerDeviceOnce& once, K kernel) {
+    return once.run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostRing) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    });
+}
+
+template <class T, int V, RowMode kMode, bool kWhole>
+int launch_pipe(const RowParams& p, const PipeShape<T>& o, cudaStream_t st) {
+    auto launch = [&](PerDeviceOnce& once, auto kernel) {
+        const int rc = allow_smem(once, kernel);
+        return rc != PCL_OK ? rc : launch_chained(kernel, dim3(o.grid), dim3(o.consumers + 32), o.smem, st, 1, p, o.q);
+    };
+    static PerDeviceOnce once256, once512;
+    if constexpr (V * Chunk<T>::E <= 16)
+        if (o.consumers == 256) return launch(once256, row_pipe_kernel<T, V, kMode, kWhole, 256>);
+    if constexpr (V * Chunk<T>::E >= 16) return launch(once512, row_pipe_kernel<T, V, kMode, kWhole, 512>);
+    return PCL_ERR_UNSUPPORTED_SHAPE;                          // (not reached: fewer than 16 elements a thread are groups of 32)
+}
+template <class T, int V, RowMode kMode>
+int launch_few(const RowParams& p, int block, cudaStream_t st) {
+    if (p.C % Chunk<T>::E == 0) return launch_chained(row_kernel<T, V, kMode, true>, dim3(p.N), dim3(block), 0, st, 1, p);
+    return launch_chained(row_kernel<T, V, kMode, false>, dim3(p.N), dim3(block), 0, st, 1, p);
+}
 template <class T, RowMode kMode>
-int launch_rows(RowParams p, cudaStream_t st) {
+int launch_rows(const RowParams& p, cudaStream_t st) {
     constexpr int E = Chunk<T>::E;
     const int chunks = row_chunks(p.C, E), sms = device_sm_count();
-    if (chunks > 1024 * kMaxChunks) {
+    if (too_long<T>(p.C)) {
         const int grid = p.N < 2 * sms ? p.N : 2 * sms;
         return launch_chained(long_row_kernel<T, kMode>, dim3(grid), dim3(1024), 0, st, 1, p);
     }
-    // few rows: one chunk a thread, for the shortest way from the first load to the last store
-    const int v = chunks <= 1024 && p.N <= 2 * sms ? 1 : chunks <= 2048 ? 2 : 4;
-    p.group = group_size(chunks, v);
-    const int block = p.group > kBlock || p.N <= sms ? p.group : kBlock, groups = block / p.group;
-    int grid = sms * (2048 / block);
-    const int unit = groups < E ? E / groups : 1;              // (a group's rows are a multiple of E apart)
-    grid = grid / unit * unit;
-    const int need = (p.N + groups - 1) / groups;
-    if (grid > need) grid = need;                              // (every group then has one row)
-    if (v == 1) return launch_chained(row_kernel<T, 1, kMode>, dim3(grid), dim3(block), 0, st, 1, p);
-    if (v == 2) return launch_chained(row_kernel<T, 2, kMode>, dim3(grid), dim3(block), 0, st, 1, p);
-    return launch_chained(row_kernel<T, 4, kMode>, dim3(grid), dim3(block), 0, st, 1, p);
+    if (p.N <= kFewRows * sms) {
+        const int v = chunks <= 1024 ? 1 : chunks <= 2048 ? 2 : 4, block = (((chunks + v - 1) / v) + 31) / 32 * 32;
+        if (v == 1) return launch_few<T, 1, kMode>(p, block, st);
+        if (v == 2) return launch_few<T, 2, kMode>(p, block, st);
+        if constexpr (E == 4) return launch_few<T, 4, kMode>(p, block, st);
+        return PCL_ERR_UNSUPPORTED_SHAPE;                      // (not reached: longer 16-bit rows are walked over twice)
+    }
+    PipeShape<T> o;
+    const int rc = pipe_shape(o, p.N, p.C, kMode != ROW_QUANTIZE && p.residual ? 2 : 1, INT_MAX, 3);
+    if (rc != PCL_OK) return rc;
+    const bool whole = p.C % E == 0;
+#define PCL_ROWS(V_) return whole ? launch_pipe<T, V_, kMode, true>(p, o, st) : launch_pipe<T, V_, kMode, false>(p, o, st)
+    if (o.v == 1) PCL_ROWS(1);
+    if (o.v == 2) PCL_ROWS(2);
+    if (o.v == 4) PCL_ROWS(4);
+    PCL_ROWS(kMostV<T>);
+#undef PCL_ROWS
 }
 
 template <RowMode kMode>
@@ -529,26 +778,36 @@ int launch_rows_of(int type, const RowParams& p, cudaStream_t st) {
     }
 }
 
+template <class T, int V, bool kWhole>
+int launch_grad_pipe(const GradParams& p, const PipeShape<T>& o, cudaStream_t st) {
+    const size_t merged = o.groups > 1 ? size_t(p.C) * 4 : 0, smem = o.smem > merged ? o.smem : merged;
+    auto launch = [&](PerDeviceOnce& once, auto kernel) {
+        const int rc = allow_smem(once, kernel);
+        return rc != PCL_OK ? rc : launch_chained(kernel, dim3(o.grid), dim3(o.consumers + 32), smem, st, 1, p, o.q);
+    };
+    static PerDeviceOnce once256, once512;
+    if constexpr (V * Chunk<T>::E <= 16)
+        if (o.consumers == 256) return launch(once256, row_grad_kernel<T, V, kWhole, 256>);
+    if constexpr (V * Chunk<T>::E >= 16) return launch(once512, row_grad_kernel<T, V, kWhole, 512>);
+    return PCL_ERR_UNSUPPORTED_SHAPE;
+}
 template <class T>
-int launch_grad(GradParams p, void* dw, cudaStream_t st) {
+int launch_grad(const GradParams& p, void* dw, cudaStream_t st) {
     constexpr int E = Chunk<T>::E;
-    const int chunks = row_chunks(p.C, E), sms = device_sm_count();
     int grid, rc;
-    if (chunks > 512 * kMaxChunks) {
+    if (too_long<T>(p.C)) {
         grid = p.N < kMostParts ? p.N : kMostParts;
         rc = launch_chained(long_row_grad_kernel<T>, dim3(grid), dim3(1024), 0, st, 1, p);
     } else {
-        const int v = chunks <= 1024 ? 2 : 4;
-        p.group = group_size(chunks, v);
-        const int block = kBlock, groups = block / p.group;
-        grid = 2 * sms < kMostParts ? 2 * sms : kMostParts;
-        const int unit = groups < E ? E / groups : 1;
-        grid = grid / unit * unit;
-        const int need = (p.N + groups - 1) / groups;
-        if (grid > need) grid = need;
-        const size_t smem = groups > 1 && p.parts ? size_t(p.C) * 4 : 0;      // (groups of up to 256 threads: 16 KB)
-        rc = v == 2 ? launch_chained(row_grad_kernel<T, 2>, dim3(grid), dim3(block), smem, st, 1, p)
-                    : launch_chained(row_grad_kernel<T, 4>, dim3(grid), dim3(block), smem, st, 1, p);
+        PipeShape<T> o;
+        rc = pipe_shape(o, p.N, p.C, p.dh ? 3 : 2, kMostParts, 2);
+        if (rc != PCL_OK) return rc;
+        grid = o.grid;
+        const bool whole = p.C % E == 0;
+        if (o.v == 1) rc = whole ? launch_grad_pipe<T, 1, true>(p, o, st) : launch_grad_pipe<T, 1, false>(p, o, st);
+        else if (o.v == 2) rc = whole ? launch_grad_pipe<T, 2, true>(p, o, st) : launch_grad_pipe<T, 2, false>(p, o, st);
+        else if (o.v == 4) rc = whole ? launch_grad_pipe<T, 4, true>(p, o, st) : launch_grad_pipe<T, 4, false>(p, o, st);
+        else rc = whole ? launch_grad_pipe<T, kMostV<T>, true>(p, o, st) : launch_grad_pipe<T, kMostV<T>, false>(p, o, st);
     }
     if (rc != PCL_OK || !dw) return rc;
     return launch_chained(sum_parts_kernel<T>, dim3((p.C + 31) / 32), dim3(kSumWarps * 32), 0, st, 1, static_cast<const float*>(p.parts), grid, p.C,
@@ -561,20 +820,20 @@ size_t rms_norm_workspace_bytes(int N, int C) { return align_up(size_t(N < kMost
 
 int launch_rms_norm_fwd(int N, int C, int type, const void* x, const void* residual, const void* w, float eps, void* h, void* y,
                         float* scale, float* rstd, cudaStream_t st) {
-    const RowParams p{N, C, 0, eps, x, residual, w, h, y, scale, rstd};
+    const RowParams p{N, C, eps, x, residual, w, h, y, scale, rstd};
     LaunchScope scope(KID_RMS_NORM, double(N) * C * (dtype_bytes(type) * (residual ? 3 : 1) + (scale ? 1 : dtype_bytes(type))), st);
     return scale ? launch_rows_of<ROW_NORM_Q8>(type, p, st) : launch_rows_of<ROW_NORM>(type, p, st);
 }
 
 int launch_quantize_rows(int N, int C, int type, const void* x, void* q, float* scale, cudaStream_t st) {
-    const RowParams p{N, C, 0, 0.f, x, nullptr, nullptr, nullptr, q, scale, nullptr};
+    const RowParams p{N, C, 0.f, x, nullptr, nullptr, nullptr, q, scale, nullptr};
     LaunchScope scope(KID_RMS_NORM, double(N) * C * (dtype_bytes(type) + 1), st);
     return launch_rows_of<ROW_QUANTIZE>(type, p, st);
 }
 
 int launch_rms_norm_bwd(int N, int C, int type, const void* h, const void* w, const float* rstd, const void* dy, const void* dh,
                         void* dx, void* dw, void* ws, cudaStream_t st) {
-    const GradParams p{N, C, 0, h, w, rstd, dy, dh, dx, dw ? static_cast<float*>(ws) : nullptr};
+    const GradParams p{N, C, h, w, rstd, dy, dh, dx, dw ? static_cast<float*>(ws) : nullptr};
     LaunchScope scope(KID_RMS_NORM, double(N) * C * dtype_bytes(type) * (dh ? 4 : 3), st);
     switch (type) {
         case DT_F32: return launch_grad<float>(p, dw, st);
