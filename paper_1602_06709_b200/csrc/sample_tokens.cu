@@ -12,9 +12,9 @@
 //   Every row: the maximum, two 16-bit logits to an instruction.
 //   Small top-k: the k-th largest of the threads' maxima is a bound that k tokens reach and few others; those go to a list in shared memory,
 //     and everything else happens there, by comparing all pairs.
-//   Other filters: a histogram over z, of weights or counts, says in which bin the part kept ends (with top-p: of the tokens whose weight is
-//     not below (1 - top_p) / K of the total; the others together do not reach what top-p leaves out).  The bin's tokens go to the list; if
-//     they do not fit, the bin is divided by the bits of its values, down to a single value.
+//   Top-p alone: a histogram of counts over z (of the tokens whose weight is not below (1 - top_p) / K of the total; the others together do not
+//     reach what top-p leaves out) says in which few bins the part kept ends; their tokens go to the list.
+//   Whatever does not fit in the list: the value at the border is found by histograms of weights or counts, finer each time.
 //   What is kept is summed by pieces of consecutive ids, and the piece in which the random number falls is searched.
 // The cost is the weights': one takes twelve operations in 64 bits, of which an SM does 64 a cycle, so a row that needs all of them takes three
 // times as long as reading it.
@@ -106,6 +106,10 @@ struct Row {
         shift = int(row * k % E);
         vectors = (K + shift + E - 1) / E;
     }
+    __device__ __forceinline__ float value(int id) const {
+        const uint32_t u[4] = {Vec<T>::load(base, id), 0u, 0u, 0u};
+        return Vec<T>::get(u, 0);
+    }
     __device__ __forceinline__ long first(int c) const { return long(c) * E - shift; }
     __device__ __forceinline__ void load(int c, uint32_t (&u)[4]) const {
         const long e = first(c);
@@ -146,18 +150,14 @@ __device__ __forceinline__ float unorder(uint32_t k) { return __uint_as_float(k 
 // x = 16 log2 of it, and a polynomial for the rest, |r| <= 1/2, through (2^(r/16) - 1) / r at the five Chebyshev nodes (relative error 9e-15).
 // Numbers become whole by adding 3 * 2^51 or 2^52 to them.
 struct Scale {
-    double top, inv, per16;                  // the row's maximum, 1 / temperature, 16 log2(e) / temperature
-    double unit;                             // 2^bits
-    double least;                            // smallest x that has a weight
-    const double* table;                     // 2^(i/16) * unit
-    bool infinite;                           // the maximum is +inf: only such logits have weight
-    __device__ __forceinline__ double x(float z) const {
-        if (infinite) return z == INFINITY ? 0.0 : -INFINITY;
-        return (double(z) - top) * per16;
-    }
-    __device__ __forceinline__ u64 weight(float z, double from) const {
-        const double v = x(z);
-        if (!(v >= from)) return 0ull;       // (NaN: -inf at an infinite temperature)
+    double top, per16;                       // the row's maximum, 16 log2(e) / temperature
+    const double* table;                     // 2^(i/16) * 2^bits
+    __device__ __forceinline__ double x(float z) const { return (double(z) - top) * per16; }
+    // (not of -inf at an infinite temperature, nor where the maximum is infinite)
+    __device__ __forceinline__ u64 weight(float z) const {
+        const double raw = x(z);
+        // at least -768, 2^-48, which is 0 in the result (of negative numbers the one with the larger first word is the lower)
+        const double v = __hiloint2double(int(min(unsigned(__double2hiint(raw)), 0xc0880000u)), __double2loint(raw));
         const double t = v + 6755399441055744.0;
         const int i = __double2loint(t);
         const double r = v - (t - 6755399441055744.0);
@@ -166,31 +166,32 @@ struct Scale {
         p = fma(r, p, 0x1.ebfbdff6988c8p-11);
         p = fma(r, p, 0x1.62e42fefa39efp-5) * r;
         double s = table[i & 15];
-        s = __hiloint2double(__double2hiint(s) + (i >> 4 << 20), __double2loint(s));
+        s = __hiloint2double(__double2hiint(s) + ((i & ~15) << 16), __double2loint(s));
         const double w = fma(s, p, s) + 4503599627370496.0;
-        return u64(__double_as_longlong(w)) & 0xfffffffffffffull;
+        return u64(unsigned(__double2hiint(w)) & 0xfffffu) << 32 | unsigned(__double2loint(w));
     }
-    __device__ __forceinline__ u64 weight(float z) const { return weight(z, least); }
 };
-constexpr double kLeastX = -16.0 * kWeightBits;
 
 struct Shared {
-    uint32_t lo[kBins], hi[kBins];           // histogram: weights in two words, or counts in the first
+    uint32_t count[kBins], high[kBins];      // histogram: counts, or weights in two words
     u64 key[kList], weight[kList];           // list: order of the value above, ~id below
     u64 piece[kPieces];
-    uint32_t ties[kPieces];
     double table[16];
     u64 warp_sum[32];
     uint32_t warp_word[32];
     float warp_z[32];
-    int bin, count;
-    u64 above;
-    uint32_t key_lo, key_hi;
+    double warp_low[32], warp_high[32];
+    int bin, last_bin, listed, found, token, border_id;
+    u64 above, found_front;
+    uint32_t key_lo, key_hi, ties;
     float border_z;
-    uint32_t border_ties;
-    int found;
-    u64 found_weight;
-    uint32_t found_ties;
+};
+
+// Where the part kept ends: tokens above `z` are kept, and of those equal to it the ones up to `id`.
+struct Border {
+    float z;
+    int id;
+    __device__ __forceinline__ bool keeps(float v, int token) const { return v > z || (v == z && token <= id); }
 };
 
 __device__ __forceinline__ void add_weight(uint32_t* lo, uint32_t* hi, u64 w) {
@@ -199,34 +200,18 @@ __device__ __forceinline__ void add_weight(uint32_t* lo, uint32_t* hi, u64 w) {
     if (up) atomicAdd(hi, up);
 }
 
-// Inclusive sums over the block's threads (in order) of two numbers; every thread also gets the totals.
-template <int kThreads>
-__device__ __forceinline__ void block_scan(Shared& s, u64& a, uint32_t& c, u64& all_a, uint32_t& all_c) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ u64 warp_sum(u64 a) {              // (of up to 2^63 in all)
+    const uint32_t x = __reduce_add_sync(0xffffffffu, uint32_t(a) & 0xffffffu), y = __reduce_add_sync(0xffffffffu, uint32_t(a >> 24) & 0xffffffu),
+                   z = __reduce_add_sync(0xffffffffu, uint32_t(a >> 48));
+    return x + (u64(y) << 24) + (u64(z) << 48);
+}
+template <class V>
+__device__ __forceinline__ V warp_scan(V a) {                 // inclusive
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const u64 x = __shfl_up_sync(0xffffffffu, a, o);
-        const uint32_t y = __shfl_up_sync(0xffffffffu, c, o);
-        if (lane >= o) { a += x; c += y; }
+        const V x = __shfl_up_sync(0xffffffffu, a, o);
+        if (int(threadIdx.x & 31) >= o) a += x;
     }
-    __syncthreads();
-    if (lane == 31) { s.warp_sum[warp] = a; s.warp_word[warp] = c; }
-    __syncthreads();
-    u64 before = 0;
-    uint32_t before_c = 0;
-    all_a = 0; all_c = 0;
-#pragma unroll 4
-    for (int i = 0; i < kThreads / 32; ++i) {
-        if (i == warp) { before = all_a; before_c = all_c; }
-        all_a += s.warp_sum[i];
-        all_c += s.warp_word[i];
-    }
-    a += before;
-    c += before_c;
-}
-__device__ __forceinline__ u64 warp_sum(u64 a) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
     return a;
 }
 template <int kThreads>
@@ -235,8 +220,20 @@ __device__ __forceinline__ u64 block_sum(Shared& s, u64 a) {
     __syncthreads();
     if ((threadIdx.x & 31) == 0) s.warp_sum[threadIdx.x >> 5] = a;
     __syncthreads();
-    a = (threadIdx.x & 31) < kThreads / 32 ? s.warp_sum[threadIdx.x & 31] : 0ull;
-    return warp_sum(a);
+    return warp_sum((threadIdx.x & 31) < kThreads / 32 ? s.warp_sum[threadIdx.x & 31] : 0ull);
+}
+// Inclusive sums over the block's threads, in order; `words` of the block's warps.
+template <int kThreads, class V>
+__device__ __forceinline__ V block_scan(V* words, V a, V& all) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    a = warp_scan(a);
+    __syncthreads();
+    if (lane == 31) words[warp] = a;
+    __syncthreads();
+    const V w = warp_scan(lane < kThreads / 32 ? words[lane] : V(0));
+    all = __shfl_sync(0xffffffffu, w, 31);
+    const V before = __shfl_sync(0xffffffffu, w, warp ? warp - 1 : 0);
+    return warp ? a + before : a;
 }
 
 // The first bin up to which the histogram holds `want`: its index and what lies in front of it go to s.bin (-1: there is none) and s.above.
@@ -246,15 +243,12 @@ __device__ __forceinline__ void find_bin(Shared& s, u64 want) {
     __syncthreads();
     if (threadIdx.x == 0) s.bin = -1;
     u64 w[kEach], a = 0, all;
-    uint32_t none = 0, none_all;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-        w[i] = u64(s.hi[kEach * threadIdx.x + i]) << 32 | s.lo[kEach * threadIdx.x + i];
+        w[i] = u64(s.high[kEach * threadIdx.x + i]) << 32 | s.count[kEach * threadIdx.x + i];
         a += w[i];
     }
-    u64 before = a;
-    block_scan<kThreads>(s, a, none, all, none_all);
-    before = a - before;
+    u64 before = block_scan<kThreads>(s.warp_sum, a, all) - a;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         if (before < want && before + w[i] >= want) { s.bin = kEach * threadIdx.x + i; s.above = before; }
@@ -263,19 +257,82 @@ __device__ __forceinline__ void find_bin(Shared& s, u64 want) {
     __syncthreads();
 }
 
-// Where the part kept ends: tokens above `z` are kept, and of those equal to it the first `ties` by id.
-struct Border { float z; uint32_t ties; };
-
-// The value at which the tokens in falling order, down to `from`, reach `want` of weight, or of their number; false: they do not.
-template <int kThreads, bool kByWeight, class T>
-__device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, u64 want, Border& border) {
+// Sums of f(value, id) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece.
+template <int kThreads, class T, class F>
+__device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0, int c1, int each, F&& f) {
     constexpr int E = Vec<T>::E;
-    const float scale = float(kBins) / (top - from);          // (top == from: infinite or NaN, and every value then is in bin 0)
+    const int lane = threadIdx.x & 31, pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
+    for (int q = threadIdx.x >> 5; q < pieces; q += kThreads / 32) {
+        u64 sum = 0;
+        for (int o = 0; o < each; ++o) {
+            const int c = c0 + (q * each + o) * 32 + lane;
+            if (c >= c1) break;
+            uint32_t u[4];
+            row.load(c, u);
+            const int id = int(row.first(c));
+#pragma unroll
+            for (int i = 0; i < E; ++i) sum += f(Vec<T>::get(u, i), id + i);
+        }
+        __syncwarp();
+        sum = warp_sum(sum);
+        if (lane == 0) s.piece[q] = sum;
+    }
+    __syncthreads();
+}
+// The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the whole row.
+template <int kThreads, class T, class F>
+__device__ __forceinline__ int locate(Shared& s, const Row<T>& row, int each, u64 target, F&& f) {
+    constexpr int E = Vec<T>::E;
+    int c0 = 0, c1 = row.vectors;
+    u64 front = 0;
+    for (;;) {
+        const int pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
+        const u64 mine = int(threadIdx.x) < pieces ? s.piece[threadIdx.x] : 0ull;
+        u64 all;
+        const u64 upto = front + block_scan<kThreads>(s.warp_sum, mine, all);
+        if (mine > 0 && upto > target && upto - mine <= target) { s.found = threadIdx.x; s.found_front = upto - mine; }
+        __syncthreads();
+        c0 += s.found * each * 32;
+        c1 = min(c0 + each * 32, c1);
+        front = s.found_front;
+        if (each <= 8) break;
+        each = (each + kPieces - 1) / kPieces;                 // (long rows: the piece in pieces)
+        sum_pieces<kThreads>(s, row, c0, c1, each, f);
+    }
+    if (threadIdx.x < 32) {                                    // a warp, 32 vectors at a time
+        for (int c = c0 + threadIdx.x; c - int(threadIdx.x) < c1; c += 32) {
+            uint32_t u[4] = {Vec<T>::kLeast, Vec<T>::kLeast, Vec<T>::kLeast, Vec<T>::kLeast};
+            if (c < c1) row.load(c, u);
+            const int id = int(row.first(c));
+            u64 w[E], a = 0;
+#pragma unroll
+            for (int i = 0; i < E; ++i) { w[i] = c < c1 ? f(Vec<T>::get(u, i), id + i) : 0ull; a += w[i]; }
+            const u64 upto = front + warp_scan(a);
+            u64 at = upto - a;
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                if (w[i] > 0 && at <= target && at + w[i] > target) s.token = id + i;
+                at += w[i];
+            }
+            front = __shfl_sync(0xffffffffu, upto, 31);
+            if (front > target) break;
+        }
+    }
+    __syncthreads();
+    return s.token;
+}
+
+// The value at which the tokens in falling order, down to `from`, reach `want` of weight, or of their number, and how many tokens of that
+// value that takes; false: they do not.  For whatever does not fit in the list.
+template <int kThreads, bool kByWeight, class T>
+__device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, u64 want, float& border, uint32_t& ties) {
+    constexpr int E = Vec<T>::E;
+    const float scale = float(kBins) / (top - from);          // (top == from: infinite, and every value then is in bin 0)
     auto bin_of = [&](float z) { const float b = (top - z) * scale; return b < float(kBins - 1) ? int(b) : b >= float(kBins - 1) ? kBins - 1 : 0; };
     uint32_t lo = 0, hi = 0, step = 0;                        // after the first histogram: bins of `step` keys from hi down to lo
     u64 above = 0;
     for (;;) {
-        for (int i = threadIdx.x; i < kBins; i += kThreads) { s.lo[i] = 0; s.hi[i] = 0; }
+        for (int i = threadIdx.x; i < kBins; i += kThreads) { s.count[i] = 0; s.high[i] = 0; }
         __syncthreads();
         auto bin_or_none = [&](float z) {
             if (step == 0) return z >= from && z > -INFINITY ? bin_of(z) : -1;
@@ -288,8 +345,8 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
                 const float z = Vec<T>::get(u, i) + 0.f;
                 const int b = bin_or_none(z);
                 if (b < 0) continue;
-                if (kByWeight) add_weight(&s.lo[b], &s.hi[b], sc.weight(z));
-                else atomicAdd(&s.lo[b], 1u);
+                if (kByWeight) add_weight(&s.count[b], &s.high[b], sc.weight(z));
+                else atomicAdd(&s.count[b], 1u);
             }
         });
         find_bin<kThreads>(s, want - above);
@@ -297,7 +354,7 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
         const int bin = s.bin;
         above += s.above;
         __syncthreads();
-        if (threadIdx.x == 0) { s.count = 0; s.key_lo = 0xffffffffu; s.key_hi = 0u; }
+        if (threadIdx.x == 0) { s.listed = 0; s.key_lo = 0xffffffffu; s.key_hi = 0u; }
         __syncthreads();
         uint32_t least = 0xffffffffu, most = 0u;
         row.template each<2>([&](uint32_t (&u)[4], int) {
@@ -308,7 +365,7 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
                 const uint32_t k = order(z);
                 least = min(least, k);
                 most = max(most, k);
-                const int at = atomicAdd(&s.count, 1);
+                const int at = atomicAdd(&s.listed, 1);
                 if (at < kList) { s.key[at] = k; s.weight[at] = kByWeight ? sc.weight(z) : 1ull; }
             }
         });
@@ -317,7 +374,7 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
         if ((threadIdx.x & 31) == 0) { atomicMin(&s.key_lo, least); atomicMax(&s.key_hi, most); }
         __syncthreads();
         lo = s.key_lo; hi = s.key_hi;
-        const int n = s.count;
+        const int n = s.listed;
         if (n <= kList || lo == hi) {
             // all pairs; a bin of one value is one pair
             for (int i = threadIdx.x; i < (lo == hi ? 1 : n); i += kThreads) {
@@ -332,16 +389,103 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
                     }
                 if (before < want && before + equal >= want) {        // (all tokens of that value write the same)
                     s.border_z = unorder(uint32_t(mine));
-                    s.border_ties = uint32_t((want - before + s.weight[i] - 1) / s.weight[i]);
+                    s.ties = uint32_t((want - before + s.weight[i] - 1) / s.weight[i]);
                 }
             }
             __syncthreads();
-            border = {s.border_z, s.border_ties};
+            border = s.border_z;
+            ties = s.ties;
             return true;
         }
         step = (hi - lo) / kBins + 1;
         __syncthreads();
     }
+}
+
+// What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list.  Leaves the sums of what is
+// kept (and not below `least`) in s.piece.
+//   A histogram of counts over z from max down to `from` bounds the weight up to each bin from both sides; the border lies in the bins in
+//   which the two bounds reach `want`.  What lies above them is summed exactly, the bins' tokens go to the list, and the exact border is found there.
+template <int kThreads, class T>
+__device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, double unit, u64 want, float least, int each,
+                                        Border& border) {
+    constexpr int E = Vec<T>::E, kEach = kBins / kThreads;
+    const float scale = float(kBins) / (top - from);
+    if (!(scale > 0.f && scale < 1e30f)) return false;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0;
+    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; s.listed = 0; s.border_id = -1; }
+    __syncthreads();
+    row.template each<4>([&](uint32_t (&u)[4], int) {
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float z = Vec<T>::get(u, i);
+            if (z >= from) atomicAdd(&s.count[min(int((top - z) * scale), kBins - 1)], 1u);
+        }
+    });
+    __syncthreads();
+    // bounds of the weight up to each bin.  (A bin's edges are rounded, by less than a thousandth of its width.)
+    const double width = double(top - from) / kBins * sc.per16 * (1.0 / 16.0);          // of a bin, in powers of two
+    double low = 0.0, high = 0.0, lows[kEach], highs[kEach], all;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int b = kEach * threadIdx.x + i;
+        const double at = double(s.count[b]) * unit * exp2(-double(b) * width), edge = double(exp2f(float(width) * 1.002f));
+        lows[i] = b == kBins - 1 ? 0.0 : at / edge * (1.0 - 1e-5);
+        highs[i] = at * double(exp2f(float(width) * 0.002f)) * (1.0 + 1e-5);
+        low += lows[i];
+        high += highs[i];
+    }
+    low = block_scan<kThreads>(s.warp_low, low, all) - low;
+    high = block_scan<kThreads>(s.warp_high, high, all) - high;
+    // (the scans are sums from other ends for other threads: 1e-12 apart)
+    int first = kBins, last = kBins - 1;
+#pragma unroll
+    for (int i = kEach - 1; i >= 0; --i) {
+        double h = high, l = low;
+#pragma unroll
+        for (int j = 0; j <= i; ++j) { h += highs[j]; l += lows[j]; }
+        if (h * (1.0 + 1e-9) >= double(want)) first = kEach * threadIdx.x + i;
+        if (l * (1.0 - 1e-9) >= double(want)) last = kEach * threadIdx.x + i;
+    }
+    first = __reduce_min_sync(0xffffffffu, first);
+    last = __reduce_min_sync(0xffffffffu, last);
+    if ((threadIdx.x & 31) == 0) { atomicMin(&s.bin, first); atomicMin(&s.last_bin, last); }
+    __syncthreads();
+    const float begin = float(s.bin), end = s.last_bin >= kBins - 1 ? INFINITY : float(s.last_bin + 1);
+    u64 above = 0;
+    sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float z, int id) -> u64 {
+        const float b = (top - z) * scale;
+        if (b < begin) {
+            const u64 w = sc.weight(z);
+            above += w;
+            return z >= least ? w : 0ull;
+        }
+        if (b < end && z >= from) {
+            const int at = atomicAdd(&s.listed, 1);
+            if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(id));
+        }
+        return 0ull;
+    });
+    const int n = s.listed;
+    if (n > kList) return false;
+    above = block_sum<kThreads>(s, above);
+    for (int i = threadIdx.x; i < n; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
+    __syncthreads();
+    if (above >= want) return false;                           // (not met: the bounds hold)
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const u64 mine = s.key[i], w = s.weight[i];
+        u64 before = above;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) before += s.key[j] > mine ? s.weight[j] : 0ull;
+        if (before >= want) continue;
+        const float z = unorder(uint32_t(mine >> 32));
+        const int id = int(~uint32_t(mine));
+        if (before + w >= want) { s.border_z = z; s.border_id = id; }
+        if (z >= least) atomicAdd(&s.piece[(id + row.shift) / E / (32 * each)], w);
+    }
+    __syncthreads();
+    border = {s.border_z, s.border_id};
+    return s.border_id >= 0;
 }
 
 template <class T, int kThreads>
@@ -354,9 +498,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     grid_dependents_launch();
     const float temperature = p.temperature ? p.temperature[n] : 1.f;
     int k = p.top_k ? p.top_k[n] : 0;
-    const float top_p = p.top_p ? p.top_p[n] : 1.f, min_p = p.min_p ? p.min_p[n] : 0.f;
+    const float top_p = p.top_p ? p.top_p[n] : 1.f, min_p = p.min_p ? p.min_p[n] : 0.f, u = p.uniform[n];
     if (k < 0 || k >= p.K) k = 0;
-    if (threadIdx.x < 16) s.table[threadIdx.x] = exp2(double(threadIdx.x) / 16.0) * double(1ull << p.bits);
+    const u64 one = 1ull << p.bits;
+    const double unit = double(one);
+    if (threadIdx.x < 16) s.table[threadIdx.x] = exp2(double(threadIdx.x) / 16.0) * unit;
     auto answer = [&](int token, float logprob) {
         p.token[n] = token;
         if (p.logprob) p.logprob[n] = logprob;
@@ -364,7 +510,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 
     // ---- the maximum (NaN if there is one)
     uint32_t m = Vec<T>::kLeast;
-    row.template each<4>([&](uint32_t (&u)[4], int) { m = Vec<T>::max2(m, Vec<T>::max2(Vec<T>::max2(u[0], u[1]), Vec<T>::max2(u[2], u[3]))); });
+    row.template each<4>([&](uint32_t (&q)[4], int) { m = Vec<T>::max2(m, Vec<T>::max2(Vec<T>::max2(q[0], q[1]), Vec<T>::max2(q[2], q[3]))); });
     const float mine = Vec<T>::top(m) + 0.f;                  // (of this thread's tokens)
     float top = mine;
 #pragma unroll
@@ -379,10 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (temperature <= 0.f || k == 1 || top_p <= 0.f) {       // the first token that has the maximum
         uint32_t at = 0xffffffffu;
         if (mine == top)
-            row.template each<2>([&](uint32_t (&u)[4], int c) {
+            row.template each<4>([&](uint32_t (&q)[4], int c) {
 #pragma unroll
                 for (int i = 0; i < E; ++i)
-                    if (Vec<T>::get(u, i) == top) at = min(at, uint32_t(row.first(c) + i));
+                    if (Vec<T>::get(q, i) == top) at = min(at, uint32_t(row.first(c) + i));
             });
         at = __reduce_min_sync(0xffffffffu, at);
         if (lane == 0) s.warp_word[warp] = at;
@@ -391,12 +537,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (threadIdx.x == 0) answer(int(at), 0.f);
         return;
     }
-    const double inv = 1.0 / double(temperature);
-    const double min_x = min_p > 0.f ? 16.0 * log2(fmin(double(min_p), 1.0)) : -INFINITY;                   // (NaN: no filter)
-    const Scale sc{double(top), inv, inv * (16.0 * 1.4426950408889634074), double(1ull << p.bits), kLeastX, s.table, top == INFINITY};
-    const double kept_x = fmax(kLeastX, min_x);               // of what the last filter keeps
-    const bool by_p = top_p < 1.f;
-    const float u = p.uniform[n];
+    const Scale sc{double(top), 16.0 * 1.4426950408889634074 / double(temperature), s.table};
+    const bool infinite = top == INFINITY, by_p = top_p < 1.f;
     auto target_of = [&](u64 total) -> u64 {
         const u64 t = u > 0.f ? u64(double(fminf(u, 1.f - 0x1p-24f)) * double(total)) : 0ull;
         return t < total ? t : total - 1;
@@ -406,61 +548,74 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         return part < 1.0 ? 1ull : u64(part) < total ? u64(part) : total;
     };
     auto logprob_of = [&](float z, u64 total) {
-        return float(sc.x(z) * (0.69314718055994530942 / 16.0) - log(double(total) / sc.unit));
+        return float((infinite ? 0.0 : sc.x(z) * (0.69314718055994530942 / 16.0)) - log(double(total) / unit));
     };
+    // the lowest value that min-p keeps: x(z) >= 16 log2(min_p), from the highest bit of its key down (NaN: no filter)
+    float least = -INFINITY;
+    if (min_p > 0.f && !infinite) {
+        const double min_x = 16.0 * log2(fmin(double(min_p), 1.0));
+        uint32_t below = 0;                                    // the highest key that is not kept, and is no -inf
+#pragma unroll 1
+        for (uint32_t b = 0x80000000u; b; b >>= 1)
+            if ((below | b) < order(top) && ((below | b) <= order(-INFINITY) || !(sc.x(unorder(below | b)) >= min_x))) below |= b;
+        least = unorder(below + 1);
+    }
 
     // ---- small top-k
-    if (k > 0 && k <= kThreads / 2) {
-        // the k-th largest of the threads' maxima, from its highest bit down (0: fewer than k threads have a finite one)
+    if (k > 0 && k <= kThreads / 2 && !infinite) {
+        // the k-th largest of the threads' maxima, from its highest bit down, or a bound that few more reach (0: fewer than k are finite)
         const uint32_t key = mine == -INFINITY ? 0u : order(mine);
         uint32_t bound = 0;
         for (int b = 31; b >= Vec<T>::kLowBit; --b) {
             const uint32_t next = bound | 1u << b;
-            if (__syncthreads_count(key >= next) >= k) bound = next;
+            const int reach = __syncthreads_count(key >= next);
+            if (reach >= k) bound = next;
+            if (reach >= k && reach <= k + 16) break;
         }
         // (the bits of a negative value's key below kLowBit are ones: the bound may be a little low, which is as good)
-        if (threadIdx.x == 0) s.count = 0;
+        if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
+        const float bound_z = bound > order(-INFINITY) ? unorder(bound) : -3.4028234663852886e38f;
         if (key >= bound && mine > -INFINITY)
-            row.template each<4>([&](uint32_t (&u4)[4], int c) {
-                if (order(Vec<T>::top(Vec<T>::max2(Vec<T>::max2(u4[0], u4[1]), Vec<T>::max2(u4[2], u4[3]))) + 0.f) < bound) return;
-#pragma unroll 1
+            row.template each<4>([&](uint32_t (&q)[4], int c) {
+                if (!(Vec<T>::top(Vec<T>::max2(Vec<T>::max2(q[0], q[1]), Vec<T>::max2(q[2], q[3]))) >= bound_z)) return;
+#pragma unroll
                 for (int i = 0; i < E; ++i) {
-                    const float z = Vec<T>::get(u4, i) + 0.f;
-                    if (z == -INFINITY || order(z) < bound) continue;
-                    const int at = atomicAdd(&s.count, 1);
-                    if (at < kList) { s.key[at] = u64(order(z)) << 32 | uint32_t(~uint32_t(row.first(c) + i)); s.weight[at] = sc.weight(z); }
+                    const float z = Vec<T>::get(q, i);
+                    if (z >= bound_z) {
+                        const int at = atomicAdd(&s.listed, 1);
+                        if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(row.first(c) + i));
+                    }
                 }
             });
         __syncthreads();
-        const int count = s.count;
+        const int count = s.listed;
         if (count <= kList) {
             constexpr int kEach = kList / kThreads;
-            u64 before[kEach], sum = 0;
-            bool in[kEach];
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) {
-                const int i = threadIdx.x + e * kThreads;
-                before[e] = 0;
-                in[e] = false;
-                if (i >= count) continue;
-                const u64 me = s.key[i];
-                int rank = 0;
-                for (int j = 0; j < count; ++j)
-                    if (s.key[j] > me) { ++rank; before[e] += s.weight[j]; }
-                in[e] = rank < k;
-                if (in[e]) sum += s.weight[i];
-            }
-            const u64 want = by_p ? part_of(block_sum<kThreads>(s, sum)) : ~0ull;
-            sum = 0;
-            u64 kept[kEach];
+            u64 before[kEach], sum = 0, kept[kEach];
+            for (int i = threadIdx.x; i < count; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
                 const int i = threadIdx.x + e * kThreads;
-                kept[e] = 0;
+                before[e] = kept[e] = 0;
                 if (i >= count) continue;
-                if (in[e] && before[e] < want) kept[e] = sc.weight(unorder(uint32_t(s.key[i] >> 32)), kept_x);
+                const u64 me = s.key[i];
+                int rank = 0;
+#pragma unroll 4
+                for (int j = 0; j < count; ++j)
+                    if (s.key[j] > me) { ++rank; before[e] += s.weight[j]; }
+                if (rank < k) kept[e] = s.weight[i];
+                sum += kept[e];
+            }
+            const u64 want = by_p ? part_of(block_sum<kThreads>(s, sum)) : ~0ull;
+            sum = 0;
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) {
+                const int i = threadIdx.x + e * kThreads;
+                if (i >= count) continue;
+                if (before[e] >= want || unorder(uint32_t(s.key[i] >> 32)) < least) kept[e] = 0;
                 s.weight[i] = kept[e];
                 sum += kept[e];
             }
@@ -471,6 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                 if (i >= count || kept[e] == 0) continue;
                 const uint32_t id = uint32_t(s.key[i]);        // (inverted: a larger one is an earlier token)
                 u64 front = 0;
+#pragma unroll 4
                 for (int j = 0; j < count; ++j) front += uint32_t(s.key[j]) > id ? s.weight[j] : 0ull;
                 if (front <= target && front + kept[e] > target) answer(int(~id), logprob_of(unorder(uint32_t(s.key[i] >> 32)), total));
             }
@@ -480,111 +636,71 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
 
     // ---- where the part kept ends
-    Border border{-INFINITY, 0xffffffffu};
-    const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), -3.4028234663852886e38));        // (what has any weight lies above)
-    if (k > 0) select<kThreads, false>(s, row, sc, top, sc.infinite ? INFINITY : floor_z, u64(k), border);     // (false: fewer have any weight)
-    if (by_p) {
-        u64 sum = 0;
-        row.template each<2>([&](uint32_t (&u4)[4], int) {
+    const int each = (row.vectors + 32 * kPieces - 1) / (32 * kPieces);           // vectors of a piece per lane
+    Border border{-INFINITY, -1};
+    bool summed = false;                                       // the pieces' sums are there
+    auto nth_of = [&](float z, uint32_t ties) {                // the border at that many tokens of value z
+        sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
+        const int id = locate<kThreads>(s, row, each, u64(ties) - 1, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
+        __syncthreads();
+        return Border{z, id};
+    };
+    if (infinite) {                                            // the tokens of +inf share everything
+        u64 count = 0;
+        row.template each<2>([&](uint32_t (&q)[4], int) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float z = Vec<T>::get(u4, i) + 0.f;
-                if (z > border.z) sum += sc.weight(z);
-            }
+            for (int i = 0; i < E; ++i) count += Vec<T>::get(q, i) == INFINITY ? 1 : 0;
         });
-        sum = block_sum<kThreads>(s, sum);
-        if (border.ties != 0xffffffffu) sum += u64(border.ties) * sc.weight(border.z);
-        const double share = (1.0 - double(top_p)) * double(sum) / sc.unit / double(p.K);
-        // (a little lower, so that roundings exclude nothing)
-        const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
-        const float from = sc.infinite ? INFINITY : float(fmax(low, double(floor_z)));
-        Border nucleus{-INFINITY, 0u};
-        if (select<kThreads, true>(s, row, sc, top, from, part_of(sum), nucleus) ||
-            select<kThreads, true>(s, row, sc, top, sc.infinite ? INFINITY : floor_z, part_of(sum), nucleus))      // (top_p next to 1)
-            border = nucleus;
-    }
-
-    // ---- sums of what is kept, by pieces of consecutive ids: a warp takes a piece
-    const int each = (row.vectors + 32 * kPieces / 2 - 1) / (32 * kPieces / 2);                // vectors of a piece per lane
-    const int pieces = (row.vectors + 32 * each - 1) / (32 * each);
-    __syncthreads();
-    for (int q = warp; q < pieces; q += kWarps) {
-        u64 sum = 0;
+        count = block_sum<kThreads>(s, count);
+        if (k > 0 && u64(k) < count) count = u64(k);
+        if (by_p) count = (part_of(count * one) + one - 1) / one;
+        border = nth_of(INFINITY, uint32_t(count));
+    } else {
+        const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), -3.4028234663852886e38));    // (what has any weight lies above)
+        float z = 0.f;
         uint32_t ties = 0;
-        for (int o = 0; o < each; ++o) {
-            const int c = (q * each + o) * 32 + lane;
-            if (c >= row.vectors) break;
-            uint32_t u4[4];
-            row.load(c, u4);
+        if (k > 0 && select<kThreads, false>(s, row, sc, top, floor_z, u64(k), z, ties)) border = nth_of(z, ties);     // (else fewer have any weight)
+        if (by_p) {
+            u64 sum = 0;
+            row.template each<2>([&](uint32_t (&q)[4], int c) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float z = Vec<T>::get(u4, i) + 0.f;
-                if (z > border.z) sum += sc.weight(z, kept_x);
-                else if (z == border.z) ++ties;
+                for (int i = 0; i < E; ++i) {
+                    const float v = Vec<T>::get(q, i);
+                    const u64 w = sc.weight(v);
+                    sum += border.keeps(v, int(row.first(c)) + i) ? w : 0ull;
+                }
+            });
+            sum = block_sum<kThreads>(s, sum);
+            // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
+            const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
+            const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
+            const float from = float(fmax(low, double(floor_z)));
+            const u64 want = part_of(sum);
+            if (k == 0) summed = nucleus<kThreads>(s, row, sc, top, from, unit, want, least, each, border);
+            if (!summed) {
+                __syncthreads();
+                if (select<kThreads, true>(s, row, sc, top, from, want, z, ties) || select<kThreads, true>(s, row, sc, top, floor_z, want, z, ties))
+                    border = nth_of(z, ties);                  // (the second: top_p next to 1)
             }
         }
-        sum = warp_sum(sum);
-        ties = __reduce_add_sync(0xffffffffu, ties);
-        if (lane == 0) { s.piece[q] = sum; s.ties[q] = ties; }
+        if (least > border.z) border = {least, 0x7fffffff};
     }
-    __syncthreads();
-    const u64 tie_weight = border.z > -INFINITY ? sc.weight(border.z, kept_x) : 0ull;
-    const bool has = int(threadIdx.x) < pieces;
-    const uint32_t my_ties = has ? s.ties[threadIdx.x] : 0u;
-    uint32_t ties = my_ties, all_ties;
-    u64 none = 0, none_all;
-    block_scan<kThreads>(s, none, ties, none_all, all_ties);
-    const uint32_t before_ties = ties - my_ties;               // in front of this thread's piece
-    const uint32_t kept_ties = before_ties >= border.ties ? 0u : min(my_ties, border.ties - before_ties);
-    const u64 here = has ? s.piece[threadIdx.x] + u64(kept_ties) * tie_weight : 0ull;
-    u64 sum = here, total;
-    uint32_t no_ties = 0, no_all;
-    block_scan<kThreads>(s, sum, no_ties, total, no_all);
-    const u64 target = target_of(total);
-    if (here > 0 && sum > target && sum - here <= target) {
-        s.found = threadIdx.x;
-        s.found_weight = sum - here;                           // in front of the piece
-        s.found_ties = before_ties;
-    }
-    __syncthreads();
 
-    // ---- within the piece: a vector to a thread
-    u64 done = s.found_weight;
-    uint32_t done_ties = s.found_ties;
-    const int c0 = s.found * each * 32, c1 = min(c0 + each * 32, row.vectors);
-    for (int o = c0; o < c1; o += kThreads) {
-        const int c = o + int(threadIdx.x);
-        uint32_t u4[4] = {Vec<T>::kLeast, Vec<T>::kLeast, Vec<T>::kLeast, Vec<T>::kLeast};
-        if (c < c1) row.load(c, u4);
-        uint32_t own = 0, all_t;
-#pragma unroll
-        for (int i = 0; i < E; ++i) own += Vec<T>::get(u4, i) + 0.f == border.z ? 1u : 0u;
-        uint32_t t = own;
-        u64 nothing = 0, nothing_all;
-        block_scan<kThreads>(s, nothing, t, nothing_all, all_t);
-        t = done_ties + t - own;                               // ties in front of this vector
-        u64 w[E], a = 0;
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float z = Vec<T>::get(u4, i) + 0.f;
-            const bool tie = z == border.z;
-            w[i] = z > border.z ? sc.weight(z, kept_x) : tie && t < border.ties ? tie_weight : 0ull;
-            t += tie ? 1u : 0u;
-            a += w[i];
-        }
-        u64 at = a, all;
-        uint32_t x = 0, all_x;
-        block_scan<kThreads>(s, at, x, all, all_x);
-        at += done - a;                                        // in front of this vector
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            if (w[i] > 0 && at <= target && at + w[i] > target) answer(int(row.first(c) + i), logprob_of(Vec<T>::get(u4, i) + 0.f, total));
-            at += w[i];
-        }
-        done += all;
-        done_ties += all_t;
-        if (done > target) break;
+    // ---- the token
+    auto kept_weight = [&](float v, int id) -> u64 {
+        const u64 w = infinite ? one : sc.weight(v);
+        return border.keeps(v, id) ? w : 0ull;
+    };
+    if (!summed) {
+        __syncthreads();
+        if (!infinite && border.id < 0)                        // (no filter)
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { const u64 w = sc.weight(v); return v > border.z ? w : 0ull; });
+        else
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, kept_weight);
     }
+    const u64 total = block_sum<kThreads>(s, int(threadIdx.x) < (row.vectors + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
+    const int token = locate<kThreads>(s, row, each, target_of(total), kept_weight);
+    if (threadIdx.x == 0) answer(token, logprob_of(row.value(token), total));
 }
 
 template <class T>
