@@ -151,24 +151,25 @@ __device__ __forceinline__ float unorder(uint32_t k) { return __uint_as_float(k 
 // Numbers become whole by adding 3 * 2^51 or 2^52 to them.
 struct Scale {
     double top, per16;                       // the row's maximum, 16 log2(e) / temperature
-    const double* table;                     // 2^(i/16) * 2^bits
+    unsigned lowest;                         // first word of -768 / per16: 2^-48, which is 0 in the result
+    const double* table;                     // 2^(i/16) * 2^bits, its exponent less by i/16 of a power of two
     __device__ __forceinline__ double x(float z) const { return (double(z) - top) * per16; }
-    // (not of -inf at an infinite temperature, nor where the maximum is infinite)
-    __device__ __forceinline__ u64 weight(float z) const {
-        const double raw = x(z);
-        // at least -768, 2^-48, which is 0 in the result (of negative numbers the one with the larger first word is the lower)
-        const double v = __hiloint2double(int(min(unsigned(__double2hiint(raw)), 0xc0880000u)), __double2loint(raw));
-        const double t = v + 6755399441055744.0;
+    // keep = false: 0.  (Not of +inf; what is not kept may be -inf or NaN.)
+    __device__ __forceinline__ u64 weight(float z, bool keep = true) const {
+        const double raw = double(z) - top;
+        // (of negative numbers the one with the larger first word is the lower)
+        const double d = __hiloint2double(int(keep ? min(unsigned(__double2hiint(raw)), lowest) : lowest), __double2loint(raw));
+        const double t = fma(d, per16, 6755399441055744.0);
         const int i = __double2loint(t);
-        const double r = v - (t - 6755399441055744.0);
+        const double r = fma(d, per16, 6755399441055744.0 - t);
         double p = fma(r, 0x1.5d893e58acc63p-30, 0x1.3b2c4ac7da565p-23);
         p = fma(r, p, 0x1.c6b08d6faa1bep-17);
         p = fma(r, p, 0x1.ebfbdff6988c8p-11);
-        p = fma(r, p, 0x1.62e42fefa39efp-5) * r;
-        double s = table[i & 15];
-        s = __hiloint2double(__double2hiint(s) + ((i & ~15) << 16), __double2loint(s));
-        const double w = fma(s, p, s) + 4503599627370496.0;
-        return u64(unsigned(__double2hiint(w)) & 0xfffffu) << 32 | unsigned(__double2loint(w));
+        p = fma(r, p, 0x1.62e42fefa39efp-5);
+        p = fma(r, p, 1.0);
+        const double s = table[i & 15];
+        const double w = fma(__hiloint2double(__double2hiint(s) + (i << 16), __double2loint(s)), p, 4503599627370496.0);
+        return u64(__double_as_longlong(w)) - 0x4330000000000000ull;
     }
 };
 
@@ -182,12 +183,15 @@ struct Shared {
     float warp_z[32];
     double warp_low[32], warp_high[32];
     int bin, last_bin, listed, found, token, border_id;
+    uint32_t fine[kBins];                    // a second histogram, of counts
     u64 above, found_front;
     uint32_t key_lo, key_hi, ties;
     float border_z;
 };
 
-// Where the part kept ends: tokens above `z` are kept, and of those equal to it the ones up to `id`.
+// Where the part kept ends: tokens above `z` are kept, and of those equal to it the ones up to `id` (kAllIds: all of them).
+constexpr int kAllIds = 0x7fffffff;
+constexpr float kLowest = -3.4028234663852886e38f;
 struct Border {
     float z;
     int id;
@@ -257,8 +261,9 @@ __device__ __forceinline__ void find_bin(Shared& s, u64 want) {
     __syncthreads();
 }
 
-// Sums of f(value, id) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece.
-template <int kThreads, class T, class F>
+// Sums of f(value, id) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece (kAdd:
+// added to it).
+template <int kThreads, bool kAdd = false, class T, class F>
 __device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0, int c1, int each, F&& f) {
     constexpr int E = Vec<T>::E;
     const int lane = threadIdx.x & 31, pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
@@ -275,7 +280,7 @@ __device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0,
         }
         __syncwarp();
         sum = warp_sum(sum);
-        if (lane == 0) s.piece[q] = sum;
+        if (lane == 0) s.piece[q] = kAdd ? s.piece[q] + sum : sum;
     }
     __syncthreads();
 }
@@ -402,18 +407,55 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
     }
 }
 
+// The bins of a histogram of counts in which the weight from the top, `above` and then that of the tokens of each bin, reaches `want`: the first
+// and the last that can be it go to s.bin and s.last_bin.  Bin b holds weights between 2^-(from + b * width) and a bin's width less, but for
+// `slack` of rounding (in powers of two) at its edges; the last bin may reach further down.
+template <int kThreads>
+__device__ __forceinline__ void find_bins(Shared& s, const uint32_t* count, double unit, double from, double width, double slack, double above, double want) {
+    constexpr int kEach = kBins / kThreads;
+    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; }
+    double low = 0.0, high = 0.0, lows[kEach], highs[kEach], all;
+    const double most = exp2(slack) * (1.0 + 1e-9), least = exp2(-width - slack) * (1.0 - 1e-9);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int b = kEach * threadIdx.x + i;
+        const double at = count[b] ? double(count[b]) * unit * exp2(-(from + double(b) * width)) : 0.0;
+        lows[i] = b == kBins - 1 ? 0.0 : at * least;
+        highs[i] = at * most + double(count[b]);               // (weights are whole numbers)
+        low += fmax(lows[i] - double(count[b]), 0.0);
+        high += highs[i];
+    }
+    low = above + block_scan<kThreads>(s.warp_low, low, all) - low;
+    high = above + block_scan<kThreads>(s.warp_high, high, all) - high;
+    // (sums in an order of their own for each thread: 1e-12 apart)
+    int first = kBins, last = kBins - 1;
+    bool early = false, late = false;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        high += highs[i];
+        low += fmax(lows[i] - double(count[kEach * threadIdx.x + i]), 0.0);
+        if (!early && high * (1.0 + 1e-9) >= want) { first = kEach * threadIdx.x + i; early = true; }
+        if (!late && low * (1.0 - 1e-9) >= want) { last = kEach * threadIdx.x + i; late = true; }
+    }
+    first = __reduce_min_sync(0xffffffffu, first);
+    last = __reduce_min_sync(0xffffffffu, last);
+    if ((threadIdx.x & 31) == 0) { atomicMin(&s.bin, first); atomicMin(&s.last_bin, last); }
+    __syncthreads();
+}
+
 // What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list.  Leaves the sums of what is
 // kept (and not below `least`) in s.piece.
-//   A histogram of counts over z from max down to `from` bounds the weight up to each bin from both sides; the border lies in the bins in
-//   which the two bounds reach `want`.  What lies above them is summed exactly, the bins' tokens go to the list, and the exact border is found there.
+//   A histogram of counts over z from the top down to `from` bounds the weight up to each bin from both sides; the border lies in the bins in
+//   which the two bounds reach `want`.  What lies above them is summed exactly, their tokens go to the list, and the exact border is found there.
+//   If they do not fit, a finer histogram of those bins, taken in the same pass, narrows them down.
 template <int kThreads, class T>
 __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, double unit, u64 want, float least, int each,
                                         Border& border) {
-    constexpr int E = Vec<T>::E, kEach = kBins / kThreads;
+    constexpr int E = Vec<T>::E;
     const float scale = float(kBins) / (top - from);
     if (!(scale > 0.f && scale < 1e30f)) return false;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0;
-    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; s.listed = 0; s.border_id = -1; }
+    for (int i = threadIdx.x; i < kBins; i += kThreads) { s.count[i] = 0; s.fine[i] = 0; }
+    if (threadIdx.x == 0) { s.listed = 0; s.border_id = -1; }
     __syncthreads();
     row.template each<4>([&](uint32_t (&u)[4], int) {
 #pragma unroll
@@ -423,55 +465,53 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
         }
     });
     __syncthreads();
-    // bounds of the weight up to each bin.  (A bin's edges are rounded, by less than a thousandth of its width.)
     const double width = double(top - from) / kBins * sc.per16 * (1.0 / 16.0);          // of a bin, in powers of two
-    double low = 0.0, high = 0.0, lows[kEach], highs[kEach], all;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-        const int b = kEach * threadIdx.x + i;
-        const double at = double(s.count[b]) * unit * exp2(-double(b) * width), edge = double(exp2f(float(width) * 1.002f));
-        lows[i] = b == kBins - 1 ? 0.0 : at / edge * (1.0 - 1e-5);
-        highs[i] = at * double(exp2f(float(width) * 0.002f)) * (1.0 + 1e-5);
-        low += lows[i];
-        high += highs[i];
-    }
-    low = block_scan<kThreads>(s.warp_low, low, all) - low;
-    high = block_scan<kThreads>(s.warp_high, high, all) - high;
-    // (the scans are sums from other ends for other threads: 1e-12 apart)
-    int first = kBins, last = kBins - 1;
-#pragma unroll
-    for (int i = kEach - 1; i >= 0; --i) {
-        double h = high, l = low;
-#pragma unroll
-        for (int j = 0; j <= i; ++j) { h += highs[j]; l += lows[j]; }
-        if (h * (1.0 + 1e-9) >= double(want)) first = kEach * threadIdx.x + i;
-        if (l * (1.0 - 1e-9) >= double(want)) last = kEach * threadIdx.x + i;
-    }
-    first = __reduce_min_sync(0xffffffffu, first);
-    last = __reduce_min_sync(0xffffffffu, last);
-    if ((threadIdx.x & 31) == 0) { atomicMin(&s.bin, first); atomicMin(&s.last_bin, last); }
-    __syncthreads();
-    const float begin = float(s.bin), end = s.last_bin >= kBins - 1 ? INFINITY : float(s.last_bin + 1);
+    find_bins<kThreads>(s, s.count, unit, 0.0, width, 1e-3 * width, 0.0, double(want));  // (positions are rounded by less than 2^-10 of a bin)
+    const int first = s.bin, last = s.last_bin;
+    if (first > last) return false;                            // (not met: the bounds hold)
+    const float begin = float(first), end = last == kBins - 1 ? INFINITY : float(last + 1), finer = float(kBins) / float(last + 1 - first);
+    auto fine_bin = [&](float b) { return min(int((b - begin) * finer), kBins - 1); };
+    auto push = [&](float z, int id) {
+        const int at = atomicAdd(&s.listed, 1);
+        if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(id));
+    };
     u64 above = 0;
     sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float z, int id) -> u64 {
         const float b = (top - z) * scale;
-        if (b < begin) {
-            const u64 w = sc.weight(z);
-            above += w;
-            return z >= least ? w : 0ull;
+        const u64 w = sc.weight(z, b < begin);
+        above += w;
+        if (b >= begin && b < end && z >= from) {
+            push(z, id);
+            atomicAdd(&s.fine[fine_bin(b)], 1u);
         }
-        if (b < end && z >= from) {
-            const int at = atomicAdd(&s.listed, 1);
-            if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(id));
-        }
-        return 0ull;
+        return z >= least ? w : 0ull;
     });
-    const int n = s.listed;
-    if (n > kList) return false;
     above = block_sum<kThreads>(s, above);
+    if (s.listed > kList) {
+        find_bins<kThreads>(s, s.fine, unit, begin * width, width / finer, 3e-3 * width, double(above), double(want));
+        const int first_fine = s.bin, last_fine = s.last_bin;
+        if (threadIdx.x == 0) s.listed = 0;
+        if (first_fine > last_fine) return false;
+        __syncthreads();
+        u64 more = 0;
+        sum_pieces<kThreads, true>(s, row, 0, row.vectors, each, [&](float z, int id) -> u64 {
+            const float b = (top - z) * scale;
+            u64 w = 0;
+            if (b >= begin && b < end && z >= from) {
+                const int f = fine_bin(b);
+                if (f < first_fine) w = sc.weight(z);
+                else if (f <= last_fine) push(z, id);
+            }
+            more += w;
+            return z >= least ? w : 0ull;
+        });
+        above += block_sum<kThreads>(s, more);
+        if (s.listed > kList) return false;
+    }
+    const int n = s.listed;
     for (int i = threadIdx.x; i < n; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
     __syncthreads();
-    if (above >= want) return false;                           // (not met: the bounds hold)
+    if (above >= want) return false;                           // (not met)
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const u64 mine = s.key[i], w = s.weight[i];
         u64 before = above;
@@ -502,7 +542,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (k < 0 || k >= p.K) k = 0;
     const u64 one = 1ull << p.bits;
     const double unit = double(one);
-    if (threadIdx.x < 16) s.table[threadIdx.x] = exp2(double(threadIdx.x) / 16.0) * unit;
+    if (threadIdx.x < 16) {
+        const double v = exp2(double(threadIdx.x) / 16.0) * unit;
+        s.table[threadIdx.x] = __hiloint2double(__double2hiint(v) - (int(threadIdx.x) << 16), __double2loint(v));
+    }
     auto answer = [&](int token, float logprob) {
         p.token[n] = token;
         if (p.logprob) p.logprob[n] = logprob;
@@ -537,7 +580,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (threadIdx.x == 0) answer(int(at), 0.f);
         return;
     }
-    const Scale sc{double(top), 16.0 * 1.4426950408889634074 / double(temperature), s.table};
+    const double per16 = fmax(16.0 * 1.4426950408889634074 / double(temperature), 1e-290);         // (an infinite temperature: all weights 1)
+    const Scale sc{double(top), per16, unsigned(__double2hiint(-768.0 / per16)), s.table};
     const bool infinite = top == INFINITY, by_p = top_p < 1.f;
     auto target_of = [&](u64 total) -> u64 {
         const u64 t = u > 0.f ? u64(double(fminf(u, 1.f - 0x1p-24f)) * double(total)) : 0ull;
@@ -550,15 +594,32 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto logprob_of = [&](float z, u64 total) {
         return float((infinite ? 0.0 : sc.x(z) * (0.69314718055994530942 / 16.0)) - log(double(total) / unit));
     };
-    // the lowest value that min-p keeps: x(z) >= 16 log2(min_p), from the highest bit of its key down (NaN: no filter)
-    float least = -INFINITY;
+    // the lowest value that min-p keeps: x(z) >= 16 log2(min_p), from a guess by steps that double, then halve (NaN: no filter)
+    float least = kLowest;
     if (min_p > 0.f && !infinite) {
         const double min_x = 16.0 * log2(fmin(double(min_p), 1.0));
-        uint32_t below = 0;                                    // the highest key that is not kept, and is no -inf
-#pragma unroll 1
-        for (uint32_t b = 0x80000000u; b; b >>= 1)
-            if ((below | b) < order(top) && ((below | b) <= order(-INFINITY) || !(sc.x(unorder(below | b)) >= min_x))) below |= b;
-        least = unorder(below + 1);
+        const uint32_t bottom = order(kLowest), most = order(top);
+        auto kept = [&](uint32_t key) { return sc.x(unorder(key)) >= min_x; };
+        const uint32_t guess = order(float(fmin(fmax(double(top) + min_x / per16, double(kLowest)), double(top))));
+        uint32_t lo = bottom - 1, hi = most;                  // the highest key that is not kept and the lowest that is, from outside
+        if (kept(guess)) {
+            hi = guess;
+            for (uint32_t step = 1; hi - bottom >= step && hi > bottom; step *= 2) {
+                if (!kept(hi - step)) { lo = hi - step; break; }
+                hi -= step;
+            }
+        } else {
+            lo = guess;
+            for (uint32_t step = 1; hi - lo > step; step *= 2) {
+                if (kept(lo + step)) { hi = lo + step; break; }
+                lo += step;
+            }
+        }
+        while (hi - lo > 1) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (kept(mid)) hi = mid; else lo = mid;
+        }
+        least = unorder(hi);
     }
 
     // ---- small top-k
@@ -575,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         // (the bits of a negative value's key below kLowBit are ones: the bound may be a little low, which is as good)
         if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
-        const float bound_z = bound > order(-INFINITY) ? unorder(bound) : -3.4028234663852886e38f;
+        const float bound_z = bound > order(-INFINITY) ? unorder(bound) : kLowest;
         if (key >= bound && mine > -INFINITY)
             row.template each<4>([&](uint32_t (&q)[4], int c) {
                 if (!(Vec<T>::top(Vec<T>::max2(Vec<T>::max2(q[0], q[1]), Vec<T>::max2(q[2], q[3]))) >= bound_z)) return;
@@ -637,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 
     // ---- where the part kept ends
     const int each = (row.vectors + 32 * kPieces - 1) / (32 * kPieces);           // vectors of a piece per lane
-    Border border{-INFINITY, -1};
+    Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
     auto nth_of = [&](float z, uint32_t ties) {                // the border at that many tokens of value z
         sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
@@ -656,7 +717,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (by_p) count = (part_of(count * one) + one - 1) / one;
         border = nth_of(INFINITY, uint32_t(count));
     } else {
-        const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), -3.4028234663852886e38));    // (what has any weight lies above)
+        const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), double(kLowest)));    // (what has any weight lies above)
         float z = 0.f;
         uint32_t ties = 0;
         if (k > 0 && select<kThreads, false>(s, row, sc, top, floor_z, u64(k), z, ties)) border = nth_of(z, ties);     // (else fewer have any weight)
@@ -666,8 +727,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const float v = Vec<T>::get(q, i);
-                    const u64 w = sc.weight(v);
-                    sum += border.keeps(v, int(row.first(c)) + i) ? w : 0ull;
+                    sum += sc.weight(v, k > 0 ? border.keeps(v, int(row.first(c)) + i) : v >= kLowest);
                 }
             });
             sum = block_sum<kThreads>(s, sum);
@@ -683,18 +743,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     border = nth_of(z, ties);                  // (the second: top_p next to 1)
             }
         }
-        if (least > border.z) border = {least, 0x7fffffff};
+        if (least > border.z) border = {least, kAllIds};
     }
 
     // ---- the token
-    auto kept_weight = [&](float v, int id) -> u64 {
-        const u64 w = infinite ? one : sc.weight(v);
-        return border.keeps(v, id) ? w : 0ull;
-    };
+    auto kept_weight = [&](float v, int id) -> u64 { return infinite ? border.keeps(v, id) ? one : 0ull : sc.weight(v, border.keeps(v, id)); };
     if (!summed) {
         __syncthreads();
-        if (!infinite && border.id < 0)                        // (no filter)
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { const u64 w = sc.weight(v); return v > border.z ? w : 0ull; });
+        if (!infinite && border.id == kAllIds)
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { return sc.weight(v, v >= border.z); });
         else
             sum_pieces<kThreads>(s, row, 0, row.vectors, each, kept_weight);
     }
