@@ -9,9 +9,10 @@
 //   that what is in flight does not depend on registers; weights, and the sums of dw, stay in registers.
 //   Few rows (at most kFewRows per SM): a block takes a row, straight to registers, in one step.
 //   Rows of more than 16384 elements are walked over twice.
-// Threads take chunks of 16 bytes that are counted in the flat tensor, not in the row, and so are aligned whatever the row length: a row
-// of odd length starts and ends inside a chunk, and those two are written element by element.  The distance between a group's rows is a
-// multiple of a chunk's elements, so that all of them start at the same place of a chunk and registers keep their columns.
+// Threads take chunks of 16 bytes that are counted in the flat tensor, not in the row, and so are aligned whatever the row length: what a row
+// of odd length has in front of its first whole chunk and behind its last are edges, an element each to the group's first threads.  The
+// distance between a group's rows is a multiple of a chunk's elements, so that all of them start at the same place of a chunk and registers keep
+// their columns.
 //
 // Sums over a row are fp32 in a fixed tree.  h is rounded when it is stored, but the norm is that of the sum before rounding.  A row whose
 // sum of squares leaves fp32's range is scaled by a power of two first.
@@ -60,44 +61,16 @@ __device__ __forceinline__ Chunk<T> load_chunk(const T* p) {
     *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(p);
     return c;
 }
-// Which elements of a chunk belong to the row: [lo, hi).  kWhole: all of them or none (rows are multiples of chunks).
-struct Span { int lo, hi; };
-template <class T, bool kWhole = false>
-__device__ __forceinline__ Chunk<T> load_span(const T* p, Span s) {
-    constexpr int E = Chunk<T>::E;
-    if (kWhole || (s.lo == 0 && s.hi == E)) return load_chunk(p);
+template <class T>
+__device__ __forceinline__ void store_chunk(T* p, const float (&v)[Chunk<T>::E]) {
     Chunk<T> c;
 #pragma unroll
-    for (int i = 0; i < E; ++i) c.e[i] = i >= s.lo && i < s.hi ? p[i] : Elem<T>::put(0.f);
-    return c;
-}
-// The weights of a chunk that starts at column c (aligned only where rows start on chunks).
-template <class T, bool kWhole>
-__device__ __forceinline__ Chunk<T> load_weights(const T* w, int c, Span s, int shift) {
-    constexpr int E = Chunk<T>::E;
-    if (kWhole || shift == 0) return load_span<T, kWhole>(w + c, s);
-    Chunk<T> v;
-#pragma unroll
-    for (int i = 0; i < E; ++i) v.e[i] = i >= s.lo && i < s.hi ? w[c + i] : Elem<T>::put(0.f);
-    return v;
-}
-template <class T, bool kWhole = false>
-__device__ __forceinline__ void store_span(T* p, Span s, const float (&v)[Chunk<T>::E]) {
-    constexpr int E = Chunk<T>::E;
-    Chunk<T> c;
-#pragma unroll
-    for (int i = 0; i < E; ++i) c.e[i] = Elem<T>::put(v[i]);
-    if (kWhole || (s.lo == 0 && s.hi == E)) {
-        *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&c);
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (i >= s.lo && i < s.hi) p[i] = c.e[i];
-    }
+    for (int i = 0; i < Chunk<T>::E; ++i) c.e[i] = Elem<T>::put(v[i]);
+    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&c);
 }
 // E values as e4m3 bytes.
-template <int E, bool kWhole = false>
-__device__ __forceinline__ void store_span_q8(uint8_t* p, Span s, const float (&v)[E]) {
+template <int E>
+__device__ __forceinline__ void store_q8(uint8_t* p, const float (&v)[E]) {
     uint32_t q[E / 4];
 #pragma unroll
     for (int i = 0; i < E / 4; ++i) {
@@ -105,14 +78,8 @@ __device__ __forceinline__ void store_span_q8(uint8_t* p, Span s, const float (&
         const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
         q[i] = lo | hi << 16;
     }
-    if (kWhole || (s.lo == 0 && s.hi == E)) {
-        if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
-        else *reinterpret_cast<uint32_t*>(p) = q[0];
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i)
-            if (i >= s.lo && i < s.hi) p[i] = uint8_t(q[i / 4] >> (8 * (i % 4)));
-    }
+    if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
+    else *reinterpret_cast<uint32_t*>(p) = q[0];
 }
 
 // |v| as an integer that orders like it; NaN is above everything, so it survives a maximum.
@@ -172,17 +139,44 @@ __device__ __forceinline__ float row_rescale(uint32_t top, float eps) {
 }
 __device__ __forceinline__ bool out_of_range(float ss, float eps) { return !(ss < 1e38f) || (ss < 1e-24f && eps < 1e-20f); }
 
-// The norm of a row whose values are in v (h in fp32): its factor r, the scale of v where the row had to be scaled first, and, of the 8-bit
-// forms, the scale of y.
-template <class T, int V, RowMode kMode, class Live>
-__device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int row, bool store, float (&v)[V][Chunk<T>::E], const Chunk<T> (&weight)[V],
-                                            const Live& live, float& r, float& inv) {
+// What a thread has of a row: V chunks, `group` apart, and, of rows that are not whole chunks (kWhole = false), maybe an element at the edges.
+template <class T, bool kWhole>
+struct Place {
+    static constexpr int E = Chunk<T>::E;
+    int C, group, rank, head;                // head: elements in front of the first whole chunk
+    int edge;                                // the column of this thread's edge element, or -1
+    __device__ __forceinline__ Place(int C_, int group_, int rank_, size_t row) : C(C_), group(group_), rank(rank_), head(0), edge(-1) {
+        if (kWhole) return;
+        head = int((E - row * C % E) % E);
+        if (head > C) head = C;
+        const int tail = (C - head) % E;
+        if (rank < head) edge = rank;
+        else if (rank < head + tail) edge = C - tail + rank - head;
+    }
+    __device__ __forceinline__ int column(int i) const { return head + (rank + i * group) * E; }
+    __device__ __forceinline__ bool live(int i) const { return column(i) + E <= C; }
+    __device__ __forceinline__ bool has_edge() const { return !kWhole && edge >= 0; }
+    __device__ __forceinline__ Chunk<T> weights(const T* w, int i) const {
+        if (kWhole) return load_chunk(w + column(i));
+        Chunk<T> v;
+#pragma unroll
+        for (int j = 0; j < E; ++j) v.e[j] = w[column(i) + j];
+        return v;
+    }
+};
+
+// The norm of a row whose values are in v and ve (h in fp32; 0 where the thread has none): its factor r, after the row was scaled where it had to
+// be, and, of the 8-bit forms, the inverse of y's scale.
+template <class T, int V, RowMode kMode, bool kWhole>
+__device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int row, bool store, const Place<T, kWhole>& at, float (&v)[V][Chunk<T>::E], float& ve,
+                                            const Chunk<T> (&weight)[V], float we, float& r, float& inv) {
     constexpr int E = Chunk<T>::E;
     auto measure = [&](float& ss, uint32_t& top) {
-        ss = 0.f; top = 0;
+        ss = kWhole || kMode == ROW_QUANTIZE ? 0.f : ve * ve;
+        top = kWhole || kMode == ROW_NORM ? 0u : magnitude(kMode == ROW_NORM_Q8 ? ve * we : ve);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (!live(i)) continue;
+            if (!at.live(i)) continue;
             float wf[E];
             if (kMode == ROW_NORM_Q8) weight[i].values(wf);
 #pragma unroll
@@ -202,15 +196,16 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
     if (kMode != ROW_QUANTIZE) {
         float s = 1.f;
         if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && top >= 0x7f800000u)) {       // (rare; every thread of the group takes it)
-            uint32_t big = 0;
+            uint32_t big = magnitude(ve);
             float none = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (live(i))
+                if (at.live(i))
 #pragma unroll
                     for (int j = 0; j < E; ++j) big = max(big, magnitude(v[i][j]));
             g.sum_and_max(none, big);
             s = row_rescale(big, p.eps);
+            ve *= s;
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
@@ -228,31 +223,36 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
         inv = 1.f / scale;
     }
 }
-template <class T, RowMode kMode, bool kWhole>
-__device__ __forceinline__ void row_store(const RowParams& p, size_t o, Span s, float (&v)[Chunk<T>::E], const Chunk<T>& weight, float r, float inv) {
+template <class T, int V, RowMode kMode, bool kWhole>
+__device__ __forceinline__ void row_store(const RowParams& p, size_t first, const Place<T, kWhole>& at, float (&v)[V][Chunk<T>::E], float ve,
+                                          const Chunk<T> (&weight)[V], float we, float r, float inv) {
     constexpr int E = Chunk<T>::E;
-    float wf[E];
-    if (kMode != ROW_QUANTIZE) weight.values(wf);
 #pragma unroll
-    for (int j = 0; j < E; ++j) {
-        if (kMode != ROW_QUANTIZE) v[j] = v[j] * r * wf[j];
-        if (kMode != ROW_NORM) v[j] *= inv;
+    for (int i = 0; i < V; ++i) {
+        if (!at.live(i)) continue;
+        float wf[E];
+        if (kMode != ROW_QUANTIZE) weight[i].values(wf);
+#pragma unroll
+        for (int j = 0; j < E; ++j) {
+            if (kMode != ROW_QUANTIZE) v[i][j] = v[i][j] * r * wf[j];
+            if (kMode != ROW_NORM) v[i][j] *= inv;
+        }
+        if (kMode == ROW_NORM) store_chunk(static_cast<T*>(p.y) + (first + at.column(i)), v[i]);
+        else store_q8<E>(static_cast<uint8_t*>(p.y) + (first + at.column(i)), v[i]);
     }
-    if (kMode == ROW_NORM) store_span<T, kWhole>(static_cast<T*>(p.y) + o, s, v);
-    else store_span_q8<E, kWhole>(static_cast<uint8_t*>(p.y) + o, s, v);
+    if (at.has_edge()) {
+        if (kMode != ROW_QUANTIZE) ve = ve * r * we;
+        if (kMode == ROW_NORM) static_cast<T*>(p.y)[first + at.edge] = Elem<T>::put(ve);
+        else static_cast<uint8_t*>(p.y)[first + at.edge] = uint8_t(__nv_cvt_float_to_fp8(ve * inv, __NV_SATFINITE, __NV_E4M3));
+    }
 }
-
-// The chunks of a thread: V of a row, `group` apart.
-template <class T>
-struct Chunks {
-    int C, group, rank, shift;               // shift: elements of the first chunk in front of the row
-    __device__ __forceinline__ int column(int i) const { return (rank + i * group) * Chunk<T>::E - shift; }
-    __device__ __forceinline__ bool live(int i) const { return column(i) < C; }
-    __device__ __forceinline__ Span span(int i) const {
-        const int c = column(i);
-        return {c < 0 ? -c : 0, C - c < Chunk<T>::E ? C - c : Chunk<T>::E};
-    }
-};
+template <class T, int V, bool kWhole>
+__device__ __forceinline__ void store_h(T* h, size_t first, const Place<T, kWhole>& at, const float (&v)[V][Chunk<T>::E], float ve) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        if (at.live(i)) store_chunk(h + (first + at.column(i)), v[i]);
+    if (at.has_edge()) h[first + at.edge] = Elem<T>::put(ve);
+}
 
 // ---- few rows: one to a block
 template <class T, int V, RowMode kMode, bool kWhole>
@@ -263,20 +263,19 @@ __global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
     const int row = blockIdx.x;
     const T* x = static_cast<const T*>(p.x);
     const T* res = static_cast<const T*>(p.residual);
-    const Chunks<T> ch{p.C, int(blockDim.x), int(threadIdx.x), kWhole ? 0 : int((size_t(row) * p.C) % E)};
-    auto live = [&](int i) { return ch.live(i); };
+    const Place<T, kWhole> at(p.C, int(blockDim.x), int(threadIdx.x), row);
     Chunk<T> weight[V];
-    float v[V][E];
+    float v[V][E], ve = 0.f, we = 0.f;
     grid_dependency_wait();
     grid_dependents_launch();
-    const size_t at = size_t(row) * p.C;
+    const size_t first = size_t(row) * p.C;
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        if (live(i)) {
-            const Chunk<T> a = load_span<T, kWhole>(x + (at + ch.column(i)), ch.span(i));
+        if (at.live(i)) {
+            const Chunk<T> a = load_chunk(x + (first + at.column(i)));
             Chunk<T> b;
-            if (kMode != ROW_QUANTIZE && res) b = load_span<T, kWhole>(res + (at + ch.column(i)), ch.span(i));
-            if (kMode != ROW_QUANTIZE) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
+            if (kMode != ROW_QUANTIZE && res) b = load_chunk(res + (first + at.column(i)));
+            if (kMode != ROW_QUANTIZE) weight[i] = at.weights(static_cast<const T*>(p.w), i);
             a.values(v[i]);
             if (kMode != ROW_QUANTIZE && res) {
                 float u[E];
@@ -285,15 +284,15 @@ __global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
                 for (int j = 0; j < E; ++j) v[i][j] += u[j];
             }
         }
-    if (kMode != ROW_QUANTIZE && p.h)
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (live(i)) store_span<T, kWhole>(static_cast<T*>(p.h) + (at + ch.column(i)), ch.span(i), v[i]);
+    if (at.has_edge()) {
+        ve = Elem<T>::get(x[first + at.edge]);
+        if (kMode != ROW_QUANTIZE && res) ve += Elem<T>::get(res[first + at.edge]);
+        if (kMode != ROW_QUANTIZE) we = Elem<T>::get(static_cast<const T*>(p.w)[at.edge]);
+    }
+    if (kMode != ROW_QUANTIZE && p.h) store_h<T, V>(static_cast<T*>(p.h), first, at, v, ve);
     float r, inv;
-    row_factors<T, V, kMode>(g, p, row, true, v, weight, live, r, inv);
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-        if (live(i)) row_store<T, kMode, kWhole>(p, at + ch.column(i), ch.span(i), v[i], weight[i], r, inv);
+    row_factors<T, V, kMode>(g, p, row, true, at, v, ve, weight, we, r, inv);
+    row_store<T, V, kMode>(p, first, at, v, ve, weight, we, r, inv);
 }
 
 // ---- many rows
@@ -356,14 +355,17 @@ __device__ __forceinline__ void pipe_produce(PipeShared& sh, const Pipe& q, uint
         for (int i = max(0, n - q.stages); i < n; ++i)
             for (int spin = 0; spin < 1 << 20 && !mbar_try_wait(&sh.full[i % q.stages], (i / q.stages) & 1); ++spin) {}
 }
-// A chunk of a slot, or, behind the copied bytes, of the tensor.
-template <class T, bool kWhole>
-__device__ __forceinline__ Chunk<T> pipe_chunk(const uint8_t* slot, const Set& o, const T* tensor, size_t element, Span s) {
-    const size_t at = element * sizeof(T) - o.from;
-    if (!kWhole && at >= o.bytes) return load_span<T, false>(tensor + element, s);
+// A chunk of a slot, and an element of it, or, behind the copied bytes, of the tensor.
+template <class T>
+__device__ __forceinline__ Chunk<T> slot_chunk(const uint8_t* slot, const Set& o, size_t element) {
     Chunk<T> c;
-    *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(slot + at);
+    *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(slot + (element * sizeof(T) - o.from));
     return c;
+}
+template <class T>
+__device__ __forceinline__ float slot_element(const uint8_t* slot, const Set& o, const T* tensor, size_t element) {
+    const size_t at = element * sizeof(T) - o.from;
+    return Elem<T>::get(at < o.bytes ? *reinterpret_cast<const T*>(slot + at) : tensor[element]);
 }
 
 template <class T, int V, RowMode kMode, bool kWhole, int kConsumers>
@@ -386,13 +388,15 @@ __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kC
         return;
     }
     Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
-    const Chunks<T> ch{p.C, q.group, g.rank, kWhole ? 0 : int((size_t(blockIdx.x) * q.per_group * groups + g.index) * p.C % E)};
-    auto live = [&](int i) { return ch.live(i); };
+    const Place<T, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
     Chunk<T> weight[V];
-    if (kMode != ROW_QUANTIZE)
+    float we = 0.f;
+    if (kMode != ROW_QUANTIZE) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (live(i)) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
+            if (at.live(i)) weight[i] = at.weights(static_cast<const T*>(p.w), i);
+        if (at.has_edge()) we = Elem<T>::get(static_cast<const T*>(p.w)[at.edge]);
+    }
     const int slots = (kMode != ROW_QUANTIZE && res ? 2 : 1) * q.slot;
     bool ok = true;                                            // (a wait ran out: the rest of the loop keeps its barriers, but stores nothing)
     int n = 0;
@@ -404,39 +408,32 @@ __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kC
         for (int k = 0; k < q.per_group; ++k) {
             const int row = o.first + k * groups + g.index;
             const bool mine = row < o.first + o.rows;          // (of the whole group)
-            const size_t at = size_t(row) * p.C;
-            float v[V][E];
+            const size_t begin = size_t(row) * p.C;
+            float v[V][E], ve = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (!live(i) || !mine) continue;
-                pipe_chunk<T, kWhole>(slot, o, x, at + ch.column(i), ch.span(i)).values(v[i]);
+                if (!at.live(i) || !mine) continue;
+                slot_chunk<T>(slot, o, begin + at.column(i)).values(v[i]);
                 if (kMode != ROW_QUANTIZE && res) {
                     float u[E];
-                    pipe_chunk<T, kWhole>(slot + q.slot, o, res, at + ch.column(i), ch.span(i)).values(u);
+                    slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(u);
 #pragma unroll
                     for (int j = 0; j < E; ++j) v[i][j] += u[j];
                 }
-                if (!kWhole) {
-                    const Span e = ch.span(i);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) v[i][j] = j >= e.lo && j < e.hi ? v[i][j] : 0.f;
-                }
+            }
+            if (at.has_edge() && mine) {
+                ve = slot_element(slot, o, x, begin + at.edge);
+                if (kMode != ROW_QUANTIZE && res) ve += slot_element(slot + q.slot, o, res, begin + at.edge);
             }
             if (k + 1 == q.per_group) {                        // the slot is read
                 __syncwarp();
                 if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[stage]);
             }
             if (!mine) continue;
-            if (kMode != ROW_QUANTIZE && p.h && ok)
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (live(i)) store_span<T, kWhole>(static_cast<T*>(p.h) + (at + ch.column(i)), ch.span(i), v[i]);
+            if (kMode != ROW_QUANTIZE && p.h && ok) store_h<T, V>(static_cast<T*>(p.h), begin, at, v, ve);
             float r, inv;
-            row_factors<T, V, kMode>(g, p, row, ok, v, weight, live, r, inv);
-            if (ok)
-#pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (live(i)) row_store<T, kMode, kWhole>(p, at + ch.column(i), ch.span(i), v[i], weight[i], r, inv);
+            row_factors<T, V, kMode>(g, p, row, ok, at, v, ve, weight, we, r, inv);
+            if (ok) row_store<T, V, kMode>(p, begin, at, v, ve, weight, we, r, inv);
         }
     }
 }
@@ -531,16 +528,16 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
         return;
     }
     Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
-    const Chunks<T> ch{p.C, q.group, g.rank, kWhole ? 0 : int((size_t(blockIdx.x) * q.per_group * groups + g.index) * p.C % E)};
-    auto live = [&](int i) { return ch.live(i); };
+    const Place<T, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
     Chunk<T> weight[V];
-    float dw[V][E];
+    float dw[V][E], we = 0.f, dwe = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
         for (int j = 0; j < E; ++j) dw[i][j] = 0.f;
-        if (live(i)) weight[i] = load_weights<T, kWhole>(static_cast<const T*>(p.w), ch.column(i), ch.span(i), ch.shift);
+        if (at.live(i)) weight[i] = at.weights(static_cast<const T*>(p.w), i);
     }
+    if (at.has_edge()) we = Elem<T>::get(static_cast<const T*>(p.w)[at.edge]);
     const float mean = 1.f / float(p.C);
     const int slots = (dh ? 3 : 2) * q.slot, rows_per_set = q.per_group * groups;
     bool ok = true;
@@ -561,36 +558,45 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
             const int row = o.first + k * groups + g.index;
             if (row >= o.first + o.rows) break;                // (of the whole group)
             if (k > 0) r = p.rstd[row];
-            const size_t at = size_t(row) * p.C;
-            float dot = 0.f;
+            const size_t begin = size_t(row) * p.C;
+            float dot = 0.f, ne = 0.f, ge = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (!live(i)) continue;
+                if (!at.live(i)) continue;
                 float x[E], y[E], wf[E];
-                pipe_chunk<T, kWhole>(slot, o, h, at + ch.column(i), ch.span(i)).values(x);
-                pipe_chunk<T, kWhole>(slot + q.slot, o, dy, at + ch.column(i), ch.span(i)).values(y);
+                slot_chunk<T>(slot, o, begin + at.column(i)).values(x);
+                slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(y);
                 weight[i].values(wf);
-                const Span e = ch.span(i);
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
-                    float t = x[j] * r * y[j];                 // dy n
-                    if (!kWhole) t = j >= e.lo && j < e.hi ? t : 0.f;
+                    const float t = x[j] * r * y[j];           // dy n
                     dw[i][j] += t;
                     dot = fmaf(t, wf[j], dot);
                 }
             }
+            if (at.has_edge()) {
+                ne = slot_element(slot, o, h, begin + at.edge) * r;
+                ge = slot_element(slot + q.slot, o, dy, begin + at.edge);
+                dwe += ne * ge;
+                dot = fmaf(ne * ge, we, dot);
+                ge *= we;
+            }
             dot = g.sum(dot) * mean;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                if (!live(i)) continue;
+                if (!at.live(i)) continue;
                 float x[E], y[E], wf[E], d[E];
-                pipe_chunk<T, kWhole>(slot, o, h, at + ch.column(i), ch.span(i)).values(x);
-                pipe_chunk<T, kWhole>(slot + q.slot, o, dy, at + ch.column(i), ch.span(i)).values(y);
-                if (dh) pipe_chunk<T, kWhole>(slot + 2 * q.slot, o, dh, at + ch.column(i), ch.span(i)).values(d);
+                slot_chunk<T>(slot, o, begin + at.column(i)).values(x);
+                slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(y);
+                if (dh) slot_chunk<T>(slot + 2 * q.slot, o, begin + at.column(i)).values(d);
                 weight[i].values(wf);
 #pragma unroll
                 for (int j = 0; j < E; ++j) d[j] = fmaf(r, fmaf(x[j] * r, -dot, y[j] * wf[j]), dh ? d[j] : 0.f);
-                if (ok) store_span<T, kWhole>(static_cast<T*>(p.dx) + (at + ch.column(i)), ch.span(i), d);
+                if (ok) store_chunk(static_cast<T*>(p.dx) + (begin + at.column(i)), d);
+            }
+            if (at.has_edge() && ok) {
+                const float d = dh ? slot_element(slot + 2 * q.slot, o, dh, begin + at.edge) : 0.f;
+                static_cast<T*>(p.dx)[begin + at.edge] = Elem<T>::put(fmaf(r, fmaf(ne, -dot, ge), d));
             }
         }
         __syncwarp();
@@ -603,18 +609,17 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
     for (int t = 0; t < groups; ++t) {
         if (groups > 1) named_barrier_sync(15, consumers);
         if (t != g.index) continue;
+        auto put = [&](int c, float v) {
+            if (groups == 1) part[c] = v;
+            else merged[c] = t == 0 ? v : merged[c] + v;
+        };
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            if (!live(i)) continue;
-            const int c = ch.column(i);
-            const Span e = ch.span(i);
+            if (!at.live(i)) continue;
 #pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (kWhole || (j >= e.lo && j < e.hi)) {
-                    if (groups == 1) part[c + j] = dw[i][j];
-                    else merged[c + j] = t == 0 ? dw[i][j] : merged[c + j] + dw[i][j];
-                }
+            for (int j = 0; j < E; ++j) put(at.column(i) + j, dw[i][j]);
         }
+        if (at.has_edge()) put(at.edge, dwe);
     }
     if (groups > 1) {
         named_barrier_sync(15, consumers);
@@ -676,8 +681,8 @@ constexpr int kMostParts = 296;              // blocks of the gradient
 constexpr int kFewRows = 2;
 constexpr int kMostRing = 216 * 1024;        // of all blocks of an SM
 
-// (a row that starts inside a chunk may have one more)
-int row_chunks(int C, int E) { return (C + E - 1) / E + (C % E != 0); }
+// (of whole chunks; a row shorter than one has one all the same)
+int row_chunks(int C, int E) { return C < E ? 1 : C / E; }
 
 // A thread takes 16 elements of a row, 32 in rows that 512 threads would not cover, fewer in rows that need no 32; groups of 32 to 512 threads
 // follow from that.
