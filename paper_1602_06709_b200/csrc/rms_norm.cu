@@ -3,7 +3,7 @@
 //   h = x + residual,  y[c] = h[c] * r * w[c],  r = 1 / sqrt(mean(h^2) + eps)
 //   dx = dh + r * (g - n * mean(g n)),  dw[c] = sum over the rows of dy[c] n[c],      g = dy w,  n = h r
 //
-// All of it is bound by memory: a row is read once, its values stay in the registers of a group of 32 to 512 threads (up to 32 each) until
+// All of it is bound by memory: a row is read once, its values stay in the registers of a group of 4 to 512 threads (up to 32 each) until
 // its sum is known, or, in the gradient, in shared memory.
 //   Many rows: persistent blocks of several groups.  One warp copies sets of consecutive rows into a ring in shared memory (cp.async.bulk), so
 //   that what is in flight does not depend on registers; weights, and the sums of dw, stay in registers.
@@ -21,6 +21,8 @@
 #include <cuda_fp8.h>
 #include <limits.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "pcl_internal.h"
 #include "pcl_ptx.cuh"
@@ -46,71 +48,131 @@ template <> struct Elem<__half> {
     static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
 };
 
-// 16 bytes of a tensor.
-template <class T> struct alignas(16) Chunk {
-    static constexpr int E = 16 / int(sizeof(T));
-    T e[E];
-    __device__ __forceinline__ void values(float (&v)[E]) const {
+// Two fp32 operations in one instruction: the kernels of ordinary row lengths are bound by instructions before they are bound by memory.
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 o;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(o.x), "=f"(o.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return o;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 o;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(o.x), "=f"(o.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return o;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 o;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(o.x), "=f"(o.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return o;
+}
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+
+// 16 bytes of a tensor, and its values in pairs.
+template <class T> struct Chunk {
+    static constexpr int E = 16 / int(sizeof(T)), P = E / 2;
+    uint32_t u[4];
+    __device__ __forceinline__ void values(float2 (&v)[P]) const {
 #pragma unroll
-        for (int i = 0; i < E; ++i) v[i] = Elem<T>::get(e[i]);
+        for (int i = 0; i < P; ++i) {
+            if constexpr (sizeof(T) == 4) v[i] = make_float2(__uint_as_float(u[2 * i]), __uint_as_float(u[2 * i + 1]));
+            else if constexpr (std::is_same_v<T, __half>) v[i] = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            else v[i] = make_float2(__uint_as_float(u[i] << 16), __uint_as_float(u[i] & 0xffff0000u));
+        }
+    }
+    __device__ __forceinline__ void pack(const float2 (&v)[P]) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                u[2 * i] = __float_as_uint(v[i].x);
+                u[2 * i + 1] = __float_as_uint(v[i].y);
+            } else if constexpr (std::is_same_v<T, __half>) {
+                const __half2 h = __floats2half2_rn(v[i].x, v[i].y);
+                u[i] = *reinterpret_cast<const uint32_t*>(&h);
+            } else {
+                const __nv_bfloat162 h = __floats2bfloat162_rn(v[i].x, v[i].y);
+                u[i] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+        }
     }
 };
 template <class T>
-__device__ __forceinline__ Chunk<T> load_chunk(const T* p) {
-    Chunk<T> c;
-    *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(p);
-    return c;
+__device__ __forceinline__ Chunk<T> load_chunk(const void* p) {
+    const uint4 q = *static_cast<const uint4*>(p);
+    return {{q.x, q.y, q.z, q.w}};
 }
 template <class T>
-__device__ __forceinline__ void store_chunk(T* p, const float (&v)[Chunk<T>::E]) {
+__device__ __forceinline__ void store_chunk(T* p, const float2 (&v)[Chunk<T>::P]) {
     Chunk<T> c;
-#pragma unroll
-    for (int i = 0; i < Chunk<T>::E; ++i) c.e[i] = Elem<T>::put(v[i]);
-    *reinterpret_cast<uint4*>(p) = *reinterpret_cast<const uint4*>(&c);
+    c.pack(v);
+    *reinterpret_cast<uint4*>(p) = make_uint4(c.u[0], c.u[1], c.u[2], c.u[3]);
 }
-// E values as e4m3 bytes.
-template <int E>
-__device__ __forceinline__ void store_q8(uint8_t* p, const float (&v)[E]) {
-    uint32_t q[E / 4];
+// Values as e4m3 bytes.
+template <int P>
+__device__ __forceinline__ void store_q8(uint8_t* p, const float2 (&v)[P]) {
+    uint32_t q[P / 2];
 #pragma unroll
-    for (int i = 0; i < E / 4; ++i) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i], v[4 * i + 1]), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * i + 2], v[4 * i + 3]), __NV_SATFINITE, __NV_E4M3);
+    for (int i = 0; i < P / 2; ++i) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(v[2 * i], __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(v[2 * i + 1], __NV_SATFINITE, __NV_E4M3);
         q[i] = lo | hi << 16;
     }
-    if constexpr (E == 8) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
+    if constexpr (P == 4) *reinterpret_cast<uint2*>(p) = make_uint2(q[0], q[1]);
     else *reinterpret_cast<uint32_t*>(p) = q[0];
 }
 
 // |v| as an integer that orders like it; NaN is above everything, so it survives a maximum.
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-// A group of threads that shares a row: whole warps, several groups to a block.  Reductions alternate between two sets of words, so that
-// one barrier each is enough.
+// A group of threads that shares a row: 4, 8 or 16 lanes of a warp, or whole warps; several groups to a block.  Reductions over several warps
+// alternate between two sets of words, so that one barrier each is enough.
 struct Group {
     int size, rank, index;       // threads, this thread's place, which group of the block
-    float2* words;               // [2][32 warps] of the block
+    float* words;                // [2][2][32] of the block: sums and maxima of its warps
+    uint32_t mask;               // the group's lanes of this warp
     int turn = 0;
+    __device__ __forceinline__ Group(int size_, float* words_)
+        : size(size_), rank(int(threadIdx.x) % size_), index(int(threadIdx.x) / size_), words(words_),
+          mask(size_ < 32 ? ((1u << size_) - 1) << (threadIdx.x & 31 & ~unsigned(size_ - 1)) : 0xffffffffu) {}
     __device__ __forceinline__ void sync() const {
         if (size == int(blockDim.x)) __syncthreads();
         else named_barrier_sync(1 + index, size);
     }
-    // The group's sum of a and maximum of m (in the same order for every thread).
+    // The group's sum of a and (kMax) maximum of m, in the same order for every thread.
+    template <bool kMax>
     __device__ __forceinline__ void sum_and_max(float& a, uint32_t& m) {
+        if (size < 32) {
+            for (int o = size >> 1; o; o >>= 1) {
+                a += __shfl_xor_sync(mask, a, o);
+                if (kMax) m = max(m, __shfl_xor_sync(mask, m, o));
+            }
+            return;
+        }
 #pragma unroll
         for (int o = 16; o; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
-        m = __reduce_max_sync(0xffffffffu, m);
+        if (kMax) m = __reduce_max_sync(0xffffffffu, m);
         if (size == 32) return;
-        float2* slot = words + turn * 32 + index * (size >> 5);
+        float* sums = words + turn * 64;
+        const int warps = size >> 5, first = index * warps;
         turn ^= 1;
-        if ((rank & 31) == 0) slot[rank >> 5] = make_float2(a, __uint_as_float(m));
+        if ((rank & 31) == 0) {
+            sums[first + (rank >> 5)] = a;
+            if (kMax) sums[32 + first + (rank >> 5)] = __uint_as_float(m);
+        }
         sync();
-        a = 0.f; m = 0;
-        for (int i = 0; i < size >> 5; ++i) { a += slot[i].x; m = max(m, __float_as_uint(slot[i].y)); }
+        a = 0.f;
+        if (kMax) m = 0;
+#pragma unroll 4
+        for (int i = first; i < first + warps; ++i) {
+            a += sums[i];
+            if (kMax) m = max(m, __float_as_uint(sums[32 + i]));
+        }
     }
     __device__ __forceinline__ float sum(float a) {
-        uint32_t none = 0;
-        sum_and_max(a, none);
+        uint32_t none;
+        sum_and_max<false>(a, none);
         return a;
     }
 };
@@ -139,54 +201,60 @@ __device__ __forceinline__ float row_rescale(uint32_t top, float eps) {
 }
 __device__ __forceinline__ bool out_of_range(float ss, float eps) { return !(ss < 1e38f) || (ss < 1e-24f && eps < 1e-20f); }
 
-// What a thread has of a row: V chunks, `group` apart, and, of rows that are not whole chunks (kWhole = false), maybe an element at the edges.
-template <class T, bool kWhole>
+// What a thread has of a row: up to V chunks, `group` apart, and, where the row is not just those (kWhole = false), maybe an element at the edges:
+// in front of the first whole chunk, or behind the last one that has a thread.
+template <class T, int V, bool kWhole>
 struct Place {
     static constexpr int E = Chunk<T>::E;
-    int C, group, rank, head;                // head: elements in front of the first whole chunk
+    int group, rank, head, chunks;           // head: elements in front of the first whole chunk
     int edge;                                // the column of this thread's edge element, or -1
-    __device__ __forceinline__ Place(int C_, int group_, int rank_, size_t row) : C(C_), group(group_), rank(rank_), head(0), edge(-1) {
+    __device__ __forceinline__ Place(int C, int group_, int rank_, size_t row) : group(group_), rank(rank_), head(0), chunks(C / E), edge(-1) {
         if (kWhole) return;
-        head = int((E - row * C % E) % E);
-        if (head > C) head = C;
-        const int tail = (C - head) % E;
+        head = min(int((E - row * C % E) % E), C);
+        chunks = min((C - head) / E, V * group);
+        const int tail = C - head - chunks * E;
         if (rank < head) edge = rank;
         else if (rank < head + tail) edge = C - tail + rank - head;
     }
     __device__ __forceinline__ int column(int i) const { return head + (rank + i * group) * E; }
-    __device__ __forceinline__ bool live(int i) const { return column(i) + E <= C; }
+    __device__ __forceinline__ bool live(int i) const { return rank + i * group < chunks; }
     __device__ __forceinline__ bool has_edge() const { return !kWhole && edge >= 0; }
     __device__ __forceinline__ Chunk<T> weights(const T* w, int i) const {
-        if (kWhole) return load_chunk(w + column(i));
-        Chunk<T> v;
+        if (kWhole) return load_chunk<T>(w + column(i));
+        float2 v[E / 2];
 #pragma unroll
-        for (int j = 0; j < E; ++j) v.e[j] = w[column(i) + j];
-        return v;
+        for (int j = 0; j < E / 2; ++j) v[j] = make_float2(Elem<T>::get(w[column(i) + 2 * j]), Elem<T>::get(w[column(i) + 2 * j + 1]));
+        Chunk<T> c;
+        c.pack(v);                           // (exact)
+        return c;
     }
 };
 
 // The norm of a row whose values are in v and ve (h in fp32; 0 where the thread has none): its factor r, after the row was scaled where it had to
 // be, and, of the 8-bit forms, the inverse of y's scale.
 template <class T, int V, RowMode kMode, bool kWhole>
-__device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int row, bool store, const Place<T, kWhole>& at, float (&v)[V][Chunk<T>::E], float& ve,
+__device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int row, bool store, const Place<T, V, kWhole>& at, float2 (&v)[V][Chunk<T>::P], float& ve,
                                             const Chunk<T> (&weight)[V], float we, float& r, float& inv) {
-    constexpr int E = Chunk<T>::E;
+    constexpr int P = Chunk<T>::P;
     auto measure = [&](float& ss, uint32_t& top) {
-        ss = kWhole || kMode == ROW_QUANTIZE ? 0.f : ve * ve;
+        float2 sum = make_float2(kWhole || kMode == ROW_QUANTIZE ? 0.f : ve * ve, 0.f);
         top = kWhole || kMode == ROW_NORM ? 0u : magnitude(kMode == ROW_NORM_Q8 ? ve * we : ve);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (!at.live(i)) continue;
-            float wf[E];
+            float2 wf[P];
             if (kMode == ROW_NORM_Q8) weight[i].values(wf);
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                if (kMode != ROW_QUANTIZE) ss = fmaf(v[i][j], v[i][j], ss);
-                if (kMode == ROW_NORM_Q8) top = max(top, magnitude(v[i][j] * wf[j]));
-                if (kMode == ROW_QUANTIZE) top = max(top, magnitude(v[i][j]));
+            for (int j = 0; j < P; ++j) {
+                if (kMode != ROW_QUANTIZE) sum = fma2(v[i][j], v[i][j], sum);
+                if (kMode != ROW_NORM) {
+                    const float2 y = kMode == ROW_NORM_Q8 ? mul2(v[i][j], wf[j]) : v[i][j];
+                    top = max(top, max(magnitude(y.x), magnitude(y.y)));
+                }
             }
         }
-        g.sum_and_max(ss, top);
+        ss = sum.x + sum.y;
+        g.sum_and_max<kMode != ROW_NORM>(ss, top);
     };
     const float mean = 1.f / float(p.C);
     float ss;
@@ -202,14 +270,14 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
             for (int i = 0; i < V; ++i)
                 if (at.live(i))
 #pragma unroll
-                    for (int j = 0; j < E; ++j) big = max(big, magnitude(v[i][j]));
-            g.sum_and_max(none, big);
+                    for (int j = 0; j < P; ++j) big = max(big, max(magnitude(v[i][j].x), magnitude(v[i][j].y)));
+            g.sum_and_max<true>(none, big);
             s = row_rescale(big, p.eps);
             ve *= s;
 #pragma unroll
             for (int i = 0; i < V; ++i)
 #pragma unroll
-                for (int j = 0; j < E; ++j) v[i][j] *= s;
+                for (int j = 0; j < P; ++j) v[i][j] = mul2(v[i][j], both(s));
             measure(ss, top);
         }
         r = __frsqrt_rn(fmaf(ss, mean, (p.eps * s) * s));
@@ -224,21 +292,21 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
     }
 }
 template <class T, int V, RowMode kMode, bool kWhole>
-__device__ __forceinline__ void row_store(const RowParams& p, size_t first, const Place<T, kWhole>& at, float (&v)[V][Chunk<T>::E], float ve,
+__device__ __forceinline__ void row_store(const RowParams& p, size_t first, const Place<T, V, kWhole>& at, float2 (&v)[V][Chunk<T>::P], float ve,
                                           const Chunk<T> (&weight)[V], float we, float r, float inv) {
-    constexpr int E = Chunk<T>::E;
+    constexpr int P = Chunk<T>::P;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
         if (!at.live(i)) continue;
-        float wf[E];
+        float2 wf[P];
         if (kMode != ROW_QUANTIZE) weight[i].values(wf);
 #pragma unroll
-        for (int j = 0; j < E; ++j) {
-            if (kMode != ROW_QUANTIZE) v[i][j] = v[i][j] * r * wf[j];
-            if (kMode != ROW_NORM) v[i][j] *= inv;
+        for (int j = 0; j < P; ++j) {
+            if (kMode != ROW_QUANTIZE) v[i][j] = mul2(mul2(v[i][j], both(r)), wf[j]);
+            if (kMode != ROW_NORM) v[i][j] = mul2(v[i][j], both(inv));
         }
         if (kMode == ROW_NORM) store_chunk(static_cast<T*>(p.y) + (first + at.column(i)), v[i]);
-        else store_q8<E>(static_cast<uint8_t*>(p.y) + (first + at.column(i)), v[i]);
+        else store_q8<P>(static_cast<uint8_t*>(p.y) + (first + at.column(i)), v[i]);
     }
     if (at.has_edge()) {
         if (kMode != ROW_QUANTIZE) ve = ve * r * we;
@@ -247,7 +315,7 @@ __device__ __forceinline__ void row_store(const RowParams& p, size_t first, cons
     }
 }
 template <class T, int V, bool kWhole>
-__device__ __forceinline__ void store_h(T* h, size_t first, const Place<T, kWhole>& at, const float (&v)[V][Chunk<T>::E], float ve) {
+__device__ __forceinline__ void store_h(T* h, size_t first, const Place<T, V, kWhole>& at, const float2 (&v)[V][Chunk<T>::P], float ve) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
         if (at.live(i)) store_chunk(h + (first + at.column(i)), v[i]);
@@ -257,31 +325,32 @@ __device__ __forceinline__ void store_h(T* h, size_t first, const Place<T, kWhol
 // ---- few rows: one to a block
 template <class T, int V, RowMode kMode, bool kWhole>
 __global__ void __launch_bounds__(1024) row_kernel(const RowParams p) {
-    constexpr int E = Chunk<T>::E;
-    __shared__ float2 words[64];
-    Group g{int(blockDim.x), int(threadIdx.x), 0, words};
+    constexpr int P = Chunk<T>::P;
+    __shared__ float words[128];
+    Group g(int(blockDim.x), words);
     const int row = blockIdx.x;
     const T* x = static_cast<const T*>(p.x);
     const T* res = static_cast<const T*>(p.residual);
-    const Place<T, kWhole> at(p.C, int(blockDim.x), int(threadIdx.x), row);
+    const Place<T, V, kWhole> at(p.C, int(blockDim.x), int(threadIdx.x), row);
     Chunk<T> weight[V];
-    float v[V][E], ve = 0.f, we = 0.f;
+    float2 v[V][P];
+    float ve = 0.f, we = 0.f;
     grid_dependency_wait();
     grid_dependents_launch();
     const size_t first = size_t(row) * p.C;
 #pragma unroll
     for (int i = 0; i < V; ++i)
         if (at.live(i)) {
-            const Chunk<T> a = load_chunk(x + (first + at.column(i)));
+            const Chunk<T> a = load_chunk<T>(x + (first + at.column(i)));
             Chunk<T> b;
-            if (kMode != ROW_QUANTIZE && res) b = load_chunk(res + (first + at.column(i)));
+            if (kMode != ROW_QUANTIZE && res) b = load_chunk<T>(res + (first + at.column(i)));
             if (kMode != ROW_QUANTIZE) weight[i] = at.weights(static_cast<const T*>(p.w), i);
             a.values(v[i]);
             if (kMode != ROW_QUANTIZE && res) {
-                float u[E];
+                float2 u[P];
                 b.values(u);
 #pragma unroll
-                for (int j = 0; j < E; ++j) v[i][j] += u[j];
+                for (int j = 0; j < P; ++j) v[i][j] = add2(v[i][j], u[j]);
             }
         }
     if (at.has_edge()) {
@@ -304,7 +373,7 @@ struct Pipe {
 constexpr int kMostStages = 8;
 struct PipeShared {
     uint64_t full[kMostStages], empty[kMostStages];
-    float2 words[64];
+    float words[128];
     uint32_t abort_flag;
 };
 // The rows of a set: the bytes that are copied start and end on multiples of 16, and end inside the tensor (where it ends inside a chunk, the
@@ -355,26 +424,24 @@ __device__ __forceinline__ void pipe_produce(PipeShared& sh, const Pipe& q, uint
         for (int i = max(0, n - q.stages); i < n; ++i)
             for (int spin = 0; spin < 1 << 20 && !mbar_try_wait(&sh.full[i % q.stages], (i / q.stages) & 1); ++spin) {}
 }
-// A chunk of a slot, and an element of it, or, behind the copied bytes, of the tensor.
-template <class T>
-__device__ __forceinline__ Chunk<T> slot_chunk(const uint8_t* slot, const Set& o, size_t element) {
-    Chunk<T> c;
-    *reinterpret_cast<uint4*>(&c) = *reinterpret_cast<const uint4*>(slot + (element * sizeof(T) - o.from));
-    return c;
+// Byte at which row `first + n` of a set starts in a slot.
+template <class T, bool kWhole>
+__device__ __forceinline__ uint32_t row_start(int s, int rows_per_set, int n, int C) {
+    const uint32_t lead = kWhole ? 0u : uint32_t(size_t(s) * rows_per_set * C * sizeof(T)) & 15u;
+    return lead + uint32_t(n) * C * uint32_t(sizeof(T));
 }
+// An element of a slot, or, behind the copied bytes (the end of a tensor that ends inside 16 bytes), of the tensor.
 template <class T>
-__device__ __forceinline__ float slot_element(const uint8_t* slot, const Set& o, const T* tensor, size_t element) {
-    const size_t at = element * sizeof(T) - o.from;
-    return Elem<T>::get(at < o.bytes ? *reinterpret_cast<const T*>(slot + at) : tensor[element]);
+__device__ __forceinline__ float slot_element(const uint8_t* slot, uint32_t at, size_t size, const T* tensor, size_t element) {
+    return Elem<T>::get(element * sizeof(T) < (size & ~size_t(15)) ? *reinterpret_cast<const T*>(slot + at) : tensor[element]);
 }
 
 template <class T, int V, RowMode kMode, bool kWhole, int kConsumers>
 __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kConsumers == 256 ? 3 : 2) row_pipe_kernel(const RowParams p, const Pipe q) {
-    constexpr int E = Chunk<T>::E;
+    constexpr int P = Chunk<T>::P;
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ PipeShared sh;
-    constexpr int consumers = kConsumers;
-    const int groups = consumers / q.group;
+    const int consumers = int(blockDim.x) - 32, groups = consumers / q.group;
     pipe_begin(sh, q.stages, consumers / 32);
     grid_dependency_wait();
     grid_dependents_launch();
@@ -387,8 +454,8 @@ __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kC
         }
         return;
     }
-    Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
-    const Place<T, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
+    Group g(q.group, sh.words);
+    const Place<T, V, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
     Chunk<T> weight[V];
     float we = 0.f;
     if (kMode != ROW_QUANTIZE) {
@@ -397,44 +464,47 @@ __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kC
             if (at.live(i)) weight[i] = at.weights(static_cast<const T*>(p.w), i);
         if (at.has_edge()) we = Elem<T>::get(static_cast<const T*>(p.w)[at.edge]);
     }
-    const int slots = (kMode != ROW_QUANTIZE && res ? 2 : 1) * q.slot;
+    const int slots = (kMode != ROW_QUANTIZE && res ? 2 : 1) * q.slot, rows_per_set = q.per_group * groups;
+    const size_t size = size_t(p.N) * p.C * sizeof(T);
     bool ok = true;                                            // (a wait ran out: the rest of the loop keeps its barriers, but stores nothing)
-    int n = 0;
-    for (int s = blockIdx.x; s < q.sets; s += gridDim.x, ++n) {
-        const int stage = n % q.stages;
-        const Set o = rows_of<T>(s, q.per_group * groups, p.N, p.C);
-        ok = ok && bounded_wait(&sh.full[stage], (n / q.stages) & 1, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
+    int stage = 0;
+    uint32_t phase = 0;
+    for (int s = blockIdx.x; s < q.sets; s += gridDim.x) {
+        ok = ok && bounded_wait(&sh.full[stage], phase, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
         const uint8_t* slot = ring + size_t(stage) * slots;
         for (int k = 0; k < q.per_group; ++k) {
-            const int row = o.first + k * groups + g.index;
-            const bool mine = row < o.first + o.rows;          // (of the whole group)
+            const int n = k * groups + g.index, row = s * rows_per_set + n;
+            const bool mine = row < p.N;                       // (of the whole group)
+            const uint8_t* from = slot + row_start<T, kWhole>(s, rows_per_set, n, p.C);
             const size_t begin = size_t(row) * p.C;
-            float v[V][E], ve = 0.f;
+            float2 v[V][P];
+            float ve = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (!at.live(i) || !mine) continue;
-                slot_chunk<T>(slot, o, begin + at.column(i)).values(v[i]);
+                load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(v[i]);
                 if (kMode != ROW_QUANTIZE && res) {
-                    float u[E];
-                    slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(u);
+                    float2 u[P];
+                    load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(u);
 #pragma unroll
-                    for (int j = 0; j < E; ++j) v[i][j] += u[j];
+                    for (int j = 0; j < P; ++j) v[i][j] = add2(v[i][j], u[j]);
                 }
             }
             if (at.has_edge() && mine) {
-                ve = slot_element(slot, o, x, begin + at.edge);
-                if (kMode != ROW_QUANTIZE && res) ve += slot_element(slot + q.slot, o, res, begin + at.edge);
+                ve = slot_element(from, at.edge * sizeof(T), size, x, begin + at.edge);
+                if (kMode != ROW_QUANTIZE && res) ve += slot_element(from + q.slot, at.edge * sizeof(T), size, res, begin + at.edge);
             }
             if (k + 1 == q.per_group) {                        // the slot is read
                 __syncwarp();
                 if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[stage]);
             }
-            if (!mine) continue;
+            if (!mine) continue;                               // (the lanes of a warp may part here: reductions are the group's own)
             if (kMode != ROW_QUANTIZE && p.h && ok) store_h<T, V>(static_cast<T*>(p.h), begin, at, v, ve);
             float r, inv;
             row_factors<T, V, kMode>(g, p, row, ok, at, v, ve, weight, we, r, inv);
             if (ok) row_store<T, V, kMode>(p, begin, at, v, ve, weight, we, r, inv);
         }
+        if (++stage == q.stages) { stage = 0; phase ^= 1u; }
     }
 }
 
@@ -442,8 +512,8 @@ __global__ void __launch_bounds__(kConsumers + 32, V * Chunk<T>::E > 16 ? 1 : kC
 // element.
 template <class T, RowMode kMode>
 __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
-    __shared__ float2 words[64];
-    Group g{int(blockDim.x), int(threadIdx.x), 0, words};
+    __shared__ float words[128];
+    Group g(int(blockDim.x), words);
     const T* x = static_cast<const T*>(p.x);
     const T* res = static_cast<const T*>(p.residual);
     const T* w = static_cast<const T*>(p.w);
@@ -464,7 +534,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
                 ss = fmaf(v, v, ss);
                 top = max(top, magnitude(kMode == ROW_NORM_Q8 ? v * Elem<T>::get(w[c]) : v));
             }
-            g.sum_and_max(ss, top);
+            g.sum_and_max<true>(ss, top);
         };
         measure();
         float r = 1.f;
@@ -473,7 +543,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
                 uint32_t big = 0;
                 float none = 0.f;
                 for (int c = g.rank; c < p.C; c += g.size) big = max(big, magnitude(value(c)));
-                g.sum_and_max(none, big);
+                g.sum_and_max<true>(none, big);
                 s = row_rescale(big, p.eps);
                 measure();
             }
@@ -509,11 +579,10 @@ struct GradParams {
 
 template <class T, int V, bool kWhole, int kConsumers>
 __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) row_grad_kernel(const GradParams p, const Pipe q) {
-    constexpr int E = Chunk<T>::E;
+    constexpr int P = Chunk<T>::P;
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ PipeShared sh;
-    constexpr int consumers = kConsumers;
-    const int groups = consumers / q.group;
+    const int consumers = int(blockDim.x) - 32, groups = consumers / q.group;
     pipe_begin(sh, q.stages, consumers / 32);
     grid_dependency_wait();
     grid_dependents_launch();
@@ -527,101 +596,137 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
         }
         return;
     }
-    Group g{q.group, int(threadIdx.x) % q.group, int(threadIdx.x) / q.group, sh.words};
-    const Place<T, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
+    Group g(q.group, sh.words);
+    const Place<T, V, kWhole> at(p.C, q.group, g.rank, size_t(blockIdx.x) * q.per_group * groups + g.index);
     Chunk<T> weight[V];
-    float dw[V][E], we = 0.f, dwe = 0.f;
+    float2 dw[V][P];
+    float we = 0.f, dwe = 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
 #pragma unroll
-        for (int j = 0; j < E; ++j) dw[i][j] = 0.f;
+        for (int j = 0; j < P; ++j) dw[i][j] = both(0.f);
         if (at.live(i)) weight[i] = at.weights(static_cast<const T*>(p.w), i);
     }
     if (at.has_edge()) we = Elem<T>::get(static_cast<const T*>(p.w)[at.edge]);
     const float mean = 1.f / float(p.C);
     const int slots = (dh ? 3 : 2) * q.slot, rows_per_set = q.per_group * groups;
+    const size_t size = size_t(p.N) * p.C * sizeof(T);
     bool ok = true;
-    int n = 0;
+    int stage = 0;
+    uint32_t phase = 0;
     auto factor = [&](int s) {                                 // rstd of the group's first row of set s
         const int row = s * rows_per_set + g.index;
         return s < q.sets && row < p.N ? p.rstd[row] : 0.f;
     };
     float next = factor(blockIdx.x);
-    for (int s = blockIdx.x; s < q.sets; s += gridDim.x, ++n) {
-        const int stage = n % q.stages;
-        const Set o = rows_of<T>(s, rows_per_set, p.N, p.C);
+    for (int s = blockIdx.x; s < q.sets; s += gridDim.x) {
         float r = next;
         next = factor(s + gridDim.x);
-        ok = ok && bounded_wait(&sh.full[stage], (n / q.stages) & 1, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
+        ok = ok && bounded_wait(&sh.full[stage], phase, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
         const uint8_t* slot = ring + size_t(stage) * slots;
         for (int k = 0; k < q.per_group; ++k) {
-            const int row = o.first + k * groups + g.index;
-            if (row >= o.first + o.rows) break;                // (of the whole group)
+            const int n = k * groups + g.index, row = s * rows_per_set + n;
+            if (row >= p.N) break;                             // (of the whole group)
             if (k > 0) r = p.rstd[row];
+            const uint8_t* from = slot + row_start<T, kWhole>(s, rows_per_set, n, p.C);
             const size_t begin = size_t(row) * p.C;
-            float dot = 0.f, ne = 0.f, ge = 0.f;
+            // dot = sum of g h = sum of dy w h;  dw += r dy h
+            float2 sum = both(0.f);
+            float xe = 0.f, ye = 0.f;
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (!at.live(i)) continue;
-                float x[E], y[E], wf[E];
-                slot_chunk<T>(slot, o, begin + at.column(i)).values(x);
-                slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(y);
+                float2 x[P], y[P], wf[P];
+                load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
+                load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
                 weight[i].values(wf);
 #pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const float t = x[j] * r * y[j];           // dy n
-                    dw[i][j] += t;
-                    dot = fmaf(t, wf[j], dot);
+                for (int j = 0; j < P; ++j) {
+                    const float2 t = mul2(mul2(x[j], both(r)), y[j]);
+                    dw[i][j] = add2(dw[i][j], t);
+                    sum = fma2(t, wf[j], sum);
                 }
             }
+            float dot = sum.x + sum.y;
             if (at.has_edge()) {
-                ne = slot_element(slot, o, h, begin + at.edge) * r;
-                ge = slot_element(slot + q.slot, o, dy, begin + at.edge);
-                dwe += ne * ge;
-                dot = fmaf(ne * ge, we, dot);
-                ge *= we;
+                xe = slot_element(from, at.edge * sizeof(T), size, h, begin + at.edge) * r;
+                ye = slot_element(from + q.slot, at.edge * sizeof(T), size, dy, begin + at.edge);
+                dwe += xe * ye;
+                dot = fmaf(xe * ye, we, dot);
+                ye *= we;
             }
             dot = g.sum(dot) * mean;
+            const float2 rr = both(r), minus = both(-dot);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 if (!at.live(i)) continue;
-                float x[E], y[E], wf[E], d[E];
-                slot_chunk<T>(slot, o, begin + at.column(i)).values(x);
-                slot_chunk<T>(slot + q.slot, o, begin + at.column(i)).values(y);
-                if (dh) slot_chunk<T>(slot + 2 * q.slot, o, begin + at.column(i)).values(d);
+                float2 x[P], y[P], wf[P], d[P];
+                load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
+                load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
+                if (dh) load_chunk<T>(from + 2 * q.slot + at.column(i) * int(sizeof(T))).values(d);
                 weight[i].values(wf);
 #pragma unroll
-                for (int j = 0; j < E; ++j) d[j] = fmaf(r, fmaf(x[j] * r, -dot, y[j] * wf[j]), dh ? d[j] : 0.f);
+                for (int j = 0; j < P; ++j) {
+                    const float2 t = fma2(mul2(x[j], rr), minus, mul2(y[j], wf[j]));
+                    d[j] = fma2(rr, t, dh ? d[j] : both(0.f));
+                }
                 if (ok) store_chunk(static_cast<T*>(p.dx) + (begin + at.column(i)), d);
             }
             if (at.has_edge() && ok) {
-                const float d = dh ? slot_element(slot + 2 * q.slot, o, dh, begin + at.edge) : 0.f;
-                static_cast<T*>(p.dx)[begin + at.edge] = Elem<T>::put(fmaf(r, fmaf(ne, -dot, ge), d));
+                const float d = dh ? slot_element(from + 2 * q.slot, at.edge * sizeof(T), size, dh, begin + at.edge) : 0.f;
+                static_cast<T*>(p.dx)[begin + at.edge] = Elem<T>::put(fmaf(r, fmaf(xe, -dot, ye), d));
             }
         }
         __syncwarp();
         if ((threadIdx.x & 31) == 0) mbar_arrive(&sh.empty[stage]);          // the slot is read
+        if (++stage == q.stages) { stage = 0; phase ^= 1u; }
     }
     if (!p.parts) return;
-    // the groups' sums in the groups' order (in the ring, which is free now), then the block's to its row of the parts
+    // the sums of a warp's groups (rows of whole chunks, so all have the same columns), then those of the block's warps or groups in their order
+    // (in the ring, which is free now), then the block's to its row of the parts
+    __syncwarp();
+    int turns = groups, my_turn = g.index;
+    if (kWhole && q.group < 32) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                for (int o = q.group; o < 32; o <<= 1) {
+                    dw[i][j].x += __shfl_xor_sync(0xffffffffu, dw[i][j].x, o);
+                    dw[i][j].y += __shfl_xor_sync(0xffffffffu, dw[i][j].y, o);
+                }
+        turns = consumers / 32;
+        my_turn = int(threadIdx.x & 31) < q.group ? int(threadIdx.x) >> 5 : -1;
+    }
     float* part = p.parts + size_t(blockIdx.x) * p.C;
     float* merged = reinterpret_cast<float*>(ring);
-    for (int t = 0; t < groups; ++t) {
-        if (groups > 1) named_barrier_sync(15, consumers);
-        if (t != g.index) continue;
-        auto put = [&](int c, float v) {
-            if (groups == 1) part[c] = v;
-            else merged[c] = t == 0 ? v : merged[c] + v;
-        };
+    for (int t = 0; t < turns; ++t) {
+        if (turns > 1) named_barrier_sync(15, consumers);
+        if (t != my_turn) continue;
+        float* to = turns == 1 ? part : merged;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             if (!at.live(i)) continue;
+            if (kWhole) {                                      // (16 bytes at a time: single stores a chunk apart write each sector eight times)
 #pragma unroll
-            for (int j = 0; j < E; ++j) put(at.column(i) + j, dw[i][j]);
+                for (int j = 0; j < P; j += 2) {
+                    float4* f = reinterpret_cast<float4*>(to + at.column(i) + 2 * j);
+                    float4 v = make_float4(dw[i][j].x, dw[i][j].y, dw[i][j + 1].x, dw[i][j + 1].y);
+                    if (t > 0) { const float4 u = *f; v = make_float4(u.x + v.x, u.y + v.y, u.z + v.z, u.w + v.w); }
+                    *f = v;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    float* f = to + at.column(i) + 2 * j;
+                    f[0] = t == 0 ? dw[i][j].x : f[0] + dw[i][j].x;
+                    f[1] = t == 0 ? dw[i][j].y : f[1] + dw[i][j].y;
+                }
+            }
         }
-        if (at.has_edge()) put(at.edge, dwe);
+        if (at.has_edge()) to[at.edge] = t == 0 ? dwe : to[at.edge] + dwe;
     }
-    if (groups > 1) {
+    if (turns > 1) {
         named_barrier_sync(15, consumers);
         for (int c = threadIdx.x; c < p.C; c += consumers) part[c] = merged[c];
     }
@@ -629,8 +734,8 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
 
 template <class T>
 __global__ void __launch_bounds__(1024) long_row_grad_kernel(const GradParams p) {
-    __shared__ float2 words[64];
-    Group g{int(blockDim.x), int(threadIdx.x), 0, words};
+    __shared__ float words[128];
+    Group g(int(blockDim.x), words);
     const T* h = static_cast<const T*>(p.h);
     const T* w = static_cast<const T*>(p.w);
     const T* dy = static_cast<const T*>(p.dy);
@@ -657,8 +762,8 @@ __global__ void __launch_bounds__(1024) long_row_grad_kernel(const GradParams p)
     }
 }
 
-// dw[c] = the sum of the parts' column c, in their order: a warp's lanes take 32 columns, its block's warps every 16th part.
-constexpr int kSumWarps = 16;
+// dw[c] = the sum of the parts' column c: a warp's lanes take 32 columns, its block's warps every 32nd part.
+constexpr int kSumWarps = 32;
 template <class T>
 __global__ void __launch_bounds__(kSumWarps * 32) sum_parts_kernel(const float* parts, int rows, int C, T* dw) {
     __shared__ float sums[kSumWarps][32];
@@ -677,28 +782,35 @@ __global__ void __launch_bounds__(kSumWarps * 32) sum_parts_kernel(const float* 
     }
 }
 
-constexpr int kMostParts = 296;              // blocks of the gradient
+// Blocks of the gradient: each leaves a row of sums, which costs a short call more than half of the SMs' second block gains (512 x 4096: 13.9 us
+// with two, 9.4 with one).
+int grad_blocks(int N) { const int sms = device_sm_count(); return N < sms ? N : N < 8 * sms ? sms : 2 * sms; }
 constexpr int kFewRows = 2;
 constexpr int kMostRing = 216 * 1024;        // of all blocks of an SM
 
 // (of whole chunks; a row shorter than one has one all the same)
 int row_chunks(int C, int E) { return C < E ? 1 : C / E; }
 
-// A thread takes 16 elements of a row, 32 in rows that 512 threads would not cover, fewer in rows that need no 32; groups of 32 to 512 threads
-// follow from that.
+// A thread takes 16 elements of a row, 32 in rows that 512 threads would not cover; a chunk in rows that 32 lanes cover then.  Groups follow from
+// that: whole warps, or, for short rows of whole chunks, 4, 8 or 16 lanes (32768 x 64 bf16 with a residual, 8 lanes: 11.0 -> 4.8 us).
 template <class T> constexpr int kMostV = 32 / Chunk<T>::E;
 template <class T> bool too_long(int C) { return row_chunks(C, Chunk<T>::E) > kPipeMost * kMostV<T>; }
 template <class T>
-struct PipeShape { Pipe q; int v, groups, consumers, grid; size_t smem; };
+struct PipeShape { Pipe q; int v, groups, consumers, grid; bool whole; size_t smem; };
 template <class T>
-int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int most_blocks, int blocks_per_sm) {
+int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int threads, int blocks_per_sm) {
     constexpr int E = Chunk<T>::E;
     const int chunks = row_chunks(C, E), sms = device_sm_count();
     o.v = chunks <= 32 ? 1 : chunks <= 64 ? 2 : chunks <= kPipeMost * kMostV<T> / 2 ? kMostV<T> / 2 : kMostV<T>;
-    o.q.group = 32;
-    while (o.q.group * o.v < chunks) o.q.group *= 2;
-    o.consumers = o.q.group > 256 ? o.q.group : 256;
-    o.groups = o.consumers / o.q.group;
+    o.q.group = ((chunks + o.v - 1) / o.v + 31) / 32 * 32;
+    // a warp less, where it leaves no more than an element for each thread (3001 x 1037 fp16 to 8 bits, 64 threads instead of 96: 11.6 -> 7.9 us)
+    const int less = o.q.group - 32;
+    if (less >= 32 && (chunks - o.v * less) * E + (C % E ? 2 * (E - 1) : 0) <= less) o.q.group = less;
+    o.whole = C % E == 0 && o.v * o.q.group >= chunks;
+    if (C % E == 0)
+        while (o.q.group <= 32 && o.q.group > 4 && o.q.group / 2 >= chunks) o.q.group /= 2;
+    o.groups = o.q.group > threads ? 1 : threads / o.q.group;
+    o.consumers = o.groups * o.q.group;
     const size_t row = size_t(C) * sizeof(T);
     // several rows to a group where they are short (and where a group's rows still start alike)
     int m = 1;
@@ -716,8 +828,8 @@ int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int most_blocks, int 
     o.q.stages = int(stages < size_t(kMostStages) ? stages : kMostStages);
     o.smem = stage * o.q.stages;
     o.grid = sms * (room == kMostRing ? 1 : blocks_per_sm);
-    if (o.grid > most_blocks) o.grid = most_blocks;
-    const int unit = C % E == 0 || rows >= E ? 1 : E / rows;    // (a group's rows are a multiple of E apart)
+    int unit = 1;
+    while (C % E != 0 && rows * unit % E != 0) unit *= 2;       // (a group's rows are a multiple of E apart)
     o.grid = o.grid / unit * unit;
     if (o.grid > o.q.sets) o.grid = o.q.sets;
     o.q.status = device_status_ptr();
@@ -738,7 +850,7 @@ int launch_pipe(const RowParams& p, const PipeShape<T>& o, cudaStream_t st) {
     };
     static PerDeviceOnce once256, once512;
     if constexpr (V * Chunk<T>::E <= 16)
-        if (o.consumers == 256) return launch(once256, row_pipe_kernel<T, V, kMode, kWhole, 256>);
+        if (o.consumers <= 256) return launch(once256, row_pipe_kernel<T, V, kMode, kWhole, 256>);
     if constexpr (V * Chunk<T>::E >= 16) return launch(once512, row_pipe_kernel<T, V, kMode, kWhole, 512>);
     return PCL_ERR_UNSUPPORTED_SHAPE;                          // (not reached: fewer than 16 elements a thread are groups of 32)
 }
@@ -763,10 +875,9 @@ int launch_rows(const RowParams& p, cudaStream_t st) {
         return PCL_ERR_UNSUPPORTED_SHAPE;                      // (not reached: longer 16-bit rows are walked over twice)
     }
     PipeShape<T> o;
-    const int rc = pipe_shape(o, p.N, p.C, kMode != ROW_QUANTIZE && p.residual ? 2 : 1, INT_MAX, 3);
+    const int rc = pipe_shape(o, p.N, p.C, kMode != ROW_QUANTIZE && p.residual ? 2 : 1, 256, 3);
     if (rc != PCL_OK) return rc;
-    const bool whole = p.C % E == 0;
-#define PCL_ROWS(V_) return whole ? launch_pipe<T, V_, kMode, true>(p, o, st) : launch_pipe<T, V_, kMode, false>(p, o, st)
+#define PCL_ROWS(V_) return o.whole ? launch_pipe<T, V_, kMode, true>(p, o, st) : launch_pipe<T, V_, kMode, false>(p, o, st)
     if (o.v == 1) PCL_ROWS(1);
     if (o.v == 2) PCL_ROWS(2);
     if (o.v == 4) PCL_ROWS(4);
@@ -785,30 +896,36 @@ int launch_rows_of(int type, const RowParams& p, cudaStream_t st) {
 
 template <class T, int V, bool kWhole>
 int launch_grad_pipe(const GradParams& p, const PipeShape<T>& o, cudaStream_t st) {
-    const size_t merged = o.groups > 1 ? size_t(p.C) * 4 : 0, smem = o.smem > merged ? o.smem : merged;
+    const size_t merged = o.consumers / 32 > 1 ? size_t(p.C) * 4 : 0, smem = o.smem > merged ? o.smem : merged;
     auto launch = [&](PerDeviceOnce& once, auto kernel) {
         const int rc = allow_smem(once, kernel);
         return rc != PCL_OK ? rc : launch_chained(kernel, dim3(o.grid), dim3(o.consumers + 32), smem, st, 1, p, o.q);
     };
     static PerDeviceOnce once256, once512;
     if constexpr (V * Chunk<T>::E <= 16)
-        if (o.consumers == 256) return launch(once256, row_grad_kernel<T, V, kWhole, 256>);
+        if (o.consumers <= 256) return launch(once256, row_grad_kernel<T, V, kWhole, 256>);
     if constexpr (V * Chunk<T>::E >= 16) return launch(once512, row_grad_kernel<T, V, kWhole, 512>);
     return PCL_ERR_UNSUPPORTED_SHAPE;
 }
 template <class T>
 int launch_grad(const GradParams& p, void* dw, cudaStream_t st) {
     constexpr int E = Chunk<T>::E;
+    const int sms = device_sm_count();
     int grid, rc;
     if (too_long<T>(p.C)) {
-        grid = p.N < kMostParts ? p.N : kMostParts;
+        grid = grad_blocks(p.N);
         rc = launch_chained(long_row_grad_kernel<T>, dim3(grid), dim3(1024), 0, st, 1, p);
     } else {
         PipeShape<T> o;
-        rc = pipe_shape(o, p.N, p.C, p.dh ? 3 : 2, kMostParts, 2);
+        const bool few = grad_blocks(p.N) <= sms && row_chunks(p.C, E) > 64;
+        rc = pipe_shape(o, p.N, p.C, p.dh ? 3 : 2, few ? 512 : 256, few ? 1 : 2);
         if (rc != PCL_OK) return rc;
+        int unit = 1;
+        while (p.C % E != 0 && o.q.per_group * o.groups * unit % E != 0) unit *= 2;
+        grid = grad_blocks(p.N) / unit * unit;
+        if (o.grid > grid && grid > 0) o.grid = grid;
         grid = o.grid;
-        const bool whole = p.C % E == 0;
+        const bool whole = o.whole;
         if (o.v == 1) rc = whole ? launch_grad_pipe<T, 1, true>(p, o, st) : launch_grad_pipe<T, 1, false>(p, o, st);
         else if (o.v == 2) rc = whole ? launch_grad_pipe<T, 2, true>(p, o, st) : launch_grad_pipe<T, 2, false>(p, o, st);
         else if (o.v == 4) rc = whole ? launch_grad_pipe<T, 4, true>(p, o, st) : launch_grad_pipe<T, 4, false>(p, o, st);
@@ -821,7 +938,7 @@ int launch_grad(const GradParams& p, void* dw, cudaStream_t st) {
 
 }  // namespace
 
-size_t rms_norm_workspace_bytes(int N, int C) { return align_up(size_t(N < kMostParts ? N : kMostParts) * C * 4, 256); }
+size_t rms_norm_workspace_bytes(int N, int C) { return align_up(size_t(grad_blocks(N)) * align_up(C, 4) * 4, 256); }
 
 int launch_rms_norm_fwd(int N, int C, int type, const void* x, const void* residual, const void* w, float eps, void* h, void* y,
                         float* scale, float* rstd, cudaStream_t st) {
