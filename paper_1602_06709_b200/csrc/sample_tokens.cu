@@ -101,10 +101,16 @@ template <class T>
 struct Row {
     static constexpr int E = Vec<T>::E;
     const T* base;                           // the row's first element
-    int K, shift, vectors;
+    const uint4* aligned;                    // vector 0
+    int K, shift, vectors, first_whole;
+    unsigned whole;                          // vectors that are the row's altogether, from first_whole on
     __device__ __forceinline__ Row(const void* logits, size_t row, int k) : base(static_cast<const T*>(logits) + row * k), K(k) {
         shift = int(row * k % E);
         vectors = (K + shift + E - 1) / E;
+        aligned = reinterpret_cast<const uint4*>(base - shift);
+        first_whole = shift ? 1 : 0;
+        const int last = (K + shift) % E ? vectors - 1 : vectors;
+        whole = last > first_whole ? unsigned(last - first_whole) : 0u;
     }
     __device__ __forceinline__ float value(int id) const {
         const uint32_t u[4] = {Vec<T>::load(base, id), 0u, 0u, 0u};
@@ -112,11 +118,11 @@ struct Row {
     }
     __device__ __forceinline__ long first(int c) const { return long(c) * E - shift; }
     __device__ __forceinline__ void load(int c, uint32_t (&u)[4]) const {
-        const long e = first(c);
-        if (e >= 0 && e + E <= K) {
-            const uint4 q = __ldg(reinterpret_cast<const uint4*>(base + e));
+        if (unsigned(c - first_whole) < whole) {
+            const uint4 q = __ldg(aligned + c);
             u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w;
         } else {
+            const long e = first(c);
 #pragma unroll
             for (int i = 0; i < 4; ++i) u[i] = Vec<T>::kLeast;
 #pragma unroll
@@ -124,17 +130,35 @@ struct Row {
                 if (e + i >= 0 && e + i < K) Vec<T>::put(u, i, Vec<T>::load(base, e + i));
         }
     }
+    __device__ __forceinline__ void load_whole(int c, uint32_t (&u)[4]) const {
+        const uint4 q = __ldg(aligned + c);
+        u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w;
+    }
     // f(vector, its index) for every vector, the block's threads side by side; kMany vectors are loaded before the first is used
     template <int kMany, class F>
     __device__ __forceinline__ void each(F&& f) const {
-        for (int c = threadIdx.x; c < vectors; c += kMany * int(blockDim.x)) {
-            uint32_t u[kMany][4];
+        const int n = int(blockDim.x), end = first_whole + int(whole);
+        int c = first_whole + int(threadIdx.x);
+        uint32_t u[kMany][4];
+        for (; c + (kMany - 1) * n < end; c += kMany * n) {
 #pragma unroll
-            for (int m = 0; m < kMany; ++m)
-                if (c + m * int(blockDim.x) < vectors) load(c + m * int(blockDim.x), u[m]);
+            for (int m = 0; m < kMany; ++m) load_whole(c + m * n, u[m]);
 #pragma unroll
-            for (int m = 0; m < kMany; ++m)
-                if (c + m * int(blockDim.x) < vectors) f(u[m], c + m * int(blockDim.x));
+            for (int m = 0; m < kMany; ++m) f(u[m], c + m * n);
+        }
+#pragma unroll
+        for (int m = 0; m < kMany - 1; ++m)
+            if (c + m * n < end) load_whole(c + m * n, u[m]);
+#pragma unroll
+        for (int m = 0; m < kMany - 1; ++m)
+            if (c + m * n < end) f(u[m], c + m * n);
+        // the row's first and last vector, where they are not whole
+        if (threadIdx.x < 2) {
+            c = threadIdx.x ? vectors - 1 : 0;
+            if ((c < first_whole || c >= end) && (threadIdx.x == 0 || vectors > 1)) {
+                load(c, u[0]);
+                f(u[0], c);
+            }
         }
     }
 };
@@ -152,7 +176,12 @@ __device__ __forceinline__ float unorder(uint32_t k) { return __uint_as_float(k 
 struct Scale {
     double top, per16;                       // the row's maximum, 16 log2(e) / temperature
     unsigned lowest;                         // first word of -768 / per16: 2^-48, which is 0 in the result
-    const double* table;                     // 2^(i/16) * 2^bits, its exponent less by i/16 of a power of two
+    uint32_t table;                          // (shared memory) 2^(i/16) * 2^bits, its exponent less by i/16 of a power of two
+    __device__ __forceinline__ double root(int i) const {
+        double v;
+        asm("ld.shared.f64 %0, [%1];" : "=d"(v) : "r"(table + (i & 15) * 8));
+        return v;
+    }
     __device__ __forceinline__ double x(float z) const { return (double(z) - top) * per16; }
     // keep = false: 0.  (Not of +inf; what is not kept may be -inf or NaN.)
     __device__ __forceinline__ u64 weight(float z, bool keep = true) const {
@@ -167,9 +196,48 @@ struct Scale {
         p = fma(r, p, 0x1.ebfbdff6988c8p-11);
         p = fma(r, p, 0x1.62e42fefa39efp-5);
         p = fma(r, p, 1.0);
-        const double s = table[i & 15];
+        const double s = root(i);
         const double w = fma(__hiloint2double(__double2hiint(s) + (i << 16), __double2loint(s)), p, 4503599627370496.0);
         return u64(__double_as_longlong(w)) - 0x4330000000000000ull;
+    }
+    // The sum of the weights of N values (kAll: of all of them, -inf among them; else of those not below `from`), step by step for all of them: their
+    // chains of dependent operations run side by side.
+    template <int N, bool kAll>
+    __device__ __forceinline__ u64 sum(const float (&z)[N], float from) const {
+        double d[N], r[N], p[N];
+        int i[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) d[n] = double(z[n]) - top;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const unsigned hi = min(unsigned(__double2hiint(d[n])), lowest);
+            d[n] = __hiloint2double(int(kAll || z[n] >= from ? hi : lowest), __double2loint(d[n]));
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const double t = fma(d[n], per16, 6755399441055744.0);
+            i[n] = __double2loint(t);
+            r[n] = 6755399441055744.0 - t;
+        }
+#pragma unroll
+        for (int n = 0; n < N; ++n) r[n] = fma(d[n], per16, r[n]);
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = fma(r[n], 0x1.5d893e58acc63p-30, 0x1.3b2c4ac7da565p-23);
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 0x1.c6b08d6faa1bep-17);
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 0x1.ebfbdff6988c8p-11);
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 0x1.62e42fefa39efp-5);
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 1.0);
+        u64 total = 0;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const double s = root(i[n]);
+            total += u64(__double_as_longlong(fma(__hiloint2double(__double2hiint(s) + (i[n] << 16), __double2loint(s)), p[n], 4503599627370496.0)));
+        }
+        return total - N * 0x4330000000000000ull;
     }
 };
 
@@ -261,28 +329,62 @@ __device__ __forceinline__ void find_bin(Shared& s, u64 want) {
     __syncthreads();
 }
 
-// Sums of f(value, id) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece (kAdd:
-// added to it).
+// Sums of f(vector, its index) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece
+// (kAdd: added to it).  The next vector is on its way while one is worked on.
 template <int kThreads, bool kAdd = false, class T, class F>
 __device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0, int c1, int each, F&& f) {
-    constexpr int E = Vec<T>::E;
     const int lane = threadIdx.x & 31, pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
-    for (int q = threadIdx.x >> 5; q < pieces; q += kThreads / 32) {
-        u64 sum = 0;
-        for (int o = 0; o < each; ++o) {
-            const int c = c0 + (q * each + o) * 32 + lane;
-            if (c >= c1) break;
-            uint32_t u[4];
-            row.load(c, u);
-            const int id = int(row.first(c));
+    int q = threadIdx.x >> 5, o = 0, c = c0 + q * each * 32 + lane;
+    u64 sum = 0;
+    uint32_t u[4], next[4];
+    if (c < c1) row.load(c, next);
+    while (q < pieces) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) sum += f(Vec<T>::get(u, i), id + i);
+        for (int i = 0; i < 4; ++i) u[i] = next[i];
+        const int at = c;
+        const bool last = ++o == each;
+        const int done = q;
+        if (last) {
+            o = 0;
+            q += kThreads / 32;
+            c = c0 + q * each * 32 + lane;
+        } else {
+            c += 32;
         }
-        __syncwarp();
-        sum = warp_sum(sum);
-        if (lane == 0) s.piece[q] = kAdd ? s.piece[q] + sum : sum;
+        if (c < c1) row.load(c, next);
+        if (at < c1) sum += f(u, at);
+        if (last) {
+            __syncwarp();
+            sum = warp_sum(sum);
+            if (lane == 0) s.piece[done] = kAdd ? s.piece[done] + sum : sum;
+            sum = 0;
+        }
     }
     __syncthreads();
+}
+// f of values and ids, one by one, as a function of a vector.
+template <class T, class F>
+__device__ __forceinline__ auto by_value(const Row<T>& row, F&& f) {
+    return [&row, f](const uint32_t (&u)[4], int c) mutable -> u64 {
+        const int id = int(row.first(c));
+        u64 sum = 0;
+#pragma unroll
+        for (int i = 0; i < Vec<T>::E; ++i) sum += f(Vec<T>::get(u, i), id + i);
+        return sum;
+    };
+}
+// The weights of the values not below `from` (kAll: of all).
+template <bool kAll, class T>
+__device__ __forceinline__ u64 vector_weight(const Scale& sc, const uint32_t (&u)[4], float from) {
+    u64 sum = 0;
+#pragma unroll
+    for (int i = 0; i < Vec<T>::E; i += 4) {
+        float z[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = Vec<T>::get(u, i + j);
+        sum += sc.sum<4, kAll>(z, from);
+    }
+    return sum;
 }
 // The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the whole row.
 template <int kThreads, class T, class F>
@@ -302,7 +404,7 @@ __device__ __forceinline__ int locate(Shared& s, const Row<T>& row, int each, u6
         front = s.found_front;
         if (each <= 8) break;
         each = (each + kPieces - 1) / kPieces;                 // (long rows: the piece in pieces)
-        sum_pieces<kThreads>(s, row, c0, c1, each, f);
+        sum_pieces<kThreads>(s, row, c0, c1, each, by_value(row, f));
     }
     if (threadIdx.x < 32) {                                    // a warp, 32 vectors at a time
         for (int c = c0 + threadIdx.x; c - int(threadIdx.x) < c1; c += 32) {
@@ -476,15 +578,30 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
         if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(id));
     };
     u64 above = 0;
-    sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float z, int id) -> u64 {
-        const float b = (top - z) * scale;
-        const u64 w = sc.weight(z, b < begin);
-        above += w;
-        if (b >= begin && b < end && z >= from) {
-            push(z, id);
-            atomicAdd(&s.fine[fine_bin(b)], 1u);
+    sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&u)[4], int c) -> u64 {
+        u64 sum = 0;
+        const int id = int(row.first(c));
+#pragma unroll
+        for (int i = 0; i < E; i += 4) {
+            float z[4], kept[4];
+            bool any = false;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float v = Vec<T>::get(u, i + j), b = (top - v) * scale;
+                z[j] = b < begin ? v : -INFINITY;
+                kept[j] = v >= least ? z[j] : -INFINITY;
+                any |= b < begin;
+                if (b >= begin && b < end && v >= from) {
+                    push(v, id + i + j);
+                    atomicAdd(&s.fine[fine_bin(b)], 1u);
+                }
+            }
+            if (!__any_sync(__activemask(), any)) continue;
+            const u64 w = sc.sum<4, true>(z, 0.f);
+            above += w;
+            sum += least > from ? sc.sum<4, true>(kept, 0.f) : w;      // (min-p above what top-p can keep)
         }
-        return z >= least ? w : 0ull;
+        return sum;
     });
     above = block_sum<kThreads>(s, above);
     if (s.listed > kList) {
@@ -494,7 +611,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
         if (first_fine > last_fine) return false;
         __syncthreads();
         u64 more = 0;
-        sum_pieces<kThreads, true>(s, row, 0, row.vectors, each, [&](float z, int id) -> u64 {
+        sum_pieces<kThreads, true>(s, row, 0, row.vectors, each, by_value(row, [&](float z, int id) -> u64 {
             const float b = (top - z) * scale;
             u64 w = 0;
             if (b >= begin && b < end && z >= from) {
@@ -504,7 +621,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
             }
             more += w;
             return z >= least ? w : 0ull;
-        });
+        }));
         above += block_sum<kThreads>(s, more);
         if (s.listed > kList) return false;
     }
@@ -581,7 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         return;
     }
     const double per16 = fmax(16.0 * 1.4426950408889634074 / double(temperature), 1e-290);         // (an infinite temperature: all weights 1)
-    const Scale sc{double(top), per16, unsigned(__double2hiint(-768.0 / per16)), s.table};
+    const Scale sc{double(top), per16, unsigned(__double2hiint(-768.0 / per16)), smem_u32(s.table)};
     const bool infinite = top == INFINITY, by_p = top_p < 1.f;
     auto target_of = [&](u64 total) -> u64 {
         const u64 t = u > 0.f ? u64(double(fminf(u, 1.f - 0x1p-24f)) * double(total)) : 0ull;
@@ -701,7 +818,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
     auto nth_of = [&](float z, uint32_t ties) {                // the border at that many tokens of value z
-        sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
+        sum_pieces<kThreads>(s, row, 0, row.vectors, each, by_value(row, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; }));
         const int id = locate<kThreads>(s, row, each, u64(ties) - 1, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
         __syncthreads();
         return Border{z, id};
@@ -723,13 +840,16 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (k > 0 && select<kThreads, false>(s, row, sc, top, floor_z, u64(k), z, ties)) border = nth_of(z, ties);     // (else fewer have any weight)
         if (by_p) {
             u64 sum = 0;
-            row.template each<2>([&](uint32_t (&q)[4], int c) {
+            if (k == 0)
+                row.template each<2>([&](uint32_t (&q)[4], int) { sum += vector_weight<true, T>(sc, q, 0.f); });
+            else
+                row.template each<2>([&](uint32_t (&q)[4], int c) {
 #pragma unroll
-                for (int i = 0; i < E; ++i) {
-                    const float v = Vec<T>::get(q, i);
-                    sum += sc.weight(v, k > 0 ? border.keeps(v, int(row.first(c)) + i) : v >= kLowest);
-                }
-            });
+                    for (int i = 0; i < E; ++i) {
+                        const float v = Vec<T>::get(q, i);
+                        sum += sc.weight(v, border.keeps(v, int(row.first(c)) + i));
+                    }
+                });
             sum = block_sum<kThreads>(s, sum);
             // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
             const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
@@ -750,10 +870,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto kept_weight = [&](float v, int id) -> u64 { return infinite ? border.keeps(v, id) ? one : 0ull : sc.weight(v, border.keeps(v, id)); };
     if (!summed) {
         __syncthreads();
-        if (!infinite && border.id == kAllIds)
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](float v, int) -> u64 { return sc.weight(v, v >= border.z); });
+        if (infinite || border.id != kAllIds)
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, by_value(row, kept_weight));
+        else if (border.z > kLowest)
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&q)[4], int) { return vector_weight<false, T>(sc, q, border.z); });
         else
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, kept_weight);
+            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&q)[4], int) { return vector_weight<true, T>(sc, q, 0.f); });
     }
     const u64 total = block_sum<kThreads>(s, int(threadIdx.x) < (row.vectors + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
     const int token = locate<kThreads>(s, row, each, target_of(total), kept_weight);
