@@ -12,8 +12,8 @@
 //   Every row: the maximum, two 16-bit logits to an instruction.
 //   Small top-k: the k-th largest of the threads' maxima is a bound that k tokens reach and few others; those go to a list in shared memory,
 //     and everything else happens there, by comparing all pairs.
-//   Top-p alone: a histogram of counts over z (of the tokens whose weight is not below (1 - top_p) / K of the total; the others together do not
-//     reach what top-p leaves out) says in which few bins the part kept ends; their tokens go to the list.
+//   Top-p alone: a histogram over z says in which few bins the part kept ends, one pass takes the exact weights, and those bins' tokens go to the
+//     list, where the exact border is found.
 //   Whatever does not fit in the list: the value at the border is found by histograms of weights or counts, finer each time.
 //   What is kept is summed by pieces of consecutive ids, and the piece in which the random number falls is searched.
 // The cost is the weights': one takes twelve operations in 64 bits, of which an SM does 64 a cycle, so a row that needs all of them takes three
@@ -30,7 +30,9 @@ namespace pcl {
 namespace {
 
 constexpr int kBins = 2048;
-constexpr int kList = 1024;                  // tokens of the list
+constexpr int kList = 4096;                  // tokens of the list
+constexpr int kMostSmall = 1024;             // of them, at most, where all of them are compared with all
+constexpr int kPairs = 512;                  // up to here they are compared pair by pair
 constexpr int kPieces = 256;                 // pieces of consecutive ids, at most
 constexpr int kWeightBits = 44;
 
@@ -201,10 +203,10 @@ struct Scale {
         const double w = fma(__hiloint2double(__double2hiint(s) + (i << 16), __double2loint(s)), p, 4503599627370496.0);
         return u64(__double_as_longlong(w)) - 0x4330000000000000ull;
     }
-    // The sum of the weights of N values (kAll: of all of them, -inf among them; else of those not below `from`), step by step for all of them: their
-    // chains of dependent operations run side by side.
+    // The weights of N values (kAll: of all of them, -inf among them; else of those not below `from`), step by step for all of them: their chains of
+    // dependent operations run side by side.  Each is 0x433 << 52 too large.
     template <int N, bool kAll>
-    __device__ __forceinline__ u64 sum(const float (&z)[N], float from) const {
+    __device__ __forceinline__ void raw_weights(const float (&z)[N], float from, u64 (&w)[N]) const {
         double d[N], r[N], p[N];
         int i[N];
 #pragma unroll
@@ -232,14 +234,13 @@ struct Scale {
         for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 0x1.62e42fefa39efp-5);
 #pragma unroll
         for (int n = 0; n < N; ++n) p[n] = fma(r[n], p[n], 1.0);
-        u64 total = 0;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             const double s = root(i[n]);
-            total += u64(__double_as_longlong(fma(__hiloint2double(__double2hiint(s) + (i[n] << 16), __double2loint(s)), p[n], 4503599627370496.0)));
+            w[n] = u64(__double_as_longlong(fma(__hiloint2double(__double2hiint(s) + (i[n] << 16), __double2loint(s)), p[n], 4503599627370496.0)));
         }
-        return total - N * 0x4330000000000000ull;
     }
+    static constexpr u64 kRaw = 0x4330000000000000ull;
 };
 
 struct Shared {
@@ -251,8 +252,8 @@ struct Shared {
     uint32_t warp_word[32];
     float warp_z[32];
     double warp_low[32], warp_high[32];
+    uint32_t warp_count[32];
     int bin, last_bin, listed, found, token, border_id;
-    uint32_t fine[kBins];                    // a second histogram, of counts
     u64 above, found_front;
     uint32_t key_lo, key_hi, ties;
     float border_z;
@@ -383,9 +384,11 @@ __device__ __forceinline__ u64 vector_weight(const Scale& sc, const uint32_t (&u
         float z[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[j] = Vec<T>::get(u, i + j);
-        sum += sc.sum<4, kAll>(z, from);
+        u64 w[4];
+        sc.template raw_weights<4, kAll>(z, from, w);
+        sum += (w[0] + w[1]) + (w[2] + w[3]);
     }
-    return sum;
+    return sum - Vec<T>::E * Scale::kRaw;
 }
 // The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the whole row.
 template <int kThreads, class T, class F>
@@ -483,7 +486,7 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
         __syncthreads();
         lo = s.key_lo; hi = s.key_hi;
         const int n = s.listed;
-        if (n <= kList || lo == hi) {
+        if (n <= kMostSmall || lo == hi) {
             // all pairs; a bin of one value is one pair
             for (int i = threadIdx.x; i < (lo == hi ? 1 : n); i += kThreads) {
                 const u64 mine = s.key[i];
@@ -510,140 +513,136 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
     }
 }
 
-// The bins of a histogram of counts in which the weight from the top, `above` and then that of the tokens of each bin, reaches `want`: the first
-// and the last that can be it go to s.bin and s.last_bin.  Bin b holds weights between 2^-(from + b * width) and a bin's width less, but for
-// `slack` of rounding (in powers of two) at its edges; the last bin may reach further down.
-template <int kThreads>
-__device__ __forceinline__ void find_bins(Shared& s, const uint32_t* count, double unit, double from, double width, double slack, double above, double want) {
-    constexpr int kEach = kBins / kThreads;
-    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; }
-    double low = 0.0, high = 0.0, lows[kEach], highs[kEach], all;
-    const double most = exp2(slack) * (1.0 + 1e-9), least = exp2(-width - slack) * (1.0 - 1e-9);
+// What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list.  Leaves the sums of what is
+// kept (and not below `least`) in s.piece, and the weight of the whole row in `total`.
+//   A histogram over z from the top down to `from` counts tokens and adds up their places in the bins (to a 64th of a bin), which gives the weight
+//   of each bin to 1 part in 4000; the border lies in the bins, one or two as a rule, where the weight up to there can be top_p of all.  One pass then
+//   takes the exact weights: of all tokens, of those above these bins, and those in them go to the list, where the exact border is found.
+constexpr int kCountBits = 13;               // of a bin's word; the rest holds the places
+template <int kThreads, class T, class Part>
+__device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, double unit, float top_p, float least, int each,
+                                        const Part& part_of, u64& total, Border& border) {
+    constexpr int E = Vec<T>::E, kEach = kBins / kThreads;
+    const float scale = float(kBins) / (top - from);
+    const bool usable = scale > 0.f && scale < 1e30f;
+    for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0;
+    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; s.listed = 0; s.border_id = -1; }
+    __syncthreads();
+    uint32_t inside = 0;
+    if (usable)
+        row.template each<4>([&](uint32_t (&u)[4], int) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float z = Vec<T>::get(u, i);
+                if (z >= from) {
+                    const int place = min(int((top - z) * (scale * 64.f)), kBins * 64 - 1);       // in 64ths of a bin
+                    atomicAdd(&s.count[place >> 6], 1u | uint32_t(place & 63) << kCountBits);
+                    ++inside;
+                }
+            }
+        });
+    __syncthreads();
+    // bounds of the weight up to each bin and of all of it: a token's place is known to 1/64 of a bin (and a rounding of 1/1000), and within a bin
+    // exp(-f * width) lies between 1 - f width and that plus (f width)^2 / 2
+    const double width = double(top - from) / kBins * sc.per16 * (0.69314718055994530942 / 16.0);       // of a bin, in nats
+    double low = 0.0, high = 0.0, lows[kEach], highs[kEach], all_low, all_high;
+    uint32_t counted = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int b = kEach * threadIdx.x + i;
-        const double at = count[b] ? double(count[b]) * unit * exp2(-(from + double(b) * width)) : 0.0;
-        lows[i] = b == kBins - 1 ? 0.0 : at * least;
-        highs[i] = at * most + double(count[b]);               // (weights are whole numbers)
-        low += fmax(lows[i] - double(count[b]), 0.0);
+        const uint32_t word = s.count[b], n = word & ((1u << kCountBits) - 1);
+        counted += n;
+        const double at = n ? unit * exp(-double(b) * width) : 0.0, places = double(word >> kCountBits) * (1.0 / 64.0) * width;
+        lows[i] = fmax(at * (double(n) - places - double(n) * width * (1.0 / 64.0 + 1e-3)) - double(n), 0.0);
+        highs[i] = at * (double(n) - places + double(n) * (width * 1e-3 + 0.5 * width * width)) + double(n);      // (weights are whole numbers)
+        if (b == kBins - 1) { lows[i] = 0.0; highs[i] = double(n) * (at * (1.0 + 1e-3 * width) + 1.0); }           // (the last bin may reach further down)
+        low += lows[i];
         high += highs[i];
     }
-    low = above + block_scan<kThreads>(s.warp_low, low, all) - low;
-    high = above + block_scan<kThreads>(s.warp_high, high, all) - high;
-    // (sums in an order of their own for each thread: 1e-12 apart)
+    low = block_scan<kThreads>(s.warp_low, low, all_low) - low;
+    high = block_scan<kThreads>(s.warp_high, high, all_high) - high;
+    uint32_t all_counted, all_inside;
+    block_scan<kThreads>(s.warp_word, counted, all_counted);
+    block_scan<kThreads>(s.warp_count, inside, all_inside);
+    if (!usable || all_counted != all_inside) return false;    // (a bin's count has overflown)
+    const double want_low = double(top_p) * all_low * (1.0 - 1e-9), want_high = double(top_p) * all_high * (1.0 + 1e-9) + 1.0;
     int first = kBins, last = kBins - 1;
     bool early = false, late = false;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         high += highs[i];
-        low += fmax(lows[i] - double(count[kEach * threadIdx.x + i]), 0.0);
-        if (!early && high * (1.0 + 1e-9) >= want) { first = kEach * threadIdx.x + i; early = true; }
-        if (!late && low * (1.0 - 1e-9) >= want) { last = kEach * threadIdx.x + i; late = true; }
+        low += lows[i];
+        if (!early && high * (1.0 + 1e-9) >= want_low) { first = kEach * threadIdx.x + i; early = true; }
+        if (!late && low * (1.0 - 1e-9) >= want_high) { last = kEach * threadIdx.x + i; late = true; }
     }
     first = __reduce_min_sync(0xffffffffu, first);
     last = __reduce_min_sync(0xffffffffu, last);
     if ((threadIdx.x & 31) == 0) { atomicMin(&s.bin, first); atomicMin(&s.last_bin, last); }
     __syncthreads();
-}
-
-// What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list.  Leaves the sums of what is
-// kept (and not below `least`) in s.piece.
-//   A histogram of counts over z from the top down to `from` bounds the weight up to each bin from both sides; the border lies in the bins in
-//   which the two bounds reach `want`.  What lies above them is summed exactly, their tokens go to the list, and the exact border is found there.
-//   If they do not fit, a finer histogram of those bins, taken in the same pass, narrows them down.
-template <int kThreads, class T>
-__device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, double unit, u64 want, float least, int each,
-                                        Border& border) {
-    constexpr int E = Vec<T>::E;
-    const float scale = float(kBins) / (top - from);
-    if (!(scale > 0.f && scale < 1e30f)) return false;
-    for (int i = threadIdx.x; i < kBins; i += kThreads) { s.count[i] = 0; s.fine[i] = 0; }
-    if (threadIdx.x == 0) { s.listed = 0; s.border_id = -1; }
-    __syncthreads();
-    row.template each<4>([&](uint32_t (&u)[4], int) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float z = Vec<T>::get(u, i);
-            if (z >= from) atomicAdd(&s.count[min(int((top - z) * scale), kBins - 1)], 1u);
-        }
-    });
-    __syncthreads();
-    const double width = double(top - from) / kBins * sc.per16 * (1.0 / 16.0);          // of a bin, in powers of two
-    find_bins<kThreads>(s, s.count, unit, 0.0, width, 1e-3 * width, 0.0, double(want));  // (positions are rounded by less than 2^-10 of a bin)
-    const int first = s.bin, last = s.last_bin;
+    first = s.bin;
+    last = s.last_bin;
     if (first > last) return false;                            // (not met: the bounds hold)
-    const float begin = float(first), end = last == kBins - 1 ? INFINITY : float(last + 1), finer = float(kBins) / float(last + 1 - first);
-    auto fine_bin = [&](float b) { return min(int((b - begin) * finer), kBins - 1); };
-    auto push = [&](float z, int id) {
-        const int at = atomicAdd(&s.listed, 1);
-        if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(id));
-    };
-    u64 above = 0;
+    const float begin = float(first) * 64.f, end = last == kBins - 1 ? INFINITY : float(last + 1) * 64.f, places = scale * 64.f;
+    u64 above = 0, sum = 0;
     sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&u)[4], int c) -> u64 {
-        u64 sum = 0;
+        u64 kept = 0;
         const int id = int(row.first(c));
 #pragma unroll
         for (int i = 0; i < E; i += 4) {
-            float z[4], kept[4];
-            bool any = false;
+            float z[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[j] = Vec<T>::get(u, i + j);
+            u64 w[4];
+            sc.template raw_weights<4, true>(z, 0.f, w);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float v = Vec<T>::get(u, i + j), b = (top - v) * scale;
-                z[j] = b < begin ? v : -INFINITY;
-                kept[j] = v >= least ? z[j] : -INFINITY;
-                any |= b < begin;
-                if (b >= begin && b < end && v >= from) {
-                    push(v, id + i + j);
-                    atomicAdd(&s.fine[fine_bin(b)], 1u);
+                w[j] -= Scale::kRaw;
+                sum += w[j];
+                const float at = (top - z[j]) * places;
+                if (at < begin) {
+                    above += w[j];
+                    if (z[j] >= least) kept += w[j];
+                } else if (at < end && z[j] >= from) {
+                    const int l = atomicAdd(&s.listed, 1);
+                    if (l < kList) { s.key[l] = u64(order(z[j] + 0.f)) << 32 | uint32_t(~uint32_t(id + i + j)); s.weight[l] = w[j]; }
                 }
             }
-            if (!__any_sync(__activemask(), any)) continue;
-            const u64 w = sc.sum<4, true>(z, 0.f);
-            above += w;
-            sum += least > from ? sc.sum<4, true>(kept, 0.f) : w;      // (min-p above what top-p can keep)
         }
-        return sum;
+        return kept;
     });
+    total = block_sum<kThreads>(s, sum);
     above = block_sum<kThreads>(s, above);
-    if (s.listed > kList) {
-        find_bins<kThreads>(s, s.fine, unit, begin * width, width / finer, 3e-3 * width, double(above), double(want));
-        const int first_fine = s.bin, last_fine = s.last_bin;
-        if (threadIdx.x == 0) s.listed = 0;
-        if (first_fine > last_fine) return false;
-        __syncthreads();
-        u64 more = 0;
-        sum_pieces<kThreads, true>(s, row, 0, row.vectors, each, by_value(row, [&](float z, int id) -> u64 {
-            const float b = (top - z) * scale;
-            u64 w = 0;
-            if (b >= begin && b < end && z >= from) {
-                const int f = fine_bin(b);
-                if (f < first_fine) w = sc.weight(z);
-                else if (f <= last_fine) push(z, id);
-            }
-            more += w;
-            return z >= least ? w : 0ull;
-        }));
-        above += block_sum<kThreads>(s, more);
-        if (s.listed > kList) return false;
-    }
     const int n = s.listed;
-    for (int i = threadIdx.x; i < n; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
-    __syncthreads();
-    if (above >= want) return false;                           // (not met)
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const u64 mine = s.key[i], w = s.weight[i];
-        u64 before = above;
+    const u64 want = part_of(total);
+    if (n > kList || above >= want) return false;              // (the second is not met)
+    // the border: the key at which `want` is reached
+    if (n <= kPairs) {
+        for (int i = threadIdx.x; i < n; i += kThreads) {
+            const u64 mine = s.key[i];
+            u64 before = above;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) before += s.key[j] > mine ? s.weight[j] : 0ull;
-        if (before >= want) continue;
-        const float z = unorder(uint32_t(mine >> 32));
-        const int id = int(~uint32_t(mine));
-        if (before + w >= want) { s.border_z = z; s.border_id = id; }
-        if (z >= least) atomicAdd(&s.piece[(id + row.shift) / E / (32 * each)], w);
+            for (int j = 0; j < n; ++j) before += s.key[j] > mine ? s.weight[j] : 0ull;
+            if (before < want && before + s.weight[i] >= want) { s.border_z = unorder(uint32_t(mine >> 32)); s.border_id = int(~uint32_t(mine)); }
+        }
+    } else {                                                   // bit by bit: the highest key from which on, upwards, there is enough
+        u64 key = 0;
+        for (int b = 63; b >= 0; --b) {
+            const u64 next = key | 1ull << b;
+            u64 upto = 0;
+            for (int i = threadIdx.x; i < n; i += kThreads) upto += s.key[i] >= next ? s.weight[i] : 0ull;
+            if (above + block_sum<kThreads>(s, upto) >= want) key = next;
+        }
+        if (threadIdx.x == 0 && key) { s.border_z = unorder(uint32_t(key >> 32)); s.border_id = int(~uint32_t(key)); }
     }
     __syncthreads();
+    if (s.border_id < 0) return false;                         // (not met)
     border = {s.border_z, s.border_id};
-    return s.border_id >= 0;
+    const u64 last_key = u64(order(border.z)) << 32 | uint32_t(~uint32_t(border.id));
+    for (int i = threadIdx.x; i < n; i += kThreads)
+        if (s.key[i] >= last_key && unorder(uint32_t(s.key[i] >> 32)) >= least)
+            atomicAdd(&s.piece[(int(~uint32_t(s.key[i])) + row.shift) / E / (32 * each)], s.weight[i]);
+    __syncthreads();
+    return true;
 }
 
 // The row of this block where the costly rows come first (rows of one kind in their order): those with top-p and no small top-k, then those that
@@ -675,7 +674,8 @@ __device__ __forceinline__ int costly_first(Shared& s, const SampleParams& p) {
 template <class T, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const SampleParams p) {
     constexpr int E = Vec<T>::E, kWarps = kThreads / 32;
-    __shared__ Shared s;
+    extern __shared__ __align__(16) uint8_t smem[];
+    Shared& s = *reinterpret_cast<Shared*>(smem);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_wait();
     grid_dependents_launch();
@@ -796,8 +796,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             });
         __syncthreads();
         const int count = s.listed;
-        if (count <= kList) {
-            constexpr int kEach = kList / kThreads;
+        if (count <= kMostSmall) {
+            constexpr int kEach = kMostSmall / kThreads;
             u64 before[kEach], sum = 0, kept[kEach];
             for (int i = threadIdx.x; i < count; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
             __syncthreads();
@@ -868,9 +868,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (k > 0 && select<kThreads, false>(s, row, sc, top, floor_z, u64(k), z, ties)) border = nth_of(z, ties);     // (else fewer have any weight)
         if (by_p) {
             u64 sum = 0;
-            if (k == 0)
-                row.template each<2>([&](uint32_t (&q)[4], int) { sum += vector_weight<true, T>(sc, q, 0.f); });
-            else
+            if (k == 0) summed = nucleus<kThreads>(s, row, sc, top, floor_z, unit, top_p, least, each, part_of, sum, border);
+            if (!summed) {
+                __syncthreads();
+                sum = 0;
                 row.template each<2>([&](uint32_t (&q)[4], int c) {
 #pragma unroll
                     for (int i = 0; i < E; ++i) {
@@ -878,15 +879,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                         sum += sc.weight(v, border.keeps(v, int(row.first(c)) + i));
                     }
                 });
-            sum = block_sum<kThreads>(s, sum);
-            // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
-            const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
-            const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
-            const float from = float(fmax(low, double(floor_z)));
-            const u64 want = part_of(sum);
-            if (k == 0) summed = nucleus<kThreads>(s, row, sc, top, from, unit, want, least, each, border);
-            if (!summed) {
-                __syncthreads();
+                sum = block_sum<kThreads>(s, sum);
+                // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
+                const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
+                const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
+                const float from = float(fmax(low, double(floor_z)));
+                const u64 want = part_of(sum);
                 if (select<kThreads, true>(s, row, sc, top, from, want, z, ties) || select<kThreads, true>(s, row, sc, top, floor_z, want, z, ties))
                     border = nth_of(z, ties);                  // (the second: top_p next to 1)
             }
@@ -910,14 +908,23 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (threadIdx.x == 0) answer(token, logprob_of(row.value(token), total));
 }
 
+template <class T, int kThreads>
+int launch_threads(const SampleParams& p, cudaStream_t st) {
+    static PerDeviceOnce once;
+    auto kernel = sample_kernel<T, kThreads>;
+    const int rc = once.run([&] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared))) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
+    });
+    return rc != PCL_OK ? rc : launch_chained(kernel, dim3(p.N), dim3(kThreads), sizeof(Shared), st, 1, p);
+}
 template <class T>
 int launch_sample(const SampleParams& p, cudaStream_t st) {
     // two blocks an SM overlap one's loads with the other's arithmetic; up to one row an SM, all threads go to it
     const int sms = device_sm_count();
-    if (p.N <= sms) return launch_chained(sample_kernel<T, 1024>, dim3(p.N), dim3(1024), 0, st, 1, p);
+    if (p.N <= sms) return launch_threads<T, 1024>(p, st);
     SampleParams q = p;
     q.ordered = p.N > 2 * sms && p.N <= kMostOrdered && (p.top_k || p.top_p || p.temperature);
-    return launch_chained(sample_kernel<T, 512>, dim3(p.N), dim3(512), 0, st, 1, q);
+    return launch_threads<T, 512>(q, st);
 }
 
 }  // namespace
