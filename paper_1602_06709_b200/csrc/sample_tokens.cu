@@ -513,7 +513,36 @@ __device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& s
     }
 }
 
-// What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list.  Leaves the sums of what is
+// The lowest finite value, not above `top`, for which f holds; f holds for `top` and for whatever lies above a value for which it does.  From a guess
+// by steps that double, then halve.
+template <class F>
+__device__ __forceinline__ float lowest_with(float guess, float top, F&& f) {
+    const uint32_t bottom = order(kLowest), most = order(top);
+    const uint32_t at = min(max(order(guess), bottom), most);
+    uint32_t lo = bottom - 1, hi = most;                      // the highest key without and the lowest with, from outside
+    if (f(unorder(at))) {
+        hi = at;
+        for (uint32_t step = 1; hi > bottom && hi - bottom >= step; step *= 2) {
+            if (!f(unorder(hi - step))) { lo = hi - step; break; }
+            hi -= step;
+        }
+    } else {
+        lo = at;
+        for (uint32_t step = 1; hi - lo > step; step *= 2) {
+            if (f(unorder(lo + step))) { hi = lo + step; break; }
+            lo += step;
+        }
+    }
+    while (hi - lo > 1) {
+        const uint32_t mid = lo + (hi - lo) / 2;
+        if (f(unorder(mid))) hi = mid;
+        else lo = mid;
+    }
+    return unorder(hi);
+}
+
+// What top-p keeps of a row without top-k: the border, or false where the tokens near it do not fit in the list, or min-p keeps less (the border then
+// is min-p's).  Leaves the sums of what is
 // kept (and not below `least`) in s.piece, and the weight of the whole row in `total`.
 //   A histogram over z from the top down to `from` counts tokens and adds up their places in the bins (to a 64th of a bin), which gives the weight
 //   of each bin to 1 part in 4000; the border lies in the bins, one or two as a rule, where the weight up to there can be top_p of all.  One pass then
@@ -582,11 +611,17 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
     first = s.bin;
     last = s.last_bin;
     if (first > last) return false;                            // (not met: the bounds hold)
-    const float begin = float(first) * 64.f, end = last == kBins - 1 ? INFINITY : float(last + 1) * 64.f, places = scale * 64.f;
+    // as bounds on the values: those from `over` on lie above the bins, those from `in` on above them or in them
+    const float places = scale * 64.f, begin = float(first) * 64.f, end = float(last + 1) * 64.f;
+    const float over = first == 0 ? INFINITY : lowest_with(top - begin / places, top, [&](float z) { return (top - z) * places < begin; });
+    const float in = last == kBins - 1 ? from : fmaxf(from, lowest_with(top - end / places, top, [&](float z) { return (top - z) * places < end; }));
+    if (least >= over) {                                       // min-p keeps less than what top-p keeps in any case
+        border = {least, kAllIds};
+        return false;
+    }
     u64 above = 0, sum = 0;
     sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&u)[4], int c) -> u64 {
         u64 kept = 0;
-        const int id = int(row.first(c));
 #pragma unroll
         for (int i = 0; i < E; i += 4) {
             float z[4];
@@ -594,20 +629,25 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
             for (int j = 0; j < 4; ++j) z[j] = Vec<T>::get(u, i + j);
             u64 w[4];
             sc.template raw_weights<4, true>(z, 0.f, w);
+            bool listed = false;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 w[j] -= Scale::kRaw;
                 sum += w[j];
-                const float at = (top - z[j]) * places;
-                if (at < begin) {
-                    above += w[j];
-                    if (z[j] >= least) kept += w[j];
-                } else if (at < end && z[j] >= from) {
-                    const int l = atomicAdd(&s.listed, 1);
-                    if (l < kList) { s.key[l] = u64(order(z[j] + 0.f)) << 32 | uint32_t(~uint32_t(id + i + j)); s.weight[l] = w[j]; }
-                }
+                kept += z[j] >= over ? w[j] : 0ull;
+                listed |= z[j] >= in && z[j] < over;
+            }
+            if (listed) {
+                const int id = int(row.first(c)) + i;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (z[j] >= in && z[j] < over) {
+                        const int l = atomicAdd(&s.listed, 1);
+                        if (l < kList) { s.key[l] = u64(order(z[j] + 0.f)) << 32 | uint32_t(~uint32_t(id + j)); s.weight[l] = w[j]; }
+                    }
             }
         }
+        above += kept;
         return kept;
     });
     total = block_sum<kThreads>(s, sum);
@@ -739,32 +779,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto logprob_of = [&](float z, u64 total) {
         return float((infinite ? 0.0 : sc.x(z) * (0.69314718055994530942 / 16.0)) - log(double(total) / unit));
     };
-    // the lowest value that min-p keeps: x(z) >= 16 log2(min_p), from a guess by steps that double, then halve (NaN: no filter)
+    // the lowest value that min-p keeps: x(z) >= 16 log2(min_p) (NaN: no filter)
     float least = kLowest;
     if (min_p > 0.f && !infinite) {
         const double min_x = 16.0 * log2(fmin(double(min_p), 1.0));
-        const uint32_t bottom = order(kLowest), most = order(top);
-        auto kept = [&](uint32_t key) { return sc.x(unorder(key)) >= min_x; };
-        const uint32_t guess = order(float(fmin(fmax(double(top) + min_x / per16, double(kLowest)), double(top))));
-        uint32_t lo = bottom - 1, hi = most;                  // the highest key that is not kept and the lowest that is, from outside
-        if (kept(guess)) {
-            hi = guess;
-            for (uint32_t step = 1; hi - bottom >= step && hi > bottom; step *= 2) {
-                if (!kept(hi - step)) { lo = hi - step; break; }
-                hi -= step;
-            }
-        } else {
-            lo = guess;
-            for (uint32_t step = 1; hi - lo > step; step *= 2) {
-                if (kept(lo + step)) { hi = lo + step; break; }
-                lo += step;
-            }
-        }
-        while (hi - lo > 1) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (kept(mid)) hi = mid; else lo = mid;
-        }
-        least = unorder(hi);
+        least = lowest_with(float(fmax(double(top) + min_x / per16, double(kLowest))), top, [&](float v) { return sc.x(v) >= min_x; });
     }
 
     // ---- small top-k
@@ -869,7 +888,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (by_p) {
             u64 sum = 0;
             if (k == 0) summed = nucleus<kThreads>(s, row, sc, top, floor_z, unit, top_p, least, each, part_of, sum, border);
-            if (!summed) {
+            if (!summed && !(k == 0 && border.z == least && least > kLowest)) {
                 __syncthreads();
                 sum = 0;
                 row.template each<2>([&](uint32_t (&q)[4], int c) {
