@@ -1,5 +1,5 @@
 """ctypes binding of libpcl_dnn.so: same names as the C ABI, argument
-marshalling only.  Tensors are torch CUDA tensors (device memory and streams
+marshalling only (of the calls whose kernels last no longer than that, compiled: csrc/fast_calls.cpp).  Tensors are torch CUDA tensors (device memory and streams
 are all torch is used for); every step of the path runs in the library's
 kernels.  There is no CPU or library fallback: if the shared library is missing
 or a call fails, an exception is raised.
@@ -62,11 +62,12 @@ class ConvDesc(ctypes.Structure):
 
 
 _lib = None
+_calls = None           # compiled checks and marshalling (csrc/fast_calls.cpp) of the calls that have them, once the library is loaded
 
 
 def lib() -> ctypes.CDLL:
     """Loads the CUDA library; fails loudly if it has not been built."""
-    global _lib
+    global _lib, _calls
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise RuntimeError(f"{LIB_PATH} is missing: run `python -m paper_1602_06709_b200.build` "
@@ -153,8 +154,24 @@ def lib() -> ctypes.CDLL:
         L.pcl_noalloc_scratch_bytes.restype = sz
         L.pcl_status_string.argtypes = [ci]
         L.pcl_status_string.restype = ctypes.c_char_p
-        _lib = L
+        try:
+            from . import _pcl_calls
+        except ImportError as e:
+            raise RuntimeError(f"{os.path.join(_HERE, '_pcl_calls.so')} is missing or unusable: run `python -m paper_1602_06709_b200.build`") from e
+        _pcl_calls.bind({n: ctypes.cast(getattr(L, n), vp).value for n in _COMPILED})
+        _lib, _calls = L, _pcl_calls
     return _lib
+
+
+_COMPILED = ["pcl_rms_norm_fwd", "pcl_rms_norm_fwd_q8", "pcl_rms_norm_bwd", "pcl_quantize_rows", "pcl_fc_q8_fwd", "pcl_grad_norm",
+             "pcl_grad_clip", "pcl_sgd_update_clipped", "pcl_sample_tokens"]
+
+
+def _done(code: int, where: str) -> bool:
+    """Whether a compiled call has been made (-1: an argument is not what it takes; the checks here say which)."""
+    if code > 0:
+        raise PclError(code, where)
+    return code == 0
 
 
 def status_string(code: int) -> str:
@@ -575,6 +592,8 @@ def _bytes8(where, like, tensors, types=(E4M3, torch.uint8)):
 
 def rms_norm_fwd(N, C, x, residual, w, eps, h, y, rstd=None, stream=None):
     """h = x + residual (residual and h may be None), y = h / sqrt(mean(h^2) + eps) * w, rstd = 1 / sqrt(mean(h^2) + eps)."""
+    if _calls is not None and _done(_calls.rms_norm_fwd(N, C, x, residual, w, eps, h, y, rstd, stream), "pcl_rms_norm_fwd"):
+        return
     d, s = _typed("pcl_rms_norm_fwd", (N, C), [(x, N * C), (residual, N * C), (w, C), (h, N * C), (y, N * C)], [(rstd, N)], stream=stream)
     _check(lib().pcl_rms_norm_fwd(N, C, d, _addr(x), _addr(residual), _addr(w), eps, _addr(h), _addr(y), _addr(rstd), s),
            "pcl_rms_norm_fwd")
@@ -582,6 +601,8 @@ def rms_norm_fwd(N, C, x, residual, w, eps, h, y, rstd=None, stream=None):
 
 def rms_norm_fwd_q8(N, C, x, residual, w, eps, h, y8, y_scale, rstd=None, stream=None):
     """rms_norm_fwd with y as e4m3 values (a float8_e4m3fn or uint8 tensor) and a scale for each row."""
+    if _calls is not None and _done(_calls.rms_norm_fwd_q8(N, C, x, residual, w, eps, h, y8, y_scale, rstd, stream), "pcl_rms_norm_fwd_q8"):
+        return
     d, s = _typed("pcl_rms_norm_fwd_q8", (N, C), [(x, N * C), (residual, N * C), (w, C), (h, N * C)], [(rstd, N), (y_scale, N)], stream=stream)
     _bytes8("pcl_rms_norm_fwd_q8", x, [(y8, N * C)])
     _check(lib().pcl_rms_norm_fwd_q8(N, C, d, _addr(x), _addr(residual), _addr(w), eps, _addr(h), _addr(y8), _addr(y_scale),
@@ -594,6 +615,8 @@ def rms_norm_workspace_bytes(N, C) -> int:
 
 def rms_norm_bwd(N, C, h, w, rstd, dy, dh, dx, dw, ws=None, stream=None):
     """dx = dh (or 0) + the gradient through the norm; dw (or None): the gradient of its weights."""
+    if _calls is not None and _done(_calls.rms_norm_bwd(N, C, h, w, rstd, dy, dh, dx, dw, ws, stream), "pcl_rms_norm_bwd"):
+        return
     d, s = _typed("pcl_rms_norm_bwd", (N, C), [(h, N * C), (w, C), (dy, N * C), (dh, N * C), (dx, N * C), (dw, C)], [(rstd, N)],
                   stream=stream, ws=ws)
     wp, wb = _ws(ws)
@@ -603,6 +626,8 @@ def rms_norm_bwd(N, C, h, w, rstd, dy, dh, dx, dw, ws=None, stream=None):
 
 def quantize_rows(N, C, x, q, scale, stream=None):
     """q: the rows of x as e4m3 values, scale: max |row| / 448."""
+    if _calls is not None and _done(_calls.quantize_rows(N, C, x, q, scale, stream), "pcl_quantize_rows"):
+        return
     d, s = _typed("pcl_quantize_rows", (N, C), [(x, N * C)], [(scale, N)], stream=stream)
     _bytes8("pcl_quantize_rows", x, [(q, N * C)])
     _check(lib().pcl_quantize_rows(N, C, d, _addr(x), _addr(q), _addr(scale), s), "pcl_quantize_rows")
@@ -614,11 +639,16 @@ def fc_q8_workspace_bytes(N, C, K) -> int:
 
 def fc_q8_fwd(N, C, K, x, x_scale, w, w_scale, bias, y, act=ACT_NONE, ws=None, stream=None):
     """y = act(x_scale[n] * w_scale[k] * (x w^T) + bias) of e4m3 operands (float8_e4m3fn or uint8 tensors)."""
+    if _calls is not None and _done(_calls.fc_q8_fwd(N, C, K, y, bias, x, x_scale, w, w_scale, act, ws, stream), "pcl_fc_q8_fwd"):
+        return
     d, s = _typed("pcl_fc_q8_fwd", (N, C, K), [(y, N * K), (bias, K)], [(x_scale, N), (w_scale, K)], stream=stream, ws=ws)
     _bytes8("pcl_fc_q8_fwd", y, [(x, N * C), (w, K * C)])
     wp, wb = _ws(ws)
     _check(lib().pcl_fc_q8_fwd(N, C, K, d, _addr(x), _addr(x_scale), _addr(w), _addr(w_scale), _addr(bias), _addr(y), act, wp, wb, s),
            "pcl_fc_q8_fwd")
+
+
+_LAYOUTS = {}
 
 
 class TensorList:
@@ -636,6 +666,8 @@ class TensorList:
                 raise ValueError("contiguous tensors on one CUDA device are wanted")
         self.dtypes = tuple(dtype_code(t) for t in self.tensors)
         self.sizes = tuple(t.numel() for t in self.tensors)
+        key = (self.device, self.sizes, self.dtypes)
+        self.layout = _LAYOUTS.setdefault(key, key)         # (one object for lists that are alike)
         self._pointers = (ctypes.c_void_p * n)(*[t.data_ptr() if t.numel() else None for t in self.tensors])
         self._sizes = (ctypes.c_size_t * n)(*self.sizes)
         self._dtypes = (ctypes.c_int * n)(*self.dtypes)
@@ -650,10 +682,8 @@ def _lists(where, lists, norm, stream, ws):
     first = lists[0]
     dev = first.device
     for other in lists[1:]:
-        if other.sizes != first.sizes or other.dtypes != first.dtypes:
-            raise ValueError(f"{where}: lists of the same sizes and types are wanted")
-        if other.device != dev:
-            raise ValueError(f"{where}: all tensors must be on the current CUDA device")
+        if other.layout is not first.layout:
+            raise ValueError(f"{where}: lists of the same sizes and types, on the same device, are wanted")
     if norm.dtype is not torch.float32:
         raise TypeError(f"{where}: a torch.float32 tensor is wanted, not {norm.dtype}")
     if norm.numel() != 1:
@@ -670,6 +700,8 @@ def grad_norm_workspace_bytes(tensors) -> int:
 
 def grad_norm(grads, norm, ws=None, stream=None):
     """norm = the 2-norm of all tensors of the list `grads` together."""
+    if _calls is not None and _done(_calls.grad_norm(grads.device, len(grads.tensors), grads.pointers, grads.counts, grads.types, norm, ws, stream), "pcl_grad_norm"):
+        return
     s = _lists("pcl_grad_norm", (grads,), norm, stream, ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_grad_norm(len(grads), grads.pointers, grads.counts, grads.types, _addr(norm), wp, wb, s), "pcl_grad_norm")
@@ -677,6 +709,9 @@ def grad_norm(grads, norm, ws=None, stream=None):
 
 def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
     """out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)); out may be grads."""
+    if _calls is not None and out.layout is grads.layout and _done(_calls.grad_clip(
+            grads.device, len(grads.tensors), grads.pointers, out.pointers, grads.counts, grads.types, max_norm, norm, ws, stream), "pcl_grad_clip"):
+        return
     s = _lists("pcl_grad_clip", (grads, out), norm, stream, ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_grad_clip(len(grads), grads.pointers, out.pointers, grads.counts, grads.types, max_norm, _addr(norm), wp, wb, s),
@@ -685,6 +720,10 @@ def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
 
 def sgd_update_clipped(params, grads, lr, max_norm, norm, ws=None, stream=None):
     """params[i] -= lr * min(1, max_norm / (norm + 1e-6)) * grads[i], in place."""
+    if _calls is not None and params.layout is grads.layout and _done(_calls.sgd_update_clipped(
+            grads.device, len(grads.tensors), params.pointers, grads.pointers, grads.counts, grads.types, lr, max_norm, norm, ws, stream),
+            "pcl_sgd_update_clipped"):
+        return
     s = _lists("pcl_sgd_update_clipped", (grads, params), norm, stream, ws)
     wp, wb = _ws(ws)
     _check(lib().pcl_sgd_update_clipped(len(grads), params.pointers, grads.pointers, grads.counts, grads.types, lr, max_norm,
@@ -697,6 +736,8 @@ def sample_tokens_workspace_bytes(N, K) -> int:
 
 def sample_tokens(N, K, logits, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, ws=None, stream=None):
     """token[n] of each row of logits, chosen by uniform[n] after temperature, top-k, top-p and min-p ([N] tensors, top_k int32)."""
+    if _calls is not None and _done(_calls.sample_tokens(N, K, logits, uniform, token, temperature, top_k, top_p, min_p, logprob, ws, stream), "pcl_sample_tokens"):
+        return
     ints = [(token, N)] if top_k is None else [(token, N), (top_k, N)]
     d, s = _typed("pcl_sample_tokens", (N, K), [(logits, N * K)], [(uniform, N), (temperature, N), (top_p, N), (min_p, N), (logprob, N)], ints,
                   stream=stream, ws=ws)

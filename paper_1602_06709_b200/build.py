@@ -1,4 +1,5 @@
-"""Builds libpcl_dnn.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libpcl_dnn.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _pcl_calls.so (compiled marshalling of
+binding.py's smallest calls) with g++."""
 from __future__ import annotations
 
 import os
@@ -17,6 +18,26 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
          "-Xcompiler", "-fPIC"]
 
 
+CALLS_SOURCE = os.path.join(CSRC, "fast_calls.cpp")
+CALLS = os.path.join(HERE, "_pcl_calls.so")
+
+
+def build_calls(force: bool = False) -> str:
+    deps = [CALLS_SOURCE, os.path.join(CSRC, "..", "..", "include", "pcl_dnn.h"), os.path.abspath(__file__)]
+    if not force and os.path.exists(CALLS) and all(os.path.getmtime(d) <= os.path.getmtime(CALLS) for d in deps):
+        return CALLS
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-I{home}/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", CALLS_SOURCE, f"-L{home}/lib", "-lc10", "-lc10_cuda",
+           "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{home}/lib", "-o", CALLS]
+    subprocess.run(cmd, check=True)
+    return CALLS
+
+
 def needs_build() -> bool:
     if not os.path.exists(LIB):
         return True
@@ -26,6 +47,7 @@ def needs_build() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
+    build_calls(force)
     if not force and not needs_build():
         return LIB
     objdir = os.path.join(HERE, "_build")
