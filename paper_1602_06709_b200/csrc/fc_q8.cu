@@ -10,6 +10,13 @@ namespace pcl {
 
 namespace {
 
+// The counters of the GEMM's split tiles; the GEMM sets itself up meanwhile.
+__global__ void __launch_bounds__(256) clear_kernel(uint4* p, int n) {
+    grid_dependency_wait();
+    grid_dependents_launch();
+    for (int i = threadIdx.x; i < n; i += 256) p[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 struct Rows8 { const uint8_t* src; uint8_t* dst; long rows; };
 
 // Rows of C bytes to rows of ldc (a multiple of 16), zeros behind.  A warp takes a row, a lane 16 bytes of it, from five aligned words.
@@ -70,7 +77,8 @@ int launch_fc_q8(int N, int C, int K, int out_type, const void* x, const float* 
     if (!gemm16_possible(a)) return PCL_ERR_UNSUPPORTED_SHAPE;
     a.split_ws = split ? ws : nullptr;
     if (split) {
-        const int rc = launch_zero(static_cast<float*>(ws), kGemm16CounterBytes / 4, st);
+        LaunchScope scope(KID_ZERO, double(kGemm16CounterBytes), st);
+        const int rc = launch_chained(clear_kernel, dim3(1), dim3(256), 0, st, 1, static_cast<uint4*>(ws), int(kGemm16CounterBytes / 16));
         if (rc != PCL_OK) return rc;
     }
     if (C % 16) {
