@@ -365,15 +365,28 @@ class Dnn(_HostFeed):
     exist at a time, in the workspace; the logits are computed twice.  Where they are fewer, keeping them is faster (1024 x 8192: a
     step of 0.63 against 0.71 ms).
     hidden_update = "orthogonal": the weight matrices between the first and the output layer are stepped along the
-    orthogonalised momentum of their gradient (pcl_orthogonal_update, rate hidden_lr); everything else by plain SGD."""
+    orthogonalised momentum of their gradient (pcl_orthogonal_update, rate hidden_lr); everything else by plain SGD.
+    residual_norm: the hidden layers, which then are of one width, add to a stream, and every layer behind the first reads the RMS norm of it
+    (pcl_rms_norm_fwd / _bwd):  s_0 = out_0,  s_j = s_{j-1} + out_j,  a_{j+1} = norm(s_j) * gain_{j+1}.
+    clip_norm: the update is that of the gradients clipped to this global norm (pcl_sgd_update_clipped), which is left in grad_norm.
+
+    answer() chooses a class for each row from the logits (pcl_sample_tokens); after quantize() it can run the layers behind the first in 8 bits
+    (pcl_rms_norm_fwd_q8, pcl_fc_q8_fwd)."""
+
+    EPS = 1e-6
 
     def __init__(self, N: int, dims=None, lr: float = 0.01, cfg: str = "cfg4", fused_update: bool = False,
-                 stored_logits: bool = True, hidden_update: str = "sgd", hidden_lr: float = 0.02, momentum: float = 0.95):
+                 stored_logits: bool = True, hidden_update: str = "sgd", hidden_lr: float = 0.02, momentum: float = 0.95,
+                 residual_norm: bool = False, clip_norm: Optional[float] = None):
         dims = dims if dims is not None else inputs.CFG4_DIMS
         if hidden_update not in ("sgd", "orthogonal"):
             raise ValueError(f"unknown hidden_update {hidden_update!r}")
         if hidden_update == "orthogonal" and fused_update:
             raise ValueError("the orthogonalised update needs stored gradients: fused_update must be off")
+        if clip_norm is not None and (fused_update or hidden_update != "sgd"):
+            raise ValueError("the clipped update needs stored gradients and plain SGD")
+        if residual_norm and (fused_update or len(set(dims[1:-1])) != 1):
+            raise ValueError("a residual stream needs hidden layers of one width, and stored gradients")
         self.N, self.dims, self.lr = N, dims, lr
         self.fused_update = fused_update      # (as in VggA: weights updated by their own weight-gradient call)
         self.stored_logits, self.hidden_update = stored_logits, hidden_update
@@ -382,6 +395,10 @@ class Dnn(_HostFeed):
         shapes = []
         for C, K in self.layers:
             shapes += [(K, C), (K,)]
+        self.residual_norm, self.clip_norm = residual_norm, clip_norm
+        self._first_gain = len(shapes)
+        if residual_norm:
+            shapes += [(C,) for C, _ in self.layers[1:]]
         self.store = _ParamStore(shapes, tail=list(range(1, len(shapes), 2)) if fused_update else ())
         for j, (C, K) in enumerate(self.layers):
             w = inputs.xavier_uniform_fc(inputs.tensor_id(cfg, f"fc{j + 1}", "w"), K, C)
@@ -402,6 +419,20 @@ class Dnn(_HostFeed):
             C, K = self.layers[-1]
             self.row_loss, self.lse = torch.empty(N, device=dev), torch.empty(N, device=dev)
             ws = max([ws] + [B.fc_softmax_xent_workspace_bytes(N, C, K, B.F32, p) for p in (B.PASS_FWD, B.PASS_BWD_DATA)])
+        if residual_norm:
+            C = dims[1]
+            for j in range(1, len(self.layers)):
+                self.gain(j).fill_(1.0)
+            self.stream = [torch.empty(N, C, device=dev) if j > 0 else None for j in range(len(self.layers) - 1)]        # s_0 is out[0]
+            self.normed = [None] + [torch.empty(N, C, device=dev) for _ in self.layers[1:]]
+            self.rstd = [None] + [torch.empty(N, device=dev) for _ in self.layers[1:]]
+            self.dstream, self.dnormed = torch.empty(N, C, device=dev), torch.empty(N, C, device=dev)
+            ws = max(ws, B.rms_norm_workspace_bytes(N, C))
+        self.grad_norm = torch.zeros(1, device=dev)
+        self._lists = None
+        if clip_norm is not None:
+            self._lists = B.TensorList([self.store.params]), B.TensorList([self.store.grads])
+            ws = max(ws, B.grad_norm_workspace_bytes(1))
         self.moments = {}
         if hidden_update == "orthogonal":
             for j in range(1, len(self.layers) - 1):
@@ -415,31 +446,57 @@ class Dnn(_HostFeed):
     def b(self, j): return self.store.p(2 * j + 1)
     def dw(self, j): return self.store.g(2 * j)
     def db(self, j): return self.store.g(2 * j + 1)
+    def gain(self, j): return self.store.p(self._first_gain + j - 1)         # of the norm in front of layer j
+    def dgain(self, j): return self.store.g(self._first_gain + j - 1)
+
+    def _stream(self, j):
+        return self.out[0] if j == 0 else self.stream[j]
 
     def _step_state(self):
         return [self.store.params, *self.moments.values()]
 
     def param_buckets(self):
-        if self.hidden_update != "sgd":
-            raise ValueError("the gradient exchange updates strips of the parameters: plain SGD only")
+        if self.hidden_update != "sgd" or self.residual_norm or self.clip_norm is not None:
+            raise ValueError("the gradient exchange updates strips of the (weights, bias) pairs: plain SGD only")
         return self.store.layer_buckets()
 
-    def forward(self, before_layer=None):
+    def _normed_input(self, j):
+        """What layer j > 0 of a residual stream reads; extends the stream by the layer below it."""
+        C = self.dims[1]
+        below = self._stream(j - 2) if j > 1 else None
+        B.rms_norm_fwd(self.N, C, self.out[j - 1], below, self.gain(j), self.EPS, self.stream[j - 1] if j > 1 else None, self.normed[j], self.rstd[j])
+        return self.normed[j]
+
+    def _layers(self, last, before_layer=None):
+        """Layers 0 .. last - 1; returns what layer `last` reads."""
         a = self.x
-        n = len(self.layers)
-        for j, (C, K) in enumerate(self.layers):
+        for j in range(last):
+            C, K = self.layers[j]
             if before_layer:
                 before_layer(j)
-            if j + 1 == n and not self.stored_logits:
-                B.fc_softmax_xent_fwd(self.N, C, K, a, self.w(j), self.b(j), self.labels, self.loss, self.row_loss, self.lse,
-                                      ws=self.ws)
-                return
-            act = B.ACT_SIGMOID if j + 1 < n else B.ACT_NONE
+            act = B.ACT_SIGMOID if j + 1 < len(self.layers) else B.ACT_NONE
             B.fc_fwd(self.N, C, K, a, self.w(j), self.b(j), self.out[j], act, self.ws)
             a = self.out[j]
+            if self.residual_norm and j + 1 < len(self.layers):
+                a = self._normed_input(j + 1)
+        return a
+
+    def forward(self, before_layer=None):
+        n = len(self.layers)
+        if not self.stored_logits:
+            a = self._layers(n - 1, before_layer)
+            if before_layer:
+                before_layer(n - 1)
+            C, K = self.layers[-1]
+            B.fc_softmax_xent_fwd(self.N, C, K, a, self.w(n - 1), self.b(n - 1), self.labels, self.loss, self.row_loss, self.lse,
+                                  ws=self.ws)
+            return
+        self._layers(n, before_layer)
         B.softmax_xent(self.N, self.dims[-1], self.out[-1], self.labels, self.loss, self.dout[-1])
 
     def backward(self, after_layer=None, after_backprop=None):
+        if self.residual_norm:
+            return self._backward_stream(after_layer, after_backprop)
         n = len(self.layers)
         for j in reversed(range(n)):
             C, K = self.layers[j]
@@ -467,7 +524,63 @@ class Dnn(_HostFeed):
             if after_backprop:
                 after_backprop(j)
 
+    def _backward_stream(self, after_layer, after_backprop):
+        """The gradient of the stream is that of every layer's output; it grows by each norm's on the way down."""
+        n = len(self.layers)
+        for j in reversed(range(n)):
+            C, K = self.layers[j]
+            a, dx = (self.normed[j], self.dnormed) if j > 0 else (self.x, None)
+            if j + 1 == n and not self.stored_logits:
+                B.fc_softmax_xent_bwd(self.N, C, K, a, self.w(j), self.b(j), self.labels, self.lse, None, dx, self.dw(j), self.db(j), ws=self.ws)
+            elif j + 1 == n:
+                B.fc_bwd(self.N, C, K, a, self.w(j), None, B.ACT_NONE, self.dout[j], dx, self.dw(j), self.db(j), self.ws)
+            else:
+                self.dout[j].copy_(self.dstream)               # (the call turns it into dz)
+                B.fc_bwd(self.N, C, K, a, self.w(j), self.out[j], B.ACT_SIGMOID, self.dout[j], dx, self.dw(j), self.db(j), self.ws)
+            if j > 0:
+                B.rms_norm_bwd(self.N, C, self._stream(j - 1), self.gain(j), self.rstd[j], self.dnormed, self.dstream if j + 1 < n else None,
+                               self.dstream, self.dgain(j), self.ws)
+            if after_layer:
+                after_layer(j)
+            if after_backprop:
+                after_backprop(j)
+
+    def quantize(self):
+        """Takes the weights of the layers behind the first, as they are now, to 8 bits for answer(eight_bit=True)."""
+        if not self.residual_norm:
+            raise ValueError("layers read 8-bit rows behind a norm only")
+        C = self.dims[1]
+        self.w8 = [None] + [(torch.empty(K, C, dtype=B.E4M3, device="cuda"), torch.empty(K, device="cuda")) for _, K in self.layers[1:]]
+        for j in range(1, len(self.layers)):
+            B.quantize_rows(self.layers[j][1], C, self.w(j), *self.w8[j])
+        self.x8, self.x8_scale = torch.empty(self.N, C, dtype=B.E4M3, device="cuda"), torch.empty(self.N, device="cuda")
+        need = max(B.fc_q8_workspace_bytes(self.N, C, K) for _, K in self.layers[1:])
+        self.ws8 = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+
+    def answer(self, uniform, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, eight_bit=False):
+        """token[n] = a class for each row of x, chosen by uniform[n] (see pcl_sample_tokens for the filters, [N] tensors)."""
+        if not self.stored_logits:
+            raise ValueError("a choice needs the logits: stored_logits must be on")
+        n = len(self.layers)
+        if eight_bit:
+            C, K = self.layers[0]
+            B.fc_fwd(self.N, C, K, self.x, self.w(0), self.b(0), self.out[0], B.ACT_SIGMOID, self.ws)
+            for j in range(1, n):
+                C, K = self.layers[j]
+                B.rms_norm_fwd_q8(self.N, C, self.out[j - 1], self._stream(j - 2) if j > 1 else None, self.gain(j), self.EPS,
+                                  self.stream[j - 1] if j > 1 else None, self.x8, self.x8_scale)
+                B.fc_q8_fwd(self.N, C, K, self.x8, self.x8_scale, *self.w8[j], self.b(j), self.out[j], B.ACT_SIGMOID if j + 1 < n else B.ACT_NONE, self.ws8)
+        else:
+            self._layers(n)
+        if not hasattr(self, "ws_answer"):
+            need = B.sample_tokens_workspace_bytes(self.N, self.dims[-1])
+            self.ws_answer = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+        B.sample_tokens(self.N, self.dims[-1], self.out[-1], uniform, token, temperature, top_k, top_p, min_p, logprob, self.ws_answer)
+
     def update(self):
+        if self.clip_norm is not None:
+            B.sgd_update_clipped(*self._lists, self.lr, self.clip_norm, self.grad_norm, self.ws)
+            return
         if self.hidden_update == "orthogonal":
             for j, (C, K) in enumerate(self.layers):
                 if j in self.moments:
@@ -476,6 +589,8 @@ class Dnn(_HostFeed):
                 else:
                     B.sgd_update(self.w(j), self.dw(j), self.lr)
                 B.sgd_update(self.b(j), self.db(j), self.lr)
+                if self.residual_norm and j > 0:
+                    B.sgd_update(self.gain(j), self.dgain(j), self.lr)
             return
         t = self.store.tail_offset if self.fused_update else 0
         B.sgd_update(self.store.params[t:], self.store.grads[t:], self.lr)
