@@ -648,9 +648,6 @@ def fc_q8_fwd(N, C, K, x, x_scale, w, w_scale, bias, y, act=ACT_NONE, ws=None, s
            "pcl_fc_q8_fwd")
 
 
-_LAYOUTS = {}
-
-
 class TensorList:
     """Several tensors (contiguous, of one device, each fp32, bf16 or fp16) as the calls over many tensors take them.  The list is of the
     tensors' memory as it is when the list is made, and keeps that memory alive."""
@@ -666,11 +663,10 @@ class TensorList:
                 raise ValueError("contiguous tensors on one CUDA device are wanted")
         self.dtypes = tuple(dtype_code(t) for t in self.tensors)
         self.sizes = tuple(t.numel() for t in self.tensors)
-        key = (self.device, self.sizes, self.dtypes)
-        self.layout = _LAYOUTS.setdefault(key, key)         # (one object for lists that are alike)
         self._pointers = (ctypes.c_void_p * n)(*[t.data_ptr() if t.numel() else None for t in self.tensors])
         self._sizes = (ctypes.c_size_t * n)(*self.sizes)
         self._dtypes = (ctypes.c_int * n)(*self.dtypes)
+        self.layout = bytes((ctypes.c_int * 1)(self.device)) + bytes(self._sizes) + bytes(self._dtypes)       # (alike for lists that are alike)
         self.pointers, self.counts, self.types = (ctypes.addressof(a) for a in (self._pointers, self._sizes, self._dtypes))
 
     def __len__(self):
@@ -682,7 +678,7 @@ def _lists(where, lists, norm, stream, ws):
     first = lists[0]
     dev = first.device
     for other in lists[1:]:
-        if other.layout is not first.layout:
+        if other.layout != first.layout:
             raise ValueError(f"{where}: lists of the same sizes and types, on the same device, are wanted")
     if norm.dtype is not torch.float32:
         raise TypeError(f"{where}: a torch.float32 tensor is wanted, not {norm.dtype}")
@@ -709,7 +705,7 @@ def grad_norm(grads, norm, ws=None, stream=None):
 
 def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
     """out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)); out may be grads."""
-    if _calls is not None and out.layout is grads.layout and _done(_calls.grad_clip(
+    if _calls is not None and out.layout == grads.layout and _done(_calls.grad_clip(
             grads.device, len(grads.tensors), grads.pointers, out.pointers, grads.counts, grads.types, max_norm, norm, ws, stream), "pcl_grad_clip"):
         return
     s = _lists("pcl_grad_clip", (grads, out), norm, stream, ws)
@@ -720,7 +716,7 @@ def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
 
 def sgd_update_clipped(params, grads, lr, max_norm, norm, ws=None, stream=None):
     """params[i] -= lr * min(1, max_norm / (norm + 1e-6)) * grads[i], in place."""
-    if _calls is not None and params.layout is grads.layout and _done(_calls.sgd_update_clipped(
+    if _calls is not None and params.layout == grads.layout and _done(_calls.sgd_update_clipped(
             grads.device, len(grads.tensors), params.pointers, grads.pointers, grads.counts, grads.types, lr, max_norm, norm, ws, stream),
             "pcl_sgd_update_clipped"):
         return

@@ -429,6 +429,7 @@ class Dnn(_HostFeed):
             self.dstream, self.dnormed = torch.empty(N, C, device=dev), torch.empty(N, C, device=dev)
             ws = max(ws, B.rms_norm_workspace_bytes(N, C))
         self.grad_norm = torch.zeros(1, device=dev)
+        self.w8 = None
         self._lists = None
         if clip_norm is not None:
             self._lists = B.TensorList([self.store.params]), B.TensorList([self.store.grads])
@@ -562,6 +563,8 @@ class Dnn(_HostFeed):
         if not self.stored_logits:
             raise ValueError("a choice needs the logits: stored_logits must be on")
         n = len(self.layers)
+        if eight_bit and self.w8 is None:
+            raise ValueError("8-bit layers need quantize() first")
         if eight_bit:
             C, K = self.layers[0]
             B.fc_fwd(self.N, C, K, self.x, self.w(0), self.b(0), self.out[0], B.ACT_SIGMOID, self.ws)

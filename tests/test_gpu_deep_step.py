@@ -155,3 +155,5 @@ def test_options_that_do_not_go_together():
         networks.Dnn(8, dims=[8, 16, 10]).quantize()
     with pytest.raises(ValueError):
         m.param_buckets()
+    with pytest.raises(ValueError):
+        make().answer(m.row_loss, m.labels, eight_bit=True)
