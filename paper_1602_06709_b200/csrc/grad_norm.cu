@@ -45,24 +45,40 @@ struct ApplyParams {
     float* norm;
 };
 
-__device__ __forceinline__ void unpack(const uint4& q, int type, float (&v)[8]) {
+// Elements of a vector of type kType.
+template <int kType> constexpr int kPer = kType == DT_F32 ? 4 : 8;
+template <int kType>
+__device__ __forceinline__ void unpack(const uint4& q, float (&v)[kPer<kType>]) {
     const uint32_t u[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (type == DT_F32) { v[i] = __uint_as_float(u[i]); v[4 + i] = 0.f; }
-        else if (type == DT_BF16) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
-        else { const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u[i])); v[2 * i] = h.x; v[2 * i + 1] = h.y; }
+        if constexpr (kType == DT_F32) {
+            v[i] = __uint_as_float(u[i]);
+        } else if constexpr (kType == DT_BF16) {
+            v[2 * i] = __uint_as_float(u[i] << 16);
+            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        } else {
+            const float2 h = __half22float2(*reinterpret_cast<const __half2*>(&u[i]));
+            v[2 * i] = h.x;
+            v[2 * i + 1] = h.y;
+        }
     }
 }
-__device__ __forceinline__ uint32_t narrow(float v, int type) {
-    if (type == DT_BF16) return __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    return __half_as_ushort(__float2half_rn(v));
-}
-__device__ __forceinline__ uint4 pack(const float (&v)[8], int type) {
-    if (type == DT_F32) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+template <int kType>
+__device__ __forceinline__ uint4 pack(const float (&v)[kPer<kType>]) {
     uint32_t u[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) u[i] = narrow(v[2 * i], type) | narrow(v[2 * i + 1], type) << 16;
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (kType == DT_F32) {
+            u[i] = __float_as_uint(v[i]);
+        } else if constexpr (kType == DT_BF16) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            u[i] = *reinterpret_cast<const uint32_t*>(&h);
+        } else {
+            const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
+            u[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+    }
     return make_uint4(u[0], u[1], u[2], u[3]);
 }
 // Element i of a vector as bits, and a vector of which only the elements [lo, hi) exist.
@@ -117,54 +133,102 @@ __device__ __forceinline__ void find_tensor(const Tensors<kMost>& p, unsigned it
     while (item < p.first[t]) --t;
 }
 
-// The elements [lo, hi) of a vector that belong to the tensor, from the vector's index and the tensor's size; all of them as a rule.
-struct Part { int lo, hi; };
-__device__ __forceinline__ Part part_of(unsigned long long vec, int per, int lead, unsigned long long n) {
-    const unsigned long long e = vec * per, end = n + lead;
-    return {e < unsigned(lead) ? int(lead - e) : 0, e + per <= end ? per : e < end ? int(end - e) : 0};
+// An item as a thread sees it: its vectors are first, first + kBlock, ... of the tensor, counted from the 16-byte boundary below its start.
+struct Item {
+    int type, lead, per;
+    bool whole;                                               // every vector of the item is the tensor's altogether
+    unsigned long long first, end;                            // end: the tensor's elements and those in front of it
+};
+template <int kMost>
+__device__ __forceinline__ Item item_of(const Tensors<kMost>& p, unsigned item, int t) {
+    Item v;
+    v.type = p.type[t];
+    v.lead = p.lead[t];
+    v.per = v.type == DT_F32 ? 4 : 8;
+    v.end = p.n[t] + v.lead;
+    const unsigned long long vec = (unsigned long long)(item - p.first[t]) * (kBlock * kVectors);
+    v.first = vec + threadIdx.x;
+    v.whole = (vec > 0 || v.lead == 0) && (vec + kBlock * kVectors) * v.per <= v.end;
+    return v;
 }
+// Which elements of a vector are the tensor's: [lo, hi).
+struct Part { int lo, hi; };
+__device__ __forceinline__ Part part_of(const Item& v, unsigned long long vec) {
+    const unsigned long long e = vec * v.per;
+    return {e < unsigned(v.lead) ? int(v.lead - e) : 0, e + v.per <= v.end ? v.per : e < v.end ? int(v.end - e) : 0};
+}
+// The item's vectors from `base` (a gradient, or what lies in the same way; aligned: on 16 bytes).
+__device__ __forceinline__ void load_item(const Item& v, const char* base, bool aligned, uint4 (&q)[kVectors]) {
+    if (v.whole && aligned) {
+        const uint4* s = reinterpret_cast<const uint4*>(base) + v.first;
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) q[i] = s[i * kBlock];
+    } else {
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            const unsigned long long vec = v.first + i * kBlock;
+            const Part e = part_of(v, vec);
+            q[i] = e.lo == 0 && e.hi == v.per && aligned ? *reinterpret_cast<const uint4*>(base + vec * 16)
+                                                         : load_some(base + vec * 16, v.type, e.lo, e.hi);
+        }
+    }
+}
+template <int kType>
+__device__ __forceinline__ void add_squares(const uint4 (&q)[kVectors], double& total) {
+    constexpr int E = kPer<kType>;
+    float s[kVectors];
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        float v[E];
+        unpack<kType>(q[i], v);
+        any |= q[i].x | q[i].y | q[i].z | q[i].w;
+        s[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) s[i] = fmaf(v[j], v[j], s[i]);
+    }
+    const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+    static_assert(kVectors == 4, "four sums");
+    if ((sum > 1e-28f && sum < 1e36f) || any == 0) {
+        total += double(sum);
+    } else {                                                  // squares that fp32 does not hold (or an infinity, or NaN)
+#pragma unroll
+        for (int i = 0; i < kVectors; ++i) {
+            float v[E];
+            unpack<kType>(q[i], v);
+#pragma unroll 1
+            for (int j = 0; j < E; ++j) total = fma(double(v[j]), double(v[j]), total);
+        }
+    }
+}
+template <int kMost>
+__device__ __forceinline__ const char* base_of(const Tensors<kMost>& p, int t, const Item& v) { return static_cast<const char*>(p.g[t]) - v.lead * (16 / v.per); }
 
+// The next item is on its way while one is worked on.
 template <int kMost>
 __global__ void __launch_bounds__(kBlock, kBlocksPerSm) sum_squares_kernel(const __grid_constant__ Tensors<kMost> p, double* partial) {
     __shared__ double words[kBlock / 32];
     grid_dependency_wait();
     grid_dependents_launch();
     double total = 0.0;
-    int t = 0;
-    for (unsigned item = blockIdx.x; item < p.items; item += gridDim.x) {
+    int t = 0, type = 0;
+    uint4 q[kVectors], next[kVectors];
+    auto fetch = [&](unsigned item) {
         find_tensor(p, item, t);
-        const int type = p.type[t], lead = p.lead[t], per = type == DT_F32 ? 4 : 8;
-        const char* base = static_cast<const char*>(p.g[t]) - lead * (16 / per);
-        const unsigned long long v0 = (unsigned long long)(item - p.first[t]) * (kBlock * kVectors) + threadIdx.x;
-        uint4 q[kVectors];
+        const Item v = item_of(p, item, t);
+        type = v.type;
+        load_item(v, base_of(p, t, v), true, next);
+    };
+    unsigned item = blockIdx.x;
+    if (item < p.items) fetch(item);
+    for (; item < p.items; item += gridDim.x) {
+        const int now = type;
 #pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            const unsigned long long vec = v0 + i * kBlock;
-            const Part e = part_of(vec, per, lead, p.n[t]);
-            q[i] = e.lo == 0 && e.hi == per ? *reinterpret_cast<const uint4*>(base + vec * 16)
-                                            : load_some(base + vec * 16, type, e.lo, e.hi);
-        }
-        float s = 0.f;
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            float v[8];
-            unpack(q[i], type, v);
-            any |= q[i].x | q[i].y | q[i].z | q[i].w;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s = fmaf(v[j], v[j], s);
-        }
-        if ((s > 1e-28f && s < 1e36f) || any == 0) {
-            total += double(s);
-        } else {                                              // squares that fp32 does not hold (or an infinity, or NaN)
-#pragma unroll
-            for (int i = 0; i < kVectors; ++i) {
-                float v[8];
-                unpack(q[i], type, v);
-#pragma unroll 1
-                for (int j = 0; j < 8; ++j) total = fma(double(v[j]), double(v[j]), total);
-            }
-        }
+        for (int i = 0; i < kVectors; ++i) q[i] = next[i];
+        if (p.items - item > gridDim.x) fetch(item + gridDim.x);
+        if (now == DT_F32) add_squares<DT_F32>(q, total);
+        else if (now == DT_BF16) add_squares<DT_BF16>(q, total);
+        else add_squares<DT_F16>(q, total);
     }
     total = block_sum(total, words);
     if (threadIdx.x == 0) partial[blockIdx.x] = total;
@@ -178,6 +242,28 @@ __global__ void __launch_bounds__(kBlock) norm_kernel(const double* partial, int
     if (threadIdx.x == 0) *norm = float(sqrt(s));
 }
 
+// out = factor g (the clipping factor), or w + factor g (-lr times it).
+template <int kType, bool kSgd>
+__device__ __forceinline__ void apply_item(const Item& v, char* out, bool aligned, const uint4 (&q)[kVectors], const uint4 (&w)[kVectors], float factor) {
+    constexpr int E = kPer<kType>;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+        float g[E], x[E];
+        unpack<kType>(q[i], g);
+        if (kSgd) unpack<kType>(w[i], x);
+#pragma unroll
+        for (int j = 0; j < E; ++j) g[j] = kSgd ? fmaf(factor, g[j], x[j]) : factor * g[j];
+        const uint4 r = pack<kType>(g);
+        const unsigned long long vec = v.first + i * kBlock;
+        if (v.whole && aligned) {
+            reinterpret_cast<uint4*>(out)[vec] = r;
+        } else {
+            const Part e = part_of(v, vec);
+            if (e.lo == 0 && e.hi == E && aligned) reinterpret_cast<uint4*>(out)[vec] = r;
+            else store_some(out + vec * 16, kType, r, e.lo, e.hi);
+        }
+    }
+}
 // kSgd: out are the weights, stepped in place; else out = f g.
 template <int kMost, bool kSgd>
 __global__ void __launch_bounds__(kBlock, kBlocksPerSm) apply_kernel(const __grid_constant__ Tensors<kMost> p, const ApplyParams a) {
@@ -188,38 +274,20 @@ __global__ void __launch_bounds__(kBlock, kBlocksPerSm) apply_kernel(const __gri
     const double ratio = double(a.max_norm) / (norm + 1e-6);
     const float f = ratio >= 1.0 ? 1.f : float(ratio);       // (a NaN stays one)
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.norm = float(norm);
-    const float step = -a.lr * f;
+    const float factor = kSgd ? -a.lr * f : f;
     int t = p.count - 1;
     for (unsigned i0 = blockIdx.x; i0 < p.items; i0 += gridDim.x) {
         const unsigned item = p.items - 1 - i0;
         find_tensor(p, item, t);
-        const int type = p.type[t], lead = p.lead[t], per = type == DT_F32 ? 4 : 8;
-        const char* base = static_cast<const char*>(p.g[t]) - lead * (16 / per);
-        char* out = static_cast<char*>(p.out[t]) - lead * (16 / per);
-        const bool even = (reinterpret_cast<uintptr_t>(out) & 15) == 0;      // out lies like g: whole vectors there too
-        const unsigned long long v0 = (unsigned long long)(item - p.first[t]) * (kBlock * kVectors) + threadIdx.x;
+        const Item v = item_of(p, item, t);
+        char* out = static_cast<char*>(p.out[t]) - v.lead * (16 / v.per);
+        const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15) == 0;      // out lies like g: whole vectors there too
         uint4 q[kVectors], w[kVectors];
-        Part e[kVectors];
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            const unsigned long long vec = v0 + i * kBlock;
-            e[i] = part_of(vec, per, lead, p.n[t]);
-            const bool whole = e[i].lo == 0 && e[i].hi == per;
-            q[i] = whole ? *reinterpret_cast<const uint4*>(base + vec * 16) : load_some(base + vec * 16, type, e[i].lo, e[i].hi);
-            if (kSgd) w[i] = whole && even ? *reinterpret_cast<const uint4*>(out + vec * 16) : load_some(out + vec * 16, type, e[i].lo, e[i].hi);
-        }
-#pragma unroll
-        for (int i = 0; i < kVectors; ++i) {
-            float g[8], x[8];
-            unpack(q[i], type, g);
-            if (kSgd) unpack(w[i], type, x);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = kSgd ? fmaf(step, g[j], x[j]) : f * g[j];
-            const uint4 r = pack(g, type);
-            char* to = out + (v0 + i * kBlock) * 16;
-            if (e[i].lo == 0 && e[i].hi == per && even) *reinterpret_cast<uint4*>(to) = r;
-            else store_some(to, type, r, e[i].lo, e[i].hi);
-        }
+        load_item(v, base_of(p, t, v), true, q);
+        if (kSgd) load_item(v, out, aligned, w);
+        if (v.type == DT_F32) apply_item<DT_F32, kSgd>(v, out, aligned, q, w, factor);
+        else if (v.type == DT_BF16) apply_item<DT_BF16, kSgd>(v, out, aligned, q, w, factor);
+        else apply_item<DT_F16, kSgd>(v, out, aligned, q, w, factor);
     }
 }
 
