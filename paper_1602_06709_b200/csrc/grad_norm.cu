@@ -22,9 +22,10 @@ namespace {
 constexpr int kBlock = 256;
 constexpr int kVectors = 4;                                  // 16-byte vectors of an item per thread
 constexpr unsigned kItemBytes = kBlock * kVectors * 16;
-// (500M bf16 gradients clipped: 4 blocks an SM with 4 vectors a thread 512 us, 6 with 4 552, 8 with 2 673, 2 with 8 676; stores or loads marked as
-// streaming 514 and 526)
-constexpr int kBlocksPerSm = 4;
+// Blocks of an SM, which the registers are shared out to: the sums and the step hold 32 registers of loads a thread, the clipped copy half of that
+// (500M bf16: 3 blocks 487 us, 4 492, 5 486, 6 487; gradients of the DNN 72, 71, 70, 70; stores marked as streaming 495, items in the order of
+// the sums 494).
+constexpr int kBlocksPerSm = 4, kCopyBlocksPerSm = 5;
 constexpr int kMostTensors = 640;                            // of a launch: its parameters are limited to 32 KB
 
 // Tensors of a launch.  lead: elements between the 16-byte boundary below a gradient and its start; first: its first item.
@@ -266,7 +267,7 @@ __device__ __forceinline__ void apply_item(const Item& v, char* out, bool aligne
 }
 // kSgd: out are the weights, stepped in place; else out = f g.
 template <int kMost, bool kSgd>
-__global__ void __launch_bounds__(kBlock, kBlocksPerSm) apply_kernel(const __grid_constant__ Tensors<kMost> p, const ApplyParams a) {
+__global__ void __launch_bounds__(kBlock, kSgd ? kBlocksPerSm : kCopyBlocksPerSm) apply_kernel(const __grid_constant__ Tensors<kMost> p, const ApplyParams a) {
     __shared__ double words[kBlock / 32];
     grid_dependency_wait();
     grid_dependents_launch();
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(kBlock, kBlocksPerSm) apply_kernel(const __gri
     }
 }
 
-int most_blocks() { return device_sm_count() * kBlocksPerSm; }
+int most_partials() { return device_sm_count() * kBlocksPerSm; }         // of a launch
 
 // Tensors [from, to) of the call.
 template <int kMost>
@@ -316,7 +317,8 @@ template <int kMost>
 int launch_one(const TensorListArgs& a, int from, int to, bool apply, double* partial, int partials, int& blocks, cudaStream_t st) {
     Tensors<kMost> p;
     fill(p, a, from, to);
-    blocks = p.items < unsigned(most_blocks()) ? int(p.items) : most_blocks();
+    const int most = device_sm_count() * (apply && !a.sgd ? kCopyBlocksPerSm : kBlocksPerSm);
+    blocks = p.items < unsigned(most) ? int(p.items) : most;
     if (blocks == 0) {
         if (!apply || from > 0) return PCL_OK;
         blocks = 1;                                           // (the norm is written all the same)
@@ -336,7 +338,7 @@ int launch_some(const TensorListArgs& a, int from, int to, bool apply, double* p
 }  // namespace
 
 size_t grad_norm_workspace_bytes(int count) {
-    return align_up(size_t((count + kMostTensors - 1) / kMostTensors) * most_blocks() * sizeof(double), 256);
+    return align_up(size_t((count + kMostTensors - 1) / kMostTensors) * most_partials() * sizeof(double), 256);
 }
 
 int launch_grad_norm(const TensorListArgs& a, void* ws, cudaStream_t st) {
