@@ -21,6 +21,9 @@ constexpr int kSlotBytes = 32768;
 constexpr int kStaging = 4096;                                // per epilogue warp: one 32-row x 128-byte tile; SYM and STEP twice that
 constexpr int kSmem16 = kStages16 * kSlotBytes + 8 * kStaging + 1024;
 constexpr int kSmem16Fetch = (kStages16 - 1) * kSlotBytes + 16 * kStaging + 1024;
+constexpr int kColumnBytes = 1024;                           // Q8, per epilogue warp: scales and bias of 128 columns
+constexpr int kStagesQ8 = kStages16 - 1;                      // (whose room that is)
+static_assert(8 * kColumnBytes <= kSlotBytes, "the scales fit in the slot");
 constexpr int kGroupM = 8;                                    // m tiles that share a sweep over n (L2 reuse)
 constexpr int kRunBlocks = 16;                               // kLong: 64-element blocks per accumulator run
 constexpr float kLog2e = 1.4426950408889634f;
@@ -86,6 +89,11 @@ __device__ __forceinline__ uint2 load_four16(const void* base, int i, int n) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) e[j] = i + j < n ? __ldg(s + j) : 0u;
     return make_uint2(e[0] | e[1] << 16, e[2] | e[3] << 16);
+}
+__device__ __forceinline__ float4 four_values(uint2 h, bool bf16) {
+    if (bf16) return make_float4(__uint_as_float(h.x << 16), __uint_as_float(h.x & 0xffff0000u), __uint_as_float(h.y << 16), __uint_as_float(h.y & 0xffff0000u));
+    const float2 lo = half2_value(h.x), hi = half2_value(h.y);
+    return make_float4(lo.x, lo.y, hi.x, hi.y);
 }
 __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
     if (bf16) {
@@ -473,22 +481,19 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                 if (row_ok) { lse = p.lse[row]; g = lse == -INFINITY ? 0.f : p.row_scale[row]; }     // (no finite logit: no gradient)
             }
         }
-        // Q8: the scales and the bias of the warp's columns, four per lane, and its row's scale
-        float4 col_scale = make_float4(0.f, 0.f, 0.f, 0.f), shift = col_scale;
+        // Q8: its row's scale, and the scales and the bias of the warp's columns, which go to its own piece of shared memory while the main loop
+        // runs (kept four to a lane and shuffled from there, 64 values a chunk: 4000 rows, 512 -> 16000 84 us; read from global memory 140)
+        const uint32_t cols_at = c.ring + c.stages * kSlotBytes + 8 * kStaging + (warp - 2) * kColumnBytes;
         if constexpr (kScaled) {
-            const int at = cbase + 4 * (lane & (kHalf / 4 - 1));
+            const int own = lane & (kHalf / 4 - 1), at = cbase + 4 * own;
             if (row_ok) g = __ldg(p.row_scale + row);
-            col_scale = load_four32(p.col_scale, at, p.N);
-            if (p.bias) {
-                if (p.out_type == DT_F32) {
-                    shift = load_four32(static_cast<const float*>(p.bias), at, p.N);
-                } else {
-                    const uint2 b = load_four16(p.bias, at, p.N);
-                    const float2 lo = half2_value(b.x), hi = half2_value(b.y);
-                    shift = p.bf16 ? make_float4(__uint_as_float(b.x << 16), __uint_as_float(b.x & 0xffff0000u), __uint_as_float(b.y << 16), __uint_as_float(b.y & 0xffff0000u))
-                                   : make_float4(lo.x, lo.y, hi.x, hi.y);
-                }
-            }
+            const float4 cs = load_four32(p.col_scale, at, p.N);
+            float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (p.bias) b = p.out_type == DT_F32 ? load_four32(static_cast<const float*>(p.bias), at, p.N) : four_values(load_four16(p.bias, at, p.N), p.bf16 != 0);
+            __syncwarp();                    // (every lane has read the tile before's)
+            st_shared_v4(cols_at + own * 16, cs.x, cs.y, cs.z, cs.w);
+            st_shared_v4(cols_at + kColumnBytes / 2 + own * 16, b.x, b.y, b.z, b.w);
+            __syncwarp();
         }
         if constexpr (kEpi == GEMM16_GENERAL || kEpi == GEMM16_FINAL) {
             // what the epilogue reads is on its way to L2 while the main loop runs
@@ -537,17 +542,13 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
                 }
             }
             if constexpr (kScaled) {
+                const float2 gg = make_float2(g, g), zero = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float cs = j % 4 == 0 ? col_scale.x : j % 4 == 1 ? col_scale.y : j % 4 == 2 ? col_scale.z : col_scale.w;
-                    v[j] = v[j] * g * __shfl_sync(0xffffffffu, cs, cc / 4 + j / 4);
-                }
-                if (p.bias) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        const float b = j % 4 == 0 ? shift.x : j % 4 == 1 ? shift.y : j % 4 == 2 ? shift.z : shift.w;
-                        v[j] += __shfl_sync(0xffffffffu, b, cc / 4 + j / 4);
-                    }
+                for (int u = 0; u < 8; ++u) {
+                    const float4 cs = ld_shared_v4(cols_at + cc * 4 + u * 16), b = ld_shared_v4(cols_at + kColumnBytes / 2 + cc * 4 + u * 16);
+                    const float2 lo = fma2(fma2(make_float2(v[4 * u], v[4 * u + 1]), gg, zero), make_float2(cs.x, cs.y), make_float2(b.x, b.y));
+                    const float2 hi = fma2(fma2(make_float2(v[4 * u + 2], v[4 * u + 3]), gg, zero), make_float2(cs.z, cs.w), make_float2(b.z, b.w));
+                    v[4 * u] = lo.x; v[4 * u + 1] = lo.y; v[4 * u + 2] = hi.x; v[4 * u + 3] = hi.y;
                 }
                 if (p.act == PCL_ACT_RELU) {
 #pragma unroll

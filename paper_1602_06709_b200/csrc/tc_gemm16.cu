@@ -40,7 +40,8 @@ tc_gemm16_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     extern __shared__ uint8_t smem_raw[];
     __shared__ Gemm16Shared sh;
     if (threadIdx.x == 0) { prefetch_tmap(&tm_a); prefetch_tmap(&tm_b); }
-    Gemm16Ctx c = gemm16_begin<kPair>(&sh, smem_raw, p.status);
+    constexpr bool kE4m3 = kEpi == GEMM16_Q8 || kEpi == GEMM16_Q8_STORE;
+    Gemm16Ctx c = gemm16_begin<kPair>(&sh, smem_raw, p.status, kE4m3 ? kStagesQ8 : kStages16);
     const Item16 tile = decode_item(p, c.first);         // (the grid has at most p.items CTAs or pairs)
     grid_dependency_wait();
     grid_dependents_launch();
@@ -49,7 +50,7 @@ tc_gemm16_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant
     if (c.warp == 0) {
         if (!produce_items<kPair, kAMn, kBMn>(c, p, tile, &tm_a, &tm_b)) drain_producer(c);
     } else if (c.warp == 1) {
-        if (c.pair_rank == 0) issue_items<kPair, kAMn, kBMn, kLong, kEpi == GEMM16_Q8 || kEpi == GEMM16_Q8_STORE>(c, p);
+        if (c.pair_rank == 0) issue_items<kPair, kAMn, kBMn, kLong, kE4m3>(c, p);
         __syncwarp();
     } else {
         finish_items<kPair, kEpi, kLong>(c, p, &tm_out, nullptr, p.src, p.out);
