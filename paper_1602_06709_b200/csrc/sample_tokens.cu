@@ -39,6 +39,7 @@ constexpr int kWeightBits = 44;
 struct SampleParams {
     int N, K, bits;                          // bits: a weight of 1 is 2^bits
     int ordered;                             // rows are taken in the order of falling cost
+    int ranks;                               // blocks that share a row
     const void* logits;
     const float *uniform, *temperature, *top_p, *min_p;
     const int* top_k;
@@ -106,6 +107,7 @@ struct Row {
     const T* base;                           // the row's first element
     const uint4* aligned;                    // vector 0
     int K, shift, vectors, first_whole;
+    int lo, hi;                              // the vectors that this block works on
     unsigned whole;                          // vectors that are the row's altogether, from first_whole on
     __device__ __forceinline__ Row(const void* logits, size_t row, int k) : base(static_cast<const T*>(logits) + row * k), K(k) {
         shift = int(row * k % E);
@@ -114,6 +116,13 @@ struct Row {
         first_whole = shift ? 1 : 0;
         const int last = (K + shift) % E ? vectors - 1 : vectors;
         whole = last > first_whole ? unsigned(last - first_whole) : 0u;
+        lo = 0;
+        hi = vectors;
+    }
+    __device__ __forceinline__ void part(int rank, int ranks) {
+        const int each = (vectors + ranks - 1) / ranks;
+        lo = min(rank * each, vectors);
+        hi = min(lo + each, vectors);
     }
     __device__ __forceinline__ float value(int id) const {
         const uint32_t u[4] = {Vec<T>::load(base, id), 0u, 0u, 0u};
@@ -137,11 +146,11 @@ struct Row {
         const uint4 q = __ldg(aligned + c);
         u[0] = q.x; u[1] = q.y; u[2] = q.z; u[3] = q.w;
     }
-    // f(vector, its index) for every vector, the block's threads side by side; kMany vectors are loaded before the first is used
+    // f(vector, its index) for every vector of the block, its threads side by side; kMany vectors are loaded before the first is used
     template <int kMany, class F>
     __device__ __forceinline__ void each(F&& f) const {
-        const int n = int(blockDim.x), end = first_whole + int(whole);
-        int c = first_whole + int(threadIdx.x);
+        const int n = int(blockDim.x), end = min(first_whole + int(whole), hi);
+        int c = max(first_whole, lo) + int(threadIdx.x);
         uint32_t u[kMany][4];
         for (; c + (kMany - 1) * n < end; c += kMany * n) {
 #pragma unroll
@@ -158,7 +167,7 @@ struct Row {
         // the row's first and last vector, where they are not whole
         if (threadIdx.x < 2) {
             c = threadIdx.x ? vectors - 1 : 0;
-            if ((c < first_whole || c >= end) && (threadIdx.x == 0 || vectors > 1)) {
+            if (unsigned(c - first_whole) >= whole && c >= lo && c < hi && (threadIdx.x == 0 || vectors > 1)) {
                 load(c, u[0]);
                 f(u[0], c);
             }
@@ -257,6 +266,72 @@ struct Shared {
     u64 above, found_front;
     uint32_t key_lo, key_hi, ties;
     float border_z;
+    u64 swap[2];                             // what this block tells the others of its cluster
+};
+
+// The blocks that share a row (one, or a cluster): what they tell each other.  Every block makes the same calls.
+__device__ __forceinline__ u64 load_of(const u64* p, uint32_t rank) {
+    u64 v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(map_to_cta(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t load_of(const uint32_t* p, uint32_t rank) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_to_cta(p, rank)) : "memory");
+    return v;
+}
+template <bool kMany>
+struct Team {
+    Shared& s;
+    uint32_t rank, ranks;
+    int turn = 0;                            // (two words in turn: one barrier each is enough)
+    __device__ __forceinline__ Team(Shared& shared, uint32_t r) : s(shared), rank(kMany ? cluster_ctarank() : 0u), ranks(kMany ? r : 1u) {}
+    __device__ __forceinline__ void sync() const {
+        if constexpr (kMany) cluster_sync_all();
+        else __syncthreads();
+    }
+    // Before the first block that others do without, and before any block ends: what they read from each other has been read.
+    __device__ __forceinline__ void part() const {
+        if constexpr (kMany) cluster_sync_all();
+    }
+    __device__ __forceinline__ bool first() const { return !kMany || rank == 0; }
+    // f over the blocks' values, in the blocks' order; before: over those of the blocks in front of this one
+    template <class F>
+    __device__ __forceinline__ u64 all(u64 mine, F&& f, u64* before = nullptr) {
+        if (before) *before = 0;
+        if constexpr (!kMany) return mine;
+        if (threadIdx.x == 0) s.swap[turn] = mine;
+        cluster_sync_all();
+        u64 v = load_of(&s.swap[turn], 0);
+        for (uint32_t r = 1; r < ranks; ++r) {
+            if (before && r == rank) *before = v;
+            v = f(v, load_of(&s.swap[turn], r));
+        }
+        turn ^= 1;
+        return v;
+    }
+    __device__ __forceinline__ u64 sum(u64 mine, u64* before = nullptr) { return all(mine, [](u64 a, u64 b) { return a + b; }, before); }
+    // A token to the first block's list.
+    __device__ __forceinline__ void push(u64 key, u64 weight, int most) const {
+        if constexpr (kMany) {
+            uint32_t at;
+            asm volatile("atom.shared::cluster.add.u32 %0, [%1], 1;" : "=r"(at) : "r"(map_to_cta(&s.listed, 0)) : "memory");
+            if (int(at) >= most) return;
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_cta(&s.key[at], 0)), "l"(key) : "memory");
+            asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_to_cta(&s.weight[at], 0)), "l"(weight) : "memory");
+        } else {
+            const int at = atomicAdd(&s.listed, 1);
+            if (at < most) { s.key[at] = key; s.weight[at] = weight; }
+        }
+    }
+    // a word of the first block, or of any
+    template <class W>
+    __device__ __forceinline__ W of(const W& word, uint32_t r = 0) const {
+        if constexpr (kMany) return load_of(&word, r);
+        else return word;
+    }
+    __device__ __forceinline__ int of(const int& word) const { return int(of(reinterpret_cast<const uint32_t&>(word))); }
+    __device__ __forceinline__ float of(const float& word) const { return __uint_as_float(of(reinterpret_cast<const uint32_t&>(word))); }
 };
 
 // Where the part kept ends: tokens above `z` are kept, and of those equal to it the ones up to `id` (kAllIds: all of them).
@@ -390,11 +465,11 @@ __device__ __forceinline__ u64 vector_weight(const Scale& sc, const uint32_t (&u
     }
     return sum - Vec<T>::E * Scale::kRaw;
 }
-// The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the whole row.
+// The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the block's vectors.
 template <int kThreads, class T, class F>
 __device__ __forceinline__ int locate(Shared& s, const Row<T>& row, int each, u64 target, F&& f) {
     constexpr int E = Vec<T>::E;
-    int c0 = 0, c1 = row.vectors;
+    int c0 = row.lo, c1 = row.hi;
     u64 front = 0;
     for (;;) {
         const int pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
@@ -548,14 +623,14 @@ __device__ __forceinline__ float lowest_with(float guess, float top, F&& f) {
 //   of each bin to 1 part in 4000; the border lies in the bins, one or two as a rule, where the weight up to there can be top_p of all.  One pass then
 //   takes the exact weights: of all tokens, of those above these bins, and those in them go to the list, where the exact border is found.
 constexpr int kCountBits = 13;               // of a bin's word; the rest holds the places
-template <int kThreads, class T, class Part>
-__device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, double unit, float top_p, float least, int each,
+template <int kThreads, bool kMany, class T, class Part>
+__device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<T>& row, const Scale& sc, float top, float from, double unit, float top_p, float least, int each,
                                         const Part& part_of, u64& total, Border& border) {
     constexpr int E = Vec<T>::E, kEach = kBins / kThreads;
     const float scale = float(kBins) / (top - from);
     const bool usable = scale > 0.f && scale < 1e30f;
     for (int i = threadIdx.x; i < kBins; i += kThreads) s.count[i] = 0;
-    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; s.listed = 0; s.border_id = -1; }
+    if (threadIdx.x == 0) { s.bin = kBins; s.last_bin = kBins - 1; }
     __syncthreads();
     uint32_t inside = 0;
     if (usable)
@@ -570,7 +645,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
                 }
             }
         });
-    __syncthreads();
+    team.sync();
     // bounds of the weight up to each bin and of all of it: a token's place is known to 1/64 of a bin (and a rounding of 1/1000), and within a bin
     // exp(-f * width) lies between 1 - f width and that plus (f width)^2 / 2
     const double width = double(top - from) / kBins * sc.per16 * (0.69314718055994530942 / 16.0);       // of a bin, in nats
@@ -579,9 +654,14 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int b = kEach * threadIdx.x + i;
-        const uint32_t word = s.count[b], n = word & ((1u << kCountBits) - 1);
+        uint32_t n = 0, place = 0;
+        for (uint32_t r = 0; r < team.ranks; ++r) {
+            const uint32_t word = team.of(s.count[b], r);
+            n += word & ((1u << kCountBits) - 1);
+            place += word >> kCountBits;
+        }
         counted += n;
-        const double at = n ? unit * exp(-double(b) * width) : 0.0, places = double(word >> kCountBits) * (1.0 / 64.0) * width;
+        const double at = n ? unit * exp(-double(b) * width) : 0.0, places = double(place) * (1.0 / 64.0) * width;
         lows[i] = fmax(at * (double(n) - places - double(n) * width * (1.0 / 64.0 + 1e-3)) - double(n), 0.0);
         highs[i] = at * (double(n) - places + double(n) * (width * 1e-3 + 0.5 * width * width)) + double(n);      // (weights are whole numbers)
         if (b == kBins - 1) { lows[i] = 0.0; highs[i] = double(n) * (at * (1.0 + 1e-3 * width) + 1.0); }           // (the last bin may reach further down)
@@ -593,6 +673,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
     uint32_t all_counted, all_inside;
     block_scan<kThreads>(s.warp_word, counted, all_counted);
     block_scan<kThreads>(s.warp_count, inside, all_inside);
+    all_inside = uint32_t(team.sum(all_inside));
     if (!usable || all_counted != all_inside) return false;    // (a bin's count has overflown)
     const double want_low = double(top_p) * all_low * (1.0 - 1e-9), want_high = double(top_p) * all_high * (1.0 + 1e-9) + 1.0;
     int first = kBins, last = kBins - 1;
@@ -620,7 +701,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
         return false;
     }
     u64 above = 0, sum = 0;
-    sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&u)[4], int c) -> u64 {
+    sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&u)[4], int c) -> u64 {
         u64 kept = 0;
 #pragma unroll
         for (int i = 0; i < E; i += 4) {
@@ -641,22 +722,20 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
                 const int id = int(row.first(c)) + i;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (z[j] >= in && z[j] < over) {
-                        const int l = atomicAdd(&s.listed, 1);
-                        if (l < kList) { s.key[l] = u64(order(z[j] + 0.f)) << 32 | uint32_t(~uint32_t(id + j)); s.weight[l] = w[j]; }
-                    }
+                    if (z[j] >= in && z[j] < over) team.push(u64(order(z[j] + 0.f)) << 32 | uint32_t(~uint32_t(id + j)), w[j], kList);
             }
         }
         above += kept;
         return kept;
     });
-    total = block_sum<kThreads>(s, sum);
-    above = block_sum<kThreads>(s, above);
-    const int n = s.listed;
+    total = team.sum(block_sum<kThreads>(s, sum));
+    above = team.sum(block_sum<kThreads>(s, above));
+    const int n = team.of(s.listed);
     const u64 want = part_of(total);
     if (n > kList || above >= want) return false;              // (the second is not met)
-    // the border: the key at which `want` is reached
-    if (n <= kPairs) {
+    // the border: the key at which `want` is reached, for the first block to find
+    if (!team.first()) {
+    } else if (n <= kPairs) {
         for (int i = threadIdx.x; i < n; i += kThreads) {
             const u64 mine = s.key[i];
             u64 before = above;
@@ -674,13 +753,16 @@ __device__ __forceinline__ bool nucleus(Shared& s, const Row<T>& row, const Scal
         }
         if (threadIdx.x == 0 && key) { s.border_z = unorder(uint32_t(key >> 32)); s.border_id = int(~uint32_t(key)); }
     }
-    __syncthreads();
-    if (s.border_id < 0) return false;                         // (not met)
-    border = {s.border_z, s.border_id};
+    team.sync();
+    border = {team.of(s.border_z), team.of(s.border_id)};
+    if (border.id < 0) return false;                           // (not met)
     const u64 last_key = u64(order(border.z)) << 32 | uint32_t(~uint32_t(border.id));
-    for (int i = threadIdx.x; i < n; i += kThreads)
-        if (s.key[i] >= last_key && unorder(uint32_t(s.key[i] >> 32)) >= least)
-            atomicAdd(&s.piece[(int(~uint32_t(s.key[i])) + row.shift) / E / (32 * each)], s.weight[i]);
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const u64 key = team.of(s.key[i]);
+        const int c = (int(~uint32_t(key)) + row.shift) / E;
+        if (key >= last_key && unorder(uint32_t(key >> 32)) >= least && c >= row.lo && c < row.hi)
+            atomicAdd(&s.piece[(c - row.lo) / (32 * each)], team.of(s.weight[i]));
+    }
     __syncthreads();
     return true;
 }
@@ -711,7 +793,7 @@ __device__ __forceinline__ int costly_first(Shared& s, const SampleParams& p) {
     return s.found;
 }
 
-template <class T, int kThreads>
+template <class T, int kThreads, bool kMany>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const SampleParams p) {
     constexpr int E = Vec<T>::E, kWarps = kThreads / 32;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -719,8 +801,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_wait();
     grid_dependents_launch();
-    const int n = p.ordered ? costly_first<kThreads>(s, p) : int(blockIdx.x);
-    const Row<T> row(p.logits, n, p.K);
+    Team<kMany> team(s, uint32_t(p.ranks));
+    const int n = p.ordered ? costly_first<kThreads>(s, p) : int(blockIdx.x / team.ranks);
+    Row<T> row(p.logits, n, p.K);
+    if constexpr (kMany) row.part(int(team.rank), int(team.ranks));
+    if (threadIdx.x == 0) { s.listed = 0; s.border_id = -1; }
     const float temperature = p.temperature ? p.temperature[n] : 1.f;
     int k = p.top_k ? p.top_k[n] : 0;
     const float top_p = p.top_p ? p.top_p[n] : 1.f, min_p = p.min_p ? p.min_p[n] : 0.f, u = p.uniform[n];
@@ -746,8 +831,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (lane == 0) s.warp_z[warp] = top;
     __syncthreads();
     for (int i = 0; i < kWarps; ++i) top = __uint_as_float(Vec<float>::max2(__float_as_uint(top), __float_as_uint(s.warp_z[i])));
+    top = __uint_as_float(uint32_t(team.all(__float_as_uint(top), [](u64 a, u64 b) { return u64(Vec<float>::max2(uint32_t(a), uint32_t(b))); })));
     if (top != top || top == -INFINITY || temperature != temperature) {
-        if (threadIdx.x == 0) answer(-1, NAN);
+        if (threadIdx.x == 0 && team.first()) answer(-1, NAN);
+        team.part();
         return;
     }
     if (temperature <= 0.f || k == 1 || top_p <= 0.f) {       // the first token that has the maximum
@@ -762,7 +849,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (lane == 0) s.warp_word[warp] = at;
         __syncthreads();
         for (int i = 0; i < kWarps; ++i) at = min(at, s.warp_word[i]);
-        if (threadIdx.x == 0) answer(int(at), 0.f);
+        at = uint32_t(team.all(at, [](u64 a, u64 b) { return a < b ? a : b; }));
+        if (threadIdx.x == 0 && team.first()) answer(int(at), 0.f);
+        team.part();
         return;
     }
     const double per16 = fmax(16.0 * 1.4426950408889634074 / double(temperature), 1e-290);         // (an infinite temperature: all weights 1)
@@ -788,17 +877,25 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 
     // ---- small top-k
     if (k > 0 && k <= kThreads / 2 && !infinite) {
-        // the k-th largest of the threads' maxima, from its highest bit down, or a bound that few more reach (0: fewer than k are finite)
+        // the q-th largest of the threads' maxima, from its highest bit down, or a bound that few more reach (0: fewer than q are finite).  Of several
+        // blocks: their share of k each, and the lowest of their bounds; where one has too few, k each and the highest.
         const uint32_t key = mine == -INFINITY ? 0u : order(mine);
-        uint32_t bound = 0;
-        for (int b = 31; b >= Vec<T>::kLowBit; --b) {
-            const uint32_t next = bound | 1u << b;
-            const int reach = __syncthreads_count(key >= next);
-            if (reach >= k) bound = next;
-            if (reach >= k && reach <= k + 16) break;
+        auto bound_of = [&](int q) {
+            uint32_t found = 0;
+            for (int b = 31; b >= Vec<T>::kLowBit; --b) {
+                const uint32_t next = found | 1u << b;
+                const int reach = __syncthreads_count(key >= next);
+                if (reach >= q) found = next;
+                if (reach >= q && reach <= q + 16) break;
+            }
+            return found;
+        };
+        uint32_t bound = bound_of((k + int(team.ranks) - 1) / int(team.ranks));
+        if constexpr (kMany) {
+            bound = uint32_t(team.all(bound, [](u64 a, u64 b) { return a < b ? a : b; }));
+            if (bound == 0) bound = uint32_t(team.all(bound_of(k), [](u64 a, u64 b) { return a > b ? a : b; }));
         }
         // (the bits of a negative value's key below kLowBit are ones: the bound may be a little low, which is as good)
-        if (threadIdx.x == 0) s.listed = 0;
         __syncthreads();
         const float bound_z = bound > order(-INFINITY) ? unorder(bound) : kLowest;
         if (key >= bound && mine > -INFINITY)
@@ -807,15 +904,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
                     const float z = Vec<T>::get(q, i);
-                    if (z >= bound_z) {
-                        const int at = atomicAdd(&s.listed, 1);
-                        if (at < kList) s.key[at] = u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(row.first(c) + i));
-                    }
+                    if (z >= bound_z) team.push(u64(order(z + 0.f)) << 32 | uint32_t(~uint32_t(row.first(c) + i)), 0ull, kMostSmall);
                 }
             });
-        __syncthreads();
-        const int count = s.listed;
+        team.sync();
+        const int count = team.of(s.listed);
         if (count <= kMostSmall) {
+            team.part();
+            if (!team.first()) return;
             constexpr int kEach = kMostSmall / kThreads;
             u64 before[kEach], sum = 0, kept[kEach];
             for (int i = threadIdx.x; i < count; i += kThreads) s.weight[i] = sc.weight(unorder(uint32_t(s.key[i] >> 32)));
@@ -861,11 +957,22 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
 
     // ---- where the part kept ends
-    const int each = (row.vectors + 32 * kPieces - 1) / (32 * kPieces);           // vectors of a piece per lane
     Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
+    const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), double(kLowest)));    // (what has any weight lies above)
+    auto pieces_each = [&] { return (row.hi - row.lo + 32 * kPieces - 1) / (32 * kPieces); };        // vectors of a piece per lane
+    u64 whole = 0;
+    if (by_p && k == 0 && !infinite) summed = nucleus<kThreads>(s, team, row, sc, top, floor_z, unit, top_p, least, pieces_each(), part_of, whole, border);
+    const bool by_least = least > kLowest && border.z == least;                                      // (min-p keeps less than top-p in any case)
+    const bool alone = kMany && (infinite || k > 0 || (by_p && !summed && !by_least));               // what is rare or needs several passes is the first
+    if (alone) {                                                                                     // block's
+        team.part();
+        if (!team.first()) return;
+        row.part(0, 1);
+    }
+    const int each = pieces_each();
     auto nth_of = [&](float z, uint32_t ties) {                // the border at that many tokens of value z
-        sum_pieces<kThreads>(s, row, 0, row.vectors, each, by_value(row, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; }));
+        sum_pieces<kThreads>(s, row, row.lo, row.hi, each, by_value(row, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; }));
         const int id = locate<kThreads>(s, row, each, u64(ties) - 1, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
         __syncthreads();
         return Border{z, id};
@@ -881,32 +988,27 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (by_p) count = (part_of(count * one) + one - 1) / one;
         border = nth_of(INFINITY, uint32_t(count));
     } else {
-        const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), double(kLowest)));    // (what has any weight lies above)
         float z = 0.f;
         uint32_t ties = 0;
         if (k > 0 && select<kThreads, false>(s, row, sc, top, floor_z, u64(k), z, ties)) border = nth_of(z, ties);     // (else fewer have any weight)
-        if (by_p) {
+        if (by_p && !summed && !by_least) {
+            __syncthreads();
             u64 sum = 0;
-            if (k == 0) summed = nucleus<kThreads>(s, row, sc, top, floor_z, unit, top_p, least, each, part_of, sum, border);
-            if (!summed && !(k == 0 && border.z == least && least > kLowest)) {
-                __syncthreads();
-                sum = 0;
-                row.template each<2>([&](uint32_t (&q)[4], int c) {
+            row.template each<2>([&](uint32_t (&q)[4], int c) {
 #pragma unroll
-                    for (int i = 0; i < E; ++i) {
-                        const float v = Vec<T>::get(q, i);
-                        sum += sc.weight(v, border.keeps(v, int(row.first(c)) + i));
-                    }
-                });
-                sum = block_sum<kThreads>(s, sum);
-                // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
-                const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
-                const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
-                const float from = float(fmax(low, double(floor_z)));
-                const u64 want = part_of(sum);
-                if (select<kThreads, true>(s, row, sc, top, from, want, z, ties) || select<kThreads, true>(s, row, sc, top, floor_z, want, z, ties))
-                    border = nth_of(z, ties);                  // (the second: top_p next to 1)
-            }
+                for (int i = 0; i < E; ++i) {
+                    const float v = Vec<T>::get(q, i);
+                    sum += sc.weight(v, border.keeps(v, int(row.first(c)) + i));
+                }
+            });
+            sum = block_sum<kThreads>(s, sum);
+            // what top-p can keep: not what weighs less than (1 - top_p) / K of the total, a little lower so that roundings exclude nothing
+            const double share = (1.0 - double(top_p)) * double(sum) / unit / double(p.K);
+            const double low = double(top) + double(temperature) * (log(share) - 1e-3) - 1e-6 * fabs(double(top));
+            const float from = float(fmax(low, double(floor_z)));
+            const u64 want = part_of(sum);
+            if (select<kThreads, true>(s, row, sc, top, from, want, z, ties) || select<kThreads, true>(s, row, sc, top, floor_z, want, z, ties))
+                border = nth_of(z, ties);                      // (the second: top_p next to 1)
         }
         if (least > border.z) border = {least, kAllIds};
     }
@@ -916,34 +1018,46 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (!summed) {
         __syncthreads();
         if (infinite || border.id != kAllIds)
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, by_value(row, kept_weight));
+            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, by_value(row, kept_weight));
         else if (border.z > kLowest)
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&q)[4], int) { return vector_weight<false, T>(sc, q, border.z); });
+            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&q)[4], int) { return vector_weight<false, T>(sc, q, border.z); });
         else
-            sum_pieces<kThreads>(s, row, 0, row.vectors, each, [&](const uint32_t (&q)[4], int) { return vector_weight<true, T>(sc, q, 0.f); });
+            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&q)[4], int) { return vector_weight<true, T>(sc, q, 0.f); });
     }
-    const u64 total = block_sum<kThreads>(s, int(threadIdx.x) < (row.vectors + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
-    const int token = locate<kThreads>(s, row, each, target_of(total), kept_weight);
-    if (threadIdx.x == 0) answer(token, logprob_of(row.value(token), total));
+    const u64 own = block_sum<kThreads>(s, int(threadIdx.x) < (row.hi - row.lo + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
+    u64 front = 0;
+    const u64 total = alone ? own : team.sum(own, &front), target = target_of(total);
+    if (target >= front && target - front < own) {
+        const int token = locate<kThreads>(s, row, each, target - front, kept_weight);
+        if (threadIdx.x == 0) answer(token, logprob_of(row.value(token), total));
+    }
+    if (!alone) team.part();
 }
 
-template <class T, int kThreads>
+template <class T, int kThreads, bool kMany>
 int launch_threads(const SampleParams& p, cudaStream_t st) {
     static PerDeviceOnce once;
-    auto kernel = sample_kernel<T, kThreads>;
+    auto kernel = sample_kernel<T, kThreads, kMany>;
     const int rc = once.run([&] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(Shared))) == cudaSuccess ? PCL_OK : PCL_ERR_CUDA;
     });
-    return rc != PCL_OK ? rc : launch_chained(kernel, dim3(p.N), dim3(kThreads), sizeof(Shared), st, 1, p);
+    return rc != PCL_OK ? rc : launch_chained(kernel, dim3(unsigned(p.N) * p.ranks), dim3(kThreads), sizeof(Shared), st, unsigned(p.ranks), p);
 }
 template <class T>
 int launch_sample(const SampleParams& p, cudaStream_t st) {
-    // two blocks an SM overlap one's loads with the other's arithmetic; up to one row an SM, all threads go to it
+    // Two blocks an SM overlap one's loads with the other's arithmetic.  Up to one row an SM, all threads go to it; with fewer and long rows a cluster of
+    // up to 8 SMs does, each with 16384 tokens or more (below that what the blocks tell each other costs more than it saves: 1 x 32003 by top-k
+    // 9.5 us on one SM, 12.5 on four; 1 x 131072 without a filter 28.7 on one, 14.1 on eight).  Clusters of 8 fill half of the SMs at most: more do not
+    // find their 8 next to each other at once (16 x 131072: 27 us on clusters of 8, 17 on 30 clusters of 4).
     const int sms = device_sm_count();
-    if (p.N <= sms) return launch_threads<T, 1024>(p, st);
     SampleParams q = p;
+    q.ranks = 1;
+    if (p.N <= sms) {
+        while (q.ranks < 8 && p.N * q.ranks * 2 <= (q.ranks < 4 ? sms : sms / 2) && p.K / (q.ranks * 2) >= 16384) q.ranks *= 2;
+        return q.ranks > 1 ? launch_threads<T, 1024, true>(q, st) : launch_threads<T, 1024, false>(q, st);
+    }
     q.ordered = p.N > 2 * sms && p.N <= kMostOrdered && (p.top_k || p.top_p || p.temperature);
-    return launch_threads<T, 512>(q, st);
+    return launch_threads<T, 512, false>(q, st);
 }
 
 }  // namespace
@@ -953,7 +1067,7 @@ size_t sample_tokens_workspace_bytes(int, int) { return 0; }
 int launch_sample_tokens(const SampleArgs& a, void*, cudaStream_t st) {
     int log_k = 0;
     while ((1ll << log_k) < a.K) ++log_k;
-    const SampleParams p{a.N, a.K, log_k > 18 ? 62 - log_k : kWeightBits, 0, a.logits, a.uniform, a.temperature, a.top_p, a.min_p, a.top_k, a.token, a.logprob};
+    const SampleParams p{a.N, a.K, log_k > 18 ? 62 - log_k : kWeightBits, 0, 1, a.logits, a.uniform, a.temperature, a.top_p, a.min_p, a.top_k, a.token, a.logprob};
     LaunchScope scope(KID_SAMPLE, double(a.N) * a.K * dtype_bytes(a.type), st);
     switch (a.type) {
         case DT_F32: return launch_sample<float>(p, st);

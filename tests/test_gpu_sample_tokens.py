@@ -208,6 +208,40 @@ def test_values_at_the_ends_of_the_settings(name, value):
     check(z, ends)
 
 
+@pytest.mark.parametrize("N,K", [(1, 32768), (4, 131075), (9, 262143), (18, 65537), (37, 65541), (74, 32771)])
+@pytest.mark.parametrize("kinds", FILTERS)
+def test_rows_shared_by_blocks(N, K, kinds):
+    """Long rows and few of them: several blocks take a row together."""
+    for t, kind in ((torch.bfloat16, "normal"), (torch.float32, "steps")):
+        check(logits(N, K, t, N + K, kind), params(N, K + 5, kinds))
+
+
+@pytest.mark.parametrize("K", [131072, 131075])
+def test_special_rows_shared_by_blocks(K):
+    z = logits(16, K, torch.float32, 9)
+    z[0] = -INF
+    z[1, K - 2] = NAN
+    z[2, 40] = INF
+    z[3, [5, K // 2, K - 1]] = INF
+    z[4] = -INF
+    z[4, K - 1] = -3.0
+    z[5, :] = torch.finfo(torch.float32).min
+    z[6, 9] = torch.finfo(torch.float32).max
+    z[7] = -INF                             # all that is left lies with one block
+    z[7, K - 300:] = logits(1, 300, torch.float32, 10)[0]
+    z[8] = -INF
+    z[8, ::K // 20] = 0.25
+    z[11] = 0.0                             # equal tokens: the border lies far on
+    z[12] = 0.0
+    p = {"uniform": np.float32([0.5, 0.5, 0.5, 0.7, 0.5, 0.25, 0.999, 0.5, 0.9, 0.5, 0.5, 0.95, 0.95, 0.6, 0.999, 0.0]),
+         "temperature": np.float32([1, 1, 1, 1, 1, 1, 1, 1, 1, 0.0, INF, 1, 1, 1, 1, 1]),
+         "top_k": np.int32([0, 0, 0, 0, 3, 0, 0, 50, 40, 0, 0, 0, 90000, 5000, 600, K]),
+         "top_p": np.float32([0.9, 1, 0.9, 0.9, 0.9, 0.5, 0.5, 0.5, 1, 0.5, 0.3, 0.8, 1, 0.9, 1, 1]),
+         "min_p": np.float32([0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 1e-3, 0])}
+    for rows in (slice(0, 16), slice(0, 5), slice(5, 8), slice(8, 16), slice(13, 14)):
+        check(z[rows].clone(), {k: v[rows] for k, v in p.items()})
+
+
 def test_row_starts_off_16_bytes():
     """An odd row length in 16-bit types: rows start at every place of 16 bytes."""
     for t in (torch.bfloat16, torch.float16):
