@@ -101,13 +101,13 @@ template <> struct Vec<__half> {
 
 // A row, in vectors that are aligned in memory: vector c holds the elements c * E - shift ...; what of the first and the last
 // one is not the row's reads as -inf.
-template <class T>
+template <class T, bool kPart>
 struct Row {
     static constexpr int E = Vec<T>::E;
     const T* base;                           // the row's first element
     const uint4* aligned;                    // vector 0
     int K, shift, vectors, first_whole;
-    int lo, hi;                              // the vectors that this block works on
+    int from, to;                            // kPart: the vectors that this block works on
     unsigned whole;                          // vectors that are the row's altogether, from first_whole on
     __device__ __forceinline__ Row(const void* logits, size_t row, int k) : base(static_cast<const T*>(logits) + row * k), K(k) {
         shift = int(row * k % E);
@@ -116,14 +116,16 @@ struct Row {
         first_whole = shift ? 1 : 0;
         const int last = (K + shift) % E ? vectors - 1 : vectors;
         whole = last > first_whole ? unsigned(last - first_whole) : 0u;
-        lo = 0;
-        hi = vectors;
+        from = 0;
+        to = vectors;
     }
     __device__ __forceinline__ void part(int rank, int ranks) {
         const int each = (vectors + ranks - 1) / ranks;
-        lo = min(rank * each, vectors);
-        hi = min(lo + each, vectors);
+        from = min(rank * each, vectors);
+        to = min(from + each, vectors);
     }
+    __device__ __forceinline__ int lo() const { return kPart ? from : 0; }
+    __device__ __forceinline__ int hi() const { return kPart ? to : vectors; }
     __device__ __forceinline__ float value(int id) const {
         const uint32_t u[4] = {Vec<T>::load(base, id), 0u, 0u, 0u};
         return Vec<T>::get(u, 0);
@@ -149,8 +151,8 @@ struct Row {
     // f(vector, its index) for every vector of the block, its threads side by side; kMany vectors are loaded before the first is used
     template <int kMany, class F>
     __device__ __forceinline__ void each(F&& f) const {
-        const int n = int(blockDim.x), end = min(first_whole + int(whole), hi);
-        int c = max(first_whole, lo) + int(threadIdx.x);
+        const int n = int(blockDim.x), end = kPart ? min(first_whole + int(whole), to) : first_whole + int(whole);
+        int c = (kPart ? max(first_whole, from) : first_whole) + int(threadIdx.x);
         uint32_t u[kMany][4];
         for (; c + (kMany - 1) * n < end; c += kMany * n) {
 #pragma unroll
@@ -167,7 +169,7 @@ struct Row {
         // the row's first and last vector, where they are not whole
         if (threadIdx.x < 2) {
             c = threadIdx.x ? vectors - 1 : 0;
-            if (unsigned(c - first_whole) >= whole && c >= lo && c < hi && (threadIdx.x == 0 || vectors > 1)) {
+            if (unsigned(c - first_whole) >= whole && c >= lo() && c < hi() && (threadIdx.x == 0 || vectors > 1)) {
                 load(c, u[0]);
                 f(u[0], c);
             }
@@ -408,8 +410,8 @@ __device__ __forceinline__ void find_bin(Shared& s, u64 want) {
 
 // Sums of f(vector, its index) over pieces of consecutive ids: the vectors [c0, c1) in pieces of 32 * each, a warp to a piece at a time, to s.piece
 // (kAdd: added to it).  The next vector is on its way while one is worked on.
-template <int kThreads, bool kAdd = false, class T, class F>
-__device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0, int c1, int each, F&& f) {
+template <int kThreads, bool kAdd = false, class T, bool kPart, class F>
+__device__ __forceinline__ void sum_pieces(Shared& s, const Row<T, kPart>& row, int c0, int c1, int each, F&& f) {
     const int lane = threadIdx.x & 31, pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
     int q = threadIdx.x >> 5, o = 0, c = c0 + q * each * 32 + lane;
     u64 sum = 0;
@@ -440,8 +442,8 @@ __device__ __forceinline__ void sum_pieces(Shared& s, const Row<T>& row, int c0,
     __syncthreads();
 }
 // f of values and ids, one by one, as a function of a vector.
-template <class T, class F>
-__device__ __forceinline__ auto by_value(const Row<T>& row, F&& f) {
+template <class T, bool kPart, class F>
+__device__ __forceinline__ auto by_value(const Row<T, kPart>& row, F&& f) {
     return [&row, f](const uint32_t (&u)[4], int c) mutable -> u64 {
         const int id = int(row.first(c));
         u64 sum = 0;
@@ -466,10 +468,10 @@ __device__ __forceinline__ u64 vector_weight(const Scale& sc, const uint32_t (&u
     return sum - Vec<T>::E * Scale::kRaw;
 }
 // The id at which the sum of f over rising ids first exceeds `target`, given s.piece of the block's vectors.
-template <int kThreads, class T, class F>
-__device__ __forceinline__ int locate(Shared& s, const Row<T>& row, int each, u64 target, F&& f) {
+template <int kThreads, class T, bool kPart, class F>
+__device__ __forceinline__ int locate(Shared& s, const Row<T, kPart>& row, int each, u64 target, F&& f) {
     constexpr int E = Vec<T>::E;
-    int c0 = row.lo, c1 = row.hi;
+    int c0 = row.lo(), c1 = row.hi();
     u64 front = 0;
     for (;;) {
         const int pieces = (c1 - c0 + 32 * each - 1) / (32 * each);
@@ -510,8 +512,8 @@ __device__ __forceinline__ int locate(Shared& s, const Row<T>& row, int each, u6
 
 // The value at which the tokens in falling order, down to `from`, reach `want` of weight, or of their number, and how many tokens of that
 // value that takes; false: they do not.  For whatever does not fit in the list.
-template <int kThreads, bool kByWeight, class T>
-__device__ __noinline__ bool select(Shared& s, const Row<T>& row, const Scale& sc, float top, float from, u64 want, float& border, uint32_t& ties) {
+template <int kThreads, bool kByWeight, class T, bool kPart>
+__device__ __noinline__ bool select(Shared& s, const Row<T, kPart>& row, const Scale& sc, float top, float from, u64 want, float& border, uint32_t& ties) {
     constexpr int E = Vec<T>::E;
     const float scale = float(kBins) / (top - from);          // (top == from: infinite, and every value then is in bin 0)
     auto bin_of = [&](float z) { const float b = (top - z) * scale; return b < float(kBins - 1) ? int(b) : b >= float(kBins - 1) ? kBins - 1 : 0; };
@@ -623,8 +625,8 @@ __device__ __forceinline__ float lowest_with(float guess, float top, F&& f) {
 //   of each bin to 1 part in 4000; the border lies in the bins, one or two as a rule, where the weight up to there can be top_p of all.  One pass then
 //   takes the exact weights: of all tokens, of those above these bins, and those in them go to the list, where the exact border is found.
 constexpr int kCountBits = 13;               // of a bin's word; the rest holds the places
-template <int kThreads, bool kMany, class T, class Part>
-__device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<T>& row, const Scale& sc, float top, float from, double unit, float top_p, float least, int each,
+template <int kThreads, bool kMany, class T, bool kPart, class Part>
+__device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<T, kPart>& row, const Scale& sc, float top, float from, double unit, float top_p, float least, int each,
                                         const Part& part_of, u64& total, Border& border) {
     constexpr int E = Vec<T>::E, kEach = kBins / kThreads;
     const float scale = float(kBins) / (top - from);
@@ -701,7 +703,7 @@ __device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<
         return false;
     }
     u64 above = 0, sum = 0;
-    sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&u)[4], int c) -> u64 {
+    sum_pieces<kThreads>(s, row, row.lo(), row.hi(), each, [&](const uint32_t (&u)[4], int c) -> u64 {
         u64 kept = 0;
 #pragma unroll
         for (int i = 0; i < E; i += 4) {
@@ -760,8 +762,8 @@ __device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<
     for (int i = threadIdx.x; i < n; i += kThreads) {
         const u64 key = team.of(s.key[i]);
         const int c = (int(~uint32_t(key)) + row.shift) / E;
-        if (key >= last_key && unorder(uint32_t(key >> 32)) >= least && c >= row.lo && c < row.hi)
-            atomicAdd(&s.piece[(c - row.lo) / (32 * each)], team.of(s.weight[i]));
+        if (key >= last_key && unorder(uint32_t(key >> 32)) >= least && c >= row.lo() && c < row.hi())
+            atomicAdd(&s.piece[(c - row.lo()) / (32 * each)], team.of(s.weight[i]));
     }
     __syncthreads();
     return true;
@@ -803,7 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     grid_dependents_launch();
     Team<kMany> team(s, uint32_t(p.ranks));
     const int n = p.ordered ? costly_first<kThreads>(s, p) : int(blockIdx.x / team.ranks);
-    Row<T> row(p.logits, n, p.K);
+    Row<T, kMany> row(p.logits, n, p.K);
     if constexpr (kMany) row.part(int(team.rank), int(team.ranks));
     if (threadIdx.x == 0) { s.listed = 0; s.border_id = -1; }
     const float temperature = p.temperature ? p.temperature[n] : 1.f;
@@ -960,7 +962,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
     const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), double(kLowest)));    // (what has any weight lies above)
-    auto pieces_each = [&] { return (row.hi - row.lo + 32 * kPieces - 1) / (32 * kPieces); };        // vectors of a piece per lane
+    auto pieces_each = [&] { return (row.hi() - row.lo() + 32 * kPieces - 1) / (32 * kPieces); };        // vectors of a piece per lane
     u64 whole = 0;
     if (by_p && k == 0 && !infinite) summed = nucleus<kThreads>(s, team, row, sc, top, floor_z, unit, top_p, least, pieces_each(), part_of, whole, border);
     const bool by_least = least > kLowest && border.z == least;                                      // (min-p keeps less than top-p in any case)
@@ -972,7 +974,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
     const int each = pieces_each();
     auto nth_of = [&](float z, uint32_t ties) {                // the border at that many tokens of value z
-        sum_pieces<kThreads>(s, row, row.lo, row.hi, each, by_value(row, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; }));
+        sum_pieces<kThreads>(s, row, row.lo(), row.hi(), each, by_value(row, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; }));
         const int id = locate<kThreads>(s, row, each, u64(ties) - 1, [&](float v, int) -> u64 { return v == z ? 1ull : 0ull; });
         __syncthreads();
         return Border{z, id};
@@ -1018,13 +1020,13 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     if (!summed) {
         __syncthreads();
         if (infinite || border.id != kAllIds)
-            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, by_value(row, kept_weight));
+            sum_pieces<kThreads>(s, row, row.lo(), row.hi(), each, by_value(row, kept_weight));
         else if (border.z > kLowest)
-            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&q)[4], int) { return vector_weight<false, T>(sc, q, border.z); });
+            sum_pieces<kThreads>(s, row, row.lo(), row.hi(), each, [&](const uint32_t (&q)[4], int) { return vector_weight<false, T>(sc, q, border.z); });
         else
-            sum_pieces<kThreads>(s, row, row.lo, row.hi, each, [&](const uint32_t (&q)[4], int) { return vector_weight<true, T>(sc, q, 0.f); });
+            sum_pieces<kThreads>(s, row, row.lo(), row.hi(), each, [&](const uint32_t (&q)[4], int) { return vector_weight<true, T>(sc, q, 0.f); });
     }
-    const u64 own = block_sum<kThreads>(s, int(threadIdx.x) < (row.hi - row.lo + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
+    const u64 own = block_sum<kThreads>(s, int(threadIdx.x) < (row.hi() - row.lo() + 32 * each - 1) / (32 * each) ? s.piece[threadIdx.x] : 0ull);
     u64 front = 0;
     const u64 total = alone ? own : team.sum(own, &front), target = target_of(total);
     if (target >= front && target - front < own) {
