@@ -667,6 +667,8 @@ class TensorList:
         self._sizes = (ctypes.c_size_t * n)(*self.sizes)
         self._dtypes = (ctypes.c_int * n)(*self.dtypes)
         self.layout = bytes((ctypes.c_int * 1)(self.device)) + bytes(self._sizes) + bytes(self._dtypes)       # (alike for lists that are alike)
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in self.tensors if t.numel())
+        self.overlaps = any(a[1] > b[0] for a, b in zip(spans, spans[1:]))       # (then it can only be read)
         self.pointers, self.counts, self.types = (ctypes.addressof(a) for a in (self._pointers, self._sizes, self._dtypes))
 
     def __len__(self):
@@ -705,6 +707,8 @@ def grad_norm(grads, norm, ws=None, stream=None):
 
 def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
     """out[i] = grads[i] * min(1, max_norm / (norm + 1e-6)); out may be grads."""
+    if out.overlaps:
+        raise ValueError("pcl_grad_clip: tensors that are written must not overlap")
     if _calls is not None and out.layout == grads.layout and _done(_calls.grad_clip(
             grads.device, len(grads.tensors), grads.pointers, out.pointers, grads.counts, grads.types, max_norm, norm, ws, stream), "pcl_grad_clip"):
         return
@@ -716,6 +720,8 @@ def grad_clip(grads, out, max_norm, norm, ws=None, stream=None):
 
 def sgd_update_clipped(params, grads, lr, max_norm, norm, ws=None, stream=None):
     """params[i] -= lr * min(1, max_norm / (norm + 1e-6)) * grads[i], in place."""
+    if params.overlaps:
+        raise ValueError("pcl_sgd_update_clipped: tensors that are written must not overlap")
     if _calls is not None and params.layout == grads.layout and _done(_calls.sgd_update_clipped(
             grads.device, len(grads.tensors), params.pointers, grads.pointers, grads.counts, grads.types, lr, max_norm, norm, ws, stream),
             "pcl_sgd_update_clipped"):

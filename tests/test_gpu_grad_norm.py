@@ -223,3 +223,22 @@ def test_more_than_2_to_31_elements():
     assert abs(float(norm) - 13) <= 13 * NORM_ERROR
     for i, v in ((n - 1, 3.0), (0, 4.0), (2 ** 31, 12.0), (5, 0.0)):
         assert abs(float(g[i]) - v * f) <= v * f * (half_step(torch.bfloat16) + 2 * NORM_ERROR)
+
+
+def test_tensors_that_are_written_twice_are_refused():
+    """A list that overlaps itself can be read (every mention counts), not written."""
+    flat = torch.arange(1.0, 65.0, device="cuda")
+    a, b = flat[:40], flat[36:]
+    twice, apart, norm, ws = B.TensorList([a, b]), B.TensorList([a.clone(), b.clone()]), scalar(), workspace(B.grad_norm_workspace_bytes(2))
+    B.grad_norm(twice, norm, ws)
+    check_norm(norm, norm_of([a, b]))
+    with pytest.raises(ValueError):
+        B.grad_clip(apart, twice, 1.0, norm, ws)
+    with pytest.raises(ValueError):
+        B.grad_clip(twice, twice, 1.0, norm, ws)
+    with pytest.raises(ValueError):
+        B.sgd_update_clipped(twice, apart, 0.1, 1.0, norm, ws)
+    B.grad_clip(twice, apart, 1.0, norm, ws)
+    assert torch.equal(flat, torch.arange(1.0, 65.0, device="cuda"))
+    B.grad_norm(B.TensorList([flat[:36], flat[36:], flat[:0]]), norm, workspace(B.grad_norm_workspace_bytes(3)))
+    assert not B.TensorList([flat[:36], flat[36:], flat[:0], flat[5:5]]).overlaps

@@ -248,8 +248,8 @@ def test_row_starts_off_16_bytes():
         check(logits(17, 1031, t, 12), params(17, 13, FILTERS[-1]))
 
 
-def test_captured_and_on_two_streams():
-    N, K = 9, 2050
+@pytest.mark.parametrize("N,K", [(9, 2050), (4, 70001)])
+def test_captured_and_on_two_streams(N, K):
     z, z2 = logits(N, K, torch.bfloat16, 14), logits(N, K, torch.bfloat16, 15)
     p, p2 = params(N, 16, FILTERS[-1]), params(N, 17, FILTERS[-1])
     d, d2 = {k: device(v) for k, v in p.items()}, {k: device(v) for k, v in p2.items()}
