@@ -17,14 +17,15 @@
 // Sums over a row are fp32 in a fixed tree.  h is rounded when it is stored, but the norm is that of the sum before rounding.  A row whose
 // sum of squares leaves fp32's range is scaled by a power of two first.
 //
-// Measured: 32768 x 4096 bf16 with a residual 195 us both ways (1.07 GB, 5.5 TB/s: 84 % of a copy's rate); 3001 x 1037 fp16 to 8 bits 7.4; gradient of
-// 5000 x 1001 fp32 18.7 (a third of it the second launch and edges); one row of 2048 bf16 3.3, nearly all of it launch and call.
+// Measured: 32768 x 4096 bf16 with a residual 168 us (1.07 GB, 6.4 TB/s), its gradient 160 (6.7 TB/s); 3001 x 1037 fp16 to 8 bits 7.4; gradient of
+// 5000 x 1001 fp32 17.7 (a third of it the second launch and edges); one row of 2048 bf16 3.3, nearly all of it launch and call.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <limits.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "pcl_internal.h"
@@ -177,6 +178,29 @@ struct Group {
         uint32_t none;
         sum_and_max<false>(a, none);
         return a;
+    }
+    // of one row or two at once
+    __device__ __forceinline__ void sums(float (&a)[1]) { a[0] = sum(a[0]); }
+    __device__ __forceinline__ void sums(float (&a)[2]) {
+        for (int o = (size < 32 ? size : 32) >> 1; o; o >>= 1) {
+            a[0] += __shfl_xor_sync(mask, a[0], o);
+            a[1] += __shfl_xor_sync(mask, a[1], o);
+        }
+        if (size <= 32) return;
+        float* sums = words + turn * 64;
+        const int warps = size >> 5, first = index * warps;
+        turn ^= 1;
+        if ((rank & 31) == 0) {
+            sums[first + (rank >> 5)] = a[0];
+            sums[32 + first + (rank >> 5)] = a[1];
+        }
+        sync();
+        a[0] = a[1] = 0.f;
+#pragma unroll 4
+        for (int i = first; i < first + warps; ++i) {
+            a[0] += sums[i];
+            a[1] += sums[32 + i];
+        }
     }
 };
 
@@ -580,7 +604,7 @@ struct GradParams {
     float* parts;                // [blocks][C]: sums of dw over each block's rows, or null
 };
 
-template <class T, int V, bool kWhole, int kConsumers>
+template <class T, int V, bool kWhole, int kConsumers, bool kPairs>
 __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) row_grad_kernel(const GradParams p, const Pipe q) {
     constexpr int P = Chunk<T>::P;
     extern __shared__ __align__(128) uint8_t ring[];
@@ -617,67 +641,87 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
     bool ok = true;
     int stage = 0;
     uint32_t phase = 0;
-    auto factor = [&](int s) {                                 // rstd of the group's first row of set s
-        const int row = s * rows_per_set + g.index;
-        return s < q.sets && row < p.N ? p.rstd[row] : 0.f;
+    // rows are taken kRows at a time: one reduction (and barrier) for both
+    constexpr int kRows = kPairs ? 2 : 1;
+    // (one row: known here, which saves 16-bit types registers, 10000 x 3333 bf16 83 -> 62 us; fp32 code is slower by it, 8000 x 2501 52 -> 56)
+    const int per_group = kPairs || sizeof(T) == 4 ? q.per_group : 1;
+    auto factors = [&](int s, int k, float (&r)[kRows]) {
+#pragma unroll
+        for (int b = 0; b < kRows; ++b) {
+            const int row = s * rows_per_set + (k + b) * groups + g.index;
+            r[b] = s < q.sets && k + b < per_group && row < p.N ? p.rstd[row] : 0.f;
+        }
     };
-    float next = factor(blockIdx.x);
+    float next[kRows];
+    factors(blockIdx.x, 0, next);
     for (int s = blockIdx.x; s < q.sets; s += gridDim.x) {
-        float r = next;
-        next = factor(s + gridDim.x);
         ok = ok && bounded_wait(&sh.full[stage], phase, &sh.abort_flag, q.status, WAIT_EPI_TMEM_FULL);
         const uint8_t* slot = ring + size_t(stage) * slots;
-        for (int k = 0; k < q.per_group; ++k) {
+        for (int k = 0; k < per_group; k += kRows) {
+            float r[kRows], xe[kRows], ye[kRows], dot[kRows];
+#pragma unroll
+            for (int b = 0; b < kRows; ++b) { r[b] = next[b]; xe[b] = ye[b] = dot[b] = 0.f; }
+            if (k + kRows < per_group) factors(s, k + kRows, next);
+            else factors(s + gridDim.x, 0, next);
             const int n = k * groups + g.index, row = s * rows_per_set + n;
             if (row >= p.N) break;                             // (of the whole group)
-            if (k > 0) r = p.rstd[row];
-            const uint8_t* from = slot + row_start<T, kWhole>(s, rows_per_set, n, p.C);
-            const size_t begin = size_t(row) * p.C;
+            const bool second = kPairs && k + 1 < per_group && row + groups < p.N;
             // dot = sum of g h = sum of dy w h;  dw += r dy h
-            float2 sum = both(0.f);
-            float xe = 0.f, ye = 0.f;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (!at.live(i)) continue;
-                float2 x[P], y[P], wf[P];
-                load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
-                load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
-                weight[i].values(wf);
+            for (int b = 0; b < kRows; ++b) {
+                if (b > 0 && !second) break;
+                const uint8_t* from = slot + row_start<T, kWhole>(s, rows_per_set, n + b * groups, p.C);
+                float2 sum = both(0.f);
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    const float2 t = mul2(mul2(x[j], both(r)), y[j]);
-                    dw[i][j] = add2(dw[i][j], t);
-                    sum = fma2(t, wf[j], sum);
+                for (int i = 0; i < V; ++i) {
+                    if (!at.live(i)) continue;
+                    float2 x[P], y[P], wf[P];
+                    load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
+                    load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
+                    weight[i].values(wf);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        const float2 t = mul2(mul2(x[j], both(r[b])), y[j]);
+                        dw[i][j] = add2(dw[i][j], t);
+                        sum = fma2(t, wf[j], sum);
+                    }
+                }
+                dot[b] = sum.x + sum.y;
+                if (at.has_edge()) {
+                    const size_t element = size_t(row + b * groups) * p.C + at.edge;
+                    xe[b] = slot_element(from, at.edge * sizeof(T), size, h, element) * r[b];
+                    ye[b] = slot_element(from + q.slot, at.edge * sizeof(T), size, dy, element);
+                    dwe += xe[b] * ye[b];
+                    dot[b] = fmaf(xe[b] * ye[b], we, dot[b]);
+                    ye[b] *= we;
                 }
             }
-            float dot = sum.x + sum.y;
-            if (at.has_edge()) {
-                xe = slot_element(from, at.edge * sizeof(T), size, h, begin + at.edge) * r;
-                ye = slot_element(from + q.slot, at.edge * sizeof(T), size, dy, begin + at.edge);
-                dwe += xe * ye;
-                dot = fmaf(xe * ye, we, dot);
-                ye *= we;
-            }
-            dot = g.sum(dot) * mean;
-            const float2 rr = both(r), minus = both(-dot);
+            g.sums(dot);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                if (!at.live(i)) continue;
-                float2 x[P], y[P], wf[P], d[P];
-                load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
-                load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
-                if (dh) load_chunk<T>(from + 2 * q.slot + at.column(i) * int(sizeof(T))).values(d);
-                weight[i].values(wf);
+            for (int b = 0; b < kRows; ++b) {
+                if (b > 0 && !second) break;
+                const uint8_t* from = slot + row_start<T, kWhole>(s, rows_per_set, n + b * groups, p.C);
+                const size_t begin = size_t(row + b * groups) * p.C;
+                const float2 rr = both(r[b]), minus = both(-dot[b] * mean);
 #pragma unroll
-                for (int j = 0; j < P; ++j) {
-                    const float2 t = fma2(mul2(x[j], rr), minus, mul2(y[j], wf[j]));
-                    d[j] = fma2(rr, t, dh ? d[j] : both(0.f));
+                for (int i = 0; i < V; ++i) {
+                    if (!at.live(i)) continue;
+                    float2 x[P], y[P], wf[P], d[P];
+                    load_chunk<T>(from + at.column(i) * int(sizeof(T))).values(x);
+                    load_chunk<T>(from + q.slot + at.column(i) * int(sizeof(T))).values(y);
+                    if (dh) load_chunk<T>(from + 2 * q.slot + at.column(i) * int(sizeof(T))).values(d);
+                    weight[i].values(wf);
+#pragma unroll
+                    for (int j = 0; j < P; ++j) {
+                        const float2 t = fma2(mul2(x[j], rr), minus, mul2(y[j], wf[j]));
+                        d[j] = fma2(rr, t, dh ? d[j] : both(0.f));
+                    }
+                    if (ok) store_chunk(static_cast<T*>(p.dx) + (begin + at.column(i)), d);
                 }
-                if (ok) store_chunk(static_cast<T*>(p.dx) + (begin + at.column(i)), d);
-            }
-            if (at.has_edge() && ok) {
-                const float d = dh ? slot_element(from + 2 * q.slot, at.edge * sizeof(T), size, dh, begin + at.edge) : 0.f;
-                static_cast<T*>(p.dx)[begin + at.edge] = Elem<T>::put(fmaf(r, fmaf(xe, -dot, ye), d));
+                if (at.has_edge() && ok) {
+                    const float d = dh ? slot_element(from + 2 * q.slot, at.edge * sizeof(T), size, dh, begin + at.edge) : 0.f;
+                    static_cast<T*>(p.dx)[begin + at.edge] = Elem<T>::put(fmaf(r[b], fmaf(xe[b], minus.x, ye[b]), d));
+                }
             }
         }
         __syncwarp();
@@ -801,7 +845,7 @@ template <class T> bool too_long(int C) { return row_chunks(C, Chunk<T>::E) > kP
 template <class T>
 struct PipeShape { Pipe q; int v, groups, consumers, grid; bool whole; size_t smem; };
 template <class T>
-int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int threads, int blocks_per_sm) {
+int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int threads, int blocks_per_sm, int wide_threads, bool pairs) {
     constexpr int E = Chunk<T>::E;
     const int chunks = row_chunks(C, E), sms = device_sm_count();
     o.v = chunks <= 32 ? 1 : chunks <= 64 ? 2 : chunks <= kPipeMost * kMostV<T> / 2 ? kMostV<T> / 2 : kMostV<T>;
@@ -815,15 +859,22 @@ int pipe_shape(PipeShape<T>& o, int N, int C, int tensors, int threads, int bloc
     o.groups = o.q.group > threads ? 1 : threads / o.q.group;
     o.consumers = o.groups * o.q.group;
     const size_t row = size_t(C) * sizeof(T);
-    // several rows to a group where they are short (and where a group's rows still start alike)
+    // several rows to a group where they are short (and where a group's rows still start alike), and two where they are worked on in pairs: 32768 x 4096
+    // bf16 gradient 185 -> 160 us, 20000 x 5120 206 -> 151
     int m = 1;
+    auto more = [&](int to) {                                  // (the rows are there, and two stages of them fit an SM)
+        return long(N) / (to * o.groups) >= 8L * sms && 2 * (align_up(size_t(to) * o.groups * row + 32, 128) * tensors) <= size_t(kMostRing);
+    };
     if (o.groups % E == 0 || C % E == 0)
-        while (m < 16 && m * o.groups * row < 4096 && long(N) / (2 * m * o.groups) >= 8L * sms) m *= 2;
+        while (m < 16 && (m * o.groups * row < 4096 || (pairs && m == 1)) && more(2 * m)) m *= 2;
     o.q.per_group = m;
     const int rows = m * o.groups;
     o.q.sets = (N + rows - 1) / rows;
     o.q.slot = int(align_up(rows * row + 32, 128));
     const size_t stage = size_t(o.q.slot) * tensors;
+    // (blocks of more than 256 threads: as many as their registers and three stages each leave room for)
+    if (o.consumers > 256) blocks_per_sm = std::min(blocks_per_sm, wide_threads / (o.consumers + 32));
+    while (o.consumers > 256 && blocks_per_sm > 1 && 3 * stage * blocks_per_sm > size_t(kMostRing)) --blocks_per_sm;
     const size_t ring = kMostRing / blocks_per_sm / 128 * 128;
     const size_t room = 2 * stage > ring ? kMostRing : ring;
     const size_t stages = room / stage;
@@ -878,7 +929,10 @@ int launch_rows(const RowParams& p, cudaStream_t st) {
         return PCL_ERR_UNSUPPORTED_SHAPE;                      // (not reached: longer 16-bit rows are walked over twice)
     }
     PipeShape<T> o;
-    const int rc = pipe_shape(o, p.N, p.C, kMode != ROW_QUANTIZE && p.residual ? 2 : 1, 256, 3);
+    // Long streams of 16-bit rows: two blocks of 512 threads (32768 x 4096 with a residual 194 -> 168 us, 65536 x 2048 191 -> 182); else three of 256
+    // (without a residual 114 -> 100, fp32 16384 x 4096 192 -> 176, to 8 bits 32768 x 4096 176 -> 152, 1500 x 4096 12.8 -> 10.5).
+    const bool wide = kMode == ROW_NORM && E == 8 && p.residual && p.C % E == 0 && chunks >= 256 && long(p.N) * chunks >= 256L * 48 * sms;
+    const int rc = pipe_shape(o, p.N, p.C, kMode != ROW_QUANTIZE && p.residual ? 2 : 1, wide ? 512 : 256, 3, 2 * (512 + 32), false);
     if (rc != PCL_OK) return rc;
 #define PCL_ROWS(V_) return o.whole ? launch_pipe<T, V_, kMode, true>(p, o, st) : launch_pipe<T, V_, kMode, false>(p, o, st)
     if (o.v == 1) PCL_ROWS(1);
@@ -904,10 +958,12 @@ int launch_grad_pipe(const GradParams& p, const PipeShape<T>& o, cudaStream_t st
         const int rc = allow_smem(once, kernel);
         return rc != PCL_OK ? rc : launch_chained(kernel, dim3(o.grid), dim3(o.consumers + 32), smem, st, 1, p, o.q);
     };
-    static PerDeviceOnce once256, once512;
+    static PerDeviceOnce once256, once512, pairs256, pairs512;
+    const bool pairs = o.q.per_group > 1 || V * Chunk<T>::E > 16;      // (4096 x 16384 bf16, a row at a time: 152 us against 133)
     if constexpr (V * Chunk<T>::E <= 16)
-        if (o.consumers <= 256) return launch(once256, row_grad_kernel<T, V, kWhole, 256>);
-    if constexpr (V * Chunk<T>::E >= 16) return launch(once512, row_grad_kernel<T, V, kWhole, 512>);
+        if (o.consumers <= 256) return pairs ? launch(pairs256, row_grad_kernel<T, V, kWhole, 256, true>) : launch(once256, row_grad_kernel<T, V, kWhole, 256, false>);
+    if constexpr (V * Chunk<T>::E >= 16)
+        return pairs ? launch(pairs512, row_grad_kernel<T, V, kWhole, 512, true>) : launch(once512, row_grad_kernel<T, V, kWhole, 512, false>);
     return PCL_ERR_UNSUPPORTED_SHAPE;
 }
 template <class T>
@@ -921,7 +977,7 @@ int launch_grad(const GradParams& p, void* dw, cudaStream_t st) {
     } else {
         PipeShape<T> o;
         const bool few = grad_blocks(p.N) <= sms && row_chunks(p.C, E) > 64;
-        rc = pipe_shape(o, p.N, p.C, p.dh ? 3 : 2, few ? 512 : 256, few ? 1 : 2);
+        rc = pipe_shape(o, p.N, p.C, p.dh ? 3 : 2, few ? 512 : 256, few ? 1 : 2, 512 + 32, true);
         if (rc != PCL_OK) return rc;
         int unit = 1;
         while (p.C % E != 0 && o.q.per_group * o.groups * unit % E != 0) unit *= 2;
