@@ -303,3 +303,71 @@ def test_streams_and_graph():
         check_grad(t, x, w, rstd, dy, None, dx, dw)
         ey = forward_reference(x2, None, w, 1e-6)[2]
         assert ((y2.double() - ey).abs() <= ey.abs() * 1.01 * half_step(t) + smallest(t)).all()
+
+
+# Enough rows for every way of sharing the blocks out: rows in pairs (odd numbers of rows, too), several rows to a group, one to three blocks an SM.
+LONG = [(2371, 4096), (9477, 1000), (18951, 33), (2403, 5120), (2371, 8192), (1201, 16384), (2500, 3333), (700, 15001), (40001, 64), (4801, 2049), (9600, 1001)]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("N,C", LONG)
+def test_gradient_of_many_rows(N, C, t):
+    h, w, dy, dh = put((N, C), t, 1.5, 1), put((C,), t, 0.3, 2, 1.0), put((N, C), t, 0.1, 3), put((N, C), t, 0.1, 4)
+    rstd = (h.double().square().mean(dim=1) + 1e-6).rsqrt().float()
+    dx, dw = guarded((N, C), t), guarded((C,), t)
+    ws = workspace(B.rms_norm_workspace_bytes(N, C))
+    for with_dh in (None, dh):
+        B.rms_norm_bwd(N, C, h, w, rstd, dy, with_dh, dx, dw, ws)
+        check_grad(t, h, w, rstd, dy, with_dh, dx, dw)
+    for over in (dy, h, dh):                                      # in place of each input
+        given = [x.clone() for x in (h, dy, dh)]
+        at = [x is over for x in (h, dy, dh)].index(True)
+        dw2 = guarded((C,), t)
+        B.rms_norm_bwd(N, C, given[0], w, rstd, given[1], given[2], given[at], dw2, ws)
+        assert torch.equal(given[at], dx) and torch.equal(dw, dw2)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("N,C", LONG + [(3700, 4096), (7301, 2048), (1803, 8192)])
+def test_forward_of_many_rows(N, C, t):
+    x, res, w = put((N, C), t, 0.7, 1), put((N, C), t, 2.0, 3), put((C,), t, 0.3, 2, 1.0)
+    h, y, rstd = guarded((N, C), t), guarded((N, C), t), guarded((N,), torch.float32)
+    B.rms_norm_fwd(N, C, x, None, w, 1e-6, None, y, rstd)
+    check_forward(N, C, t, x, None, w, 1e-6, None, y, rstd)
+    B.rms_norm_fwd(N, C, x, res, w, 1e-6, h, y, rstd)
+    check_forward(N, C, t, x, res, w, 1e-6, h, y, rstd)
+    x2, res2 = x.clone(), res.clone()
+    B.rms_norm_fwd(N, C, x2, res2, w, 1e-6, res2, x2)             # both in place
+    assert torch.equal(x2, y) and torch.equal(res2, h)
+    q, scale = bytes8((N, C)), guarded((N,), torch.float32)
+    B.rms_norm_fwd_q8(N, C, x, res, w, 1e-6, None, q, scale)
+    _, _, ey = forward_reference(x, res, w, 1e-6)
+    check_q8(q, scale, ey, additions(C) / 2 + 8)
+
+
+@pytest.mark.parametrize("C", [96, 100, 4096, 40001])
+def test_rows_out_of_range_among_many(C):
+    """Rows that are scaled first, zeros, infinities and NaN in the middle of many ordinary ones, which do not notice."""
+    N, t = 3700 if C < 10000 else 500, torch.float32
+    x, w = put((N, C), t, 1.0, 5).clamp_(-4, 4), put((C,), t, 0.3, 2, 1.0)
+    plain, y, rstd = guarded((N, C), t), guarded((N, C), t), guarded((N,), torch.float32)
+    B.rms_norm_fwd(N, C, x, None, w, 0.0, None, plain, rstd)
+    odd = x.clone()
+    odd[5::50] *= 1e30
+    odd[6::50] *= 1e-30
+    odd[7::50] = 0
+    odd[8::50, C // 2] = float("inf")
+    odd[9::50, C - 1] = float("nan")
+    B.rms_norm_fwd(N, C, odd, None, w, 0.0, None, y, rstd)
+    place = torch.arange(N, device="cuda") % 50
+    same = (place < 5) | (place > 9)
+    assert torch.equal(y[same], plain[same]) and torch.isnan(y[place == 9]).all() and torch.isnan(y[place == 7]).all()
+    k = additions(C)
+    scaled = (place == 5) | (place == 6)
+    _, er, ey = forward_reference(odd[scaled], None, w, 0.0)
+    assert ((rstd[scaled].double() - er).abs() <= er * (k / 2 + 4) * U + 2.0 ** -149).all()
+    assert ((y[scaled].double() - ey).abs() <= ey.abs() * (k / 2 + 8) * U + 2.0 ** -100).all()
+    q, scale = bytes8((N, C)), guarded((N,), torch.float32)
+    B.rms_norm_fwd_q8(N, C, odd, None, w, 0.0, None, q, scale)
+    check_q8(q[scaled], scale[scaled], ey, k / 2 + 8)
+    assert torch.isfinite(scale[same]).all() and not torch.isfinite(scale[place == 8]).any() and torch.isnan(scale[place == 9]).all()
