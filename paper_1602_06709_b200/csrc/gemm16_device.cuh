@@ -69,6 +69,7 @@ struct Gemm16Params {
     const float* lse;
     const float* row_scale;
     const float* col_scale; int act;
+    int slot_bytes;                          // what a block's copies bring to a CTA
     unsigned int* status;
 };
 
@@ -350,7 +351,7 @@ __device__ __forceinline__ bool produce_items(Gemm16Ctx& c, const Gemm16Params& 
         const int rb = tile.n * kBN + (kPair ? int(c.pair_rank) * (tile_width(p, tile.n, kBN) / 2) : 0);
         for (int kb = tile.k0; kb < tile.k1; ++kb) {
             if (!bounded_wait_addr_warp(empty0 + 8 * c.stage, c.phase ^ 1u, &c.sh->abort_flag, c.status, WAIT_PRODUCER_EMPTY)) return false;
-            if (c.pair_rank == 0) mbar_expect_tx_addr(full0 + 8 * c.stage, kPair ? 2 * kSlotBytes : kSlotBytes);
+            if (c.pair_rank == 0) mbar_expect_tx_addr(full0 + 8 * c.stage, kPair ? 2 * p.slot_bytes : p.slot_bytes);
             const uint32_t dst = c.ring + c.stage * kSlotBytes, bar = full_dst0 + 8 * c.stage;
             if constexpr (kAMn) {
                 tma_load_3d_addr<kPair>(dst, tm_a, bar, ra, kb * 64, tile.b);
@@ -935,6 +936,7 @@ inline int fill_params16(Gemm16Params& p, const Gemm16Args& a, const Plan16& pl)
     const int tile = pl.pair ? 256 : 128;
     p = Gemm16Params{};
     p.M = a.M; p.N = a.N; p.batch = a.batch;
+    p.slot_bytes = kSlotBytes;
     p.k_blocks = (a.K + 63) / 64;
     p.last_slices = (a.K - (p.k_blocks - 1) * 64 + 15) / 16;
     p.m_tiles = (a.M + tile - 1) / tile;

@@ -150,3 +150,20 @@ def test_more_than_2_to_31_elements():
     B.fc_q8_fwd(N, C, K, x, xs, w, ws, None, y, ws=workspace(B.fc_q8_workspace_bytes(N, C, K)))
     for r in (slice(0, 2), slice(2 ** 31 // K - 1, 2 ** 31 // K + 2), slice(N - 2, N)):
         check(y[r], torch.bfloat16, B.ACT_NONE, *expected(x[r], xs[r], w, ws, None, B.ACT_NONE))
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("N", [1, 8, 9, 64, 113, 120, 121])
+@pytest.mark.parametrize("C,K", [(4096, 16384), (1037, 300), (64, 40)])
+def test_few_rows_behind_a_call_of_nan(N, C, K, t):
+    """Rows of a tile that x does not have hold what another call left in shared memory: NaN there do not reach the result."""
+    big = 512
+    nan, one, y0 = guarded((big, 512), torch.uint8, fill=0x7f), guarded((20480,), torch.float32, fill=1.0), guarded((big, 20480), torch.bfloat16, fill=0)
+    w0 = guarded((20480, 512), torch.uint8, fill=0x7f)
+    x, w = whole((N, C), 1), whole((K, C), 2)
+    xs, ws, y = scales(N, 0.1, 3), scales(K, 5.0 / C ** 0.5, 4), guarded((N, K), t)
+    space = workspace(B.fc_q8_workspace_bytes(N, C, K))
+    B.fc_q8_fwd(big, 512, 20480, nan, one[:big], w0, one, None, y0, ws=workspace(B.fc_q8_workspace_bytes(big, 512, 20480)))
+    B.fc_q8_fwd(N, C, K, x, xs, w, ws, None, y, ws=space)
+    check(y, t, B.ACT_NONE, *expected(x, xs, w, ws, None, B.ACT_NONE))
+    assert torch.isnan(y0).all()
