@@ -168,7 +168,7 @@ int launch_gemm16(const Gemm16Args& a, cudaStream_t st) {
     if (rc != PCL_OK) return rc;
     if (a.epi == GEMM16_Q8 && a.M <= 120) {
         // few rows: no more of them are copied (the others hold what was there before, in rows of the result that nobody reads); filling 128 rows, most
-        // of them with zeros, took longer than the weights: 4096 -> 16384, 1 row 23.4 -> 17.4 us, 16 rows 19.9 -> 17.6
+        // of them with zeros, took longer than the weights: 4096 -> 16384 in pairs, 1 row 23.4 -> 17.4 us, 16 rows 19.9 -> 17.6
         const int rows = int(align_up(a.M, 8));
         p.slot_bytes = (rows + 128) * 128;
         rc = make_tmap16(&m.a, a.a.ptr, t16, a.K, a.M, a.batch, a.a.ld, a.a.batch_stride, 64, uint32_t(rows));
