@@ -141,6 +141,7 @@ struct Group {
         : size(size_), rank(int(threadIdx.x) % size_), index(int(threadIdx.x) / size_), words(words_),
           mask(size_ < 32 ? ((1u << size_) - 1) << (threadIdx.x & 31 & ~unsigned(size_ - 1)) : 0xffffffffu) {}
     __device__ __forceinline__ void sync() const {
+        __syncwarp();                        // (a warp's first lane has just stored its sums alone, and the barrier wants whole warps)
         if (size == int(blockDim.x)) __syncthreads();
         else named_barrier_sync(1 + index, size);
     }
@@ -748,6 +749,7 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
     float* part = p.parts + size_t(blockIdx.x) * p.C;
     float* merged = reinterpret_cast<float*>(ring);
     for (int t = 0; t < turns; ++t) {
+        __syncwarp();                        // (lanes of a warp part at `continue`, and the barrier wants whole warps)
         if (turns > 1) named_barrier_sync(15, consumers);
         if (t != my_turn) continue;
         float* to = turns == 1 ? part : merged;
@@ -773,6 +775,7 @@ __global__ void __launch_bounds__(kConsumers + 32, kConsumers == 256 ? 2 : 1) ro
         }
         if (at.has_edge()) to[at.edge] = t == 0 ? dwe : to[at.edge] + dwe;
     }
+    __syncwarp();
     if (turns > 1) {
         named_barrier_sync(15, consumers);
         for (int c = threadIdx.x; c < p.C; c += consumers) part[c] = merged[c];

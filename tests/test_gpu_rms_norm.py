@@ -371,3 +371,18 @@ def test_rows_out_of_range_among_many(C):
     B.rms_norm_fwd_q8(N, C, odd, None, w, 0.0, None, q, scale)
     check_q8(q[scaled], scale[scaled], ey, k / 2 + 8)
     assert torch.isfinite(scale[same]).all() and not torch.isfinite(scale[place == 8]).any() and torch.isnan(scale[place == 9]).all()
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("C", [8, 16, 24, 32, 40, 64, 96, 128])
+@pytest.mark.parametrize("N", [5, 297, 4099, 21001])
+def test_weight_gradient_of_short_rows(N, C, t):
+    """Rows that 4, 8 or 16 lanes of a warp share: only the first group's lanes hold the warp's sums of dw when the block's are put together."""
+    h, w, dy = put((N, C), t, 1.5, 1), put((C,), t, 0.3, 2, 1.0), put((N, C), t, 0.1, 3)
+    rstd = (h.double().square().mean(dim=1) + 1e-6).rsqrt().float()
+    dx, dw, again = guarded((N, C), t), guarded((C,), t), guarded((C,), t)
+    ws = workspace(B.rms_norm_workspace_bytes(N, C))
+    B.rms_norm_bwd(N, C, h, w, rstd, dy, None, dx, dw, ws)
+    check_grad(t, h, w, rstd, dy, None, dx, dw)
+    B.rms_norm_bwd(N, C, h, w, rstd, dy, None, dx, again, ws)
+    assert torch.equal(dw, again) and B.last_device_status() == B.OK
