@@ -962,7 +962,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ---- where the part kept ends
     Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
-    const float floor_z = float(fmax(double(top) - 31.0 * double(temperature), double(kLowest)));    // (what has any weight lies above)
+    // what has any weight lies above: weights are rounded to the nearest 2^-bits, so they end (bits + 1) ln 2 temperatures below the largest (and a margin
+    // for this bound's own roundings)
+    const float floor_z = float(fmax(double(top) - (0.69314718055994530942 * (p.bits + 1) + 0.05) * double(temperature), double(kLowest)));
     auto pieces_each = [&] { return (row.hi() - row.lo() + 32 * kPieces - 1) / (32 * kPieces); };        // vectors of a piece per lane
     u64 whole = 0;
     if (by_p && k == 0 && !infinite) summed = nucleus<kThreads>(s, team, row, sc, top, floor_z, unit, top_p, least, pieces_each(), part_of, whole, border);

@@ -279,3 +279,15 @@ def test_more_than_2_to_31_logits():
     B.sample_tokens(N, K, z, u, token, top_p=top_p, ws=workspace(B.sample_tokens_workspace_bytes(N, K)))
     for n in (0, 2 ** 31 // K - 1, 2 ** 31 // K, N - 1):
         assert int(token[n]) == pick(z[n].double().cpu().numpy(), 0.5, top_p=float(np.float32(0.8)))[0]
+
+
+@pytest.mark.parametrize("t,T", [(torch.float32, 1.0), (torch.float32, 0.5), (torch.float32, 3.0), (torch.float16, 1.0)])
+@pytest.mark.parametrize("N,K", [(1, 4000), (300, 4000), (1, 40000)])
+@pytest.mark.parametrize("k", [257, 600, 2500])
+def test_top_k_among_the_least_weights(k, N, K, t, T):
+    """A weight of 45 ln 2 = 31.19 temperatures below the largest still rounds to 2^-44: top-k counts such tokens like all others."""
+    z = guarded((N, K), t, fill=-40.0 * T)
+    z[:, 2:3000] = -31.05 * T
+    z[:, 0] = -31.15 * T                    # of rank 3000, in front of all others
+    z[:, 1] = 0.0
+    check(z, {"uniform": np.zeros(N, dtype=np.float32), "top_k": np.full(N, k, dtype=np.int32), "temperature": np.full(N, T, dtype=np.float32)})
