@@ -291,3 +291,61 @@ def test_top_k_among_the_least_weights(k, N, K, t, T):
     z[:, 0] = -31.15 * T                    # of rank 3000, in front of all others
     z[:, 1] = 0.0
     check(z, {"uniform": np.zeros(N, dtype=np.float32), "top_k": np.full(N, k, dtype=np.int32), "temperature": np.full(N, T, dtype=np.float32)})
+
+
+def pick_held(z, u, temperature, top_k, top_p, min_p):
+    """pick with the weights as they are held, whole multiples of 2^-44 of the largest (K <= 2^18): at a random number of 0 it matters which tokens
+    weigh nothing."""
+    z = np.asarray(z, dtype=np.float64) + 0.0
+    if temperature <= 0 or top_k == 1:
+        return int(np.argmax(z)), 0.0
+    d = (z - z.max()) / temperature
+    order = np.argsort(-z, kind="stable")
+    keep = np.ones(len(z), dtype=bool)
+    if 0 < top_k <= len(z):
+        keep[top_k:] = False
+    held = np.rint(np.exp(d) * 2.0 ** 44).astype(np.int64)           # (131072 of them sum to 2^61 at most)
+    w = held[order] * keep
+    if top_p < 1:
+        keep &= np.cumsum(w) - w < top_p * float(w.sum())
+    if min_p > 0:
+        keep &= np.exp(d[order]) >= min_p
+    ids = np.sort(order[keep])
+    c = np.cumsum(held[ids])
+    at = int(np.argmax(c > u * float(c[-1])))
+    return int(ids[at]), float(d[ids[at]] - math.log(float(c[-1]) * 2.0 ** -44))
+
+
+LONG_K = [0, 50, 256, 257, 5000, 20000]
+
+
+def long_rows(N, K, t, seed):
+    """Rows of all kinds, and settings of all kinds that come together with each of them."""
+    z = guarded((N, K), t, fill=0)
+    kinds = ["normal", "steps", "equal", "masked", "peaks", "zeros"]
+    for i, kind in enumerate(kinds):
+        rows = torch.arange(i, N, len(kinds), device="cuda")
+        z[rows] = logits(len(rows), K, t, seed + i, kind)
+    r = np.random.default_rng(seed)
+    p = {"uniform": r.random(N, dtype=np.float32), "temperature": r.choice([0.0, 0.4, 1.0, 1.0, 1.0, 2.5, 30.0], N).astype(np.float32),
+         "top_k": np.asarray(r.choice(LONG_K, N), dtype=np.int32), "top_p": np.where(r.random(N) < 0.5, r.uniform(0.05, 0.999, N), 1.0).astype(np.float32),
+         "min_p": np.where(r.random(N) < 0.4, 10 ** r.uniform(-4, -0.01, N), 0.0).astype(np.float32)}
+    p["uniform"][::7] = 0.0
+    return z, p
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("N,K", [(160, 33000), (320, 33001), (160, 131075), (320, 131072)])
+def test_long_rows_and_many(N, K, t):
+    """More rows than SMs: blocks of 512 threads, with the rows in their order (160) or with the costly ones first (320)."""
+    z, p = long_rows(N, K, t, N + K)
+    token, logprob = run(z, p)
+    for n in np.random.default_rng(1).permutation(N)[:96 if K < 100000 else 40]:
+        args = {k: (int(v[n]) if v.dtype == np.int32 else float(v[n])) for k, v in p.items() if k != "uniform"}
+        want, l = pick_held(z[n].double().cpu().numpy(), float(p["uniform"][n]), **args)
+        assert token[n] == want, (n, token[n], want, args, p["uniform"][n])
+        assert logprob[n] == l or abs(logprob[n] - l) <= abs(l) * 2.0 ** -24 + 6e-14 * K + 1e-12
+    # a row's answer is its own: the same alone, where one block or a cluster of 1024 threads each has it
+    for n in range(0, N, 23):
+        one = run(z[n:n + 1].clone(), {k: v[n:n + 1] for k, v in p.items()})
+        assert one[0][0] == token[n] and (one[1][0] == logprob[n])
