@@ -772,8 +772,11 @@ __device__ __forceinline__ bool nucleus(Shared& s, Team<kMany>& team, const Row<
 
 // The row of this block where the costly rows come first (rows of one kind in their order): those with top-p and no small top-k, then those that
 // need the weights of all tokens, then the others; a late costly row would leave the other SMs idle (512 x 131072, mixed settings: bf16 183 us in the
-// order of the rows, 175 so, fp32 205 and 183; rows that all cost the same lose 2 us by it, 108 to 110).
-constexpr int kMostOrdered = 8192;
+// order of the rows, 175 so, fp32 205 and 183; rows that all cost the same lose 2 us by it, 108 to 110).  Every block reads the settings of all rows for
+// it, so that it is done only where a row is long next to their number: mixed bf16, 600 x 32000 68 us without and 61 with, 2000 x 131072 393 and 342, but
+// 2000 x 32000 152 and 156, 8192 x 1000 with a temperature 203 and 463.
+constexpr int kMostOrdered = 8192;           // (16 bits count the rows of a kind)
+constexpr int kOrderedPerRow = 32;           // tokens of a row for each row of the call
 template <int kThreads>
 __device__ __forceinline__ int costly_first(Shared& s, const SampleParams& p) {
     const int each = (p.N + kThreads - 1) / kThreads, first = threadIdx.x * each, last = min(first + each, p.N);
@@ -1061,7 +1064,7 @@ int launch_sample(const SampleParams& p, cudaStream_t st) {
         while (q.ranks < 8 && p.N * q.ranks * 2 <= (q.ranks < 4 ? sms : sms / 2) && p.K / (q.ranks * 2) >= 16384) q.ranks *= 2;
         return q.ranks > 1 ? launch_threads<T, 1024, true>(q, st) : launch_threads<T, 1024, false>(q, st);
     }
-    q.ordered = p.N > 2 * sms && p.N <= kMostOrdered && (p.top_k || p.top_p || p.temperature);
+    q.ordered = p.N > 2 * sms && p.N <= kMostOrdered && long(p.K) >= long(kOrderedPerRow) * p.N && (p.top_k || p.top_p || p.temperature);
     return launch_threads<T, 512, false>(q, st);
 }
 

@@ -349,3 +349,26 @@ def test_long_rows_and_many(N, K, t):
     for n in range(0, N, 23):
         one = run(z[n:n + 1].clone(), {k: v[n:n + 1] for k, v in p.items()})
         assert one[0][0] == token[n] and (one[1][0] == logprob[n])
+
+
+@pytest.mark.parametrize("N,K", [(297, 9503), (297, 9504), (400, 12799), (400, 12800)])
+def test_either_side_of_the_ordering(N, K):
+    """From 32 tokens for each row on the costly rows come first."""
+    check(logits(N, K, torch.bfloat16, 21, "steps"), params(N, 22, FILTERS[-1]))
+
+
+def test_settings_of_many_short_rows_cost_little():
+    """A temperature for each row of 8192 short ones: not much more than none (it was more than twice the time while blocks looked at all rows')."""
+    N, K = 8192, 1000
+    z, u, one = logits(N, K, torch.bfloat16, 23), torch.rand(N, device="cuda"), torch.ones(N, device="cuda")
+    token = guarded((N,), torch.int32, fill=0)
+    times = {}
+    for name, temperature in (("none", None), ("each", one)) * 12:
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        for _ in range(4):
+            B.sample_tokens(N, K, z, u, token, temperature=temperature)
+        b.record()
+        torch.cuda.synchronize()
+        times.setdefault(name, []).append(a.elapsed_time(b))
+    assert sorted(times["each"])[6] < 1.5 * sorted(times["none"])[6]
