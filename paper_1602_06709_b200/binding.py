@@ -8,8 +8,11 @@ from __future__ import annotations
 
 import ctypes
 import os
+import warnings
 
 import torch
+
+from . import build
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libpcl_dnn.so")
@@ -154,17 +157,29 @@ def lib() -> ctypes.CDLL:
         L.pcl_noalloc_scratch_bytes.restype = sz
         L.pcl_status_string.argtypes = [ci]
         L.pcl_status_string.restype = ctypes.c_char_p
-        try:
-            from . import _pcl_calls
-        except ImportError as e:
-            raise RuntimeError(f"{os.path.join(_HERE, '_pcl_calls.so')} is missing or unusable: run `python -m paper_1602_06709_b200.build`") from e
-        _pcl_calls.bind({n: ctypes.cast(getattr(L, n), vp).value for n in _COMPILED})
-        _lib, _calls = L, _pcl_calls
+        _lib, _calls = L, _compiled_calls(L)
     return _lib
 
 
 _COMPILED = ["pcl_rms_norm_fwd", "pcl_rms_norm_fwd_q8", "pcl_rms_norm_bwd", "pcl_quantize_rows", "pcl_fc_q8_fwd", "pcl_grad_norm",
              "pcl_grad_clip", "pcl_sgd_update_clipped", "pcl_sample_tokens"]
+
+
+def _compiled_calls(L):
+    """The compiled marshalling, bound to the library; None where it was not built, or for another Python or torch: every call has its checks here
+    too, which take a few microseconds longer."""
+    try:
+        from . import _pcl_calls
+    except ImportError as e:
+        why = str(e)
+    else:
+        want, have = build.calls_built_for(), getattr(_pcl_calls, "built_for", None)
+        if have == want:
+            _pcl_calls.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in _COMPILED})
+            return _pcl_calls
+        why = f"it was built for {have}, this is {want}"
+    warnings.warn(f"{os.path.join(_HERE, '_pcl_calls.so')} is not used ({why}): run `python -m paper_1602_06709_b200.build`", RuntimeWarning, stacklevel=3)
+    return None
 
 
 def _done(code: int, where: str) -> bool:

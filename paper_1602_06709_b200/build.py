@@ -20,21 +20,40 @@ FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std
 
 CALLS_SOURCE = os.path.join(CSRC, "fast_calls.cpp")
 CALLS = os.path.join(HERE, "_pcl_calls.so")
+CALLS_STAMP = os.path.join(HERE, "_build", "pcl_calls_built_for")
+
+
+def calls_built_for() -> str:
+    """What _pcl_calls.so depends on besides its sources: it holds this in `built_for`, and is used with nothing else."""
+    import torch
+    return f"{sys.implementation.cache_tag} torch-{torch.__version__}"
 
 
 def build_calls(force: bool = False) -> str:
     deps = [CALLS_SOURCE, os.path.join(CSRC, "..", "..", "include", "pcl_dnn.h"), os.path.abspath(__file__)]
+    built_for = calls_built_for()
     if not force and os.path.exists(CALLS) and all(os.path.getmtime(d) <= os.path.getmtime(CALLS) for d in deps):
-        return CALLS
+        try:
+            with open(CALLS_STAMP) as f:
+                if f.read() == built_for:
+                    return CALLS
+        except OSError:
+            pass
     import sysconfig
 
     import torch
     home = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(NVCC))
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f'-DPCL_BUILT_FOR="{built_for}"',
            f"-I{home}/include", f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", CALLS_SOURCE, f"-L{home}/lib", "-lc10", "-lc10_cuda",
            "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{home}/lib", "-o", CALLS]
+    if os.path.exists(CALLS):
+        os.remove(CALLS)                                       # (one of older sources must not stay where this fails)
     subprocess.run(cmd, check=True)
+    os.makedirs(os.path.dirname(CALLS_STAMP), exist_ok=True)
+    with open(CALLS_STAMP, "w") as f:
+        f.write(built_for)
     return CALLS
 
 
@@ -47,7 +66,10 @@ def needs_build() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    build_calls(force)
+    try:
+        build_calls(force)
+    except (OSError, subprocess.CalledProcessError) as e:      # (no g++, no headers of Python or torch: binding.py does without)
+        print(f"{CALLS} was not built, binding.py checks all calls itself: {e}", file=sys.stderr)
     if not force and not needs_build():
         return LIB
     objdir = os.path.join(HERE, "_build")

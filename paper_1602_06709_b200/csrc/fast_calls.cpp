@@ -309,4 +309,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pcl_calls", nullptr, -1, methods,
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__pcl_calls() { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__pcl_calls() {
+    PyObject* m = PyModule_Create(&module);
+    if (m && PyModule_AddStringConstant(m, "built_for", PCL_BUILT_FOR) < 0) { Py_DECREF(m); return nullptr; }
+    return m;
+}
