@@ -394,8 +394,10 @@ int pcl_orthogonal_update(int count, int M, int N, int dtype, void* w, const voi
 /* RMS norm of the N rows of a residual stream.
  *   h = x + residual (h = x for residual == NULL),   rstd[n] = 1 / sqrt(mean_c h[n,c]^2 + eps),   y[n,c] = h[n,c] * rstd[n] * w[c]
  * The norm is that of the sum before it is rounded to dtype; sums are fp32 in a fixed order.  Rows whose squares leave fp32's range are
- * scaled by a power of two first, so any finite row has a finite rstd; an infinity or NaN makes its row's results NaN (finite
- * elements beside an infinity: 0).  Results are defined by the formula at eps = 0 too (a row of zeros: NaN).
+ * scaled by a power of two first, so y is right for any finite row; an infinity or NaN makes its row's results NaN (finite
+ * elements beside an infinity: 0).  Results are defined by the formula at eps = 0 too (a row of zeros: NaN).  rstd is rounded to fp32: at eps = 0 it
+ * is inf for rows whose root mean square is not above 2^-128 (y is right there, but a gradient from that rstd is not finite), finite for all other
+ * finite rows, and for every finite row at eps > 0.
  * x, residual: [N][C] in; w: [C] in; h: [N][C] out or NULL (NULL where residual is); y: [N][C] out; all of type dtype; rstd: fp32 [N] out
  * or NULL.  h may be x or residual, y may be any input of its size.  Sizes up to 2^31 - 65537 each; eps finite and >= 0. */
 int pcl_rms_norm_fwd(int N, int C, int dtype, const void* x, const void* residual, const void* w, float eps,

@@ -386,3 +386,29 @@ def test_weight_gradient_of_short_rows(N, C, t):
     check_grad(t, h, w, rstd, dy, None, dx, dw)
     B.rms_norm_bwd(N, C, h, w, rstd, dy, None, dx, again, ws)
     assert torch.equal(dw, again) and B.last_device_status() == B.OK
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("C", [96, 1037, 40001])
+@pytest.mark.parametrize("N", [4, 400])
+def test_subnormal_rows(N, C, t):
+    """At eps = 0 the rstd of a row of subnormal numbers may not be a number of fp32: it is inf then, and y right all the same; at the smallest eps
+    it is finite."""
+    # multiples of 2^-133, which bf16 has too: the root mean square lies about 2^-130, and about 2^-126 in every other row
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = guarded((N, C), t, fill=0)
+    x.copy_((torch.randint(1, 16, (N, C), device="cuda", generator=g).double() * 2.0 ** -133).float())
+    x[1::2] *= 16
+    w = put((C,), t, 0.3, 2, 1.0)
+    y, rstd, q, scale = guarded((N, C), t), guarded((N,), torch.float32), bytes8((N, C)), guarded((N,), torch.float32)
+    B.rms_norm_fwd(N, C, x, None, w, 0.0, None, y, rstd)
+    _, er, ey = forward_reference(x, None, w, 0.0)
+    k = additions(C)
+    assert torch.isinf(rstd[0::2]).all() and (er[0::2] > 2.0 ** 128).all() and (er[1::2] < 2.0 ** 127.5).all()
+    assert ((rstd[1::2].double() - er[1::2]).abs() <= er[1::2] * (k / 2 + 4) * U).all()
+    assert ((y.double() - ey).abs() <= ey.abs() * (half_step(t) + (k / 2 + 8) * U * (1 + half_step(t)))).all()
+    B.rms_norm_fwd_q8(N, C, x, None, w, 0.0, None, q, scale)
+    check_q8(q, scale, ey, k / 2 + 8)
+    B.rms_norm_fwd(N, C, x, None, w, 2.0 ** -149, None, y, rstd)
+    _, er, ey = forward_reference(x, None, w, 2.0 ** -149)
+    assert ((rstd.double() - er).abs() <= er * (k / 2 + 4) * U).all()
