@@ -217,17 +217,22 @@ struct RowParams {
     float *scale, *rstd;
 };
 
-// The sum of squares left fp32's range, or lost all of its bits: the row times a power of two, with the values near 1, but no
+// The sum of squares left fp32's range, or lost all of its bits: the row times a power of two, with the largest value between 1/2 and 1, but no
 // further up than eps times its square stays in range.
-__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((min(max(e, -126), 126) + 127) << 23); }
+__device__ __forceinline__ float power_of_two(int e) { return e < -126 ? __int_as_float(0x00800000 >> (-126 - e)) : __int_as_float((min(e, 126) + 127) << 23); }
 __device__ __forceinline__ int exponent(float v) { return (__float_as_int(v) >> 23) - 127; }      // of a positive number; -127: subnormal
 __device__ __forceinline__ float row_rescale(uint32_t top, float eps) {
     const float t = __uint_as_float(top);
     if (!(t > 0.f) || t == INFINITY) return 1.f;              // (zeros, infinities and NaN stay what they are)
-    const int up = -exponent(t);
+    const int up = -exponent(t) - 1;
     return power_of_two(eps > 0.f ? min(up, (100 - exponent(eps)) / 2) : up);
 }
 __device__ __forceinline__ bool out_of_range(float ss, float eps) { return !(ss < 1e38f) || (ss < 1e-24f && eps < 1e-20f); }
+// The same of the products of values and weights, whose largest is top and which r takes to y: above fp32's range, or so small that their
+// roundings (half of 2^-149) reach a scale above its least.
+__device__ __forceinline__ bool products_out_of_range(uint32_t top, float r) {
+    return top >= 0x7f800000u || (top < 0x00800000u && (__uint_as_float(top) + 0x1p-149f) * r > kLargestE4m3 * kLeastScale);
+}
 
 // What a thread has of a row: up to V chunks, `group` apart, and, where the row is not just those (kWhole = false), maybe an element at the edges:
 // in front of the first whole chunk, or behind the last one that has a thread.
@@ -291,7 +296,8 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
     r = 1.f;
     if (kMode != ROW_QUANTIZE) {
         float s = 1.f;
-        if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && top >= 0x7f800000u)) {       // (rare; every thread of the group takes it)
+        if (kMode == ROW_NORM_Q8) r = __frsqrt_rn(fmaf(ss, mean, p.eps));
+        if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, r))) {       // (rare; every thread of the group takes it)
             uint32_t big = magnitude(ve);
             float none = 0.f;
 #pragma unroll
@@ -567,7 +573,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
         measure();
         float r = 1.f;
         if (kMode != ROW_QUANTIZE) {
-            if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && top >= 0x7f800000u)) {
+            if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, __frsqrt_rn(fmaf(ss, 1.f / float(p.C), p.eps))))) {
                 uint32_t big = 0;
                 float none = 0.f;
                 for (int c = g.rank; c < p.C; c += g.size) big = max(big, magnitude(value(c)));

@@ -412,3 +412,22 @@ def test_subnormal_rows(N, C, t):
     B.rms_norm_fwd(N, C, x, None, w, 2.0 ** -149, None, y, rstd)
     _, er, ey = forward_reference(x, None, w, 2.0 ** -149)
     assert ((rstd.double() - er).abs() <= er * (k / 2 + 4) * U).all()
+
+
+@pytest.mark.parametrize("C", [96, 1037, 40001])
+@pytest.mark.parametrize("N", [4, 400])
+@pytest.mark.parametrize("size,gain,eps", [(1e-10, 3e-35, 0.0), (1e-21, 1e-23, 1e-20), (1.9, 3.3e38, 1e-6), (3.3e38, 3.3e38, 0.0), (3.3e38, 1e-30, 0.0), (1e-38, 3.3e38, 0.0),
+                                           (1e-40, 1e-30, 0.0)])
+def test_q8_of_products_out_of_range(size, gain, eps, N, C):
+    """Values times weights leave fp32's range where the norm's results do not."""
+    x, w = guarded((N, C), torch.float32, fill=0), guarded((C,), torch.float32, fill=0)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    sign = torch.randint(0, 2, (N, C), device="cuda", generator=g) * 2 - 1
+    x.copy_((sign * size).float())                            # (|n| = 1: results are as large as the weights)
+    w.copy_((torch.rand(C, device="cuda", generator=g, dtype=torch.float64) * 0.5 + 0.5) * gain)
+    q, scale, rstd = bytes8((N, C)), guarded((N,), torch.float32), guarded((N,), torch.float32)
+    B.rms_norm_fwd_q8(N, C, x, None, w, eps, None, q, scale, rstd)
+    _, er, ey = forward_reference(x, None, w, float(torch.tensor(eps)))
+    k = additions(C)
+    check_q8(q, scale, ey, k / 2 + 8)
+    assert (scale.double() >= ey.abs().amax(dim=1) / 448 * (1 - (k / 2 + 8) * U)).all()
