@@ -485,9 +485,14 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
         // Q8: its row's scale, and the scales and the bias of the warp's columns, which go to its own piece of shared memory while the main loop
         // runs (kept four to a lane and shuffled from there, 64 values a chunk: 4000 rows, 512 -> 16000 84 us; read from global memory 140)
         const uint32_t cols_at = c.ring + c.stages * kSlotBytes + 8 * kStaging + (warp - 2) * kColumnBytes;
+        bool far = false, any_far = false;   // the row's scale takes sums (2^-18 to 2^49) to where fp32 has no room left; any row's of the warp
         if constexpr (kScaled) {
             const int own = lane & (kHalf / 4 - 1), at = cbase + 4 * own;
-            if (row_ok) g = __ldg(p.row_scale + row);
+            if (row_ok) {
+                g = __ldg(p.row_scale + row);
+                far = !(fabsf(g) >= 0x1p-100f && fabsf(g) <= 0x1p70f);
+            }
+            any_far = __any_sync(0xffffffffu, far);
             const float4 cs = load_four32(p.col_scale, at, p.N);
             float4 b = make_float4(0.f, 0.f, 0.f, 0.f);
             if (p.bias) b = p.out_type == DT_F32 ? load_four32(static_cast<const float*>(p.bias), at, p.N) : four_values(load_four16(p.bias, at, p.N), p.bf16 != 0);
@@ -544,6 +549,21 @@ __device__ __forceinline__ bool finish_items(Gemm16Ctx& c, const Gemm16Params& p
             }
             if constexpr (kScaled) {
                 const float2 gg = make_float2(g, g), zero = make_float2(0.f, 0.f);
+                if (any_far) {
+                    // where a far scale meets one on the other side of 1, the two are multiplied first
+                    auto scaled = [&](float a, float cs, float b) {
+                        const bool cross = far && (fabsf(g) < 1.f) != (fabsf(cs) < 1.f);
+                        return fmaf(fmaf(a, cross ? g * cs : g, 0.f), cross ? 1.f : cs, b);
+                    };
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float4 cs = ld_shared_v4(cols_at + cc * 4 + u * 16), b = ld_shared_v4(cols_at + kColumnBytes / 2 + cc * 4 + u * 16);
+                        v[4 * u] = scaled(v[4 * u], cs.x, b.x);
+                        v[4 * u + 1] = scaled(v[4 * u + 1], cs.y, b.y);
+                        v[4 * u + 2] = scaled(v[4 * u + 2], cs.z, b.z);
+                        v[4 * u + 3] = scaled(v[4 * u + 3], cs.w, b.w);
+                    }
+                } else
 #pragma unroll
                 for (int u = 0; u < 8; ++u) {
                     const float4 cs = ld_shared_v4(cols_at + cc * 4 + u * 16), b = ld_shared_v4(cols_at + kColumnBytes / 2 + cc * 4 + u * 16);

@@ -167,3 +167,29 @@ def test_few_rows_behind_a_call_of_nan(N, C, K, t):
     B.fc_q8_fwd(N, C, K, x, xs, w, ws, None, y, ws=space)
     check(y, t, B.ACT_NONE, *expected(x, xs, w, ws, None, B.ACT_NONE))
     assert torch.isnan(y0).all()
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", [B.ACT_NONE, B.ACT_RELU])
+@pytest.mark.parametrize("xs,ws", [(1e36, 1e-38), (1e-38, 1e36), (2.0 ** -126, 1e30), (1e30, 2.0 ** -126), (1e35, 1e-10)])
+@pytest.mark.parametrize("N,C,K", [(5, 4096, 72), (300, 1037, 301)])
+def test_scales_far_apart(N, C, K, xs, ws, act, t):
+    """Scales that cancel: neither may take the sum out of fp32's range on the way; beside them rows of ordinary scales, which do not notice."""
+    x, w = whole((N, C), 1), whole((K, C), 2)
+    a, b = scales(N, xs, 3), scales(K, ws, 4)
+    b[::2] = scales(len(b[::2]), 1.0, 6)
+    a[1::3] = 1.5
+    a.clamp_(min=2.0 ** -126), b.clamp_(min=2.0 ** -126)       # (the least that a scale can be)
+    y = guarded((N, K), t)
+    B.fc_q8_fwd(N, C, K, x, a, w, b, None, y, act, workspace(B.fc_q8_workspace_bytes(N, C, K)))
+    want, size, z = expected(x, a, w, b, None, act)
+    fits = want.abs() < torch.finfo(t).max * 0.99
+    assert bool(fits.any())
+    zero = torch.zeros_like(want)
+    check(torch.where(fits, y.double(), zero), t, act, *(torch.where(fits, v, zero) for v in (want, size, z)))
+    assert (torch.isinf(y) | fits | (want.abs() < torch.finfo(t).max * 1.01)).all()
+    plain, again = a.clone(), guarded((N, K), t)
+    plain[0::3] = 1.0
+    plain[2::3] = 1.0
+    B.fc_q8_fwd(N, C, K, x, plain, w, b, None, again, act, workspace(B.fc_q8_workspace_bytes(N, C, K)))
+    assert torch.equal(again[1::3], y[1::3])
