@@ -228,10 +228,11 @@ __device__ __forceinline__ float row_rescale(uint32_t top, float eps) {
     return power_of_two(eps > 0.f ? min(up, (100 - exponent(eps)) / 2) : up);
 }
 __device__ __forceinline__ bool out_of_range(float ss, float eps) { return !(ss < 1e38f) || (ss < 1e-24f && eps < 1e-20f); }
-// The same of the products of values and weights, whose largest is top and which r takes to y: above fp32's range, or so small that their
-// roundings (half of 2^-149) reach a scale above its least.
-__device__ __forceinline__ bool products_out_of_range(uint32_t top, float r) {
-    return top >= 0x7f800000u || (top < 0x00800000u && (__uint_as_float(top) + 0x1p-149f) * r > kLargestE4m3 * kLeastScale);
+// The same of the products of values and weights, whose largest is top and which 1 / sqrt(mean) takes to y: above fp32's range, or so small that
+// their roundings (half of 2^-149) reach a scale above its least.
+__device__ __forceinline__ bool products_out_of_range(uint32_t top, float mean) {
+    if (top - 0x00800000u < 0x7f000000u) return false;        // (an ordinary number)
+    return top >= 0x7f800000u || (__uint_as_float(top) + 0x1p-149f) * __frsqrt_rn(mean) > kLargestE4m3 * kLeastScale;
 }
 
 // What a thread has of a row: up to V chunks, `group` apart, and, where the row is not just those (kWhole = false), maybe an element at the edges:
@@ -296,8 +297,7 @@ __device__ __forceinline__ void row_factors(Group& g, const RowParams& p, int ro
     r = 1.f;
     if (kMode != ROW_QUANTIZE) {
         float s = 1.f;
-        if (kMode == ROW_NORM_Q8) r = __frsqrt_rn(fmaf(ss, mean, p.eps));
-        if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, r))) {       // (rare; every thread of the group takes it)
+        if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, fmaf(ss, mean, p.eps)))) {       // (rare; every thread of the group takes it)
             uint32_t big = magnitude(ve);
             float none = 0.f;
 #pragma unroll
@@ -573,7 +573,7 @@ __global__ void __launch_bounds__(1024) long_row_kernel(const RowParams p) {
         measure();
         float r = 1.f;
         if (kMode != ROW_QUANTIZE) {
-            if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, __frsqrt_rn(fmaf(ss, 1.f / float(p.C), p.eps))))) {
+            if (out_of_range(ss, p.eps) || (kMode == ROW_NORM_Q8 && products_out_of_range(top, fmaf(ss, 1.f / float(p.C), p.eps)))) {
                 uint32_t big = 0;
                 float none = 0.f;
                 for (int c = g.rank; c < p.C; c += g.size) big = max(big, magnitude(value(c)));

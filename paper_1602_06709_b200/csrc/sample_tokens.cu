@@ -41,6 +41,7 @@ struct SampleParams {
     int N, K, bits;                          // bits: a weight of 1 is 2^bits
     int ordered;                             // rows are taken in the order of falling cost
     int ranks;                               // blocks that share a row
+    double reach;                            // how many temperatures below the largest a weight is 0
     const void* logits;
     const float *uniform, *temperature, *top_p, *min_p;
     const int* top_k;
@@ -965,9 +966,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ---- where the part kept ends
     Border border{kLowest, kAllIds};
     bool summed = false;                                       // the pieces' sums are there
-    // what has any weight lies above: weights are rounded to the nearest 2^-bits, so they end (bits + 1) ln 2 temperatures below the largest (and a margin
-    // for this bound's own roundings)
-    const float floor_z = float(fmax(double(top) - (0.69314718055994530942 * (p.bits + 1) + 0.05) * double(temperature), double(kLowest)));
+    const float floor_z = float(fmax(double(top) - p.reach * double(temperature), double(kLowest)));       // (what has any weight lies above)
     auto pieces_each = [&] { return (row.hi() - row.lo() + 32 * kPieces - 1) / (32 * kPieces); };        // vectors of a piece per lane
     u64 whole = 0;
     if (by_p && k == 0 && !infinite) summed = nucleus<kThreads>(s, team, row, sc, top, floor_z, unit, top_p, least, pieces_each(), part_of, whole, border);
@@ -1075,7 +1074,9 @@ size_t sample_tokens_workspace_bytes(int, int) { return 0; }
 int launch_sample_tokens(const SampleArgs& a, void*, cudaStream_t st) {
     int log_k = 0;
     while ((1ll << log_k) < a.K) ++log_k;
-    const SampleParams p{a.N, a.K, log_k > 18 ? 62 - log_k : kWeightBits, 0, 1, a.logits, a.uniform, a.temperature, a.top_p, a.min_p, a.top_k, a.token, a.logprob};
+    const int bits = log_k > 18 ? 62 - log_k : kWeightBits;
+    // weights are rounded to the nearest 2^-bits, so they end (bits + 1) ln 2 below the largest (and a margin for roundings on the way)
+    const SampleParams p{a.N, a.K, bits, 0, 1, 0.69314718055994530942 * (bits + 1) + 0.05, a.logits, a.uniform, a.temperature, a.top_p, a.min_p, a.top_k, a.token, a.logprob};
     LaunchScope scope(KID_SAMPLE, double(a.N) * a.K * dtype_bytes(a.type), st);
     switch (a.type) {
         case DT_F32: return launch_sample<float>(p, st);
