@@ -119,6 +119,17 @@ class Args {
     int dtype = -1, device = -1;
 };
 
+// The library's call, with the interpreter free for other threads: a launch waits where a stream's queue is full, maybe for a host function that
+// needs the interpreter.  (The tensors are the caller's arguments, who holds them.)
+template <class F>
+int unlocked(F&& call) {
+    int code;
+    Py_BEGIN_ALLOW_THREADS
+    code = call();
+    Py_END_ALLOW_THREADS
+    return code;
+}
+
 template <class F>
 PyObject* guarded(Args& a, F&& call) {
     try {
@@ -142,7 +153,7 @@ PyObject* rms_norm_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void* y = a.typed(all);
         float* rstd = a.real32(N, true);
         void* st = a.stream();
-        return a.ok ? fn.rms_norm_fwd(N, C, a.dtype, x, res, w, eps, h, y, rstd, st) : -1;
+        return a.ok ? unlocked([&] { return fn.rms_norm_fwd(N, C, a.dtype, x, res, w, eps, h, y, rstd, st); }) : -1;
     });
 }
 
@@ -160,7 +171,7 @@ PyObject* rms_norm_fwd_q8(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float* scale = a.real32(N);
         float* rstd = a.real32(N, true);
         void* st = a.stream();
-        return a.ok ? fn.rms_norm_fwd_q8(N, C, a.dtype, x, res, w, eps, h, y, scale, rstd, st) : -1;
+        return a.ok ? unlocked([&] { return fn.rms_norm_fwd_q8(N, C, a.dtype, x, res, w, eps, h, y, scale, rstd, st); }) : -1;
     });
 }
 
@@ -178,7 +189,7 @@ PyObject* rms_norm_bwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void* dw = a.typed(C, true);
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.rms_norm_bwd(N, C, a.dtype, h, w, rstd, dy, dh, dx, dw, ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.rms_norm_bwd(N, C, a.dtype, h, w, rstd, dy, dh, dx, dw, ws.p, ws.bytes, st); }) : -1;
     });
 }
 
@@ -191,7 +202,7 @@ PyObject* quantize_rows(PyObject*, PyObject* const* args, Py_ssize_t n) {
         void* q = a.bytes(all);
         float* scale = a.real32(N);
         void* st = a.stream();
-        return a.ok ? fn.quantize_rows(N, C, a.dtype, x, q, scale, st) : -1;
+        return a.ok ? unlocked([&] { return fn.quantize_rows(N, C, a.dtype, x, q, scale, st); }) : -1;
     });
 }
 
@@ -208,7 +219,7 @@ PyObject* fc_q8_fwd(PyObject*, PyObject* const* args, Py_ssize_t n) {
         const long act = a.integer();
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.fc_q8_fwd(N, C, K, a.dtype, x, xs, w, ws_, bias, y, int(act), ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.fc_q8_fwd(N, C, K, a.dtype, x, xs, w, ws_, bias, y, int(act), ws.p, ws.bytes, st); }) : -1;
     });
 }
 
@@ -226,7 +237,7 @@ PyObject* sample_tokens(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float* logprob = a.real32(N, true);
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.sample_tokens(N, K, a.dtype, z, u, temperature, top_k, top_p, min_p, token, logprob, ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.sample_tokens(N, K, a.dtype, z, u, temperature, top_k, top_p, min_p, token, logprob, ws.p, ws.bytes, st); }) : -1;
     });
 }
 
@@ -242,7 +253,7 @@ PyObject* grad_norm(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float* norm = a.real32(1);
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.grad_norm(count, grads, sizes, types, norm, ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.grad_norm(count, grads, sizes, types, norm, ws.p, ws.bytes, st); }) : -1;
     });
 }
 
@@ -259,7 +270,7 @@ PyObject* grad_clip(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float* norm = a.real32(1);
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.grad_clip(count, grads, out, sizes, types, most, norm, ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.grad_clip(count, grads, out, sizes, types, most, norm, ws.p, ws.bytes, st); }) : -1;
     });
 }
 
@@ -276,7 +287,7 @@ PyObject* sgd_update_clipped(PyObject*, PyObject* const* args, Py_ssize_t n) {
         float* norm = a.real32(1);
         const Args::Workspace ws = a.workspace();
         void* st = a.stream();
-        return a.ok ? fn.sgd_update_clipped(count, w, grads, sizes, types, lr, most, norm, ws.p, ws.bytes, st) : -1;
+        return a.ok ? unlocked([&] { return fn.sgd_update_clipped(count, w, grads, sizes, types, lr, most, norm, ws.p, ws.bytes, st); }) : -1;
     });
 }
 

@@ -113,3 +113,33 @@ def test_both_take_and_refuse_the_same(name, monkeypatch):
                     elif isinstance(a, torch.Tensor):
                         assert same(a, b), (key, k)
     assert 3 < taken < tried
+
+
+def test_other_threads_run_meanwhile():
+    """The library is called with the interpreter free: here a function that waits half a second stands in its place."""
+    import ctypes
+    import threading
+    import time
+    lib = B.lib()
+    table = {n: ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in B._COMPILED}
+    wait = ctypes.cast(ctypes.CDLL(None).usleep, ctypes.c_void_p).value
+    n = 500000                                                 # (the call's first argument: microseconds)
+    x, w = torch.zeros(n, 1, device="cuda"), torch.ones(1, device="cuda")
+    ticks, stop = [], threading.Event()
+
+    def tick():
+        while not stop.wait(0.01):
+            ticks.append(time.monotonic())
+
+    B._calls.bind({**table, "pcl_rms_norm_fwd": wait})
+    other = threading.Thread(target=tick)
+    try:
+        other.start()
+        begin = time.monotonic()
+        assert B._calls.rms_norm_fwd(n, 1, x, None, w, 1e-6, None, x, None, None) == 0
+        end = time.monotonic()
+    finally:
+        B._calls.bind(table)
+        stop.set()
+        other.join()
+    assert end - begin > 0.4 and sum(begin + 0.05 < t < end - 0.05 for t in ticks) > 5
