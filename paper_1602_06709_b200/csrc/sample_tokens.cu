@@ -16,9 +16,11 @@
 //     list, where the exact border is found.
 //   Whatever does not fit in the list: the value at the border is found by histograms of weights or counts, finer each time.
 //   What is kept is summed by pieces of consecutive ids, and the piece in which the random number falls is searched.
-// The cost is the weights': one takes ten operations in 64 bits, of which an SM does 64 a cycle, so a row that needs all of them takes three
-// times as long as reading it.  Measured, 512 rows of 131072 bf16 logits (20.5 us to read): top-k 51 us, no filter 109, min-p 117, top-p 280, mixed
-// 175 (about 160 with masked tokens); one row of 32003: 9.5, 13, 14, 27 us; one of 131072: 13.5, 14, 15, 33.
+// The cost is the weights', and the chains of dependent operations that they are: without a filter the 64-bit pipe is active for 38 % of the time and
+// the issue slots are used for 59 %, top-p 18 and 60 %, so neither is the limit by itself; warps wait for fixed latencies, for each other at barriers
+// and for loads.  Measured, 512 rows of 131072 bf16 logits (20.5 us to read): top-k 51 us, no filter 109, min-p 117, top-p 258-280, mixed 175 (about 160
+// with masked tokens); one row of 32003: 9.5, 13, 14, 27 us; one of 131072: 13.5, 14, 15, 33.  Dear forms: top-k of 5000 in the 512 rows 340, top-p
+// where few different values fill a bin (steps of 2: 727; all equal: 1230).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
