@@ -3,7 +3,7 @@
 // The products are exact and summed in fp32 by the tensor core; scales, bias and activation are the GEMM's epilogue (tc_gemm16.cu).
 //
 // Bound by the tensor cores for many rows, by the reading of w for few.  Measured: 8192 rows, 4096 -> 16384 bf16 390 us by itself (2.8 PFLOP/s, the
-// tensor pipe active for 93 % of the time), 434-445 in a long run under the power cap; 16 rows of it 15.1-15.9 us (67 MB, 4.3-4.5 TB/s).
+// tensor pipe active for 93 % of the time), 434-450 in a long run under the power cap; 16 rows of it 15.1-15.9 us (67 MB, 4.3-4.5 TB/s).
 //
 // TMA wants rows that start on multiples of 16 bytes: with C % 16 != 0 both operands are copied to padded rows first.
 #include "pcl_internal.h"

@@ -11,7 +11,7 @@
 // loses nothing, the same squares are taken in 64 bits.
 //
 // Measured, over several cards and runs: norm of 500M bf16 elements 145 us (6.9 TB/s), with clipped copies 487-496 (3 GB, 6.0-6.2 TB/s); clipped step of
-// VGG-A's 133M fp32 parameters 333-339 us (2.1 GB, 6.3-6.4 TB/s); clipped copies of the DNN's 34M fp32 gradients 70.
+// VGG-A's 133M fp32 parameters 333-340 us (2.1 GB, 6.3-6.4 TB/s); clipped copies of the DNN's 34M fp32 gradients 70.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>

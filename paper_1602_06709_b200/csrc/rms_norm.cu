@@ -17,7 +17,7 @@
 // Sums over a row are fp32 in a fixed tree.  h is rounded when it is stored, but the norm is that of the sum before rounding.  A row whose
 // sum of squares leaves fp32's range is scaled by a power of two first.
 //
-// Measured, over several cards and runs: 32768 x 4096 bf16 with a residual 170-176 us (1.07 GB, 6.1-6.3 TB/s), its gradient 165-176 (6.1-6.5 TB/s);
+// Measured, over several cards and runs: 32768 x 4096 bf16 with a residual 170-177 us (1.07 GB, 6.1-6.3 TB/s), its gradient 165-177 (6.1-6.5 TB/s);
 // 3001 x 1037 fp16 to 8 bits 7.4; gradient of 5000 x 1001 fp32 18.2 (a third of it the second launch and edges); one row of 2048 bf16 3.3-3.8, nearly
 // all of it launch and call.  Rows of more than 16384 elements are far from that: 2048 x 32768 bf16 with a residual 375, its gradient 564 (by bytes: 82).
 #include <cuda_bf16.h>
